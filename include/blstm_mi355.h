@@ -104,6 +104,64 @@ int softmax_xent_fwd_bwd(blstm_ctx* ctx, const void* theta, const void* z, const
 int softmax_xent_fwd_bwd_noalloc(blstm_ctx* ctx, const void* theta, const void* z, const int32_t* labels,
                                  float* loss_dev, void* dz, float* grad, void* stream);
 
+/* ---- the softmax layer beyond cross-entropy ------------------------------------------------------------------
+   With u = W_s z + b_s the logits of a frame and p = softmax(u): log-probabilities of given labels, the largest logits, the
+   distillation loss against a teacher's largest logits, and the clipped policy loss.  Common to the four:
+   - theta and z as for softmax_xent_fwd_bwd; s is the context's loss scale.  No workspace needs to be bound: `scratch` is
+     scratch_bytes bytes (at least softmax_scratch_bytes) of caller-owned device memory, 16-byte aligned, that holds nothing
+     between calls.  Calls that overlap (streams, threads, replayed graphs) need scratch and outputs of their own; they may
+     share the context unless profiling is on.  A call never reads what an earlier one left in scratch.
+   - labels [T][B] int32.  BLSTM_NO_LABEL marks a frame that counts for nothing (padding, an empty sequence): whatever z and the
+     call's other inputs hold there, it adds nothing to the loss, its row of dz is zero, and W_s and b_s get nothing from it.
+     Any other label outside [0, V) is never used as an index: the frame's loss term and log-probability are NaN, its
+     gradients nothing.
+   - The calls with gradients write loss_dev[0], dz [T][B][P or 2H] and, of grad, the slices W_s and b_s (overwritten): what
+     softmax_xent_fwd_bwd writes, in its place in front of blstm_backward (BLSTM_OPT_DEFER_SOFTMAX_WGRAD does not concern
+     them; what an earlier softmax_xent_fwd_bwd left to blstm_backward is dropped).  Mode 1: logits and all sums in float,
+     dE/du enters the product for dz as one bf16 number and those for W_s and b_s as the sum of two (2^-18), so that the gradients are
+     good to float.  The same inputs give the same bits. */
+#define BLSTM_NO_LABEL (-1)
+#define BLSTM_MAX_TOP 256                      /* the most entries of a list of largest logits */
+/* call = one of these in softmax_scratch_bytes */
+#define SOFTMAX_LOGPROB 0
+#define SOFTMAX_TOPK    1
+#define SOFTMAX_DISTILL 2
+#define SOFTMAX_POLICY  3
+/* Bytes of scratch a call needs (K: of the two with lists, else ignored); 0 and an error text if there is no such call. */
+size_t softmax_scratch_bytes(const blstm_ctx* ctx, int call, int K);
+
+/* logp [T][B] float = log p[label], 0 for a frame without label. */
+int softmax_logprob(blstm_ctx* ctx, const void* theta, const void* z, const int32_t* labels, float* logp,
+                    void* scratch, size_t scratch_bytes, void* stream);
+
+/* The K largest logits of every frame, 1 <= K <= min(V, BLSTM_MAX_TOP): values [T][B][K] float by falling value, classes
+   [T][B][K] int32, of equal values the lower class first.  NaN counts as less than everything. */
+int softmax_topk(blstm_ctx* ctx, const void* theta, const void* z, int K, float* values, int32_t* classes,
+                 void* scratch, size_t scratch_bytes, void* stream);
+
+/* Distillation from a teacher's largest logits.  teacher_values [T][B][K] float, teacher_classes [T][B][K] int32 in any order, as
+   softmax_topk writes them or shorter: an entry of class BLSTM_NO_LABEL or of value -inf is not used (any other class outside
+   [0, V): not used either, and the frame's loss term is NaN).  A class that stands in a list twice has the sum of both
+   probabilities.  With q = softmax over a frame's used entries of value / temperature, p' = softmax(u / temperature):
+     E = s sum over frames of  hard_weight (-log p[label])  +  soft_weight temperature^2 sum_k q_k (log q_k - log p'[class_k])
+   A frame without used entries has the first term only, one without label the second.  hard_weight 0: labels are not
+   read and may be NULL.  temperature > 0, hard_weight >= 0, soft_weight > 0, 1 <= K <= min(V, BLSTM_MAX_TOP). */
+int softmax_distill_fwd_bwd(blstm_ctx* ctx, const void* theta, const void* z, const int32_t* labels_or_null,
+                            const float* teacher_values, const int32_t* teacher_classes, int K, float temperature,
+                            float hard_weight, float soft_weight, float* loss_dev, void* dz, float* grad,
+                            void* scratch, size_t scratch_bytes, void* stream);
+
+/* The clipped policy loss on sampled labels, with a KL term to reference weights.  advantage, old_logp, ref_logp and logp: [T][B]
+   float (softmax_logprob's, on the weights that sampled and on the reference's).  With lp = log p[label], r = exp(lp - old_logp):
+     E = s sum over frames of  -min(r A, min(max(r, 1 - clip_low), 1 + clip_high) A)
+                               + kl_weight (exp(ref_logp - lp) - (ref_logp - lp) - 1)
+   old_logp NULL: the present weights sampled, r = 1 and the gradient is -A grad lp.  ref_logp NULL: no KL term.  logp, if not NULL,
+   receives lp.  0 <= clip_low <= 1, clip_high >= 0, kl_weight >= 0. */
+int softmax_policy_fwd_bwd(blstm_ctx* ctx, const void* theta, const void* z, const int32_t* labels, const float* advantage,
+                           const float* old_logp_or_null, const float* ref_logp_or_null, float clip_low, float clip_high,
+                           float kl_weight, float* loss_dev, float* logp_or_null, void* dz, float* grad,
+                           void* scratch, size_t scratch_bytes, void* stream);
+
 /* Back-propagation through the bottleneck and through time (Eq. 1b): writes every slice of grad
    except W_s and b_s.  Must follow blstm_forward on the same ctx, theta and x. */
 int blstm_backward(blstm_ctx* ctx, const void* theta, const void* x, const void* dz, float* grad, void* stream);

@@ -16,10 +16,14 @@ LIB_PATH = os.path.join(_HERE, "libblstm_mi355.so")
 
 BLSTM_WX, BLSTM_UH, BLSTM_B, BLSTM_WP, BLSTM_BP, BLSTM_WS, BLSTM_BS = range(7)
 BLSTM_MAX_REPLICAS = 64
+BLSTM_NO_LABEL = -1
+BLSTM_MAX_TOP = 256
+SOFTMAX_LOGPROB, SOFTMAX_TOPK, SOFTMAX_DISTILL, SOFTMAX_POLICY = range(4)
 
 EXPORTS = [
     "blstm_create", "blstm_destroy", "blstm_param_count", "blstm_workspace_bytes", "blstm_param_offset",
-    "blstm_bind", "blstm_forward", "softmax_xent_fwd_bwd", "softmax_xent_fwd_bwd_noalloc", "blstm_backward", "sgd_step", "adpsgd_mix",
+    "blstm_bind", "blstm_forward", "softmax_xent_fwd_bwd", "softmax_xent_fwd_bwd_noalloc",
+    "softmax_scratch_bytes", "softmax_logprob", "softmax_topk", "softmax_distill_fwd_bwd", "softmax_policy_fwd_bwd", "blstm_backward", "sgd_step", "adpsgd_mix",
     "sgd_mix_pair", "sync_average", "blstm_lr_schedule",
     "adpsgd_ring_partner", "blstm_shadow_refresh", "blstm_set_option", "blstm_weights_changed", "blstm_device_status", "blstm_profile_enable", "blstm_profile_read",
     "blstm_profile_classes", "blstm_profile_name", "blstm_last_error",
@@ -66,6 +70,16 @@ def lib():
     L.softmax_xent_fwd_bwd.restype = c_int
     L.softmax_xent_fwd_bwd_noalloc.argtypes = L.softmax_xent_fwd_bwd.argtypes
     L.softmax_xent_fwd_bwd_noalloc.restype = c_int
+    L.softmax_scratch_bytes.argtypes = [c_void_p, c_int, c_int]
+    L.softmax_scratch_bytes.restype = c_size_t
+    L.softmax_logprob.argtypes = [c_void_p] * 6 + [c_size_t, c_void_p]
+    L.softmax_logprob.restype = c_int
+    L.softmax_topk.argtypes = [c_void_p] * 3 + [c_int] + [c_void_p] * 3 + [c_size_t, c_void_p]
+    L.softmax_topk.restype = c_int
+    L.softmax_distill_fwd_bwd.argtypes = [c_void_p] * 6 + [c_int] + [c_float] * 3 + [c_void_p] * 4 + [c_size_t, c_void_p]
+    L.softmax_distill_fwd_bwd.restype = c_int
+    L.softmax_policy_fwd_bwd.argtypes = [c_void_p] * 7 + [c_float] * 3 + [c_void_p] * 5 + [c_size_t, c_void_p]
+    L.softmax_policy_fwd_bwd.restype = c_int
     L.blstm_backward.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
     L.blstm_backward.restype = c_int
     L.sgd_step.argtypes = [c_void_p, c_void_p, c_void_p, c_size_t, c_float, c_float, c_void_p, c_void_p]
@@ -175,6 +189,45 @@ def softmax_xent_fwd_bwd(ctx, theta, z, labels, loss_dev, dz, grad, stream=None)
 def softmax_xent_fwd_bwd_noalloc(ctx, theta, z, labels, loss_dev, dz, grad, stream=None):
     return _check(lib().softmax_xent_fwd_bwd_noalloc(ctx, _ptr(theta), _ptr(z), _ptr(labels), _ptr(loss_dev), _ptr(dz),
                                                      _ptr(grad), _stream(stream)))
+
+
+def softmax_scratch_bytes(ctx, call, K=0):
+    """Bytes of scratch that one of the calls below needs (call: SOFTMAX_LOGPROB, _TOPK, _DISTILL or _POLICY)."""
+    n = int(lib().softmax_scratch_bytes(ctx, call, K))
+    if n == 0:
+        raise BlstmError(-2, blstm_last_error())
+    return n
+
+
+def _scratch(scratch, nbytes):
+    """Address and size of a call's scratch: a tensor's own size unless one is given."""
+    if nbytes is None:
+        nbytes = 0 if scratch is None else scratch.numel() * scratch.element_size()
+    return _ptr(scratch), nbytes
+
+
+def softmax_logprob(ctx, theta, z, labels, logp, scratch, scratch_bytes=None, stream=None):
+    return _check(lib().softmax_logprob(ctx, _ptr(theta), _ptr(z), _ptr(labels), _ptr(logp), *_scratch(scratch, scratch_bytes), _stream(stream)))
+
+
+def softmax_topk(ctx, theta, z, K, values, classes, scratch, scratch_bytes=None, stream=None):
+    return _check(lib().softmax_topk(ctx, _ptr(theta), _ptr(z), K, _ptr(values), _ptr(classes), *_scratch(scratch, scratch_bytes),
+                                     _stream(stream)))
+
+
+def softmax_distill_fwd_bwd(ctx, theta, z, labels_or_null, teacher_values, teacher_classes, K, temperature, hard_weight, soft_weight,
+                            loss_dev, dz, grad, scratch, scratch_bytes=None, stream=None):
+    return _check(lib().softmax_distill_fwd_bwd(ctx, _ptr(theta), _ptr(z), _ptr(labels_or_null), _ptr(teacher_values),
+                                                _ptr(teacher_classes), K, temperature, hard_weight, soft_weight, _ptr(loss_dev),
+                                                _ptr(dz), _ptr(grad), *_scratch(scratch, scratch_bytes), _stream(stream)))
+
+
+def softmax_policy_fwd_bwd(ctx, theta, z, labels, advantage, old_logp_or_null, ref_logp_or_null, clip_low, clip_high, kl_weight,
+                           loss_dev, logp_or_null, dz, grad, scratch, scratch_bytes=None, stream=None):
+    return _check(lib().softmax_policy_fwd_bwd(ctx, _ptr(theta), _ptr(z), _ptr(labels), _ptr(advantage), _ptr(old_logp_or_null),
+                                               _ptr(ref_logp_or_null), clip_low, clip_high, kl_weight, _ptr(loss_dev),
+                                               _ptr(logp_or_null), _ptr(dz), _ptr(grad), *_scratch(scratch, scratch_bytes),
+                                               _stream(stream)))
 
 
 def blstm_backward(ctx, theta, x, dz, grad, stream=None):

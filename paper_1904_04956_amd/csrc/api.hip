@@ -14,6 +14,7 @@
 #include "../../include/blstm_mi355.h"
 #include "gemm.hpp"
 #include "kernels.hpp"
+#include "losses.hpp"
 #include "xcd.hpp"
 
 using namespace blstm;
@@ -401,6 +402,233 @@ int twin_backward(blstm_ctx* ctx, const void* theta, const void* x, const void* 
     return BLSTM_OK;
 }
 
+// ---- the softmax layer beyond cross-entropy: scratch and launch order ------------------------------------------------
+// Where a call's scratch lies (byte offsets).  Rows of z and of W_s that are not whole 16-byte words are copied to padded ones
+// (Zp columns), and what the products then leave padded goes back to its compact place.
+struct LossScratch {
+    int Zp;                   // width of the products: Z rounded up to eight
+    bool copy_w, compact;     // W_s is copied; dz and dW_s are compacted
+    long long ldu;            // row distance of the logits / of dE/du
+    int chunk;                // rows whose logits are held at a time (calls without gradients)
+    size_t zc, wp, dzp, dwp, label_logit, entry_logit, entry_q, soft_const, soft_state, pmax, psum, ptau, rows, row_loss, hi, lo, u, partial, partial_bytes, bytes;
+};
+static_assert(BLSTM_MAX_TOP == LOSS_MAX_TOP, "the kernels' lists must hold every entry");
+// Logits held at a time where they are only read once more: 128 MiB stay in the last-level cache.
+constexpr size_t kLossChunkBytes = (size_t)128 << 20;
+
+LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
+    LossScratch l{};
+    const size_t M = (size_t)c->M, V = (size_t)c->V, e = c->esz;
+    const bool bf = c->st == DT_BF16, gradient = call == SOFTMAX_DISTILL || call == SOFTMAX_POLICY;
+    l.Zp = (c->zdim + 7) & ~7;
+    l.compact = l.Zp != c->zdim;
+    l.copy_w = l.compact || c->off_ws * e % 16 != 0;
+    l.ldu = (c->V + 7) & ~7;
+    size_t w = 0;
+    auto put = [&](size_t* at, size_t bytes) { *at = w; w += up256(bytes); };
+    const size_t per_row = (size_t)l.ldu * 4;
+    size_t chunk = kLossChunkBytes / per_row & ~size_t(127);
+    if (chunk < 128) chunk = 128;
+    l.chunk = (int)(chunk < M ? chunk : M);
+    if (l.copy_w) put(&l.wp, V * l.Zp * e);
+    if (gradient || l.copy_w) put(&l.zc, M * l.Zp * e);
+    if (bf && call != SOFTMAX_TOPK) {
+        const size_t strips = (size_t)loss_strips(c->V);
+        put(&l.label_logit, M * 4);
+        put(&l.pmax, strips * M * 4);
+        put(&l.psum, strips * M * 4);
+        if (call == SOFTMAX_DISTILL) {
+            put(&l.ptau, strips * M * 4);
+            put(&l.entry_logit, M * K * 4);
+            put(&l.entry_q, M * K * 4);
+            put(&l.soft_const, M * 4);
+            put(&l.soft_state, M * 4);
+        }
+        if (gradient) {
+            put(&l.rows, M * sizeof(LossRow));
+            put(&l.hi, M * (size_t)l.ldu * 2);
+            put(&l.lo, M * (size_t)l.ldu * 2);
+        }
+    } else {
+        put(&l.u, (gradient ? M : (size_t)l.chunk) * per_row);
+    }
+    size_t need = 0;
+    auto upd = [&](size_t b) { if (b > need) need = b; };
+    if (!bf || call == SOFTMAX_TOPK) upd(gemm_partial_bytes(gradient ? c->M : l.chunk, c->V, l.Zp, 1, c->st, true));
+    if (gradient) {
+        put(&l.row_loss, M * 4);
+        if (l.compact) { put(&l.dzp, M * l.Zp * e); put(&l.dwp, V * l.Zp * 4); }
+        upd(gemm_partial_bytes(c->M, l.Zp, c->V, 1, c->st));
+        upd(gemm_partial_bytes(c->V, l.Zp, bf ? 2 * c->M : c->M, 1, c->st));
+    }
+    l.partial_bytes = up256(need);
+    put(&l.partial, l.partial_bytes);
+    l.bytes = w > 0 ? w : 256;
+    return l;
+}
+
+// What the four calls have in common: their arguments' checks, and the operands as the products read them.
+struct LossCall {
+    LossScratch l;
+    char* base;
+    hipStream_t st;
+    const void* W;            // rows of Zp
+    const void* b;
+    const void* z;            // the caller's, rows of the model's width
+    const void* zc;           // rows of Zp; the caller's z where no copy is made
+    template <typename T> T* at(size_t off) const { return reinterpret_cast<T*>(base + off); }
+};
+
+int loss_check(const char* name, const blstm_ctx* ctx, int call, int K, const void* theta, const void* z, void* scratch, size_t scratch_bytes, LossScratch* l) {
+    if (K < 0 || ((call == SOFTMAX_TOPK || call == SOFTMAX_DISTILL) && (K < 1 || K > BLSTM_MAX_TOP || K > ctx->V)))
+        return fail(BLSTM_ERR_DIM, "%s: K must be in 1..min(V, %d)", name, BLSTM_MAX_TOP);
+    if (!scratch) return fail(BLSTM_ERR_NULL, "%s: null scratch", name);
+    if (!aligned16(theta) || !aligned16(z) || !aligned16(scratch)) return fail(BLSTM_ERR_ALIGN, "%s: pointers must be 16-byte aligned", name);
+    *l = loss_scratch(ctx, call, K);
+    if (scratch_bytes < l->bytes) return fail(BLSTM_ERR_WORKSPACE, "%s: %zu bytes of scratch given, %zu needed", name, scratch_bytes, l->bytes);
+    return BLSTM_OK;
+}
+
+int loss_begin(blstm_ctx* ctx, const LossScratch& l, const void* theta, const void* z, void* scratch, hipStream_t st, LossCall* c) {
+    c->l = l; c->base = static_cast<char*>(scratch); c->st = st;
+    c->W = ::at(theta, ctx->off_ws, ctx->esz); c->b = ::at(theta, ctx->off_bs, ctx->esz);
+    c->z = z;
+    c->zc = z;
+    if (l.copy_w) {
+        const BlockTensor t{ctx->off_ws, 0, 1, ctx->V, ctx->V, 1, ctx->zdim, l.Zp};
+        RUN(PC_MISC, "padded softmax layer", launch_pad_blocks(&t, 1, theta, c->base + l.wp, ctx->st, st));
+        c->W = c->base + l.wp;
+    }
+    return BLSTM_OK;
+}
+
+// Logits of `rows` frames from row `first` on into u (float).
+int loss_logits(blstm_ctx* ctx, const LossCall& c, int first, int rows, float* u) {
+    hipStream_t st = c.st;
+    GemmDesc d{};
+    d.nseg = 1; d.batch = 1; d.in_type = ctx->st; d.out_type = DT_F32;
+    d.partial = c.at<float>(c.l.partial); d.partial_bytes = c.l.partial_bytes;
+    d.M = rows; d.N = ctx->V;
+    d.seg[0] = GemmSeg{::at(c.zc, (size_t)first * c.l.Zp, ctx->esz), c.W, c.l.Zp, c.l.Zp, 0, 0, c.l.Zp};
+    d.C = u; d.ldc = c.l.ldu; d.c_pad = padded_rows(ctx->V, c.l.ldu);
+    d.long_parts = true;
+    d.bias = c.b;
+    RUN(PC_GEMM_LOGITS, "logits", launch_gemm(d, st));
+    return BLSTM_OK;
+}
+
+// From dE/du (bf16: hi + lo, float: u): dz, dW_s and db_s.
+int loss_products(blstm_ctx* ctx, const LossCall& c, void* dz, float* grad) {
+    hipStream_t st = c.st;
+    const LossScratch& l = c.l;
+    const int M = ctx->M, V = ctx->V, Z = l.Zp;
+    const bool bf = ctx->st == DT_BF16;
+    const void* U = c.base + (bf ? l.hi : l.u);
+    auto desc = [&](DType out) {
+        GemmDesc d{};
+        d.nseg = 1; d.batch = 1; d.in_type = ctx->st; d.out_type = out;
+        d.partial = c.at<float>(l.partial); d.partial_bytes = l.partial_bytes;
+        d.a_pad = padded_rows(V, l.ldu);
+        return d;
+    };
+    {   // dz = du W_s
+        GemmDesc d = desc(ctx->st);
+        d.M = M; d.N = Z; d.btrans = true;
+        d.seg[0] = GemmSeg{U, c.W, l.ldu, Z, 0, 0, V};
+        d.C = l.compact ? c.base + l.dzp : static_cast<char*>(dz); d.ldc = Z;
+        RUN(PC_GEMM_SOFTMAX_BWD, "dz", launch_gemm(d, st));
+    }
+    {   // dW_s = du^T z with db_s as the row sums of du^T
+        GemmDesc d = desc(DT_F32);
+        d.M = V; d.N = Z; d.atrans = true; d.btrans = true;
+        d.seg[0] = GemmSeg{U, c.zc, l.ldu, Z, 0, 0, M};
+        if (bf) { d.nseg = 2; d.seg[1] = d.seg[0]; d.seg[1].A = c.base + l.lo; }
+        d.C = l.compact ? c.at<float>(l.dwp) : grad + ctx->off_ws; d.ldc = Z;
+        d.rowsum = grad + ctx->off_bs;
+        RUN(PC_GEMM_SOFTMAX_BWD, "dW_s", launch_gemm(d, st));
+    }
+    if (l.compact) {
+        const BlockTensor tz{0, 0, 1, M, M, 1, ctx->zdim, Z}, tw{ctx->off_ws, 0, 1, V, V, 1, ctx->zdim, Z};
+        RUN(PC_MISC, "dz", launch_compact_blocks(&tz, 1, c.base + l.dzp, dz, ctx->st, st));
+        RUN(PC_MISC, "softmax layer's gradient", launch_compact_blocks(&tw, 1, c.base + l.dwp, grad, DT_F32, st));
+    }
+    return BLSTM_OK;
+}
+
+// Forward, per-row terms and gradients of one call: log-probabilities (neither policy nor teacher), the policy loss or distillation.
+int loss_run(blstm_ctx* ctx, const LossCall& given, const int32_t* labels, const PolicyArgs* policy, const TeacherArgs* teacher, float* loss_dev, float* logp, void* dz, float* grad) {
+    LossCall c = given;
+    hipStream_t st = c.st;
+    const LossScratch& l = c.l;
+    const int M = ctx->M, V = ctx->V;
+    const bool gradient = policy || teacher;
+    if (gradient || l.copy_w) c.zc = c.base + l.zc;
+    const bool bf = ctx->st == DT_BF16;
+    if (bf || gradient || l.copy_w) {
+        LossPrepArgs a{};
+        a.z = c.z; a.zc = c.zc == c.z ? nullptr : c.base + l.zc; a.M = M; a.V = V; a.Z = ctx->zdim; a.ldzc = l.Zp;
+        a.labels = labels;
+        a.keep = !gradient;
+        if (teacher) a.teacher = *teacher;
+        if (bf) {
+            a.W = static_cast<const unsigned short*>(c.W); a.bias = static_cast<const unsigned short*>(c.b);
+            a.label_logit = c.at<float>(l.label_logit);
+            a.entry_logit = c.at<float>(l.entry_logit); a.entry_q = c.at<float>(l.entry_q);
+            a.soft_const = c.at<float>(l.soft_const); a.soft_state = c.at<int>(l.soft_state);
+        }
+        RUN(PC_SOFTMAX_ROWS, "rows of the loss", launch_loss_prep(a, ctx->st, st));
+    }
+    if (!bf) {
+        const int step = gradient ? M : l.chunk;
+        for (int m = 0; m < M; m += step) {
+            const int n = M - m < step ? M - m : step;
+            const int rc = loss_logits(ctx, c, m, n, c.at<float>(l.u));
+            if (rc != BLSTM_OK) return rc;
+            LossRowsArgs a{};
+            a.u = c.at<float>(l.u); a.ldu = l.ldu; a.M = n; a.V = V; a.s = ctx->s;
+            a.labels = labels ? labels + m : nullptr; a.policy = policy; a.teacher = teacher;
+            a.logp = logp ? logp + m : nullptr; a.row_loss = c.at<float>(l.row_loss);
+            RUN(PC_SOFTMAX_ROWS, "softmax rows", launch_loss_rows_f32(a, st));
+        }
+    } else {
+        LossTileArgs t{};
+        t.z = static_cast<const unsigned short*>(c.zc); t.W = static_cast<const unsigned short*>(c.W); t.bias = static_cast<const unsigned short*>(c.b);
+        t.M = M; t.V = V; t.ld = l.Zp;
+        t.inv_tau = teacher && teacher->inv_tau != 1.0f ? teacher->inv_tau : 0.0f;
+        t.part_max = c.at<float>(l.pmax); t.part_sum = c.at<float>(l.psum); t.part_sum_tau = c.at<float>(l.ptau);
+        t.rows = c.at<LossRow>(l.rows);
+        t.hi = c.at<unsigned short>(l.hi); t.lo = c.at<unsigned short>(l.lo); t.ldu = l.ldu;
+        RUN(PC_GEMM_LOGITS, "sums of the softmax", launch_loss_stats(t, st));
+        LossMergeArgs g{};
+        g.M = M; g.V = V; g.strips = loss_strips(V);
+        g.part_max = t.part_max; g.part_sum = t.part_sum; g.part_sum_tau = t.inv_tau != 0.0f ? t.part_sum_tau : nullptr;
+        g.labels = labels; g.label_logit = c.at<float>(l.label_logit); g.s = ctx->s;
+        g.policy = policy; g.teacher = teacher;
+        g.soft_const = c.at<float>(l.soft_const); g.soft_state = c.at<int>(l.soft_state);
+        g.logp = logp; g.row_loss = c.at<float>(l.row_loss); g.rows = gradient ? c.at<LossRow>(l.rows) : nullptr;
+        RUN(PC_SOFTMAX_ROWS, "rows of the softmax", launch_loss_merge(g, st));
+        if (gradient) {
+            RUN(PC_GEMM_LOGITS, "du", launch_loss_grad(t, st));
+            if (teacher) {
+                LossEntriesArgs n{};
+                n.rows = t.rows; n.classes = teacher->classes; n.entry_logit = c.at<float>(l.entry_logit); n.entry_q = c.at<float>(l.entry_q);
+                n.inv_tau = t.inv_tau; n.weight = ctx->s * teacher->soft * teacher->tau;
+                n.M = M; n.V = V; n.K = teacher->K; n.hi = t.hi; n.lo = t.lo; n.ldu = l.ldu;
+                RUN(PC_SOFTMAX_ROWS, "du of the teacher's classes", launch_loss_entries(n, st));
+            }
+        }
+    }
+    if (!gradient) return BLSTM_OK;
+    RUN(PC_MISC, "loss sum", launch_sum_to_scalar(c.at<float>(l.row_loss), M, loss_dev, st));
+    return loss_products(ctx, c, dz, grad);
+}
+
+// What softmax_xent_fwd_bwd left to the next blstm_backward is written by the call itself.
+void drop_deferred(blstm_ctx* ctx) {
+    ctx->pend_z = nullptr;
+    if (ctx->twin) ctx->twin->pend_z = nullptr;
+}
+
 }  // namespace
 
 extern "C" {
@@ -782,6 +1010,86 @@ int softmax_xent_fwd_bwd_noalloc(blstm_ctx* ctx, const void* theta, const void* 
     SoftmaxScratch sc{base, ctx->ldu, reinterpret_cast<float*>(base + first), reinterpret_cast<float*>(base + first + rows), ctx->soft_part};
     if (ctx->twin) ctx->twin->pend_z = nullptr;         // (this call writes what an earlier one may have left to the twin's backward pass)
     return softmax_xent_run(ctx, sc, theta, z, labels, loss_dev, dz, grad, static_cast<hipStream_t>(stream), false);
+}
+
+size_t softmax_scratch_bytes(const blstm_ctx* ctx, int call, int K) {
+    if (!ctx) { fail(BLSTM_ERR_NULL, "softmax_scratch_bytes: null argument"); return 0; }
+    if (call < SOFTMAX_LOGPROB || call > SOFTMAX_POLICY) { fail(BLSTM_ERR_DIM, "softmax_scratch_bytes: no call %d", call); return 0; }
+    if ((call == SOFTMAX_TOPK || call == SOFTMAX_DISTILL) && (K < 1 || K > BLSTM_MAX_TOP || K > ctx->V)) {
+        fail(BLSTM_ERR_DIM, "softmax_scratch_bytes: K must be in 1..min(V, %d)", BLSTM_MAX_TOP);
+        return 0;
+    }
+    return loss_scratch(ctx, call, K).bytes;
+}
+
+int softmax_logprob(blstm_ctx* ctx, const void* theta, const void* z, const int32_t* labels, float* logp, void* scratch, size_t scratch_bytes, void* stream) {
+    if (!ctx || !theta || !z || !labels || !logp) return fail(BLSTM_ERR_NULL, "softmax_logprob: null argument");
+    LossScratch l;
+    int rc = loss_check("softmax_logprob", ctx, SOFTMAX_LOGPROB, 0, theta, z, scratch, scratch_bytes, &l);
+    if (rc != BLSTM_OK) return rc;
+    LossCall c;
+    rc = loss_begin(ctx, l, theta, z, scratch, static_cast<hipStream_t>(stream), &c);
+    return rc != BLSTM_OK ? rc : loss_run(ctx, c, labels, nullptr, nullptr, nullptr, logp, nullptr, nullptr);
+}
+
+int softmax_topk(blstm_ctx* ctx, const void* theta, const void* z, int K, float* values, int32_t* classes, void* scratch, size_t scratch_bytes, void* stream) {
+    if (!ctx || !theta || !z || !values || !classes) return fail(BLSTM_ERR_NULL, "softmax_topk: null argument");
+    LossScratch l;
+    int rc = loss_check("softmax_topk", ctx, SOFTMAX_TOPK, K, theta, z, scratch, scratch_bytes, &l);
+    if (rc != BLSTM_OK) return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    LossCall c;
+    rc = loss_begin(ctx, l, theta, z, scratch, st, &c);
+    if (rc != BLSTM_OK) return rc;
+    if (l.copy_w) {
+        const BlockTensor t{0, 0, 1, ctx->M, ctx->M, 1, ctx->zdim, l.Zp};
+        RUN(PC_MISC, "padded z", launch_pad_blocks(&t, 1, z, c.base + l.zc, ctx->st, st));
+        c.zc = c.base + l.zc;
+    }
+    for (int m = 0; m < ctx->M; m += l.chunk) {
+        const int n = ctx->M - m < l.chunk ? ctx->M - m : l.chunk;
+        rc = loss_logits(ctx, c, m, n, c.at<float>(l.u));
+        if (rc != BLSTM_OK) return rc;
+        RUN(PC_SOFTMAX_ROWS, "largest logits", launch_row_topk(c.at<float>(l.u), l.ldu, n, ctx->V, K, values + (size_t)m * K, classes + (size_t)m * K, st));
+    }
+    return BLSTM_OK;
+}
+
+int softmax_distill_fwd_bwd(blstm_ctx* ctx, const void* theta, const void* z, const int32_t* labels, const float* teacher_values,
+                            const int32_t* teacher_classes, int K, float temperature, float hard_weight, float soft_weight,
+                            float* loss_dev, void* dz, float* grad, void* scratch, size_t scratch_bytes, void* stream) {
+    if (!ctx || !theta || !z || !teacher_values || !teacher_classes || !loss_dev || !dz || !grad) return fail(BLSTM_ERR_NULL, "softmax_distill_fwd_bwd: null argument");
+    if (!(temperature > 0.0f) || !(1.0f / temperature > 0.0f) || temperature * temperature > 3e38f || !(hard_weight >= 0.0f && hard_weight <= 3e38f) || !(soft_weight > 0.0f && soft_weight <= 3e38f))
+        return fail(BLSTM_ERR_DIM, "softmax_distill_fwd_bwd: temperature and soft_weight must be positive, hard_weight not negative, all finite");
+    if (hard_weight != 0.0f && !labels) return fail(BLSTM_ERR_NULL, "softmax_distill_fwd_bwd: hard_weight needs labels");
+    LossScratch l;
+    int rc = loss_check("softmax_distill_fwd_bwd", ctx, SOFTMAX_DISTILL, K, theta, z, scratch, scratch_bytes, &l);
+    if (rc != BLSTM_OK) return rc;
+    if (!aligned16(dz) || !aligned16(grad)) return fail(BLSTM_ERR_ALIGN, "softmax_distill_fwd_bwd: pointers must be 16-byte aligned");
+    drop_deferred(ctx);
+    LossCall c;
+    rc = loss_begin(ctx, l, theta, z, scratch, static_cast<hipStream_t>(stream), &c);
+    if (rc != BLSTM_OK) return rc;
+    const TeacherArgs t{teacher_values, teacher_classes, K, 1.0f / temperature, hard_weight, soft_weight, temperature};
+    return loss_run(ctx, c, hard_weight != 0.0f ? labels : nullptr, nullptr, &t, loss_dev, nullptr, dz, grad);
+}
+
+int softmax_policy_fwd_bwd(blstm_ctx* ctx, const void* theta, const void* z, const int32_t* labels, const float* advantage,
+                           const float* old_logp, const float* ref_logp, float clip_low, float clip_high, float kl_weight,
+                           float* loss_dev, float* logp, void* dz, float* grad, void* scratch, size_t scratch_bytes, void* stream) {
+    if (!ctx || !theta || !z || !labels || !advantage || !loss_dev || !dz || !grad) return fail(BLSTM_ERR_NULL, "softmax_policy_fwd_bwd: null argument");
+    if (!(clip_low >= 0.0f && clip_low <= 1.0f) || !(clip_high >= 0.0f && clip_high <= 3e38f) || !(kl_weight >= 0.0f && kl_weight <= 3e38f))
+        return fail(BLSTM_ERR_DIM, "softmax_policy_fwd_bwd: clip_low must be in 0..1, clip_high and kl_weight not negative and finite");
+    LossScratch l;
+    int rc = loss_check("softmax_policy_fwd_bwd", ctx, SOFTMAX_POLICY, 0, theta, z, scratch, scratch_bytes, &l);
+    if (rc != BLSTM_OK) return rc;
+    if (!aligned16(dz) || !aligned16(grad)) return fail(BLSTM_ERR_ALIGN, "softmax_policy_fwd_bwd: pointers must be 16-byte aligned");
+    drop_deferred(ctx);
+    LossCall c;
+    rc = loss_begin(ctx, l, theta, z, scratch, static_cast<hipStream_t>(stream), &c);
+    if (rc != BLSTM_OK) return rc;
+    const PolicyArgs p{advantage, old_logp, ref_logp, clip_low, clip_high, kl_weight};
+    return loss_run(ctx, c, labels, &p, nullptr, loss_dev, logp, dz, grad);
 }
 
 int blstm_backward(blstm_ctx* ctx, const void* theta, const void* x, const void* dz, float* grad, void* stream) {

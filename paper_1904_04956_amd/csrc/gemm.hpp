@@ -26,7 +26,7 @@ struct GemmDesc {
     long long sBias;
     const float* add;         // float [M][N] added to the product, or null
     long long ldadd, sAdd;
-    float* rowsum;            // rowsum[m] = sum_k A(m,k) of segment 0 (bias gradients), or null
+    float* rowsum;            // rowsum[m] = sum_k A(m,k) of both segments (bias gradients), or null
     long long sRowsum;
     float* partial;           // scratch for split-K partial tiles (float), or null: never split
     size_t partial_bytes;

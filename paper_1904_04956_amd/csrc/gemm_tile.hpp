@@ -48,7 +48,7 @@ struct Params {
     void* C; long long ldc;
     const void* bias;               // element type of the inputs
     const float* add; long long ldadd;
-    float* rowsum;                  // rowsum[m] = sum_k A(m,k) over segment 0, or null
+    float* rowsum;                  // rowsum[m] = sum_k A(m,k) over both segments, or null
     float* partial;                 // split-K: float [batch][splits][M][N], or null
     float* rs_partial;              // split-K: float [batch][splits][M] row sums
     int M, N, ntm, ntn, splits;
@@ -545,7 +545,7 @@ __device__ __forceinline__ void gemm_tile(const Params& P, int lin, const int sp
 #pragma unroll
                 for (int q = 0; q < CHUNKS / 2; ++q) {
                     mma<TI>(acc, fa[q], fb[q]);
-                    if (RS && do_rs && it < ntiles[0]) {
+                    if (RS && do_rs) {
 #pragma unroll
                         for (int i = 0; i < NRS; ++i) rs[i] = add_row(rs[i], fa[q][i]);
                     }
@@ -580,7 +580,7 @@ __device__ __forceinline__ void gemm_tile(const Params& P, int lin, const int sp
                 if (NF == 2) { if (q + 1 < CHUNKS / 2) lfrag(a_s, b_s, q + 1, af[(q + 1) % NF], bf[(q + 1) % NF]); }
                 else lfrag(a_s, b_s, q, af[0], bf[0]);
                 mma<TI>(acc, af[q % NF], bf[q % NF]);
-                if (RS && do_rs && it < ntiles[0]) {
+                if (RS && do_rs) {
 #pragma unroll
                     for (int i = 0; i < NRS; ++i) rs[i] = add_row(rs[i], af[q % NF][i]);
                 }
@@ -671,7 +671,7 @@ __device__ __forceinline__ void gemm_tile(const Params& P, int lin, const int sp
             if (NF == 2) { if (q + 1 < CHUNKS / 2) lfrag(a_s, b_s, q + 1, af[(q + 1) % NF], bf[(q + 1) % NF]); }
             else lfrag(a_s, b_s, q, af[0], bf[0]);
             mma<TI>(acc, af[q % NF], bf[q % NF]);
-            if (RS && do_rs && it < ntiles[0]) {
+            if (RS && do_rs) {
 #pragma unroll
                 for (int i = 0; i < NRS; ++i) rs[i] = add_row(rs[i], af[q % NF][i]);
             }

@@ -1,0 +1,132 @@
+// Launchers of the softmax layer's operators beyond cross-entropy (losses.hip, losses_rows.hip).  All pointers are device pointers.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+#include "gemm.hpp"
+
+namespace blstm {
+
+constexpr int LOSS_STRIP = 64;                       // classes of one partial sum of a row
+constexpr int LOSS_MAX_TOP = 256;                    // BLSTM_MAX_TOP of the C header
+
+// What a row's dE/du is made of: du_v = a exp2(u_v log2e - m2) + at exp2(u_v log2e / tau - mt2) - hot [v = label].
+// A row that counts for nothing has a = at = hot = 0, label = -1 and m2 = mt2 = +inf.
+struct LossRow {
+    float m2, a, mt2, at;
+    float hot;
+    int label;
+    float max;                                       // of the row's logits
+    float pad;
+};
+
+// u log2e - m2 is one multiply-add, whose m2 = max log2e is rounded: the same for all classes of a row, so that it cancels, but 2^-24 of
+// itself off.  From LOSS_FAR on (the type's lowest value as a bias rules a class out, and with it whole strips) it is (u - max) log2e.
+constexpr float LOSS_FAR = 1e5f;
+
+// The policy loss of one frame: present or absent old / reference log-probabilities, where the ratio is clipped, weight of the KL term.
+struct PolicyArgs {
+    const float* advantage;
+    const float* old_logp;                           // null: the weights that sampled are the present ones, ratio 1
+    const float* ref_logp;                           // null: no KL term
+    float clip_low, clip_high, kl_weight;
+};
+// A teacher's list: [M][K]; entries with class -1 or value -inf are not used.
+struct TeacherArgs {
+    const float* values;
+    const int32_t* classes;
+    int K;
+    float inv_tau, hard, soft;                       // 1/tau, weights of the two terms (soft: times tau^2 in the loss, tau in the gradient)
+    float tau;
+};
+
+// Rows ahead of the products: zc = z with the rows that count for nothing set to zero, rows of ldzc elements, zeros behind Z.
+// bf16 (the float rows hold their logits, see launch_loss_rows_f32): the label's logit, the entries' logits, q and the row's sum q (log q - u / tau).
+struct LossPrepArgs {
+    const void* z;
+    void* zc;                                        // or null: not wanted
+    bool keep;                                       // rows that count for nothing are copied as they are
+    int M, V, Z, ldzc;
+    const unsigned short* W;                         // rows of ldzc elements, zeros behind Z; null: only zc is wanted
+    const unsigned short* bias;
+    const int32_t* labels;                           // or null
+    float* label_logit;                              // [M]
+    TeacherArgs teacher;                             // K = 0: none
+    float* entry_logit;                              // [M][K]
+    float* entry_q;                                  // [M][K], 0: not used
+    float* soft_const;                               // [M]
+    int* soft_state;                                 // [M]: bit 0: some entry is used; bit 1: some class is out of range (the loss is NaN)
+};
+hipError_t launch_loss_prep(const LossPrepArgs& a, DType type, hipStream_t st);
+
+// bf16: the logits' tiles straight into what is wanted of them; the matrix itself is not written.
+struct LossTileArgs {
+    const unsigned short* z;                         // [M][ld], zeros in columns Z .. ld - 1
+    const unsigned short* W;                         // [V][ld], likewise
+    const unsigned short* bias;
+    int M, V, ld;                                    // ld: a multiple of eight, at least Z
+    float inv_tau;                                   // of the second sum (0: none)
+    float* part_max;                                 // [strips][M] maximum of a strip's logits
+    float* part_sum;                                 // [strips][M] sum of exp2(u log2e - max log2e)
+    float* part_sum_tau;                             // [strips][M] the same at the temperature
+    const LossRow* rows;                             // gradient: [M]
+    unsigned short* hi;                              // [M][ldu] du rounded to bf16, zeros in columns V .. ldu - 1
+    unsigned short* lo;                              // [M][ldu] what the rounding left, rounded
+    long long ldu;
+};
+inline int loss_strips(int V) { return (V + 2 * LOSS_STRIP - 1) / (2 * LOSS_STRIP) * 2; }
+hipError_t launch_loss_stats(const LossTileArgs& a, hipStream_t st);
+hipError_t launch_loss_grad(const LossTileArgs& a, hipStream_t st);
+
+// Joins the strips of every row, then what the call wants of a row: logp, loss term, LossRow (null: not wanted).
+struct LossMergeArgs {
+    int M, V, strips;
+    const float* part_max;
+    const float* part_sum;
+    const float* part_sum_tau;                       // or null
+    const int32_t* labels;
+    const float* label_logit;
+    float s;                                         // loss scale
+    const PolicyArgs* policy;                        // host pointers: exactly one of the two, or neither (log-probabilities)
+    const TeacherArgs* teacher;
+    const float* soft_const;
+    const int* soft_state;
+    float* logp;
+    float* row_loss;
+    LossRow* rows;
+};
+hipError_t launch_loss_merge(const LossMergeArgs& a, hipStream_t st);
+
+// The teacher's entries in du, exactly: each once rounded from its own value.
+struct LossEntriesArgs {
+    const LossRow* rows;
+    const int32_t* classes;
+    const float* entry_logit;
+    const float* entry_q;
+    float inv_tau, weight;                           // weight: s soft tau
+    int M, V, K;
+    unsigned short* hi;
+    unsigned short* lo;
+    long long ldu;
+};
+hipError_t launch_loss_entries(const LossEntriesArgs& a, hipStream_t st);
+
+// float: everything of a row from its logits u [M][ldu], which dE/du overwrites (gradient false: they stay).
+struct LossRowsArgs {
+    float* u;
+    long long ldu;
+    int M, V;
+    float s;
+    const int32_t* labels;
+    const PolicyArgs* policy;                        // host pointers, as above
+    const TeacherArgs* teacher;
+    bool gradient;
+    float* logp;
+    float* row_loss;
+};
+hipError_t launch_loss_rows_f32(const LossRowsArgs& a, hipStream_t st);
+
+// The K largest of every row of u [M][ldu] with their columns, by falling value, equal ones by rising column.
+hipError_t launch_row_topk(const float* u, long long ldu, int M, int V, int K, float* values, int32_t* classes, hipStream_t st);
+
+}  // namespace blstm

@@ -1,0 +1,494 @@
+// What the softmax layer's losses do row by row: ahead of the products, behind them, on float logits, and the selection of
+// the K largest.  With u the logits of a frame, y its label, q the teacher's distribution over the entries of its list:
+//   log p_y = u_y - log sum_v exp u_v
+//   policy:  r = exp(log p_y - old), l = -min(r A, clip(r) A) + k (exp(ref - log p_y) - (ref - log p_y) - 1)
+//            g = dl/dlog p_y = -(r A, unless the clip is what the minimum takes) + k (1 - exp(ref - log p_y)),  dl/du = g (1_y - p)
+//   distill: l = h (-log p_y) + w tau^2 sum_k q_k (log q_k - log p'_k), p' = softmax(u / tau)
+//            dl/du = h (p - 1_y) + w tau (p' - sum_k q_k 1_k)
+#include "common.hpp"
+#include "losses.hpp"
+
+namespace blstm {
+namespace {
+
+constexpr float LOG2E = 1.44269504f, LN2 = 0.693147181f;
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+// Between a wavefront's LDS stores and its other lanes' loads of them.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+enum { LIST_USED = 1, LIST_BAD = 2 };
+
+// A class list of one row in LDS, as its wavefront sees it.
+struct ListLds { int cls[LOSS_MAX_TOP]; float q[LOSS_MAX_TOP], log_q[LOSS_MAX_TOP], logit[LOSS_MAX_TOP]; };
+
+// q over the used entries of a row, by one wavefront.  Returns LIST_USED if there are any, and LIST_BAD if some class is out of range.
+// An entry that is not used has class -1 and q 0.  (A value of -inf is a probability of zero: it would make a list
+// of nothing else a division of zero by zero.)
+__device__ int teacher_list(const TeacherArgs& t, long long m, int V, ListLds& s) {
+    const int lane = threadIdx.x & 63;
+    float top = -INFINITY;
+    bool bad = false, some = false;
+    for (int k = lane; k < t.K; k += 64) {
+        const int c = t.classes[m * t.K + k];
+        const float v = t.values[m * t.K + k];
+        const bool in = (unsigned)c < (unsigned)V;
+        bad |= !in && c != -1;
+        const bool used = in && !(v == -INFINITY);
+        some |= used;
+        s.cls[k] = used ? c : -1;
+        s.log_q[k] = v * t.inv_tau;
+        if (used) top = fmaxf(top, v * t.inv_tau);
+    }
+    top = wave_max(top);
+    float sum = 0.0f;
+    for (int k = lane; k < t.K; k += 64) {
+        const float e = s.cls[k] >= 0 ? expf(s.log_q[k] - top) : 0.0f;
+        s.q[k] = e;
+        sum += e;
+    }
+    sum = wave_sum(sum);
+    for (int k = lane; k < t.K; k += 64) {
+        const bool used = s.cls[k] >= 0;
+        s.q[k] = used ? s.q[k] / sum : 0.0f;
+        s.log_q[k] = used ? s.log_q[k] - top - logf(sum) : 0.0f;
+    }
+    wave_sync();
+    return (__any(some) ? LIST_USED : 0) | (__any(bad) ? LIST_BAD : 0);
+}
+
+// Sum of q of the entries with entry k's class (a class may stand in a list more than once).
+__device__ __forceinline__ float class_weight(const ListLds& s, int K, int k) {
+    float w = 0.0f;
+    for (int j = 0; j < K; ++j) w += s.cls[j] == s.cls[k] ? s.q[j] : 0.0f;
+    return w;
+}
+
+struct PolicyTerms { float loss, g; };
+__device__ __forceinline__ PolicyTerms policy_terms(const PolicyArgs& p, long long m, float lp) {
+    const float A = p.advantage[m];
+    float loss = 0.0f, g = 0.0f;
+    if (A != 0.0f) {                                     // (an infinite ratio times an advantage of zero is no number)
+        const float r = p.old_logp ? expf(lp - p.old_logp[m]) : 1.0f;
+        const float inner = r * A, outer = fminf(fmaxf(r, 1.0f - p.clip_low), 1.0f + p.clip_high) * A;
+        loss = inner > outer ? -outer : -inner;          // (a NaN ratio stays one)
+        const bool cut = (A > 0.0f && r > 1.0f + p.clip_high) || (A < 0.0f && r < 1.0f - p.clip_low);
+        g = cut ? 0.0f : -inner;
+    }
+    if (p.ref_logp) {
+        const float d = p.ref_logp[m] - lp, e = expm1f(d);
+        loss += p.kl_weight * (e - d);
+        g -= p.kl_weight * e;
+    }
+    return {loss, g};
+}
+
+// ---- ahead of the products: a wavefront a row -----------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void loss_prep_kernel(LossPrepArgs a) {
+    __shared__ ListLds lists[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long m = (long long)blockIdx.x * 4 + wave;
+    if (m >= a.M) return;
+    ListLds& s = lists[wave];
+    const int lab = a.labels ? a.labels[m] : -1;
+    const bool lab_ok = (unsigned)lab < (unsigned)a.V;
+    int state = 0;
+    if (a.teacher.K > 0) state = teacher_list(a.teacher, m, a.V, s);
+    const bool live = a.keep || lab_ok || (state & LIST_USED);
+    const T* z = static_cast<const T*>(a.z) + m * a.Z;
+    if (a.zc) {
+        T* zc = static_cast<T*>(a.zc) + m * a.ldzc;
+        for (int k = lane; k < a.ldzc; k += 64) zc[k] = live && k < a.Z ? z[k] : (T)0;
+    }
+    if (!a.W) return;
+    if constexpr (sizeof(T) == 2) {
+        // sixteen lanes a product, eight elements a lane and step
+        const int l16 = lane & 15, g = lane >> 4;
+        auto logit = [&](int c) {
+            float acc = 0.0f;
+            const bf16_t* w = a.W + (long long)c * a.ldzc;   // (zeros behind Z)
+            for (int k = l16 * 8; k < a.Z; k += 128) {
+                const uint4 wv = *reinterpret_cast<const uint4*>(w + k);
+                const uint32_t ww[4] = {wv.x, wv.y, wv.z, wv.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int e = k + 2 * q;
+                    if (e < a.Z) acc = fmaf(bf2f(z[e]), bf2f((bf16_t)(ww[q] & 0xFFFFu)), acc);
+                    if (e + 1 < a.Z) acc = fmaf(bf2f(z[e + 1]), bf2f((bf16_t)(ww[q] >> 16)), acc);
+                }
+            }
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) acc += __shfl_xor(acc, o, 64);
+            return acc + bf2f(a.bias[c]);
+        };
+        const float u = lab_ok ? logit(lab) : 0.0f;
+        if (lane == 0) a.label_logit[m] = u;
+        if (a.teacher.K > 0) {
+            float part = 0.0f;
+            for (int k0 = 0; k0 < a.teacher.K; k0 += 4) {
+                const int k = k0 + g;
+                const int c = k < a.teacher.K ? s.cls[k] : -1;
+                const float v = c >= 0 ? logit(c) : 0.0f;
+                if (l16 == 0 && k < a.teacher.K) {
+                    a.entry_logit[m * a.teacher.K + k] = v;
+                    a.entry_q[m * a.teacher.K + k] = s.q[k];
+                    if (c >= 0) part += s.q[k] * (s.log_q[k] - v * a.teacher.inv_tau);
+                }
+            }
+            part = l16 == 0 ? part : 0.0f;
+            part = wave_sum(part);
+            if (lane == 0) { a.soft_const[m] = part; a.soft_state[m] = state; }
+        }
+    }
+}
+
+// ---- behind the sums of the strips: 64 rows a workgroup, its wavefronts share the strips ------------------------------
+template <bool TAU, bool POLICY, bool TEACHER>
+__global__ __launch_bounds__(512) void loss_merge_kernel(LossMergeArgs a, PolicyArgs policy, TeacherArgs teacher) {
+    __shared__ float sh_max[8][64], sh_sum[8][64], sh_tau[8][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long m = (long long)blockIdx.x * 64 + lane;
+    const bool in = m < a.M;
+    float mx = -INFINITY;
+    if (in) {
+#pragma unroll 8
+        for (int i = wave; i < a.strips; i += 8) mx = fmaxf(mx, a.part_max[(long long)i * a.M + m]);
+    }
+    sh_max[wave][lane] = mx;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 8; ++w) mx = fmaxf(mx, sh_max[w][lane]);
+    const float m2 = mx * LOG2E, lt = LOG2E * teacher.inv_tau, mt2 = TAU ? mx * lt : 0.0f;
+    const bool far = fabsf(mx) > LOSS_FAR;
+    float sum = 0.0f, tau = 0.0f;
+    if (in) {
+#pragma unroll 4
+        for (int i = wave; i < a.strips; i += 8) {
+            const float pm = a.part_max[(long long)i * a.M + m];
+            const bool away = far || fabsf(pm) > LOSS_FAR;
+            sum += a.part_sum[(long long)i * a.M + m] * __builtin_amdgcn_exp2f(away ? (pm - mx) * LOG2E : pm * LOG2E - m2);
+            if (TAU) tau += a.part_sum_tau[(long long)i * a.M + m] * __builtin_amdgcn_exp2f(away ? (pm - mx) * lt : pm * lt - mt2);
+        }
+    }
+    sh_sum[wave][lane] = sum;
+    if (TAU) sh_tau[wave][lane] = tau;
+    __syncthreads();
+    if (wave != 0 || !in) return;
+    sum = 0.0f; tau = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) { sum += sh_sum[w][lane]; if (TAU) tau += sh_tau[w][lane]; }
+    const int lab = a.labels ? a.labels[m] : -1;
+    const bool lab_ok = (unsigned)lab < (unsigned)a.V;
+    const float nan = __builtin_nanf("");
+    // u_y - max in the scale of the sums, whose maximum is rounded once: the same number in all of them
+    const float up = far ? a.label_logit[m] - mx : fmaf(a.label_logit[m], LOG2E, -m2) * LN2;
+    const float lp = lab_ok ? up - logf(sum) : lab == -1 ? 0.0f : nan;
+    if (a.logp) a.logp[m] = lp;
+    if (!a.rows) return;
+    LossRow r{};
+    r.m2 = INFINITY; r.mt2 = INFINITY; r.label = -1; r.max = INFINITY;
+    float loss = 0.0f;
+    if (POLICY) {
+        if (lab_ok) {
+            const PolicyTerms t = policy_terms(policy, m, lp);
+            loss = a.s * t.loss;
+            r.m2 = m2; r.a = -a.s * t.g / sum; r.hot = -a.s * t.g; r.label = lab;
+        } else if (lab != -1) loss = nan;
+    }
+    if (TEACHER) {
+        const int state = a.soft_state[m];
+        if (lab_ok && teacher.hard != 0.0f) {
+            loss = a.s * teacher.hard * -lp;
+            r.m2 = m2; r.a = a.s * teacher.hard / sum; r.hot = a.s * teacher.hard; r.label = lab;
+        } else if (lab != -1 && teacher.hard != 0.0f) loss = nan;
+        if (state & LIST_USED) {
+            const float lse = TAU ? mt2 * LN2 + logf(tau) : m2 * LN2 + logf(sum);   // (of u / tau)
+            loss += a.s * teacher.soft * teacher.tau * teacher.tau * (a.soft_const[m] + lse);
+            const float at = a.s * teacher.soft * teacher.tau;
+            if (TAU) { r.mt2 = mt2; r.at = at / tau; }
+            else { r.m2 = m2; r.a += at / sum; }
+        }
+        if (state & LIST_BAD) loss = nan;
+    }
+    if (r.a != 0.0f || r.at != 0.0f) r.max = mx;         // (a NaN is not 0)
+    a.row_loss[m] = loss;
+    a.rows[m] = r;
+}
+
+// ---- the teacher's entries of du: a wavefront a row -------------------------------------------------------------------
+__global__ __launch_bounds__(256) void loss_entries_kernel(LossEntriesArgs a) {
+    __shared__ ListLds lists[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long m = (long long)blockIdx.x * 4 + wave;
+    if (m >= a.M) return;
+    ListLds& s = lists[wave];
+    for (int k = lane; k < a.K; k += 64) {
+        const int c = a.classes[m * a.K + k];
+        const float q = a.entry_q[m * a.K + k];
+        s.cls[k] = q > 0.0f && (unsigned)c < (unsigned)a.V ? c : -1;
+        s.q[k] = q;
+    }
+    wave_sync();
+    const LossRow r = a.rows[m];
+    const float lt = LOG2E * a.inv_tau;
+    for (int k = lane; k < a.K; k += 64) {
+        const int c = s.cls[k];
+        if (c < 0) continue;
+        const float u = a.entry_logit[m * a.K + k];
+        const bool far = fabsf(r.max) > LOSS_FAR;
+        float v = r.a * __builtin_amdgcn_exp2f(far ? (u - r.max) * LOG2E : fmaf(u, LOG2E, -r.m2)) + r.at * __builtin_amdgcn_exp2f(far ? (u - r.max) * lt : fmaf(u, lt, -r.mt2));
+        if (c == r.label) v -= r.hot;
+        v -= a.weight * class_weight(s, a.K, k);
+        const bf16_t hi = f2bf(v);
+        a.hi[m * a.ldu + c] = hi;                        // (of entries with one class each writes the same)
+        a.lo[m * a.ldu + c] = f2bf(v - bf2f(hi));
+    }
+}
+
+// ---- float: a workgroup a row of logits -----------------------------------------------------------------------------------
+template <bool MAX>
+__device__ __forceinline__ float rows_reduce(float v, float* sh) {
+    v = MAX ? wave_max(v) : wave_sum(v);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = sh[0];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) v = MAX ? fmaxf(v, sh[w]) : v + sh[w];
+    return v;
+}
+
+template <bool TAU, bool POLICY, bool TEACHER, bool GRADIENT>
+__global__ __launch_bounds__(512) void loss_rows_f32_kernel(LossRowsArgs a, PolicyArgs policy, TeacherArgs teacher) {
+    __shared__ float sh[8];
+    __shared__ ListLds list;
+    __shared__ float consts[8];
+    const long long m = blockIdx.x;
+    float* row = a.u + m * a.ldu;
+    const int V = a.V, V4 = V & ~3;
+    const int lab = a.labels ? a.labels[m] : -1;
+    const bool lab_ok = (unsigned)lab < (unsigned)V;
+    float mx = -INFINITY;
+    for (int v = threadIdx.x * 4; v < V4; v += 2048) {
+        const float4 x = *reinterpret_cast<const float4*>(row + v);
+        mx = fmaxf(fmaxf(fmaxf(mx, x.x), fmaxf(x.y, x.z)), x.w);
+    }
+    for (int v = V4 + threadIdx.x; v < V; v += 512) mx = fmaxf(mx, row[v]);
+    mx = rows_reduce<true>(mx, sh);
+    float sum = 0.0f, tau = 0.0f;
+    const float it = teacher.inv_tau;
+    auto add = [&](float x) {
+        sum += expf(x - mx);
+        if (TAU) tau += expf((x - mx) * it);
+    };
+    for (int v = threadIdx.x * 4; v < V4; v += 2048) {
+        const float4 x = *reinterpret_cast<const float4*>(row + v);
+        add(x.x); add(x.y); add(x.z); add(x.w);
+    }
+    for (int v = V4 + threadIdx.x; v < V; v += 512) add(row[v]);
+    sum = rows_reduce<false>(sum, sh);
+    if (TAU) tau = rows_reduce<false>(tau, sh);
+    if (threadIdx.x < 64) {
+        const float nan = __builtin_nanf("");
+        const float lp = lab_ok ? row[lab] - mx - logf(sum) : lab == -1 ? 0.0f : nan;
+        float loss = 0.0f, ca = 0.0f, cat = 0.0f, hot = 0.0f;
+        if (POLICY) {
+            if (lab_ok) {
+                const PolicyTerms t = policy_terms(policy, m, lp);
+                loss = a.s * t.loss; ca = -a.s * t.g / sum; hot = -a.s * t.g;
+            } else if (lab != -1) loss = nan;
+        }
+        if (TEACHER) {
+            const int state = teacher_list(teacher, m, V, list);
+            if (lab_ok && teacher.hard != 0.0f) {
+                loss = a.s * teacher.hard * -lp;
+                ca = a.s * teacher.hard / sum; hot = a.s * teacher.hard;
+            } else if (lab != -1 && teacher.hard != 0.0f) loss = nan;
+            float part = 0.0f;
+            for (int k = threadIdx.x; k < teacher.K; k += 64) {
+                const int c = list.cls[k];
+                const float u = c >= 0 ? row[c] : 0.0f;
+                list.logit[k] = u;
+                if (c >= 0) part += list.q[k] * (list.log_q[k] - (u - mx) * it);
+            }
+            part = wave_sum(part);
+            if (state & LIST_USED) {
+                const float total = TAU ? tau : sum;
+                loss += a.s * teacher.soft * teacher.tau * teacher.tau * (part + logf(total));
+                const float at = a.s * teacher.soft * teacher.tau / total;
+                if (TAU) cat = at; else ca += at;
+            }
+            if (state & LIST_BAD) loss = nan;
+        }
+        if (threadIdx.x == 0) {
+            if (a.logp) a.logp[m] = lp;
+            if (GRADIENT) a.row_loss[m] = loss;
+            consts[0] = ca; consts[1] = cat; consts[2] = hot;
+        }
+    }
+    if (!GRADIENT) return;
+    __syncthreads();                                     // (the label's and the entries' logits are read)
+    const float ca = consts[0], cat = consts[1], hot = consts[2];
+    const bool hard = ca != 0.0f || ca != ca, soft = TAU && (cat != 0.0f || cat != cat);
+    auto grad = [&](float x, int v) {
+        float g = hard ? ca * expf(x - mx) : 0.0f;       // (a row that counts for nothing is zero whatever it holds)
+        if (soft) g += cat * expf((x - mx) * it);
+        return v == lab && lab_ok ? g - hot : g;
+    };
+    for (int v = threadIdx.x * 4; v < V4; v += 2048) {
+        float4 x = *reinterpret_cast<const float4*>(row + v);
+        x.x = grad(x.x, v); x.y = grad(x.y, v + 1); x.z = grad(x.z, v + 2); x.w = grad(x.w, v + 3);
+        *reinterpret_cast<float4*>(row + v) = x;
+    }
+    const int pad = (int)min(a.ldu, (long long)((V + 7) & ~7));
+    for (int v = V4 + threadIdx.x; v < pad; v += 512) row[v] = v < V ? grad(row[v], v) : 0.0f;
+    if (TEACHER) {
+        __syncthreads();
+        const float weight = a.s * teacher.soft * teacher.tau;
+        for (int k = threadIdx.x; k < teacher.K; k += 512)
+            if (list.cls[k] >= 0) row[list.cls[k]] = grad(list.logit[k], list.cls[k]) - weight * class_weight(list, teacher.K, k);
+    }
+}
+
+// ---- the K largest of a row ------------------------------------------------------------------------------------------------
+// Values as whole numbers of the same order, NaN below all; +0 and -0 are equal.
+__device__ __forceinline__ uint32_t order_key(float x) {
+    if (x != x) return 0u;
+    const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);
+    return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+// Finds the K-th largest key eight bits at a time, then, where more entries have that key than are wanted, the last column of
+// them that is; what is above is collected in any order and put in its place by its rank.
+__global__ __launch_bounds__(512) void row_topk_kernel(const float* u, long long ldu, int V, int K, float* values, int32_t* classes) {
+    __shared__ unsigned hist[256];
+    __shared__ unsigned found, above, equal, count;
+    __shared__ unsigned long long list[LOSS_MAX_TOP];
+    const long long m = blockIdx.x;
+    const float* row = u + m * ldu;
+    const int tid = threadIdx.x;
+    // bin of the `want`-th entry from the top of hist: `found`, entries above it: `above`, in it: `equal`
+    auto pick = [&](unsigned want) {
+        __syncthreads();
+        if (tid < 64) {
+            unsigned own = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) own += hist[255 - 4 * tid - j];
+            unsigned before = own;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) { const unsigned t = __shfl_up(before, o, 64); if (tid >= o) before += t; }
+            before -= own;
+            if (before < want && before + own >= want) {
+                unsigned run = before;
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned h = hist[255 - 4 * tid - j];
+                    if (run < want && run + h >= want) { found = 255 - 4 * tid - j; above = run; equal = h; }
+                    run += h;
+                }
+            }
+        }
+        __syncthreads();
+    };
+    auto clear = [&] { __syncthreads(); if (tid < 256) hist[tid] = 0; __syncthreads(); };
+    unsigned prefix = 0, want = (unsigned)K;             // the K-th largest agrees with prefix above the present byte; want-th among those
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        clear();
+        for (int v = tid; v < V; v += 512) {
+            const uint32_t k = order_key(row[v]);
+            if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+        }
+        pick(want);
+        want -= above;
+        prefix |= found << shift;
+    }
+    unsigned last = 0xFFFFFFFFu;                         // of the entries with the K-th key, those up to this column
+    if (equal != want) {
+        unsigned inv = 0, w = want;                      // (the want-th largest of the columns counted from the end)
+        for (int shift = 16; shift >= 0; shift -= 8) {
+            clear();
+            for (int v = tid; v < V; v += 512) {
+                const unsigned k = 0xFFFFFFu - (unsigned)v;
+                if (order_key(row[v]) == prefix && (shift == 16 || (k >> (shift + 8)) == (inv >> (shift + 8)))) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+            }
+            pick(w);
+            w -= above;
+            inv |= found << shift;
+        }
+        last = 0xFFFFFFu - inv;
+    }
+    if (tid == 0) count = 0;
+    __syncthreads();
+    for (int v = tid; v < V; v += 512) {
+        const uint32_t k = order_key(row[v]);
+        if (k > prefix || (k == prefix && (unsigned)v <= last)) {
+            const unsigned i = atomicAdd(&count, 1u);
+            if (i < (unsigned)K) list[i] = ((unsigned long long)k << 32) | (0xFFFFFFFFu - (unsigned)v);
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < K; i += 512) {
+        const unsigned long long k = list[i];
+        int rank = 0;
+        for (int j = 0; j < K; ++j) rank += list[j] > k;
+        const unsigned c = 0xFFFFFFFFu - (unsigned)(k & 0xFFFFFFFFu);
+        values[m * K + rank] = row[c];
+        classes[m * K + rank] = (int32_t)c;
+    }
+}
+
+}  // namespace
+
+hipError_t launch_loss_prep(const LossPrepArgs& a, DType type, hipStream_t st) {
+    const dim3 grid((unsigned)((a.M + 3) / 4));
+    if (type == DT_BF16) hipLaunchKernelGGL(loss_prep_kernel<bf16_t>, grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(loss_prep_kernel<float>, grid, dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_loss_merge(const LossMergeArgs& a, hipStream_t st) {
+    const dim3 grid((unsigned)((a.M + 63) / 64));
+    const PolicyArgs p = a.policy ? *a.policy : PolicyArgs{};
+    const TeacherArgs t = a.teacher ? *a.teacher : TeacherArgs{};
+    if (a.policy) hipLaunchKernelGGL((loss_merge_kernel<false, true, false>), grid, dim3(512), 0, st, a, p, t);
+    else if (a.teacher && a.part_sum_tau) hipLaunchKernelGGL((loss_merge_kernel<true, false, true>), grid, dim3(512), 0, st, a, p, t);
+    else if (a.teacher) hipLaunchKernelGGL((loss_merge_kernel<false, false, true>), grid, dim3(512), 0, st, a, p, t);
+    else hipLaunchKernelGGL((loss_merge_kernel<false, false, false>), grid, dim3(512), 0, st, a, p, t);
+    return hipGetLastError();
+}
+
+hipError_t launch_loss_entries(const LossEntriesArgs& a, hipStream_t st) {
+    hipLaunchKernelGGL(loss_entries_kernel, dim3((unsigned)((a.M + 3) / 4)), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_loss_rows_f32(const LossRowsArgs& a, hipStream_t st) {
+    const dim3 grid((unsigned)a.M), block(512);
+    const PolicyArgs p = a.policy ? *a.policy : PolicyArgs{};
+    const TeacherArgs t = a.teacher ? *a.teacher : TeacherArgs{};
+    if (a.policy) hipLaunchKernelGGL((loss_rows_f32_kernel<false, true, false, true>), grid, block, 0, st, a, p, t);
+    else if (a.teacher && t.inv_tau != 1.0f) hipLaunchKernelGGL((loss_rows_f32_kernel<true, false, true, true>), grid, block, 0, st, a, p, t);
+    else if (a.teacher) hipLaunchKernelGGL((loss_rows_f32_kernel<false, false, true, true>), grid, block, 0, st, a, p, t);
+    else hipLaunchKernelGGL((loss_rows_f32_kernel<false, false, false, false>), grid, block, 0, st, a, p, t);
+    return hipGetLastError();
+}
+
+hipError_t launch_row_topk(const float* u, long long ldu, int M, int V, int K, float* values, int32_t* classes, hipStream_t st) {
+    hipLaunchKernelGGL(row_topk_kernel, dim3((unsigned)M), dim3(512), 0, st, u, ldu, V, K, values, classes);
+    return hipGetLastError();
+}
+
+}  // namespace blstm

@@ -51,6 +51,7 @@ class Learner:
         self.z = torch.zeros((T, B, self.zdim), dtype=self.act_dtype, device=dev)
         self.dz = torch.zeros((T, B, self.zdim), dtype=self.act_dtype, device=dev)
         self.loss = torch.zeros(1, dtype=torch.float32, device=dev)
+        self.scratch = None       # of the softmax layer's calls beyond cross-entropy, made when one is first used
         self.held = None          # HYBRID only: the pulled weights the next gradient is taken on
 
     def close(self):
@@ -96,6 +97,46 @@ class Learner:
         bl.blstm_forward(self.ctx, th, self.x, self.z, stream)
         bl.softmax_xent_fwd_bwd(self.ctx, th, self.z, self.labels, self.loss, self.dz, self.grad, stream)
         bl.blstm_backward(self.ctx, th, self.x, self.dz, self.grad, stream)
+
+    # ---- the softmax layer beyond cross-entropy ------------------------------------------
+    def loss_scratch(self, call, K=0):
+        """Scratch of one of the softmax layer's calls (binding.SOFTMAX_*), kept for the next time."""
+        need = bl.softmax_scratch_bytes(self.ctx, call, K)
+        if self.scratch is None or self.scratch.numel() < need:
+            self.scratch = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return self.scratch
+
+    def log_probs(self, labels=None, weights=None, stream=None):
+        """log p[label] [T][B] of the batch (of `labels` if given, else its own): a forward pass, then the softmax layer."""
+        th = self.theta_fwd if weights is None else weights
+        bl.blstm_forward(self.ctx, th, self.x, self.z, stream)
+        out = torch.empty(self.labels.shape, dtype=torch.float32, device=self.device)
+        bl.softmax_logprob(self.ctx, th, self.z, self.labels if labels is None else labels, out, self.loss_scratch(bl.SOFTMAX_LOGPROB), None, stream)
+        return out
+
+    def top_logits(self, K, weights=None, stream=None):
+        """Values and classes [T][B][K] of the batch's K largest logits: what a student's calgrad_distill takes."""
+        th = self.theta_fwd if weights is None else weights
+        bl.blstm_forward(self.ctx, th, self.x, self.z, stream)
+        shape = (*self.labels.shape, K)
+        values, classes = torch.empty(shape, dtype=torch.float32, device=self.device), torch.empty(shape, dtype=torch.int32, device=self.device)
+        bl.softmax_topk(self.ctx, th, self.z, K, values, classes, self.loss_scratch(bl.SOFTMAX_TOPK, K), None, stream)
+        return values, classes
+
+    def calgrad_distill(self, values, classes, temperature=1.0, hard_weight=0.5, soft_weight=0.5, stream=None):
+        """calgrad() with the loss against a teacher's lists [T][B][K] (and, with a hard_weight, the batch's labels)."""
+        K = classes.shape[-1]
+        bl.blstm_forward(self.ctx, self.theta_fwd, self.x, self.z, stream)
+        bl.softmax_distill_fwd_bwd(self.ctx, self.theta_fwd, self.z, self.labels if hard_weight != 0 else None, values, classes, K, temperature, hard_weight,
+                                   soft_weight, self.loss, self.dz, self.grad, self.loss_scratch(bl.SOFTMAX_DISTILL, K), None, stream)
+        bl.blstm_backward(self.ctx, self.theta_fwd, self.x, self.dz, self.grad, stream)
+
+    def calgrad_policy(self, advantage, old_logp=None, ref_logp=None, clip_low=0.2, clip_high=0.2, kl_weight=0.0, logp=None, stream=None):
+        """calgrad() with the clipped policy loss on the batch's labels, which were sampled."""
+        bl.blstm_forward(self.ctx, self.theta_fwd, self.x, self.z, stream)
+        bl.softmax_policy_fwd_bwd(self.ctx, self.theta_fwd, self.z, self.labels, advantage, old_logp, ref_logp, clip_low, clip_high, kl_weight, self.loss, logp,
+                                  self.dz, self.grad, self.loss_scratch(bl.SOFTMAX_POLICY), None, stream)
+        bl.blstm_backward(self.ctx, self.theta_fwd, self.x, self.dz, self.grad, stream)
 
     def apply(self, lr, stream=None):
         """W' = apply(W, g)."""

@@ -1,0 +1,185 @@
+"""The softmax layer beyond cross-entropy without a GPU: the float64 oracle against finite differences and identities, the calls'
+refusals, their scratch, and what they launch."""
+import json
+
+import numpy as np
+import pytest
+
+from oracle import softmax_losses as sl
+from paper_1904_04956_amd import binding as bl
+from tests.test_dispatch_cpu import recorder  # noqa: F401
+
+
+def draw(seed, M=6, V=9, Z=5, K=4):
+    r = np.random.default_rng(seed)
+    W, b, z = r.normal(size=(V, Z)), r.normal(size=V), r.normal(size=(M, Z))
+    labels = r.integers(0, V, M)
+    classes = np.stack([r.permutation(V)[:K] for _ in range(M)]).astype(np.int32)
+    return r, W, b, z, labels, r.normal(size=(M, K)), classes
+
+
+def differences(f, x, step=1e-6):
+    out = np.zeros_like(x)
+    for i in np.ndindex(x.shape):
+        a, c = x.copy(), x.copy()
+        a[i] += step
+        c[i] -= step
+        out[i] = (f(a) - f(c)) / (2 * step)
+    return out
+
+
+@pytest.mark.parametrize("hard,temperature", [(0.0, 1.0), (0.7, 1.0), (0.7, 2.5)])
+def test_distillation_gradients_are_the_losses_differences(hard, temperature):
+    r, W, b, z, labels, values, classes = draw(1)
+    labels[1] = labels[4] = sl.NO_LABEL
+    classes[2, :] = sl.NO_LABEL                # no entry; frame 4 has neither
+    classes[4, :] = sl.NO_LABEL
+    classes[3, 1] = classes[3, 0]              # a class twice
+    values[5, 2] = -np.inf
+    f = lambda W, b, z: sl.distill(W, b, z, labels, values, classes, 0.3, temperature, hard, 0.8)  # noqa: E731
+    _, dz, dW, db = f(W, b, z)
+    for got, x, at in ((dz, z, lambda v: f(W, b, v)[0]), (dW, W, lambda v: f(v, b, z)[0]), (db, b, lambda v: f(W, v, z)[0])):
+        assert np.abs(got - differences(at, x)).max() < 1e-8
+    assert np.all(dz[4] == 0) and (hard or np.all(dz[2] == 0))
+
+
+@pytest.mark.parametrize("old,ref", [(True, True), (False, True), (True, False), (False, False)])
+def test_policy_gradients_are_the_losses_differences(old, ref):
+    r, W, b, z, labels, _, _ = draw(2, M=12)
+    lp = sl.logprob(W, b, z, labels)
+    labels[3] = sl.NO_LABEL
+    A = r.normal(size=12)
+    o = lp + 0.4 * r.normal(size=12) if old else None          # some ratios lie beyond the clip
+    q = lp + 0.3 * r.normal(size=12) if ref else None
+    if old:
+        f = lambda W, b, z: sl.policy(W, b, z, labels, A, o, q, 0.3, 0.2, 0.25, 0.1)  # noqa: E731
+        assert {bool(x) for x in (np.exp(lp - o) * A > np.clip(np.exp(lp - o), 0.8, 1.25) * A)} == {True, False}
+    else:
+        # (with r = 1 the loss does not move with the ratio: its gradient is that of -A log p)
+        def f(W, b, z):
+            out = sl.policy(W, b, z, labels, A, None, q, 0.3, 0.2, 0.25, 0.1)
+            live = labels != sl.NO_LABEL
+            return (out[0] - 0.3 * (A * (out[1] - 0.0))[live].sum(), *out[1:])
+    _, _, dz, dW, db = f(W, b, z)
+    for got, x, at in ((dz, z, lambda v: f(W, b, v)[0]), (dW, W, lambda v: f(v, b, z)[0]), (db, b, lambda v: f(W, v, z)[0])):
+        assert np.abs(got - differences(at, x)).max() < 1e-8
+    assert np.all(dz[3] == 0)
+
+
+def test_what_counts_for_nothing_may_hold_anything():
+    r, W, b, z, labels, values, classes = draw(3)
+    labels[2] = sl.NO_LABEL
+    classes[2] = sl.NO_LABEL
+    first = sl.distill(W, b, z, labels, values, classes, 1.0, 2.0, 0.5, 0.5)
+    z2, values2 = z.copy(), values.copy()
+    z2[2], values2[2] = np.nan, np.inf
+    second = sl.distill(W, b, z2, labels, values2, classes, 1.0, 2.0, 0.5, 0.5)
+    for x, y in zip(first, second):
+        assert np.array_equal(x, y)
+
+
+def test_a_teacher_that_is_the_student_gives_no_gradient():
+    r, W, b, z, labels, _, _ = draw(4)
+    u = z @ W.T + b
+    values, classes = sl.topk(u, 9)
+    loss, dz, dW, db = sl.distill(W, b, z, None, values, classes, 1.0, 1.7, 0.0, 1.0)
+    assert abs(loss) < 1e-12 and np.abs(dz).max() < 1e-12
+
+
+def test_equal_logits_come_by_class_and_nan_last():
+    values, classes = sl.topk(np.array([[1.0, 3.0, np.nan, 3.0, -np.inf, 0.0, -0.0]]), 7)
+    assert classes[0].tolist() == [1, 3, 0, 5, 6, 4, 2]
+
+
+# ---- refusals ------------------------------------------------------------------------------------------------------
+
+@pytest.fixture
+def ctx():
+    c = bl.blstm_create(2, 2, 2, 4, 1, 0, 300, 1)
+    yield c
+    bl.blstm_destroy(c)
+
+
+CALLS = {"logprob": (bl.SOFTMAX_LOGPROB, 0), "topk": (bl.SOFTMAX_TOPK, 3), "distill": (bl.SOFTMAX_DISTILL, 3), "policy": (bl.SOFTMAX_POLICY, 0)}
+
+
+def call(ctx, name, **change):
+    """The call with arguments that pass every check (addresses that are never followed), but for those given."""
+    which, K = CALLS[name]
+    a = dict(theta=4096, z=4096, labels=4096, K=3, values=4096, classes=4096, advantage=4096, old=4096, ref=4096, temperature=2.0, hard=0.5, soft=0.5,
+             low=0.2, high=0.2, kl=0.1, loss=4096, logp=4096, dz=4096, grad=4096, scratch=4096, nbytes=bl.softmax_scratch_bytes(ctx, which, K))
+    a.update(change)
+    if name == "logprob":
+        return bl.softmax_logprob(ctx, a["theta"], a["z"], a["labels"], a["logp"], a["scratch"], a["nbytes"], 0)
+    if name == "topk":
+        return bl.softmax_topk(ctx, a["theta"], a["z"], a["K"], a["values"], a["classes"], a["scratch"], a["nbytes"], 0)
+    if name == "distill":
+        return bl.softmax_distill_fwd_bwd(ctx, a["theta"], a["z"], a["labels"], a["values"], a["classes"], a["K"], a["temperature"], a["hard"], a["soft"],
+                                          a["loss"], a["dz"], a["grad"], a["scratch"], a["nbytes"], 0)
+    return bl.softmax_policy_fwd_bwd(ctx, a["theta"], a["z"], a["labels"], a["advantage"], a["old"], a["ref"], a["low"], a["high"], a["kl"],
+                                     a["loss"], a["logp"], a["dz"], a["grad"], a["scratch"], a["nbytes"], 0)
+
+
+NAN, INF = float("nan"), float("inf")
+REFUSED = [(n, dict(change), code) for n, need, code in (
+    ("logprob", ("theta", "z", "labels", "logp", "scratch"), -1), ("topk", ("theta", "z", "values", "classes", "scratch"), -1),
+    ("distill", ("theta", "z", "labels", "values", "classes", "loss", "dz", "grad", "scratch"), -1),
+    ("policy", ("theta", "z", "labels", "advantage", "loss", "dz", "grad", "scratch"), -1)) for change in [[(k, None)] for k in need]]
+REFUSED += [(n, {k: 4100}, -4) for n in CALLS for k in ("theta", "z", "scratch")]
+REFUSED += [(n, {k: 4100}, -4) for n in ("distill", "policy") for k in ("dz", "grad")]
+REFUSED += [(n, dict(nbytes=0), -3) for n in CALLS]
+REFUSED += [(n, dict(K=k), -2) for n in ("topk", "distill") for k in (0, -1, bl.BLSTM_MAX_TOP + 1)]
+REFUSED += [("distill", {k: v}, -2) for k, v in (("temperature", 0.0), ("temperature", -1.0), ("temperature", NAN), ("temperature", INF), ("temperature", 1e30), ("hard", -0.1), ("hard", NAN),
+                                                 ("hard", INF), ("soft", 0.0), ("soft", NAN), ("soft", INF))]
+REFUSED += [("policy", {k: v}, -2) for k, v in (("low", -0.1), ("low", 1.1), ("low", NAN), ("high", -0.1), ("high", NAN), ("high", INF), ("kl", -0.1), ("kl", NAN), ("kl", INF))]
+
+
+@pytest.mark.parametrize("name,change,code", REFUSED, ids=lambda v: str(v))
+def test_refused_before_any_launch(ctx, name, change, code):
+    with pytest.raises(bl.BlstmError) as e:
+        call(ctx, name, **change)
+    assert e.value.code == code and f"softmax_{name}" in str(e.value)
+
+
+def test_lists_are_no_longer_than_the_classes():
+    c = bl.blstm_create(2, 2, 2, 4, 1, 0, 5, 0)
+    try:
+        assert bl.softmax_scratch_bytes(c, bl.SOFTMAX_TOPK, 5) > 0
+        for which in (bl.SOFTMAX_TOPK, bl.SOFTMAX_DISTILL):
+            for K in (0, 6):
+                with pytest.raises(bl.BlstmError):
+                    bl.softmax_scratch_bytes(c, which, K)
+        for which in (-1, 4):
+            with pytest.raises(bl.BlstmError):
+                bl.softmax_scratch_bytes(c, which, 1)
+        assert bl.lib().softmax_scratch_bytes(None, 0, 0) == 0
+    finally:
+        bl.blstm_destroy(c)
+
+
+def test_no_workspace_is_needed_and_none_is_larger(ctx):
+    # the scratch is the calls' own: what blstm_bind asks for has not grown with them
+    c = bl.blstm_create(21, 256, 260, 512, 4, 256, 32000, 1)
+    try:
+        M, V = 21 * 256, 32000
+        assert bl.softmax_scratch_bytes(c, bl.SOFTMAX_LOGPROB) < 64 << 20
+        assert bl.softmax_scratch_bytes(c, bl.SOFTMAX_POLICY) < M * V * 4 + (512 << 20)
+    finally:
+        bl.blstm_destroy(c)
+
+
+def test_a_deferred_weight_gradient_is_dropped(recorder):  # noqa: F811
+    # the call writes the slices of grad that softmax_xent_fwd_bwd had left to blstm_backward: nothing may come over them again
+    a, b = recorder("""
+        out = []
+        for policy in (0, 1):
+            m = Model(T=4, B=16, D=8, H=64, L=1, P=0, V=200)
+            m.option(bl.BLSTM_OPT_DEFER_SOFTMAX_WGRAD, 1)
+            m.forward(); m.xent()
+            if policy:
+                n = bl.softmax_scratch_bytes(m.ctx, bl.SOFTMAX_POLICY)
+                bl.softmax_policy_fwd_bwd(m.ctx, P, P, P, P, None, None, 0.2, 0.2, 0.0, P, None, P, P, P, n, 0)
+            # (given another gradient vector, blstm_backward refuses only while something is left to it)
+            out.append(bl.lib().blstm_backward(m.ctx, P, P, P, 2 * P, None))
+    """)
+    assert (a, b) == (-2, 0)
