@@ -410,11 +410,29 @@ struct LossScratch {
     bool copy_w, compact;     // W_s is copied; dz and dW_s are compacted
     long long ldu;            // row distance of the logits / of dE/du
     int chunk;                // rows whose logits are held at a time (calls without gradients)
+    bool fused;               // the kernels of losses_fused.hip: no du in memory
+    int row_parts, class_parts;
+    size_t bias_f, consts, part, part_ref, part_sum, cparts, cparts_b;
     size_t zc, wp, dzp, dwp, label_logit, entry_logit, entry_q, soft_const, soft_state, pmax, psum, ptau, rows, row_loss, hi, lo, u, partial, partial_bytes, bytes;
 };
 static_assert(BLSTM_MAX_TOP == LOSS_MAX_TOP, "the kernels' lists must hold every entry");
 // Logits held at a time where they are only read once more: 128 MiB stay in the last-level cache.
 constexpr size_t kLossChunkBytes = (size_t)128 << 20;
+
+// Into how many parts the classes of a workgroup's 256 rows are cut, and the rows of a workgroup's 128 classes: the least estimated
+// time (us) of rounds of one workgroup a CU, tile by tile, with what is written and read again for every part.
+int loss_parts(long long groups, long long tiles, double tile_us, double part_us) {
+    int best = 1;
+    double least = 0.0;
+    for (long long p = 1; p <= tiles && p <= 256; ++p) {
+        const double rounds = (double)((groups * p + 255) / 256), t = rounds * ((double)((tiles + p - 1) / p) * tile_us + 4.0) + (p > 1 ? 3.0 : 0.0) + part_us * (double)p;
+        if (p == 1 || t < least) { least = t; best = (int)p; }
+    }
+    const long long per = (tiles + best - 1) / best;
+    return (int)((tiles + per - 1) / per);               // (no empty part)
+}
+int loss_row_parts(int M, int V, int Zp) { return loss_parts((M + 255) / 256, (V + 63) / 64, 2.2 * Zp / 256, 2.0 * M * Zp * 4 / 4e6); }
+int loss_class_parts(int M, int V, int Zp) { return loss_parts((V + 127) / 128, (M + 63) / 64, 1.8 * Zp / 256, 2.0 * V * Zp * 4 / 4e6); }
 
 LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
     LossScratch l{};
@@ -435,6 +453,21 @@ LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
     if (bf && call != SOFTMAX_TOPK) {
         const size_t strips = (size_t)loss_strips(c->V);
         put(&l.label_logit, M * 4);
+        l.fused = call == SOFTMAX_POLICY && l.Zp <= LOSS_FUSED_WIDTH;
+        if (l.fused) {
+            l.row_parts = loss_row_parts(c->M, c->V, l.Zp);
+            l.class_parts = loss_class_parts(c->M, c->V, l.Zp);
+            const size_t Mp = (M + 63) & ~size_t(63), P = (size_t)l.row_parts, C = (size_t)l.class_parts;
+            put(&l.bias_f, ((V + 63) & ~size_t(63)) * 4);
+            put(&l.consts, 6 * Mp * 4);
+            put(&l.part, P * M * l.Zp * 4);
+            put(&l.part_ref, P * M * 4);
+            put(&l.part_sum, P * M * 4);
+            if (C > 1) { put(&l.cparts, C * V * c->zdim * 4); put(&l.cparts_b, C * V * 4); }
+            put(&l.row_loss, M * 4);
+            l.bytes = w;
+            return l;
+        }
         put(&l.pmax, strips * M * 4);
         put(&l.psum, strips * M * 4);
         if (call == SOFTMAX_DISTILL) {
@@ -555,6 +588,39 @@ int loss_products(blstm_ctx* ctx, const LossCall& c, void* dz, float* grad) {
     return BLSTM_OK;
 }
 
+// bf16, z of up to LOSS_FUSED_WIDTH: rows, dz, classes.
+int loss_run_fused(blstm_ctx* ctx, const LossCall& c, const int32_t* labels, const PolicyArgs* policy, const TeacherArgs* teacher, float* loss_dev, float* logp, void* dz, float* grad) {
+    hipStream_t st = c.st;
+    const LossScratch& l = c.l;
+    const float log2e = 1.44269504f;
+    LossFusedArgs f{};
+    f.z = reinterpret_cast<const unsigned short*>(c.base + l.zc); f.W = static_cast<const unsigned short*>(c.W);
+    f.bias = c.at<float>(l.bias_f); f.consts = c.at<float>(l.consts);
+    f.M = ctx->M; f.Mp = (ctx->M + 63) & ~63; f.V = ctx->V; f.Z = ctx->zdim; f.ld = l.Zp;
+    f.k1 = log2e; f.k = log2e;
+    f.parts = l.row_parts;
+    f.out = c.at<float>(l.part); f.part_ref = c.at<float>(l.part_ref); f.part_sum = c.at<float>(l.part_sum);
+    RUN(PC_GEMM_LOGITS, "rows of the softmax", launch_loss_fused_rows(f, false, false, st));
+    LossDzArgs d{};
+    d.M = f.M; d.Mp = f.Mp; d.V = f.V; d.Z = f.Z; d.ld = f.ld; d.parts = f.parts;
+    d.part = f.out; d.part_ref = f.part_ref; d.part_sum = f.part_sum; d.W = f.W;
+    d.labels = labels; d.label_logit = c.at<float>(l.label_logit); d.s = ctx->s;
+    d.policy = policy; d.teacher = teacher;
+    d.logp = logp; d.row_loss = c.at<float>(l.row_loss); d.consts = c.at<float>(l.consts);
+    d.dz = static_cast<unsigned short*>(dz);
+    RUN(PC_SOFTMAX_ROWS, "dz", launch_loss_dz(d, false, st));
+    float* dw = grad + ctx->off_ws;
+    float* db = grad + ctx->off_bs;
+    f.parts = l.class_parts;
+    f.out = l.class_parts > 1 ? c.at<float>(l.cparts) : dw; f.out_db = l.class_parts > 1 ? c.at<float>(l.cparts_b) : db;
+    f.ldo = ctx->zdim; f.vec = ctx->zdim % 4 == 0 && aligned16(f.out);
+    RUN(PC_GEMM_SOFTMAX_BWD, "dW_s", launch_loss_fused_classes(f, false, st));
+    if (l.class_parts > 1)
+        RUN(PC_GEMM_SOFTMAX_BWD, "dW_s", launch_loss_classes_sum(f.out, f.out_db, f.parts, (long long)ctx->V * ctx->zdim, ctx->V, dw, db, st));
+    RUN(PC_MISC, "loss sum", launch_sum_to_scalar(c.at<float>(l.row_loss), ctx->M, loss_dev, st));
+    return BLSTM_OK;
+}
+
 // Forward, per-row terms and gradients of one call: log-probabilities (neither policy nor teacher), the policy loss or distillation.
 int loss_run(blstm_ctx* ctx, const LossCall& given, const int32_t* labels, const PolicyArgs* policy, const TeacherArgs* teacher, float* loss_dev, float* logp, void* dz, float* grad) {
     LossCall c = given;
@@ -573,11 +639,13 @@ int loss_run(blstm_ctx* ctx, const LossCall& given, const int32_t* labels, const
         if (bf) {
             a.W = static_cast<const unsigned short*>(c.W); a.bias = static_cast<const unsigned short*>(c.b);
             a.label_logit = c.at<float>(l.label_logit);
+            if (l.fused) a.bias_f = c.at<float>(l.bias_f);
             a.entry_logit = c.at<float>(l.entry_logit); a.entry_q = c.at<float>(l.entry_q);
             a.soft_const = c.at<float>(l.soft_const); a.soft_state = c.at<int>(l.soft_state);
         }
         RUN(PC_SOFTMAX_ROWS, "rows of the loss", launch_loss_prep(a, ctx->st, st));
     }
+    if (l.fused) return loss_run_fused(ctx, c, labels, policy, teacher, loss_dev, logp, dz, grad);
     if (!bf) {
         const int step = gradient ? M : l.chunk;
         for (int m = 0; m < M; m += step) {

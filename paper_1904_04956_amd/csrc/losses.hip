@@ -7,12 +7,10 @@
 // lane holds 32 classes of one row, half of a strip of 64: maximum and sums are in its registers, and one exchange with the
 // other half of the wavefront completes them.
 #include "gemm_tile.hpp"
-#include "losses.hpp"
+#include "losses_terms.hpp"
 
 namespace blstm {
 namespace {
-
-constexpr float LOG2E = 1.44269504f;
 
 template <bool TAU, bool GRAD>
 __global__ __launch_bounds__(256, 2) void loss_tile_kernel(LossTileArgs a, int ntm, int ntv) {

@@ -49,6 +49,7 @@ struct LossPrepArgs {
     int M, V, Z, ldzc;
     const unsigned short* W;                         // rows of ldzc elements, zeros behind Z; null: only zc is wanted
     const unsigned short* bias;
+    float* bias_f;                                   // [V rounded up to 64] the bias as floats, -inf behind it; or null
     const int32_t* labels;                           // or null
     float* label_logit;                              // [M]
     TeacherArgs teacher;                             // K = 0: none
@@ -77,6 +78,50 @@ struct LossTileArgs {
 inline int loss_strips(int V) { return (V + 2 * LOSS_STRIP - 1) / (2 * LOSS_STRIP) * 2; }
 hipError_t launch_loss_stats(const LossTileArgs& a, hipStream_t st);
 hipError_t launch_loss_grad(const LossTileArgs& a, hipStream_t st);
+
+// z of up to 256, bf16 (losses_fused.hip).
+constexpr int LOSS_FUSED_WIDTH = 256;
+struct LossFusedArgs {
+    const unsigned short* z;                         // [M][ld], zeros in columns Z .. ld - 1
+    const unsigned short* W;                         // [V][ld], likewise
+    const float* bias;                               // [V rounded up to 64], -inf beyond V
+    const float* consts;                             // [6][Mp]: LossRow's m2, a, mt2, at, hot, label (as bits); rows M .. Mp - 1 count for nothing
+    int M, Mp, V, Z, ld;                             // Mp: M rounded up to 64
+    float k1, k;                                     // scale of the first exponential, and of the second (rows, sums not known: the only one)
+    int parts;                                       // of the classes (rows kernel) or of the rows (classes kernel), a workgroup each
+    float* out;                                      // rows: [parts][M][ld]; classes: [parts][V][ldo], columns 0 .. Z - 1
+    float* part_ref;                                 // rows, sums not known: [parts][M] reference and sum
+    float* part_sum;
+    float* out_db;                                   // classes: [parts][V]
+    long long ldo;
+    int vec;                                         // classes: rows of out take 16-byte stores
+};
+hipError_t launch_loss_fused_rows(const LossFusedArgs& a, bool known, bool tau, hipStream_t st);
+hipError_t launch_loss_fused_classes(const LossFusedArgs& a, bool tau, hipStream_t st);
+// dz from the parts of launch_loss_fused_rows, exactly completed by the label's and the teacher's classes; with known false the
+// rows' losses and constants too.
+struct LossDzArgs {
+    int M, Mp, V, Z, ld, parts;
+    const float* part;
+    const float* part_ref;
+    const float* part_sum;
+    const unsigned short* W;                         // rows of ld
+    const int32_t* labels;
+    const float* label_logit;
+    float s;
+    const PolicyArgs* policy;                        // host pointers: one of the two
+    const TeacherArgs* teacher;
+    const float* entry_q;
+    const float* soft_const;
+    const int* soft_state;
+    float* logp;                                     // or null
+    float* row_loss;
+    float* consts;                                   // [6][Mp]
+    unsigned short* dz;                              // [M][Z]
+};
+hipError_t launch_loss_dz(const LossDzArgs& a, bool known, hipStream_t st);
+// out = sum of parts of n floats, out_b of V, in order.
+hipError_t launch_loss_classes_sum(const float* p, const float* pb, int parts, long long n, int V, float* out, float* out_b, hipStream_t st);
 
 // Joins the strips of every row, then what the call wants of a row: logp, loss term, LossRow (null: not wanted).
 struct LossMergeArgs {

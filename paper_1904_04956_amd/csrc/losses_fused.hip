@@ -1,0 +1,502 @@
+// The softmax layer's losses for z of up to 256, bf16 operands: dE/du and the logits exist in registers only.
+//
+//   rows      a workgroup keeps 256 rows of z in registers and walks over the classes: u = W_s z + b_s, then sum_v w_v W_v with
+//             w = exp(u - reference) and their sum (the reference moves with the running maximum), or with w = dE/du itself
+//             where the sums are known.  The label's and the teacher's classes, few a row, are added behind it, exactly.
+//   classes   a workgroup keeps 128 classes of W_s in registers and walks over the rows: dE/du from the rows' sums, then
+//             dW_s = du^T z and db_s.  du goes into the product as the sum of two bf16 numbers (of three where a label is).
+//
+// Both read a tile [64][Z] in LDS twice: by rows for the logits (ds_read_b128) and by columns for what is made of them
+// (ds_read_b64_tr_b16 transposes on the way).  16-byte chunk c of row r lies at chunk c ^ sw(r): the eight rows that a phase
+// of the first reads, and the four of the second, are on different banks.  The output of the first product (lane: row or
+// class, registers: the other) is the operand of the second after one exchange between the lane halves.
+#include "gemm_tile.hpp"
+#include "losses_terms.hpp"
+
+namespace blstm {
+namespace {
+
+constexpr float SLACK = 8.0f;                           // powers of two by which a weight may pass one before the reference moves
+
+__device__ __forceinline__ int sw(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+
+// The lane's number, made anew: kept across a loop, or what follows from it ahead of one, it would take registers that there are not.
+__device__ __forceinline__ int fresh_lane() {
+    int l;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+    return l;
+}
+
+// A ring of tiles of 64 rows, NK slabs of 64 columns, loaded by eight wavefronts straight into LDS.
+template <int NK>
+struct Ring {
+    static constexpr int CPR = 8 * NK, ROWB = 128 * NK, TILE = 64 * ROWB, STAGE = TILE + 2048, STAGES = 3;
+    static __device__ __forceinline__ void dma16(unsigned lds, const char* base, unsigned voff) {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(base) : "memory");
+    }
+    static __device__ __forceinline__ void dma4(unsigned lds, const char* base, unsigned voff) {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(base) : "memory");
+    }
+    // rows first .. first + 63 of p (those beyond `rows` repeat the last one, chunks beyond a row's end its last chunk)
+    static __device__ __forceinline__ void tile(unsigned lds, const bf16_t* p, int first, int rows, int ld, int wv) {
+        const unsigned lane = (unsigned)fresh_lane();
+        const char* base = reinterpret_cast<const char*>(p + (long long)first * ld);
+        const int last = rows - 1 - first, lastc = ld / 8 - 1;
+#pragma unroll
+        for (int j = 0; j < NK; ++j) {
+            const unsigned i = (unsigned)(j * 8 + wv) * 64u + lane, x = i % CPR;
+            const int r = (int)(i / CPR), c = (int)(x & ~7u) | ((int)(x & 7u) ^ sw(r));
+            dma16(lds + (unsigned)((j * 8 + wv) * 1024), base, (unsigned)(__mul24(min(r, last), ld * 2) + min(c, lastc) * 16));
+        }
+    }
+};
+
+// A lane's reads of a tile.  By rows: chunk 2 q + half of row l32 is at row ^ 32 (q % 4), 128 (q / 4) on.  By columns: of sixteen rows,
+// columns 32 zb .., the first four of each eight at col ^ 64 (zb % 2), 128 (zb / 2) on, the other four 4 rows and chunk ^ 1 on.
+template <int NK>
+struct Reads {
+    int row, col;
+    __device__ __forceinline__ Reads(int lane) {
+        const int l32 = lane & 31, half = lane >> 5, li = lane & 15, g = lane >> 4;
+        row = l32 * Ring<NK>::ROWB + ((half ^ sw(l32)) << 4);
+        const int r = 8 * half + (li >> 2), x = (2 * (g & 1) + ((li & 3) >> 1)) ^ ((li >> 2) << 1);
+        col = r * Ring<NK>::ROWB + (x << 4) + (li & 1) * 8;
+    }
+    __device__ __forceinline__ uint4 by_row(const char* s, int q) const { return *reinterpret_cast<const uint4*>(s + (row ^ ((q & 3) << 5)) + 128 * (q >> 2)); }
+    __device__ __forceinline__ uint4 by_col(const char* s, int zb) const {
+        const char* p = s + (col ^ ((zb & 1) << 6)) + 128 * (zb >> 1);
+        const char* p4 = s + (col ^ ((zb & 1) << 6) ^ 16) + 128 * (zb >> 1) + 4 * Ring<NK>::ROWB;
+        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)p));
+        const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)p4));
+        return make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
+};
+
+__device__ __forceinline__ f32x16_t mma32(const uint4& a, const uint4& b, const f32x16_t& c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+// Eight values of a lane, packed, at 8 (e / 4) + 4 half + e % 4 of sixteen, as the operand of a product over the sixteen.
+__device__ __forceinline__ uint4 fragment(const unsigned (&p)[4]) {
+    const auto a = __builtin_amdgcn_permlane32_swap(p[0], p[2], false, false), b = __builtin_amdgcn_permlane32_swap(p[1], p[3], false, false);
+    return make_uint4(a[0], b[0], a[1], b[1]);
+}
+
+// The order of a block of N operands read from LDS and multiplied: FIRST reads, then MMA products and READS reads in turn, DEPTH operands
+// ahead (the compiler puts each read in front of its product, whose wait is then all of the LDS's latency).
+template <int FIRST, int N, int MMA, int READS, int DEPTH>
+__device__ __forceinline__ void ahead() {
+    __builtin_amdgcn_sched_group_barrier(0x100, FIRST, 0);
+    each<0, N - DEPTH>([](auto) { __builtin_amdgcn_sched_group_barrier(0x8, MMA, 0); __builtin_amdgcn_sched_group_barrier(0x100, READS, 0); });
+    __builtin_amdgcn_sched_group_barrier(0x8, MMA * DEPTH, 0);
+}
+constexpr int DEPTH = 4;
+
+// ---- rows -------------------------------------------------------------------------------------------------------------------
+// KNOWN: w = a exp2(u log2e - m2) (+ at exp2(u k - mt2)) from the rows' constants, else w = exp2(u k - reference).
+template <int NK, bool KNOWN, bool TAU>
+__global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
+    typedef Ring<NK> R;
+    extern __shared__ uint4 smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
+    const int part = (int)blockIdx.x % a.parts, row0 = (int)blockIdx.x / a.parts * 256;
+    const int ntv = (a.V + 63) / 64, per = (ntv + a.parts - 1) / a.parts, t0 = part * per, n = min(per, ntv - t0);
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
+    const Reads<NK> at(lane);
+    const int m = row0 + wv * 32 + l32;
+    uint4 zf[4 * NK];
+#pragma unroll
+    for (int q = 0; q < 4 * NK; ++q) {
+        const int c = 2 * q + half;
+        zf[q] = c * 8 < a.ld ? *reinterpret_cast<const uint4*>(a.z + (long long)min(m, a.M - 1) * a.ld + c * 8) : make_uint4(0, 0, 0, 0);
+    }
+    float m2 = 0.0f, ca = 0.0f, mt2 = 0.0f, cat = 0.0f;
+    if (KNOWN && m < a.Mp) {
+        m2 = a.consts[m]; ca = a.consts[a.Mp + m];
+        if (TAU) { mt2 = a.consts[2 * a.Mp + m]; cat = a.consts[3 * a.Mp + m]; }
+    }
+    __builtin_amdgcn_s_waitcnt(0);                      // (known to the compiler: it would wait for these loads, and the ring's with them, in the loop)
+    auto issue = [&](int it) __attribute__((always_inline)) {
+        const unsigned s = lds0 + (unsigned)(it % R::STAGES * R::STAGE);
+        R::tile(s, a.W, (t0 + it) * 64, a.V, a.ld, wv);
+        R::dma4(s + R::TILE, reinterpret_cast<const char*>(a.bias + (long long)(t0 + it) * 64), (unsigned)(fresh_lane() * 4));
+    };
+    f32x16_t o[2 * NK];
+#pragma unroll
+    for (int zb = 0; zb < 2 * NK; ++zb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[zb][e] = 0.0f;
+    // (below every logit that is not ruled out)
+    float ref = -LOSS_FAR * LOG2E, sum = 0.0f;
+    const float k = a.k;
+    if (n > 0) issue(0);
+    if (n > 1) issue(1);
+    for (int it = 0; it < n; ++it) {
+        if (it + 1 < n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(NK + 1) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (it + 2 < n) issue(it + 2);                  // (over tile it - 1, which every wavefront is done with)
+        const char* stage = reinterpret_cast<const char*>(smem) + it % R::STAGES * R::STAGE;
+        const float* bias = reinterpret_cast<const float*>(stage + R::TILE);
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+            const char* s = stage + sub * 32 * R::ROWB;
+            f32x16_t u;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float4 b = *reinterpret_cast<const float4*>(bias + sub * 32 + 8 * g + 4 * half);
+                u[4 * g] = b.x; u[4 * g + 1] = b.y; u[4 * g + 2] = b.z; u[4 * g + 3] = b.w;
+            }
+#pragma unroll
+            for (int q = 0; q < 4 * NK; ++q) u = mma32(at.by_row(s, q), zf[q], u);
+            ahead<4 + DEPTH, 4 * NK, 1, 1, DEPTH>();
+            if constexpr (!KNOWN) {
+                float mx = u[0];
+#pragma unroll
+                for (int e = 1; e < 16; ++e) mx = fmaxf(mx, u[e]);
+                if (__any(mx * k > ref + SLACK)) {
+                    const float now = fmaxf(ref, fmaxf(mx, __shfl_xor(mx, 32, 64)) * k), scale = __builtin_amdgcn_exp2f(ref - now);
+                    ref = now;
+                    sum *= scale;
+#pragma unroll
+                    for (int zb = 0; zb < 2 * NK; ++zb)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[zb][e] *= scale;
+                }
+            }
+            uint4 f[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {               // sixteen classes, a step of the second product
+                unsigned p[4];
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    float w[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float x = u[8 * t + e + i];
+                        if constexpr (KNOWN) {
+                            w[i] = ca * __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -m2));
+                            if (TAU) w[i] = fmaf(cat, __builtin_amdgcn_exp2f(fmaf(x, k, -mt2)), w[i]);
+                        } else {
+                            w[i] = __builtin_amdgcn_exp2f(fmaf(x, k, -ref));
+                            sum += w[i];
+                        }
+                    }
+                    p[e / 2] = pack2(w[0], w[1]);
+                }
+                f[t] = fragment(p);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int zb = 0; zb < 2 * NK; ++zb) o[zb] = mma32(at.by_col(s + t * 16 * R::ROWB, zb), f[t], o[zb]);
+            ahead<2 * DEPTH, 4 * NK, 1, 2, DEPTH>();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    if (m >= a.M) return;
+    const long long to = (long long)part * a.M + m;
+#pragma unroll
+    for (int zb = 0; zb < 2 * NK; ++zb)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int z = zb * 32 + 8 * g + 4 * half;
+            if (z < a.ld) *reinterpret_cast<float4*>(a.out + to * a.ld + z) = make_float4(o[zb][4 * g], o[zb][4 * g + 1], o[zb][4 * g + 2], o[zb][4 * g + 3]);
+        }
+    if (!KNOWN) {
+        sum += __shfl_xor(sum, 32, 64);
+        if (half == 0) { a.part_ref[to] = ref; a.part_sum[to] = sum; }
+    }
+}
+
+// ---- classes ----------------------------------------------------------------------------------------------------------------
+template <int NK, bool TAU>
+__global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
+    typedef Ring<NK> R;
+    extern __shared__ uint4 smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
+    const int cg = wv & 3, rh = wv >> 2;                // the wavefront's 32 classes, and its 32 of a tile's 64 rows
+    const int ntv = (a.V + 127) / 128, ct = (int)blockIdx.x % ntv, part = (int)blockIdx.x / ntv;
+    const int ntm = (a.M + 63) / 64, per = (ntm + a.parts - 1) / a.parts, t0 = part * per, n = min(per, ntm - t0);
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
+    const Reads<NK> at(lane);
+    const int class0 = ct * 128 + cg * 32, v = class0 + l32;
+    uint4 wf[4 * NK];
+#pragma unroll
+    for (int q = 0; q < 4 * NK; ++q) {
+        const int c = 2 * q + half;
+        wf[q] = c * 8 < a.ld ? *reinterpret_cast<const uint4*>(a.W + (long long)min(v, a.V - 1) * a.ld + c * 8) : make_uint4(0, 0, 0, 0);
+    }
+    const float b = v < a.V ? a.bias[v] : -INFINITY, k1 = a.k1, b2 = b * k1, bt = b * a.k, k = a.k;
+    __builtin_amdgcn_s_waitcnt(0);                      // (known to the compiler: it would wait for these loads, and the ring's with them, in the loop)
+    auto issue = [&](int it) __attribute__((always_inline)) {
+        const unsigned s = lds0 + (unsigned)(it % R::STAGES * R::STAGE);
+        R::tile(s, a.z, (t0 + it) * 64, a.M, a.ld, wv);
+        // the rows' constants, an array a wavefront
+        R::dma4(s + R::TILE + (unsigned)(wv * 256), reinterpret_cast<const char*>(a.consts + (long long)min(wv, 5) * a.Mp + (long long)(t0 + it) * 64), (unsigned)(fresh_lane() * 4));
+    };
+    f32x16_t o[2 * NK];
+#pragma unroll
+    for (int zb = 0; zb < 2 * NK; ++zb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[zb][e] = 0.0f;
+    float db = 0.0f;
+    if (n > 0) issue(0);
+    if (n > 1) issue(1);
+    for (int it = 0; it < n; ++it) {
+        if (it + 1 < n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(NK + 1) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (it + 2 < n) issue(it + 2);
+        const char* stage = reinterpret_cast<const char*>(smem) + it % R::STAGES * R::STAGE;
+        const char* s = stage + rh * 32 * R::ROWB;
+        const float* consts = reinterpret_cast<const float*>(stage + R::TILE) + rh * 32;   // [6][64]
+        f32x16_t u;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) u[e] = 0.0f;
+#pragma unroll
+        for (int q = 0; q < 4 * NK; ++q) u = mma32(at.by_row(s, q), wf[q], u);
+        ahead<DEPTH, 4 * NK, 1, 1, DEPTH>();
+        __builtin_amdgcn_sched_barrier(0);
+        // a label among these classes: one product of 32 x 32 in V / 1024
+        const int* labels = reinterpret_cast<const int*>(consts + 320);
+        const bool any_hot = __any((unsigned)(labels[fresh_lane() & 31] - class0) < 32u);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {                   // sixteen rows, a step of the second product
+            float d[8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = 8 * (2 * t + h) + 4 * half;
+                const float4 m2 = *reinterpret_cast<const float4*>(consts + r), ca = *reinterpret_cast<const float4*>(consts + 64 + r);
+                const float ms[4] = {m2.x, m2.y, m2.z, m2.w}, cs[4] = {ca.x, ca.y, ca.z, ca.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) d[4 * h + i] = cs[i] * __builtin_amdgcn_exp2f(fmaf(u[8 * t + 4 * h + i], k1, b2 - ms[i]));
+                if (TAU) {
+                    const float4 mt = *reinterpret_cast<const float4*>(consts + 128 + r), ct_ = *reinterpret_cast<const float4*>(consts + 192 + r);
+                    const float mts[4] = {mt.x, mt.y, mt.z, mt.w}, cts[4] = {ct_.x, ct_.y, ct_.z, ct_.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) d[4 * h + i] = fmaf(cts[i], __builtin_amdgcn_exp2f(fmaf(u[8 * t + 4 * h + i], k, bt - mts[i])), d[4 * h + i]);
+                }
+            }
+            if (any_hot) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int r = 8 * (2 * t + (e >> 2)) + 4 * half + (e & 3);
+                    if (labels[r] == class0 + (fresh_lane() & 31)) d[e] -= consts[256 + r];
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) db += d[e];
+            auto split = [&] {                          // d rounded, as the operand; d: what the rounding left
+                unsigned p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[e] = pack2(d[2 * e], d[2 * e + 1]);
+                    d[2 * e] -= __builtin_bit_cast(float, p[e] << 16);
+                    d[2 * e + 1] -= __builtin_bit_cast(float, p[e] & 0xFFFF0000u);
+                }
+                return fragment(p);
+            };
+            const uint4 hi = split(), lo = split();
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int zb = 0; zb < 2 * NK; ++zb) {
+                const uint4 x = at.by_col(s + t * 16 * R::ROWB, zb);
+                o[zb] = mma32(x, hi, o[zb]);
+                o[zb] = mma32(x, lo, o[zb]);
+            }
+            ahead<2 * 2, 2 * NK, 2, 2, 2>();
+            __builtin_amdgcn_sched_barrier(0);
+            if (any_hot) {                              // (where du is large: a third part of it)
+                const uint4 rest = split();
+#pragma unroll
+                for (int zb = 0; zb < 2 * NK; ++zb) o[zb] = mma32(at.by_col(s + t * 16 * R::ROWB, zb), rest, o[zb]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    const int ln = fresh_lane(), n32 = ln & 31, hf = ln >> 5, cls = ct * 128 + cg * 32 + n32;
+    // the two halves of the rows together, through LDS; register e of a lane: column 32 zb + 8 (e / 4) + 4 half + e % 4 of class l32
+    db += __shfl_xor(db, 32, 64);
+    float* sh = reinterpret_cast<float*>(smem);         // [4][16][64] a block of 32 columns, then [4][32]
+    float* out = a.out + (long long)part * a.V * a.ldo;
+    float* out_db = a.out_db + (long long)part * a.V;
+    __syncthreads();
+    if (rh == 1) {
+#pragma unroll
+        for (int zb = 0; zb < 2 * NK; ++zb)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) *reinterpret_cast<float4*>(sh + (((cg * 2 * NK + zb) * 4 + g) * 64 + ln) * 4) = make_float4(o[zb][4 * g], o[zb][4 * g + 1], o[zb][4 * g + 2], o[zb][4 * g + 3]);
+        if (hf == 0) sh[32768 + cg * 32 + n32] = db;
+    }
+    __syncthreads();
+    if (rh == 1 || cls >= a.V) return;
+    if (hf == 0) out_db[cls] = db + sh[32768 + cg * 32 + n32];
+#pragma unroll
+    for (int zb = 0; zb < 2 * NK; ++zb)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float4 x = *reinterpret_cast<const float4*>(sh + (((cg * 2 * NK + zb) * 4 + g) * 64 + ln) * 4);
+            const float y[4] = {o[zb][4 * g] + x.x, o[zb][4 * g + 1] + x.y, o[zb][4 * g + 2] + x.z, o[zb][4 * g + 3] + x.w};
+            const int z = zb * 32 + 8 * g + 4 * hf;
+            if (a.vec && z + 4 <= a.Z) *reinterpret_cast<float4*>(out + (long long)cls * a.ldo + z) = make_float4(y[0], y[1], y[2], y[3]);
+            else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) if (z + i < a.Z) out[(long long)cls * a.ldo + z + i] = y[i];
+            }
+        }
+}
+
+// The parts of dW_s and db_s in order.
+__global__ __launch_bounds__(256) void loss_classes_sum_kernel(const float* __restrict__ p, const float* __restrict__ pb, int parts, long long n, int V, float* __restrict__ out, float* __restrict__ out_b) {
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n + V; i += (long long)gridDim.x * 256) {
+        const bool w = i < n;
+        const float* x = w ? p + i : pb + (i - n);
+        const long long step = w ? n : V;
+        float s = x[0];
+#pragma unroll 4
+        for (int k = 1; k < parts; ++k) s += x[k * step];
+        if (w) out[i] = s; else out_b[i - n] = s;
+    }
+}
+
+// ---- behind the rows: a wavefront a row, four columns a lane -----------------------------------------------------------------
+// KNOWN: the rows' constants and losses are there and the parts are sums of du W; else they are made here from the parts' references
+// and sums, which are brought to the largest reference.
+template <bool KNOWN, bool POLICY>
+__global__ __launch_bounds__(256) void loss_dz_kernel(LossDzArgs a, PolicyArgs policy, TeacherArgs teacher) {
+    const int lane = threadIdx.x & 63;
+    const long long m = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (m >= a.M) {                                      // the last tile's rows that are none
+        if (m < a.Mp && lane < 6) a.consts[lane * (long long)a.Mp + m] = lane == 0 || lane == 2 ? INFINITY : lane == 5 ? __builtin_bit_cast(float, -1) : 0.0f;
+        return;
+    }
+    float m2 = 0.0f, c1 = 1.0f, hot = 0.0f;
+    int lab = a.labels ? a.labels[m] : -1;
+    bool some = false;                                   // entries of the teacher's that count
+    if (KNOWN) {
+        hot = a.consts[4 * (long long)a.Mp + m];
+        some = a.soft_state[m] & 1;
+    } else {
+        float ref = -INFINITY;
+        for (int p = lane; p < a.parts; p += 64) ref = fmaxf(ref, a.part_ref[(long long)p * a.M + m]);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor(ref, o, 64));
+        float sum = 0.0f;
+        for (int p = lane; p < a.parts; p += 64) sum += a.part_sum[(long long)p * a.M + m] * __builtin_amdgcn_exp2f(a.part_ref[(long long)p * a.M + m] - ref);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+        m2 = ref;
+        const bool lab_ok = (unsigned)lab < (unsigned)a.V;
+        const float nan = __builtin_nanf(""), log_sum = logf(sum);
+        const float lp = lab_ok ? fmaf(a.label_logit[m], LOG2E, -ref) * LN2 - log_sum : lab == -1 ? 0.0f : nan;
+        float loss = 0.0f;
+        c1 = 0.0f;
+        if (POLICY) {
+            if (lab_ok) {
+                const PolicyTerms t = policy_terms(policy, m, lp);
+                loss = a.s * t.loss; c1 = -a.s * t.g / sum; hot = -a.s * t.g;
+            } else if (lab != -1) loss = nan;
+            if (a.logp && lane == 0) a.logp[m] = lp;
+        } else {
+            const int state = a.soft_state[m];
+            some = state & 1;
+            if (lab_ok) { loss = a.s * teacher.hard * -lp; c1 = a.s * teacher.hard / sum; hot = a.s * teacher.hard; }
+            else if (lab != -1) loss = nan;
+            if (some) {
+                loss += a.s * teacher.soft * teacher.tau * teacher.tau * (a.soft_const[m] + (ref * LN2 + log_sum));
+                c1 += a.s * teacher.soft * teacher.tau / sum;
+            }
+            if (state & 2) loss = nan;
+        }
+        const bool counts = lab_ok || some;
+        if (!lab_ok) lab = -1;
+        if (lane < 6)
+            a.consts[lane * (long long)a.Mp + m] = lane == 0 ? (counts ? m2 : INFINITY) : lane == 1 ? c1 : lane == 2 ? INFINITY : lane == 3 ? 0.0f : lane == 4 ? hot : __builtin_bit_cast(float, lab);
+        if (lane == 0) a.row_loss[m] = loss;
+    }
+    const bool counts = KNOWN ? true : ((unsigned)lab < (unsigned)a.V || some);
+    const int z0 = lane * 4;
+    if (z0 >= a.ld) return;
+    float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (counts) {
+        for (int p = 0; p < a.parts; ++p) {
+            const long long at = (long long)p * a.M + m;
+            const float4 v = *reinterpret_cast<const float4*>(a.part + at * a.ld + z0);
+            const float w = KNOWN ? 1.0f : __builtin_amdgcn_exp2f(a.part_ref[at] - m2);
+            x[0] = fmaf(v.x, w, x[0]); x[1] = fmaf(v.y, w, x[1]); x[2] = fmaf(v.z, w, x[2]); x[3] = fmaf(v.w, w, x[3]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] *= c1;
+        auto add = [&](int c, float w) {                 // w W_c
+            const uint2 b = *reinterpret_cast<const uint2*>(a.W + (long long)c * a.ld + z0);
+            x[0] = fmaf(w, bf2f((bf16_t)(b.x & 0xFFFFu)), x[0]); x[1] = fmaf(w, bf2f((bf16_t)(b.x >> 16)), x[1]);
+            x[2] = fmaf(w, bf2f((bf16_t)(b.y & 0xFFFFu)), x[2]); x[3] = fmaf(w, bf2f((bf16_t)(b.y >> 16)), x[3]);
+        };
+        if (hot != 0.0f && (unsigned)lab < (unsigned)a.V) add(lab, -hot);
+        if (!POLICY && some) {
+            const float weight = a.s * teacher.soft * teacher.tau;
+            for (int k = 0; k < teacher.K; ++k) {
+                const float q = a.entry_q[m * teacher.K + k];
+                if (q > 0.0f) add(teacher.classes[m * teacher.K + k], -weight * q);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) if (z0 + i < a.Z) a.dz[m * a.Z + z0 + i] = f2bf(x[i]);
+}
+
+template <int NK, bool KNOWN, bool TAU>
+hipError_t rows_nk(const LossFusedArgs& a, hipStream_t st) {
+    constexpr size_t lds = (size_t)Ring<NK>::STAGES * Ring<NK>::STAGE;
+    static thread_local bool attr_set = false;
+    const hipError_t e = allow_lds(&loss_rows_kernel<NK, KNOWN, TAU>, lds, &attr_set);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((loss_rows_kernel<NK, KNOWN, TAU>), dim3((unsigned)((a.M + 255) / 256 * a.parts)), dim3(512), lds, st, a);
+    return hipGetLastError();
+}
+template <int NK, bool TAU>
+hipError_t classes_nk(const LossFusedArgs& a, hipStream_t st) {
+    constexpr size_t ring = (size_t)Ring<NK>::STAGES * Ring<NK>::STAGE, join = 32768 * 4 + 512, lds = ring > join ? ring : join;
+    static thread_local bool attr_set = false;
+    const hipError_t e = allow_lds(&loss_classes_kernel<NK, TAU>, lds, &attr_set);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((loss_classes_kernel<NK, TAU>), dim3((unsigned)((a.V + 127) / 128 * a.parts)), dim3(512), lds, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_loss_fused_rows(const LossFusedArgs& a, bool known, bool tau, hipStream_t st) {
+    const int nk = (a.ld + 63) / 64;
+#define BLSTM_ROWS(NK) return known ? (tau ? rows_nk<NK, true, true>(a, st) : rows_nk<NK, true, false>(a, st)) : rows_nk<NK, false, false>(a, st)
+    if (nk == 1) BLSTM_ROWS(1);
+    if (nk == 2) BLSTM_ROWS(2);
+    if (nk == 3) BLSTM_ROWS(3);
+    BLSTM_ROWS(4);
+#undef BLSTM_ROWS
+}
+hipError_t launch_loss_fused_classes(const LossFusedArgs& a, bool tau, hipStream_t st) {
+    const int nk = (a.ld + 63) / 64;
+#define BLSTM_CLASSES(NK) return tau ? classes_nk<NK, true>(a, st) : classes_nk<NK, false>(a, st)
+    if (nk == 1) BLSTM_CLASSES(1);
+    if (nk == 2) BLSTM_CLASSES(2);
+    if (nk == 3) BLSTM_CLASSES(3);
+    BLSTM_CLASSES(4);
+#undef BLSTM_CLASSES
+}
+hipError_t launch_loss_dz(const LossDzArgs& a, bool known, hipStream_t st) {
+    const dim3 grid((unsigned)(a.Mp / 4));
+    const PolicyArgs p = a.policy ? *a.policy : PolicyArgs{};
+    const TeacherArgs t = a.teacher ? *a.teacher : TeacherArgs{};
+    if (a.policy) hipLaunchKernelGGL((loss_dz_kernel<false, true>), grid, dim3(256), 0, st, a, p, t);
+    else if (known) hipLaunchKernelGGL((loss_dz_kernel<true, false>), grid, dim3(256), 0, st, a, p, t);
+    else hipLaunchKernelGGL((loss_dz_kernel<false, false>), grid, dim3(256), 0, st, a, p, t);
+    return hipGetLastError();
+}
+hipError_t launch_loss_classes_sum(const float* p, const float* pb, int parts, long long n, int V, float* out, float* out_b, hipStream_t st) {
+    const long long blocks = (n + V + 255) / 256;
+    hipLaunchKernelGGL(loss_classes_sum_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, p, pb, parts, n, V, out, out_b);
+    return hipGetLastError();
+}
+
+}  // namespace blstm

@@ -6,12 +6,10 @@
 //   distill: l = h (-log p_y) + w tau^2 sum_k q_k (log q_k - log p'_k), p' = softmax(u / tau)
 //            dl/du = h (p - 1_y) + w tau (p' - sum_k q_k 1_k)
 #include "common.hpp"
-#include "losses.hpp"
+#include "losses_terms.hpp"
 
 namespace blstm {
 namespace {
-
-constexpr float LOG2E = 1.44269504f, LN2 = 0.693147181f;
 
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
@@ -78,30 +76,19 @@ __device__ __forceinline__ float class_weight(const ListLds& s, int K, int k) {
     return w;
 }
 
-struct PolicyTerms { float loss, g; };
-__device__ __forceinline__ PolicyTerms policy_terms(const PolicyArgs& p, long long m, float lp) {
-    const float A = p.advantage[m];
-    float loss = 0.0f, g = 0.0f;
-    if (A != 0.0f) {                                     // (an infinite ratio times an advantage of zero is no number)
-        const float r = p.old_logp ? expf(lp - p.old_logp[m]) : 1.0f;
-        const float inner = r * A, outer = fminf(fmaxf(r, 1.0f - p.clip_low), 1.0f + p.clip_high) * A;
-        loss = inner > outer ? -outer : -inner;          // (a NaN ratio stays one)
-        const bool cut = (A > 0.0f && r > 1.0f + p.clip_high) || (A < 0.0f && r < 1.0f - p.clip_low);
-        g = cut ? 0.0f : -inner;
-    }
-    if (p.ref_logp) {
-        const float d = p.ref_logp[m] - lp, e = expm1f(d);
-        loss += p.kl_weight * (e - d);
-        g -= p.kl_weight * e;
-    }
-    return {loss, g};
-}
-
 // ---- ahead of the products: a wavefront a row -----------------------------------------------------------------------
 template <typename T>
 __global__ __launch_bounds__(256) void loss_prep_kernel(LossPrepArgs a) {
     __shared__ ListLds lists[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if constexpr (sizeof(T) == 2) {
+        const int first = (a.M + 3) / 4;                 // workgroups behind the rows': the bias
+        if ((int)blockIdx.x >= first) {
+            const int v = ((int)blockIdx.x - first) * 256 + (int)threadIdx.x;
+            if (v < ((a.V + 63) & ~63)) a.bias_f[v] = v < a.V ? bf2f(a.bias[v]) : -INFINITY;
+            return;
+        }
+    }
     const long long m = (long long)blockIdx.x * 4 + wave;
     if (m >= a.M) return;
     ListLds& s = lists[wave];
@@ -453,7 +440,7 @@ __global__ __launch_bounds__(512) void row_topk_kernel(const float* u, long long
 }  // namespace
 
 hipError_t launch_loss_prep(const LossPrepArgs& a, DType type, hipStream_t st) {
-    const dim3 grid((unsigned)((a.M + 3) / 4));
+    const dim3 grid((unsigned)((a.M + 3) / 4 + (a.bias_f ? (a.V + 255) / 256 : 0)));
     if (type == DT_BF16) hipLaunchKernelGGL(loss_prep_kernel<bf16_t>, grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL(loss_prep_kernel<float>, grid, dim3(256), 0, st, a);
     return hipGetLastError();
