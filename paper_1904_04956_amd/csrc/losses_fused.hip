@@ -7,9 +7,8 @@
 //             dW_s = du^T z and db_s.  du goes into the product as the sum of two bf16 numbers (of three where a label is).
 //
 // Both read a tile [64][Z] in LDS twice: by rows for the logits (ds_read_b128) and by columns for what is made of them
-// (ds_read_b64_tr_b16 transposes on the way).  16-byte chunk c of row r lies at chunk c ^ sw(r): of the 256 bytes that LDS
-// delivers a clock, sixteen rows' chunk in the first and four rows' 64 bytes in the second, all are on different banks (spread over
-// 128 bytes, with two accesses a bank, 43008 frames of 32000 classes took 1135 us in the rows kernel, 1625 in the classes kernel; now XX, YY).  The output of the first product (lane: row or
+// (ds_read_b64_tr_b16 transposes on the way).  16-byte chunk c of row r lies at chunk c ^ sw(r): the eight rows that a phase
+// of the first reads, and the four of the second, are on different banks.  The output of the first product (lane: row or
 // class, registers: the other) is the operand of the second after one exchange between the lane halves.
 #include "gemm_tile.hpp"
 #include "losses_terms.hpp"
@@ -19,8 +18,7 @@ namespace {
 
 constexpr float SLACK = 8.0f;                           // powers of two by which a weight may pass one before the reference moves
 
-// (rows of an odd number of 128 bytes are by themselves on alternating halves of the banks)
-template <int NK> __device__ __forceinline__ int sw(int r) { return NK % 2 == 0 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3); }
+__device__ __forceinline__ int sw(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
 
 // The lane's number, made anew: kept across a loop, or what follows from it ahead of one, it would take registers that there are not.
 __device__ __forceinline__ int fresh_lane() {
@@ -47,60 +45,30 @@ struct Ring {
 #pragma unroll
         for (int j = 0; j < NK; ++j) {
             const unsigned i = (unsigned)(j * 8 + wv) * 64u + lane, x = i % CPR;
-            const int r = (int)(i / CPR), c = (int)x ^ sw<NK>(r);
+            const int r = (int)(i / CPR), c = (int)(x & ~7u) | ((int)(x & 7u) ^ sw(r));
             dma16(lds + (unsigned)((j * 8 + wv) * 1024), base, (unsigned)(__mul24(min(r, last), ld * 2) + min(c, lastc) * 16));
         }
     }
 };
 
-// A lane's reads of a tile.  G: chunks that sw mixes.  By rows: chunk 2 q + half of row l32 is at row ^ 32 (q % (G / 2)), 16 G bytes on for
-// every G / 2.  By columns: of sixteen rows, columns 32 zb .., the first four of each eight at col ^ 64 (zb % (G / 4)), the other
-// four 4 rows and chunk ^ 1 on.
+// A lane's reads of a tile.  By rows: chunk 2 q + half of row l32 is at row ^ 32 (q % 4), 128 (q / 4) on.  By columns: of sixteen rows,
+// columns 32 zb .., the first four of each eight at col ^ 64 (zb % 2), 128 (zb / 2) on, the other four 4 rows and chunk ^ 1 on.
 template <int NK>
 struct Reads {
-    static constexpr int G = NK % 2 == 0 ? 16 : 8;
-    unsigned row, col;                                  // in the ring's first stage; every stage is a whole number of 256 bytes on
-    __device__ __forceinline__ Reads(unsigned lds0, int lane) {
+    int row, col;
+    __device__ __forceinline__ Reads(int lane) {
         const int l32 = lane & 31, half = lane >> 5, li = lane & 15, g = lane >> 4;
-        row = lds0 + l32 * Ring<NK>::ROWB + ((half ^ sw<NK>(l32)) << 4);
-        const int r = 8 * half + (li >> 2);
-        col = lds0 + r * Ring<NK>::ROWB + (((2 * (g & 1) + ((li & 3) >> 1)) ^ sw<NK>(r)) << 4) + (li & 1) * 8;
+        row = l32 * Ring<NK>::ROWB + ((half ^ sw(l32)) << 4);
+        const int r = 8 * half + (li >> 2), x = (2 * (g & 1) + ((li & 3) >> 1)) ^ ((li >> 2) << 1);
+        col = r * Ring<NK>::ROWB + (x << 4) + (li & 1) * 8;
     }
-    // (made anew where it is used: kept, these addresses take more registers than there are)
-    template <int X>
-    static __device__ __forceinline__ unsigned flip(unsigned a) {
-        unsigned b;
-        if constexpr (X == 0) return a;
-        asm volatile("v_xor_b32 %0, %2, %1" : "=v"(b) : "v"(a), "i"(X));
-        return b;
-    }
-    typedef __attribute__((address_space(3))) const u32x4_t* lds_u4;
-    typedef __attribute__((address_space(3))) const f32x4_t* lds_f4;
-    // f(operand, q) of every chunk of a row, f(operand, step, zb) of every block of columns of STEPS times sixteen rows: those with
-    // an address in common together.  AT: bytes beyond `from`.
-    template <int AT, typename F>
-    static __device__ __forceinline__ void by_row(unsigned from, F&& f) {
-        each<0, (4 * NK < G / 2 ? 4 * NK : G / 2)>([&](auto x) {
-            const unsigned at = flip<(decltype(x)::value << 5)>(from);
-            each<0, (4 * NK + G / 2 - 1) / (G / 2)>([&](auto y) {
-                const u32x4_t v = *(lds_u4)(uintptr_t)(at + (unsigned)(AT + 16 * G * decltype(y)::value));
-                f(make_uint4(v[0], v[1], v[2], v[3]), std::integral_constant<int, decltype(x)::value + decltype(y)::value * (G / 2)>{});
-            });
-        });
-    }
-    template <int AT, int STEPS, typename F>
-    static __device__ __forceinline__ void by_col(unsigned from, F&& f) {
-        each<0, (2 * NK < G / 4 ? 2 * NK : G / 4)>([&](auto x) {
-            const unsigned at = flip<(decltype(x)::value << 6)>(from), at4 = flip<(decltype(x)::value << 6) ^ 16>(from);
-            each<0, STEPS>([&](auto t) {
-                each<0, 2 * NK / (G / 4)>([&](auto y) {
-                    constexpr unsigned on = AT + decltype(t)::value * 16 * Ring<NK>::ROWB + 16 * G * decltype(y)::value;
-                    const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(uintptr_t)(at + on)));
-                    const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(uintptr_t)(at4 + on + 4 * Ring<NK>::ROWB)));
-                    f(make_uint4(lo.x, lo.y, hi.x, hi.y), t, std::integral_constant<int, decltype(x)::value + decltype(y)::value * (G / 4)>{});
-                });
-            });
-        });
+    __device__ __forceinline__ uint4 by_row(const char* s, int q) const { return *reinterpret_cast<const uint4*>(s + (row ^ ((q & 3) << 5)) + 128 * (q >> 2)); }
+    __device__ __forceinline__ uint4 by_col(const char* s, int zb) const {
+        const char* p = s + (col ^ ((zb & 1) << 6)) + 128 * (zb >> 1);
+        const char* p4 = s + (col ^ ((zb & 1) << 6) ^ 16) + 128 * (zb >> 1) + 4 * Ring<NK>::ROWB;
+        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)p));
+        const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)p4));
+        return make_uint4(lo.x, lo.y, hi.x, hi.y);
     }
 };
 
@@ -134,7 +102,7 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
     const int part = (int)blockIdx.x % a.parts, row0 = (int)blockIdx.x / a.parts * 256;
     const int ntv = (a.V + 63) / 64, per = (ntv + a.parts - 1) / a.parts, t0 = part * per, n = min(per, ntv - t0);
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
-    const Reads<NK> at(lds0, lane);
+    const Reads<NK> at(lane);
     const int m = row0 + wv * 32 + l32;
     uint4 zf[4 * NK];
 #pragma unroll
@@ -167,16 +135,19 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
         if (it + 1 < n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(NK + 1) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (it + 2 < n) issue(it + 2);                  // (over tile it - 1, which every wavefront is done with)
-        const unsigned stage = (unsigned)(it % R::STAGES * R::STAGE), rows = at.row + stage, cols = at.col + stage, bias = lds0 + stage + 16 * half;
-        each<0, 2>([&](auto sub_) __attribute__((always_inline)) {
-            constexpr int sub = decltype(sub_)::value, S = sub * 32 * R::ROWB;
+        const char* stage = reinterpret_cast<const char*>(smem) + it % R::STAGES * R::STAGE;
+        const float* bias = reinterpret_cast<const float*>(stage + R::TILE);
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+            const char* s = stage + sub * 32 * R::ROWB;
             f32x16_t u;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const f32x4_t b = *(typename Reads<NK>::lds_f4)(uintptr_t)(bias + (unsigned)(R::TILE + sub * 128 + 32 * g));
-                u[4 * g] = b[0]; u[4 * g + 1] = b[1]; u[4 * g + 2] = b[2]; u[4 * g + 3] = b[3];
+                const float4 b = *reinterpret_cast<const float4*>(bias + sub * 32 + 8 * g + 4 * half);
+                u[4 * g] = b.x; u[4 * g + 1] = b.y; u[4 * g + 2] = b.z; u[4 * g + 3] = b.w;
             }
-            at.template by_row<S>(rows, [&](const uint4& x, auto q) { u = mma32(x, zf[q], u); });
+#pragma unroll
+            for (int q = 0; q < 4 * NK; ++q) u = mma32(at.by_row(s, q), zf[q], u);
             ahead<4 + DEPTH, 4 * NK, 1, 1, DEPTH>();
             if constexpr (!KNOWN) {
                 float mx = u[0];
@@ -215,10 +186,13 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
                 f[t] = fragment(p);
             }
             __builtin_amdgcn_sched_barrier(0);
-            at.template by_col<S, 2>(cols, [&](const uint4& x, auto t, auto zb) { o[zb] = mma32(x, f[t], o[zb]); });
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int zb = 0; zb < 2 * NK; ++zb) o[zb] = mma32(at.by_col(s + t * 16 * R::ROWB, zb), f[t], o[zb]);
             ahead<2 * DEPTH, 4 * NK, 1, 2, DEPTH>();
             __builtin_amdgcn_sched_barrier(0);
-        });
+        }
     }
     if (m >= a.M) return;
     const long long to = (long long)part * a.M + m;
@@ -245,7 +219,7 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
     const int ntv = (a.V + 127) / 128, ct = (int)blockIdx.x % ntv, part = (int)blockIdx.x / ntv;
     const int ntm = (a.M + 63) / 64, per = (ntm + a.parts - 1) / a.parts, t0 = part * per, n = min(per, ntm - t0);
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
-    const Reads<NK> at(lds0, lane);
+    const Reads<NK> at(lane);
     const int class0 = ct * 128 + cg * 32, v = class0 + l32;
     uint4 wf[4 * NK];
 #pragma unroll
@@ -274,19 +248,20 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (it + 2 < n) issue(it + 2);
         const char* stage = reinterpret_cast<const char*>(smem) + it % R::STAGES * R::STAGE;
-        const unsigned from = (unsigned)(it % R::STAGES * R::STAGE + rh * 32 * R::ROWB), rows = at.row + from, cols = at.col + from;
+        const char* s = stage + rh * 32 * R::ROWB;
         const float* consts = reinterpret_cast<const float*>(stage + R::TILE) + rh * 32;   // [6][64]
         f32x16_t u;
 #pragma unroll
         for (int e = 0; e < 16; ++e) u[e] = 0.0f;
-        at.template by_row<0>(rows, [&](const uint4& x, auto q) { u = mma32(x, wf[q], u); });
+#pragma unroll
+        for (int q = 0; q < 4 * NK; ++q) u = mma32(at.by_row(s, q), wf[q], u);
         ahead<DEPTH, 4 * NK, 1, 1, DEPTH>();
         __builtin_amdgcn_sched_barrier(0);
         // a label among these classes: one product of 32 x 32 in V / 1024
         const int* labels = reinterpret_cast<const int*>(consts + 320);
         const bool any_hot = __any((unsigned)(labels[fresh_lane() & 31] - class0) < 32u);
-        each<0, 2>([&](auto t_) __attribute__((always_inline)) {   // sixteen rows, a step of the second product
-            constexpr int t = decltype(t_)::value;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {                   // sixteen rows, a step of the second product
             float d[8];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -323,18 +298,21 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
             };
             const uint4 hi = split(), lo = split();
             __builtin_amdgcn_sched_barrier(0);
-            at.template by_col<t * 16 * R::ROWB, 1>(cols, [&](const uint4& x, auto, auto zb) {
+#pragma unroll
+            for (int zb = 0; zb < 2 * NK; ++zb) {
+                const uint4 x = at.by_col(s + t * 16 * R::ROWB, zb);
                 o[zb] = mma32(x, hi, o[zb]);
                 o[zb] = mma32(x, lo, o[zb]);
-            });
+            }
             ahead<2 * 2, 2 * NK, 2, 2, 2>();
             __builtin_amdgcn_sched_barrier(0);
             if (any_hot) {                              // (where du is large: a third part of it)
                 const uint4 rest = split();
-                at.template by_col<t * 16 * R::ROWB, 1>(cols, [&](const uint4& x, auto, auto zb) { o[zb] = mma32(x, rest, o[zb]); });
+#pragma unroll
+                for (int zb = 0; zb < 2 * NK; ++zb) o[zb] = mma32(at.by_col(s + t * 16 * R::ROWB, zb), rest, o[zb]);
             }
             __builtin_amdgcn_sched_barrier(0);
-        });
+        }
     }
     const int ln = fresh_lane(), n32 = ln & 31, hf = ln >> 5, cls = ct * 128 + cg * 32 + n32;
     // the two halves of the rows together, through LDS; register e of a lane: column 32 zb + 8 (e / 4) + 4 half + e % 4 of class l32
