@@ -410,6 +410,7 @@ struct LossScratch {
     bool copy_w, compact;     // W_s is copied; dz and dW_s are compacted
     long long ldu;            // row distance of the logits / of dE/du
     int chunk;                // rows whose logits are held at a time (calls without gradients)
+    bool strips;              // largest logits: by the strips' maxima
     bool fused;               // the kernels of losses_fused.hip: no du in memory
     int row_parts, class_parts;
     size_t bias_f, consts, part, part_ref, part_sum, cparts, cparts_b;
@@ -484,6 +485,8 @@ LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
         }
     } else {
         put(&l.u, (gradient ? M : (size_t)l.chunk) * per_row);
+        l.strips = call == SOFTMAX_TOPK && c->V <= LOSS_TOP_STRIPS * LOSS_STRIP;
+        if (l.strips) put(&l.pmax, (size_t)loss_strips(c->V) * l.chunk * 4);
     }
     size_t need = 0;
     auto upd = [&](size_t b) { if (b > need) need = b; };
@@ -1116,9 +1119,22 @@ int softmax_topk(blstm_ctx* ctx, const void* theta, const void* z, int K, float*
     }
     for (int m = 0; m < ctx->M; m += l.chunk) {
         const int n = ctx->M - m < l.chunk ? ctx->M - m : l.chunk;
-        rc = loss_logits(ctx, c, m, n, c.at<float>(l.u));
+        float* u = c.at<float>(l.u);
+        float* v = values + (size_t)m * K;
+        int32_t* cls = classes + (size_t)m * K;
+        if (l.strips && ctx->st == DT_BF16) {            // (the maxima come with the logits)
+            LossTileArgs t{};
+            t.z = static_cast<const unsigned short*>(c.zc) + (size_t)m * l.Zp; t.W = static_cast<const unsigned short*>(c.W); t.bias = static_cast<const unsigned short*>(c.b);
+            t.M = n; t.V = ctx->V; t.ld = l.Zp;
+            t.part_max = c.at<float>(l.pmax); t.logits = u; t.ldu = l.ldu;
+            RUN(PC_GEMM_LOGITS, "logits", launch_loss_logits(t, st));
+            RUN(PC_SOFTMAX_ROWS, "largest logits", launch_row_topk(u, l.ldu, n, ctx->V, K, t.part_max, true, v, cls, st));
+            continue;
+        }
+        rc = loss_logits(ctx, c, m, n, u);
         if (rc != BLSTM_OK) return rc;
-        RUN(PC_SOFTMAX_ROWS, "largest logits", launch_row_topk(c.at<float>(l.u), l.ldu, n, ctx->V, K, values + (size_t)m * K, classes + (size_t)m * K, st));
+        if (l.strips) RUN(PC_SOFTMAX_ROWS, "largest logits", launch_row_topk(u, l.ldu, n, ctx->V, K, c.at<float>(l.pmax), false, v, cls, st));
+        else RUN(PC_SOFTMAX_ROWS, "largest logits", launch_row_topk_wide(u, l.ldu, n, ctx->V, K, v, cls, st));
     }
     return BLSTM_OK;
 }

@@ -12,7 +12,10 @@
 namespace blstm {
 namespace {
 
-template <bool TAU, bool GRAD>
+// What becomes of the logits: the strips' maxima and sums, du, or the logits themselves in float with the strips' maxima.
+enum { SUMS, GRAD, LOGITS };
+
+template <bool TAU, int WHAT>
 __global__ __launch_bounds__(256, 2) void loss_tile_kernel(LossTileArgs a, int ntm, int ntv) {
     constexpr int SLAB = 128 * CHUNKS, BK = 64;
     extern __shared__ uint4 smem[];                     // [2][classes' slab, rows' slab], then the classes' bias
@@ -25,7 +28,7 @@ __global__ __launch_bounds__(256, 2) void loss_tile_kernel(LossTileArgs a, int n
     if (lin < nt8) lin = (lin & 7) * (nt8 >> 3) + (lin >> 3);
     const int col0 = lin / ntm * 128, row0 = lin % ntm * 128;
     // classes beyond the last one: their products repeat its weights, and the bias makes nothing of them
-    if (tid < 128) bias_s[tid] = col0 + tid < a.V ? bf2f(a.bias[col0 + tid]) : -INFINITY;
+    if (tid < 128) bias_s[tid] = col0 + tid < a.V ? bf2f(a.bias[col0 + tid]) : WHAT == LOGITS ? __builtin_nanf("") : -INFINITY;   // (NaN is not a maximum)
 
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
     const int nslab = (a.ld + BK - 1) / BK;
@@ -96,7 +99,24 @@ __global__ __launch_bounds__(256, 2) void loss_tile_kernel(LossTileArgs a, int n
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int m = row0 + wm * 64 + i * 32 + l32;
-        if constexpr (!GRAD) {
+        if constexpr (WHAT == LOGITS) {
+            float mx = acc[0][i][0];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, acc[j][i][e]);
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            if (m < a.M) {
+                if (half == 0) a.part_max[(long long)(col0 / 64 + wn) * a.M + m] = mx;
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const int n = col0 + wn * 64 + j * 32 + 8 * g + 4 * half;
+                        if (n < a.ldu) *reinterpret_cast<float4*>(a.logits + m * a.ldu + n) = make_float4(acc[j][i][4 * g], acc[j][i][4 * g + 1], acc[j][i][4 * g + 2], acc[j][i][4 * g + 3]);
+                    }
+            }
+        } else if constexpr (WHAT == SUMS) {
             float mx = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 2; ++j)
@@ -174,24 +194,25 @@ __global__ __launch_bounds__(256, 2) void loss_tile_kernel(LossTileArgs a, int n
     }
 }
 
-template <bool TAU, bool GRAD>
+template <bool TAU, int WHAT>
 hipError_t launch_tile(const LossTileArgs& a, hipStream_t st) {
     constexpr size_t lds = 4 * 128 * CHUNKS * 16 + 128 * sizeof(float);
     static thread_local bool attr_set = false;
-    const hipError_t e = allow_lds(&loss_tile_kernel<TAU, GRAD>, lds, &attr_set);
+    const hipError_t e = allow_lds(&loss_tile_kernel<TAU, WHAT>, lds, &attr_set);
     if (e != hipSuccess) return e;
     const int ntm = (a.M + 127) / 128, ntv = (a.V + 127) / 128;
-    hipLaunchKernelGGL((loss_tile_kernel<TAU, GRAD>), dim3((unsigned)(ntm * ntv)), dim3(256), lds, st, a, ntm, ntv);
+    hipLaunchKernelGGL((loss_tile_kernel<TAU, WHAT>), dim3((unsigned)(ntm * ntv)), dim3(256), lds, st, a, ntm, ntv);
     return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_loss_stats(const LossTileArgs& a, hipStream_t st) {
-    return a.inv_tau != 0.0f ? launch_tile<true, false>(a, st) : launch_tile<false, false>(a, st);
+    return a.inv_tau != 0.0f ? launch_tile<true, SUMS>(a, st) : launch_tile<false, SUMS>(a, st);
 }
 hipError_t launch_loss_grad(const LossTileArgs& a, hipStream_t st) {
-    return a.inv_tau != 0.0f ? launch_tile<true, true>(a, st) : launch_tile<false, true>(a, st);
+    return a.inv_tau != 0.0f ? launch_tile<true, GRAD>(a, st) : launch_tile<false, GRAD>(a, st);
 }
+hipError_t launch_loss_logits(const LossTileArgs& a, hipStream_t st) { return launch_tile<false, LOGITS>(a, st); }
 
 }  // namespace blstm

@@ -74,10 +74,12 @@ struct LossTileArgs {
     unsigned short* hi;                              // [M][ldu] du rounded to bf16, zeros in columns V .. ldu - 1
     unsigned short* lo;                              // [M][ldu] what the rounding left, rounded
     long long ldu;
+    float* logits;                                   // [M][ldu]
 };
 inline int loss_strips(int V) { return (V + 2 * LOSS_STRIP - 1) / (2 * LOSS_STRIP) * 2; }
 hipError_t launch_loss_stats(const LossTileArgs& a, hipStream_t st);
 hipError_t launch_loss_grad(const LossTileArgs& a, hipStream_t st);
+hipError_t launch_loss_logits(const LossTileArgs& a, hipStream_t st);   // logits and part_max
 
 // z of up to 256, bf16 (losses_fused.hip).
 constexpr int LOSS_FUSED_WIDTH = 256;
@@ -171,7 +173,11 @@ struct LossRowsArgs {
 };
 hipError_t launch_loss_rows_f32(const LossRowsArgs& a, hipStream_t st);
 
-// The K largest of every row of u [M][ldu] with their columns, by falling value, equal ones by rising column.
-hipError_t launch_row_topk(const float* u, long long ldu, int M, int V, int K, float* values, int32_t* classes, hipStream_t st);
+// The K largest of every row of u [M][ldu] with their columns, by falling value, equal ones by rising column, NaN last.  part_max
+// [strips][M]: maxima of strips of LOSS_STRIP columns (NaN: nothing but NaN), or, with have_max false, room for them; at most LOSS_TOP_STRIPS strips.
+constexpr int LOSS_TOP_STRIPS = 1024;
+hipError_t launch_row_topk(const float* u, long long ldu, int M, int V, int K, float* part_max, bool have_max, float* values, int32_t* classes, hipStream_t st);
+// The same without strips, for any V.
+hipError_t launch_row_topk_wide(const float* u, long long ldu, int M, int V, int K, float* values, int32_t* classes, hipStream_t st);
 
 }  // namespace blstm

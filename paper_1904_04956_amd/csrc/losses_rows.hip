@@ -359,9 +359,155 @@ __device__ __forceinline__ uint32_t order_key(float x) {
     const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);
     return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
-// Finds the K-th largest key eight bits at a time, then, where more entries have that key than are wanted, the last column of
+// One row a wavefront.  The K largest of a row lie in the K strips whose best entries come first (K entries come before every entry of
+// another strip), so that of 32000 logits 500 maxima and 64 K logits are read.  The key of the K-th best strip, found bit by bit
+// with ballots over keys in registers, bounds the K largest from below; what of the chosen strips reaches it is collected in order of its column, and
+// cut back to the K best whenever the list is full: what comes later then has to be larger.
+constexpr int TOP_LIST = 1024;                           // entries of a list: cut back with 64 still free
+struct TopLds { uint32_t key[TOP_LIST], col[TOP_LIST]; };
+
+// Of key[0 .. N - 1] of a wavefront's lanes (entry i of lane l is number 64 i + l), the K-th largest; *first_equal: how many of its equals
+// are among the K.  (K entries at least are given; what is none has key 0 and counts as the last.)
+template <int N>
+__device__ uint32_t kth_largest(const uint32_t (&key)[N], int K, int* first_equal) {
+    uint32_t t = 0;
+    int above = 0;                                       // entries larger than any that agrees with t so far
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t c = t | (1u << bit);
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) n += __popcll(__ballot((key[i] >> bit) == (c >> bit)));
+        if (above + n >= K) t = c; else above += n;
+    }
+    *first_equal = K - above;
+    return t;
+}
+
+// Cuts the list's n entries back to the K best, in order; returns the smallest key kept.
+__device__ uint32_t cut_back(TopLds& s, int n, int K) {
+    const int lane = threadIdx.x & 63;
+    uint32_t key[TOP_LIST / 64], col[TOP_LIST / 64];
+#pragma unroll
+    for (int i = 0; i < TOP_LIST / 64; ++i) {
+        const int at = 64 * i + lane;
+        key[i] = at < n ? s.key[at] : 0u;
+        col[i] = at < n ? s.col[at] : 0u;
+    }
+    int equal;
+    const uint32_t t = kth_largest(key, K, &equal);
+    wave_sync();
+    int kept = 0, seen = 0;
+#pragma unroll
+    for (int i = 0; i < TOP_LIST / 64; ++i) {
+        const bool in = 64 * i + lane < n;
+        const unsigned long long same = __ballot(in && key[i] == t), below = (1ull << lane) - 1;
+        const bool keep = in && (key[i] > t || (key[i] == t && seen + __popcll(same & below) < equal));
+        const unsigned long long k = __ballot(keep);
+        if (keep) { const int to = kept + __popcll(k & below); s.key[to] = key[i]; s.col[to] = col[i]; }
+        kept += __popcll(k);
+        seen += __popcll(same);
+    }
+    wave_sync();
+    return t;
+}
+
+__global__ __launch_bounds__(256) void row_topk_kernel(const float* u, long long ldu, int M, int V, int K, int strips, const float* part_max, float* values, int32_t* classes) {
+    __shared__ TopLds lists[4];
+    constexpr int N = LOSS_TOP_STRIPS / 64, AHEAD = 8;
+    const int lane = threadIdx.x & 63;
+    const long long m = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (m >= M) return;
+    TopLds& s = lists[threadIdx.x >> 6];
+    const float* row = u + m * ldu;
+    const unsigned long long below = (1ull << lane) - 1;
+    uint32_t key[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) key[i] = 64 * i + lane < strips ? order_key(part_max[(long long)(64 * i + lane) * M + m]) : 0u;
+    int equal = strips;
+    uint32_t t = 0;
+    if (strips > K) t = kth_largest(key, K, &equal);
+    // the chosen strips' numbers, in order, through the list's second half
+    int chosen = 0, seen = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const bool in = 64 * i + lane < strips;
+        const unsigned long long same = __ballot(in && key[i] == t);
+        const bool keep = in && (strips <= K || key[i] > t || (key[i] == t && seen + __popcll(same & below) < equal));
+        const unsigned long long k = __ballot(keep);
+        if (keep) s.col[TOP_LIST - LOSS_MAX_TOP + chosen + __popcll(k & below)] = (uint32_t)(64 * i + lane);
+        chosen += __popcll(k);
+        seen += __popcll(same);
+    }
+    wave_sync();
+    uint32_t strip[LOSS_MAX_TOP / 64];                   // number 64 i + l of the chosen strips at lane l
+#pragma unroll
+    for (int i = 0; i < LOSS_MAX_TOP / 64; ++i) strip[i] = 64 * i + lane < chosen ? s.col[TOP_LIST - LOSS_MAX_TOP + 64 * i + lane] : 0u;
+    wave_sync();
+    int n = 0;
+    bool beyond = false;                                 // only what is larger than t is wanted any more
+#pragma unroll
+    for (int part = 0; part < LOSS_MAX_TOP / 64; ++part) {
+        const int here = min(64, chosen - 64 * part);
+        for (int j0 = 0; j0 < here; j0 += AHEAD) {
+            float x[AHEAD];
+            int col[AHEAD];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                col[j] = j0 + j < here ? (int)__builtin_amdgcn_readlane((int)strip[part], j0 + j) * LOSS_STRIP + lane : V;
+                x[j] = col[j] < V ? row[col[j]] : 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                const uint32_t k = order_key(x[j]);
+                const bool take = col[j] < V && (beyond ? k > t : k >= t);
+                const unsigned long long b = __ballot(take);
+                if (b == 0) continue;
+                if (take) { const int to = n + __popcll(b & below); s.key[to] = k; s.col[to] = (uint32_t)col[j]; }
+                n += __popcll(b);
+                if (n > TOP_LIST - 64) {
+                    wave_sync();
+                    t = cut_back(s, n, K);
+                    n = K;
+                    beyond = true;
+                }
+            }
+        }
+    }
+    wave_sync();
+    if (n > K) { cut_back(s, n, K); n = K; }
+    // places by rank: the list is in order of the columns, so that of equal keys the one in front is the better
+    for (int i = lane; i < K; i += 64) {
+        const uint32_t k = s.key[i], c = s.col[i];
+        int rank = 0;
+        for (int j = 0; j < K; ++j) rank += s.key[j] > k || (s.key[j] == k && j < i);
+        values[m * K + rank] = row[c];
+        classes[m * K + rank] = (int32_t)c;
+    }
+}
+
+// Maxima of the strips of every row (float logits, whose product does not make them): sixteen lanes a strip.
+__global__ __launch_bounds__(256) void strip_max_kernel(const float* u, long long ldu, int M, int V, int strips, float* part_max) {
+    const long long m = blockIdx.x;
+    const float* row = u + m * ldu;
+    const int l16 = threadIdx.x & 15;
+    for (int s = blockIdx.y * 64 + (threadIdx.x >> 4), k = 0; k < 4; ++k, s += 16) {
+        const int c = s * LOSS_STRIP + l16 * 4;
+        float mx = __builtin_nanf("");
+        if (c + 4 <= V) {
+            const float4 x = *reinterpret_cast<const float4*>(row + c);
+            mx = fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w));
+        } else {
+            for (int i = c; i < V; ++i) mx = fmaxf(mx, row[i]);
+        }
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+        if (l16 == 0 && s < strips) part_max[(long long)s * M + m] = mx;
+    }
+}
+
+// Any number of columns.  Finds the K-th largest key eight bits at a time, then, where more entries have that key than are wanted, the last column of
 // them that is; what is above is collected in any order and put in its place by its rank.
-__global__ __launch_bounds__(512) void row_topk_kernel(const float* u, long long ldu, int V, int K, float* values, int32_t* classes) {
+__global__ __launch_bounds__(512) void row_topk_wide_kernel(const float* u, long long ldu, int V, int K, float* values, int32_t* classes) {
     __shared__ unsigned hist[256];
     __shared__ unsigned found, above, equal, count;
     __shared__ unsigned long long list[LOSS_MAX_TOP];
@@ -473,8 +619,20 @@ hipError_t launch_loss_rows_f32(const LossRowsArgs& a, hipStream_t st) {
     return hipGetLastError();
 }
 
-hipError_t launch_row_topk(const float* u, long long ldu, int M, int V, int K, float* values, int32_t* classes, hipStream_t st) {
-    hipLaunchKernelGGL(row_topk_kernel, dim3((unsigned)M), dim3(512), 0, st, u, ldu, V, K, values, classes);
+hipError_t launch_row_topk(const float* u, long long ldu, int M, int V, int K, float* part_max, bool have_max, float* values, int32_t* classes, hipStream_t st) {
+    const int strips = (V + LOSS_STRIP - 1) / LOSS_STRIP;
+    if (strips > LOSS_TOP_STRIPS) return hipErrorInvalidValue;
+    if (!have_max) {
+        hipLaunchKernelGGL(strip_max_kernel, dim3((unsigned)M, (unsigned)((strips + 63) / 64)), dim3(256), 0, st, u, ldu, M, V, strips, part_max);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(row_topk_kernel, dim3((unsigned)((M + 3) / 4)), dim3(256), 0, st, u, ldu, M, V, K, strips, part_max, values, classes);
+    return hipGetLastError();
+}
+
+hipError_t launch_row_topk_wide(const float* u, long long ldu, int M, int V, int K, float* values, int32_t* classes, hipStream_t st) {
+    hipLaunchKernelGGL(row_topk_wide_kernel, dim3((unsigned)M), dim3(512), 0, st, u, ldu, V, K, values, classes);
     return hipGetLastError();
 }
 
