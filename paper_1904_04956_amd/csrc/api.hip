@@ -418,7 +418,7 @@ struct LossScratch {
 };
 static_assert(BLSTM_MAX_TOP == LOSS_MAX_TOP, "the kernels' lists must hold every entry");
 // Logits held at a time where they are only read once more: 128 MiB stay in the last-level cache.
-constexpr size_t kLossChunkBytes = (size_t)128 << 20;
+constexpr size_t kLossChunkBytes = (size_t)1 << 30;
 
 // Into how many parts the classes of a workgroup's 256 rows are cut, and the rows of a workgroup's 128 classes: the least estimated
 // time (us) of rounds of one workgroup a CU, tile by tile, with what is written and read again for every part.

@@ -366,10 +366,10 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 constexpr int TOP_LIST = 1024;                           // entries of a list: cut back with 64 still free
 struct TopLds { uint32_t key[TOP_LIST], col[TOP_LIST]; };
 
-// Of key[0 .. N - 1] of a wavefront's lanes (entry i of lane l is number 64 i + l), the K-th largest; *first_equal: how many of its equals
-// are among the K.  (K entries at least are given; what is none has key 0 and counts as the last.)
+// Of key[0 .. N - 1] of a wavefront's lanes (entry i of lane l is number 64 i + l), the K best are those above t and, in order, the first
+// `equal` of those that are t.  (K entries at least are given; what is none has key 0 and counts as the last.)
 template <int N>
-__device__ uint32_t kth_largest(const uint32_t (&key)[N], int K, int* first_equal) {
+__device__ uint32_t kth_largest(const uint32_t (&key)[N], int K, int* equal) {
     uint32_t t = 0;
     int above = 0;                                       // entries larger than any that agrees with t so far
     for (int bit = 31; bit >= 0; --bit) {
@@ -377,28 +377,30 @@ __device__ uint32_t kth_largest(const uint32_t (&key)[N], int K, int* first_equa
         int n = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) n += __popcll(__ballot((key[i] >> bit) == (c >> bit)));
-        if (above + n >= K) t = c; else above += n;
+        if (above + n == K) { *equal = 0; return c - 1; }   // (all of these, whatever their lower bits: about half of the bits are never looked at)
+        if (above + n > K) t = c; else above += n;
     }
-    *first_equal = K - above;
+    *equal = K - above;
     return t;
 }
 
-// Cuts the list's n entries back to the K best, in order; returns the smallest key kept.
+// Cuts the list's n <= 64 N entries back to the K best, in order; nothing below what it returns is kept.
+template <int N>
 __device__ uint32_t cut_back(TopLds& s, int n, int K) {
     const int lane = threadIdx.x & 63;
-    uint32_t key[TOP_LIST / 64], col[TOP_LIST / 64];
+    uint32_t key[N], col[N];
 #pragma unroll
-    for (int i = 0; i < TOP_LIST / 64; ++i) {
+    for (int i = 0; i < N; ++i) {
         const int at = 64 * i + lane;
         key[i] = at < n ? s.key[at] : 0u;
         col[i] = at < n ? s.col[at] : 0u;
     }
     int equal;
-    const uint32_t t = kth_largest(key, K, &equal);
+    const uint32_t t = kth_largest<N>(key, K, &equal);
     wave_sync();
     int kept = 0, seen = 0;
 #pragma unroll
-    for (int i = 0; i < TOP_LIST / 64; ++i) {
+    for (int i = 0; i < N; ++i) {
         const bool in = 64 * i + lane < n;
         const unsigned long long same = __ballot(in && key[i] == t), below = (1ull << lane) - 1;
         const bool keep = in && (key[i] > t || (key[i] == t && seen + __popcll(same & below) < equal));
@@ -411,9 +413,10 @@ __device__ uint32_t cut_back(TopLds& s, int n, int K) {
     return t;
 }
 
+template <int N>
 __global__ __launch_bounds__(256) void row_topk_kernel(const float* u, long long ldu, int M, int V, int K, int strips, const float* part_max, float* values, int32_t* classes) {
     __shared__ TopLds lists[4];
-    constexpr int N = LOSS_TOP_STRIPS / 64, AHEAD = 8;
+    constexpr int AHEAD = 16;                            // strips on their way
     const int lane = threadIdx.x & 63;
     const long long m = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (m >= M) return;
@@ -425,7 +428,7 @@ __global__ __launch_bounds__(256) void row_topk_kernel(const float* u, long long
     for (int i = 0; i < N; ++i) key[i] = 64 * i + lane < strips ? order_key(part_max[(long long)(64 * i + lane) * M + m]) : 0u;
     int equal = strips;
     uint32_t t = 0;
-    if (strips > K) t = kth_largest(key, K, &equal);
+    if (strips > K) t = kth_largest<N>(key, K, &equal);
     // the chosen strips' numbers, in order, through the list's second half
     int chosen = 0, seen = 0;
 #pragma unroll
@@ -459,22 +462,25 @@ __global__ __launch_bounds__(256) void row_topk_kernel(const float* u, long long
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
                 const uint32_t k = order_key(x[j]);
-                const bool take = col[j] < V && (beyond ? k > t : k >= t);
+                const bool take = col[j] < V && (k > t || (k == t && !beyond));
                 const unsigned long long b = __ballot(take);
                 if (b == 0) continue;
                 if (take) { const int to = n + __popcll(b & below); s.key[to] = k; s.col[to] = (uint32_t)col[j]; }
                 n += __popcll(b);
                 if (n > TOP_LIST - 64) {
                     wave_sync();
-                    t = cut_back(s, n, K);
+                    t = cut_back<TOP_LIST / 64>(s, n, K);
                     n = K;
-                    beyond = true;
+                    beyond = true;                       // (of what comes with t from here on, none is in front of those kept)
                 }
             }
         }
     }
     wave_sync();
-    if (n > K) { cut_back(s, n, K); n = K; }
+    if (n > K) {
+        if (n <= 128) cut_back<2>(s, n, K);
+        else cut_back<TOP_LIST / 64>(s, n, K);
+    }
     // places by rank: the list is in order of the columns, so that of equal keys the one in front is the better
     for (int i = lane; i < K; i += 64) {
         const uint32_t k = s.key[i], c = s.col[i];
@@ -627,7 +633,10 @@ hipError_t launch_row_topk(const float* u, long long ldu, int M, int V, int K, f
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(row_topk_kernel, dim3((unsigned)((M + 3) / 4)), dim3(256), 0, st, u, ldu, M, V, K, strips, part_max, values, classes);
+    const dim3 grid((unsigned)((M + 3) / 4));
+    if (strips <= 128) hipLaunchKernelGGL(row_topk_kernel<2>, grid, dim3(256), 0, st, u, ldu, M, V, K, strips, part_max, values, classes);
+    else if (strips <= 512) hipLaunchKernelGGL(row_topk_kernel<8>, grid, dim3(256), 0, st, u, ldu, M, V, K, strips, part_max, values, classes);
+    else hipLaunchKernelGGL(row_topk_kernel<LOSS_TOP_STRIPS / 64>, grid, dim3(256), 0, st, u, ldu, M, V, K, strips, part_max, values, classes);
     return hipGetLastError();
 }
 
