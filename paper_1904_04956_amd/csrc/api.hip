@@ -3,6 +3,7 @@
 // kernels of gemm.hip, cell.hip, softmax.hip and update.hip.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -412,8 +413,8 @@ struct LossScratch {
     int chunk;                // rows whose logits are held at a time (calls without gradients)
     bool strips;              // largest logits: by the strips' maxima
     bool fused;               // the kernels of losses_fused.hip: no du in memory
-    int row_parts, class_parts;
-    size_t bias_f, consts, part, part_ref, part_sum, cparts, cparts_b;
+    int row_parts, sum_parts, class_parts;
+    size_t bias_f, consts, part, part_ref, part_sum, part_sum2, cparts, cparts_b, tile_count, tile_from, entries;
     size_t zc, wp, dzp, dwp, label_logit, entry_logit, entry_q, soft_const, soft_state, pmax, psum, ptau, rows, row_loss, hi, lo, u, partial, partial_bytes, bytes;
 };
 static_assert(BLSTM_MAX_TOP == LOSS_MAX_TOP, "the kernels' lists must hold every entry");
@@ -432,6 +433,8 @@ int loss_parts(long long groups, long long tiles, double tile_us, double part_us
     const long long per = (tiles + best - 1) / best;
     return (int)((tiles + per - 1) / per);               // (no empty part)
 }
+int loss_sum_parts(int M, int V, int Zp) { return loss_parts((M + 511) / 512, (V + 63) / 64, 2.2 * Zp / 256, 4.0 * M / 4e6); }   // (two workgroups a CU)
+size_t loss_tiles(int M, int V) { return (size_t)((M + 63) / 64) * ((V + 127) / 128); }
 int loss_row_parts(int M, int V, int Zp) { return loss_parts((M + 255) / 256, (V + 63) / 64, 2.2 * Zp / 256, 2.0 * M * Zp * 4 / 4e6); }
 int loss_class_parts(int M, int V, int Zp) { return loss_parts((V + 127) / 128, (M + 63) / 64, 1.8 * Zp / 256, 2.0 * V * Zp * 4 / 4e6); }
 
@@ -454,18 +457,33 @@ LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
     if (bf && call != SOFTMAX_TOPK) {
         const size_t strips = (size_t)loss_strips(c->V);
         put(&l.label_logit, M * 4);
-        l.fused = call == SOFTMAX_POLICY && l.Zp <= LOSS_FUSED_WIDTH;
+        l.fused = l.Zp <= LOSS_FUSED_WIDTH;
         if (l.fused) {
-            l.row_parts = loss_row_parts(c->M, c->V, l.Zp);
-            l.class_parts = loss_class_parts(c->M, c->V, l.Zp);
-            const size_t Mp = (M + 63) & ~size_t(63), P = (size_t)l.row_parts, C = (size_t)l.class_parts;
             put(&l.bias_f, ((V + 63) & ~size_t(63)) * 4);
-            put(&l.consts, 6 * Mp * 4);
-            put(&l.part, P * M * l.Zp * 4);
-            put(&l.part_ref, P * M * 4);
-            put(&l.part_sum, P * M * 4);
-            if (C > 1) { put(&l.cparts, C * V * c->zdim * 4); put(&l.cparts_b, C * V * 4); }
-            put(&l.row_loss, M * 4);
+            l.sum_parts = loss_sum_parts(c->M, c->V, l.Zp);
+            l.row_parts = gradient ? loss_row_parts(c->M, c->V, l.Zp) : 0;
+            const size_t parts = (size_t)(l.row_parts > l.sum_parts ? l.row_parts : l.sum_parts);
+            put(&l.part_ref, parts * M * 4);
+            put(&l.part_sum, parts * M * 4);
+            if (gradient) {
+                const size_t Mp = (M + 63) & ~size_t(63);
+                l.class_parts = loss_class_parts(c->M, c->V, l.Zp);
+                put(&l.consts, 6 * Mp * 4);
+                put(&l.part, (size_t)l.row_parts * M * l.Zp * 4);
+                if (l.class_parts > 1) { put(&l.cparts, (size_t)l.class_parts * V * c->zdim * 4); put(&l.cparts_b, (size_t)l.class_parts * V * 4); }
+                put(&l.row_loss, M * 4);
+            }
+            if (call == SOFTMAX_DISTILL) {
+                const size_t tiles = loss_tiles(c->M, c->V);
+                put(&l.part_sum2, (size_t)l.sum_parts * M * 4);
+                put(&l.entry_logit, M * K * 4);
+                put(&l.entry_q, M * K * 4);
+                put(&l.soft_const, M * 4);
+                put(&l.soft_state, M * 4);
+                put(&l.tile_count, tiles * 4);
+                put(&l.tile_from, (tiles + 1) * 4);
+                put(&l.entries, (M * K + LOSS_LIST_SLACK) * 8);
+            }
             l.bytes = w;
             return l;
         }
@@ -486,6 +504,8 @@ LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
     } else {
         put(&l.u, (gradient ? M : (size_t)l.chunk) * per_row);
         l.strips = call == SOFTMAX_TOPK && c->V <= LOSS_TOP_STRIPS * LOSS_STRIP;
+        l.fused = bf && l.strips && l.Zp <= LOSS_FUSED_WIDTH;
+        if (l.fused) put(&l.bias_f, ((V + 63) & ~size_t(63)) * 4);
         if (l.strips) put(&l.pmax, (size_t)loss_strips(c->V) * l.chunk * 4);
     }
     size_t need = 0;
@@ -591,33 +611,59 @@ int loss_products(blstm_ctx* ctx, const LossCall& c, void* dz, float* grad) {
     return BLSTM_OK;
 }
 
-// bf16, z of up to LOSS_FUSED_WIDTH: rows, dz, classes.
+// bf16, z of up to LOSS_FUSED_WIDTH.  Log-probabilities: the rows' sums.  Gradients: the rows kernel, which makes dz (with its own sums where one
+// exponential a logit is enough; a label's and a teacher's at a temperature are two distributions, whose sums come first), then the classes kernel.
 int loss_run_fused(blstm_ctx* ctx, const LossCall& c, const int32_t* labels, const PolicyArgs* policy, const TeacherArgs* teacher, float* loss_dev, float* logp, void* dz, float* grad) {
     hipStream_t st = c.st;
     const LossScratch& l = c.l;
     const float log2e = 1.44269504f;
+    const bool gradient = policy || teacher, both = teacher && teacher->hard != 0.0f && teacher->inv_tau != 1.0f;
     LossFusedArgs f{};
-    f.z = reinterpret_cast<const unsigned short*>(c.base + l.zc); f.W = static_cast<const unsigned short*>(c.W);
+    f.z = static_cast<const unsigned short*>(c.zc); f.W = static_cast<const unsigned short*>(c.W);
     f.bias = c.at<float>(l.bias_f); f.consts = c.at<float>(l.consts);
     f.M = ctx->M; f.Mp = (ctx->M + 63) & ~63; f.V = ctx->V; f.Z = ctx->zdim; f.ld = l.Zp;
-    f.k1 = log2e; f.k = log2e;
+    f.k1 = log2e; f.k = teacher ? log2e * teacher->inv_tau : log2e;
+    f.part_ref = c.at<float>(l.part_ref); f.part_sum = c.at<float>(l.part_sum);
+    if (teacher) {
+        LossListArgs e{};
+        e.M = ctx->M; e.V = ctx->V; e.K = teacher->K; e.classes = teacher->classes; e.q = c.at<float>(l.entry_q); e.weight = ctx->s * teacher->soft * teacher->tau;
+        e.count = c.at<int>(l.tile_count); e.from = c.at<int>(l.tile_from); e.entries = c.at<uint2>(l.entries);
+        RUN(PC_SOFTMAX_ROWS, "the teacher's classes by tiles", launch_loss_lists(e, st));
+    }
+    if (!gradient || both) {
+        f.parts = l.sum_parts;
+        f.part_sum2 = both ? c.at<float>(l.part_sum2) : nullptr;
+        RUN(PC_GEMM_LOGITS, "sums of the softmax", launch_loss_fused_sums(f, both, false, st));
+        LossMergeArgs g{};
+        g.M = ctx->M; g.V = ctx->V; g.strips = f.parts;
+        g.part_max = f.part_ref; g.part_sum = f.part_sum; g.part_sum_tau = f.part_sum2;
+        g.labels = labels; g.label_logit = c.at<float>(l.label_logit); g.s = ctx->s;
+        g.teacher = teacher; g.soft_const = c.at<float>(l.soft_const); g.soft_state = c.at<int>(l.soft_state);
+        g.logp = logp; g.row_loss = c.at<float>(l.row_loss);
+        g.consts = gradient ? c.at<float>(l.consts) : nullptr; g.Mp = f.Mp;
+        RUN(PC_SOFTMAX_ROWS, "rows of the softmax", launch_loss_merge(g, st));
+        if (!gradient) return BLSTM_OK;
+    }
     f.parts = l.row_parts;
-    f.out = c.at<float>(l.part); f.part_ref = c.at<float>(l.part_ref); f.part_sum = c.at<float>(l.part_sum);
-    RUN(PC_GEMM_LOGITS, "rows of the softmax", launch_loss_fused_rows(f, false, false, st));
+    f.out = c.at<float>(l.part);
+    RUN(PC_GEMM_LOGITS, "rows of the softmax", launch_loss_fused_rows(f, both, both, st));
     LossDzArgs d{};
     d.M = f.M; d.Mp = f.Mp; d.V = f.V; d.Z = f.Z; d.ld = f.ld; d.parts = f.parts;
     d.part = f.out; d.part_ref = f.part_ref; d.part_sum = f.part_sum; d.W = f.W;
     d.labels = labels; d.label_logit = c.at<float>(l.label_logit); d.s = ctx->s;
     d.policy = policy; d.teacher = teacher;
+    d.entry_q = c.at<float>(l.entry_q); d.soft_const = c.at<float>(l.soft_const); d.soft_state = c.at<int>(l.soft_state);
     d.logp = logp; d.row_loss = c.at<float>(l.row_loss); d.consts = c.at<float>(l.consts);
     d.dz = static_cast<unsigned short*>(dz);
-    RUN(PC_SOFTMAX_ROWS, "dz", launch_loss_dz(d, false, st));
+    RUN(PC_SOFTMAX_ROWS, "dz", launch_loss_dz(d, both, st));
     float* dw = grad + ctx->off_ws;
     float* db = grad + ctx->off_bs;
     f.parts = l.class_parts;
     f.out = l.class_parts > 1 ? c.at<float>(l.cparts) : dw; f.out_db = l.class_parts > 1 ? c.at<float>(l.cparts_b) : db;
     f.ldo = ctx->zdim; f.vec = ctx->zdim % 4 == 0 && aligned16(f.out);
-    RUN(PC_GEMM_SOFTMAX_BWD, "dW_s", launch_loss_fused_classes(f, false, st));
+    if (!both) f.k1 = f.k;                               // (the only exponential is the first)
+    if (teacher) { f.entries = c.at<uint2>(l.entries); f.entries_from = c.at<int>(l.tile_from); }
+    RUN(PC_GEMM_SOFTMAX_BWD, "dW_s", launch_loss_fused_classes(f, both, st));
     if (l.class_parts > 1)
         RUN(PC_GEMM_SOFTMAX_BWD, "dW_s", launch_loss_classes_sum(f.out, f.out_db, f.parts, (long long)ctx->V * ctx->zdim, ctx->V, dw, db, st));
     RUN(PC_MISC, "loss sum", launch_sum_to_scalar(c.at<float>(l.row_loss), ctx->M, loss_dev, st));
@@ -642,7 +688,13 @@ int loss_run(blstm_ctx* ctx, const LossCall& given, const int32_t* labels, const
         if (bf) {
             a.W = static_cast<const unsigned short*>(c.W); a.bias = static_cast<const unsigned short*>(c.b);
             a.label_logit = c.at<float>(l.label_logit);
-            if (l.fused) a.bias_f = c.at<float>(l.bias_f);
+            if (l.fused) {
+                a.bias_f = c.at<float>(l.bias_f); a.bias_pad = -INFINITY;
+                if (teacher) {
+                    a.tile_count = c.at<int>(l.tile_count);
+                    RUN(PC_MISC, "counts", launch_fill_u32(reinterpret_cast<unsigned*>(a.tile_count), (int)loss_tiles(M, V), 0u, st));
+                }
+            }
             a.entry_logit = c.at<float>(l.entry_logit); a.entry_q = c.at<float>(l.entry_q);
             a.soft_const = c.at<float>(l.soft_const); a.soft_state = c.at<int>(l.soft_state);
         }
@@ -1117,12 +1169,26 @@ int softmax_topk(blstm_ctx* ctx, const void* theta, const void* z, int K, float*
         RUN(PC_MISC, "padded z", launch_pad_blocks(&t, 1, z, c.base + l.zc, ctx->st, st));
         c.zc = c.base + l.zc;
     }
+    if (l.fused) {
+        LossPrepArgs a{};                                // (no rows: the bias alone)
+        a.V = ctx->V; a.bias = static_cast<const unsigned short*>(c.b); a.bias_f = c.at<float>(l.bias_f); a.bias_pad = __builtin_nanf("");
+        RUN(PC_MISC, "bias", launch_loss_prep(a, DT_BF16, st));
+    }
     for (int m = 0; m < ctx->M; m += l.chunk) {
         const int n = ctx->M - m < l.chunk ? ctx->M - m : l.chunk;
         float* u = c.at<float>(l.u);
         float* v = values + (size_t)m * K;
         int32_t* cls = classes + (size_t)m * K;
-        if (l.strips && ctx->st == DT_BF16) {            // (the maxima come with the logits)
+        if (l.fused) {                                   // (the maxima come with the logits)
+            LossFusedArgs f{};
+            f.z = static_cast<const unsigned short*>(c.zc) + (size_t)m * l.Zp; f.W = static_cast<const unsigned short*>(c.W); f.bias = c.at<float>(l.bias_f);
+            f.M = n; f.V = ctx->V; f.ld = l.Zp; f.parts = loss_sum_parts(n, ctx->V, l.Zp);
+            f.out = u; f.ldo = l.ldu; f.part_ref = c.at<float>(l.pmax);
+            RUN(PC_GEMM_LOGITS, "logits", launch_loss_fused_sums(f, false, true, st));
+            RUN(PC_SOFTMAX_ROWS, "largest logits", launch_row_topk(u, l.ldu, n, ctx->V, K, f.part_ref, true, v, cls, st));
+            continue;
+        }
+        if (l.strips && ctx->st == DT_BF16) {
             LossTileArgs t{};
             t.z = static_cast<const unsigned short*>(c.zc) + (size_t)m * l.Zp; t.W = static_cast<const unsigned short*>(c.W); t.bias = static_cast<const unsigned short*>(c.b);
             t.M = n; t.V = ctx->V; t.ld = l.Zp;

@@ -49,12 +49,14 @@ struct LossPrepArgs {
     int M, V, Z, ldzc;
     const unsigned short* W;                         // rows of ldzc elements, zeros behind Z; null: only zc is wanted
     const unsigned short* bias;
-    float* bias_f;                                   // [V rounded up to 64] the bias as floats, -inf behind it; or null
+    float* bias_f;                                   // [V rounded up to 64] the bias as floats, bias_pad behind it; or null
+    float bias_pad;
+    int* tile_count;                                 // entries by tiles of 64 rows and 128 classes, zero before the launch; or null
     const int32_t* labels;                           // or null
     float* label_logit;                              // [M]
     TeacherArgs teacher;                             // K = 0: none
     float* entry_logit;                              // [M][K]
-    float* entry_q;                                  // [M][K], 0: not used
+    float* entry_q;                                  // [M][K], 0: not used; of entries with one class, the first has all
     float* soft_const;                               // [M]
     int* soft_state;                                 // [M]: bit 0: some entry is used; bit 1: some class is out of range (the loss is NaN)
 };
@@ -94,11 +96,17 @@ struct LossFusedArgs {
     float* out;                                      // rows: [parts][M][ld]; classes: [parts][V][ldo], columns 0 .. Z - 1
     float* part_ref;                                 // rows, sums not known: [parts][M] reference and sum
     float* part_sum;
+    float* part_sum2;                                // sums: at the scale k
     float* out_db;                                   // classes: [parts][V]
+    const uint2* entries;                            // classes: the teacher's, row | class << 6 within a tile and weight q, by tiles of 64 rows and 128 classes; or null
+    const int* entries_from;                         // [tiles + 1]
     long long ldo;
     int vec;                                         // classes: rows of out take 16-byte stores
 };
 hipError_t launch_loss_fused_rows(const LossFusedArgs& a, bool known, bool tau, hipStream_t st);
+// The rows' sums alone at the scale k1 and, with second, k from references part_ref (a logit); or, with logits, u into out [M][ldo] (ldo a multiple
+// of four; NaN behind V counts as no maximum) and the maxima of strips of 64 classes into part_ref [strips][M].
+hipError_t launch_loss_fused_sums(const LossFusedArgs& a, bool second, bool logits, hipStream_t st);
 hipError_t launch_loss_fused_classes(const LossFusedArgs& a, bool tau, hipStream_t st);
 // dz from the parts of launch_loss_fused_rows, exactly completed by the label's and the teacher's classes; with known false the
 // rows' losses and constants too.
@@ -122,6 +130,18 @@ struct LossDzArgs {
     unsigned short* dz;                              // [M][Z]
 };
 hipError_t launch_loss_dz(const LossDzArgs& a, bool known, hipStream_t st);
+// The teacher's entries in order of their tiles, from the tiles' counts (which become zero).  entries: room for M K, and 256 more that are read.
+constexpr int LOSS_LIST_SLACK = 256;
+struct LossListArgs {
+    int M, V, K;
+    const int32_t* classes;
+    const float* q;                                  // [M][K], 0: none
+    float weight;
+    int* count;                                      // [tiles]
+    int* from;                                       // [tiles + 1]
+    uint2* entries;
+};
+hipError_t launch_loss_lists(const LossListArgs& a, hipStream_t st);
 // out = sum of parts of n floats, out_b of V, in order.
 hipError_t launch_loss_classes_sum(const float* p, const float* pb, int parts, long long n, int V, float* out, float* out_b, hipStream_t st);
 
@@ -140,7 +160,9 @@ struct LossMergeArgs {
     const int* soft_state;
     float* logp;
     float* row_loss;
-    LossRow* rows;
+    LossRow* rows;                                   // or
+    float* consts;                                   // [6][Mp], rows M .. Mp - 1 too
+    int Mp;
 };
 hipError_t launch_loss_merge(const LossMergeArgs& a, hipStream_t st);
 

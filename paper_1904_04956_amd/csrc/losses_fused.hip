@@ -31,6 +31,7 @@ __device__ __forceinline__ int fresh_lane() {
 template <int NK>
 struct Ring {
     static constexpr int CPR = 8 * NK, ROWB = 128 * NK, TILE = 64 * ROWB, STAGE = TILE + 2048, STAGES = 3;
+    static constexpr int LIST = 2048;                   // bytes of a teacher's entries behind it, where there are any
     static __device__ __forceinline__ void dma16(unsigned lds, const char* base, unsigned voff) {
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(base) : "memory");
     }
@@ -174,7 +175,7 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
                     for (int i = 0; i < 2; ++i) {
                         const float x = u[8 * t + e + i];
                         if constexpr (KNOWN) {
-                            w[i] = ca * __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -m2));
+                            w[i] = ca * __builtin_amdgcn_exp2f(fmaf(x, a.k1, -m2));
                             if (TAU) w[i] = fmaf(cat, __builtin_amdgcn_exp2f(fmaf(x, k, -mt2)), w[i]);
                         } else {
                             w[i] = __builtin_amdgcn_exp2f(fmaf(x, k, -ref));
@@ -209,10 +210,109 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
     }
 }
 
+// ---- rows, the sums alone -----------------------------------------------------------------------------------------------------
+// Reference and sum of exponentials of every row and part (SUMS2: at two scales, from one reference), or the logits themselves with the
+// maxima of strips of 64 classes (LOGITS).  Two workgroups a CU, four wavefronts a SIMD, so that some multiply while others take exponentials.
+// Rows as in the rows kernel: of the 128 x 128 tiles that larger z take, both operands come from L2 for half the products.
+enum { SUMS, SUMS2, LOGITS };
+template <int NK, int WHAT>
+__global__ __launch_bounds__(512, 4) void loss_sums_kernel(LossFusedArgs a) {
+    typedef Ring<NK> R;
+    extern __shared__ uint4 smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
+    const int part = (int)blockIdx.x % a.parts, row0 = (int)blockIdx.x / a.parts * 256;
+    const int ntv = (a.V + 63) / 64, per = (ntv + a.parts - 1) / a.parts, t0 = part * per, n = min(per, ntv - t0);
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
+    const Reads<NK> at(lane);
+    const int m = row0 + wv * 32 + l32;
+    uint4 zf[4 * NK];
+#pragma unroll
+    for (int q = 0; q < 4 * NK; ++q) {
+        const int c = 2 * q + half;
+        zf[q] = c * 8 < a.ld ? *reinterpret_cast<const uint4*>(a.z + (long long)min(m, a.M - 1) * a.ld + c * 8) : make_uint4(0, 0, 0, 0);
+    }
+    __builtin_amdgcn_s_waitcnt(0);
+    auto issue = [&](int it) __attribute__((always_inline)) {
+        const unsigned s = lds0 + (unsigned)((it & 1) * R::STAGE);
+        R::tile(s, a.W, (t0 + it) * 64, a.V, a.ld, wv);
+        R::dma4(s + R::TILE, reinterpret_cast<const char*>(a.bias + (long long)(t0 + it) * 64), (unsigned)(fresh_lane() * 4));
+    };
+    float top = -LOSS_FAR, sum = 0.0f, sum2 = 0.0f;
+    const float k1 = a.k1, k = a.k, slack = SLACK / fmaxf(k1, WHAT == SUMS2 ? k : 0.0f);
+    issue(0);
+    for (int it = 0; it < n; ++it) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (it + 1 < n) issue(it + 1);
+        const char* stage = reinterpret_cast<const char*>(smem) + (it & 1) * R::STAGE;
+        const float* bias = reinterpret_cast<const float*>(stage + R::TILE);
+        float strip = __builtin_nanf("");
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+            const char* s = stage + sub * 32 * R::ROWB;
+            f32x16_t u;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float4 b = *reinterpret_cast<const float4*>(bias + sub * 32 + 8 * g + 4 * half);
+                u[4 * g] = b.x; u[4 * g + 1] = b.y; u[4 * g + 2] = b.z; u[4 * g + 3] = b.w;
+            }
+#pragma unroll
+            for (int q = 0; q < 4 * NK; ++q) u = mma32(at.by_row(s, q), zf[q], u);
+            ahead<4 + DEPTH, 4 * NK, 1, 1, DEPTH>();
+            __builtin_amdgcn_sched_barrier(0);
+            float mx = u[0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) mx = fmaxf(mx, u[e]);
+            if constexpr (WHAT == LOGITS) {
+                strip = fmaxf(strip, mx);
+                if (m < a.M) {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const int v = (t0 + it) * 64 + sub * 32 + 8 * g + 4 * half;
+                        if (v < a.ldo) *reinterpret_cast<float4*>(a.out + m * a.ldo + v) = make_float4(u[4 * g], u[4 * g + 1], u[4 * g + 2], u[4 * g + 3]);
+                    }
+                }
+            } else {
+                if (__any(mx > top + slack)) {
+                    const float now = fmaxf(top, fmaxf(mx, __shfl_xor(mx, 32, 64)));
+                    sum *= __builtin_amdgcn_exp2f((top - now) * k1);
+                    if (WHAT == SUMS2) sum2 *= __builtin_amdgcn_exp2f((top - now) * k);
+                    top = now;
+                }
+                const float m1 = top * k1, m2 = top * k;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    sum += __builtin_amdgcn_exp2f(fmaf(u[e], k1, -m1));
+                    if (WHAT == SUMS2) sum2 += __builtin_amdgcn_exp2f(fmaf(u[e], k, -m2));
+                }
+            }
+        }
+        if constexpr (WHAT == LOGITS) {
+            strip = fmaxf(strip, __shfl_xor(strip, 32, 64));
+            if (half == 0 && m < a.M) a.part_ref[(long long)(t0 + it) * a.M + m] = strip;
+        }
+    }
+    if constexpr (WHAT != LOGITS) {
+        sum += __shfl_xor(sum, 32, 64);
+        if (WHAT == SUMS2) sum2 += __shfl_xor(sum2, 32, 64);
+        if (half == 0 && m < a.M) {
+            const long long to = (long long)part * a.M + m;
+            a.part_ref[to] = top;
+            a.part_sum[to] = sum;
+            if (WHAT == SUMS2) a.part_sum2[to] = sum2;
+        }
+    }
+}
+
 // ---- classes ----------------------------------------------------------------------------------------------------------------
-template <int NK, bool TAU>
+// ENTRIES: of a teacher's lists, those of a tile's 64 rows and the workgroup's 128 classes come with the tile, in any order; a wavefront puts its own
+// into a block of 32 x 32 in LDS, from which du takes them, and clears them again.
+// (written by an earlier launch: read with scalar loads, which the ring's waits do not count)
+typedef const __attribute__((address_space(4))) int* const_int;
+constexpr int SPOT = 36;                                // floats between a block's classes: eight lanes' reads on banks of their own
+template <int NK, bool TAU, bool ENTRIES>
 __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
     typedef Ring<NK> R;
+    constexpr int STAGE = R::STAGE + (ENTRIES ? R::LIST : 0), LOADS = NK + 1 + (ENTRIES ? 1 : 0);
     extern __shared__ uint4 smem[];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
     const int cg = wv & 3, rh = wv >> 2;                // the wavefront's 32 classes, and its 32 of a tile's 64 rows
@@ -230,10 +330,11 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
     const float b = v < a.V ? a.bias[v] : -INFINITY, k1 = a.k1, b2 = b * k1, bt = b * a.k, k = a.k;
     __builtin_amdgcn_s_waitcnt(0);                      // (known to the compiler: it would wait for these loads, and the ring's with them, in the loop)
     auto issue = [&](int it) __attribute__((always_inline)) {
-        const unsigned s = lds0 + (unsigned)(it % R::STAGES * R::STAGE);
+        const unsigned s = lds0 + (unsigned)(it % R::STAGES * STAGE);
         R::tile(s, a.z, (t0 + it) * 64, a.M, a.ld, wv);
         // the rows' constants, an array a wavefront
         R::dma4(s + R::TILE + (unsigned)(wv * 256), reinterpret_cast<const char*>(a.consts + (long long)min(wv, 5) * a.Mp + (long long)(t0 + it) * 64), (unsigned)(fresh_lane() * 4));
+        if constexpr (ENTRIES) R::dma4(s + R::STAGE + (unsigned)(wv * 256), reinterpret_cast<const char*>(a.entries + ((const_int)(uintptr_t)a.entries_from)[(long long)(t0 + it) * ntv + ct]) + wv * 256, (unsigned)(fresh_lane() * 4));
     };
     f32x16_t o[2 * NK];
 #pragma unroll
@@ -241,13 +342,17 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[zb][e] = 0.0f;
     float db = 0.0f;
+    float* spots = reinterpret_cast<float*>(reinterpret_cast<char*>(smem) + R::STAGES * STAGE) + wv * 32 * SPOT;
+    if constexpr (ENTRIES) {
+        for (int k = lane; k < 32 * SPOT; k += 64) spots[k] = 0.0f;
+    }
     if (n > 0) issue(0);
     if (n > 1) issue(1);
     for (int it = 0; it < n; ++it) {
-        if (it + 1 < n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(NK + 1) : "memory");
+        if (it + 1 < n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LOADS) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (it + 2 < n) issue(it + 2);
-        const char* stage = reinterpret_cast<const char*>(smem) + it % R::STAGES * R::STAGE;
+        const char* stage = reinterpret_cast<const char*>(smem) + it % R::STAGES * STAGE;
         const char* s = stage + rh * 32 * R::ROWB;
         const float* consts = reinterpret_cast<const float*>(stage + R::TILE) + rh * 32;   // [6][64]
         f32x16_t u;
@@ -257,6 +362,29 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
         for (int q = 0; q < 4 * NK; ++q) u = mma32(at.by_row(s, q), wf[q], u);
         ahead<DEPTH, 4 * NK, 1, 1, DEPTH>();
         __builtin_amdgcn_sched_barrier(0);
+        // the teacher's entries of these rows and classes
+        int listed = 0;
+        bool any_spot = false;
+        auto spread = [&](bool clear) {
+            const int from = ((const_int)(uintptr_t)a.entries_from)[(long long)(t0 + it) * ntv + ct];
+            const int ln = fresh_lane();
+            for (int k = ln; k < listed; k += 64) {
+                const uint2 e = k < R::LIST / 8 ? reinterpret_cast<const uint2*>(stage + R::STAGE)[k] : a.entries[from + k];
+                const int r = (int)(e.x & 63u), cl = (int)(e.x >> 6);
+                if (r >> 5 != rh || cl >> 5 != cg) continue;
+                spots[(cl & 31) * SPOT + (r & 31)] = clear ? 0.0f : __builtin_bit_cast(float, e.y);
+                any_spot = true;
+            }
+        };
+        if constexpr (ENTRIES) {
+            const const_int at_ = (const_int)(uintptr_t)a.entries_from + (long long)(t0 + it) * ntv + ct;
+            listed = at_[1] - at_[0];
+            spread(false);
+            any_spot = __any(any_spot);
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        }
         // a label among these classes: one product of 32 x 32 in V / 1024
         const int* labels = reinterpret_cast<const int*>(consts + 320);
         const bool any_hot = __any((unsigned)(labels[fresh_lane() & 31] - class0) < 32u);
@@ -275,6 +403,13 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
                     const float mts[4] = {mt.x, mt.y, mt.z, mt.w}, cts[4] = {ct_.x, ct_.y, ct_.z, ct_.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) d[4 * h + i] = fmaf(cts[i], __builtin_amdgcn_exp2f(fmaf(u[8 * t + 4 * h + i], k, bt - mts[i])), d[4 * h + i]);
+                }
+            }
+            if (ENTRIES && any_spot) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float4 x = *reinterpret_cast<const float4*>(spots + (fresh_lane() & 31) * SPOT + 8 * (2 * t + h) + 4 * half);
+                    d[4 * h] -= x.x; d[4 * h + 1] -= x.y; d[4 * h + 2] -= x.z; d[4 * h + 3] -= x.w;
                 }
             }
             if (any_hot) {
@@ -313,6 +448,7 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+        if (ENTRIES && any_spot) spread(true);          // (a wavefront's LDS accesses keep their order)
     }
     const int ln = fresh_lane(), n32 = ln & 31, hf = ln >> 5, cls = ct * 128 + cg * 32 + n32;
     // the two halves of the rows together, through LDS; register e of a lane: column 32 zb + 8 (e / 4) + 4 half + e % 4 of class l32
@@ -344,6 +480,45 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
                 for (int i = 0; i < 4; ++i) if (z + i < a.Z) out[(long long)cls * a.ldo + z + i] = y[i];
             }
         }
+}
+
+// ---- a teacher's entries by tiles of 64 rows and 128 classes --------------------------------------------------------------------
+// (their numbers are counted by loss_prep_kernel) from[i] = sum of count[0 .. i - 1], from[n] the sum of all; one workgroup.
+__global__ __launch_bounds__(1024) void loss_offsets_kernel(const int* count, int* from, int n) {
+    __shared__ int sh[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int run = 0;
+    for (int i0 = 0; i0 < n; i0 += 8192) {
+        int x[8], own = 0;
+        const int i = i0 + (int)threadIdx.x * 8;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { x[k] = i + k < n ? count[i + k] : 0; own += x[k]; }
+        int before = own;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) { const int t = __shfl_up(before, o, 64); if (lane >= o) before += t; }
+        __syncthreads();
+        if (lane == 63) sh[wave] = before;
+        __syncthreads();
+        int all = 0;
+        before += run - own;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) { if (w < wave) before += sh[w]; all += sh[w]; }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { if (i + k < n) from[i + k] = before; before += x[k]; }
+        run += all;
+    }
+    if (threadIdx.x == 0) from[n] = run;
+}
+// Puts every entry with a probability into its tile's list (whose order is of no matter: a row's classes are different ones).
+__global__ __launch_bounds__(256) void loss_lists_kernel(const int32_t* classes, const float* q, float weight, long long n, int K, int ntv, int* count, const int* from, uint2* entries) {
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+        const float p = q[i];
+        if (!(p > 0.0f)) continue;
+        const int m = (int)(i / K), c = classes[i];
+        const long long b = (long long)(m >> 6) * ntv + (c >> 7);
+        const int to = from[b] + atomicSub(&count[b], 1) - 1;
+        entries[to] = make_uint2((unsigned)(m & 63) | (unsigned)(c & 127) << 6, __builtin_bit_cast(unsigned, weight * p));
+    }
 }
 
 // The parts of dW_s and db_s in order.
@@ -454,13 +629,22 @@ hipError_t rows_nk(const LossFusedArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((loss_rows_kernel<NK, KNOWN, TAU>), dim3((unsigned)((a.M + 255) / 256 * a.parts)), dim3(512), lds, st, a);
     return hipGetLastError();
 }
-template <int NK, bool TAU>
-hipError_t classes_nk(const LossFusedArgs& a, hipStream_t st) {
-    constexpr size_t ring = (size_t)Ring<NK>::STAGES * Ring<NK>::STAGE, join = 32768 * 4 + 512, lds = ring > join ? ring : join;
+template <int NK, int WHAT>
+hipError_t sums_nk(const LossFusedArgs& a, hipStream_t st) {
+    constexpr size_t lds = 2 * (size_t)Ring<NK>::STAGE;
     static thread_local bool attr_set = false;
-    const hipError_t e = allow_lds(&loss_classes_kernel<NK, TAU>, lds, &attr_set);
+    const hipError_t e = allow_lds(&loss_sums_kernel<NK, WHAT>, lds, &attr_set);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((loss_classes_kernel<NK, TAU>), dim3((unsigned)((a.V + 127) / 128 * a.parts)), dim3(512), lds, st, a);
+    hipLaunchKernelGGL((loss_sums_kernel<NK, WHAT>), dim3((unsigned)((a.M + 255) / 256 * a.parts)), dim3(512), lds, st, a);
+    return hipGetLastError();
+}
+template <int NK, bool TAU, bool ENTRIES>
+hipError_t classes_nk(const LossFusedArgs& a, hipStream_t st) {
+    constexpr size_t ring = (size_t)Ring<NK>::STAGES * (Ring<NK>::STAGE + (ENTRIES ? Ring<NK>::LIST : 0)) + (ENTRIES ? 8 * 32 * SPOT * 4 : 0), join = 32768 * 4 + 512, lds = ring > join ? ring : join;
+    static thread_local bool attr_set = false;
+    const hipError_t e = allow_lds(&loss_classes_kernel<NK, TAU, ENTRIES>, lds, &attr_set);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((loss_classes_kernel<NK, TAU, ENTRIES>), dim3((unsigned)((a.V + 127) / 128 * a.parts)), dim3(512), lds, st, a);
     return hipGetLastError();
 }
 
@@ -475,9 +659,18 @@ hipError_t launch_loss_fused_rows(const LossFusedArgs& a, bool known, bool tau, 
     BLSTM_ROWS(4);
 #undef BLSTM_ROWS
 }
+hipError_t launch_loss_fused_sums(const LossFusedArgs& a, bool second, bool logits, hipStream_t st) {
+    const int nk = (a.ld + 63) / 64;
+#define BLSTM_SUMS(NK) return logits ? sums_nk<NK, LOGITS>(a, st) : second ? sums_nk<NK, SUMS2>(a, st) : sums_nk<NK, SUMS>(a, st)
+    if (nk == 1) BLSTM_SUMS(1);
+    if (nk == 2) BLSTM_SUMS(2);
+    if (nk == 3) BLSTM_SUMS(3);
+    BLSTM_SUMS(4);
+#undef BLSTM_SUMS
+}
 hipError_t launch_loss_fused_classes(const LossFusedArgs& a, bool tau, hipStream_t st) {
     const int nk = (a.ld + 63) / 64;
-#define BLSTM_CLASSES(NK) return tau ? classes_nk<NK, true>(a, st) : classes_nk<NK, false>(a, st)
+#define BLSTM_CLASSES(NK) return a.entries ? (tau ? classes_nk<NK, true, true>(a, st) : classes_nk<NK, false, true>(a, st)) : classes_nk<NK, false, false>(a, st)
     if (nk == 1) BLSTM_CLASSES(1);
     if (nk == 2) BLSTM_CLASSES(2);
     if (nk == 3) BLSTM_CLASSES(3);
@@ -491,6 +684,15 @@ hipError_t launch_loss_dz(const LossDzArgs& a, bool known, hipStream_t st) {
     if (a.policy) hipLaunchKernelGGL((loss_dz_kernel<false, true>), grid, dim3(256), 0, st, a, p, t);
     else if (known) hipLaunchKernelGGL((loss_dz_kernel<true, false>), grid, dim3(256), 0, st, a, p, t);
     else hipLaunchKernelGGL((loss_dz_kernel<false, false>), grid, dim3(256), 0, st, a, p, t);
+    return hipGetLastError();
+}
+hipError_t launch_loss_lists(const LossListArgs& a, hipStream_t st) {
+    const int ntv = (a.V + 127) / 128;
+    hipLaunchKernelGGL(loss_offsets_kernel, dim3(1), dim3(1024), 0, st, a.count, a.from, (a.M + 63) / 64 * ntv);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const long long n = (long long)a.M * a.K, blocks = (n + 255) / 256;
+    hipLaunchKernelGGL(loss_lists_kernel, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st, a.classes, a.q, a.weight, n, a.K, ntv, a.count, a.from, a.entries);
     return hipGetLastError();
 }
 hipError_t launch_loss_classes_sum(const float* p, const float* pb, int parts, long long n, int V, float* out, float* out_b, hipStream_t st) {

@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void loss_prep_kernel(LossPrepArgs a) {
         const int first = (a.M + 3) / 4;                 // workgroups behind the rows': the bias
         if ((int)blockIdx.x >= first) {
             const int v = ((int)blockIdx.x - first) * 256 + (int)threadIdx.x;
-            if (v < ((a.V + 63) & ~63)) a.bias_f[v] = v < a.V ? bf2f(a.bias[v]) : -INFINITY;
+            if (v < ((a.V + 63) & ~63)) a.bias_f[v] = v < a.V ? bf2f(a.bias[v]) : a.bias_pad;
             return;
         }
     }
@@ -133,9 +133,19 @@ __global__ __launch_bounds__(256) void loss_prep_kernel(LossPrepArgs a) {
                 const float v = c >= 0 ? logit(c) : 0.0f;
                 if (l16 == 0 && k < a.teacher.K) {
                     a.entry_logit[m * a.teacher.K + k] = v;
-                    a.entry_q[m * a.teacher.K + k] = s.q[k];
                     if (c >= 0) part += s.q[k] * (s.log_q[k] - v * a.teacher.inv_tau);
                 }
+            }
+            for (int k = lane; k < a.teacher.K; k += 64) {
+                const int c = s.cls[k];
+                float q = 0.0f;
+                if (c >= 0 && s.q[k] > 0.0f) {
+                    bool first = true;
+                    for (int j = 0; j < k; ++j) first &= s.cls[j] != c || !(s.q[j] > 0.0f);
+                    if (first) q = class_weight(s, a.teacher.K, k);
+                }
+                a.entry_q[m * a.teacher.K + k] = q;
+                if (a.tile_count && q > 0.0f) atomicAdd(&a.tile_count[(m >> 6) * ((a.V + 127) >> 7) + (c >> 7)], 1);
             }
             part = l16 == 0 ? part : 0.0f;
             part = wave_sum(part);
@@ -175,7 +185,16 @@ __global__ __launch_bounds__(512) void loss_merge_kernel(LossMergeArgs a, Policy
     sh_sum[wave][lane] = sum;
     if (TAU) sh_tau[wave][lane] = tau;
     __syncthreads();
-    if (wave != 0 || !in) return;
+    if (wave != 0) return;
+    auto put = [&](const LossRow& r) {
+        const float x[6] = {r.m2, r.a, r.mt2, r.at, r.hot, __builtin_bit_cast(float, r.label)};
+#pragma unroll
+        for (int i = 0; i < 6; ++i) a.consts[i * (long long)a.Mp + m] = x[i];
+    };
+    if (!in) {
+        if (a.consts && m < a.Mp) { LossRow r{}; r.m2 = INFINITY; r.mt2 = INFINITY; r.label = -1; put(r); }
+        return;
+    }
     sum = 0.0f; tau = 0.0f;
 #pragma unroll
     for (int w = 0; w < 8; ++w) { sum += sh_sum[w][lane]; if (TAU) tau += sh_tau[w][lane]; }
@@ -186,7 +205,7 @@ __global__ __launch_bounds__(512) void loss_merge_kernel(LossMergeArgs a, Policy
     const float up = far ? a.label_logit[m] - mx : fmaf(a.label_logit[m], LOG2E, -m2) * LN2;
     const float lp = lab_ok ? up - logf(sum) : lab == -1 ? 0.0f : nan;
     if (a.logp) a.logp[m] = lp;
-    if (!a.rows) return;
+    if (!a.rows && !a.consts) return;
     LossRow r{};
     r.m2 = INFINITY; r.mt2 = INFINITY; r.label = -1; r.max = INFINITY;
     float loss = 0.0f;
@@ -214,7 +233,7 @@ __global__ __launch_bounds__(512) void loss_merge_kernel(LossMergeArgs a, Policy
     }
     if (r.a != 0.0f || r.at != 0.0f) r.max = mx;         // (a NaN is not 0)
     a.row_loss[m] = loss;
-    a.rows[m] = r;
+    if (a.consts) put(r); else a.rows[m] = r;
 }
 
 // ---- the teacher's entries of du: a wavefront a row -------------------------------------------------------------------
@@ -240,9 +259,9 @@ __global__ __launch_bounds__(256) void loss_entries_kernel(LossEntriesArgs a) {
         const bool far = fabsf(r.max) > LOSS_FAR;
         float v = r.a * __builtin_amdgcn_exp2f(far ? (u - r.max) * LOG2E : fmaf(u, LOG2E, -r.m2)) + r.at * __builtin_amdgcn_exp2f(far ? (u - r.max) * lt : fmaf(u, lt, -r.mt2));
         if (c == r.label) v -= r.hot;
-        v -= a.weight * class_weight(s, a.K, k);
+        v -= a.weight * s.q[k];
         const bf16_t hi = f2bf(v);
-        a.hi[m * a.ldu + c] = hi;                        // (of entries with one class each writes the same)
+        a.hi[m * a.ldu + c] = hi;
         a.lo[m * a.ldu + c] = f2bf(v - bf2f(hi));
     }
 }
