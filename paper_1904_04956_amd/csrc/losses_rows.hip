@@ -7,6 +7,7 @@
 //            dl/du = h (p - 1_y) + w tau (p' - sum_k q_k 1_k)
 #include "common.hpp"
 #include "losses_terms.hpp"
+#include <type_traits>
 
 namespace blstm {
 namespace {
@@ -104,36 +105,80 @@ __global__ __launch_bounds__(256) void loss_prep_kernel(LossPrepArgs a) {
     }
     if (!a.W) return;
     if constexpr (sizeof(T) == 2) {
-        // sixteen lanes a product, eight elements a lane and step
+        // sixteen lanes a product, eight elements a lane and step; the row's elements of up to PREP_STEPS steps stay in registers
+        constexpr int PREP_STEPS = 4;
         const int l16 = lane & 15, g = lane >> 4;
-        auto logit = [&](int c) {
-            float acc = 0.0f;
-            const bf16_t* w = a.W + (long long)c * a.ldzc;   // (zeros behind Z)
-            for (int k = l16 * 8; k < a.Z; k += 128) {
-                const uint4 wv = *reinterpret_cast<const uint4*>(w + k);
-                const uint32_t ww[4] = {wv.x, wv.y, wv.z, wv.w};
+        typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+        auto row_words = [&](int k) {
+            uint4 r = make_uint4(0, 0, 0, 0);
+            if (k + 8 <= a.Z && a.Z % 8 == 0) r = *reinterpret_cast<const uint4*>(z + k);
+            else if (k < a.Z) {
+                uint32_t w[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int e = k + 2 * q;
-                    if (e < a.Z) acc = fmaf(bf2f(z[e]), bf2f((bf16_t)(ww[q] & 0xFFFFu)), acc);
-                    if (e + 1 < a.Z) acc = fmaf(bf2f(z[e + 1]), bf2f((bf16_t)(ww[q] >> 16)), acc);
+                for (int q = 0; q < 4; ++q)
+                    w[q] = (k + 2 * q < a.Z ? (uint32_t)z[k + 2 * q] : 0u) | (k + 2 * q + 1 < a.Z ? (uint32_t)z[k + 2 * q + 1] << 16 : 0u);
+                r = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            return r;
+        };
+        uint4 zr[PREP_STEPS];
+#pragma unroll
+        for (int i = 0; i < PREP_STEPS; ++i) zr[i] = row_words(l16 * 8 + 128 * i);
+        auto dot = [](const uint4& x, const uint4& w, float acc) {
+            acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x.x), __builtin_bit_cast(bf16x2_t, w.x), acc, false);
+            acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x.y), __builtin_bit_cast(bf16x2_t, w.y), acc, false);
+            acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x.z), __builtin_bit_cast(bf16x2_t, w.z), acc, false);
+            return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x.w), __builtin_bit_cast(bf16x2_t, w.w), acc, false);
+        };
+        // the logits of COUNT classes at once (below 0: none, 0)
+        auto logits = [&](auto count, const int (&c)[4], float (&u)[4]) __attribute__((always_inline)) {
+            constexpr int COUNT = decltype(count)::value;
+#pragma unroll
+            for (int n = 0; n < COUNT; ++n) u[n] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < PREP_STEPS; ++i) {
+                const int k = l16 * 8 + 128 * i;
+                if (128 * i < a.ldzc) {
+                    uint4 w[COUNT];
+#pragma unroll
+                    for (int n = 0; n < COUNT; ++n) w[n] = k < a.ldzc && c[n] >= 0 ? *reinterpret_cast<const uint4*>(a.W + (long long)c[n] * a.ldzc + k) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int n = 0; n < COUNT; ++n) u[n] = dot(zr[i], w[n], u[n]);
                 }
             }
+            for (int k = l16 * 8 + 128 * PREP_STEPS; k < a.ldzc; k += 128) {
+                const uint4 x = row_words(k);
 #pragma unroll
-            for (int o = 8; o > 0; o >>= 1) acc += __shfl_xor(acc, o, 64);
-            return acc + bf2f(a.bias[c]);
+                for (int n = 0; n < COUNT; ++n) if (c[n] >= 0) u[n] = dot(x, *reinterpret_cast<const uint4*>(a.W + (long long)c[n] * a.ldzc + k), u[n]);
+            }
+#pragma unroll
+            for (int n = 0; n < COUNT; ++n) {
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) u[n] += __shfl_xor(u[n], o, 64);
+                if (c[n] >= 0) u[n] += bf2f(a.bias[c[n]]);
+            }
         };
-        const float u = lab_ok ? logit(lab) : 0.0f;
-        if (lane == 0) a.label_logit[m] = u;
+        {
+            const int c[4] = {lab_ok ? lab : -1, -1, -1, -1};
+            float u[4];
+            logits(std::integral_constant<int, 1>{}, c, u);
+            if (lane == 0) a.label_logit[m] = u[0];
+        }
         if (a.teacher.K > 0) {
             float part = 0.0f;
-            for (int k0 = 0; k0 < a.teacher.K; k0 += 4) {
-                const int k = k0 + g;
-                const int c = k < a.teacher.K ? s.cls[k] : -1;
-                const float v = c >= 0 ? logit(c) : 0.0f;
-                if (l16 == 0 && k < a.teacher.K) {
-                    a.entry_logit[m * a.teacher.K + k] = v;
-                    if (c >= 0) part += s.q[k] * (s.log_q[k] - v * a.teacher.inv_tau);
+            for (int k0 = 0; k0 < a.teacher.K; k0 += 16) {
+                int c[4];
+                float u[4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) { const int k = k0 + 4 * n + g; c[n] = k < a.teacher.K ? s.cls[k] : -1; }
+                logits(std::integral_constant<int, 4>{}, c, u);
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const int k = k0 + 4 * n + g;
+                    if (l16 == 0 && k < a.teacher.K) {
+                        a.entry_logit[m * a.teacher.K + k] = u[n];
+                        if (c[n] >= 0) part += s.q[k] * (s.log_q[k] - u[n] * a.teacher.inv_tau);
+                    }
                 }
             }
             for (int k = lane; k < a.teacher.K; k += 64) {
