@@ -414,7 +414,7 @@ struct LossScratch {
     bool strips;              // largest logits: by the strips' maxima
     bool fused;               // the kernels of losses_fused.hip: no du in memory
     int row_parts, sum_parts, class_parts;
-    size_t bias_f, consts, part, part_ref, part_sum, part_sum2, cparts, cparts_b, tile_count, tile_from, entries;
+    size_t bias_f, consts, part, part_ref, part_sum, part_sum2, cparts, cparts_b, tile_count, tile_left, tile_from, entries;
     size_t zc, wp, dzp, dwp, label_logit, entry_logit, entry_q, soft_const, soft_state, pmax, psum, ptau, rows, row_loss, hi, lo, u, partial, partial_bytes, bytes;
 };
 static_assert(BLSTM_MAX_TOP == LOSS_MAX_TOP, "the kernels' lists must hold every entry");
@@ -480,8 +480,9 @@ LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
                 put(&l.entry_q, M * K * 4);
                 put(&l.soft_const, M * 4);
                 put(&l.soft_state, M * 4);
-                put(&l.tile_count, tiles * 4);
-                put(&l.tile_from, (tiles + 1) * 4);
+                put(&l.tile_count, (tiles + 1) * 4);
+                put(&l.tile_left, tiles * 4);
+                put(&l.tile_from, tiles * 4);
                 put(&l.entries, (M * K + LOSS_LIST_SLACK) * 8);
             }
             l.bytes = w;
@@ -627,7 +628,7 @@ int loss_run_fused(blstm_ctx* ctx, const LossCall& c, const int32_t* labels, con
     if (teacher) {
         LossListArgs e{};
         e.M = ctx->M; e.V = ctx->V; e.K = teacher->K; e.classes = teacher->classes; e.q = c.at<float>(l.entry_q); e.weight = ctx->s * teacher->soft * teacher->tau;
-        e.count = c.at<int>(l.tile_count); e.from = c.at<int>(l.tile_from); e.entries = c.at<uint2>(l.entries);
+        e.count = c.at<int>(l.tile_count); e.left = c.at<int>(l.tile_left); e.from = c.at<int>(l.tile_from); e.entries = c.at<uint2>(l.entries);
         RUN(PC_SOFTMAX_ROWS, "the teacher's classes by tiles", launch_loss_lists(e, st));
     }
     if (!gradient || both) {
@@ -662,7 +663,7 @@ int loss_run_fused(blstm_ctx* ctx, const LossCall& c, const int32_t* labels, con
     f.out = l.class_parts > 1 ? c.at<float>(l.cparts) : dw; f.out_db = l.class_parts > 1 ? c.at<float>(l.cparts_b) : db;
     f.ldo = ctx->zdim; f.vec = ctx->zdim % 4 == 0 && aligned16(f.out);
     if (!both) f.k1 = f.k;                               // (the only exponential is the first)
-    if (teacher) { f.entries = c.at<uint2>(l.entries); f.entries_from = c.at<int>(l.tile_from); }
+    if (teacher) { f.entries = c.at<uint2>(l.entries); f.entries_from = c.at<int>(l.tile_from); f.entries_count = c.at<int>(l.tile_count); }
     RUN(PC_GEMM_SOFTMAX_BWD, "dW_s", launch_loss_fused_classes(f, both, st));
     if (l.class_parts > 1)
         RUN(PC_GEMM_SOFTMAX_BWD, "dW_s", launch_loss_classes_sum(f.out, f.out_db, f.parts, (long long)ctx->V * ctx->zdim, ctx->V, dw, db, st));
@@ -692,7 +693,7 @@ int loss_run(blstm_ctx* ctx, const LossCall& given, const int32_t* labels, const
                 a.bias_f = c.at<float>(l.bias_f); a.bias_pad = -INFINITY;
                 if (teacher) {
                     a.tile_count = c.at<int>(l.tile_count);
-                    RUN(PC_MISC, "counts", launch_fill_u32(reinterpret_cast<unsigned*>(a.tile_count), (int)loss_tiles(M, V), 0u, st));
+                    RUN(PC_MISC, "counts", launch_fill_u32(reinterpret_cast<unsigned*>(a.tile_count), (int)loss_tiles(M, V) + 1, 0u, st));
                 }
             }
             a.entry_logit = c.at<float>(l.entry_logit); a.entry_q = c.at<float>(l.entry_q);

@@ -51,7 +51,7 @@ struct LossPrepArgs {
     const unsigned short* bias;
     float* bias_f;                                   // [V rounded up to 64] the bias as floats, bias_pad behind it; or null
     float bias_pad;
-    int* tile_count;                                 // entries by tiles of 64 rows and 128 classes, zero before the launch; or null
+    int* tile_count;                                 // numbers of entries by tiles of 64 rows and 128 classes, zero before the launch; or null
     const int32_t* labels;                           // or null
     float* label_logit;                              // [M]
     TeacherArgs teacher;                             // K = 0: none
@@ -99,7 +99,8 @@ struct LossFusedArgs {
     float* part_sum2;                                // sums: at the scale k
     float* out_db;                                   // classes: [parts][V]
     const uint2* entries;                            // classes: the teacher's, row | class << 6 within a tile and weight q, by tiles of 64 rows and 128 classes; or null
-    const int* entries_from;                         // [tiles + 1]
+    const int* entries_from;                         // [tiles] where a tile's lie, and how many
+    const int* entries_count;
     long long ldo;
     int vec;                                         // classes: rows of out take 16-byte stores
 };
@@ -130,15 +131,16 @@ struct LossDzArgs {
     unsigned short* dz;                              // [M][Z]
 };
 hipError_t launch_loss_dz(const LossDzArgs& a, bool known, hipStream_t st);
-// The teacher's entries in order of their tiles, from the tiles' counts (which become zero).  entries: room for M K, and 256 more that are read.
+// The teacher's entries by tiles, from the tiles' counts.  entries: room for M K, and 256 more that are read.
 constexpr int LOSS_LIST_SLACK = 256;
 struct LossListArgs {
     int M, V, K;
     const int32_t* classes;
     const float* q;                                  // [M][K], 0: none
     float weight;
-    int* count;                                      // [tiles]
-    int* from;                                       // [tiles + 1]
+    int* count;                                      // [tiles + 1], the last one zero before the launch
+    int* left;                                       // [tiles]
+    int* from;                                       // [tiles]
     uint2* entries;
 };
 hipError_t launch_loss_lists(const LossListArgs& a, hipStream_t st);

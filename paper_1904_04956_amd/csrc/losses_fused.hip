@@ -327,7 +327,7 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
         const int c = 2 * q + half;
         wf[q] = c * 8 < a.ld ? *reinterpret_cast<const uint4*>(a.W + (long long)min(v, a.V - 1) * a.ld + c * 8) : make_uint4(0, 0, 0, 0);
     }
-    const float b = v < a.V ? a.bias[v] : -INFINITY, k1 = a.k1, b2 = b * k1, bt = b * a.k, k = a.k;
+    const float b = v < a.V ? a.bias[v] : -INFINITY, k1 = a.k1, k = a.k;
     __builtin_amdgcn_s_waitcnt(0);                      // (known to the compiler: it would wait for these loads, and the ring's with them, in the loop)
     auto issue = [&](int it) __attribute__((always_inline)) {
         const unsigned s = lds0 + (unsigned)(it % R::STAGES * STAGE);
@@ -355,6 +355,32 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
         const char* stage = reinterpret_cast<const char*>(smem) + it % R::STAGES * STAGE;
         const char* s = stage + rh * 32 * R::ROWB;
         const float* consts = reinterpret_cast<const float*>(stage + R::TILE) + rh * 32;   // [6][64]
+        // the teacher's entries of these rows and classes, one a lane (and more where there are more)
+        int listed = 0, spot = -1;
+        auto spot_of = [&](const uint2& e) { return (int)(e.x >> 5 & 1u) == rh && (int)(e.x >> 11) == cg ? (int)(e.x >> 6 & 31u) * SPOT + (int)(e.x & 31u) : -1; };
+        auto others = [&](bool clear) {
+            const int from = ((const_int)(uintptr_t)a.entries_from)[(long long)(t0 + it) * ntv + ct];
+            bool any = false;
+            for (int k = 64 + fresh_lane(); k < listed; k += 64) {
+                const uint2 e = k < R::LIST / 8 ? reinterpret_cast<const uint2*>(stage + R::STAGE)[k] : a.entries[from + k];
+                const int to = spot_of(e);
+                if (to >= 0) { spots[to] = clear ? 0.0f : __builtin_bit_cast(float, e.y); any = true; }
+            }
+            return any;
+        };
+        bool any_spot = false;
+        if constexpr (ENTRIES) {
+            listed = ((const_int)(uintptr_t)a.entries_count)[(long long)(t0 + it) * ntv + ct];
+            const int ln = fresh_lane();
+            if (ln < listed) {
+                const uint2 e = reinterpret_cast<const uint2*>(stage + R::STAGE)[ln];
+                spot = spot_of(e);
+                if (spot >= 0) spots[spot] = __builtin_bit_cast(float, e.y);
+            }
+            any_spot = spot >= 0;
+            if (listed > 64) any_spot |= others(false);
+            any_spot = __any(any_spot);
+        }
         f32x16_t u;
 #pragma unroll
         for (int e = 0; e < 16; ++e) u[e] = 0.0f;
@@ -362,29 +388,6 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
         for (int q = 0; q < 4 * NK; ++q) u = mma32(at.by_row(s, q), wf[q], u);
         ahead<DEPTH, 4 * NK, 1, 1, DEPTH>();
         __builtin_amdgcn_sched_barrier(0);
-        // the teacher's entries of these rows and classes
-        int listed = 0;
-        bool any_spot = false;
-        auto spread = [&](bool clear) {
-            const int from = ((const_int)(uintptr_t)a.entries_from)[(long long)(t0 + it) * ntv + ct];
-            const int ln = fresh_lane();
-            for (int k = ln; k < listed; k += 64) {
-                const uint2 e = k < R::LIST / 8 ? reinterpret_cast<const uint2*>(stage + R::STAGE)[k] : a.entries[from + k];
-                const int r = (int)(e.x & 63u), cl = (int)(e.x >> 6);
-                if (r >> 5 != rh || cl >> 5 != cg) continue;
-                spots[(cl & 31) * SPOT + (r & 31)] = clear ? 0.0f : __builtin_bit_cast(float, e.y);
-                any_spot = true;
-            }
-        };
-        if constexpr (ENTRIES) {
-            const const_int at_ = (const_int)(uintptr_t)a.entries_from + (long long)(t0 + it) * ntv + ct;
-            listed = at_[1] - at_[0];
-            spread(false);
-            any_spot = __any(any_spot);
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        }
         // a label among these classes: one product of 32 x 32 in V / 1024
         const int* labels = reinterpret_cast<const int*>(consts + 320);
         const bool any_hot = __any((unsigned)(labels[fresh_lane() & 31] - class0) < 32u);
@@ -397,15 +400,16 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
                 const float4 m2 = *reinterpret_cast<const float4*>(consts + r), ca = *reinterpret_cast<const float4*>(consts + 64 + r);
                 const float ms[4] = {m2.x, m2.y, m2.z, m2.w}, cs[4] = {ca.x, ca.y, ca.z, ca.w};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) d[4 * h + i] = cs[i] * __builtin_amdgcn_exp2f(fmaf(u[8 * t + 4 * h + i], k1, b2 - ms[i]));
+                for (int i = 0; i < 4; ++i) d[4 * h + i] = cs[i] * __builtin_amdgcn_exp2f(fmaf(u[8 * t + 4 * h + i] + b, k1, -ms[i]));
                 if (TAU) {
                     const float4 mt = *reinterpret_cast<const float4*>(consts + 128 + r), ct_ = *reinterpret_cast<const float4*>(consts + 192 + r);
                     const float mts[4] = {mt.x, mt.y, mt.z, mt.w}, cts[4] = {ct_.x, ct_.y, ct_.z, ct_.w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) d[4 * h + i] = fmaf(cts[i], __builtin_amdgcn_exp2f(fmaf(u[8 * t + 4 * h + i], k, bt - mts[i])), d[4 * h + i]);
+                    for (int i = 0; i < 4; ++i) d[4 * h + i] = fmaf(cts[i], __builtin_amdgcn_exp2f(fmaf(u[8 * t + 4 * h + i] + b, k, -mts[i])), d[4 * h + i]);
                 }
             }
             if (ENTRIES && any_spot) {
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float4 x = *reinterpret_cast<const float4*>(spots + (fresh_lane() & 31) * SPOT + 8 * (2 * t + h) + 4 * half);
@@ -448,7 +452,10 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (ENTRIES && any_spot) spread(true);          // (a wavefront's LDS accesses keep their order)
+        if (ENTRIES && any_spot) {                      // (a wavefront's LDS accesses keep their order)
+            if (spot >= 0) spots[spot] = 0.0f;
+            if (listed > 64) others(true);
+        }
     }
     const int ln = fresh_lane(), n32 = ln & 31, hf = ln >> 5, cls = ct * 128 + cg * 32 + n32;
     // the two halves of the rows together, through LDS; register e of a lane: column 32 zb + 8 (e / 4) + 4 half + e % 4 of class l32
@@ -483,40 +490,31 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
 }
 
 // ---- a teacher's entries by tiles of 64 rows and 128 classes --------------------------------------------------------------------
-// (their numbers are counted by loss_prep_kernel) from[i] = sum of count[0 .. i - 1], from[n] the sum of all; one workgroup.
-__global__ __launch_bounds__(1024) void loss_offsets_kernel(const int* count, int* from, int n) {
-    __shared__ int sh[16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int run = 0;
-    for (int i0 = 0; i0 < n; i0 += 8192) {
-        int x[8], own = 0;
-        const int i = i0 + (int)threadIdx.x * 8;
+// (Their numbers are counted by loss_prep_kernel.)  A place for every tile's list, wherever it comes to lie: the workgroups take theirs from one
+// counter (in order of the tiles, by one workgroup, 21000 tiles took 21 us).
+__global__ __launch_bounds__(256) void loss_places_kernel(const int* count, int* left, int* from, int* taken, int n) {
+    __shared__ int sh[5];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = (int)blockIdx.x * 256 + (int)threadIdx.x;
+    const int own = i < n ? count[i] : 0;
+    int before = own;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) { x[k] = i + k < n ? count[i + k] : 0; own += x[k]; }
-        int before = own;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) { const int t = __shfl_up(before, o, 64); if (lane >= o) before += t; }
-        __syncthreads();
-        if (lane == 63) sh[wave] = before;
-        __syncthreads();
-        int all = 0;
-        before += run - own;
-#pragma unroll
-        for (int w = 0; w < 16; ++w) { if (w < wave) before += sh[w]; all += sh[w]; }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) { if (i + k < n) from[i + k] = before; before += x[k]; }
-        run += all;
-    }
-    if (threadIdx.x == 0) from[n] = run;
+    for (int o = 1; o < 64; o <<= 1) { const int t = __shfl_up(before, o, 64); if (lane >= o) before += t; }
+    if (lane == 63) sh[wave] = before;
+    __syncthreads();
+    if (threadIdx.x == 0) sh[4] = atomicAdd(taken, sh[0] + sh[1] + sh[2] + sh[3]);
+    __syncthreads();
+    before += sh[4] - own;
+    for (int w = 0; w < wave; ++w) before += sh[w];
+    if (i < n) { from[i] = before; left[i] = own; }
 }
 // Puts every entry with a probability into its tile's list (whose order is of no matter: a row's classes are different ones).
-__global__ __launch_bounds__(256) void loss_lists_kernel(const int32_t* classes, const float* q, float weight, long long n, int K, int ntv, int* count, const int* from, uint2* entries) {
+__global__ __launch_bounds__(256) void loss_lists_kernel(const int32_t* classes, const float* q, float weight, long long n, int K, int ntv, int* left, const int* from, uint2* entries) {
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
         const float p = q[i];
         if (!(p > 0.0f)) continue;
         const int m = (int)(i / K), c = classes[i];
         const long long b = (long long)(m >> 6) * ntv + (c >> 7);
-        const int to = from[b] + atomicSub(&count[b], 1) - 1;
+        const int to = from[b] + atomicSub(&left[b], 1) - 1;
         entries[to] = make_uint2((unsigned)(m & 63) | (unsigned)(c & 127) << 6, __builtin_bit_cast(unsigned, weight * p));
     }
 }
@@ -538,11 +536,12 @@ __global__ __launch_bounds__(256) void loss_classes_sum_kernel(const float* __re
 // KNOWN: the rows' constants and losses are there and the parts are sums of du W; else they are made here from the parts' references
 // and sums, which are brought to the largest reference.  All loads of a step are independent: one by one, 128 parts and 64 classes
 // took 49 us for 168 rows.
-template <bool KNOWN, bool POLICY>
+// SHARE: wavefronts a row, four or, where rows are many, one (43008 rows: 69 us with four, 29 with one).
+template <bool KNOWN, bool POLICY, int SHARE>
 __global__ __launch_bounds__(256) void loss_dz_kernel(LossDzArgs a, PolicyArgs policy, TeacherArgs teacher) {
     __shared__ float4 sh[3][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const long long m = blockIdx.x;
+    const int lane = threadIdx.x & 63, wf = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = SHARE == 4 ? wf : 0;
+    const long long m = SHARE == 4 ? (long long)blockIdx.x : (long long)blockIdx.x * 4 + wf;
     if (m >= a.M) {                                      // the last tile's rows that are none
         if (wave == 0 && lane < 6) a.consts[lane * (long long)a.Mp + m] = lane == 0 || lane == 2 ? INFINITY : lane == 5 ? __builtin_bit_cast(float, -1) : 0.0f;
         return;
@@ -573,7 +572,7 @@ __global__ __launch_bounds__(256) void loss_dz_kernel(LossDzArgs a, PolicyArgs p
                 const PolicyTerms t = policy_terms(policy, m, lp);
                 loss = a.s * t.loss; c1 = -a.s * t.g / sum; hot = -a.s * t.g;
             } else if (lab != -1) loss = nan;
-            if (a.logp && threadIdx.x == 0) a.logp[m] = lp;
+            if (a.logp && wave == 0 && lane == 0) a.logp[m] = lp;
         } else {
             const int state = a.soft_state[m];
             some = state & 1;
@@ -589,7 +588,7 @@ __global__ __launch_bounds__(256) void loss_dz_kernel(LossDzArgs a, PolicyArgs p
         if (!lab_ok) lab = -1;
         if (wave == 0 && lane < 6)
             a.consts[lane * (long long)a.Mp + m] = lane == 0 ? (counts ? m2 : INFINITY) : lane == 1 ? c1 : lane == 2 ? INFINITY : lane == 3 ? 0.0f : lane == 4 ? hot : __builtin_bit_cast(float, lab);
-        if (threadIdx.x == 0) a.row_loss[m] = loss;
+        if (wave == 0 && lane == 0) a.row_loss[m] = loss;
     }
     const bool lab_ok = (unsigned)lab < (unsigned)a.V, counts = KNOWN || lab_ok || some;
     const bool in = lane * 4 < a.ld;
@@ -603,11 +602,11 @@ __global__ __launch_bounds__(256) void loss_dz_kernel(LossDzArgs a, PolicyArgs p
             x[0] = fmaf(v.x, w, x[0]); x[1] = fmaf(v.y, w, x[1]); x[2] = fmaf(v.z, w, x[2]); x[3] = fmaf(v.w, w, x[3]);
         };
         int p = wave;
-        for (; p + 28 < a.parts; p += 32) {
+        for (; p + 7 * SHARE < a.parts; p += 8 * SHARE) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) add_part(p + 4 * k);
+            for (int k = 0; k < 8; ++k) add_part(p + SHARE * k);
         }
-        for (; p < a.parts; p += 4) add_part(p);
+        for (; p < a.parts; p += SHARE) add_part(p);
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] *= c1;
         auto add = [&](int c, float w) {                 // w W_c
@@ -624,19 +623,22 @@ __global__ __launch_bounds__(256) void loss_dz_kernel(LossDzArgs a, PolicyArgs p
                 const float q = have ? a.entry_q[m * teacher.K + k0 + lane] : 0.0f;
                 const int c = q > 0.0f ? teacher.classes[m * teacher.K + k0 + lane] : 0;
                 const float w = -weight * q;
-                for (int j = wave; j < 64 && k0 + j < teacher.K; j += 16) {
+                for (int j = wave; j < 64 && k0 + j < teacher.K; j += 4 * SHARE) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        add(__builtin_amdgcn_readlane(c, j + 4 * i), __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), j + 4 * i)));
+                        add(__builtin_amdgcn_readlane(c, j + SHARE * i), __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), j + SHARE * i)));
                 }
             }
         }
     }
-    if (wave > 0) sh[wave - 1][lane] = make_float4(x[0], x[1], x[2], x[3]);
-    __syncthreads();
-    if (wave > 0 || !in) return;
+    if constexpr (SHARE == 4) {
+        if (wave > 0) sh[wave - 1][lane] = make_float4(x[0], x[1], x[2], x[3]);
+        __syncthreads();
+        if (wave > 0) return;
 #pragma unroll
-    for (int w = 0; w < 3; ++w) { const float4 y = sh[w][lane]; x[0] += y.x; x[1] += y.y; x[2] += y.z; x[3] += y.w; }
+        for (int w = 0; w < 3; ++w) { const float4 y = sh[w][lane]; x[0] += y.x; x[1] += y.y; x[2] += y.z; x[3] += y.w; }
+    }
+    if (!in) return;
 #pragma unroll
     for (int i = 0; i < 4; ++i) if (z0 + i < a.Z) a.dz[m * a.Z + z0 + i] = f2bf(x[i]);
 }
@@ -698,22 +700,25 @@ hipError_t launch_loss_fused_classes(const LossFusedArgs& a, bool tau, hipStream
     BLSTM_CLASSES(4);
 #undef BLSTM_CLASSES
 }
-hipError_t launch_loss_dz(const LossDzArgs& a, bool known, hipStream_t st) {
-    const dim3 grid((unsigned)a.Mp);
+template <int SHARE>
+static hipError_t dz_shared(const LossDzArgs& a, bool known, hipStream_t st) {
+    const dim3 grid((unsigned)(SHARE == 4 ? a.Mp : a.Mp / 4));
     const PolicyArgs p = a.policy ? *a.policy : PolicyArgs{};
     const TeacherArgs t = a.teacher ? *a.teacher : TeacherArgs{};
-    if (a.policy) hipLaunchKernelGGL((loss_dz_kernel<false, true>), grid, dim3(256), 0, st, a, p, t);
-    else if (known) hipLaunchKernelGGL((loss_dz_kernel<true, false>), grid, dim3(256), 0, st, a, p, t);
-    else hipLaunchKernelGGL((loss_dz_kernel<false, false>), grid, dim3(256), 0, st, a, p, t);
+    if (a.policy) hipLaunchKernelGGL((loss_dz_kernel<false, true, SHARE>), grid, dim3(256), 0, st, a, p, t);
+    else if (known) hipLaunchKernelGGL((loss_dz_kernel<true, false, SHARE>), grid, dim3(256), 0, st, a, p, t);
+    else hipLaunchKernelGGL((loss_dz_kernel<false, false, SHARE>), grid, dim3(256), 0, st, a, p, t);
     return hipGetLastError();
 }
+hipError_t launch_loss_dz(const LossDzArgs& a, bool known, hipStream_t st) { return a.M <= 8192 ? dz_shared<4>(a, known, st) : dz_shared<1>(a, known, st); }
 hipError_t launch_loss_lists(const LossListArgs& a, hipStream_t st) {
     const int ntv = (a.V + 127) / 128;
-    hipLaunchKernelGGL(loss_offsets_kernel, dim3(1), dim3(1024), 0, st, a.count, a.from, (a.M + 63) / 64 * ntv);
+    const int tiles = (a.M + 63) / 64 * ntv;
+    hipLaunchKernelGGL(loss_places_kernel, dim3((unsigned)((tiles + 255) / 256)), dim3(256), 0, st, a.count, a.left, a.from, a.count + tiles, tiles);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const long long n = (long long)a.M * a.K, blocks = (n + 255) / 256;
-    hipLaunchKernelGGL(loss_lists_kernel, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st, a.classes, a.q, a.weight, n, a.K, ntv, a.count, a.from, a.entries);
+    hipLaunchKernelGGL(loss_lists_kernel, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st, a.classes, a.q, a.weight, n, a.K, ntv, a.left, a.from, a.entries);
     return hipGetLastError();
 }
 hipError_t launch_loss_classes_sum(const float* p, const float* pb, int parts, long long n, int V, float* out, float* out_b, hipStream_t st) {

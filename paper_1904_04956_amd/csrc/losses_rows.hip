@@ -199,38 +199,11 @@ __global__ __launch_bounds__(256) void loss_prep_kernel(LossPrepArgs a) {
     }
 }
 
-// ---- behind the sums of the strips: 64 rows a workgroup, its wavefronts share the strips ------------------------------
+// What a row's largest logit (or another reference) and its sums give, by one lane.  `in`: the row is none of those that fill the last tile.
 template <bool TAU, bool POLICY, bool TEACHER>
-__global__ __launch_bounds__(512) void loss_merge_kernel(LossMergeArgs a, PolicyArgs policy, TeacherArgs teacher) {
-    __shared__ float sh_max[8][64], sh_sum[8][64], sh_tau[8][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long m = (long long)blockIdx.x * 64 + lane;
-    const bool in = m < a.M;
-    float mx = -INFINITY;
-    if (in) {
-#pragma unroll 8
-        for (int i = wave; i < a.strips; i += 8) mx = fmaxf(mx, a.part_max[(long long)i * a.M + m]);
-    }
-    sh_max[wave][lane] = mx;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < 8; ++w) mx = fmaxf(mx, sh_max[w][lane]);
-    const float m2 = mx * LOG2E, lt = LOG2E * teacher.inv_tau, mt2 = TAU ? mx * lt : 0.0f;
+__device__ __forceinline__ void merge_end(const LossMergeArgs& a, const PolicyArgs& policy, const TeacherArgs& teacher, long long m, bool in, float mx, float sum, float tau) {
+    const float m2 = mx * LOG2E, mt2 = TAU ? mx * (LOG2E * teacher.inv_tau) : 0.0f;
     const bool far = fabsf(mx) > LOSS_FAR;
-    float sum = 0.0f, tau = 0.0f;
-    if (in) {
-#pragma unroll 4
-        for (int i = wave; i < a.strips; i += 8) {
-            const float pm = a.part_max[(long long)i * a.M + m];
-            const bool away = far || fabsf(pm) > LOSS_FAR;
-            sum += a.part_sum[(long long)i * a.M + m] * __builtin_amdgcn_exp2f(away ? (pm - mx) * LOG2E : pm * LOG2E - m2);
-            if (TAU) tau += a.part_sum_tau[(long long)i * a.M + m] * __builtin_amdgcn_exp2f(away ? (pm - mx) * lt : pm * lt - mt2);
-        }
-    }
-    sh_sum[wave][lane] = sum;
-    if (TAU) sh_tau[wave][lane] = tau;
-    __syncthreads();
-    if (wave != 0) return;
     auto put = [&](const LossRow& r) {
         const float x[6] = {r.m2, r.a, r.mt2, r.at, r.hot, __builtin_bit_cast(float, r.label)};
 #pragma unroll
@@ -240,9 +213,6 @@ __global__ __launch_bounds__(512) void loss_merge_kernel(LossMergeArgs a, Policy
         if (a.consts && m < a.Mp) { LossRow r{}; r.m2 = INFINITY; r.mt2 = INFINITY; r.label = -1; put(r); }
         return;
     }
-    sum = 0.0f; tau = 0.0f;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) { sum += sh_sum[w][lane]; if (TAU) tau += sh_tau[w][lane]; }
     const int lab = a.labels ? a.labels[m] : -1;
     const bool lab_ok = (unsigned)lab < (unsigned)a.V;
     const float nan = __builtin_nanf("");
@@ -279,6 +249,66 @@ __global__ __launch_bounds__(512) void loss_merge_kernel(LossMergeArgs a, Policy
     if (r.a != 0.0f || r.at != 0.0f) r.max = mx;         // (a NaN is not 0)
     a.row_loss[m] = loss;
     if (a.consts) put(r); else a.rows[m] = r;
+}
+
+// ---- behind the sums of the strips: 64 rows a workgroup, its wavefronts share the strips ------------------------------
+template <bool TAU, bool POLICY, bool TEACHER>
+__global__ __launch_bounds__(512) void loss_merge_kernel(LossMergeArgs a, PolicyArgs policy, TeacherArgs teacher) {
+    __shared__ float sh_max[8][64], sh_sum[8][64], sh_tau[8][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long m = (long long)blockIdx.x * 64 + lane;
+    const bool in = m < a.M;
+    float mx = -INFINITY;
+    if (in) {
+#pragma unroll 8
+        for (int i = wave; i < a.strips; i += 8) mx = fmaxf(mx, a.part_max[(long long)i * a.M + m]);
+    }
+    sh_max[wave][lane] = mx;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 8; ++w) mx = fmaxf(mx, sh_max[w][lane]);
+    const float m2 = mx * LOG2E, lt = LOG2E * teacher.inv_tau, mt2 = TAU ? mx * lt : 0.0f;
+    const bool far = fabsf(mx) > LOSS_FAR;
+    float sum = 0.0f, tau = 0.0f;
+    if (in) {
+#pragma unroll 4
+        for (int i = wave; i < a.strips; i += 8) {
+            const float pm = a.part_max[(long long)i * a.M + m];
+            const bool away = far || fabsf(pm) > LOSS_FAR;
+            sum += a.part_sum[(long long)i * a.M + m] * __builtin_amdgcn_exp2f(away ? (pm - mx) * LOG2E : pm * LOG2E - m2);
+            if (TAU) tau += a.part_sum_tau[(long long)i * a.M + m] * __builtin_amdgcn_exp2f(away ? (pm - mx) * lt : pm * lt - mt2);
+        }
+    }
+    sh_sum[wave][lane] = sum;
+    if (TAU) sh_tau[wave][lane] = tau;
+    __syncthreads();
+    if (wave != 0) return;
+    sum = 0.0f; tau = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) { sum += sh_sum[w][lane]; if (TAU) tau += sh_tau[w][lane]; }
+    merge_end<TAU, POLICY, TEACHER>(a, policy, teacher, m, in, mx, sum, tau);
+}
+
+// ---- the same, a wavefront a row: for few parts (a part a lane) ----------------------------------------------------------------
+template <bool TAU, bool TEACHER>
+__global__ __launch_bounds__(256) void loss_merge_row_kernel(LossMergeArgs a, TeacherArgs teacher) {
+    const int lane = threadIdx.x & 63;
+    const long long m = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const bool in = m < a.M;
+    float mx = -INFINITY, sum = 0.0f, tau = 0.0f;
+    if (in) {
+        for (int i = lane; i < a.strips; i += 64) mx = fmaxf(mx, a.part_max[(long long)i * a.M + m]);
+        mx = wave_max(mx);
+        const float lt = LOG2E * teacher.inv_tau;
+        for (int i = lane; i < a.strips; i += 64) {
+            const float d = a.part_max[(long long)i * a.M + m] - mx;
+            sum += a.part_sum[(long long)i * a.M + m] * __builtin_amdgcn_exp2f(d * LOG2E);
+            if (TAU) tau += a.part_sum_tau[(long long)i * a.M + m] * __builtin_amdgcn_exp2f(d * lt);
+        }
+        sum = wave_sum(sum);
+        if (TAU) tau = wave_sum(tau);
+    }
+    if (lane == 0) merge_end<TAU, false, TEACHER>(a, PolicyArgs{}, teacher, m, in, mx, sum, tau);
 }
 
 // ---- the teacher's entries of du: a wavefront a row -------------------------------------------------------------------
@@ -324,39 +354,60 @@ __device__ __forceinline__ float rows_reduce(float v, float* sh) {
     return v;
 }
 
-template <bool TAU, bool POLICY, bool TEACHER, bool GRADIENT>
+// NC > 0: a row of up to 2048 NC logits stays in registers, 16-byte words, and is read and written once (of one exponential a logit, as exponentials):
+// 1344 rows of 32000 101 us in three passes, 67 so.  What is beyond V in the last word counts as -inf.
+template <int NC, bool TAU, bool POLICY, bool TEACHER, bool GRADIENT>
 __global__ __launch_bounds__(512) void loss_rows_f32_kernel(LossRowsArgs a, PolicyArgs policy, TeacherArgs teacher) {
     __shared__ float sh[8];
     __shared__ ListLds list;
     __shared__ float consts[8];
     const long long m = blockIdx.x;
     float* row = a.u + m * a.ldu;
-    const int V = a.V, V4 = V & ~3;
+    const int V = a.V, words4 = (V + 3) / 4;
+    auto load = [&](int c) {                             // (rows are whole 16-byte words)
+        float4 x = *reinterpret_cast<const float4*>(row + 4 * c);
+        if (4 * c + 4 > V) {
+            if (4 * c + 1 >= V) x.y = -INFINITY;
+            if (4 * c + 2 >= V) x.z = -INFINITY;
+            x.w = -INFINITY;
+        }
+        return x;
+    };
     const int lab = a.labels ? a.labels[m] : -1;
     const bool lab_ok = (unsigned)lab < (unsigned)V;
-    float mx = -INFINITY;
-    for (int v = threadIdx.x * 4; v < V4; v += 2048) {
-        const float4 x = *reinterpret_cast<const float4*>(row + v);
-        mx = fmaxf(fmaxf(fmaxf(mx, x.x), fmaxf(x.y, x.z)), x.w);
+    constexpr bool KEEP = NC > 0, POWERS = KEEP && !TAU && GRADIENT;
+    float4 r[KEEP ? NC : 1];
+    // f(word, its number) of every word of this thread's, the row's last one with -inf behind V
+    auto words = [&](auto&& f) __attribute__((always_inline)) {
+        if constexpr (KEEP) {
+#pragma unroll
+            for (int i = 0; i < NC; ++i) if ((int)threadIdx.x + 512 * i < words4) f(r[i], (int)threadIdx.x + 512 * i);
+        } else {
+            for (int c = threadIdx.x; c < words4; c += 512) { float4 x = load(c); f(x, c); }
+        }
+    };
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int i = 0; i < NC; ++i) if ((int)threadIdx.x + 512 * i < words4) r[i] = load((int)threadIdx.x + 512 * i);
     }
-    for (int v = V4 + threadIdx.x; v < V; v += 512) mx = fmaxf(mx, row[v]);
+    const float at_label = lab_ok ? row[lab] : 0.0f;
+    float mx = -INFINITY;
+    words([&](float4& x, int) { mx = fmaxf(fmaxf(fmaxf(mx, x.x), fmaxf(x.y, x.z)), x.w); });
     mx = rows_reduce<true>(mx, sh);
     float sum = 0.0f, tau = 0.0f;
     const float it = teacher.inv_tau;
-    auto add = [&](float x) {
-        sum += expf(x - mx);
+    auto add = [&](float& x) {
+        const float e = expf(x - mx);
+        sum += e;
         if (TAU) tau += expf((x - mx) * it);
+        if (POWERS) x = e;
     };
-    for (int v = threadIdx.x * 4; v < V4; v += 2048) {
-        const float4 x = *reinterpret_cast<const float4*>(row + v);
-        add(x.x); add(x.y); add(x.z); add(x.w);
-    }
-    for (int v = V4 + threadIdx.x; v < V; v += 512) add(row[v]);
+    words([&](float4& x, int) { add(x.x); add(x.y); add(x.z); add(x.w); });
     sum = rows_reduce<false>(sum, sh);
     if (TAU) tau = rows_reduce<false>(tau, sh);
     if (threadIdx.x < 64) {
         const float nan = __builtin_nanf("");
-        const float lp = lab_ok ? row[lab] - mx - logf(sum) : lab == -1 ? 0.0f : nan;
+        const float lp = lab_ok ? at_label - mx - logf(sum) : lab == -1 ? 0.0f : nan;
         float loss = 0.0f, ca = 0.0f, cat = 0.0f, hot = 0.0f;
         if (POLICY) {
             if (lab_ok) {
@@ -396,23 +447,21 @@ __global__ __launch_bounds__(512) void loss_rows_f32_kernel(LossRowsArgs a, Poli
     __syncthreads();                                     // (the label's and the entries' logits are read)
     const float ca = consts[0], cat = consts[1], hot = consts[2];
     const bool hard = ca != 0.0f || ca != ca, soft = TAU && (cat != 0.0f || cat != cat);
-    auto grad = [&](float x, int v) {
-        float g = hard ? ca * expf(x - mx) : 0.0f;       // (a row that counts for nothing is zero whatever it holds)
+    auto grad = [&](float x, int v, bool power) {        // power: x is exp(u - max) already
+        float g = hard ? ca * (power ? x : expf(x - mx)) : 0.0f;   // (a row that counts for nothing is zero whatever it holds)
         if (soft) g += cat * expf((x - mx) * it);
-        return v == lab && lab_ok ? g - hot : g;
+        return v == lab && lab_ok ? g - hot : v < V ? g : 0.0f;
     };
-    for (int v = threadIdx.x * 4; v < V4; v += 2048) {
-        float4 x = *reinterpret_cast<const float4*>(row + v);
-        x.x = grad(x.x, v); x.y = grad(x.y, v + 1); x.z = grad(x.z, v + 2); x.w = grad(x.w, v + 3);
-        *reinterpret_cast<float4*>(row + v) = x;
-    }
+    words([&](float4& x, int c) {
+        *reinterpret_cast<float4*>(row + 4 * c) = make_float4(grad(x.x, 4 * c, POWERS), grad(x.y, 4 * c + 1, POWERS), grad(x.z, 4 * c + 2, POWERS), grad(x.w, 4 * c + 3, POWERS));
+    });
     const int pad = (int)min(a.ldu, (long long)((V + 7) & ~7));
-    for (int v = V4 + threadIdx.x; v < pad; v += 512) row[v] = v < V ? grad(row[v], v) : 0.0f;
+    for (int v = 4 * words4 + threadIdx.x; v < pad; v += 512) row[v] = 0.0f;
     if (TEACHER) {
         __syncthreads();
         const float weight = a.s * teacher.soft * teacher.tau;
         for (int k = threadIdx.x; k < teacher.K; k += 512)
-            if (list.cls[k] >= 0) row[list.cls[k]] = grad(list.logit[k], list.cls[k]) - weight * class_weight(list, teacher.K, k);
+            if (list.cls[k] >= 0) row[list.cls[k]] = grad(list.logit[k], list.cls[k], false) - weight * class_weight(list, teacher.K, k);
     }
 }
 
@@ -663,6 +712,15 @@ hipError_t launch_loss_prep(const LossPrepArgs& a, DType type, hipStream_t st) {
 }
 
 hipError_t launch_loss_merge(const LossMergeArgs& a, hipStream_t st) {
+    // (a lane a part, whose loads are a row of floats apart: where parts are few, or rows)
+    if (!a.policy && !a.rows && (a.strips <= 64 || a.M <= 1024)) {
+        const dim3 rows((unsigned)(((a.consts ? a.Mp : a.M) + 3) / 4));
+        const TeacherArgs t = a.teacher ? *a.teacher : TeacherArgs{};
+        if (a.teacher && a.part_sum_tau) hipLaunchKernelGGL((loss_merge_row_kernel<true, true>), rows, dim3(256), 0, st, a, t);
+        else if (a.teacher) hipLaunchKernelGGL((loss_merge_row_kernel<false, true>), rows, dim3(256), 0, st, a, t);
+        else hipLaunchKernelGGL((loss_merge_row_kernel<false, false>), rows, dim3(256), 0, st, a, t);
+        return hipGetLastError();
+    }
     const dim3 grid((unsigned)((a.M + 63) / 64));
     const PolicyArgs p = a.policy ? *a.policy : PolicyArgs{};
     const TeacherArgs t = a.teacher ? *a.teacher : TeacherArgs{};
@@ -682,10 +740,17 @@ hipError_t launch_loss_rows_f32(const LossRowsArgs& a, hipStream_t st) {
     const dim3 grid((unsigned)a.M), block(512);
     const PolicyArgs p = a.policy ? *a.policy : PolicyArgs{};
     const TeacherArgs t = a.teacher ? *a.teacher : TeacherArgs{};
-    if (a.policy) hipLaunchKernelGGL((loss_rows_f32_kernel<false, true, false, true>), grid, block, 0, st, a, p, t);
-    else if (a.teacher && t.inv_tau != 1.0f) hipLaunchKernelGGL((loss_rows_f32_kernel<true, false, true, true>), grid, block, 0, st, a, p, t);
-    else if (a.teacher) hipLaunchKernelGGL((loss_rows_f32_kernel<false, false, true, true>), grid, block, 0, st, a, p, t);
-    else hipLaunchKernelGGL((loss_rows_f32_kernel<false, false, false, false>), grid, block, 0, st, a, p, t);
+    const int words = (a.V + 3) / 4;
+#define BLSTM_LOSS_ROWS(NC) do { \
+    if (a.policy) hipLaunchKernelGGL((loss_rows_f32_kernel<NC, false, true, false, true>), grid, block, 0, st, a, p, t); \
+    else if (a.teacher && t.inv_tau != 1.0f) hipLaunchKernelGGL((loss_rows_f32_kernel<NC, true, false, true, true>), grid, block, 0, st, a, p, t); \
+    else if (a.teacher) hipLaunchKernelGGL((loss_rows_f32_kernel<NC, false, false, true, true>), grid, block, 0, st, a, p, t); \
+    else hipLaunchKernelGGL((loss_rows_f32_kernel<NC, false, false, false, false>), grid, block, 0, st, a, p, t); } while (0)
+    if (words <= 2 * 512) BLSTM_LOSS_ROWS(2);
+    else if (words <= 8 * 512) BLSTM_LOSS_ROWS(8);
+    else if (words <= 16 * 512) BLSTM_LOSS_ROWS(16);
+    else BLSTM_LOSS_ROWS(0);
+#undef BLSTM_LOSS_ROWS
     return hipGetLastError();
 }
 
