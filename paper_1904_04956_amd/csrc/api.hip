@@ -433,10 +433,10 @@ int loss_parts(long long groups, long long tiles, double tile_us, double part_us
     const long long per = (tiles + best - 1) / best;
     return (int)((tiles + per - 1) / per);               // (no empty part)
 }
-int loss_sum_parts(int M, int V, int Zp) { return loss_parts((M + 511) / 512, (V + 63) / 64, 2.2 * Zp / 256, 4.0 * M / 4e6); }   // (two workgroups a CU)
+int loss_sum_parts(int M, int V, int Zp) { return loss_parts((M + 511) / 512, (V + 63) / 64, 4.2 * Zp / 256, 16.0 * M / 4e6); }   // (two workgroups a CU)
 size_t loss_tiles(int M, int V) { return (size_t)((M + 63) / 64) * ((V + 127) / 128); }
-int loss_row_parts(int M, int V, int Zp) { return loss_parts((M + 255) / 256, (V + 63) / 64, 2.2 * Zp / 256, 2.0 * M * Zp * 4 / 4e6); }
-int loss_class_parts(int M, int V, int Zp) { return loss_parts((V + 127) / 128, (M + 63) / 64, 1.8 * Zp / 256, 2.0 * V * Zp * 4 / 4e6); }
+int loss_row_parts(int M, int V, int Zp) { return loss_parts((M + 255) / 256, (V + 63) / 64, 3.4 * Zp / 256, 1.5 * M * Zp * 4 / 4e6); }
+int loss_class_parts(int M, int V, int Zp) { return loss_parts((V + 127) / 128, (M + 63) / 64, 2.4 * Zp / 256, 2.5 * V * Zp * 4 / 4e6); }
 
 LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
     LossScratch l{};
@@ -664,10 +664,10 @@ int loss_run_fused(blstm_ctx* ctx, const LossCall& c, const int32_t* labels, con
     f.ldo = ctx->zdim; f.vec = ctx->zdim % 4 == 0 && aligned16(f.out);
     if (!both) f.k1 = f.k;                               // (the only exponential is the first)
     if (teacher) { f.entries = c.at<uint2>(l.entries); f.entries_from = c.at<int>(l.tile_from); f.entries_count = c.at<int>(l.tile_count); }
-    RUN(PC_GEMM_SOFTMAX_BWD, "dW_s", launch_loss_fused_classes(f, both, st));
+    f.row_loss = d.row_loss; f.loss = loss_dev;
+    RUN(PC_GEMM_SOFTMAX_BWD, "dW_s and the loss", launch_loss_fused_classes(f, both, st));
     if (l.class_parts > 1)
         RUN(PC_GEMM_SOFTMAX_BWD, "dW_s", launch_loss_classes_sum(f.out, f.out_db, f.parts, (long long)ctx->V * ctx->zdim, ctx->V, dw, db, st));
-    RUN(PC_MISC, "loss sum", launch_sum_to_scalar(c.at<float>(l.row_loss), ctx->M, loss_dev, st));
     return BLSTM_OK;
 }
 

@@ -98,6 +98,8 @@ struct LossFusedArgs {
     float* part_sum;
     float* part_sum2;                                // sums: at the scale k
     float* out_db;                                   // classes: [parts][V]
+    const float* row_loss;                           // classes: [M], whose sum goes to loss[0]
+    float* loss;
     const uint2* entries;                            // classes: the teacher's, row | class << 6 within a tile and weight q, by tiles of 64 rows and 128 classes; or null
     const int* entries_from;                         // [tiles] where a tile's lie, and how many
     const int* entries_count;

@@ -320,6 +320,23 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
     const int ntm = (a.M + 63) / 64, per = (ntm + a.parts - 1) / a.parts, t0 = part * per, n = min(per, ntm - t0);
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
     const Reads<NK> at(lane);
+    if (blockIdx.x == 0 && a.loss) {                    // the rows' loss terms, in a fixed order (a launch less)
+        float* sh = reinterpret_cast<float*>(smem);
+        float s = 0.0f;
+        for (int i0 = tid; i0 < a.M; i0 += 8 * 512) {
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = i0 + 512 * j < a.M ? a.row_loss[i0 + 512 * j] : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += x[j];
+        }
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off, 64);
+        if (lane == 0) sh[wv] = s;
+        __syncthreads();
+        if (tid == 0) { s = sh[0]; for (int w = 1; w < 8; ++w) s += sh[w]; a.loss[0] = s; }
+        __syncthreads();
+    }
     const int class0 = ct * 128 + cg * 32, v = class0 + l32;
     uint4 wf[4 * NK];
 #pragma unroll
@@ -458,35 +475,47 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
         }
     }
     const int ln = fresh_lane(), n32 = ln & 31, hf = ln >> 5, cls = ct * 128 + cg * 32 + n32;
-    // the two halves of the rows together, through LDS; register e of a lane: column 32 zb + 8 (e / 4) + 4 half + e % 4 of class l32
+    // the two halves of the rows together, through LDS, and out along the rows of dW_s; register e of a lane: column 32 zb + 8 (e / 4) + 4 half + e % 4 of
+    // class n32.  (Rows of LDS a 16-byte word longer: neighbouring classes on neighbouring banks.)
     db += __shfl_xor(db, 32, 64);
-    float* sh = reinterpret_cast<float*>(smem);         // [4][16][64] a block of 32 columns, then [4][32]
+    constexpr int LD = 64 * NK + 4;
+    float* sh = reinterpret_cast<float*>(smem);         // [128][LD], then [128]
+    float* mine = sh + (cg * 32 + n32) * LD + 4 * hf;
     float* out = a.out + (long long)part * a.V * a.ldo;
-    float* out_db = a.out_db + (long long)part * a.V;
     __syncthreads();
     if (rh == 1) {
 #pragma unroll
         for (int zb = 0; zb < 2 * NK; ++zb)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) *reinterpret_cast<float4*>(sh + (((cg * 2 * NK + zb) * 4 + g) * 64 + ln) * 4) = make_float4(o[zb][4 * g], o[zb][4 * g + 1], o[zb][4 * g + 2], o[zb][4 * g + 3]);
-        if (hf == 0) sh[32768 + cg * 32 + n32] = db;
+            for (int g = 0; g < 4; ++g) *reinterpret_cast<float4*>(mine + 32 * zb + 8 * g) = make_float4(o[zb][4 * g], o[zb][4 * g + 1], o[zb][4 * g + 2], o[zb][4 * g + 3]);
+        if (hf == 0) sh[128 * LD + cg * 32 + n32] = db;
     }
     __syncthreads();
-    if (rh == 1 || cls >= a.V) return;
-    if (hf == 0) out_db[cls] = db + sh[32768 + cg * 32 + n32];
+    if (rh == 0) {
 #pragma unroll
-    for (int zb = 0; zb < 2 * NK; ++zb)
+        for (int zb = 0; zb < 2 * NK; ++zb)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const float4 x = *reinterpret_cast<const float4*>(sh + (((cg * 2 * NK + zb) * 4 + g) * 64 + ln) * 4);
-            const float y[4] = {o[zb][4 * g] + x.x, o[zb][4 * g + 1] + x.y, o[zb][4 * g + 2] + x.z, o[zb][4 * g + 3] + x.w};
-            const int z = zb * 32 + 8 * g + 4 * hf;
-            if (a.vec && z + 4 <= a.Z) *reinterpret_cast<float4*>(out + (long long)cls * a.ldo + z) = make_float4(y[0], y[1], y[2], y[3]);
-            else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) if (z + i < a.Z) out[(long long)cls * a.ldo + z + i] = y[i];
+            for (int g = 0; g < 4; ++g) {
+                float4* p = reinterpret_cast<float4*>(mine + 32 * zb + 8 * g);
+                const float4 x = *p;
+                *p = make_float4(o[zb][4 * g] + x.x, o[zb][4 * g + 1] + x.y, o[zb][4 * g + 2] + x.z, o[zb][4 * g + 3] + x.w);
             }
+        if (hf == 0 && cls < a.V) a.out_db[(long long)part * a.V + cls] = db + sh[128 * LD + cg * 32 + n32];
+    }
+    __syncthreads();
+    const int rows = min(128, a.V - ct * 128);
+    for (int i = wv * 64 + ln; i < rows * 16 * NK; i += 512) {
+        const int r = i / (16 * NK), z = i % (16 * NK) * 4;
+        const float4 x = *reinterpret_cast<const float4*>(sh + r * LD + z);
+        float* to = out + (long long)(ct * 128 + r) * a.ldo + z;
+        if (a.vec && z + 4 <= a.Z) *reinterpret_cast<float4*>(to) = x;
+        else {
+            if (z < a.Z) to[0] = x.x;
+            if (z + 1 < a.Z) to[1] = x.y;
+            if (z + 2 < a.Z) to[2] = x.z;
+            if (z + 3 < a.Z) to[3] = x.w;
         }
+    }
 }
 
 // ---- a teacher's entries by tiles of 64 rows and 128 classes --------------------------------------------------------------------
@@ -663,7 +692,7 @@ hipError_t sums_nk(const LossFusedArgs& a, hipStream_t st) {
 }
 template <int NK, bool TAU, bool ENTRIES>
 hipError_t classes_nk(const LossFusedArgs& a, hipStream_t st) {
-    constexpr size_t ring = (size_t)Ring<NK>::STAGES * (Ring<NK>::STAGE + (ENTRIES ? Ring<NK>::LIST : 0)) + (ENTRIES ? 8 * 32 * SPOT * 4 : 0), join = 32768 * 4 + 512, lds = ring > join ? ring : join;
+    constexpr size_t ring = (size_t)Ring<NK>::STAGES * (Ring<NK>::STAGE + (ENTRIES ? Ring<NK>::LIST : 0)) + (ENTRIES ? 8 * 32 * SPOT * 4 : 0), join = (128 * (64 * NK + 4) + 128) * 4, lds = ring > join ? ring : join;
     static thread_local bool attr_set = false;
     const hipError_t e = allow_lds(&loss_classes_kernel<NK, TAU, ENTRIES>, lds, &attr_set);
     if (e != hipSuccess) return e;
