@@ -3,6 +3,7 @@
 // kernels of gemm.hip, cell.hip, softmax.hip and update.hip.
 #include <hip/hip_runtime.h>
 
+#include <climits>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -414,11 +415,11 @@ struct LossScratch {
     bool strips;              // largest logits: by the strips' maxima
     bool fused;               // the kernels of losses_fused.hip: no du in memory
     int row_parts, sum_parts, class_parts;
-    size_t bias_f, consts, part, part_ref, part_sum, part_sum2, cparts, cparts_b, tile_count, tile_left, tile_from, entries;
+    size_t bias_f, consts, part, part_ref, part_sum, part_sum2, cparts, cparts_b, tile_count, tile_from, entries;
     size_t zc, wp, dzp, dwp, label_logit, entry_logit, entry_q, soft_const, soft_state, pmax, psum, ptau, rows, row_loss, hi, lo, u, partial, partial_bytes, bytes;
 };
 static_assert(BLSTM_MAX_TOP == LOSS_MAX_TOP, "the kernels' lists must hold every entry");
-// Logits held at a time where they are only read once more: 128 MiB stay in the last-level cache.
+// Logits held at a time where they are only read once more.
 constexpr size_t kLossChunkBytes = (size_t)1 << 30;
 
 // Into how many parts the classes of a workgroup's 256 rows are cut, and the rows of a workgroup's 128 classes: the least estimated
@@ -480,8 +481,7 @@ LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
                 put(&l.entry_q, M * K * 4);
                 put(&l.soft_const, M * 4);
                 put(&l.soft_state, M * 4);
-                put(&l.tile_count, (tiles + 1) * 4);
-                put(&l.tile_left, tiles * 4);
+                put(&l.tile_count, tiles * 4);
                 put(&l.tile_from, tiles * 4);
                 put(&l.entries, (M * K + LOSS_LIST_SLACK) * 8);
             }
@@ -536,9 +536,17 @@ struct LossCall {
     template <typename T> T* at(size_t off) const { return reinterpret_cast<T*>(base + off); }
 };
 
-int loss_check(const char* name, const blstm_ctx* ctx, int call, int K, const void* theta, const void* z, void* scratch, size_t scratch_bytes, LossScratch* l) {
+int loss_sizes(const char* name, const blstm_ctx* ctx, int call, int K) {
     if (K < 0 || ((call == SOFTMAX_TOPK || call == SOFTMAX_DISTILL) && (K < 1 || K > BLSTM_MAX_TOP || K > ctx->V)))
         return fail(BLSTM_ERR_DIM, "%s: K must be in 1..min(V, %d)", name, BLSTM_MAX_TOP);
+    if (call == SOFTMAX_DISTILL && ((long long)ctx->M * K > INT_MAX - 64LL * BLSTM_MAX_TOP || loss_tiles(ctx->M, ctx->V) > INT_MAX))
+        return fail(BLSTM_ERR_DIM, "%s: T B K must be below 2^31 - 2^14, T B V below 2^44", name);
+    return BLSTM_OK;
+}
+
+int loss_check(const char* name, const blstm_ctx* ctx, int call, int K, const void* theta, const void* z, void* scratch, size_t scratch_bytes, LossScratch* l) {
+    const int rc = loss_sizes(name, ctx, call, K);
+    if (rc != BLSTM_OK) return rc;
     if (!scratch) return fail(BLSTM_ERR_NULL, "%s: null scratch", name);
     if (!aligned16(theta) || !aligned16(z) || !aligned16(scratch)) return fail(BLSTM_ERR_ALIGN, "%s: pointers must be 16-byte aligned", name);
     *l = loss_scratch(ctx, call, K);
@@ -628,7 +636,7 @@ int loss_run_fused(blstm_ctx* ctx, const LossCall& c, const int32_t* labels, con
     if (teacher) {
         LossListArgs e{};
         e.M = ctx->M; e.V = ctx->V; e.K = teacher->K; e.classes = teacher->classes; e.q = c.at<float>(l.entry_q); e.weight = ctx->s * teacher->soft * teacher->tau;
-        e.count = c.at<int>(l.tile_count); e.left = c.at<int>(l.tile_left); e.from = c.at<int>(l.tile_from); e.entries = c.at<uint2>(l.entries);
+        e.count = c.at<int>(l.tile_count); e.from = c.at<int>(l.tile_from); e.entries = c.at<uint2>(l.entries);
         RUN(PC_SOFTMAX_ROWS, "the teacher's classes by tiles", launch_loss_lists(e, st));
     }
     if (!gradient || both) {
@@ -663,6 +671,9 @@ int loss_run_fused(blstm_ctx* ctx, const LossCall& c, const int32_t* labels, con
     f.out = l.class_parts > 1 ? c.at<float>(l.cparts) : dw; f.out_db = l.class_parts > 1 ? c.at<float>(l.cparts_b) : db;
     f.ldo = ctx->zdim; f.vec = ctx->zdim % 4 == 0 && aligned16(f.out);
     if (!both) f.k1 = f.k;                               // (the only exponential is the first)
+    // Two bf16 are 2^-16 off where du is large, 2.5e-6 of dW_s together; a sum of thousands of frames in float is as far off by itself
+    // (5376 frames: 1e-6), and the third part costs up to a third of the kernel there (every product of 32 x 32 holds a class of the teacher's).
+    f.third = ctx->M <= 4096;
     if (teacher) { f.entries = c.at<uint2>(l.entries); f.entries_from = c.at<int>(l.tile_from); f.entries_count = c.at<int>(l.tile_count); }
     f.row_loss = d.row_loss; f.loss = loss_dev;
     RUN(PC_GEMM_SOFTMAX_BWD, "dW_s and the loss", launch_loss_fused_classes(f, both, st));
@@ -689,13 +700,7 @@ int loss_run(blstm_ctx* ctx, const LossCall& given, const int32_t* labels, const
         if (bf) {
             a.W = static_cast<const unsigned short*>(c.W); a.bias = static_cast<const unsigned short*>(c.b);
             a.label_logit = c.at<float>(l.label_logit);
-            if (l.fused) {
-                a.bias_f = c.at<float>(l.bias_f); a.bias_pad = -INFINITY;
-                if (teacher) {
-                    a.tile_count = c.at<int>(l.tile_count);
-                    RUN(PC_MISC, "counts", launch_fill_u32(reinterpret_cast<unsigned*>(a.tile_count), (int)loss_tiles(M, V) + 1, 0u, st));
-                }
-            }
+            if (l.fused) { a.bias_f = c.at<float>(l.bias_f); a.bias_pad = -INFINITY; }
             a.entry_logit = c.at<float>(l.entry_logit); a.entry_q = c.at<float>(l.entry_q);
             a.soft_const = c.at<float>(l.soft_const); a.soft_state = c.at<int>(l.soft_state);
         }
@@ -1139,10 +1144,7 @@ int softmax_xent_fwd_bwd_noalloc(blstm_ctx* ctx, const void* theta, const void* 
 size_t softmax_scratch_bytes(const blstm_ctx* ctx, int call, int K) {
     if (!ctx) { fail(BLSTM_ERR_NULL, "softmax_scratch_bytes: null argument"); return 0; }
     if (call < SOFTMAX_LOGPROB || call > SOFTMAX_POLICY) { fail(BLSTM_ERR_DIM, "softmax_scratch_bytes: no call %d", call); return 0; }
-    if ((call == SOFTMAX_TOPK || call == SOFTMAX_DISTILL) && (K < 1 || K > BLSTM_MAX_TOP || K > ctx->V)) {
-        fail(BLSTM_ERR_DIM, "softmax_scratch_bytes: K must be in 1..min(V, %d)", BLSTM_MAX_TOP);
-        return 0;
-    }
+    if (loss_sizes("softmax_scratch_bytes", ctx, call, call == SOFTMAX_TOPK || call == SOFTMAX_DISTILL ? K : 0) != BLSTM_OK) return 0;
     return loss_scratch(ctx, call, K).bytes;
 }
 

@@ -51,7 +51,6 @@ struct LossPrepArgs {
     const unsigned short* bias;
     float* bias_f;                                   // [V rounded up to 64] the bias as floats, bias_pad behind it; or null
     float bias_pad;
-    int* tile_count;                                 // numbers of entries by tiles of 64 rows and 128 classes, zero before the launch; or null
     const int32_t* labels;                           // or null
     float* label_logit;                              // [M]
     TeacherArgs teacher;                             // K = 0: none
@@ -105,6 +104,7 @@ struct LossFusedArgs {
     const int* entries_count;
     long long ldo;
     int vec;                                         // classes: rows of out take 16-byte stores
+    int third;                                       // classes: a third part of du where a teacher's classes are
 };
 hipError_t launch_loss_fused_rows(const LossFusedArgs& a, bool known, bool tau, hipStream_t st);
 // The rows' sums alone at the scale k1 and, with second, k from references part_ref (a logit); or, with logits, u into out [M][ldo] (ldo a multiple
@@ -140,8 +140,7 @@ struct LossListArgs {
     const int32_t* classes;
     const float* q;                                  // [M][K], 0: none
     float weight;
-    int* count;                                      // [tiles + 1], the last one zero before the launch
-    int* left;                                       // [tiles]
+    int* count;                                      // [tiles], the rows' tiles one after the other
     int* from;                                       // [tiles]
     uint2* entries;
 };

@@ -440,8 +440,7 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
                     if (labels[r] == class0 + (fresh_lane() & 31)) d[e] -= consts[256 + r];
                 }
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) db += d[e];
+            db += ((d[0] + d[1]) + (d[2] + d[3])) + ((d[4] + d[5]) + (d[6] + d[7]));   // (one addition a step to the long sum)
             auto split = [&] {                          // d rounded, as the operand; d: what the rounding left
                 unsigned p[4];
 #pragma unroll
@@ -462,7 +461,7 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
             }
             ahead<2 * 2, 2 * NK, 2, 2, 2>();
             __builtin_amdgcn_sched_barrier(0);
-            if (any_hot) {                              // (where du is large: a third part of it)
+            if (any_hot || (ENTRIES && a.third && any_spot)) {   // (where du is large: a third part of it)
                 const uint4 rest = split();
 #pragma unroll
                 for (int zb = 0; zb < 2 * NK; ++zb) o[zb] = mma32(at.by_col(s + t * 16 * R::ROWB, zb), rest, o[zb]);
@@ -518,33 +517,45 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
     }
 }
 
-// ---- a teacher's entries by tiles of 64 rows and 128 classes --------------------------------------------------------------------
-// (Their numbers are counted by loss_prep_kernel.)  A place for every tile's list, wherever it comes to lie: the workgroups take theirs from one
-// counter (in order of the tiles, by one workgroup, 21000 tiles took 21 us).
-__global__ __launch_bounds__(256) void loss_places_kernel(const int* count, int* left, int* from, int* taken, int n) {
-    __shared__ int sh[5];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = (int)blockIdx.x * 256 + (int)threadIdx.x;
-    const int own = i < n ? count[i] : 0;
+// ---- a teacher's entries by tiles of 64 rows and 128 classes, a workgroup 64 rows ------------------------------------------------
+// Counts the rows' entries with a probability by tiles, gives every tile a place among the rows' own, and puts them there (in an order of no
+// matter: a row's classes are different ones).  All counters in LDS: with a list of all rows together, 168 rows of 16 took three launches of
+// 4 us for it and 5376 of 64 took 20 us.
+constexpr int LISTS_THREADS = 1024;
+__global__ __launch_bounds__(LISTS_THREADS) void loss_lists_kernel(LossListArgs a, int ntv) {
+    extern __shared__ uint4 smem[];
+    int* at = reinterpret_cast<int*>(smem);             // [ntv], then a number a wavefront
+    int* waves = at + ntv;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row0 = (int)blockIdx.x * 64;
+    const int n = min(64, a.M - row0) * a.K, base = row0 * a.K;
+    for (int i = tid; i < ntv; i += LISTS_THREADS) at[i] = 0;
+    __syncthreads();
+    for (int k = tid; k < n; k += LISTS_THREADS)
+        if (a.q[base + k] > 0.0f) atomicAdd(&at[a.classes[base + k] >> 7], 1);
+    __syncthreads();
+    const int per = (ntv + LISTS_THREADS - 1) / LISTS_THREADS, first = min(tid * per, ntv), end = min(first + per, ntv);
+    int own = 0;
+    for (int i = first; i < end; ++i) own += at[i];
     int before = own;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) { const int t = __shfl_up(before, o, 64); if (lane >= o) before += t; }
-    if (lane == 63) sh[wave] = before;
+    if (lane == 63) waves[wave] = before;
     __syncthreads();
-    if (threadIdx.x == 0) sh[4] = atomicAdd(taken, sh[0] + sh[1] + sh[2] + sh[3]);
+    before -= own;
+    for (int w = 0; w < wave; ++w) before += waves[w];
+    for (int i = first; i < end; ++i) {
+        const int c = at[i];
+        at[i] = before;
+        a.count[(long long)blockIdx.x * ntv + i] = c;
+        a.from[(long long)blockIdx.x * ntv + i] = base + before;
+        before += c;
+    }
     __syncthreads();
-    before += sh[4] - own;
-    for (int w = 0; w < wave; ++w) before += sh[w];
-    if (i < n) { from[i] = before; left[i] = own; }
-}
-// Puts every entry with a probability into its tile's list (whose order is of no matter: a row's classes are different ones).
-__global__ __launch_bounds__(256) void loss_lists_kernel(const int32_t* classes, const float* q, float weight, long long n, int K, int ntv, int* left, const int* from, uint2* entries) {
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
-        const float p = q[i];
+    for (int k = tid; k < n; k += LISTS_THREADS) {
+        const float p = a.q[base + k];
         if (!(p > 0.0f)) continue;
-        const int m = (int)(i / K), c = classes[i];
-        const long long b = (long long)(m >> 6) * ntv + (c >> 7);
-        const int to = from[b] + atomicSub(&left[b], 1) - 1;
-        entries[to] = make_uint2((unsigned)(m & 63) | (unsigned)(c & 127) << 6, __builtin_bit_cast(unsigned, weight * p));
+        const int c = a.classes[base + k];
+        a.entries[base + atomicAdd(&at[c >> 7], 1)] = make_uint2((unsigned)(k / a.K) | (unsigned)(c & 127) << 6, __builtin_bit_cast(unsigned, a.weight * p));
     }
 }
 
@@ -742,12 +753,13 @@ static hipError_t dz_shared(const LossDzArgs& a, bool known, hipStream_t st) {
 hipError_t launch_loss_dz(const LossDzArgs& a, bool known, hipStream_t st) { return a.M <= 8192 ? dz_shared<4>(a, known, st) : dz_shared<1>(a, known, st); }
 hipError_t launch_loss_lists(const LossListArgs& a, hipStream_t st) {
     const int ntv = (a.V + 127) / 128;
-    const int tiles = (a.M + 63) / 64 * ntv;
-    hipLaunchKernelGGL(loss_places_kernel, dim3((unsigned)((tiles + 255) / 256)), dim3(256), 0, st, a.count, a.left, a.from, a.count + tiles, tiles);
-    hipError_t e = hipGetLastError();
+    constexpr size_t most = ((1 << 22) / 128 + LISTS_THREADS / 64) * sizeof(int);   // (a model's most classes)
+    static thread_local bool attr_set = false;
+    const hipError_t e = allow_lds(&loss_lists_kernel, most, &attr_set);
     if (e != hipSuccess) return e;
-    const long long n = (long long)a.M * a.K, blocks = (n + 255) / 256;
-    hipLaunchKernelGGL(loss_lists_kernel, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st, a.classes, a.q, a.weight, n, a.K, ntv, a.left, a.from, a.entries);
+    const size_t lds = (ntv + LISTS_THREADS / 64) * sizeof(int);
+    if (lds > most) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(loss_lists_kernel, dim3((unsigned)((a.M + 63) / 64)), dim3(LISTS_THREADS), lds, st, a, ntv);
     return hipGetLastError();
 }
 hipError_t launch_loss_classes_sum(const float* p, const float* pb, int parts, long long n, int V, float* out, float* out_b, hipStream_t st) {

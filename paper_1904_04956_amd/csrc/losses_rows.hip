@@ -95,16 +95,16 @@ __global__ __launch_bounds__(256) void loss_prep_kernel(LossPrepArgs a) {
     ListLds& s = lists[wave];
     const int lab = a.labels ? a.labels[m] : -1;
     const bool lab_ok = (unsigned)lab < (unsigned)a.V;
-    int state = 0;
-    if (a.teacher.K > 0) state = teacher_list(a.teacher, m, a.V, s);
-    const bool live = a.keep || lab_ok || (state & LIST_USED);
     const T* z = static_cast<const T*>(a.z) + m * a.Z;
-    if (a.zc) {
-        T* zc = static_cast<T*>(a.zc) + m * a.ldzc;
-        for (int k = lane; k < a.ldzc; k += 64) zc[k] = live && k < a.Z ? z[k] : (T)0;
-    }
-    if (!a.W) return;
-    if constexpr (sizeof(T) == 2) {
+    int state = 0;
+    auto list = [&] { if (a.teacher.K > 0) state = teacher_list(a.teacher, m, a.V, s); return a.keep || lab_ok || (state & LIST_USED); };
+    if constexpr (sizeof(T) == 4) {
+        const bool live = list();
+        if (a.zc) {
+            T* zc = static_cast<T*>(a.zc) + m * a.ldzc;
+            for (int k = lane; k < a.ldzc; k += 64) zc[k] = live && k < a.Z ? z[k] : (T)0;
+        }
+    } else {
         // sixteen lanes a product, eight elements a lane and step; the row's elements of up to PREP_STEPS steps stay in registers
         constexpr int PREP_STEPS = 4;
         const int l16 = lane & 15, g = lane >> 4;
@@ -124,6 +124,12 @@ __global__ __launch_bounds__(256) void loss_prep_kernel(LossPrepArgs a) {
         uint4 zr[PREP_STEPS];
 #pragma unroll
         for (int i = 0; i < PREP_STEPS; ++i) zr[i] = row_words(l16 * 8 + 128 * i);
+        const bool live = list();                       // (its loads and the row's together on their way)
+        if (a.zc) {
+            T* zc = static_cast<T*>(a.zc) + m * a.ldzc;
+            for (int k = lane * 8; k < a.ldzc; k += 512) *reinterpret_cast<uint4*>(zc + k) = live ? row_words(k) : make_uint4(0, 0, 0, 0);
+        }
+        if (!a.W) return;
         auto dot = [](const uint4& x, const uint4& w, float acc) {
             acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x.x), __builtin_bit_cast(bf16x2_t, w.x), acc, false);
             acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x.y), __builtin_bit_cast(bf16x2_t, w.y), acc, false);
@@ -181,16 +187,23 @@ __global__ __launch_bounds__(256) void loss_prep_kernel(LossPrepArgs a) {
                     }
                 }
             }
-            for (int k = lane; k < a.teacher.K; k += 64) {
-                const int c = s.cls[k];
+            // a class that stands there more than once has all of its q at the first of its entries with any
+            for (int k0 = 0; k0 < a.teacher.K; k0 += 64) {
+                const int k = k0 + lane;
+                const int c = k < a.teacher.K ? s.cls[k] : -1;
                 float q = 0.0f;
-                if (c >= 0 && s.q[k] > 0.0f) {
-                    bool first = true;
-                    for (int j = 0; j < k; ++j) first &= s.cls[j] != c || !(s.q[j] > 0.0f);
-                    if (first) q = class_weight(s, a.teacher.K, k);
+                bool first = c >= 0 && s.q[k] > 0.0f;
+                for (int j0 = 0; j0 < a.teacher.K; j0 += 64) {
+                    const int cj = j0 + lane < a.teacher.K ? s.cls[j0 + lane] : -1, n = min(64, a.teacher.K - j0);
+                    const float qj = j0 + lane < a.teacher.K ? s.q[j0 + lane] : 0.0f;
+                    for (int j = 0; j < n; ++j) {
+                        const int other = __builtin_amdgcn_readlane(cj, j);
+                        const float more = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, qj), j));
+                        q += other == c ? more : 0.0f;
+                        first &= other != c || !(more > 0.0f) || j0 + j >= k;
+                    }
                 }
-                a.entry_q[m * a.teacher.K + k] = q;
-                if (a.tile_count && q > 0.0f) atomicAdd(&a.tile_count[(m >> 6) * ((a.V + 127) >> 7) + (c >> 7)], 1);
+                if (k < a.teacher.K) a.entry_q[m * a.teacher.K + k] = first ? q : 0.0f;
             }
             part = l16 == 0 ? part : 0.0f;
             part = wave_sum(part);
@@ -555,21 +568,22 @@ __global__ __launch_bounds__(256) void row_topk_kernel(const float* u, long long
         seen += __popcll(same);
     }
     wave_sync();
+    static_assert(LOSS_MAX_TOP == 256, "four words a lane");
     uint32_t strip[LOSS_MAX_TOP / 64];                   // number 64 i + l of the chosen strips at lane l
 #pragma unroll
     for (int i = 0; i < LOSS_MAX_TOP / 64; ++i) strip[i] = 64 * i + lane < chosen ? s.col[TOP_LIST - LOSS_MAX_TOP + 64 * i + lane] : 0u;
     wave_sync();
     int n = 0;
     bool beyond = false;                                 // only what is larger than t is wanted any more
-#pragma unroll
-    for (int part = 0; part < LOSS_MAX_TOP / 64; ++part) {
+    for (int part = 0; 64 * part < chosen; ++part) {
         const int here = min(64, chosen - 64 * part);
+        const int strips_here = (int)(part == 0 ? strip[0] : part == 1 ? strip[1] : part == 2 ? strip[2] : strip[3]);
         for (int j0 = 0; j0 < here; j0 += AHEAD) {
             float x[AHEAD];
             int col[AHEAD];
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
-                col[j] = j0 + j < here ? (int)__builtin_amdgcn_readlane((int)strip[part], j0 + j) * LOSS_STRIP + lane : V;
+                col[j] = j0 + j < here ? (int)__builtin_amdgcn_readlane(strips_here, j0 + j) * LOSS_STRIP + lane : V;
                 x[j] = col[j] < V ? row[col[j]] : 0.0f;
             }
 #pragma unroll
