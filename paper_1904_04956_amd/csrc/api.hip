@@ -409,7 +409,7 @@ int twin_backward(blstm_ctx* ctx, const void* theta, const void* x, const void* 
 // (Zp columns), and what the products then leave padded goes back to its compact place.
 struct LossScratch {
     int Zp;                   // width of the products: Z rounded up to eight
-    bool copy_w, compact;     // W_s is copied; dz and dW_s are compacted
+    bool compact;             // W_s is copied (else it starts at a whole 16-byte word: everything in front of it has eight times some rows); dz and dW_s are compacted
     long long ldu;            // row distance of the logits / of dE/du
     int chunk;                // rows whose logits are held at a time (calls without gradients)
     bool strips;              // largest logits: by the strips' maxima
@@ -445,7 +445,6 @@ LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
     const bool bf = c->st == DT_BF16, gradient = call == SOFTMAX_DISTILL || call == SOFTMAX_POLICY;
     l.Zp = (c->zdim + 7) & ~7;
     l.compact = l.Zp != c->zdim;
-    l.copy_w = l.compact || c->off_ws * e % 16 != 0;
     l.ldu = (c->V + 7) & ~7;
     size_t w = 0;
     auto put = [&](size_t* at, size_t bytes) { *at = w; w += up256(bytes); };
@@ -453,8 +452,8 @@ LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
     size_t chunk = kLossChunkBytes / per_row & ~size_t(127);
     if (chunk < 128) chunk = 128;
     l.chunk = (int)(chunk < M ? chunk : M);
-    if (l.copy_w) put(&l.wp, V * l.Zp * e);
-    if (gradient || l.copy_w) put(&l.zc, M * l.Zp * e);
+    if (l.compact) put(&l.wp, V * l.Zp * e);
+    if (gradient || l.compact) put(&l.zc, M * l.Zp * e);
     if (bf && call != SOFTMAX_TOPK) {
         const size_t strips = (size_t)loss_strips(c->V);
         put(&l.label_logit, M * 4);
@@ -559,7 +558,7 @@ int loss_begin(blstm_ctx* ctx, const LossScratch& l, const void* theta, const vo
     c->W = ::at(theta, ctx->off_ws, ctx->esz); c->b = ::at(theta, ctx->off_bs, ctx->esz);
     c->z = z;
     c->zc = z;
-    if (l.copy_w) {
+    if (l.compact) {
         const BlockTensor t{ctx->off_ws, 0, 1, ctx->V, ctx->V, 1, ctx->zdim, l.Zp};
         RUN(PC_MISC, "padded softmax layer", launch_pad_blocks(&t, 1, theta, c->base + l.wp, ctx->st, st));
         c->W = c->base + l.wp;
@@ -689,9 +688,9 @@ int loss_run(blstm_ctx* ctx, const LossCall& given, const int32_t* labels, const
     const LossScratch& l = c.l;
     const int M = ctx->M, V = ctx->V;
     const bool gradient = policy || teacher;
-    if (gradient || l.copy_w) c.zc = c.base + l.zc;
+    if (gradient || l.compact) c.zc = c.base + l.zc;
     const bool bf = ctx->st == DT_BF16;
-    if (bf || gradient || l.copy_w) {
+    if (bf || gradient || l.compact) {
         LossPrepArgs a{};
         a.z = c.z; a.zc = c.zc == c.z ? nullptr : c.base + l.zc; a.M = M; a.V = V; a.Z = ctx->zdim; a.ldzc = l.Zp;
         a.labels = labels;
@@ -1167,7 +1166,7 @@ int softmax_topk(blstm_ctx* ctx, const void* theta, const void* z, int K, float*
     LossCall c;
     rc = loss_begin(ctx, l, theta, z, scratch, st, &c);
     if (rc != BLSTM_OK) return rc;
-    if (l.copy_w) {
+    if (l.compact) {
         const BlockTensor t{0, 0, 1, ctx->M, ctx->M, 1, ctx->zdim, l.Zp};
         RUN(PC_MISC, "padded z", launch_pad_blocks(&t, 1, z, c.base + l.zc, ctx->st, st));
         c.zc = c.base + l.zc;

@@ -531,3 +531,115 @@ def test_a_teacher_a_student_and_a_policy_step(dims, mode):
     finally:
         teacher.close()
         student.close()
+
+
+@pytest.mark.parametrize("shape", [(2, 4150, 140, 40), (1, 8200, 70, 264), (1, 90, 40000, 24)], ids=layer_id)
+@pytest.mark.parametrize("mode", [1, 0])
+def test_many_frames_and_many_classes(shape, mode):
+    # more than 8192 frames, classes in parts of the rows, float rows that no workgroup holds in registers
+    test_policy(shape, mode, "ragged", True, True)
+    test_distillation(shape, mode, "ragged", 2.0, 0.5)
+    test_distillation(shape, mode, "ragged", 2.0, 0.0)
+    test_log_probabilities(shape, mode, "ragged")
+
+
+@pytest.mark.parametrize("shape,K,tau,hard", [((2, 70, 200, 96), 150, 2.0, 0.5), ((2, 70, 200, 96), 150, 2.0, 0.0), ((1, 130, 300, 256), 256, 1.0, 0.5), ((2, 70, 260, 264), 129, 3.0, 0.25),
+                                              ((1, 70, 140000, 16), 40, 2.0, 0.5), ((3, 1400, 150, 32), 100, 2.0, 0.0)], ids=layer_id)
+@pytest.mark.parametrize("mode", [1, 0])
+def test_long_lists(shape, K, tau, hard, mode):
+    # several thousand entries in a block of 64 frames and 128 classes, or more blocks than threads that count them
+    T, B, V, Z = shape
+    layer = Layer(T, B, V, Z, mode, 31, loss_scale=0.125)
+    try:
+        lab = layer.labels("ragged")
+        values, classes = layer.lists(K, "ragged")
+        classes[5, :] = classes[5, 0] if classes[5, 0] >= 0 else 7      # one class all along a list
+        given = lab if hard else np.full_like(lab, sl.NO_LABEL)
+        q, some = sl.teacher_distribution(values, classes, V, tau)
+        ref = sl.distill(layer.W, layer.b, layer.z.double().numpy(), given, values, classes, float(layer.s), tau, hard, 0.75)
+        got = layer.distill(lab if hard else None, values, classes, tau, hard, 0.75)
+        live = (given != sl.NO_LABEL) | some
+        _, rel = layer.errors(live, max(1.0, 1 / tau))
+        du = du_of(layer, given, None, q, some, tau, hard, 0.75)
+        layer.check_gradients(got, ref[1:], du, live, rel + K * U + 64 * U * (1 + 8 / tau))
+        again = layer.distill(lab if hard else None, values, classes, tau, hard, 0.75)
+        for key in ("loss", "dz", "dW", "db"):
+            assert np.array_equal(got[key], again[key]), key
+    finally:
+        layer.close()
+
+
+@pytest.mark.parametrize("mode", [1, 0])
+@pytest.mark.parametrize("T,B,V,Z,K", [(1, 67, 140000, 16, 256), (1, 4600, 60000, 16, 20), (1, 2, 70001, 264, 3)])
+def test_the_largest_of_very_many(T, B, V, Z, K, mode):
+    # more strips than a wavefront chooses from, and more logits than are held at a time
+    import torch
+    layer = grid_layer(T, B, V, Z, mode, 32)
+    try:
+        values, classes = run_topk(layer, K)
+        W = layer.theta[layer.at_w:layer.at_w + V * Z].view(V, Z).float().cuda()
+        b = layer.theta[layer.at_b:layer.at_b + V].float().cuda()
+        for m0 in range(0, layer.M, 512):
+            u = layer.z[m0:m0 + 512].float().cuda() @ W.t() + b             # (exact, as every product and sum)
+            # equal values by falling order of V - class: whole numbers of 1/64
+            key = (u * 64).round().long() * (1 << 22) + ((1 << 22) - 1 - torch.arange(V, device="cuda"))
+            at = (1 << 22) - 1 - (torch.topk(key, K, dim=1).values & ((1 << 22) - 1))
+            assert np.array_equal(classes[m0:m0 + 512], at.cpu().numpy())
+            assert np.array_equal(values[m0:m0 + 512], u.gather(1, at).double().cpu().numpy())
+    finally:
+        layer.close()
+
+
+@pytest.mark.parametrize("mode", [1, 0])
+@pytest.mark.parametrize("Z", [64, 67, 320])
+def test_calls_without_gradients_in_a_replayed_graph_and_on_a_stream(mode, Z):
+    import torch
+    layer = grid_layer(3, 50, 900, Z, mode, 33)
+    bl = layer.bl
+    try:
+        theta, z, lab = layer.dev(layer.theta), layer.dev(layer.z).clone(), layer.dev(layer.labels("ragged"))
+        side = torch.cuda.Stream()
+
+        def made():
+            return dict(logp=torch.zeros(layer.M, device="cuda"), values=torch.zeros(layer.M, 11, device="cuda"), classes=torch.zeros(layer.M, 11, dtype=torch.int32, device="cuda"),
+                        s1=layer.scratch(bl.SOFTMAX_LOGPROB), s2=layer.scratch(bl.SOFTMAX_TOPK, 11))
+
+        def calls(o, stream=None):
+            bl.softmax_logprob(layer.ctx, theta, z, lab, o["logp"], o["s1"], None, stream)
+            bl.softmax_topk(layer.ctx, theta, z, 11, o["values"], o["classes"], o["s2"], None, stream)
+
+        held, eager = made(), made()
+        torch.cuda.synchronize()
+        calls(held, side)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            calls(held)
+        for k in range(4):
+            z.copy_(layer.z[torch.randperm(layer.M, generator=torch.Generator().manual_seed(k))])
+            for key in ("s1", "s2"):
+                held[key].fill_(0xFF)
+            graph.replay()
+            calls(eager)
+            torch.cuda.synchronize()
+            for key in ("logp", "values", "classes"):
+                assert torch.equal(held[key], eager[key]), (k, key)
+    finally:
+        layer.close()
+
+
+@pytest.mark.parametrize("mode", [1, 0])
+@pytest.mark.parametrize("Z,dims", [(64, dict(D=7, H=3)), (0, dict(D=5, H=4)), (5, dict(D=3, H=5)), (0, dict(D=3, H=133))], ids=str)
+def test_other_widths_of_the_model(mode, Z, dims):
+    # cells and bottlenecks of odd widths in front of W_s, z as wide as the cells of both directions
+    layer = Layer(2, 33, 150, Z or 2 * dims["H"], mode, 34, **dims, **({} if Z else dict(P=0)))
+    try:
+        lab = layer.labels("ragged")
+        live = lab != sl.NO_LABEL
+        A = layer.rng.normal(size=layer.M).astype(np.float32)
+        want = sl.policy(layer.W, layer.b, layer.z.double().numpy(), lab, A, None, None, float(layer.s), 0.2, 0.2, 0.0)
+        got = layer.policy(lab, A, None, None, 0.2, 0.2, 0.0)
+        eu, rel = layer.errors(live)
+        layer.check_gradients(got, want[2:], du_of(layer, lab, np.abs(A)), live, rel + 32 * U)
+    finally:
+        layer.close()

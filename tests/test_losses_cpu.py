@@ -183,3 +183,18 @@ def test_a_deferred_weight_gradient_is_dropped(recorder):  # noqa: F811
             out.append(bl.lib().blstm_backward(m.ctx, P, P, P, 2 * P, None))
     """)
     assert (a, b) == (-2, 0)
+
+
+def test_lists_beyond_32_bits_are_refused():
+    # T B K entries, and T B V / 2^13 blocks of them
+    for T, B, V, K, ok in ((1 << 12, 1 << 12, 128, 127, True), (1 << 12, 1 << 12, 128, 128, False), (1 << 12, 1 << 12, (1 << 20) + 1, 1, False)):
+        c = bl.blstm_create(T, B, 2, 4, 1, 0, V, 1)
+        try:
+            if ok:
+                assert bl.softmax_scratch_bytes(c, bl.SOFTMAX_DISTILL, K) > 1 << 32
+            else:
+                with pytest.raises(bl.BlstmError):
+                    bl.softmax_scratch_bytes(c, bl.SOFTMAX_DISTILL, K)
+                assert bl.softmax_scratch_bytes(c, bl.SOFTMAX_TOPK, K) > 0
+        finally:
+            bl.blstm_destroy(c)
