@@ -51,7 +51,7 @@ class Learner:
         self.z = torch.zeros((T, B, self.zdim), dtype=self.act_dtype, device=dev)
         self.dz = torch.zeros((T, B, self.zdim), dtype=self.act_dtype, device=dev)
         self.loss = torch.zeros(1, dtype=torch.float32, device=dev)
-        self.scratch = None       # of the softmax layer's calls beyond cross-entropy, made when one is first used
+        self.scratch = {}         # of the softmax layer's calls beyond cross-entropy, each made when it is first used
         self.held = None          # HYBRID only: the pulled weights the next gradient is taken on
 
     def close(self):
@@ -99,19 +99,25 @@ class Learner:
         bl.blstm_backward(self.ctx, th, self.x, self.dz, self.grad, stream)
 
     # ---- the softmax layer beyond cross-entropy ------------------------------------------
-    def loss_scratch(self, call, K=0):
-        """Scratch of one of the softmax layer's calls (binding.SOFTMAX_*), kept for the next time."""
-        need = bl.softmax_scratch_bytes(self.ctx, call, K)
-        if self.scratch is None or self.scratch.numel() < need:
-            self.scratch = torch.empty(need, dtype=torch.uint8, device=self.device)
-        return self.scratch
+    def loss_scratch(self, call, K=0, stream=None):
+        """Scratch of one of the softmax layer's calls (binding.SOFTMAX_*), kept for the next time: a captured graph holds its address."""
+        if (call, K) not in self.scratch:
+            self.scratch[call, K] = self._empty((bl.softmax_scratch_bytes(self.ctx, call, K),), torch.uint8, stream)
+        return self.scratch[call, K]
+
+    def _empty(self, shape, dtype, stream):
+        """Memory for a call on `stream` (the allocator hands out what other work on the stream that it belongs to may still be writing)."""
+        if stream is not None and not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream), device=self.device)
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
 
     def log_probs(self, labels=None, weights=None, stream=None):
         """log p[label] [T][B] of the batch (of `labels` if given, else its own): a forward pass, then the softmax layer."""
         th = self.theta_fwd if weights is None else weights
         bl.blstm_forward(self.ctx, th, self.x, self.z, stream)
-        out = torch.empty(self.labels.shape, dtype=torch.float32, device=self.device)
-        bl.softmax_logprob(self.ctx, th, self.z, self.labels if labels is None else labels, out, self.loss_scratch(bl.SOFTMAX_LOGPROB), None, stream)
+        out = self._empty(self.labels.shape, torch.float32, stream)
+        bl.softmax_logprob(self.ctx, th, self.z, self.labels if labels is None else labels, out, self.loss_scratch(bl.SOFTMAX_LOGPROB, 0, stream), None, stream)
         return out
 
     def top_logits(self, K, weights=None, stream=None):
@@ -119,8 +125,8 @@ class Learner:
         th = self.theta_fwd if weights is None else weights
         bl.blstm_forward(self.ctx, th, self.x, self.z, stream)
         shape = (*self.labels.shape, K)
-        values, classes = torch.empty(shape, dtype=torch.float32, device=self.device), torch.empty(shape, dtype=torch.int32, device=self.device)
-        bl.softmax_topk(self.ctx, th, self.z, K, values, classes, self.loss_scratch(bl.SOFTMAX_TOPK, K), None, stream)
+        values, classes = self._empty(shape, torch.float32, stream), self._empty(shape, torch.int32, stream)
+        bl.softmax_topk(self.ctx, th, self.z, K, values, classes, self.loss_scratch(bl.SOFTMAX_TOPK, K, stream), None, stream)
         return values, classes
 
     def calgrad_distill(self, values, classes, temperature=1.0, hard_weight=0.5, soft_weight=0.5, stream=None):
@@ -128,14 +134,14 @@ class Learner:
         K = classes.shape[-1]
         bl.blstm_forward(self.ctx, self.theta_fwd, self.x, self.z, stream)
         bl.softmax_distill_fwd_bwd(self.ctx, self.theta_fwd, self.z, self.labels if hard_weight != 0 else None, values, classes, K, temperature, hard_weight,
-                                   soft_weight, self.loss, self.dz, self.grad, self.loss_scratch(bl.SOFTMAX_DISTILL, K), None, stream)
+                                   soft_weight, self.loss, self.dz, self.grad, self.loss_scratch(bl.SOFTMAX_DISTILL, K, stream), None, stream)
         bl.blstm_backward(self.ctx, self.theta_fwd, self.x, self.dz, self.grad, stream)
 
     def calgrad_policy(self, advantage, old_logp=None, ref_logp=None, clip_low=0.2, clip_high=0.2, kl_weight=0.0, logp=None, stream=None):
         """calgrad() with the clipped policy loss on the batch's labels, which were sampled."""
         bl.blstm_forward(self.ctx, self.theta_fwd, self.x, self.z, stream)
         bl.softmax_policy_fwd_bwd(self.ctx, self.theta_fwd, self.z, self.labels, advantage, old_logp, ref_logp, clip_low, clip_high, kl_weight, self.loss, logp,
-                                  self.dz, self.grad, self.loss_scratch(bl.SOFTMAX_POLICY), None, stream)
+                                  self.dz, self.grad, self.loss_scratch(bl.SOFTMAX_POLICY, 0, stream), None, stream)
         bl.blstm_backward(self.ctx, self.theta_fwd, self.x, self.dz, self.grad, stream)
 
     def apply(self, lr, stream=None):

@@ -643,3 +643,39 @@ def test_other_widths_of_the_model(mode, Z, dims):
         layer.check_gradients(got, want[2:], du_of(layer, lab, np.abs(A)), live, rel + 32 * U)
     finally:
         layer.close()
+
+
+def test_a_learner_on_streams_and_in_a_graph_keeps_its_scratch():
+    import torch
+    from paper_1904_04956_amd import binding as bl
+    from paper_1904_04956_amd.harness import Learner
+    lrn = Learner(T=4, B=10, D=12, H=16, L=1, P=24, V=150, mode=1)
+    try:
+        rng = np.random.default_rng(35)
+        lrn.set_theta(rng.uniform(-0.1, 0.1, lrn.n).astype(np.float32))
+        lrn.set_batch(rng.standard_normal((4, 10, 12)).astype(np.float32), rng.integers(0, 150, (4, 10)).astype(np.int32))
+        lp, (values, classes) = lrn.log_probs(), lrn.top_logits(5)
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        for stream in (side, side.cuda_stream):
+            got, (v, c) = lrn.log_probs(stream=stream), lrn.top_logits(5, stream=stream)
+            side.synchronize()
+            assert torch.equal(got, lp) and torch.equal(v, values) and torch.equal(c, classes)
+        adv = torch.ones_like(lp)
+        lrn.calgrad_policy(adv, stream=side)
+        side.synchronize()
+        grad = lrn.grad.clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            lrn.calgrad_policy(adv)
+        at = lrn.loss_scratch(bl.SOFTMAX_POLICY).data_ptr()
+        for k in range(3):
+            lrn.calgrad_distill(values, classes, temperature=2.0)        # (other scratch, larger)
+            lrn.top_logits(100 + k)
+            torch.cuda.synchronize()
+            lrn.grad.fill_(-1.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(lrn.grad, grad) and lrn.loss_scratch(bl.SOFTMAX_POLICY).data_ptr() == at
+    finally:
+        lrn.close()
