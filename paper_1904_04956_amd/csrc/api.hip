@@ -423,21 +423,26 @@ static_assert(BLSTM_MAX_TOP == LOSS_MAX_TOP, "the kernels' lists must hold every
 constexpr size_t kLossChunkBytes = (size_t)1 << 30;
 
 // Into how many parts the classes of a workgroup's 256 rows are cut, and the rows of a workgroup's 128 classes: the least estimated
-// time (us) of rounds of one workgroup a CU, tile by tile, with what is written and read again for every part.
-int loss_parts(long long groups, long long tiles, double tile_us, double part_us) {
+// time (us) of rounds of `slots` workgroups, tile by tile (faster where a CU has one workgroup alone), with what is written and read
+// again for every part.  Against every number of parts around it, policy loss and log-probabilities of 64 .. 5376 rows of 2000, 8000 and
+// 32000 classes: the best or up to 4 % from it, 8 % where a call takes 60 us (336 rows of 32000: 86 us with 42 parts of the rows kernel,
+// 73 with 125, 101 with two of the classes kernel; 5376 rows of 2000: 309 us without parts of the classes kernel, 89 with them).
+int loss_parts(long long groups, long long tiles, int slots, double alone_us, double tile_us, double part_us) {
     int best = 1;
     double least = 0.0;
     for (long long p = 1; p <= tiles && p <= 256; ++p) {
-        const double rounds = (double)((groups * p + 255) / 256), t = rounds * ((double)((tiles + p - 1) / p) * tile_us + 4.0) + (p > 1 ? 3.0 : 0.0) + part_us * (double)p;
+        const long long rounds = (groups * p + slots - 1) / slots;
+        const double each = groups * p <= 256 ? alone_us : tile_us;
+        const double t = (double)rounds * ((double)((tiles + p - 1) / p) * each + 4.0) + (p > 1 ? 3.0 : 0.0) + part_us * (double)p;
         if (p == 1 || t < least) { least = t; best = (int)p; }
     }
     const long long per = (tiles + best - 1) / best;
     return (int)((tiles + per - 1) / per);               // (no empty part)
 }
-int loss_sum_parts(int M, int V, int Zp) { return loss_parts((M + 511) / 512, (V + 63) / 64, 4.2 * Zp / 256, 16.0 * M / 4e6); }   // (two workgroups a CU)
+int loss_sum_parts(int M, int V, int Zp) { return loss_parts((M + 255) / 256, (V + 63) / 64, 512, 2.2 * Zp / 256, 4.2 * Zp / 256, 0.005 + 16.0 * M / 4e6); }
+int loss_row_parts(int M, int V, int Zp) { return loss_parts((M + 255) / 256, (V + 63) / 64, 256, 3.4 * Zp / 256, 3.4 * Zp / 256, 1.5 * M * Zp * 4 / 4e6); }
+int loss_class_parts(int M, int V, int Zp) { return loss_parts((V + 127) / 128, (M + 63) / 64, 256, 2.4 * Zp / 256, 2.4 * Zp / 256, 2.5 * V * Zp * 4 / 4e6); }
 size_t loss_tiles(int M, int V) { return (size_t)((M + 63) / 64) * ((V + 127) / 128); }
-int loss_row_parts(int M, int V, int Zp) { return loss_parts((M + 255) / 256, (V + 63) / 64, 3.4 * Zp / 256, 1.5 * M * Zp * 4 / 4e6); }
-int loss_class_parts(int M, int V, int Zp) { return loss_parts((V + 127) / 128, (M + 63) / 64, 2.4 * Zp / 256, 2.5 * V * Zp * 4 / 4e6); }
 
 LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
     LossScratch l{};
