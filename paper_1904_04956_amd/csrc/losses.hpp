@@ -17,7 +17,7 @@ struct LossRow {
     float hot;
     int label;
     float max;                                       // of the row's logits
-    float pad;
+    float pad;                                       // (two 16-byte loads)
 };
 
 // u log2e - m2 is one multiply-add, whose m2 = max log2e is rounded: the same for all classes of a row, so that it cancels, but 2^-24 of

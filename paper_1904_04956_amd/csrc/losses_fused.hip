@@ -4,7 +4,18 @@
 //             w = exp(u - reference) and their sum (the reference moves with the running maximum), or with w = dE/du itself
 //             where the sums are known.  The label's and the teacher's classes, few a row, are added behind it, exactly.
 //   classes   a workgroup keeps 128 classes of W_s in registers and walks over the rows: dE/du from the rows' sums, then
-//             dW_s = du^T z and db_s.  du goes into the product as the sum of two bf16 numbers (of three where a label is).
+//             dW_s = du^T z and db_s.  du goes into the product as the sum of two bf16 numbers (2^-16; of three where a label is, and
+//             where a teacher's classes are and frames are few), into db_s as the float that it is.
+//
+// Why so: M rows of V float logits are written, read and written again by anything that keeps them (688 MB for 5376 rows of 32000, at
+// 4.8 TB/s as long as the whole product takes); made twice, they cost a product of M V Z each.  In dz a weight is one bf16
+// number, whose rounding (2^-8) the result's own rounding to bf16 matches; the label's class, where du is large, is added in float.
+//
+// Bound by the matrix units' turns with the rest of a wavefront: two wavefronts a SIMD, each of which multiplies, takes its
+// exponentials, transposes and multiplies again; the other covers part of it.  Z = 256, V = 32000, 43008 rows (705 GFLOP a unit of
+// M V Z; the matrix units reach 1.66 PFLOP/s from registers): rows 1130 us (two units, 1.25 PFLOP/s), classes 1650 us (three, 1.28);
+// 3633 rows: 122 and 168 us.  Two distributions (5376 rows, lists of 64): sums 105, rows 175, classes 335 us.  At 168 .. 336 rows
+// the parts of dz and the loads of W_s weigh as much: rows 21 .. 29 us, classes 26 .. 34.
 //
 // Both read a tile [64][Z] in LDS twice: by rows for the logits (ds_read_b128) and by columns for what is made of them
 // (ds_read_b64_tr_b16 transposes on the way).  16-byte chunk c of row r lies at chunk c ^ sw(r): the eight rows that a phase
@@ -212,7 +223,8 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
 
 // ---- rows, the sums alone -----------------------------------------------------------------------------------------------------
 // Reference and sum of exponentials of every row and part (SUMS2: at two scales, from one reference), or the logits themselves with the
-// maxima of strips of 64 classes (LOGITS).  Two workgroups a CU, four wavefronts a SIMD, so that some multiply while others take exponentials.
+// maxima of strips of 64 classes (LOGITS).  5376 rows of 32000, Z = 256 (88 GFLOP): 90 us (980 TFLOP/s), SUMS2 105, LOGITS 230, whose
+// 688 MB are stored at 3 TB/s (past L2 or with loads that do not wait for them no faster).  Two workgroups a CU, four wavefronts a SIMD, so that some multiply while others take exponentials.
 // Rows as in the rows kernel: of the 128 x 128 tiles that larger z take, both operands come from L2 for half the products.
 enum { SUMS, SUMS2, LOGITS };
 template <int NK, int WHAT>
