@@ -412,6 +412,7 @@ struct LossScratch {
     bool compact;             // W_s is copied (else it starts at a whole 16-byte word: everything in front of it has eight times some rows); dz and dW_s are compacted
     long long ldu;            // row distance of the logits / of dE/du
     int chunk;                // rows whose logits are held at a time (calls without gradients)
+    bool third;               // dE/du is split into three bf16 numbers for dW_s (fused: where a label or a teacher's classes are) instead of two
     bool strips;              // largest logits: by the strips' maxima
     bool fused;               // the kernels of losses_fused.hip: no du in memory
     int row_parts, sum_parts, class_parts;
@@ -421,6 +422,11 @@ struct LossScratch {
 static_assert(BLSTM_MAX_TOP == LOSS_MAX_TOP, "the kernels' lists must hold every entry");
 // Logits held at a time where they are only read once more.
 constexpr size_t kLossChunkBytes = (size_t)1 << 30;
+
+// Frames up to which dE/du has a third bf16 part.  Two are 2^-16 off where it is large, 2.5e-6 of dW_s together, where a sum of few
+// frames in float is 2e-7 off by itself, of 5376 1e-6 and of 43008 2e-6.  The third part costs a fifth of dW_s's product of wider z and nothing to
+// a third of the classes kernel (that much where every product of 32 x 32 holds a class of the teacher's).
+constexpr int kLossThirdRows = 4096;
 
 // Into how many parts the classes of a workgroup's 256 rows are cut, and the rows of a workgroup's 128 classes: the least estimated
 // time (us) of rounds of `slots` workgroups, tile by tile (faster where a CU has one workgroup alone), with what is written and read
@@ -458,7 +464,8 @@ LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
     if (chunk < 128) chunk = 128;
     l.chunk = (int)(chunk < M ? chunk : M);
     if (l.compact) put(&l.wp, V * l.Zp * e);
-    if (gradient || l.compact) put(&l.zc, M * l.Zp * e);
+    l.third = bf && gradient && c->M <= kLossThirdRows;
+    if (gradient || l.compact) put(&l.zc, (l.third && l.Zp > LOSS_FUSED_WIDTH ? 2 : 1) * M * l.Zp * e);
     if (bf && call != SOFTMAX_TOPK) {
         const size_t strips = (size_t)loss_strips(c->V);
         put(&l.label_logit, M * 4);
@@ -504,7 +511,7 @@ LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
         if (gradient) {
             put(&l.rows, M * sizeof(LossRow));
             put(&l.hi, M * (size_t)l.ldu * 2);
-            put(&l.lo, M * (size_t)l.ldu * 2);
+            put(&l.lo, (l.third ? 2 : 1) * M * (size_t)l.ldu * 2);
         }
     } else {
         put(&l.u, (gradient ? M : (size_t)l.chunk) * per_row);
@@ -518,9 +525,10 @@ LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
     if (!bf || call == SOFTMAX_TOPK) upd(gemm_partial_bytes(gradient ? c->M : l.chunk, c->V, l.Zp, 1, c->st, true));
     if (gradient) {
         put(&l.row_loss, M * 4);
-        if (l.compact) { put(&l.dzp, M * l.Zp * e); put(&l.dwp, V * l.Zp * 4); }
+        if (bf || l.compact) put(&l.dzp, M * l.Zp * 4);
+        if (l.compact) put(&l.dwp, V * l.Zp * 4);
         upd(gemm_partial_bytes(c->M, l.Zp, c->V, 1, c->st));
-        upd(gemm_partial_bytes(c->V, l.Zp, bf ? 2 * c->M : c->M, 1, c->st));
+        upd(gemm_partial_bytes(c->V, l.Zp, bf ? (l.third ? 3 : 2) * c->M : c->M, 1, c->st));
     }
     l.partial_bytes = up256(need);
     put(&l.partial, l.partial_bytes);
@@ -587,7 +595,7 @@ int loss_logits(blstm_ctx* ctx, const LossCall& c, int first, int rows, float* u
 }
 
 // From dE/du (bf16: hi + lo, float: u): dz, dW_s and db_s.
-int loss_products(blstm_ctx* ctx, const LossCall& c, void* dz, float* grad) {
+int loss_products(blstm_ctx* ctx, const LossCall& c, const TeacherArgs* teacher, void* dz, float* grad) {
     hipStream_t st = c.st;
     const LossScratch& l = c.l;
     const int M = ctx->M, V = ctx->V, Z = l.Zp;
@@ -601,24 +609,31 @@ int loss_products(blstm_ctx* ctx, const LossCall& c, void* dz, float* grad) {
         return d;
     };
     {   // dz = du W_s
-        GemmDesc d = desc(ctx->st);
+        GemmDesc d = desc(DT_F32);
         d.M = M; d.N = Z; d.btrans = true;
         d.seg[0] = GemmSeg{U, c.W, l.ldu, Z, 0, 0, V};
-        d.C = l.compact ? c.base + l.dzp : static_cast<char*>(dz); d.ldc = Z;
+        d.C = bf || l.compact ? c.base + l.dzp : static_cast<char*>(dz); d.ldc = Z;
         RUN(PC_GEMM_SOFTMAX_BWD, "dz", launch_gemm(d, st));
+        if (bf) {
+            LossDzEndArgs e{};
+            e.M = M; e.Z = ctx->zdim; e.ld = Z; e.dz_f = c.at<float>(l.dzp); e.rows = c.at<LossRow>(l.rows);
+            if (teacher) { e.K = teacher->K; e.classes = teacher->classes; e.entry_q = c.at<float>(l.entry_q); }
+            e.lo = c.at<unsigned short>(l.lo); e.ldu = l.ldu; e.W = static_cast<const unsigned short*>(c.W); e.dz = static_cast<unsigned short*>(dz);
+            RUN(PC_SOFTMAX_ROWS, "dz", launch_loss_dz_end(e, st));
+        }
     }
     {   // dW_s = du^T z with db_s as the row sums of du^T
         GemmDesc d = desc(DT_F32);
         d.M = V; d.N = Z; d.atrans = true; d.btrans = true;
         d.seg[0] = GemmSeg{U, c.zc, l.ldu, Z, 0, 0, M};
-        if (bf) { d.nseg = 2; d.seg[1] = d.seg[0]; d.seg[1].A = c.base + l.lo; }
+        if (bf) { d.nseg = 2; d.seg[1] = d.seg[0]; d.seg[1].A = c.base + l.lo; if (l.third) d.seg[1].K = 2 * M; }   // (z stands there twice)
         d.C = l.compact ? c.at<float>(l.dwp) : grad + ctx->off_ws; d.ldc = Z;
         d.rowsum = grad + ctx->off_bs;
         RUN(PC_GEMM_SOFTMAX_BWD, "dW_s", launch_gemm(d, st));
     }
     if (l.compact) {
         const BlockTensor tz{0, 0, 1, M, M, 1, ctx->zdim, Z}, tw{ctx->off_ws, 0, 1, V, V, 1, ctx->zdim, Z};
-        RUN(PC_MISC, "dz", launch_compact_blocks(&tz, 1, c.base + l.dzp, dz, ctx->st, st));
+        if (!bf) RUN(PC_MISC, "dz", launch_compact_blocks(&tz, 1, c.base + l.dzp, dz, ctx->st, st));
         RUN(PC_MISC, "softmax layer's gradient", launch_compact_blocks(&tw, 1, c.base + l.dwp, grad, DT_F32, st));
     }
     return BLSTM_OK;
@@ -675,9 +690,7 @@ int loss_run_fused(blstm_ctx* ctx, const LossCall& c, const int32_t* labels, con
     f.out = l.class_parts > 1 ? c.at<float>(l.cparts) : dw; f.out_db = l.class_parts > 1 ? c.at<float>(l.cparts_b) : db;
     f.ldo = ctx->zdim; f.vec = ctx->zdim % 4 == 0 && aligned16(f.out);
     if (!both) f.k1 = f.k;                               // (the only exponential is the first)
-    // Two bf16 are 2^-16 off where du is large, 2.5e-6 of dW_s together; a sum of thousands of frames in float is as far off by itself
-    // (5376 frames: 1e-6), and the third part costs up to a third of the kernel there (every product of 32 x 32 holds a class of the teacher's).
-    f.third = ctx->M <= 4096;
+    f.third = l.third;
     if (teacher) { f.entries = c.at<uint2>(l.entries); f.entries_from = c.at<int>(l.tile_from); f.entries_count = c.at<int>(l.tile_count); }
     f.row_loss = d.row_loss; f.loss = loss_dev;
     RUN(PC_GEMM_SOFTMAX_BWD, "dW_s and the loss", launch_loss_fused_classes(f, both, st));
@@ -699,7 +712,7 @@ int loss_run(blstm_ctx* ctx, const LossCall& given, const int32_t* labels, const
         LossPrepArgs a{};
         a.z = c.z; a.zc = c.zc == c.z ? nullptr : c.base + l.zc; a.M = M; a.V = V; a.Z = ctx->zdim; a.ldzc = l.Zp;
         a.labels = labels;
-        a.keep = !gradient;
+        a.keep = !gradient; a.twice = l.third && !l.fused;
         if (teacher) a.teacher = *teacher;
         if (bf) {
             a.W = static_cast<const unsigned short*>(c.W); a.bias = static_cast<const unsigned short*>(c.b);
@@ -730,7 +743,7 @@ int loss_run(blstm_ctx* ctx, const LossCall& given, const int32_t* labels, const
         t.inv_tau = teacher && teacher->inv_tau != 1.0f ? teacher->inv_tau : 0.0f;
         t.part_max = c.at<float>(l.pmax); t.part_sum = c.at<float>(l.psum); t.part_sum_tau = c.at<float>(l.ptau);
         t.rows = c.at<LossRow>(l.rows);
-        t.hi = c.at<unsigned short>(l.hi); t.lo = c.at<unsigned short>(l.lo); t.ldu = l.ldu;
+        t.hi = c.at<unsigned short>(l.hi); t.lo = c.at<unsigned short>(l.lo); t.ldu = l.ldu; t.third = l.third;
         RUN(PC_GEMM_LOGITS, "sums of the softmax", launch_loss_stats(t, st));
         LossMergeArgs g{};
         g.M = M; g.V = V; g.strips = loss_strips(V);
@@ -746,14 +759,14 @@ int loss_run(blstm_ctx* ctx, const LossCall& given, const int32_t* labels, const
                 LossEntriesArgs n{};
                 n.rows = t.rows; n.classes = teacher->classes; n.entry_logit = c.at<float>(l.entry_logit); n.entry_q = c.at<float>(l.entry_q);
                 n.inv_tau = t.inv_tau; n.weight = ctx->s * teacher->soft * teacher->tau;
-                n.M = M; n.V = V; n.K = teacher->K; n.hi = t.hi; n.lo = t.lo; n.ldu = l.ldu;
+                n.M = M; n.V = V; n.K = teacher->K; n.hi = t.hi; n.lo = t.lo; n.ldu = l.ldu; n.third = l.third;
                 RUN(PC_SOFTMAX_ROWS, "du of the teacher's classes", launch_loss_entries(n, st));
             }
         }
     }
     if (!gradient) return BLSTM_OK;
     RUN(PC_MISC, "loss sum", launch_sum_to_scalar(c.at<float>(l.row_loss), M, loss_dev, st));
-    return loss_products(ctx, c, dz, grad);
+    return loss_products(ctx, c, teacher, dz, grad);
 }
 
 // What softmax_xent_fwd_bwd left to the next blstm_backward is written by the call itself.

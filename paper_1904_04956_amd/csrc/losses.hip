@@ -11,8 +11,8 @@
 // larger tile of one workgroup a CU would halve that and leave its exponentials without anything beside them.  5985 rows of 32000
 // classes, z of 524 (201 GFLOP): the sums 300 us (670 TFLOP/s), du 480 us, 766 MB of stores among them; 1344 rows, z of 1024: 99 us (890).
 //
-// du is kept as two bf16 numbers, hi and what the rounding left: both enter dW_s and db_s (2^-16 of the larger value), hi alone
-// enters dz, whose own rounding to bf16 is as large.
+// du is kept as bf16 numbers: hi, what the rounding left, and, where frames are few, what that left.  All enter dW_s and db_s; hi alone
+// enters the product for dz, to which the second is added where du is large.
 #include "gemm_tile.hpp"
 #include "losses_terms.hpp"
 
@@ -179,23 +179,26 @@ __global__ __launch_bounds__(256, 2) void loss_tile_kernel(LossTileArgs a, int n
 #pragma unroll
                     for (int e = 0; e < 16; ++e) d[e] -= rel == j * 32 + 8 * (e >> 2) + 4 * half + (e & 3) ? r.hot : 0.0f;
                 }
-                unsigned hi[8], lo[8];
+                // d rounded, to `to`; then d is what the rounding left
+                auto part = [&](unsigned short* to) __attribute__((always_inline)) {
+                    unsigned p[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    hi[e] = pack_bf2(d[2 * e], d[2 * e + 1]);
-                    lo[e] = pack_bf2(d[2 * e] - bf2f((bf16_t)(hi[e] & 0xFFFFu)), d[2 * e + 1] - bf2f((bf16_t)(hi[e] >> 16)));
-                }
-                // an exchange between the lane halves makes four neighbouring classes eight
-#pragma unroll
-                for (int g = 0; g < 4; g += 2) {
-                    const int n = col0 + wn * 64 + j * 32 + 8 * (g + half);
-                    const auto h0 = __builtin_amdgcn_permlane32_swap(hi[2 * g], hi[2 * g + 2], false, false), h1 = __builtin_amdgcn_permlane32_swap(hi[2 * g + 1], hi[2 * g + 3], false, false);
-                    const auto l0 = __builtin_amdgcn_permlane32_swap(lo[2 * g], lo[2 * g + 2], false, false), l1 = __builtin_amdgcn_permlane32_swap(lo[2 * g + 1], lo[2 * g + 3], false, false);
-                    if (m < a.M && n < a.ldu) {
-                        *reinterpret_cast<uint4*>(a.hi + m * a.ldu + n) = make_uint4(h0[0], h1[0], h0[1], h1[1]);
-                        *reinterpret_cast<uint4*>(a.lo + m * a.ldu + n) = make_uint4(l0[0], l1[0], l0[1], l1[1]);
+                    for (int e = 0; e < 8; ++e) {
+                        p[e] = pack_bf2(d[2 * e], d[2 * e + 1]);
+                        d[2 * e] -= bf2f((bf16_t)(p[e] & 0xFFFFu));
+                        d[2 * e + 1] -= bf2f((bf16_t)(p[e] >> 16));
                     }
-                }
+                    // an exchange between the lane halves makes four neighbouring classes eight
+#pragma unroll
+                    for (int g = 0; g < 4; g += 2) {
+                        const int n = col0 + wn * 64 + j * 32 + 8 * (g + half);
+                        const auto x = __builtin_amdgcn_permlane32_swap(p[2 * g], p[2 * g + 2], false, false), y = __builtin_amdgcn_permlane32_swap(p[2 * g + 1], p[2 * g + 3], false, false);
+                        if (m < a.M && n < a.ldu) *reinterpret_cast<uint4*>(to + m * a.ldu + n) = make_uint4(x[0], y[0], x[1], y[1]);
+                    }
+                };
+                part(a.hi);
+                part(a.lo);
+                if (a.third) part(a.lo + a.M * a.ldu);
             }
         }
     }

@@ -47,6 +47,7 @@ struct LossPrepArgs {
     void* zc;                                        // or null: not wanted
     bool keep;                                       // rows that count for nothing are copied as they are
     int M, V, Z, ldzc;
+    int twice;                                       // (bf16) zc is written a second time behind the first
     const unsigned short* W;                         // rows of ldzc elements, zeros behind Z; null: only zc is wanted
     const unsigned short* bias;
     float* bias_f;                                   // [V rounded up to 64] the bias as floats, bias_pad behind it; or null
@@ -73,7 +74,8 @@ struct LossTileArgs {
     float* part_sum_tau;                             // [strips][M] the same at the temperature
     const LossRow* rows;                             // gradient: [M]
     unsigned short* hi;                              // [M][ldu] du rounded to bf16, zeros in columns V .. ldu - 1
-    unsigned short* lo;                              // [M][ldu] what the rounding left, rounded
+    unsigned short* lo;                              // [M][ldu] what the rounding left, rounded; with third, [M][ldu] of what that left behind it
+    int third;
     long long ldu;
     float* logits;                                   // [M][ldu]
 };
@@ -180,8 +182,22 @@ struct LossEntriesArgs {
     unsigned short* hi;
     unsigned short* lo;
     long long ldu;
+    int third;                                       // as in LossTileArgs
 };
 hipError_t launch_loss_entries(const LossEntriesArgs& a, hipStream_t st);
+// dz, rounded, from the product of du's first part in float and, of the second, the label's and the teacher's classes.
+struct LossDzEndArgs {
+    int M, Z, ld, K;                                 // K 0: no teacher
+    const float* dz_f;                               // [M][ld]
+    const LossRow* rows;
+    const int32_t* classes;                          // [M][K]
+    const float* entry_q;                            // [M][K], 0: none
+    const unsigned short* lo;
+    long long ldu;
+    const unsigned short* W;                         // [V][ld]
+    unsigned short* dz;                              // [M][Z]
+};
+hipError_t launch_loss_dz_end(const LossDzEndArgs& a, hipStream_t st);
 
 // float: everything of a row from its logits u [M][ldu], which dE/du overwrites (gradient false: they stay).
 struct LossRowsArgs {
