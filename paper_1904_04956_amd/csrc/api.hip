@@ -674,7 +674,7 @@ int loss_run_fused(blstm_ctx* ctx, const LossCall& c, const int32_t* labels, con
     }
     f.parts = l.row_parts;
     f.out = c.at<float>(l.part);
-    RUN(PC_GEMM_LOGITS, "rows of the softmax", launch_loss_fused_rows(f, both, both, st));
+    RUN(PC_GEMM_LOGITS, "rows of the softmax", launch_loss_fused_rows(f, both, st));
     LossDzArgs d{};
     d.M = f.M; d.Mp = f.Mp; d.V = f.V; d.Z = f.Z; d.ld = f.ld; d.parts = f.parts;
     d.part = f.out; d.part_ref = f.part_ref; d.part_sum = f.part_sum; d.W = f.W;

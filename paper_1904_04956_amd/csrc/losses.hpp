@@ -108,7 +108,7 @@ struct LossFusedArgs {
     int vec;                                         // classes: rows of out take 16-byte stores
     int third;                                       // classes: a third part of du where a teacher's classes are
 };
-hipError_t launch_loss_fused_rows(const LossFusedArgs& a, bool known, bool tau, hipStream_t st);
+hipError_t launch_loss_fused_rows(const LossFusedArgs& a, bool known, hipStream_t st);   // known: the two distributions' sums
 // The rows' sums alone at the scale k1 and, with second, k from references part_ref (a logit); or, with logits, u into out [M][ldo] (ldo a multiple
 // of four; NaN behind V counts as no maximum) and the maxima of strips of 64 classes into part_ref [strips][M].
 hipError_t launch_loss_fused_sums(const LossFusedArgs& a, bool second, bool logits, hipStream_t st);

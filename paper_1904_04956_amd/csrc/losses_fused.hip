@@ -105,8 +105,8 @@ __device__ __forceinline__ void ahead() {
 constexpr int DEPTH = 4;
 
 // ---- rows -------------------------------------------------------------------------------------------------------------------
-// KNOWN: w = a exp2(u log2e - m2) (+ at exp2(u k - mt2)) from the rows' constants, else w = exp2(u k - reference).
-template <int NK, bool KNOWN, bool TAU>
+// KNOWN: w = a exp2(u log2e - m2) + at exp2(u k - mt2) from the rows' constants, else w = exp2(u k - reference).
+template <int NK, bool KNOWN>
 __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
     typedef Ring<NK> R;
     extern __shared__ uint4 smem[];
@@ -124,8 +124,7 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
     }
     float m2 = 0.0f, ca = 0.0f, mt2 = 0.0f, cat = 0.0f;
     if (KNOWN && m < a.Mp) {
-        m2 = a.consts[m]; ca = a.consts[a.Mp + m];
-        if (TAU) { mt2 = a.consts[2 * a.Mp + m]; cat = a.consts[3 * a.Mp + m]; }
+        m2 = a.consts[m]; ca = a.consts[a.Mp + m]; mt2 = a.consts[2 * a.Mp + m]; cat = a.consts[3 * a.Mp + m];
     }
     __builtin_amdgcn_s_waitcnt(0);                      // (known to the compiler: it would wait for these loads, and the ring's with them, in the loop)
     auto issue = [&](int it) __attribute__((always_inline)) {
@@ -187,7 +186,7 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
                         const float x = u[8 * t + e + i];
                         if constexpr (KNOWN) {
                             w[i] = ca * __builtin_amdgcn_exp2f(fmaf(x, a.k1, -m2));
-                            if (TAU) w[i] = fmaf(cat, __builtin_amdgcn_exp2f(fmaf(x, k, -mt2)), w[i]);
+                            w[i] = fmaf(cat, __builtin_amdgcn_exp2f(fmaf(x, k, -mt2)), w[i]);
                         } else {
                             w[i] = __builtin_amdgcn_exp2f(fmaf(x, k, -ref));
                             sum += w[i];
@@ -702,13 +701,13 @@ __global__ __launch_bounds__(256) void loss_dz_kernel(LossDzArgs a, PolicyArgs p
     for (int i = 0; i < 4; ++i) if (z0 + i < a.Z) a.dz[m * a.Z + z0 + i] = f2bf(x[i]);
 }
 
-template <int NK, bool KNOWN, bool TAU>
+template <int NK, bool KNOWN>
 hipError_t rows_nk(const LossFusedArgs& a, hipStream_t st) {
     constexpr size_t lds = (size_t)Ring<NK>::STAGES * Ring<NK>::STAGE;
     static thread_local bool attr_set = false;
-    const hipError_t e = allow_lds(&loss_rows_kernel<NK, KNOWN, TAU>, lds, &attr_set);
+    const hipError_t e = allow_lds(&loss_rows_kernel<NK, KNOWN>, lds, &attr_set);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((loss_rows_kernel<NK, KNOWN, TAU>), dim3((unsigned)((a.M + 255) / 256 * a.parts)), dim3(512), lds, st, a);
+    hipLaunchKernelGGL((loss_rows_kernel<NK, KNOWN>), dim3((unsigned)((a.M + 255) / 256 * a.parts)), dim3(512), lds, st, a);
     return hipGetLastError();
 }
 template <int NK, int WHAT>
@@ -732,9 +731,9 @@ hipError_t classes_nk(const LossFusedArgs& a, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_loss_fused_rows(const LossFusedArgs& a, bool known, bool tau, hipStream_t st) {
+hipError_t launch_loss_fused_rows(const LossFusedArgs& a, bool known, hipStream_t st) {
     const int nk = (a.ld + 63) / 64;
-#define BLSTM_ROWS(NK) return known ? (tau ? rows_nk<NK, true, true>(a, st) : rows_nk<NK, true, false>(a, st)) : rows_nk<NK, false, false>(a, st)
+#define BLSTM_ROWS(NK) return known ? rows_nk<NK, true>(a, st) : rows_nk<NK, false>(a, st)
     if (nk == 1) BLSTM_ROWS(1);
     if (nk == 2) BLSTM_ROWS(2);
     if (nk == 3) BLSTM_ROWS(3);
