@@ -118,8 +118,8 @@ int softmax_xent_fwd_bwd_noalloc(blstm_ctx* ctx, const void* theta, const void* 
    - The calls with gradients write loss_dev[0], dz [T][B][P or 2H] and, of grad, the slices W_s and b_s (overwritten): what
      softmax_xent_fwd_bwd writes, in its place in front of blstm_backward (BLSTM_OPT_DEFER_SOFTMAX_WGRAD does not concern
      them; what an earlier softmax_xent_fwd_bwd left to blstm_backward is dropped).  Mode 1: logits and all sums in float,
-     dE/du enters the product for dz as one bf16 number and those for W_s and b_s as the sum of two (2^-16) at least.  The
-     same inputs give the same bits.  A class is ruled out by a bias of -inf or of the type's lowest value; in mode 1 logits
+     dE/du (where a label or a teacher's class is, the difference, not its two sides) enters the product for dz as one bf16
+     number and those for W_s and b_s as the sum of two (2^-16) at least.  The same inputs give the same bits.  A class is ruled out by a bias of -inf or of the type's lowest value; in mode 1 logits
      below -1e5 are ruled out too, and the results of a frame all of whose logits are have no meaning. */
 #define BLSTM_NO_LABEL (-1)
 #define BLSTM_MAX_TOP 256                      /* the most entries of a list of largest logits */

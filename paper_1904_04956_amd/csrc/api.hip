@@ -416,7 +416,7 @@ struct LossScratch {
     bool strips;              // largest logits: by the strips' maxima
     bool fused;               // the kernels of losses_fused.hip: no du in memory
     int row_parts, sum_parts, class_parts;
-    size_t bias_f, consts, part, part_ref, part_sum, part_sum2, cparts, cparts_b, tile_count, tile_from, entries;
+    size_t bias_f, consts, part, part_ref, part_sum, part_sum2, cparts, cparts_b, tile_count, tile_from, entries, marks;
     size_t zc, wp, dzp, dwp, label_logit, entry_logit, entry_q, soft_const, soft_state, pmax, psum, ptau, rows, row_loss, hi, lo, u, partial, partial_bytes, bytes;
 };
 static_assert(BLSTM_MAX_TOP == LOSS_MAX_TOP, "the kernels' lists must hold every entry");
@@ -495,6 +495,7 @@ LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
                 put(&l.tile_count, tiles * 4);
                 put(&l.tile_from, tiles * 4);
                 put(&l.entries, (M * K + LOSS_LIST_SLACK) * 8);
+                put(&l.marks, (size_t)loss_mark_words(c->V) * ((M + 255) & ~size_t(255)) * 4);
             }
             l.bytes = w;
             return l;
@@ -649,13 +650,15 @@ int loss_run_fused(blstm_ctx* ctx, const LossCall& c, const int32_t* labels, con
     LossFusedArgs f{};
     f.z = static_cast<const unsigned short*>(c.zc); f.W = static_cast<const unsigned short*>(c.W);
     f.bias = c.at<float>(l.bias_f); f.consts = c.at<float>(l.consts);
-    f.M = ctx->M; f.Mp = (ctx->M + 63) & ~63; f.V = ctx->V; f.Z = ctx->zdim; f.ld = l.Zp;
+    f.M = ctx->M; f.Mp = (ctx->M + 63) & ~63; f.Mr = (ctx->M + 255) & ~255; f.V = ctx->V; f.Z = ctx->zdim; f.ld = l.Zp;
     f.k1 = log2e; f.k = teacher ? log2e * teacher->inv_tau : log2e;
     f.part_ref = c.at<float>(l.part_ref); f.part_sum = c.at<float>(l.part_sum);
+    f.labels = gradient ? labels : nullptr;
     if (teacher) {
         LossListArgs e{};
         e.M = ctx->M; e.V = ctx->V; e.K = teacher->K; e.classes = teacher->classes; e.q = c.at<float>(l.entry_q); e.weight = ctx->s * teacher->soft * teacher->tau;
         e.count = c.at<int>(l.tile_count); e.from = c.at<int>(l.tile_from); e.entries = c.at<uint2>(l.entries);
+        e.labels = labels; e.marks = c.at<uint32_t>(l.marks); e.Mr = f.Mr;
         RUN(PC_SOFTMAX_ROWS, "the teacher's classes by tiles", launch_loss_lists(e, st));
     }
     if (!gradient || both) {
@@ -674,13 +677,14 @@ int loss_run_fused(blstm_ctx* ctx, const LossCall& c, const int32_t* labels, con
     }
     f.parts = l.row_parts;
     f.out = c.at<float>(l.part);
+    if (teacher) f.marks = c.at<uint32_t>(l.marks);
     RUN(PC_GEMM_LOGITS, "rows of the softmax", launch_loss_fused_rows(f, both, st));
     LossDzArgs d{};
     d.M = f.M; d.Mp = f.Mp; d.V = f.V; d.Z = f.Z; d.ld = f.ld; d.parts = f.parts;
     d.part = f.out; d.part_ref = f.part_ref; d.part_sum = f.part_sum; d.W = f.W;
     d.labels = labels; d.label_logit = c.at<float>(l.label_logit); d.s = ctx->s;
     d.policy = policy; d.teacher = teacher;
-    d.entry_q = c.at<float>(l.entry_q); d.soft_const = c.at<float>(l.soft_const); d.soft_state = c.at<int>(l.soft_state);
+    d.entry_logit = c.at<float>(l.entry_logit); d.entry_q = c.at<float>(l.entry_q); d.soft_const = c.at<float>(l.soft_const); d.soft_state = c.at<int>(l.soft_state);
     d.logp = logp; d.row_loss = c.at<float>(l.row_loss); d.consts = c.at<float>(l.consts);
     d.dz = static_cast<unsigned short*>(dz);
     RUN(PC_SOFTMAX_ROWS, "dz", launch_loss_dz(d, both, st));

@@ -90,11 +90,15 @@ struct LossFusedArgs {
     const unsigned short* z;                         // [M][ld], zeros in columns Z .. ld - 1
     const unsigned short* W;                         // [V][ld], likewise
     const float* bias;                               // [V rounded up to 64], -inf beyond V
-    const float* consts;                             // [6][Mp]: LossRow's m2, a, mt2, at, hot, label (as bits); rows M .. Mp - 1 count for nothing
+    const float* consts;                             // [6][Mp]: LossRow's m2, a, mt2, at, then minus all of du at the label, the label (as bits); rows M .. Mp - 1 count for nothing
     int M, Mp, V, Z, ld;                             // Mp: M rounded up to 64
     float k1, k;                                     // scale of the first exponential, and of the second (rows, sums not known: the only one)
     int parts;                                       // of the classes (rows kernel) or of the rows (classes kernel), a workgroup each
     float* out;                                      // rows: [parts][M][ld]; classes: [parts][V][ldo], columns 0 .. Z - 1
+    // rows: classes that stay out of the product and of the sums; launch_loss_dz adds them
+    const int32_t* labels;                           // [M] the label's, or null; sums at two scales: stays out of both, launch_loss_merge adds it
+    const uint32_t* marks;                           // those of [classes / 32, rounded up to even][Mr], a bit a class; or null (then the label's)
+    int Mr;                                          // M rounded up to 256
     float* part_ref;                                 // rows, sums not known: [parts][M] reference and sum
     float* part_sum;
     float* part_sum2;                                // sums: at the scale k
@@ -113,8 +117,8 @@ hipError_t launch_loss_fused_rows(const LossFusedArgs& a, bool known, hipStream_
 // of four; NaN behind V counts as no maximum) and the maxima of strips of 64 classes into part_ref [strips][M].
 hipError_t launch_loss_fused_sums(const LossFusedArgs& a, bool second, bool logits, hipStream_t st);
 hipError_t launch_loss_fused_classes(const LossFusedArgs& a, bool tau, hipStream_t st);
-// dz from the parts of launch_loss_fused_rows, exactly completed by the label's and the teacher's classes; with known false the
-// rows' losses and constants too.
+// dz from the parts of launch_loss_fused_rows and the label's and the teacher's classes, in float; with known false the rows' losses and
+// constants too.
 struct LossDzArgs {
     int M, Mp, V, Z, ld, parts;
     const float* part;
@@ -126,17 +130,19 @@ struct LossDzArgs {
     float s;
     const PolicyArgs* policy;                        // host pointers: one of the two
     const TeacherArgs* teacher;
+    const float* entry_logit;                        // [M][K], of entries with a probability
     const float* entry_q;
     const float* soft_const;
     const int* soft_state;
     float* logp;                                     // or null
     float* row_loss;
-    float* consts;                                   // [6][Mp]
+    float* consts;                                   // as in LossFusedArgs
     unsigned short* dz;                              // [M][Z]
 };
 hipError_t launch_loss_dz(const LossDzArgs& a, bool known, hipStream_t st);
-// The teacher's entries by tiles, from the tiles' counts.  entries: room for M K, and 256 more that are read.
+// The teacher's entries by tiles, from the tiles' counts, and the marks of the rows kernel.  entries: room for M K, and 256 more that are read.
 constexpr int LOSS_LIST_SLACK = 256;
+__host__ __device__ inline int loss_mark_words(int V) { return (V + 63) / 64 * 2; }
 struct LossListArgs {
     int M, V, K;
     const int32_t* classes;
@@ -145,6 +151,9 @@ struct LossListArgs {
     int* count;                                      // [tiles], the rows' tiles one after the other
     int* from;                                       // [tiles]
     uint2* entries;
+    const int32_t* labels;                           // or null
+    uint32_t* marks;                                 // [loss_mark_words(V)][Mr]
+    int Mr;
 };
 hipError_t launch_loss_lists(const LossListArgs& a, hipStream_t st);
 // out = sum of parts of n floats, out_b of V, in order.
@@ -166,7 +175,7 @@ struct LossMergeArgs {
     float* logp;
     float* row_loss;
     LossRow* rows;                                   // or
-    float* consts;                                   // [6][Mp], rows M .. Mp - 1 too
+    float* consts;                                   // as in LossFusedArgs, rows M .. Mp - 1 too; the sums then lack the label's class
     int Mp;
 };
 hipError_t launch_loss_merge(const LossMergeArgs& a, hipStream_t st);

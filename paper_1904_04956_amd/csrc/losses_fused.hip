@@ -2,25 +2,28 @@
 //
 //   rows      a workgroup keeps 256 rows of z in registers and walks over the classes: u = W_s z + b_s, then sum_v w_v W_v with
 //             w = exp(u - reference) and their sum (the reference moves with the running maximum), or with w = dE/du itself
-//             where the sums are known.  The label's and the teacher's classes, few a row, are added behind it, exactly.
+//             where the sums are known.  The label's and the teacher's classes, few a row, stay out and are added behind it, in float.
 //   classes   a workgroup keeps 128 classes of W_s in registers and walks over the rows: dE/du from the rows' sums, then
 //             dW_s = du^T z and db_s.  du goes into the product as the sum of two bf16 numbers (2^-16; of three where a label is, and
 //             where a teacher's classes are and frames are few), into db_s as the float that it is.
 //
 // Why so: M rows of V float logits are written, read and written again by anything that keeps them (688 MB for 5376 rows of 32000, at
 // 4.8 TB/s as long as the whole product takes); made twice, they cost a product of M V Z each.  In dz a weight is one bf16
-// number, whose rounding (2^-8) the result's own rounding to bf16 matches; the label's class, where du is large, is added in float.
+// number, whose rounding (2^-8) the result's own rounding to bf16 matches.  Of a label's or a teacher's class du is a difference of probabilities: where
+// the model is good, far smaller than they are and than what a rounded probability would be off.
 //
 // Bound by the matrix units' turns with the rest of a wavefront: two wavefronts a SIMD, each of which multiplies, takes its
 // exponentials, transposes and multiplies again; the other covers part of it.  Z = 256, V = 32000, 43008 rows (705 GFLOP a unit of
 // M V Z; the matrix units reach 1.66 PFLOP/s from registers): rows 1130 us (two units, 1.25 PFLOP/s), classes 1650 us (three, 1.28);
-// 3633 rows: 122 and 168 us.  Two distributions (5376 rows, lists of 64): sums 105, rows 175, classes 335 us.  At 168 .. 336 rows
+// 3633 rows: 122 and 168 us.  Two distributions (5376 rows, lists of 64): sums 112, rows 188 (176 without the marks), classes 335 us.  At 168 .. 336 rows
 // the parts of dz and the loads of W_s weigh as much: rows 21 .. 29 us, classes 26 .. 34.
 //
 // Both read a tile [64][Z] in LDS twice: by rows for the logits (ds_read_b128) and by columns for what is made of them
 // (ds_read_b64_tr_b16 transposes on the way).  16-byte chunk c of row r lies at chunk c ^ sw(r): the eight rows that a phase
 // of the first reads, and the four of the second, are on different banks.  The output of the first product (lane: row or
 // class, registers: the other) is the operand of the second after one exchange between the lane halves.
+#include <climits>
+
 #include "gemm_tile.hpp"
 #include "losses_terms.hpp"
 
@@ -43,6 +46,7 @@ template <int NK>
 struct Ring {
     static constexpr int CPR = 8 * NK, ROWB = 128 * NK, TILE = 64 * ROWB, STAGE = TILE + 2048, STAGES = 3;
     static constexpr int LIST = 2048;                   // bytes of a teacher's entries behind it, where there are any
+    static constexpr int MARK = 2048;                   // ... and of 256 rows' marks
     static __device__ __forceinline__ void dma16(unsigned lds, const char* base, unsigned voff) {
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(base) : "memory");
     }
@@ -106,9 +110,11 @@ constexpr int DEPTH = 4;
 
 // ---- rows -------------------------------------------------------------------------------------------------------------------
 // KNOWN: w = a exp2(u log2e - m2) + at exp2(u k - mt2) from the rows' constants, else w = exp2(u k - reference).
-template <int NK, bool KNOWN>
+// MARKS: what stays out is marked, a bit a class, and comes with the tile; else it is the label.  Either counts as ruled out.
+template <int NK, bool KNOWN, bool MARKS>
 __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
     typedef Ring<NK> R;
+    constexpr int STAGE = R::STAGE + (MARKS ? R::MARK : 0), LOADS = NK + 1 + (MARKS ? 1 : 0);
     extern __shared__ uint4 smem[];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
     const int part = (int)blockIdx.x % a.parts, row0 = (int)blockIdx.x / a.parts * 256;
@@ -126,11 +132,16 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
     if (KNOWN && m < a.Mp) {
         m2 = a.consts[m]; ca = a.consts[a.Mp + m]; mt2 = a.consts[2 * a.Mp + m]; cat = a.consts[3 * a.Mp + m];
     }
+    const int label = !MARKS && m < a.M ? a.labels[m] : -1;
     __builtin_amdgcn_s_waitcnt(0);                      // (known to the compiler: it would wait for these loads, and the ring's with them, in the loop)
     auto issue = [&](int it) __attribute__((always_inline)) {
-        const unsigned s = lds0 + (unsigned)(it % R::STAGES * R::STAGE);
+        const unsigned s = lds0 + (unsigned)(it % R::STAGES * STAGE);
         R::tile(s, a.W, (t0 + it) * 64, a.V, a.ld, wv);
         R::dma4(s + R::TILE, reinterpret_cast<const char*>(a.bias + (long long)(t0 + it) * 64), (unsigned)(fresh_lane() * 4));
+        if constexpr (MARKS) {                           // the wavefront's 32 rows, two words each
+            const int ln = fresh_lane();
+            R::dma4(s + R::STAGE + (unsigned)(wv * 256), reinterpret_cast<const char*>(a.marks + (long long)(t0 + it) * 2 * a.Mr + row0 + wv * 32), (unsigned)(((ln >> 5) * a.Mr + (ln & 31)) * 4));
+        }
     };
     f32x16_t o[2 * NK];
 #pragma unroll
@@ -143,10 +154,10 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
     if (n > 0) issue(0);
     if (n > 1) issue(1);
     for (int it = 0; it < n; ++it) {
-        if (it + 1 < n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(NK + 1) : "memory");
+        if (it + 1 < n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LOADS) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (it + 2 < n) issue(it + 2);                  // (over tile it - 1, which every wavefront is done with)
-        const char* stage = reinterpret_cast<const char*>(smem) + it % R::STAGES * R::STAGE;
+        const char* stage = reinterpret_cast<const char*>(smem) + it % R::STAGES * STAGE;
         const float* bias = reinterpret_cast<const float*>(stage + R::TILE);
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub) {
@@ -159,7 +170,18 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
             }
 #pragma unroll
             for (int q = 0; q < 4 * NK; ++q) u = mma32(at.by_row(s, q), zf[q], u);
-            ahead<4 + DEPTH, 4 * NK, 1, 1, DEPTH>();
+            unsigned out = 0;                            // (bit 8 (e / 4) + e % 4: class e of the lane stays out)
+            if constexpr (MARKS) out = *reinterpret_cast<const unsigned*>(stage + R::STAGE + wv * 256 + sub * 128 + (fresh_lane() & 31) * 4);
+            ahead<4 + (MARKS ? 1 : 0) + DEPTH, 4 * NK, 1, 1, DEPTH>();
+            if constexpr (!MARKS) {
+                const unsigned at_label = (unsigned)(label - ((t0 + it) * 64 + sub * 32));
+                out = at_label < 32u ? 1u << at_label : 0u;
+            }
+            if (__any(out != 0)) {
+                out >>= 4 * half;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) u[e] = out & 1u << (8 * (e >> 2) + (e & 3)) ? -INFINITY : u[e];
+            }
             if constexpr (!KNOWN) {
                 float mx = u[0];
 #pragma unroll
@@ -221,8 +243,8 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
 }
 
 // ---- rows, the sums alone -----------------------------------------------------------------------------------------------------
-// Reference and sum of exponentials of every row and part (SUMS2: at two scales, from one reference), or the logits themselves with the
-// maxima of strips of 64 classes (LOGITS).  5376 rows of 32000, Z = 256 (88 GFLOP): 90 us (980 TFLOP/s), SUMS2 105, LOGITS 230, whose
+// Reference and sum of exponentials of every row and part (SUMS2: at two scales, from one reference, without the label's class), or the logits themselves with the
+// maxima of strips of 64 classes (LOGITS).  5376 rows of 32000, Z = 256 (88 GFLOP): 90 us (980 TFLOP/s), SUMS2 112 (106 with the label in its sums), LOGITS 230, whose
 // 688 MB are stored at 3 TB/s (past L2 or with loads that do not wait for them no faster).  Two workgroups a CU, four wavefronts a SIMD, so that some multiply while others take exponentials.
 // Rows as in the rows kernel: of the 128 x 128 tiles that larger z take, both operands come from L2 for half the products.
 enum { SUMS, SUMS2, LOGITS };
@@ -242,6 +264,7 @@ __global__ __launch_bounds__(512, 4) void loss_sums_kernel(LossFusedArgs a) {
         const int c = 2 * q + half;
         zf[q] = c * 8 < a.ld ? *reinterpret_cast<const uint4*>(a.z + (long long)min(m, a.M - 1) * a.ld + c * 8) : make_uint4(0, 0, 0, 0);
     }
+    const int label = WHAT == SUMS2 && m < a.M ? a.labels[m] : -1;
     __builtin_amdgcn_s_waitcnt(0);
     auto issue = [&](int it) __attribute__((always_inline)) {
         const unsigned s = lds0 + (unsigned)((it & 1) * R::STAGE);
@@ -270,6 +293,13 @@ __global__ __launch_bounds__(512, 4) void loss_sums_kernel(LossFusedArgs a) {
             for (int q = 0; q < 4 * NK; ++q) u = mma32(at.by_row(s, q), zf[q], u);
             ahead<4 + DEPTH, 4 * NK, 1, 1, DEPTH>();
             __builtin_amdgcn_sched_barrier(0);
+            if constexpr (WHAT == SUMS2) {
+                const int at_label = label - ((t0 + it) * 64 + sub * 32);
+                if (__any((unsigned)at_label < 32u)) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) u[e] = at_label == 8 * (e >> 2) + 4 * half + (e & 3) ? -INFINITY : u[e];
+                }
+            }
             float mx = u[0];
 #pragma unroll
             for (int e = 1; e < 16; ++e) mx = fmaxf(mx, u[e]);
@@ -436,19 +466,19 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
                     for (int i = 0; i < 4; ++i) d[4 * h + i] = fmaf(cts[i], __builtin_amdgcn_exp2f(fmaf(u[8 * t + 4 * h + i] + b, k, -mts[i])), d[4 * h + i]);
                 }
             }
+            if (any_hot) {                              // (a label's du is one of the constants)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int r = 8 * (2 * t + (e >> 2)) + 4 * half + (e & 3);
+                    if (labels[r] == class0 + (fresh_lane() & 31)) d[e] = -consts[256 + r];
+                }
+            }
             if (ENTRIES && any_spot) {
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float4 x = *reinterpret_cast<const float4*>(spots + (fresh_lane() & 31) * SPOT + 8 * (2 * t + h) + 4 * half);
                     d[4 * h] -= x.x; d[4 * h + 1] -= x.y; d[4 * h + 2] -= x.z; d[4 * h + 3] -= x.w;
-                }
-            }
-            if (any_hot) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int r = 8 * (2 * t + (e >> 2)) + 4 * half + (e & 3);
-                    if (labels[r] == class0 + (fresh_lane() & 31)) d[e] -= consts[256 + r];
                 }
             }
             // (with lists there is no register left for db_off: 335 us became 374)
@@ -539,9 +569,32 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
 // Counts the rows' entries with a probability by tiles, gives every tile a place among the rows' own, and puts them there (in an order of no
 // matter: a row's classes are different ones).  All counters in LDS: with a list of all rows together, 168 rows of 16 took three launches of
 // 4 us for it and 5376 of 64 took 20 us.
-constexpr int LISTS_THREADS = 1024;
+// Behind those, a workgroup 32 rows and MARK_WORDS words of the marks: the entries with a probability and the label.
+constexpr int LISTS_THREADS = 1024, MARK_WORDS = 512;
 __global__ __launch_bounds__(LISTS_THREADS) void loss_lists_kernel(LossListArgs a, int ntv) {
     extern __shared__ uint4 smem[];
+    const int lists = (a.M + 63) / 64;
+    if ((int)blockIdx.x >= lists) {
+        uint32_t* word = reinterpret_cast<uint32_t*>(smem);   // [words][32]
+        const int all = loss_mark_words(a.V), blocks = (all + MARK_WORDS - 1) / MARK_WORDS;
+        const int row0 = ((int)blockIdx.x - lists) / blocks * 32, word0 = ((int)blockIdx.x - lists) % blocks * MARK_WORDS, words = min(MARK_WORDS, all - word0);
+        const int rows = min(32, a.M - row0);            // (none or less: the last rows of the last 256)
+        for (int i = threadIdx.x; i < words * 32; i += LISTS_THREADS) word[i] = 0;
+        __syncthreads();
+        auto mark = [&](int row, int c) {
+            const int w = (c >> 5) - word0;
+            if (w >= 0 && w < words) atomicOr(&word[w * 32 + row], 1u << (c & 31));
+        };
+        for (int k = threadIdx.x; k < rows * a.K; k += LISTS_THREADS)
+            if (a.q[row0 * a.K + k] > 0.0f) mark(k / a.K, a.classes[row0 * a.K + k]);
+        if (a.labels && (int)threadIdx.x < rows) {
+            const int lab = a.labels[row0 + threadIdx.x];
+            if ((unsigned)lab < (unsigned)a.V) mark(threadIdx.x, lab);
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < words * 32; i += LISTS_THREADS) a.marks[(long long)(word0 + (i >> 5)) * a.Mr + row0 + (i & 31)] = word[i];
+        return;
+    }
     int* at = reinterpret_cast<int*>(smem);             // [ntv], then a number a wavefront
     int* waves = at + ntv;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row0 = (int)blockIdx.x * 64;
@@ -592,7 +645,8 @@ __global__ __launch_bounds__(256) void loss_classes_sum_kernel(const float* __re
 
 // ---- behind the rows: a workgroup a row, four columns a lane, its wavefronts share the parts and the teacher's classes ---------
 // KNOWN: the rows' constants and losses are there and the parts are sums of du W; else they are made here from the parts' references
-// and sums, which are brought to the largest reference.  All loads of a step are independent: one by one, 128 parts and 64 classes
+// and sums, which are brought to the largest reference, and the logits of the classes that the parts lack.  Of those classes, the label's
+// and the teacher's, dE/du is made here in float: 1 - p of a label from the sum of all others, p' - q as a difference.  All loads of a step are independent: one by one, 128 parts and 64 classes
 // took 49 us for 168 rows.
 // SHARE: wavefronts a row, four or, where rows are many, one (43008 rows: 69 us with four, 29 with one).
 template <bool KNOWN, bool POLICY, int SHARE>
@@ -604,14 +658,28 @@ __global__ __launch_bounds__(256) void loss_dz_kernel(LossDzArgs a, PolicyArgs p
         if (wave == 0 && lane < 6) a.consts[lane * (long long)a.Mp + m] = lane == 0 || lane == 2 ? INFINITY : lane == 5 ? __builtin_bit_cast(float, -1) : 0.0f;
         return;
     }
-    float m2 = 0.0f, c1 = 1.0f, hot = 0.0f;
+    float m2 = 0.0f, c1 = 1.0f, mt2 = 0.0f, ct = 0.0f, at_label = 0.0f;   // at_label: du there, but for the teacher's q
     int lab = a.labels ? a.labels[m] : -1;
+    const float k = POLICY || KNOWN ? LOG2E : LOG2E * teacher.inv_tau, kt = LOG2E * teacher.inv_tau;
     bool some = false;                                   // entries of the teacher's that count
+    // entry i's class, logit and q (nothing: class -1, q 0)
+    struct Entry { int c; float u, q; };
+    auto entry = [&](int i) {
+        Entry e{-1, 0.0f, i < teacher.K ? a.entry_q[m * teacher.K + i] : 0.0f};
+        if (e.q > 0.0f) { e.c = teacher.classes[m * teacher.K + i]; e.u = a.entry_logit[m * teacher.K + i]; }
+        else e.q = 0.0f;
+        return e;
+    };
     if (KNOWN) {
-        hot = a.consts[4 * (long long)a.Mp + m];
+        m2 = a.consts[m]; c1 = a.consts[a.Mp + m]; mt2 = a.consts[2 * (long long)a.Mp + m]; ct = a.consts[3 * (long long)a.Mp + m];
+        at_label = -a.consts[4 * (long long)a.Mp + m];
         some = a.soft_state[m] & 1;
     } else {
-        float ref = -INFINITY;
+        const bool lab_ok = (unsigned)lab < (unsigned)a.V;
+        const float lu = lab_ok ? a.label_logit[m] : 0.0f;
+        const int listed = POLICY ? 0 : teacher.K;
+        float ref = lab_ok ? lu * k : -INFINITY;
+        for (int i = lane; i < listed; i += 64) { const Entry e = entry(i); if (e.c >= 0) ref = fmaxf(ref, e.u * k); }
         for (int p = lane; p < a.parts; p += 64) ref = fmaxf(ref, a.part_ref[(long long)p * a.M + m]);
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor(ref, o, 64));
@@ -619,33 +687,40 @@ __global__ __launch_bounds__(256) void loss_dz_kernel(LossDzArgs a, PolicyArgs p
         for (int p = lane; p < a.parts; p += 64) sum += a.part_sum[(long long)p * a.M + m] * __builtin_amdgcn_exp2f(a.part_ref[(long long)p * a.M + m] - ref);
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+        float taught = 0.0f;
+        for (int i = lane; i < listed; i += 64) { const Entry e = entry(i); if (e.c >= 0 && e.c != lab) taught += __builtin_amdgcn_exp2f(fmaf(e.u, k, -ref)); }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) taught += __shfl_xor(taught, o, 64);
+        sum += taught;
+        const float others = sum, w_label = lab_ok ? __builtin_amdgcn_exp2f(fmaf(lu, k, -ref)) : 0.0f;
+        sum += w_label;
         m2 = ref;
-        const bool lab_ok = (unsigned)lab < (unsigned)a.V;
         const float nan = __builtin_nanf(""), log_sum = logf(sum);
-        const float lp = lab_ok ? fmaf(a.label_logit[m], LOG2E, -ref) * LN2 - log_sum : lab == -1 ? 0.0f : nan;
+        const float lp = lab_ok ? fmaf(lu, LOG2E, -ref) * LN2 - log_sum : lab == -1 ? 0.0f : nan;
         float loss = 0.0f;
         c1 = 0.0f;
         if (POLICY) {
             if (lab_ok) {
                 const PolicyTerms t = policy_terms(policy, m, lp);
-                loss = a.s * t.loss; c1 = -a.s * t.g / sum; hot = -a.s * t.g;
+                loss = a.s * t.loss; c1 = -a.s * t.g / sum; at_label = a.s * t.g * (others / sum);
             } else if (lab != -1) loss = nan;
             if (a.logp && wave == 0 && lane == 0) a.logp[m] = lp;
         } else {
             const int state = a.soft_state[m];
             some = state & 1;
-            if (lab_ok) { loss = a.s * teacher.hard * -lp; c1 = a.s * teacher.hard / sum; hot = a.s * teacher.hard; }
+            if (lab_ok) { loss = a.s * teacher.hard * -lp; c1 = a.s * teacher.hard / sum; at_label = -a.s * teacher.hard * (others / sum); }
             else if (lab != -1) loss = nan;
             if (some) {
                 loss += a.s * teacher.soft * teacher.tau * teacher.tau * (a.soft_const[m] + (ref * LN2 + log_sum));
                 c1 += a.s * teacher.soft * teacher.tau / sum;
+                at_label += a.s * teacher.soft * teacher.tau / sum * w_label;
             }
             if (state & 2) loss = nan;
         }
         const bool counts = lab_ok || some;
         if (!lab_ok) lab = -1;
         if (wave == 0 && lane < 6)
-            a.consts[lane * (long long)a.Mp + m] = lane == 0 ? (counts ? m2 : INFINITY) : lane == 1 ? c1 : lane == 2 ? INFINITY : lane == 3 ? 0.0f : lane == 4 ? hot : __builtin_bit_cast(float, lab);
+            a.consts[lane * (long long)a.Mp + m] = lane == 0 ? (counts ? m2 : INFINITY) : lane == 1 ? c1 : lane == 2 ? INFINITY : lane == 3 ? 0.0f : lane == 4 ? -at_label : __builtin_bit_cast(float, lab);
         if (wave == 0 && lane == 0) a.row_loss[m] = loss;
     }
     const bool lab_ok = (unsigned)lab < (unsigned)a.V, counts = KNOWN || lab_ok || some;
@@ -666,21 +741,24 @@ __global__ __launch_bounds__(256) void loss_dz_kernel(LossDzArgs a, PolicyArgs p
         }
         for (; p < a.parts; p += SHARE) add_part(p);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] *= c1;
+        for (int i = 0; i < 4; ++i) x[i] *= KNOWN ? 1.0f : c1;
         auto add = [&](int c, float w) {                 // w W_c
             const uint2 b = *reinterpret_cast<const uint2*>(a.W + (long long)c * a.ld + z0);
             x[0] = fmaf(w, bf2f((bf16_t)(b.x & 0xFFFFu)), x[0]); x[1] = fmaf(w, bf2f((bf16_t)(b.x >> 16)), x[1]);
             x[2] = fmaf(w, bf2f((bf16_t)(b.y & 0xFFFFu)), x[2]); x[3] = fmaf(w, bf2f((bf16_t)(b.y >> 16)), x[3]);
         };
-        if (wave == 0 && hot != 0.0f && lab_ok) add(lab, -hot);
+        if (wave == 0 && lab_ok) add(lab, at_label);
         if (!POLICY && some) {
             const float weight = a.s * teacher.soft * teacher.tau;
             for (int k0 = 0; k0 < teacher.K; k0 += 64) {
                 // 64 entries a lane each; the wavefront's sixteen, four at a time (one that is none: nothing times the first class)
-                const bool have = k0 + lane < teacher.K;
-                const float q = have ? a.entry_q[m * teacher.K + k0 + lane] : 0.0f;
-                const int c = q > 0.0f ? teacher.classes[m * teacher.K + k0 + lane] : 0;
-                const float w = -weight * q;
+                const Entry e = entry(k0 + lane);
+                float w = -weight * e.q;
+                if (e.c >= 0 && e.c != lab) {            // (the label's probability is in at_label)
+                    w = fmaf(c1, __builtin_amdgcn_exp2f(fmaf(e.u, k, -m2)), w);
+                    if (KNOWN) w = fmaf(ct, __builtin_amdgcn_exp2f(fmaf(e.u, kt, -mt2)), w);
+                }
+                const int c = max(e.c, 0);
                 for (int j = wave; j < 64 && k0 + j < teacher.K; j += 4 * SHARE) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
@@ -701,13 +779,13 @@ __global__ __launch_bounds__(256) void loss_dz_kernel(LossDzArgs a, PolicyArgs p
     for (int i = 0; i < 4; ++i) if (z0 + i < a.Z) a.dz[m * a.Z + z0 + i] = f2bf(x[i]);
 }
 
-template <int NK, bool KNOWN>
+template <int NK, bool KNOWN, bool MARKS>
 hipError_t rows_nk(const LossFusedArgs& a, hipStream_t st) {
-    constexpr size_t lds = (size_t)Ring<NK>::STAGES * Ring<NK>::STAGE;
+    constexpr size_t lds = (size_t)Ring<NK>::STAGES * (Ring<NK>::STAGE + (MARKS ? Ring<NK>::MARK : 0));
     static thread_local bool attr_set = false;
-    const hipError_t e = allow_lds(&loss_rows_kernel<NK, KNOWN>, lds, &attr_set);
+    const hipError_t e = allow_lds(&loss_rows_kernel<NK, KNOWN, MARKS>, lds, &attr_set);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((loss_rows_kernel<NK, KNOWN>), dim3((unsigned)((a.M + 255) / 256 * a.parts)), dim3(512), lds, st, a);
+    hipLaunchKernelGGL((loss_rows_kernel<NK, KNOWN, MARKS>), dim3((unsigned)((a.M + 255) / 256 * a.parts)), dim3(512), lds, st, a);
     return hipGetLastError();
 }
 template <int NK, int WHAT>
@@ -733,7 +811,7 @@ hipError_t classes_nk(const LossFusedArgs& a, hipStream_t st) {
 
 hipError_t launch_loss_fused_rows(const LossFusedArgs& a, bool known, hipStream_t st) {
     const int nk = (a.ld + 63) / 64;
-#define BLSTM_ROWS(NK) return known ? rows_nk<NK, true>(a, st) : rows_nk<NK, false>(a, st)
+#define BLSTM_ROWS(NK) return known ? rows_nk<NK, true, true>(a, st) : a.marks ? rows_nk<NK, false, true>(a, st) : rows_nk<NK, false, false>(a, st)
     if (nk == 1) BLSTM_ROWS(1);
     if (nk == 2) BLSTM_ROWS(2);
     if (nk == 3) BLSTM_ROWS(3);
@@ -775,9 +853,12 @@ hipError_t launch_loss_lists(const LossListArgs& a, hipStream_t st) {
     static thread_local bool attr_set = false;
     const hipError_t e = allow_lds(&loss_lists_kernel, most, &attr_set);
     if (e != hipSuccess) return e;
-    const size_t lds = (ntv + LISTS_THREADS / 64) * sizeof(int);
+    const int words = loss_mark_words(a.V);
+    const size_t lists = (ntv + LISTS_THREADS / 64) * sizeof(int), marks = (size_t)(words < MARK_WORDS ? words : MARK_WORDS) * 32 * sizeof(uint32_t), lds = lists > marks ? lists : marks;
     if (lds > most) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(loss_lists_kernel, dim3((unsigned)((a.M + 63) / 64)), dim3(LISTS_THREADS), lds, st, a, ntv);
+    const long long grid = (a.M + 63) / 64 + (long long)(a.Mr / 32) * ((words + MARK_WORDS - 1) / MARK_WORDS);
+    if (grid > INT_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(loss_lists_kernel, dim3((unsigned)grid), dim3(LISTS_THREADS), lds, st, a, ntv);
     return hipGetLastError();
 }
 hipError_t launch_loss_classes_sum(const float* p, const float* pb, int parts, long long n, int V, float* out, float* out_b, hipStream_t st) {

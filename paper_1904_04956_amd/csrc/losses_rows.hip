@@ -220,6 +220,11 @@ __global__ __launch_bounds__(256) void loss_prep_kernel(LossPrepArgs a) {
     }
 }
 
+// The reference of a row whose sums lack the label's class: not far below that class's logit.
+__device__ __forceinline__ float merge_reference(const LossMergeArgs& a, long long m, float mx) {
+    return a.consts && a.labels && (unsigned)a.labels[m] < (unsigned)a.V ? fmaxf(mx, a.label_logit[m]) : mx;
+}
+
 // What a row's largest logit (or another reference) and its sums give, by one lane.  `in`: the row is none of those that fill the last tile.
 template <bool TAU, bool POLICY, bool TEACHER>
 __device__ __forceinline__ void merge_end(const LossMergeArgs& a, const PolicyArgs& policy, const TeacherArgs& teacher, long long m, bool in, float mx, float sum, float tau) {
@@ -239,6 +244,12 @@ __device__ __forceinline__ void merge_end(const LossMergeArgs& a, const PolicyAr
     const float nan = __builtin_nanf("");
     // u_y - max in the scale of the sums, whose maximum is rounded once: the same number in all of them
     const float up = far ? a.label_logit[m] - mx : fmaf(a.label_logit[m], LOG2E, -m2) * LN2;
+    const float others = sum;                            // (a.consts: of all but the label, so that 1 - p is a sum and no difference)
+    float label_tau = 0.0f;
+    if (a.consts && lab_ok) {
+        sum += __builtin_amdgcn_exp2f(fmaf(a.label_logit[m], LOG2E, -m2));
+        if (TAU) { label_tau = __builtin_amdgcn_exp2f(fmaf(a.label_logit[m], LOG2E * teacher.inv_tau, -mt2)); tau += label_tau; }
+    }
     const float lp = lab_ok ? up - logf(sum) : lab == -1 ? 0.0f : nan;
     if (a.logp) a.logp[m] = lp;
     if (!a.rows && !a.consts) return;
@@ -268,6 +279,7 @@ __device__ __forceinline__ void merge_end(const LossMergeArgs& a, const PolicyAr
         if (state & LIST_BAD) loss = nan;
     }
     if (r.a != 0.0f || r.at != 0.0f) r.max = mx;         // (a NaN is not 0)
+    if (a.consts && lab_ok) r.hot = r.hot * (others / sum) - r.at * label_tau;
     a.row_loss[m] = loss;
     if (a.consts) put(r); else a.rows[m] = r;
 }
@@ -288,6 +300,7 @@ __global__ __launch_bounds__(512) void loss_merge_kernel(LossMergeArgs a, Policy
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < 8; ++w) mx = fmaxf(mx, sh_max[w][lane]);
+    if (in) mx = merge_reference(a, m, mx);
     const float m2 = mx * LOG2E, lt = LOG2E * teacher.inv_tau, mt2 = TAU ? mx * lt : 0.0f;
     const bool far = fabsf(mx) > LOSS_FAR;
     float sum = 0.0f, tau = 0.0f;
@@ -319,7 +332,7 @@ __global__ __launch_bounds__(256) void loss_merge_row_kernel(LossMergeArgs a, Te
     float mx = -INFINITY, sum = 0.0f, tau = 0.0f;
     if (in) {
         for (int i = lane; i < a.strips; i += 64) mx = fmaxf(mx, a.part_max[(long long)i * a.M + m]);
-        mx = wave_max(mx);
+        mx = merge_reference(a, m, wave_max(mx));
         const float lt = LOG2E * teacher.inv_tau;
         for (int i = lane; i < a.strips; i += 64) {
             const float d = a.part_max[(long long)i * a.M + m] - mx;
