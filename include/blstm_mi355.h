@@ -119,10 +119,12 @@ int softmax_xent_fwd_bwd_noalloc(blstm_ctx* ctx, const void* theta, const void* 
      softmax_xent_fwd_bwd writes, in its place in front of blstm_backward (BLSTM_OPT_DEFER_SOFTMAX_WGRAD does not concern
      them; what an earlier softmax_xent_fwd_bwd left to blstm_backward is dropped).  Mode 1: logits and all sums in float,
      dE/du (where a label or a teacher's class is, the difference, not its two sides) enters the product for dz as one bf16
-     number and those for W_s and b_s as the sum of two (2^-16) at least.  The same inputs give the same bits.  A class is ruled out by a bias of -inf or of the type's lowest value; in mode 1 logits
-     below -1e5 are ruled out too, and the results of a frame all of whose logits are have no meaning. */
+     number and those for W_s and b_s as the sum of two (2^-16) at least.  The same inputs give the same bits.  A class is ruled
+     out by a bias of -inf or of the type's lowest value; in mode 1 logits below -1e5 are ruled out too, and the results of a
+     frame all of whose logits are have no meaning. */
 #define BLSTM_NO_LABEL (-1)
 #define BLSTM_MAX_TOP 256                      /* the most entries of a list of largest logits */
+#define BLSTM_MIN_TEMPERATURE 1e-4f            /* the lowest temperature of a distillation */
 /* call = one of these in softmax_scratch_bytes */
 #define SOFTMAX_LOGPROB 0
 #define SOFTMAX_TOPK    1
@@ -146,7 +148,7 @@ int softmax_topk(blstm_ctx* ctx, const void* theta, const void* z, int K, float*
    probabilities.  With q = softmax over a frame's used entries of value / temperature, p' = softmax(u / temperature):
      E = s sum over frames of  hard_weight (-log p[label])  +  soft_weight temperature^2 sum_k q_k (log q_k - log p'[class_k])
    A frame without used entries has the first term only, one without label the second.  hard_weight 0: labels are not
-   read and may be NULL.  temperature > 0, hard_weight >= 0, soft_weight > 0, 1 <= K <= min(V, BLSTM_MAX_TOP),
+   read and may be NULL.  temperature >= BLSTM_MIN_TEMPERATURE, hard_weight >= 0, soft_weight > 0, 1 <= K <= min(V, BLSTM_MAX_TOP),
    T B K below 2^31 - 2^14 and T B V below 2^44. */
 int softmax_distill_fwd_bwd(blstm_ctx* ctx, const void* theta, const void* z, const int32_t* labels_or_null,
                             const float* teacher_values, const int32_t* teacher_classes, int K, float temperature,

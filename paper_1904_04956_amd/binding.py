@@ -18,6 +18,7 @@ BLSTM_WX, BLSTM_UH, BLSTM_B, BLSTM_WP, BLSTM_BP, BLSTM_WS, BLSTM_BS = range(7)
 BLSTM_MAX_REPLICAS = 64
 BLSTM_NO_LABEL = -1
 BLSTM_MAX_TOP = 256
+BLSTM_MIN_TEMPERATURE = 1e-4
 SOFTMAX_LOGPROB, SOFTMAX_TOPK, SOFTMAX_DISTILL, SOFTMAX_POLICY = range(4)
 
 EXPORTS = [

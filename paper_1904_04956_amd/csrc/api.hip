@@ -1233,8 +1233,9 @@ int softmax_distill_fwd_bwd(blstm_ctx* ctx, const void* theta, const void* z, co
                             const int32_t* teacher_classes, int K, float temperature, float hard_weight, float soft_weight,
                             float* loss_dev, void* dz, float* grad, void* scratch, size_t scratch_bytes, void* stream) {
     if (!ctx || !theta || !z || !teacher_values || !teacher_classes || !loss_dev || !dz || !grad) return fail(BLSTM_ERR_NULL, "softmax_distill_fwd_bwd: null argument");
-    if (!(temperature > 0.0f) || !(1.0f / temperature > 0.0f) || temperature * temperature > 3e38f || !(hard_weight >= 0.0f && hard_weight <= 3e38f) || !(soft_weight > 0.0f && soft_weight <= 3e38f))
-        return fail(BLSTM_ERR_DIM, "softmax_distill_fwd_bwd: temperature and soft_weight must be positive, hard_weight not negative, all finite");
+    // (exponents are u log2e / temperature less a rounded reference: 2^-24 of a logit of LOSS_FAR over this is below the 2^7 that an exponential spans)
+    if (!(temperature >= BLSTM_MIN_TEMPERATURE) || !(1.0f / temperature > 0.0f) || temperature * temperature > 3e38f || !(hard_weight >= 0.0f && hard_weight <= 3e38f) || !(soft_weight > 0.0f && soft_weight <= 3e38f))
+        return fail(BLSTM_ERR_DIM, "softmax_distill_fwd_bwd: temperature must be at least %g, soft_weight positive, hard_weight not negative, all finite", BLSTM_MIN_TEMPERATURE);
     if (hard_weight != 0.0f && !labels) return fail(BLSTM_ERR_NULL, "softmax_distill_fwd_bwd: hard_weight needs labels");
     LossScratch l;
     int rc = loss_check("softmax_distill_fwd_bwd", ctx, SOFTMAX_DISTILL, K, theta, z, scratch, scratch_bytes, &l);

@@ -198,3 +198,11 @@ def test_lists_beyond_32_bits_are_refused():
                 assert bl.softmax_scratch_bytes(c, bl.SOFTMAX_TOPK, K) > 0
         finally:
             bl.blstm_destroy(c)
+
+
+@pytest.mark.parametrize("temperature", [1e-39, 1e-30, 0.9 * bl.BLSTM_MIN_TEMPERATURE])
+def test_temperatures_that_the_exponents_cannot_hold_are_refused(ctx, temperature):
+    # logits of up to 1e5 over the temperature: times 2^-24 still below the exponents' range of 2^7
+    with pytest.raises(bl.BlstmError) as e:
+        call(ctx, "distill", temperature=temperature)
+    assert e.value.code == -2 and "softmax_distill" in str(e.value)
