@@ -130,7 +130,7 @@ __global__ __launch_bounds__(256, 2) void loss_tile_kernel(LossTileArgs a, int n
 #pragma unroll
                 for (int e = 0; e < 16; ++e) mx = fmaxf(mx, acc[j][i][e]);
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            const float m2 = mx * LOG2E, mt2 = mx * lt;
+            const float m2 = rounded_product(mx, LOG2E), mt2 = rounded_product(mx, lt);
             float sum = 0.0f, tau = 0.0f;
             auto add = [&](auto power) {
 #pragma unroll

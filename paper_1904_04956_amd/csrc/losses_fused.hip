@@ -149,8 +149,8 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[zb][e] = 0.0f;
     // (below every logit that is not ruled out)
-    float ref = -LOSS_FAR * LOG2E, sum = 0.0f;
     const float k = a.k;
+    float ref = -LOSS_FAR * k, sum = 0.0f;
     if (n > 0) issue(0);
     if (n > 1) issue(1);
     for (int it = 0; it < n; ++it) {
@@ -315,11 +315,11 @@ __global__ __launch_bounds__(512, 4) void loss_sums_kernel(LossFusedArgs a) {
             } else {
                 if (__any(mx > top + slack)) {
                     const float now = fmaxf(top, fmaxf(mx, __shfl_xor(mx, 32, 64)));
-                    sum *= __builtin_amdgcn_exp2f((top - now) * k1);
-                    if (WHAT == SUMS2) sum2 *= __builtin_amdgcn_exp2f((top - now) * k);
+                    sum *= __builtin_amdgcn_exp2f(rounded_product(top, k1) - rounded_product(now, k1));
+                    if (WHAT == SUMS2) sum2 *= __builtin_amdgcn_exp2f(rounded_product(top, k) - rounded_product(now, k));
                     top = now;
                 }
-                const float m1 = top * k1, m2 = top * k;
+                const float m1 = rounded_product(top, k1), m2 = rounded_product(top, k);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     sum += __builtin_amdgcn_exp2f(fmaf(u[e], k1, -m1));

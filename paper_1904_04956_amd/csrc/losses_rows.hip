@@ -228,7 +228,7 @@ __device__ __forceinline__ float merge_reference(const LossMergeArgs& a, long lo
 // What a row's largest logit (or another reference) and its sums give, by one lane.  `in`: the row is none of those that fill the last tile.
 template <bool TAU, bool POLICY, bool TEACHER>
 __device__ __forceinline__ void merge_end(const LossMergeArgs& a, const PolicyArgs& policy, const TeacherArgs& teacher, long long m, bool in, float mx, float sum, float tau) {
-    const float m2 = mx * LOG2E, mt2 = TAU ? mx * (LOG2E * teacher.inv_tau) : 0.0f;
+    const float m2 = rounded_product(mx, LOG2E), mt2 = TAU ? rounded_product(mx, LOG2E * teacher.inv_tau) : 0.0f;
     const bool far = fabsf(mx) > LOSS_FAR;
     auto put = [&](const LossRow& r) {
         const float x[6] = {r.m2, r.a, r.mt2, r.at, r.hot, __builtin_bit_cast(float, r.label)};
@@ -301,7 +301,7 @@ __global__ __launch_bounds__(512) void loss_merge_kernel(LossMergeArgs a, Policy
 #pragma unroll
     for (int w = 0; w < 8; ++w) mx = fmaxf(mx, sh_max[w][lane]);
     if (in) mx = merge_reference(a, m, mx);
-    const float m2 = mx * LOG2E, lt = LOG2E * teacher.inv_tau, mt2 = TAU ? mx * lt : 0.0f;
+    const float m2 = rounded_product(mx, LOG2E), lt = LOG2E * teacher.inv_tau, mt2 = TAU ? rounded_product(mx, lt) : 0.0f;
     const bool far = fabsf(mx) > LOSS_FAR;
     float sum = 0.0f, tau = 0.0f;
     if (in) {
@@ -309,8 +309,8 @@ __global__ __launch_bounds__(512) void loss_merge_kernel(LossMergeArgs a, Policy
         for (int i = wave; i < a.strips; i += 8) {
             const float pm = a.part_max[(long long)i * a.M + m];
             const bool away = far || fabsf(pm) > LOSS_FAR;
-            sum += a.part_sum[(long long)i * a.M + m] * __builtin_amdgcn_exp2f(away ? (pm - mx) * LOG2E : pm * LOG2E - m2);
-            if (TAU) tau += a.part_sum_tau[(long long)i * a.M + m] * __builtin_amdgcn_exp2f(away ? (pm - mx) * lt : pm * lt - mt2);
+            sum += a.part_sum[(long long)i * a.M + m] * __builtin_amdgcn_exp2f(away ? (pm - mx) * LOG2E : rounded_product(pm, LOG2E) - m2);
+            if (TAU) tau += a.part_sum_tau[(long long)i * a.M + m] * __builtin_amdgcn_exp2f(away ? (pm - mx) * lt : rounded_product(pm, lt) - mt2);
         }
     }
     sh_sum[wave][lane] = sum;
@@ -333,11 +333,12 @@ __global__ __launch_bounds__(256) void loss_merge_row_kernel(LossMergeArgs a, Te
     if (in) {
         for (int i = lane; i < a.strips; i += 64) mx = fmaxf(mx, a.part_max[(long long)i * a.M + m]);
         mx = merge_reference(a, m, wave_max(mx));
-        const float lt = LOG2E * teacher.inv_tau;
+        const float lt = LOG2E * teacher.inv_tau, m2 = rounded_product(mx, LOG2E), mt2 = rounded_product(mx, lt);
         for (int i = lane; i < a.strips; i += 64) {
-            const float d = a.part_max[(long long)i * a.M + m] - mx;
-            sum += a.part_sum[(long long)i * a.M + m] * __builtin_amdgcn_exp2f(d * LOG2E);
-            if (TAU) tau += a.part_sum_tau[(long long)i * a.M + m] * __builtin_amdgcn_exp2f(d * lt);
+            const float pm = a.part_max[(long long)i * a.M + m];
+            const bool away = fabsf(mx) > LOSS_FAR || fabsf(pm) > LOSS_FAR;
+            sum += a.part_sum[(long long)i * a.M + m] * __builtin_amdgcn_exp2f(away ? (pm - mx) * LOG2E : rounded_product(pm, LOG2E) - m2);
+            if (TAU) tau += a.part_sum_tau[(long long)i * a.M + m] * __builtin_amdgcn_exp2f(away ? (pm - mx) * lt : rounded_product(pm, lt) - mt2);
         }
         sum = wave_sum(sum);
         if (TAU) tau = wave_sum(tau);

@@ -15,6 +15,14 @@ __device__ __forceinline__ unsigned pack2(float lo, float hi) {
     return __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2_t{lo, hi}), bf16x2_t));
 }
 
+// a b, rounded, and no part of a multiply-add.  The exponent of a sum's term is fmaf(u, k, -r) with r the rounded product of the reference and k: the
+// same r in every term, so that its rounding (2^-24 of u over the temperature) cancels, as long as sums are brought to another r by the
+// difference of the two.
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
+}
+
 struct PolicyTerms { float loss, g; };
 __device__ __forceinline__ PolicyTerms policy_terms(const PolicyArgs& p, long long m, float lp) {
     const float A = p.advantage[m];

@@ -125,3 +125,38 @@ def test_a_student_close_to_its_teacher(shape, tau, hard, mode):
         check(layer, got, want[1:], du, parts, live)
     finally:
         layer.close()
+
+
+@pytest.mark.parametrize("mode", [1, 0])
+@pytest.mark.parametrize("Z", [64, 264])
+@pytest.mark.parametrize("tau,hard", [(0.01, 0.0), (2.0 ** -13, 0.0), (0.01, 0.5)])
+def test_small_temperatures_and_logits_far_below_zero(tau, hard, Z, mode):
+    # 2000 below zero and, over a temperature of 0.01 or 2^-13, 2e5 or 2e7: the temperature does not move where a class counts as ruled out
+    layer = exact_layer(2, 35, 300, Z, mode, 43, loss_scale=0.125)
+    try:
+        K, soft, s = 16, 0.75, float(layer.s)
+        low = 2048.0
+        layer.theta[layer.at_b:layer.at_b + layer.V] = -low
+        z = layer.z.double().numpy()
+        u = z @ layer.W.T + layer.b
+        lab = best_labels(layer, u)
+        given = lab if hard else np.full_like(lab, sl.NO_LABEL)
+        classes = np.argsort(-u, axis=1, kind="stable")[:, :K].astype(np.int32)
+        # (the teacher's are not far below zero, and a few of them count)
+        values = (tau * layer.rng.normal(size=(layer.M, K))).astype(np.float32)
+        classes[layer.rng.random(layer.M) < 0.1] = sl.NO_LABEL
+        q, some = sl.teacher_distribution(values, classes, layer.V, tau)
+        live = (given != sl.NO_LABEL) | some
+        want = sl.distill(layer.W, layer.b, z, given, values, classes, s, tau, hard, soft)
+        got = layer.distill(lab if hard else None, values, classes, tau, hard, soft)
+        labelled = given != sl.NO_LABEL
+        hot = np.zeros_like(u)
+        hot[np.flatnonzero(labelled), given[labelled]] = 1.0
+        ph, pt = np.exp(sl._log_softmax(u)) * labelled[:, None], np.exp(sl._log_softmax(u / tau)) * some[:, None]
+        du = s * (hard * (ph - hot) + soft * tau * (pt - q))
+        x = u.max(axis=1, keepdims=True) - u
+        parts = s * ((layer.V + 64 + 2 * x) * hard * (ph + hot) + (layer.V + 64 + 2 * x / tau) * soft * tau * pt + (K + 64) * soft * tau * q)
+        check(layer, got, want[1:], du, parts, live)
+        assert np.isfinite(got["loss"])
+    finally:
+        layer.close()
