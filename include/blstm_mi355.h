@@ -159,8 +159,8 @@ int softmax_distill_fwd_bwd(blstm_ctx* ctx, const void* theta, const void* z, co
    float (softmax_logprob's, on the weights that sampled and on the reference's).  With lp = log p[label], r = exp(lp - old_logp):
      E = s sum over frames of  -min(r A, min(max(r, 1 - clip_low), 1 + clip_high) A)
                                + kl_weight (exp(ref_logp - lp) - (ref_logp - lp) - 1)
-   old_logp NULL: the present weights sampled, r = 1 and the gradient is -A grad lp.  ref_logp NULL: no KL term.  logp, if not NULL,
-   receives lp.  0 <= clip_low <= 1, clip_high >= 0, kl_weight >= 0. */
+   old_logp NULL: the present weights sampled, r = 1 and the gradient is -A grad lp.  ref_logp NULL or kl_weight 0: no KL
+   term, ref_logp is not read.  logp, if not NULL, receives lp.  0 <= clip_low <= 1, clip_high >= 0, kl_weight >= 0. */
 int softmax_policy_fwd_bwd(blstm_ctx* ctx, const void* theta, const void* z, const int32_t* labels, const float* advantage,
                            const float* old_logp_or_null, const float* ref_logp_or_null, float clip_low, float clip_high,
                            float kl_weight, float* loss_dev, float* logp_or_null, void* dz, float* grad,

@@ -1263,7 +1263,8 @@ int softmax_policy_fwd_bwd(blstm_ctx* ctx, const void* theta, const void* z, con
     LossCall c;
     rc = loss_begin(ctx, l, theta, z, scratch, static_cast<hipStream_t>(stream), &c);
     if (rc != BLSTM_OK) return rc;
-    const PolicyArgs p{advantage, old_logp, ref_logp, clip_low, clip_high, kl_weight};
+    // (a weight of zero is no term: the term itself may be infinite)
+    const PolicyArgs p{advantage, old_logp, kl_weight != 0.0f ? ref_logp : nullptr, clip_low, clip_high, kl_weight};
     return loss_run(ctx, c, labels, &p, nullptr, loss_dev, logp, dz, grad);
 }
 

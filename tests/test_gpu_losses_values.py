@@ -1,0 +1,32 @@
+"""The softmax layer's losses at the ends of what their inputs may hold: terms that are switched off, probabilities of nothing, values that are
+no numbers, logits far from zero."""
+import numpy as np
+import pytest
+
+from oracle import softmax_losses as sl
+from tests.test_gpu_losses import Layer, U
+from tests.test_gpu_losses_confident import best_labels, exact_layer
+
+pytestmark = pytest.mark.gpu
+KEYS = ("loss", "dz", "dW", "db")
+
+
+def same(x, y, keys=KEYS):
+    return all(np.array_equal(x[k], y[k]) for k in keys)
+
+
+@pytest.mark.parametrize("mode", [1, 0])
+@pytest.mark.parametrize("Z", [64, 264])
+def test_a_kl_weight_of_zero_is_no_term(Z, mode):
+    # whatever the reference's log-probabilities are: exp(ref - lp) may be infinite, and they may be no numbers
+    layer = Layer(2, 20, 90, Z, mode, 51)
+    try:
+        lab = layer.labels("whole")
+        lp = layer.logprob(lab).astype(np.float32)
+        A = layer.rng.normal(size=layer.M).astype(np.float32)
+        ref = lp.copy()
+        ref[3], ref[7], ref[11], ref[12] = lp[3] + 200, np.inf, np.nan, -np.inf
+        got, want = layer.policy(lab, A, lp, ref, 0.2, 0.2, 0.0), layer.policy(lab, A, lp, None, 0.2, 0.2, 0.0)
+        assert np.isfinite(want["loss"]) and same(got, want, KEYS + ("logp",))
+    finally:
+        layer.close()
