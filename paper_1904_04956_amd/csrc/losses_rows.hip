@@ -54,13 +54,14 @@ __device__ int teacher_list(const TeacherArgs& t, long long m, int V, ListLds& s
         const bool used = in && !(v == -INFINITY);
         some |= used;
         s.cls[k] = used ? c : -1;
-        s.log_q[k] = v * t.inv_tau;
-        if (used) top = fmaxf(top, v * t.inv_tau);
+        s.log_q[k] = v;
+        if (used) top = fmaxf(top, v);
     }
     top = wave_max(top);
     float sum = 0.0f;
     for (int k = lane; k < t.K; k += 64) {
-        const float e = s.cls[k] >= 0 ? expf(s.log_q[k] - top) : 0.0f;
+        s.log_q[k] = (s.log_q[k] - top) * t.inv_tau;   // (the distance first: a value over the temperature may be beyond a float's range)
+        const float e = s.cls[k] >= 0 ? expf(s.log_q[k]) : 0.0f;
         s.q[k] = e;
         sum += e;
     }
@@ -68,7 +69,7 @@ __device__ int teacher_list(const TeacherArgs& t, long long m, int V, ListLds& s
     for (int k = lane; k < t.K; k += 64) {
         const bool used = s.cls[k] >= 0;
         s.q[k] = used ? s.q[k] / sum : 0.0f;
-        s.log_q[k] = used ? s.log_q[k] - top - logf(sum) : 0.0f;
+        s.log_q[k] = used ? s.log_q[k] - logf(sum) : 0.0f;
     }
     wave_sync();
     return (__any(some) ? LIST_USED : 0) | (__any(bad) ? LIST_BAD : 0);
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(256) void loss_prep_kernel(LossPrepArgs a) {
                     const int k = k0 + 4 * n + g;
                     if (l16 == 0 && k < a.teacher.K) {
                         a.entry_logit[m * a.teacher.K + k] = u[n];
-                        if (c[n] >= 0) part += s.q[k] * (s.log_q[k] - u[n] * a.teacher.inv_tau);
+                        if (c[n] >= 0 && s.q[k] != 0.0f) part += s.q[k] * (s.log_q[k] - u[n] * a.teacher.inv_tau);   // (0 log 0 is nothing, whatever u is)
                     }
                 }
             }
@@ -500,7 +501,7 @@ __global__ __launch_bounds__(512) void loss_rows_f32_kernel(LossRowsArgs a, Poli
                 const int c = list.cls[k];
                 const float u = c >= 0 ? row[c] : 0.0f;
                 list.logit[k] = u;
-                if (c >= 0) part += list.q[k] * (list.log_q[k] - (u - mx) * it);
+                if (c >= 0 && list.q[k] != 0.0f) part += list.q[k] * (list.log_q[k] - (u - mx) * it);   // (0 log 0 is nothing, whatever u is)
             }
             part = wave_sum(part);
             if (state & LIST_USED) {

@@ -30,3 +30,27 @@ def test_a_kl_weight_of_zero_is_no_term(Z, mode):
         assert np.isfinite(want["loss"]) and same(got, want, KEYS + ("logp",))
     finally:
         layer.close()
+
+
+@pytest.mark.parametrize("mode", [1, 0])
+@pytest.mark.parametrize("Z", [64, 264])
+@pytest.mark.parametrize("tau", [0.5, 1.0, 2.0])
+@pytest.mark.parametrize("ruled_out", [-float("inf"), None])
+def test_a_teachers_class_without_probability_is_as_if_it_were_not_there(tau, ruled_out, Z, mode):
+    # a class that the teacher and the student rule out: 0 (log 0 - (-inf)) is nothing, and the lowest value over 0.5 is -inf
+    layer = Layer(2, 20, 90, Z, mode, 52)
+    try:
+        lab = layer.labels("whole")
+        lab = np.where(lab < 10, lab + 10, lab).astype(np.int32)
+        layer.theta[layer.at_b:layer.at_b + 10] = layer.torch.finfo(layer.kind).min if ruled_out is None else ruled_out
+        values, classes = layer.lists(6, "whole")
+        classes = classes % 80 + 10                       # (a class may be there twice)
+        classes[:, 2], classes[:, 5] = 3, 4
+        values[:, 2], values[:, 5] = np.finfo(np.float32).min, -1e30
+        less = classes.copy()
+        less[:, [2, 5]] = sl.NO_LABEL
+        for hard in (0.0, 0.5):
+            got, want = layer.distill(lab, values, classes, tau, hard, 0.5), layer.distill(lab, values, less, tau, hard, 0.5)
+            assert np.isfinite(want["loss"]) and same(got, want), (got["loss"], want["loss"])
+    finally:
+        layer.close()
