@@ -144,7 +144,7 @@ int softmax_topk(blstm_ctx* ctx, const void* theta, const void* z, int K, float*
 
 /* Distillation from a teacher's largest logits.  teacher_values [T][B][K] float, teacher_classes [T][B][K] int32 in any order, as
    softmax_topk writes them or shorter: an entry of class BLSTM_NO_LABEL or of value -inf is not used (any other class outside
-   [0, V): not used either, and the frame's loss term is NaN).  A class that stands in a list twice has the sum of both
+   [0, V), or a class with a value of NaN or +inf: not used either, and the frame's loss term is NaN).  A class that stands in a list twice has the sum of both
    probabilities.  With q = softmax over a frame's used entries of value / temperature, p' = softmax(u / temperature):
      E = s sum over frames of  hard_weight (-log p[label])  +  soft_weight temperature^2 sum_k q_k (log q_k - log p'[class_k])
    A frame without used entries has the first term only, one without label the second.  hard_weight 0: labels are not

@@ -58,7 +58,7 @@ struct LossPrepArgs {
     float* entry_logit;                              // [M][K]
     float* entry_q;                                  // [M][K], 0: not used; of entries with one class, the first has all
     float* soft_const;                               // [M]
-    int* soft_state;                                 // [M]: bit 0: some entry is used; bit 1: some class is out of range (the loss is NaN)
+    int* soft_state;                                 // [M]: bit 0: some entry is used; bit 1: some class is out of range, or its value NaN or infinite (the loss is NaN)
 };
 hipError_t launch_loss_prep(const LossPrepArgs& a, DType type, hipStream_t st);
 

@@ -39,8 +39,8 @@ enum { LIST_USED = 1, LIST_BAD = 2 };
 // A class list of one row in LDS, as its wavefront sees it.
 struct ListLds { int cls[LOSS_MAX_TOP]; float q[LOSS_MAX_TOP], log_q[LOSS_MAX_TOP], logit[LOSS_MAX_TOP]; };
 
-// q over the used entries of a row, by one wavefront.  Returns LIST_USED if there are any, and LIST_BAD if some class is out of range.
-// An entry that is not used has class -1 and q 0.  (A value of -inf is a probability of zero: it would make a list
+// q over the used entries of a row, by one wavefront.  Returns LIST_USED if there are any, and LIST_BAD if some class is out of range or its value no
+// number.  An entry that is not used has class -1 and q 0.  (A value of -inf is a probability of zero: it would make a list
 // of nothing else a division of zero by zero.)
 __device__ int teacher_list(const TeacherArgs& t, long long m, int V, ListLds& s) {
     const int lane = threadIdx.x & 63;
@@ -50,8 +50,8 @@ __device__ int teacher_list(const TeacherArgs& t, long long m, int V, ListLds& s
         const int c = t.classes[m * t.K + k];
         const float v = t.values[m * t.K + k];
         const bool in = (unsigned)c < (unsigned)V;
-        bad |= !in && c != -1;
-        const bool used = in && !(v == -INFINITY);
+        bad |= in ? !(v < INFINITY) : c != -1;
+        const bool used = in && v > -INFINITY && v < INFINITY;
         some |= used;
         s.cls[k] = used ? c : -1;
         s.log_q[k] = v;

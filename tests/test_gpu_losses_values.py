@@ -54,3 +54,26 @@ def test_a_teachers_class_without_probability_is_as_if_it_were_not_there(tau, ru
             assert np.isfinite(want["loss"]) and same(got, want), (got["loss"], want["loss"])
     finally:
         layer.close()
+
+
+@pytest.mark.parametrize("mode", [1, 0])
+@pytest.mark.parametrize("Z", [64, 264])
+@pytest.mark.parametrize("value", [np.nan, np.inf])
+def test_a_teachers_value_that_is_no_number_is_not_used_and_its_frames_loss_is_nan(value, Z, mode):
+    layer = Layer(2, 20, 90, Z, mode, 53)
+    try:
+        lab = layer.labels("whole")
+        values, classes = layer.lists(6, "whole")
+        values[4, 1] = value
+        values[9, :] = value                              # nothing else in the list
+        classes[15, 3], values[15, 3] = sl.NO_LABEL, value   # (not used in any case)
+        less = classes.copy()
+        less[4, 1] = less[9, :] = sl.NO_LABEL
+        for tau, hard in ((1.0, 0.5), (2.0, 0.5), (2.0, 0.0)):
+            got, want = layer.distill(lab, values, classes, tau, hard, 0.5), layer.distill(lab, values, less, tau, hard, 0.5)
+            assert np.isnan(got["loss"]) and np.isfinite(want["loss"]) and same(got, want, KEYS[1:])
+        less[15, 3] = classes[15, 3] = sl.NO_LABEL
+        got = layer.distill(lab, values, less, 2.0, 0.5, 0.5)
+        assert np.isfinite(got["loss"])
+    finally:
+        layer.close()
