@@ -490,7 +490,7 @@ LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
                 put(&l.part_sum2, (size_t)l.sum_parts * M * 4);
                 put(&l.entry_logit, M * K * 4);
                 put(&l.entry_q, M * K * 4);
-                put(&l.soft_const, M * 4);
+                put(&l.soft_const, 2 * M * 4);
                 put(&l.soft_state, M * 4);
                 put(&l.tile_count, tiles * 4);
                 put(&l.tile_from, tiles * 4);
@@ -506,7 +506,7 @@ LossScratch loss_scratch(const blstm_ctx* c, int call, int K) {
             put(&l.ptau, strips * M * 4);
             put(&l.entry_logit, M * K * 4);
             put(&l.entry_q, M * K * 4);
-            put(&l.soft_const, M * 4);
+            put(&l.soft_const, 2 * M * 4);
             put(&l.soft_state, M * 4);
         }
         if (gradient) {

@@ -41,7 +41,7 @@ struct TeacherArgs {
 };
 
 // Rows ahead of the products: zc = z with the rows that count for nothing set to zero, rows of ldzc elements, zeros behind Z.
-// bf16 (the float rows hold their logits, see launch_loss_rows_f32): the label's logit, the entries' logits, q and the row's sum q (log q - u / tau).
+// bf16 (the float rows hold their logits, see launch_loss_rows_f32): the label's logit, the entries' logits, q and the row's sum q (log q - (u - ref) / tau).
 struct LossPrepArgs {
     const void* z;
     void* zc;                                        // or null: not wanted
@@ -57,7 +57,7 @@ struct LossPrepArgs {
     TeacherArgs teacher;                             // K = 0: none
     float* entry_logit;                              // [M][K]
     float* entry_q;                                  // [M][K], 0: not used; of entries with one class, the first has all
-    float* soft_const;                               // [M]
+    float* soft_const;                               // [M] sum q (log q - (u - ref) / tau), then [M] ref
     int* soft_state;                                 // [M]: bit 0: some entry is used; bit 1: some class is out of range, or its value NaN or infinite (the loss is NaN)
 };
 hipError_t launch_loss_prep(const LossPrepArgs& a, DType type, hipStream_t st);

@@ -711,7 +711,7 @@ __global__ __launch_bounds__(256) void loss_dz_kernel(LossDzArgs a, PolicyArgs p
             if (lab_ok) { loss = a.s * teacher.hard * -lp; c1 = a.s * teacher.hard / sum; at_label = -a.s * teacher.hard * (others / sum); }
             else if (lab != -1) loss = nan;
             if (some) {
-                loss += a.s * teacher.soft * teacher.tau * teacher.tau * (a.soft_const[m] + (ref * LN2 + log_sum));
+                loss += a.s * teacher.soft * teacher.tau * teacher.tau * (a.soft_const[m] + (fmaf(-a.soft_const[a.M + m], k, ref) * LN2 + log_sum));
                 c1 += a.s * teacher.soft * teacher.tau / sum;
                 at_label += a.s * teacher.soft * teacher.tau / sum * w_label;
             }

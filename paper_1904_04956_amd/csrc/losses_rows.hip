@@ -180,7 +180,6 @@ __global__ __launch_bounds__(256) void loss_prep_kernel(LossPrepArgs a) {
             if (lane == 0) a.label_logit[m] = u[0];
         }
         if (a.teacher.K > 0) {
-            float part = 0.0f;
             for (int k0 = 0; k0 < a.teacher.K; k0 += 16) {
                 int c[4];
                 float u[4];
@@ -190,12 +189,17 @@ __global__ __launch_bounds__(256) void loss_prep_kernel(LossPrepArgs a) {
 #pragma unroll
                 for (int n = 0; n < 4; ++n) {
                     const int k = k0 + 4 * n + g;
-                    if (l16 == 0 && k < a.teacher.K) {
-                        a.entry_logit[m * a.teacher.K + k] = u[n];
-                        if (c[n] >= 0 && s.q[k] != 0.0f) part += s.q[k] * (s.log_q[k] - u[n] * a.teacher.inv_tau);   // (0 log 0 is nothing, whatever u is)
-                    }
+                    if (l16 == 0 && k < a.teacher.K) { a.entry_logit[m * a.teacher.K + k] = u[n]; s.logit[k] = u[n]; }
                 }
             }
+            // sum q (log q - (u - ref) / tau), 0 log 0 being nothing, whatever u is; ref: the largest u, so that an offset of all logits takes no digits
+            wave_sync();
+            float ref = -INFINITY, part = 0.0f;
+            for (int k = lane; k < a.teacher.K; k += 64) if (s.cls[k] >= 0 && s.q[k] > 0.0f) ref = fmaxf(ref, s.logit[k]);
+            ref = wave_max(ref);
+            if (ref == -INFINITY) ref = 0.0f;
+            for (int k = lane; k < a.teacher.K; k += 64) if (s.cls[k] >= 0 && s.q[k] != 0.0f) part += s.q[k] * (s.log_q[k] - (s.logit[k] - ref) * a.teacher.inv_tau);
+            part = wave_sum(part);
             // a class that stands there more than once has all of its q at the first of its entries with any
             for (int k0 = 0; k0 < a.teacher.K; k0 += 64) {
                 const int k = k0 + lane;
@@ -214,9 +218,7 @@ __global__ __launch_bounds__(256) void loss_prep_kernel(LossPrepArgs a) {
                 }
                 if (k < a.teacher.K) a.entry_q[m * a.teacher.K + k] = first ? q : 0.0f;
             }
-            part = l16 == 0 ? part : 0.0f;
-            part = wave_sum(part);
-            if (lane == 0) { a.soft_const[m] = part; a.soft_state[m] = state; }
+            if (lane == 0) { a.soft_const[m] = part; a.soft_const[a.M + m] = ref; a.soft_state[m] = state; }
         }
     }
 }
@@ -271,7 +273,9 @@ __device__ __forceinline__ void merge_end(const LossMergeArgs& a, const PolicyAr
             r.m2 = m2; r.a = a.s * teacher.hard / sum; r.hot = a.s * teacher.hard; r.label = lab;
         } else if (lab != -1 && teacher.hard != 0.0f) loss = nan;
         if (state & LIST_USED) {
-            const float lse = TAU ? mt2 * LN2 + logf(tau) : m2 * LN2 + logf(sum);   // (of u / tau)
+            // log sum exp((u - ref) / tau), ref being the terms'
+            const float ref = a.soft_const[a.M + m], lt = LOG2E * teacher.inv_tau;
+            const float lse = (far ? (mx - ref) * (TAU ? teacher.inv_tau : 1.0f) : (TAU ? fmaf(-ref, lt, mt2) : fmaf(-ref, LOG2E, m2)) * LN2) + logf(TAU ? tau : sum);
             loss += a.s * teacher.soft * teacher.tau * teacher.tau * (a.soft_const[m] + lse);
             const float at = a.s * teacher.soft * teacher.tau;
             if (TAU) { r.mt2 = mt2; r.at = at / tau; }

@@ -77,3 +77,37 @@ def test_a_teachers_value_that_is_no_number_is_not_used_and_its_frames_loss_is_n
         assert np.isfinite(got["loss"])
     finally:
         layer.close()
+
+
+@pytest.mark.parametrize("mode", [1, 0])
+@pytest.mark.parametrize("Z", [64, 264])
+@pytest.mark.parametrize("tau,hard", [(1.0, 0.5), (2.0, 0.5), (2.0, 0.0), (0.25, 0.5)])
+def test_an_offset_of_all_logits_is_none_of_the_losses(tau, hard, Z, mode):
+    # Logits exact in float, all of them 32768 lower, the teacher's 4096 higher.  What is left of a frame's terms are sums of V and K terms, some logarithms and products, and
+    # the roundings of distances from the largest logit (x, over the temperature) and of log q.
+    layer = exact_layer(2, 35, 300, Z, mode, 54, loss_scale=0.125)
+    try:
+        K, soft, s = 16, 0.75, float(layer.s)
+        layer.theta[layer.at_b:layer.at_b + layer.V] = -32768.0
+        z = layer.z.double().numpy()
+        u = z @ layer.W.T + layer.b
+        lab = best_labels(layer, u)
+        given = lab if hard else np.full_like(lab, sl.NO_LABEL)
+        classes = np.argsort(-u, axis=1, kind="stable")[:, :K].astype(np.int32)
+        values = (np.round(16 * (np.take_along_axis(u, classes.astype(np.int64), axis=1) + 0.5 * layer.rng.normal(size=(layer.M, K)))) / 16 + 32768 + 4096).astype(np.float32)
+        classes[layer.rng.random(layer.M) < 0.1] = sl.NO_LABEL
+        some, labelled = (classes >= 0).any(axis=1), given != sl.NO_LABEL
+        want = sl.distill(layer.W, layer.b, z, given, values, classes, s, tau, hard, soft)
+        got = layer.distill(lab if hard else None, values, classes, tau, hard, soft)
+        top = u.max(axis=1)
+        xk = np.where(some, top - np.take_along_axis(u, np.maximum(classes, 0), axis=1).min(axis=1), 0) / tau
+        xy = np.where(labelled, top - u[np.arange(layer.M), np.maximum(given, 0)], 0)
+        vk = np.where(some, values.max(axis=1) - values.min(axis=1), 0).astype(np.float64) / tau
+        log_v = np.log(layer.V)
+        each = hard * labelled * (layer.V + 64 + 8 * (xy + log_v)) + soft * tau * tau * some * (layer.V + K + 64 + 8 * (xk + vk + log_v))
+        size = hard * labelled * (xy + log_v) + soft * tau * tau * some * (xk + vk + log_v)
+        assert abs(got["loss"] - want[0]) <= s * U * (each.sum() + layer.M * size.sum()), (got["loss"] - want[0]) / (s * U * (each.sum() + layer.M * size.sum()))
+        lp = sl.logprob(layer.W, layer.b, z, lab)
+        assert np.all(np.abs(layer.logprob(lab) - lp) <= U * (layer.V + 64 + 8 * (np.abs(lp) + log_v)))
+    finally:
+        layer.close()
