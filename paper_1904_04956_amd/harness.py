@@ -101,9 +101,11 @@ class Learner:
     # ---- the softmax layer beyond cross-entropy ------------------------------------------
     def loss_scratch(self, call, K=0, stream=None):
         """Scratch of one of the softmax layer's calls (binding.SOFTMAX_*), kept for the next time: a captured graph holds its address."""
-        if (call, K) not in self.scratch:
-            self.scratch[call, K] = self._empty((bl.softmax_scratch_bytes(self.ctx, call, K),), torch.uint8, stream)
-        return self.scratch[call, K]
+        # (only a distillation's size depends on K)
+        n, key = bl.softmax_scratch_bytes(self.ctx, call, K), (call, K if call == bl.SOFTMAX_DISTILL else 0)
+        if key not in self.scratch:
+            self.scratch[key] = self._empty((n,), torch.uint8, stream)
+        return self.scratch[key]
 
     def _empty(self, shape, dtype, stream):
         """Memory for a call on `stream` (the allocator hands out what other work on the stream that it belongs to may still be writing)."""
