@@ -114,18 +114,26 @@ class Learner:
         with torch.cuda.stream(stream):
             return torch.empty(shape, dtype=dtype, device=self.device)
 
+    def _forward_on(self, weights, stream):
+        """A forward pass on `weights` if given, else on the learner's own; returns which."""
+        if weights is None:
+            self.forward(stream)
+            return self.theta_fwd
+        # the copies that passes keep go by address, and another call's weights may have lain at this one
+        self.weights_changed()
+        bl.blstm_forward(self.ctx, weights, self.x, self.z, stream)
+        return weights
+
     def log_probs(self, labels=None, weights=None, stream=None):
         """log p[label] [T][B] of the batch (of `labels` if given, else its own): a forward pass, then the softmax layer."""
-        th = self.theta_fwd if weights is None else weights
-        bl.blstm_forward(self.ctx, th, self.x, self.z, stream)
+        th = self._forward_on(weights, stream)
         out = self._empty(self.labels.shape, torch.float32, stream)
         bl.softmax_logprob(self.ctx, th, self.z, self.labels if labels is None else labels, out, self.loss_scratch(bl.SOFTMAX_LOGPROB, 0, stream), None, stream)
         return out
 
     def top_logits(self, K, weights=None, stream=None):
         """Values and classes [T][B][K] of the batch's K largest logits: what a student's calgrad_distill takes."""
-        th = self.theta_fwd if weights is None else weights
-        bl.blstm_forward(self.ctx, th, self.x, self.z, stream)
+        th = self._forward_on(weights, stream)
         shape = (*self.labels.shape, K)
         values, classes = self._empty(shape, torch.float32, stream), self._empty(shape, torch.int32, stream)
         bl.softmax_topk(self.ctx, th, self.z, K, values, classes, self.loss_scratch(bl.SOFTMAX_TOPK, K, stream), None, stream)

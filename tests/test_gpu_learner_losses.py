@@ -32,3 +32,27 @@ def test_lists_of_every_length_share_their_scratch():
         assert lrn.loss_scratch(bl.SOFTMAX_DISTILL, 100).numel() > lrn.loss_scratch(bl.SOFTMAX_DISTILL, 1).numel()
     finally:
         lrn.close()
+
+
+@pytest.mark.parametrize("dims", [dict(), dict(T=21, B=40, D=40, H=301, L=2, P=67)], ids=["whole words", "padded widths"])
+def test_given_weights_are_read_anew_in_every_call(dims):
+    # weights that are made for one call often lie where those of an earlier call lay: the copies that a pass keeps go by that address
+    import torch
+    lrn, other = learner(62, **dims), learner(63, **dims)
+    try:
+        own_lp, own_top = lrn.log_probs(), lrn.top_logits(5)
+        other.x.copy_(lrn.x), other.labels.copy_(lrn.labels)
+        want = {"own": (own_lp, own_top), "other": (other.log_probs(), other.top_logits(5))}
+        assert not torch.equal(want["other"][0], own_lp)
+        buffer = torch.empty_like(lrn.theta_fwd)
+        for name, src in (("own", lrn), ("other", other), ("own", lrn)):
+            buffer.copy_(src.theta_fwd)
+            assert torch.equal(lrn.log_probs(weights=buffer), want[name][0])
+        for name, src in (("other", other), ("own", lrn)):
+            buffer.copy_(src.theta_fwd)
+            values, classes = lrn.top_logits(5, weights=buffer)
+            assert torch.equal(values, want[name][1][0]) and torch.equal(classes, want[name][1][1])
+        assert torch.equal(lrn.log_probs(), own_lp)
+    finally:
+        lrn.close()
+        other.close()
