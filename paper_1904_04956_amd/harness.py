@@ -13,6 +13,19 @@ from . import binding as bl
 from . import inputs
 
 
+def checked(name, tensor, dtype, shape, device):
+    """`tensor`, if it is what a call reads or writes: the library sees an address and nothing else."""
+    if not isinstance(tensor, torch.Tensor):
+        raise TypeError(f"{name} must be a tensor, not {type(tensor).__name__}")
+    if tensor.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {tensor.dtype}")
+    if tuple(tensor.shape) != tuple(shape) or not tensor.is_contiguous():
+        raise ValueError(f"{name} must be {tuple(shape)} and contiguous, not {tuple(tensor.shape)} with strides {tensor.stride()}")
+    if tensor.device != device:
+        raise ValueError(f"{name} must be on {device}, not on {tensor.device}")
+    return tensor
+
+
 class Learner:
     """Buffers of one learner: master weights, bf16 shadow, gradient, batch, workspace."""
 
@@ -99,6 +112,12 @@ class Learner:
         bl.blstm_backward(self.ctx, th, self.x, self.dz, self.grad, stream)
 
     # ---- the softmax layer beyond cross-entropy ------------------------------------------
+    # (tensors of frames are [T][B] or [T B], float32, labels and classes int32, all contiguous and on the learner's device: else TypeError or ValueError)
+    def _frames(self, name, tensor, dtype=torch.float32, width=()):
+        T, B = self.labels.shape
+        flat = isinstance(tensor, torch.Tensor) and tensor.shape[:1] == (T * B,) and tensor.dim() == 1 + len(width)
+        return checked(name, tensor, dtype, (T * B, *width) if flat else (T, B, *width), self.x.device)
+
     def loss_scratch(self, call, K=0, stream=None):
         """Scratch of one of the softmax layer's calls (binding.SOFTMAX_*), kept for the next time: a captured graph holds its address."""
         # (only a distillation's size depends on K)
@@ -119,6 +138,7 @@ class Learner:
         if weights is None:
             self.forward(stream)
             return self.theta_fwd
+        checked("weights", weights, self.act_dtype, (self.n,), self.x.device)
         # the copies that passes keep go by address, and another call's weights may have lain at this one
         self.weights_changed()
         bl.blstm_forward(self.ctx, weights, self.x, self.z, stream)
@@ -126,9 +146,10 @@ class Learner:
 
     def log_probs(self, labels=None, weights=None, stream=None):
         """log p[label] [T][B] of the batch (of `labels` if given, else its own): a forward pass, then the softmax layer."""
+        labels = self.labels if labels is None else self._frames("labels", labels, torch.int32)
         th = self._forward_on(weights, stream)
         out = self._empty(self.labels.shape, torch.float32, stream)
-        bl.softmax_logprob(self.ctx, th, self.z, self.labels if labels is None else labels, out, self.loss_scratch(bl.SOFTMAX_LOGPROB, 0, stream), None, stream)
+        bl.softmax_logprob(self.ctx, th, self.z, labels, out, self.loss_scratch(bl.SOFTMAX_LOGPROB, 0, stream), None, stream)
         return out
 
     def top_logits(self, K, weights=None, stream=None):
@@ -141,7 +162,9 @@ class Learner:
 
     def calgrad_distill(self, values, classes, temperature=1.0, hard_weight=0.5, soft_weight=0.5, stream=None):
         """calgrad() with the loss against a teacher's lists [T][B][K] (and, with a hard_weight, the batch's labels)."""
-        K = classes.shape[-1]
+        K = classes.shape[-1] if isinstance(classes, torch.Tensor) and classes.dim() > 0 else 0
+        self._frames("classes", classes, torch.int32, (K,))
+        self._frames("values", values, torch.float32, (K,))
         bl.blstm_forward(self.ctx, self.theta_fwd, self.x, self.z, stream)
         bl.softmax_distill_fwd_bwd(self.ctx, self.theta_fwd, self.z, self.labels if hard_weight != 0 else None, values, classes, K, temperature, hard_weight,
                                    soft_weight, self.loss, self.dz, self.grad, self.loss_scratch(bl.SOFTMAX_DISTILL, K, stream), None, stream)
@@ -149,6 +172,10 @@ class Learner:
 
     def calgrad_policy(self, advantage, old_logp=None, ref_logp=None, clip_low=0.2, clip_high=0.2, kl_weight=0.0, logp=None, stream=None):
         """calgrad() with the clipped policy loss on the batch's labels, which were sampled."""
+        self._frames("advantage", advantage)
+        for name, t in (("old_logp", old_logp), ("ref_logp", ref_logp), ("logp", logp)):
+            if t is not None:
+                self._frames(name, t)
         bl.blstm_forward(self.ctx, self.theta_fwd, self.x, self.z, stream)
         bl.softmax_policy_fwd_bwd(self.ctx, self.theta_fwd, self.z, self.labels, advantage, old_logp, ref_logp, clip_low, clip_high, kl_weight, self.loss, logp,
                                   self.dz, self.grad, self.loss_scratch(bl.SOFTMAX_POLICY, 0, stream), None, stream)

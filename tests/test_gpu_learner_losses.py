@@ -56,3 +56,35 @@ def test_given_weights_are_read_anew_in_every_call(dims):
     finally:
         lrn.close()
         other.close()
+
+
+def test_arguments_of_another_kind_are_refused():
+    import torch
+    lrn = learner(64)
+    try:
+        T, B, V = DIMS["T"], DIMS["B"], DIMS["V"]
+        values, classes = lrn.top_logits(5)
+        lp = lrn.log_probs()
+        whole = torch.zeros((T, B, 10), device="cuda")
+        for bad in (dict(values=values.double()), dict(classes=classes.long()), dict(classes=classes[:, :4].contiguous()), dict(values=values[..., :3].contiguous()), dict(values=whole[..., ::2]),
+                    dict(values=values.cpu()), dict(classes=classes.transpose(0, 1).contiguous()), dict(values=values.cpu().numpy())):
+            with pytest.raises((TypeError, ValueError)):
+                lrn.calgrad_distill(**dict(dict(values=values, classes=classes), **bad))
+        for bad in (dict(advantage=lp[:-1].contiguous()), dict(advantage=lp.double()), dict(old_logp=lp.t()), dict(ref_logp=lp.half()), dict(logp=torch.empty((T, B - 1), device="cuda")),
+                    dict(advantage=lp.cpu())):
+            with pytest.raises((TypeError, ValueError)):
+                lrn.calgrad_policy(**dict(dict(advantage=lp), **bad))
+        for bad in (dict(labels=lrn.labels.long()), dict(labels=lrn.labels[:2]), dict(weights=lrn.theta), dict(weights=lrn.theta_fwd[:-1])):
+            with pytest.raises((TypeError, ValueError)):
+                lrn.log_probs(**bad)
+        with pytest.raises((TypeError, ValueError)):
+            lrn.top_logits(5, weights=lrn.theta)
+        # and what a program gives as it should is taken
+        lrn.calgrad_distill(values, classes, temperature=2.0)
+        grad = lrn.grad.clone()
+        lrn.calgrad_distill(values.view(T * B, 5), classes.view(T * B, 5), temperature=2.0)
+        assert torch.equal(lrn.grad, grad)
+        lrn.calgrad_policy(lp, lp.view(-1), lp, logp=torch.empty_like(lp))
+        assert np.isfinite(lrn.loss_value())
+    finally:
+        lrn.close()
