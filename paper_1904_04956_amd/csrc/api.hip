@@ -773,10 +773,11 @@ int loss_run(blstm_ctx* ctx, const LossCall& given, const int32_t* labels, const
     return loss_products(ctx, c, teacher, dz, grad);
 }
 
-// What softmax_xent_fwd_bwd left to the next blstm_backward is written by the call itself.
+// What softmax_xent_fwd_bwd left to the next blstm_backward is written by the call itself.  (Calls of several threads share the context: where
+// nothing is pending, they only read it.)
 void drop_deferred(blstm_ctx* ctx) {
-    ctx->pend_z = nullptr;
-    if (ctx->twin) ctx->twin->pend_z = nullptr;
+    if (ctx->pend_z) ctx->pend_z = nullptr;
+    if (ctx->twin && ctx->twin->pend_z) ctx->twin->pend_z = nullptr;
 }
 
 }  // namespace

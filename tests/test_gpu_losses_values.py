@@ -111,3 +111,56 @@ def test_an_offset_of_all_logits_is_none_of_the_losses(tau, hard, Z, mode):
         assert np.all(np.abs(layer.logprob(lab) - lp) <= U * (layer.V + 64 + 8 * (np.abs(lp) + log_v)))
     finally:
         layer.close()
+
+
+def test_threads_that_share_a_context():
+    # each with a stream, scratch and outputs of its own; the calls of one thread are the others' in another order
+    import threading
+    import torch
+    layer = Layer(4, 60, 700, 96, 1, 55)
+    bl = layer.bl
+    try:
+        lab, A = layer.labels("ragged"), layer.rng.normal(size=layer.M).astype(np.float32)
+        values, classes = layer.lists(7, "ragged")
+        theta, z, dlab, dA, dv, dc = (layer.dev(t) for t in (layer.theta, layer.z, lab, A, values, classes))
+
+        def made():
+            return [layer.outputs() for _ in range(2)], [layer.scratch(bl.SOFTMAX_POLICY), layer.scratch(bl.SOFTMAX_DISTILL, 7), layer.scratch(bl.SOFTMAX_LOGPROB)], torch.zeros(layer.M, device="cuda")
+
+        def calls(held, order, stream):
+            (p, d), (s1, s2, s3), logp = held
+            for k in order:
+                if k == 0:
+                    bl.softmax_policy_fwd_bwd(layer.ctx, theta, z, dlab, dA, None, None, 0.2, 0.2, 0.0, p["loss"], None, p["dz"], p["grad"], s1, None, stream)
+                elif k == 1:
+                    bl.softmax_distill_fwd_bwd(layer.ctx, theta, z, dlab, dv, dc, 7, 2.0, 0.5, 0.5, d["loss"], d["dz"], d["grad"], s2, None, stream)
+                else:
+                    bl.softmax_logprob(layer.ctx, theta, z, dlab, logp, s3, None, stream)
+
+        want = made()
+        calls(want, (0, 1, 2), torch.cuda.current_stream())
+        sets, streams = [made() for _ in range(4)], [torch.cuda.Stream() for _ in range(4)]
+        torch.cuda.synchronize()
+        failed = []
+
+        def work(k):
+            try:
+                for _ in range(5):
+                    calls(sets[k], [(k + j) % 3 for j in range(3)], streams[k])
+            except Exception as e:
+                failed.append(e)
+
+        threads = [threading.Thread(target=work, args=(k,)) for k in range(4)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        torch.cuda.synchronize()
+        assert not failed
+        for outs, _, logp in sets:
+            for got, ref in zip(outs, want[0]):
+                for key in ("loss", "dz", "grad"):
+                    assert torch.equal(got[key], ref[key]), key
+            assert torch.equal(logp, want[2])
+    finally:
+        layer.close()
