@@ -95,9 +95,8 @@ struct LossFusedArgs {
     float k1, k;                                     // scale of the first exponential, and of the second (rows, sums not known: the only one)
     int parts;                                       // of the classes (rows kernel) or of the rows (classes kernel), a workgroup each
     float* out;                                      // rows: [parts][M][ld]; classes: [parts][V][ldo], columns 0 .. Z - 1
-    // rows: classes that stay out of the product and of the sums; launch_loss_dz adds them
-    const int32_t* labels;                           // [M] the label's, or null; sums at two scales: stays out of both, launch_loss_merge adds it
-    const uint32_t* marks;                           // those of [classes / 32, rounded up to even][Mr], a bit a class; or null (then the label's)
+    const int32_t* labels;                           // [M] rows (sums not known), sums at two scales: the label's class stays out; launch_loss_dz, launch_loss_merge add it; or null
+    const uint32_t* marks;                           // rows: [loss_mark_words(V)][Mr], a bit a class that stays out of the product; launch_loss_dz adds it; or null: the label's alone
     int Mr;                                          // M rounded up to 256
     float* part_ref;                                 // rows, sums not known: [parts][M] reference and sum
     float* part_sum;

@@ -110,7 +110,8 @@ constexpr int DEPTH = 4;
 
 // ---- rows -------------------------------------------------------------------------------------------------------------------
 // KNOWN: w = a exp2(u log2e - m2) + at exp2(u k - mt2) from the rows' constants, else w = exp2(u k - reference).
-// MARKS: what stays out is marked, a bit a class, and comes with the tile; else it is the label.  Either counts as ruled out.
+// The label counts as ruled out.  MARKS: what else stays out of the product is marked, a bit a class (the label's too), and comes with the tile; it is in the sum,
+// whose logits are the classes kernel's to the last bits but one, where those of the lists are another product's.
 template <int NK, bool KNOWN, bool MARKS>
 __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
     typedef Ring<NK> R;
@@ -132,7 +133,7 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
     if (KNOWN && m < a.Mp) {
         m2 = a.consts[m]; ca = a.consts[a.Mp + m]; mt2 = a.consts[2 * a.Mp + m]; cat = a.consts[3 * a.Mp + m];
     }
-    const int label = !MARKS && m < a.M ? a.labels[m] : -1;
+    const int label = !KNOWN && a.labels && m < a.M ? a.labels[m] : -1;
     __builtin_amdgcn_s_waitcnt(0);                      // (known to the compiler: it would wait for these loads, and the ring's with them, in the loop)
     auto issue = [&](int it) __attribute__((always_inline)) {
         const unsigned s = lds0 + (unsigned)(it % R::STAGES * STAGE);
@@ -173,16 +174,18 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
             unsigned out = 0;                            // (bit 8 (e / 4) + e % 4: class e of the lane stays out)
             if constexpr (MARKS) out = *reinterpret_cast<const unsigned*>(stage + R::STAGE + wv * 256 + sub * 128 + (fresh_lane() & 31) * 4);
             ahead<4 + (MARKS ? 1 : 0) + DEPTH, 4 * NK, 1, 1, DEPTH>();
-            if constexpr (!MARKS) {
+            unsigned ruled = out;
+            if constexpr (!KNOWN) {
                 const unsigned at_label = (unsigned)(label - ((t0 + it) * 64 + sub * 32));
-                out = at_label < 32u ? 1u << at_label : 0u;
+                ruled = at_label < 32u ? 1u << at_label : 0u;
             }
-            if (__any(out != 0)) {
-                out >>= 4 * half;
+            if (__any(ruled != 0)) {
+                ruled >>= 4 * half;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) u[e] = out & 1u << (8 * (e >> 2) + (e & 3)) ? -INFINITY : u[e];
+                for (int e = 0; e < 16; ++e) u[e] = ruled & 1u << (8 * (e >> 2) + (e & 3)) ? -INFINITY : u[e];
             }
             if constexpr (!KNOWN) {
+                if (MARKS) out >>= 4 * half;
                 float mx = u[0];
 #pragma unroll
                 for (int e = 1; e < 16; ++e) mx = fmaxf(mx, u[e]);
@@ -212,6 +215,7 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
                         } else {
                             w[i] = __builtin_amdgcn_exp2f(fmaf(x, k, -ref));
                             sum += w[i];
+                            if (MARKS) w[i] = out & 1u << (8 * (2 * t + (e >> 2)) + (e & 3) + i) ? 0.0f : w[i];
                         }
                     }
                     p[e / 2] = pack2(w[0], w[1]);
@@ -645,8 +649,8 @@ __global__ __launch_bounds__(256) void loss_classes_sum_kernel(const float* __re
 
 // ---- behind the rows: a workgroup a row, four columns a lane, its wavefronts share the parts and the teacher's classes ---------
 // KNOWN: the rows' constants and losses are there and the parts are sums of du W; else they are made here from the parts' references
-// and sums, which are brought to the largest reference, and the logits of the classes that the parts lack.  Of those classes, the label's
-// and the teacher's, dE/du is made here in float: 1 - p of a label from the sum of all others, p' - q as a difference.  All loads of a step are independent: one by one, 128 parts and 64 classes
+// and sums, which are brought to the largest reference, and the label's logit, which they lack.  Of the label's and the teacher's classes, which the parts
+// lack, dE/du is made here in float: 1 - p of a label from the sum of all others, p' - q as a difference.  All loads of a step are independent: one by one, 128 parts and 64 classes
 // took 49 us for 168 rows.
 // SHARE: wavefronts a row, four or, where rows are many, one (43008 rows: 69 us with four, 29 with one).
 template <bool KNOWN, bool POLICY, int SHARE>
@@ -677,9 +681,7 @@ __global__ __launch_bounds__(256) void loss_dz_kernel(LossDzArgs a, PolicyArgs p
     } else {
         const bool lab_ok = (unsigned)lab < (unsigned)a.V;
         const float lu = lab_ok ? a.label_logit[m] : 0.0f;
-        const int listed = POLICY ? 0 : teacher.K;
         float ref = lab_ok ? lu * k : -INFINITY;
-        for (int i = lane; i < listed; i += 64) { const Entry e = entry(i); if (e.c >= 0) ref = fmaxf(ref, e.u * k); }
         for (int p = lane; p < a.parts; p += 64) ref = fmaxf(ref, a.part_ref[(long long)p * a.M + m]);
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor(ref, o, 64));
@@ -687,11 +689,6 @@ __global__ __launch_bounds__(256) void loss_dz_kernel(LossDzArgs a, PolicyArgs p
         for (int p = lane; p < a.parts; p += 64) sum += a.part_sum[(long long)p * a.M + m] * __builtin_amdgcn_exp2f(a.part_ref[(long long)p * a.M + m] - ref);
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-        float taught = 0.0f;
-        for (int i = lane; i < listed; i += 64) { const Entry e = entry(i); if (e.c >= 0 && e.c != lab) taught += __builtin_amdgcn_exp2f(fmaf(e.u, k, -ref)); }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) taught += __shfl_xor(taught, o, 64);
-        sum += taught;
         const float others = sum, w_label = lab_ok ? __builtin_amdgcn_exp2f(fmaf(lu, k, -ref)) : 0.0f;
         sum += w_label;
         m2 = ref;
