@@ -113,8 +113,8 @@ int softmax_xent_fwd_bwd_noalloc(blstm_ctx* ctx, const void* theta, const void* 
      share the context unless profiling is on.  A call never reads what an earlier one left in scratch.
    - labels [T][B] int32.  BLSTM_NO_LABEL marks a frame that counts for nothing (padding, an empty sequence): whatever z and the
      call's other inputs hold there, it adds nothing to the loss, its row of dz is zero, and W_s and b_s get nothing from it.
-     Any other label outside [0, V) is never used as an index: the frame's loss term and log-probability are NaN, its
-     gradients nothing.
+     Any other label outside [0, V) is never used as an index: the frame's loss term and log-probability are NaN, and the label
+     adds nothing to the gradients (a distillation's teacher still does).
    - The calls with gradients write loss_dev[0], dz [T][B][P or 2H] and, of grad, the slices W_s and b_s (overwritten): what
      softmax_xent_fwd_bwd writes, in its place in front of blstm_backward (BLSTM_OPT_DEFER_SOFTMAX_WGRAD does not concern
      them; what an earlier softmax_xent_fwd_bwd left to blstm_backward is dropped).  Mode 1: logits and all sums in float,

@@ -22,8 +22,6 @@
 // (ds_read_b64_tr_b16 transposes on the way).  16-byte chunk c of row r lies at chunk c ^ sw(r): the eight rows that a phase
 // of the first reads, and the four of the second, are on different banks.  The output of the first product (lane: row or
 // class, registers: the other) is the operand of the second after one exchange between the lane halves.
-#include <climits>
-
 #include "gemm_tile.hpp"
 #include "losses_terms.hpp"
 
@@ -110,8 +108,9 @@ constexpr int DEPTH = 4;
 
 // ---- rows -------------------------------------------------------------------------------------------------------------------
 // KNOWN: w = a exp2(u log2e - m2) + at exp2(u k - mt2) from the rows' constants, else w = exp2(u k - reference).
-// The label counts as ruled out.  MARKS: what else stays out of the product is marked, a bit a class (the label's too), and comes with the tile; it is in the sum,
-// whose logits are the classes kernel's to the last bits but one, where those of the lists are another product's.
+// The label counts as ruled out.  MARKS: the teacher's classes stay out of the product; they are marked, a bit a class (the label's too), and the marks come
+// with the tile.  They are in the sum, with the same product's logits as all others: with those of the lists, another product's, the rows' sums and the classes
+// kernel, which makes p' - q of them, were 2.5e-5 apart where the two are close, and are 8e-6.
 template <int NK, bool KNOWN, bool MARKS>
 __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
     typedef Ring<NK> R;
@@ -247,9 +246,9 @@ __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
 }
 
 // ---- rows, the sums alone -----------------------------------------------------------------------------------------------------
-// Reference and sum of exponentials of every row and part (SUMS2: at two scales, from one reference, without the label's class), or the logits themselves with the
-// maxima of strips of 64 classes (LOGITS).  5376 rows of 32000, Z = 256 (88 GFLOP): 90 us (980 TFLOP/s), SUMS2 112 (106 with the label in its sums), LOGITS 230, whose
-// 688 MB are stored at 3 TB/s (past L2 or with loads that do not wait for them no faster).  Two workgroups a CU, four wavefronts a SIMD, so that some multiply while others take exponentials.
+// Reference and sum of exponentials of every row and part (SUMS2: at two scales, from one reference, without the label's class), or the
+// logits themselves with the maxima of strips of 64 classes (LOGITS).  5376 rows of 32000, Z = 256 (88 GFLOP): 90 us (980 TFLOP/s), SUMS2
+// 112 (106 with the label in its sums), LOGITS 230, whose 688 MB are stored at 3 TB/s (past L2 or with loads that do not wait for them no faster).  Two workgroups a CU, four wavefronts a SIMD, so that some multiply while others take exponentials.
 // Rows as in the rows kernel: of the 128 x 128 tiles that larger z take, both operands come from L2 for half the products.
 enum { SUMS, SUMS2, LOGITS };
 template <int NK, int WHAT>
@@ -649,10 +648,10 @@ __global__ __launch_bounds__(256) void loss_classes_sum_kernel(const float* __re
 
 // ---- behind the rows: a workgroup a row, four columns a lane, its wavefronts share the parts and the teacher's classes ---------
 // KNOWN: the rows' constants and losses are there and the parts are sums of du W; else they are made here from the parts' references
-// and sums, which are brought to the largest reference, and the label's logit, which they lack.  Of the label's and the teacher's classes, which the parts
-// lack, dE/du is made here in float: 1 - p of a label from the sum of all others, p' - q as a difference.  All loads of a step are independent: one by one, 128 parts and 64 classes
-// took 49 us for 168 rows.
-// SHARE: wavefronts a row, four or, where rows are many, one (43008 rows: 69 us with four, 29 with one).
+// and sums, which are brought to the largest reference, and the label's logit, which they lack.  The parts lack the label's and the
+// teacher's classes, whose dE/du is made here in float: 1 - p of a label from the sum of all others, p' - q as a difference.
+// All loads of a step are independent: one by one, 128 parts and 64 classes took 49 us for 168 rows.
+// SHARE: wavefronts a row, four or, where rows are many, one (43008 rows: 69 us with four, 30 with one).
 template <bool KNOWN, bool POLICY, int SHARE>
 __global__ __launch_bounds__(256) void loss_dz_kernel(LossDzArgs a, PolicyArgs policy, TeacherArgs teacher) {
     __shared__ float4 sh[3][64];
@@ -853,9 +852,8 @@ hipError_t launch_loss_lists(const LossListArgs& a, hipStream_t st) {
     const int words = loss_mark_words(a.V);
     const size_t lists = (ntv + LISTS_THREADS / 64) * sizeof(int), marks = (size_t)(words < MARK_WORDS ? words : MARK_WORDS) * 32 * sizeof(uint32_t), lds = lists > marks ? lists : marks;
     if (lds > most) return hipErrorInvalidValue;
-    const long long grid = (a.M + 63) / 64 + (long long)(a.Mr / 32) * ((words + MARK_WORDS - 1) / MARK_WORDS);
-    if (grid > INT_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(loss_lists_kernel, dim3((unsigned)grid), dim3(LISTS_THREADS), lds, st, a, ntv);
+    const unsigned grid = (unsigned)((a.M + 63) / 64 + a.Mr / 32 * ((words + MARK_WORDS - 1) / MARK_WORDS));   // (below 2^26: T B V is below 2^44)
+    hipLaunchKernelGGL(loss_lists_kernel, dim3(grid), dim3(LISTS_THREADS), lds, st, a, ntv);
     return hipGetLastError();
 }
 hipError_t launch_loss_classes_sum(const float* p, const float* pb, int parts, long long n, int V, float* out, float* out_b, hipStream_t st) {
