@@ -179,7 +179,7 @@ struct LossMergeArgs {
 };
 hipError_t launch_loss_merge(const LossMergeArgs& a, hipStream_t st);
 
-// The teacher's entries in du, exactly: each once rounded from its own value.
+// The teacher's entries in du: each rounded to its parts from p' - q in float.
 struct LossEntriesArgs {
     const LossRow* rows;
     const int32_t* classes;

@@ -110,7 +110,7 @@ constexpr int DEPTH = 4;
 // KNOWN: w = a exp2(u log2e - m2) + at exp2(u k - mt2) from the rows' constants, else w = exp2(u k - reference).
 // The label counts as ruled out.  MARKS: the teacher's classes stay out of the product; they are marked, a bit a class (the label's too), and the marks come
 // with the tile.  They are in the sum, with the same product's logits as all others: with those of the lists, another product's, the rows' sums and the classes
-// kernel, which makes p' - q of them, were 2.5e-5 apart where the two are close, and are 8e-6.
+// kernel, which makes p' - q of them, were 2.5e-5 apart where the two are close, and are 7e-6.
 template <int NK, bool KNOWN, bool MARKS>
 __global__ __launch_bounds__(512, 2) void loss_rows_kernel(LossFusedArgs a) {
     typedef Ring<NK> R;
@@ -442,9 +442,11 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
             if (listed > 64) any_spot |= others(false);
             any_spot = __any(any_spot);
         }
-        f32x16_t u;
+        f32x16_t u;                                     // (the bias first, as in the walks over the classes: the same logits, bit by bit)
+        float first = b;
+        asm volatile("" : "+v"(first));                 // (sixteen copies of it made ahead of the loop are sixteen registers too many)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) u[e] = 0.0f;
+        for (int e = 0; e < 16; ++e) u[e] = first;
 #pragma unroll
         for (int q = 0; q < 4 * NK; ++q) u = mma32(at.by_row(s, q), wf[q], u);
         ahead<DEPTH, 4 * NK, 1, 1, DEPTH>();
@@ -461,12 +463,12 @@ __global__ __launch_bounds__(512, 2) void loss_classes_kernel(LossFusedArgs a) {
                 const float4 m2 = *reinterpret_cast<const float4*>(consts + r), ca = *reinterpret_cast<const float4*>(consts + 64 + r);
                 const float ms[4] = {m2.x, m2.y, m2.z, m2.w}, cs[4] = {ca.x, ca.y, ca.z, ca.w};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) d[4 * h + i] = cs[i] * __builtin_amdgcn_exp2f(fmaf(u[8 * t + 4 * h + i] + b, k1, -ms[i]));
+                for (int i = 0; i < 4; ++i) d[4 * h + i] = cs[i] * __builtin_amdgcn_exp2f(fmaf(u[8 * t + 4 * h + i], k1, -ms[i]));
                 if (TAU) {
                     const float4 mt = *reinterpret_cast<const float4*>(consts + 128 + r), ct_ = *reinterpret_cast<const float4*>(consts + 192 + r);
                     const float mts[4] = {mt.x, mt.y, mt.z, mt.w}, cts[4] = {ct_.x, ct_.y, ct_.z, ct_.w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) d[4 * h + i] = fmaf(cts[i], __builtin_amdgcn_exp2f(fmaf(u[8 * t + 4 * h + i] + b, k, -mts[i])), d[4 * h + i]);
+                    for (int i = 0; i < 4; ++i) d[4 * h + i] = fmaf(cts[i], __builtin_amdgcn_exp2f(fmaf(u[8 * t + 4 * h + i], k, -mts[i])), d[4 * h + i]);
                 }
             }
             if (any_hot) {                              // (a label's du is one of the constants)

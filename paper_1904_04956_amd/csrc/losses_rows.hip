@@ -351,7 +351,7 @@ __global__ __launch_bounds__(256) void loss_merge_row_kernel(LossMergeArgs a, Te
     if (lane == 0) merge_end<TAU, false, TAU>(a, PolicyArgs{}, teacher, m, in, mx, sum, tau);
 }
 
-// ---- the teacher's entries of du: a wavefront a row -------------------------------------------------------------------
+// ---- the teacher's entries of du, p' - q: a wavefront a row ------------------------------------------------------------
 __global__ __launch_bounds__(256) void loss_entries_kernel(LossEntriesArgs a) {
     __shared__ ListLds lists[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -370,10 +370,15 @@ __global__ __launch_bounds__(256) void loss_entries_kernel(LossEntriesArgs a) {
     for (int k = lane; k < a.K; k += 64) {
         const int c = s.cls[k];
         if (c < 0) continue;
-        const float u = a.entry_logit[m * a.K + k];
-        const bool far = fabsf(r.max) > LOSS_FAR;
-        float v = r.a * __builtin_amdgcn_exp2f(far ? (u - r.max) * LOG2E : fmaf(u, LOG2E, -r.m2)) + r.at * __builtin_amdgcn_exp2f(far ? (u - r.max) * lt : fmaf(u, lt, -r.mt2));
-        if (c == r.label) v -= r.hot;
+        float v;
+        if (a.third) {                                   // (what the tiles made there is whole in three parts, of the very logits that the sums have seen)
+            v = (bf2f(a.hi[m * a.ldu + c]) + bf2f(a.lo[m * a.ldu + c])) + bf2f(a.lo[(a.M + m) * a.ldu + c]);
+        } else {                                         // (two are 2^-16 of it off: more than another product's logit in float is)
+            const float u = a.entry_logit[m * a.K + k];
+            const bool far = fabsf(r.max) > LOSS_FAR;
+            v = r.a * __builtin_amdgcn_exp2f(far ? (u - r.max) * LOG2E : fmaf(u, LOG2E, -r.m2)) + r.at * __builtin_amdgcn_exp2f(far ? (u - r.max) * lt : fmaf(u, lt, -r.mt2));
+            if (c == r.label) v -= r.hot;
+        }
         v -= a.weight * s.q[k];
         const bf16_t hi = f2bf(v);
         a.hi[m * a.ldu + c] = hi;

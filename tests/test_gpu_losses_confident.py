@@ -160,3 +160,30 @@ def test_small_temperatures_and_logits_far_below_zero(tau, hard, Z, mode):
         assert np.isfinite(got["loss"])
     finally:
         layer.close()
+
+
+@pytest.mark.parametrize("mode", [1, 0])
+@pytest.mark.parametrize("Z", [64, 250, 256, 264, 640])
+@pytest.mark.parametrize("kind", ["policy", "tau 1", "tau 2", "teacher 1", "teacher 2"])
+def test_the_classes_of_a_frame_see_the_logits_that_its_sum_has_seen(kind, Z, mode):
+    # dE/du of a frame adds up to nothing, as its probabilities and the teacher's add up to one.  Every logit is 32768 and some, whose roundings (2^-9, and others in another order of
+    # the product's sum) are thousands of times what the sums of V terms may leave: so whatever makes the probabilities has to have the logits of the sum, bit by bit.
+    # One frame: db_s is its dE/du, in float.
+    layer = Layer(1, 1, 600, Z, mode, 44, scale=4 / np.sqrt(Z), loss_scale=1.0)
+    try:
+        W = layer.theta[layer.at_w:layer.at_w + 600 * Z].view(600, Z)
+        W[:, 5], layer.z[0, 5] = 256.0, 128.0
+        u = layer.z.double().numpy() @ layer.W.T + layer.b
+        lab = u.argmax(axis=1).astype(np.int32)
+        if kind == "policy":
+            du = layer.policy(lab, np.ones(1, dtype=np.float32), None, None, 0.2, 0.2, 0.0)["db"]
+        else:
+            classes = np.argsort(-u, axis=1, kind="stable")[:, :16].astype(np.int32)
+            values = np.take_along_axis(u, classes.astype(np.int64), axis=1).astype(np.float32)
+            tau, hard = float(kind[-1]), 0.0 if kind.startswith("teacher") else 0.5
+            du = layer.distill(lab if hard else None, values, classes, tau, hard, 0.5)["db"]
+        assert np.abs(du).sum() > 0.1
+        # (a probability is right to V + 64 roundings of itself at most; the parts of dE/du are up to 1 and 2 in sum)
+        assert abs(du.sum()) <= 4 * (600 + 64) * U, du.sum()
+    finally:
+        layer.close()
