@@ -176,6 +176,33 @@ int blstm_backward(blstm_ctx* ctx, const void* theta, const void* x, const void*
 int sgd_step(float* theta_master, void* theta_bf16_or_null, const float* grad, size_t n,
              float lr, float momentum, float* velocity_or_null, void* stream);
 
+/* ---- the orthogonalised update --------------------------------------------------------------------------------
+   Another apply(W, g).  Of a matrix G [R][C], |G| its Frobenius norm, O(G) is what five Newton-Schulz steps make of X = G / |G|:
+     X <- a X + b S X + c S^2 X,  S = X X^T (R <= C; else X <- a X + b X S + c X S^2,  S = X^T X),  (a, b, c) = (3.4445, -4.7750, 2.0315)
+   G's singular vectors with singular values of 0.7 to 1.2, the smallest ones less (they grow 485-fold at most).  O of a zero matrix is zero; an infinity or a NaN anywhere
+   in G makes all of O(G) NaN.  Mode 1 multiplies in halves (11 bits, of values scaled for them; sums in float): O(G) is off by about 3e-4 of its norm.
+   Mode 0 multiplies pairs of halves: about 1e-6.  The same inputs give the same bits.
+   `scratch` as for the softmax calls: caller-owned, 16-byte aligned, holds nothing between calls; calls that overlap need one each. */
+#define MUON_NESTEROV 1                        /* the update's direction is grad + momentum * velocity, else the velocity */
+#define MUON_GATES    2                        /* muon_step: each gate's block [H][..] of W_x and U_h is a matrix of its own, else the four together are one */
+#define MUON_SOFTMAX  4                        /* muon_step: W_s is orthogonalised as well */
+
+/* X <- O(G) of `count` matrices [rows][cols], one behind the other.  G float; X bfloat16 in mode 1, float in mode 0. */
+size_t muon_orthogonalize_scratch_bytes(int count, int rows, int cols, int mode);      /* 0 and an error text for sizes it does not take */
+int muon_orthogonalize(const float* G, void* X, int count, int rows, int cols, int mode, void* scratch, size_t scratch_bytes, void* stream);
+
+/* The update of `count` matrices [rows][cols] (a low-rank adapter's factors, say): v <- momentum * v + grad; d = v, or grad + momentum * v;
+   theta <- (1 - lr * weight_decay) * theta - lr * sqrt(max(1, rows / cols)) * O(d).  theta_bf16 and velocity as in sgd_step (momentum 0: velocity is not read
+   or written and may be NULL).  0 <= momentum < 1, weight_decay >= 0, flags 0 or MUON_NESTEROV.  Scratch: muon_orthogonalize_scratch_bytes. */
+int muon_matrices_step(float* theta_master, void* theta_bf16_or_null, const float* grad, float* velocity_or_null, int count, int rows, int cols, int mode,
+                       float lr, float momentum, float weight_decay, int flags, void* scratch, size_t scratch_bytes, void* stream);
+
+/* The update of a model's whole vector in ctx's layout and mode (no workspace needs to be bound): W_x, U_h and W_p, with MUON_SOFTMAX W_s, as in muon_matrices_step;
+   the biases, else W_s too: theta <- theta - lr_rest * d. */
+size_t muon_scratch_bytes(const blstm_ctx* ctx, int flags);                            /* 0 and an error text if it cannot be */
+int muon_step(const blstm_ctx* ctx, float* theta_master, void* theta_bf16_or_null, const float* grad, float* velocity_or_null, float lr, float lr_rest,
+              float momentum, float weight_decay, int flags, void* scratch, size_t scratch_bytes, void* stream);
+
 /* Eq. 4, second line, for one matching of R replicas: for every pair {i, partner[i]} both members
    become (theta_i + theta_j)/2; partner[i] == i leaves replica i untouched.
    theta_master: HOST array of R device pointers (n floats each); theta_bf16_or_null: HOST array of R

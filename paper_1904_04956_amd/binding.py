@@ -20,11 +20,13 @@ BLSTM_NO_LABEL = -1
 BLSTM_MAX_TOP = 256
 BLSTM_MIN_TEMPERATURE = 1e-4
 SOFTMAX_LOGPROB, SOFTMAX_TOPK, SOFTMAX_DISTILL, SOFTMAX_POLICY = range(4)
+MUON_NESTEROV, MUON_GATES, MUON_SOFTMAX = 1, 2, 4
 
 EXPORTS = [
     "blstm_create", "blstm_destroy", "blstm_param_count", "blstm_workspace_bytes", "blstm_param_offset",
     "blstm_bind", "blstm_forward", "softmax_xent_fwd_bwd", "softmax_xent_fwd_bwd_noalloc",
     "softmax_scratch_bytes", "softmax_logprob", "softmax_topk", "softmax_distill_fwd_bwd", "softmax_policy_fwd_bwd", "blstm_backward", "sgd_step", "adpsgd_mix",
+    "muon_orthogonalize_scratch_bytes", "muon_orthogonalize", "muon_matrices_step", "muon_scratch_bytes", "muon_step",
     "sgd_mix_pair", "sync_average", "blstm_lr_schedule",
     "adpsgd_ring_partner", "blstm_shadow_refresh", "blstm_set_option", "blstm_weights_changed", "blstm_device_status", "blstm_profile_enable", "blstm_profile_read",
     "blstm_profile_classes", "blstm_profile_name", "blstm_last_error",
@@ -85,6 +87,16 @@ def lib():
     L.blstm_backward.restype = c_int
     L.sgd_step.argtypes = [c_void_p, c_void_p, c_void_p, c_size_t, c_float, c_float, c_void_p, c_void_p]
     L.sgd_step.restype = c_int
+    L.muon_orthogonalize_scratch_bytes.argtypes = [c_int] * 4
+    L.muon_orthogonalize_scratch_bytes.restype = c_size_t
+    L.muon_orthogonalize.argtypes = [c_void_p] * 2 + [c_int] * 4 + [c_void_p, c_size_t, c_void_p]
+    L.muon_orthogonalize.restype = c_int
+    L.muon_matrices_step.argtypes = [c_void_p] * 4 + [c_int] * 4 + [c_float] * 3 + [c_int, c_void_p, c_size_t, c_void_p]
+    L.muon_matrices_step.restype = c_int
+    L.muon_scratch_bytes.argtypes = [c_void_p, c_int]
+    L.muon_scratch_bytes.restype = c_size_t
+    L.muon_step.argtypes = [c_void_p] * 5 + [c_float] * 4 + [c_int, c_void_p, c_size_t, c_void_p]
+    L.muon_step.restype = c_int
     L.adpsgd_mix.argtypes = [POINTER(c_void_p), POINTER(c_void_p), c_size_t, c_int, POINTER(c_int32), c_void_p]
     L.adpsgd_mix.restype = c_int
     L.sgd_mix_pair.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_float, c_float,
@@ -238,6 +250,36 @@ def blstm_backward(ctx, theta, x, dz, grad, stream=None):
 def sgd_step(theta_master, theta_bf16_or_null, grad, n, lr, momentum=0.0, velocity_or_null=None, stream=None):
     return _check(lib().sgd_step(_ptr(theta_master), _ptr(theta_bf16_or_null), _ptr(grad), n, lr, momentum,
                                  _ptr(velocity_or_null), _stream(stream)))
+
+
+def _bytes(n):
+    if n == 0:
+        raise BlstmError(-2, blstm_last_error())
+    return int(n)
+
+
+def muon_orthogonalize_scratch_bytes(count, rows, cols, mode):
+    return _bytes(lib().muon_orthogonalize_scratch_bytes(count, rows, cols, mode))
+
+
+def muon_orthogonalize(G, X, count, rows, cols, mode, scratch, scratch_bytes=None, stream=None):
+    return _check(lib().muon_orthogonalize(_ptr(G), _ptr(X), count, rows, cols, mode, *_scratch(scratch, scratch_bytes), _stream(stream)))
+
+
+def muon_matrices_step(theta_master, theta_bf16_or_null, grad, velocity_or_null, count, rows, cols, mode, lr, momentum, weight_decay, flags, scratch,
+                       scratch_bytes=None, stream=None):
+    return _check(lib().muon_matrices_step(_ptr(theta_master), _ptr(theta_bf16_or_null), _ptr(grad), _ptr(velocity_or_null), count, rows, cols, mode,
+                                           lr, momentum, weight_decay, flags, *_scratch(scratch, scratch_bytes), _stream(stream)))
+
+
+def muon_scratch_bytes(ctx, flags=0):
+    return _bytes(lib().muon_scratch_bytes(ctx, flags))
+
+
+def muon_step(ctx, theta_master, theta_bf16_or_null, grad, velocity_or_null, lr, lr_rest, momentum, weight_decay, flags, scratch, scratch_bytes=None,
+              stream=None):
+    return _check(lib().muon_step(ctx, _ptr(theta_master), _ptr(theta_bf16_or_null), _ptr(grad), _ptr(velocity_or_null), lr, lr_rest, momentum,
+                                  weight_decay, flags, *_scratch(scratch, scratch_bytes), _stream(stream)))
 
 
 def adpsgd_mix(theta_master, theta_bf16_or_null, n, R, partner, stream=None):

@@ -17,6 +17,7 @@
 #include "gemm.hpp"
 #include "kernels.hpp"
 #include "losses.hpp"
+#include "muon.hpp"
 #include "xcd.hpp"
 
 using namespace blstm;
@@ -775,6 +776,55 @@ int loss_run(blstm_ctx* ctx, const LossCall& given, const int32_t* labels, const
 
 // What softmax_xent_fwd_bwd left to the next blstm_backward is written by the call itself.  (Calls of several threads share the context: where
 // nothing is pending, they only read it.)
+// ---- the orthogonalised update ---------------------------------------------------------------------------------------
+// The flat vector as groups of tensors of one shape at constant distances (layers beyond the first are alike).
+bool muon_model_plan(const blstm_ctx* c, int flags, MuonPlan* plan) {
+    MuonGroup g[MUON_MAX_GROUPS];
+    int n = 0;
+    auto add = [&](size_t at, long long outer, int parts, int count, int rows, int cols, bool ortho) {
+        MuonGroup q{};
+        q.at = (long long)at; q.outer = outer; q.inner_count = parts; q.inner = (long long)rows * cols;
+        q.count = count * parts; q.rows = rows; q.cols = cols; q.ortho = ortho;
+        g[n++] = q;
+    };
+    const int H = c->H, parts = flags & MUON_GATES ? 4 : 1;
+    for (int first = 0; first < 2; ++first) {             // layer 0, then the others
+        const int layers = first == 0 ? 1 : c->L - 1;
+        if (layers == 0) break;
+        const long long dist = (long long)c->off_wx[1][first] - (long long)c->off_wx[0][first];
+        add(c->off_wx[0][first], dist, parts, 2 * layers, 4 * H / parts, c->din(first), true);
+        add(c->off_uh[0][first], dist, parts, 2 * layers, 4 * H / parts, H, true);
+        add(c->off_b[0][first], dist, 1, 2 * layers, 4 * H, 1, false);
+    }
+    if (c->P > 0) {
+        add(c->off_wp, 0, 1, 1, c->P, 2 * H, true);
+        add(c->off_bp, 0, 1, 1, c->P, 1, false);
+    }
+    add(c->off_ws, 0, 1, 1, c->V, c->zdim, (flags & MUON_SOFTMAX) != 0);
+    add(c->off_bs, 0, 1, 1, c->V, 1, false);
+    return muon_plan(g, n, c->st == DT_F32, plan);
+}
+
+int muon_matrices_plan(const char* name, int count, int rows, int cols, int mode, MuonPlan* plan) {
+    if (count < 1 || rows < 1 || cols < 1 || (mode != 0 && mode != 1)) return fail(BLSTM_ERR_DIM, "%s: count, rows and cols must be positive, mode 0 or 1", name);
+    MuonGroup q{};
+    q.inner_count = count; q.inner = (long long)rows * cols;
+    q.count = count; q.rows = rows; q.cols = cols; q.ortho = true;
+    if ((long long)rows * cols > (1LL << 40) / count || !muon_plan(&q, 1, mode == 0, plan)) return fail(BLSTM_ERR_DIM, "%s: too many elements", name);
+    return BLSTM_OK;
+}
+
+int muon_check(const char* name, const MuonArgs& a, int flags, int known, const MuonPlan& plan, const void* scratch, size_t scratch_bytes) {
+    if (!a.theta || !a.grad || !scratch) return fail(BLSTM_ERR_NULL, "%s: null argument", name);
+    if (!(a.momentum >= 0.0f && a.momentum < 1.0f) || !(a.decay >= 0.0f)) return fail(BLSTM_ERR_DIM, "%s: momentum must be in [0, 1), weight_decay >= 0", name);
+    if (flags & ~known) return fail(BLSTM_ERR_DIM, "%s: unknown flags 0x%x", name, (unsigned)(flags & ~known));
+    if (a.momentum != 0.0f && !a.velocity) return fail(BLSTM_ERR_NULL, "%s: momentum needs a velocity buffer", name);
+    if (!aligned16(a.theta) || !aligned16(a.grad) || !aligned16(scratch) || (a.shadow && !aligned16(a.shadow)) || (a.velocity && !aligned16(a.velocity)))
+        return fail(BLSTM_ERR_ALIGN, "%s: pointers must be 16-byte aligned", name);
+    if (scratch_bytes < plan.bytes) return fail(BLSTM_ERR_WORKSPACE, "%s: %zu bytes of scratch given, %zu needed", name, scratch_bytes, plan.bytes);
+    return BLSTM_OK;
+}
+
 void drop_deferred(blstm_ctx* ctx) {
     if (ctx->pend_z) ctx->pend_z = nullptr;
     if (ctx->twin && ctx->twin->pend_z) ctx->twin->pend_z = nullptr;
@@ -1466,6 +1516,51 @@ int sgd_step(float* theta, void* shadow, const float* grad, size_t n, float lr, 
         return fail(BLSTM_ERR_ALIGN, "sgd_step: pointers must be 16-byte aligned");
     return check_hip(launch_sgd(theta, static_cast<unsigned short*>(shadow), grad, n, lr, momentum, velocity,
                                 static_cast<hipStream_t>(stream)), "sgd_step");
+}
+
+size_t muon_scratch_bytes(const blstm_ctx* ctx, int flags) {
+    MuonPlan p;
+    if (!ctx) { fail(BLSTM_ERR_NULL, "muon_scratch_bytes: null argument"); return 0; }
+    if (flags & ~(MUON_NESTEROV | MUON_GATES | MUON_SOFTMAX)) { fail(BLSTM_ERR_DIM, "muon_scratch_bytes: unknown flags"); return 0; }
+    if (!muon_model_plan(ctx, flags, &p)) { fail(BLSTM_ERR_DIM, "muon_scratch_bytes: too many elements"); return 0; }
+    return p.bytes;
+}
+
+int muon_step(const blstm_ctx* ctx, float* theta, void* shadow, const float* grad, float* velocity, float lr, float lr_rest, float momentum,
+              float weight_decay, int flags, void* scratch, size_t scratch_bytes, void* stream) {
+    if (!ctx) return fail(BLSTM_ERR_NULL, "muon_step: null argument");
+    MuonPlan p;
+    if (!muon_model_plan(ctx, flags, &p)) return fail(BLSTM_ERR_DIM, "muon_step: too many elements");
+    const MuonArgs a{theta, static_cast<unsigned short*>(shadow), grad, momentum != 0.0f ? velocity : nullptr, nullptr, 0, lr, lr_rest, momentum, weight_decay, (flags & MUON_NESTEROV) != 0};
+    const int rc = muon_check("muon_step", a, flags, MUON_NESTEROV | MUON_GATES | MUON_SOFTMAX, p, scratch, scratch_bytes);
+    return rc != BLSTM_OK ? rc : check_hip(launch_muon(p, a, scratch, static_cast<hipStream_t>(stream)), "muon_step");
+}
+
+size_t muon_orthogonalize_scratch_bytes(int count, int rows, int cols, int mode) {
+    MuonPlan p;
+    return muon_matrices_plan("muon_orthogonalize_scratch_bytes", count, rows, cols, mode, &p) == BLSTM_OK ? p.bytes : 0;
+}
+
+int muon_orthogonalize(const float* G, void* X, int count, int rows, int cols, int mode, void* scratch, size_t scratch_bytes, void* stream) {
+    MuonPlan p;
+    const int rc = muon_matrices_plan("muon_orthogonalize", count, rows, cols, mode, &p);
+    if (rc != BLSTM_OK) return rc;
+    if (!G || !X || !scratch) return fail(BLSTM_ERR_NULL, "muon_orthogonalize: null argument");
+    if (!aligned16(G) || !aligned16(X) || !aligned16(scratch)) return fail(BLSTM_ERR_ALIGN, "muon_orthogonalize: pointers must be 16-byte aligned");
+    if (scratch_bytes < p.bytes) return fail(BLSTM_ERR_WORKSPACE, "muon_orthogonalize: %zu bytes of scratch given, %zu needed", scratch_bytes, p.bytes);
+    MuonArgs a{};
+    a.grad = G; a.out = X; a.out_bf16 = mode;
+    return check_hip(launch_muon(p, a, scratch, static_cast<hipStream_t>(stream)), "muon_orthogonalize");
+}
+
+int muon_matrices_step(float* theta, void* shadow, const float* grad, float* velocity, int count, int rows, int cols, int mode, float lr, float momentum,
+                       float weight_decay, int flags, void* scratch, size_t scratch_bytes, void* stream) {
+    MuonPlan p;
+    int rc = muon_matrices_plan("muon_matrices_step", count, rows, cols, mode, &p);
+    if (rc != BLSTM_OK) return rc;
+    const MuonArgs a{theta, static_cast<unsigned short*>(shadow), grad, momentum != 0.0f ? velocity : nullptr, nullptr, 0, lr, 0.0f, momentum, weight_decay, (flags & MUON_NESTEROV) != 0};
+    rc = muon_check("muon_matrices_step", a, flags, MUON_NESTEROV, p, scratch, scratch_bytes);
+    return rc != BLSTM_OK ? rc : check_hip(launch_muon(p, a, scratch, static_cast<hipStream_t>(stream)), "muon_matrices_step");
 }
 
 int adpsgd_mix(float* const* theta, void* const* shadow, size_t n, int R, const int32_t* partner, void* stream) {

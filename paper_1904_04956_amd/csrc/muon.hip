@@ -1,0 +1,619 @@
+// The orthogonalised update.  Of a matrix d (a momentum) with m rows and n columns, m <= n (or the other way round: columns and rows change places):
+//   X <- d / |d|_F,  then five times  S = X X^T,  B = b S + c S^2,  X <- a X + B X      (a, b, c) = (3.4445, -4.7750, 2.0315)
+// which keeps the singular vectors and takes every singular value s to a s + b s^3 + c s^5: in five steps what is not tiny lands in 0.7 .. 1.2.
+//
+// Numbers.  Everything that a product reads is a half (the matrix cores' rate is that of bf16, with three more bits) times 2^8, which keeps the
+// entries of a normalised matrix, 1/sqrt(m n), and what their rounding leaves over away from the subnormals; none exceeds 2^8 for X and S and
+// about 2^12 for B.  Products accumulate in float.  X itself is kept as the sum of two halves (22 bits): a rounding of X adds noise in all
+// directions alike, and where a few directions hold most of |d| (gradients do) that noise is as large as the others; the step's other
+// roundings pass through B X, which is small where the singular value is.  So mode 1 multiplies by the first half only and adds a X from both: off by
+// about 3e-4 of X.  Mode 0 multiplies both halves (three products): off by about 1e-6.
+// The diagonals of S and B, which near the end are most of them, stay out of the halves and the products, in float: with D the diagonal and R the rest,
+// S^2 = D^2 + D R + R D + R^2, and B X = D X + R X (rounded with the rest they alone put X off by 2e-3).
+// The Frobenius norm is summed in double (squares of floats leave float's range) in a fixed order.
+//
+// S and B are symmetric: tiles on and above the diagonal are computed, and stored twice.
+#include "gemm_tile.hpp"
+#include "muon.hpp"
+#include <algorithm>
+
+namespace blstm {
+namespace {
+
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+
+constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
+constexpr int NS_STEPS = 5;
+constexpr float UP = 256.0f, DOWN = 1.0f / 256.0f;      // what lies in scratch is 2^8 times its value
+constexpr int FLAT = 8192;                              // elements of a unit of the flat passes
+constexpr int CAST = 4096;
+
+enum { PH_GRAM = 0, PH_SQUARE = 1, PH_APPLY = 2, PH_LAST = 3 };
+
+template <typename F>
+__device__ __forceinline__ int group_of(const MuonPlan& p, int id, F&& first) {      // the last group that starts at or before id (empty ones share a start)
+    int k = 0;
+    for (int i = 1; i < p.n; ++i) if (id >= first(p.g[i])) k = i;
+    return __builtin_amdgcn_readfirstlane(k);
+}
+// (the same in every lane: said for the scalar operand of a load)
+__device__ __forceinline__ const char* uniform(const void* p) {
+    const unsigned long long v = (unsigned long long)p;
+    return reinterpret_cast<const char*>((unsigned long long)__builtin_amdgcn_readfirstlane((unsigned)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((unsigned)v));
+}
+__device__ __forceinline__ long long tensor_at(const MuonGroup& g, int k) { return g.at + (long long)(k / g.inner_count) * g.outer + (long long)(k % g.inner_count) * g.inner; }
+
+// ---- v <- momentum v + g, the squares' sums, and the whole update of what is not orthogonalised ----------------------
+// 12 bytes an element of a matrix, 20 (22 with the bf16 copy) of the others.
+__device__ __forceinline__ double block_sum(double v, double* lds) {
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return lds[0] + lds[1] + lds[2] + lds[3];
+}
+__global__ __launch_bounds__(256) void muon_momentum_kernel(MuonPlan p, MuonArgs a, double* sums) {
+    __shared__ double lds[4];
+    const MuonGroup& g = p.g[group_of(p, blockIdx.x, [](const MuonGroup& x) { return x.chunk0; })];
+    const int local = blockIdx.x - g.chunk0, k = local / g.chunks, c = local % g.chunks;
+    const long long size = (long long)g.rows * g.cols, e0 = (long long)c * FLAT, at = tensor_at(g, k) + e0;
+    const int len = (int)min((long long)FLAT, size - e0);
+    const float* grad = a.grad + at;
+    float* vel = a.velocity ? a.velocity + at : nullptr;
+    float* theta = a.theta ? a.theta + at : nullptr;
+    unsigned short* shadow = a.shadow ? a.shadow + at : nullptr;
+    const bool step = !g.ortho;
+    double sum = 0.0;
+    auto one = [&](float gr, float& v) {              // the update's direction; v becomes the new velocity
+        if (!vel) return gr;
+        v = a.momentum * v + gr;
+        return a.nesterov ? gr + a.momentum * v : v;
+    };
+    const int head = (int)min((long long)((4 - (at & 3)) & 3), (long long)len), words = (len - head) / 4;
+#pragma unroll 2
+    for (int i = threadIdx.x; i < words; i += 256) {
+        const int o = head + 4 * i;
+        const f32x4_t gr = *reinterpret_cast<const f32x4_t*>(grad + o);
+        f32x4_t v = vel ? *reinterpret_cast<const f32x4_t*>(vel + o) : gr, d, w;
+        if (step) w = *reinterpret_cast<const f32x4_t*>(theta + o);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { float x = v[e]; d[e] = one(gr[e], x); v[e] = x; }
+        if (vel) *reinterpret_cast<f32x4_t*>(vel + o) = v;
+        if (step) {
+            w = w - a.lr_rest * d;
+            *reinterpret_cast<f32x4_t*>(theta + o) = w;
+            if (shadow) { u32x2_t q; q[0] = pack_bf2(w[0], w[1]); q[1] = pack_bf2(w[2], w[3]); *reinterpret_cast<u32x2_t*>(shadow + o) = q; }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += (double)d[e] * d[e];
+        }
+    }
+    // (what lies before the first and behind the last whole word)
+    const int rest = len - 4 * words;
+    if ((int)threadIdx.x < rest) {
+        const int o = (int)threadIdx.x < head ? threadIdx.x : threadIdx.x + 4 * words;
+        float v = vel ? vel[o] : 0.0f;
+        const float d = one(grad[o], v);
+        if (vel) vel[o] = v;
+        if (step) {
+            const float w = theta[o] - a.lr_rest * d;
+            theta[o] = w;
+            if (shadow) shadow[o] = f2bf(w);
+        } else sum += (double)d * d;
+    }
+    if (!step) {
+        const double all = block_sum(sum, lds);
+        if (threadIdx.x == 0) sums[blockIdx.x] = all;
+    }
+}
+
+// ---- d / |d|_F as two halves, zero-padded ---------------------------------------------------------------------------
+__device__ __forceinline__ void put_halves(_Float16* hi, _Float16* lo, const float (&v)[8]) {
+    f16x8_t h, l;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { h[e] = (_Float16)v[e]; l[e] = (_Float16)(v[e] - (float)h[e]); }
+    *reinterpret_cast<f16x8_t*>(hi) = h;
+    if (lo) *reinterpret_cast<f16x8_t*>(lo) = l;
+}
+__global__ __launch_bounds__(256) void muon_cast_kernel(MuonPlan p, MuonArgs a, const double* sums, _Float16* ws) {
+    __shared__ double lds[4];
+    const MuonGroup& g = p.g[group_of(p, blockIdx.x, [](const MuonGroup& x) { return x.cast0; })];
+    const int local = blockIdx.x - g.cast0, k = local / g.casts, c = local % g.casts;
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < g.chunks; i += 256) sum += sums[g.chunk0 + k * g.chunks + i];
+    const double norm2 = block_sum(sum, lds);
+    // (a zero matrix stays one; an infinity or NaN anywhere makes all of it NaN)
+    const double scale = norm2 == 0.0 ? 0.0 : UP / sqrt(norm2);
+    const float whole = norm2 <= 1.7e308 ? 0.0f : __builtin_nanf("");
+    const long long at = tensor_at(g, k);
+    _Float16* x = ws + g.x[0] + (long long)k * g.rp * g.cp;
+    const bool vec = (at & 3) == 0 && (g.cols & 3) == 0;
+#pragma unroll
+    for (int q = 0; q < CAST / 2048; ++q) {
+        const long long e = (long long)c * CAST + q * 2048 + threadIdx.x * 8;
+        const int r = (int)(e / g.cp), c0 = (int)(e % g.cp);
+        float d[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) d[j] = 0.0f;
+        if (r < g.rows) {
+            const long long o = at + (long long)r * g.cols + c0;
+            const int n = min(8, g.cols - c0);
+            float gr[8], v[8];
+            if (vec) {
+#pragma unroll
+                for (int w = 0; w < 2; ++w) if (4 * w < n) {
+                    const f32x4_t y = *reinterpret_cast<const f32x4_t*>(a.grad + o + 4 * w);
+                    const f32x4_t z = a.velocity ? *reinterpret_cast<const f32x4_t*>(a.velocity + o + 4 * w) : y;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) { gr[4 * w + j] = y[j]; v[4 * w + j] = z[j]; }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) if (j < n) { gr[j] = a.grad[o + j]; v[j] = a.velocity ? a.velocity[o + j] : 0.0f; }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) if (j < n) {
+                const float f = !a.velocity ? gr[j] : a.nesterov ? gr[j] + a.momentum * v[j] : v[j];
+                d[j] = (float)(f * scale) + whole;
+            }
+        }
+        put_halves(x + e, x + g.xplane + e, d);
+    }
+}
+
+// ---- the products ---------------------------------------------------------------------------------------------------
+// One tile of sum_k A(row, k) B(col, k), 64 TM x 64 TN, on 2 x 2 wavefronts.  A slab of 64 k is brought to LDS by global_load_lds: an operand whose
+// k is fast in memory as rows of eight 16-byte chunks, one whose k is slow as it lies in memory, to be transposed by the LDS read (layouts and
+// swizzles: gemm_tile.hpp).  Two buffers: the next slab's loads run while this one is multiplied.  ONE buffer: a slab's fragments are all read into registers,
+// the next slab's loads go out behind a barrier and the products run from registers; two workgroups a CU take turns.
+struct NsOperand { const _Float16* p; long long ld, plane; };      // tile origin; elements to the second halves
+
+template <int TM, int TN, bool SPLIT, bool AS, bool BS, bool ONE>
+__device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand& A, const NsOperand& B, int slab0, int slab1, uint4* smem) {
+    static_assert(!ONE || !SPLIT, "the registers hold one plane's fragments");
+    constexpr int BM = 64 * TM, BN = 64 * TN, PL = SPLIT ? 2 : 1, PA = BM * 8, PB = BN * 8, STAGE = PL * (PA + PB);   // (in 16-byte words)
+    constexpr int NIA = 2 * TM, NIB = 2 * TN, CPA = BM / 8, CPB = BN / 8;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv >> 1, wn = wv & 1;
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
+    unsigned voa[NIA], vob[NIB];
+    auto place = [&](auto cpr, bool slow, int j, long long ld) {
+        constexpr int CPR = decltype(cpr)::value;
+        const int jj = 4 * j + wv, kt = (64 / CPR) * jj + lane / CPR, pos = lane % CPR, r = 8 * jj + (lane >> 3);
+        const int mc = (((pos >> 1) ^ tr_swz<CPR>(kt)) << 1) | (pos & 1), kc = (lane & 7) ^ swz(r);
+        return slow ? (unsigned)(kt * ld * 2 + mc * 16) : (unsigned)(r * ld * 2 + kc * 16);
+    };
+#pragma unroll
+    for (int j = 0; j < NIA; ++j) voa[j] = place(std::integral_constant<int, (CPA < 64 ? CPA : 64)>{}, AS, j, A.ld);
+#pragma unroll
+    for (int j = 0; j < NIB; ++j) vob[j] = place(std::integral_constant<int, (CPB < 64 ? CPB : 64)>{}, BS, j, B.ld);
+    auto dma = [](unsigned lds_addr, const char* gbase, unsigned voff) __attribute__((always_inline)) {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(voff), "s"(gbase) : "memory");
+    };
+    auto issue = [&](int it) __attribute__((always_inline)) {
+        const char* pa = uniform(A.p + (AS ? (long long)it * 64 * A.ld : (long long)it * 64));
+        const char* pb = uniform(B.p + (BS ? (long long)it * 64 * B.ld : (long long)it * 64));
+        const unsigned sb = lds0 + (ONE ? 0u : (unsigned)(((it - slab0) & 1) * STAGE * 16));
+#pragma unroll
+        for (int pl = 0; pl < PL; ++pl) {
+#pragma unroll
+            for (int j = 0; j < NIA; ++j) dma(sb + (unsigned)(pl * PA * 16 + (4 * j + wv) * 1024), pl ? uniform(pa + A.plane * 2) : pa, voa[j]);
+#pragma unroll
+            for (int j = 0; j < NIB; ++j) dma(sb + (unsigned)((PL * PA + pl * PB) * 16 + (4 * j + wv) * 1024), pl ? uniform(pb + B.plane * 2) : pb, vob[j]);
+        }
+    };
+    // fragment reads: lane l holds k = 8 (l / 32) .. of row l % 32 of its 32-row block
+    const int arow = wm * 32 * TM + (lane & 31), brow = wn * 32 * TN + (lane & 31);
+    int ra[4], rb[4], ta[TM], tb[TN];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        ra[q] = arow * CHUNKS + ((2 * q + (lane >> 5)) ^ swz(arow));
+        rb[q] = brow * CHUNKS + ((2 * q + (lane >> 5)) ^ swz(brow));
+    }
+    {
+        const int g = lane >> 4, li = lane & 15;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+            ta[i] = (8 * (g >> 1) + (li >> 2)) * (BM * 2) + (((wm * 2 * TM + 2 * i + (g & 1)) ^ tr_swz<CPA>(li >> 2)) << 5) + (li & 3) * 8;
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+            tb[i] = (8 * (g >> 1) + (li >> 2)) * (BN * 2) + (((wn * 2 * TN + 2 * i + (g & 1)) ^ tr_swz<CPB>(li >> 2)) << 5) + (li & 3) * 8;
+    }
+    auto frag_a = [&](const uint4* s, int i, int q) __attribute__((always_inline)) {
+        if constexpr (AS) return lfrag_tr<BM * 2>(reinterpret_cast<const char*>(s) + ta[i], 16 * q);
+        else return s[ra[(i & 1) ? (q ^ 2) : q] + i * 32 * CHUNKS];
+    };
+    auto frag_b = [&](const uint4* s, int i, int q) __attribute__((always_inline)) {
+        if constexpr (BS) return lfrag_tr<BN * 2>(reinterpret_cast<const char*>(s) + tb[i], 16 * q);
+        else return s[rb[(i & 1) ? (q ^ 2) : q] + i * 32 * CHUNKS];
+    };
+    auto mma = [&](const uint4 (&x)[TM], const uint4 (&y)[TN]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, x[i]), __builtin_bit_cast(f16x8_t, y[j]), acc[i][j], 0, 0, 0);
+    };
+    if (slab0 < slab1) issue(slab0);
+    if constexpr (ONE) {
+        uint4 fa[4][TM], fb[4][TN];
+        for (int it = slab0; it < slab1; ++it) {
+            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+#pragma unroll
+                for (int i = 0; i < TM; ++i) fa[q][i] = frag_a(smem, i, q);
+#pragma unroll
+                for (int i = 0; i < TN; ++i) fb[q][i] = frag_b(smem + PA, i, q);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if (it + 1 < slab1) issue(it + 1);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) mma(fa[q], fb[q]);
+        }
+    } else {
+        for (int it = slab0; it < slab1; ++it) {
+            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+            if (it + 1 < slab1) issue(it + 1);
+            const uint4* sa = smem + ((it - slab0) & 1) * STAGE;
+            const uint4* sb = sa + PL * PA;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                uint4 af[PL][TM], bf[PL][TN];
+#pragma unroll
+                for (int pl = 0; pl < PL; ++pl) {
+#pragma unroll
+                    for (int i = 0; i < TM; ++i) af[pl][i] = frag_a(sa + pl * PA, i, q);
+#pragma unroll
+                    for (int i = 0; i < TN; ++i) bf[pl][i] = frag_b(sb + pl * PB, i, q);
+                }
+                if constexpr (SPLIT) { mma(af[1], bf[0]); mma(af[0], bf[1]); }
+                mma(af[0], bf[0]);
+            }
+        }
+    }
+    __syncthreads();                                        // the epilogue reuses the buffers
+}
+
+// The tile's values, eight of a row at a time, each wavefront its own part through its own stretch of LDS, whose reads are conflict-free along
+// rows and columns.  What an element is combined with is loaded for a whole block of 32 rows before the first store (stores and loads in turn are a round trip
+// each): load(row, column) -> aux; f(row, column, values, aux) changes the values and stores them; mirror(row, column, values) gets the same
+// values of the transposed tile (`twice`).
+template <int TM, int TN, typename L, typename F, typename G>
+__device__ __forceinline__ void ns_values(const f32x16_t (&acc)[TM][TN], uint4* smem, bool twice, L&& load, F&& f, G&& mirror) {
+    constexpr int LD = 32 * TN + 4, NQ = 2 * TN;
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, wm = wv >> 1, wn = wv & 1;
+    float* s = reinterpret_cast<float*>(smem) + wv * 32 * LD;
+    const int col0 = wn * 32 * TN;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int row0 = wm * 32 * TM + 32 * i;
+        decltype(load(0, 0)) aux[NQ];
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) { const int c = lane + 64 * q; aux[q] = load(row0 + c / (4 * TN), col0 + c % (4 * TN) * 8); }
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[(8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)) * LD + 32 * j + (lane & 31)] = acc[i][j][e];
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            const int c = lane + 64 * q, r = c / (4 * TN), c0 = c % (4 * TN) * 8;
+            f32x4_t* at = reinterpret_cast<f32x4_t*>(s + r * LD + c0);
+            const f32x4_t x = at[0], y = at[1];
+            float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+            f(row0 + r, col0 + c0, v, aux[q]);
+            if (twice) { at[0] = f32x4_t{v[0], v[1], v[2], v[3]}; at[1] = f32x4_t{v[4], v[5], v[6], v[7]}; }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (twice) {
+            // 32 TN columns of 32 rows, a column's eight rows a lane
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) {
+                const int c = lane + 64 * q, col = c % (32 * TN), r0 = c / (32 * TN) * 8;
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = s[(r0 + e) * LD + col];
+                mirror(col0 + col, row0 + r0, v);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+    }
+}
+struct Halves { f16x8_t h, l; f32x4_t d0, d1; float di; };
+
+// tile number t of those on and above the diagonal, column by column: row <= column
+__device__ __forceinline__ void upper(int t, int* row, int* col) {
+    int c = 0;
+    while (t > c) { t -= c + 1; ++c; }
+    *row = t; *col = c;
+}
+
+template <int TM, int TN, bool SPLIT, int PH, bool ONE>
+__global__ __launch_bounds__(256, SPLIT && TM == 2 ? 1 : 2) void ns_product_kernel(MuonPlan p, MuonArgs a, _Float16* ws, float* diag, float* part, int from) {
+    extern __shared__ uint4 smem[];
+    constexpr int BM = 64 * TM, BN = 64 * TN;
+    // ids go round-robin to the eight XCDs: each takes a contiguous range of tiles
+    int lin = blockIdx.x;
+    const int n8 = gridDim.x & ~7;
+    if (lin < n8) lin = (lin & 7) * (n8 >> 3) + (lin >> 3);
+    const MuonGroup& g = p.g[group_of(p, lin, [](const MuonGroup& x) { return PH == PH_GRAM ? x.gram0 : PH == PH_SQUARE ? x.square0 : x.apply0; })];
+    f32x16_t acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    if constexpr (PH == PH_GRAM || PH == PH_SQUARE) {
+        static_assert(TM == TN, "tiles on the diagonal are squares");
+        int local = lin - (PH == PH_GRAM ? g.gram0 : g.square0), split = 0;
+        if (PH == PH_GRAM) { split = local % g.splits; local /= g.splits; }
+        const int k = local / g.grams;
+        int tr, tc;
+        upper(local % g.grams, &tr, &tc);
+        _Float16* s = ws + g.s + (long long)k * g.mp * g.mp;
+        float* sd = diag + g.diag + (long long)k * g.mp;
+        float* bd = sd + (long long)g.count * g.mp;
+        _Float16* out = PH == PH_GRAM ? s : ws + g.b + (long long)k * g.mp * g.mp;
+        auto mirror = [&](int r, int c, const float (&v)[8]) {
+            const long long o = (long long)(tc * BM + r) * g.mp + tr * BM + c;
+            put_halves(out + o, SPLIT ? out + g.splane + o : nullptr, v);
+        };
+        if constexpr (PH == PH_GRAM) {
+            const _Float16* x = ws + g.x[from] + (long long)k * g.rp * g.cp;
+            const int slabs = (g.tall ? g.rp : g.cp) / 64, per = (slabs + g.splits - 1) / g.splits;
+            const int s0 = min(slabs, split * per), s1 = min(slabs, s0 + per);
+            if (g.tall) ns_tile<TM, TN, SPLIT, true, true, ONE>(acc, {x + tr * BM, g.cp, g.xplane}, {x + tc * BM, g.cp, g.xplane}, s0, s1, smem);
+            else ns_tile<TM, TN, SPLIT, false, false, ONE>(acc, {x + (long long)tr * BM * g.cp, g.cp, g.xplane}, {x + (long long)tc * BM * g.cp, g.cp, g.xplane}, s0, s1, smem);
+            const bool whole = g.splits == 1;
+            float* sum = part + g.part + ((long long)local * g.splits + split) * BM * BM;
+            ns_values(acc, smem, whole && tr != tc, [](int, int) { return 0; }, [&](int r, int c, float (&v)[8], int) {
+                if (!whole) {
+                    *reinterpret_cast<f32x4_t*>(sum + r * BM + c) = f32x4_t{v[0], v[1], v[2], v[3]};
+                    *reinterpret_cast<f32x4_t*>(sum + r * BM + c + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
+                    return;
+                }
+                const int row = tr * BM + r, col = tc * BM + c, on = row - col;
+                const long long o = (long long)row * g.mp + col;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[e] *= DOWN;
+                    if (on == e) { sd[row] = DOWN * v[e]; v[e] = 0.0f; }
+                }
+                put_halves(out + o, SPLIT ? out + g.splane + o : nullptr, v);
+            }, mirror);
+        } else {
+            const NsOperand A{s + (long long)tr * BM * g.mp, g.mp, g.splane}, B{s + (long long)tc * BM * g.mp, g.mp, g.splane};
+            ns_tile<TM, TN, SPLIT, false, false, ONE>(acc, A, B, 0, g.mp / 64, smem);
+            ns_values(acc, smem, tr != tc, [&](int r, int c) {
+                const int row = tr * BM + r, col = tc * BM + c;
+                const _Float16* at = s + (long long)row * g.mp + col;
+                Halves x;
+                x.h = *reinterpret_cast<const f16x8_t*>(at);
+                if constexpr (SPLIT) x.l = *reinterpret_cast<const f16x8_t*>(at + g.splane); else x.l = f16x8_t{};
+                x.di = sd[row];
+                x.d0 = *reinterpret_cast<const f32x4_t*>(sd + col);
+                x.d1 = *reinterpret_cast<const f32x4_t*>(sd + col + 4);
+                return x;
+            }, [&](int r, int c, float (&v)[8], const Halves& x) {
+                const int row = tr * BM + r, col = tc * BM + c, on = row - col;
+                const long long o = (long long)row * g.mp + col;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float y = (float)x.h[e] + (float)x.l[e], full = NS_C * DOWN * v[e];
+                    if (on == e) bd[row] = NS_B * x.di + NS_C * x.di * x.di + DOWN * full;
+                    v[e] = on == e ? 0.0f : NS_B * y + NS_C * (x.di + (e < 4 ? x.d0[e & 3] : x.d1[e & 3])) * y + full;
+                }
+                put_halves(out + o, SPLIT ? out + g.splane + o : nullptr, v);
+            }, mirror);
+        }
+    } else {
+        const int local = lin - g.apply0, k = local / g.applies, t = local % g.applies, nc = g.cp / BN;
+        const int tr = t / nc, tc = t % nc;
+        const _Float16* x = ws + g.x[from] + (long long)k * g.rp * g.cp;
+        const _Float16* b = ws + g.b + (long long)k * g.mp * g.mp;
+        if (g.tall) ns_tile<TM, TN, SPLIT, false, false, ONE>(acc, {x + (long long)tr * BM * g.cp, g.cp, g.xplane}, {b + (long long)tc * BN * g.mp, g.mp, g.splane}, 0, g.mp / 64, smem);
+        else ns_tile<TM, TN, SPLIT, false, true, ONE>(acc, {b + (long long)tr * BM * g.mp, g.mp, g.splane}, {x + tc * BN, g.cp, g.xplane}, 0, g.mp / 64, smem);
+        _Float16* to = ws + g.x[from ^ 1] + (long long)k * g.rp * g.cp;
+        const long long at = tensor_at(g, k);
+        const float* bd = diag + g.diag + (long long)(g.count + k) * g.mp;
+        const float shrink = 1.0f - a.lr * a.decay, step = a.lr * sqrtf(fmaxf(1.0f, (float)g.rows / (float)g.cols)) * DOWN;
+        ns_values(acc, smem, false, [&](int r, int c) {
+            const int row = tr * BM + r, col = tc * BN + c;
+            const _Float16* y = x + (long long)row * g.cp + col;
+            Halves u;
+            u.h = *reinterpret_cast<const f16x8_t*>(y);
+            u.l = *reinterpret_cast<const f16x8_t*>(y + g.xplane);
+            if (g.tall) { u.d0 = *reinterpret_cast<const f32x4_t*>(bd + col); u.d1 = *reinterpret_cast<const f32x4_t*>(bd + col + 4); }
+            else { const float d = bd[row]; u.d0 = u.d1 = f32x4_t{d, d, d, d}; }
+            return u;
+        }, [&](int r, int c, float (&v)[8], const Halves& u) {
+            const int row = tr * BM + r, col = tc * BN + c;
+            const long long o = (long long)row * g.cp + col;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (NS_A + (e < 4 ? u.d0[e & 3] : u.d1[e & 3])) * ((float)u.h[e] + (float)u.l[e]) + DOWN * v[e];
+            if constexpr (PH == PH_APPLY) put_halves(to + o, to + g.xplane + o, v);
+            else {
+                if (row >= g.rows || col >= g.cols) return;
+                const long long q = at + (long long)row * g.cols + col;
+                const int n = min(8, g.cols - col);
+                if (a.theta) {
+                    if (n == 8 && (q & 3) == 0) {
+                        f32x4_t w[2];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) w[i] = *reinterpret_cast<const f32x4_t*>(a.theta + q + 4 * i);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) w[i][e] = shrink * w[i][e] - step * v[4 * i + e];
+                            *reinterpret_cast<f32x4_t*>(a.theta + q + 4 * i) = w[i];
+                            if (a.shadow) { u32x2_t z; z[0] = pack_bf2(w[i][0], w[i][1]); z[1] = pack_bf2(w[i][2], w[i][3]); *reinterpret_cast<u32x2_t*>(a.shadow + q + 4 * i) = z; }
+                        }
+                    } else {
+                        float w[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) w[e] = e < n ? a.theta[q + e] : 0.0f;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) if (e < n) {
+                            w[e] = shrink * w[e] - step * v[e];
+                            a.theta[q + e] = w[e];
+                            if (a.shadow) a.shadow[q + e] = f2bf(w[e]);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) if (e < n) {
+                        if (a.out_bf16) static_cast<unsigned short*>(a.out)[q + e] = f2bf(DOWN * v[e]);
+                        else static_cast<float*>(a.out)[q + e] = DOWN * v[e];
+                    }
+                }
+            }
+        }, [](int, int, const float (&)[8]) {});
+    }
+}
+
+// The parts of split Gram tiles, in order: 64 x 64 of a tile a workgroup.
+template <int T, bool SPLIT>
+__global__ __launch_bounds__(256) void ns_gram_sum_kernel(MuonPlan p, _Float16* ws, float* diag, const float* part) {
+    constexpr int BM = 64 * T, LD = 65;
+    __shared__ float s[64 * LD];
+    const MuonGroup& g = p.g[group_of(p, blockIdx.x, [](const MuonGroup& x) { return x.sum0; })];
+    const int local = blockIdx.x - g.sum0, tile = local / (T * T), sub = local % (T * T), k = tile / g.grams;
+    int tr, tc;
+    upper(tile % g.grams, &tr, &tc);
+    const int sr = sub / T * 64, sc = sub % T * 64;
+    const float* from = part + g.part + (long long)tile * g.splits * BM * BM;
+    const int r = threadIdx.x >> 2, c0 = (threadIdx.x & 3) * 16;
+    f32x4_t v[4] = {};
+    for (int i = 0; i < g.splits; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v[w] += *reinterpret_cast<const f32x4_t*>(from + (long long)i * BM * BM + (sr + r) * BM + sc + c0 + 4 * w);
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool own = tr == tc && sr + r == sc + c0 + 4 * w + e;
+            if (own) diag[g.diag + (long long)k * g.mp + tr * BM + sr + r] = DOWN * DOWN * v[w][e];
+            s[r * LD + c0 + 4 * w + e] = own ? 0.0f : DOWN * v[w][e];
+        }
+    __syncthreads();
+    _Float16* out = ws + g.s + (long long)k * g.mp * g.mp;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        float x[8];
+        const long long o = (long long)(tr * BM + sr + r) * g.mp + tc * BM + sc + c0 + 8 * w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = s[r * LD + c0 + 8 * w + e];
+        put_halves(out + o, SPLIT ? out + g.splane + o : nullptr, x);
+        if (tr == tc) continue;
+        const long long m = (long long)(tc * BM + sc + r) * g.mp + tr * BM + sr + c0 + 8 * w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = s[(c0 + 8 * w + e) * LD + r];
+        put_halves(out + m, SPLIT ? out + g.splane + m : nullptr, x);
+    }
+}
+
+constexpr int lds_bytes(int TM, int TN, bool split, bool one) {
+    const int loop = (one ? 1 : 2) * (split ? 2 : 1) * 64 * (TM + TN) * 128, values = 4 * 32 * (32 * TN + 4) * 4;
+    return loop > values ? loop : values;
+}
+template <int TM, int TN, bool SPLIT, int PH, bool ONE>
+void run_product(int n, const MuonPlan& p, const MuonArgs& a, _Float16* ws, float* diag, float* part, int from, hipStream_t st) {
+    ns_product_kernel<TM, TN, SPLIT, PH, ONE><<<n, 256, lds_bytes(TM, TN, SPLIT, ONE), st>>>(p, a, ws, diag, part, from);
+}
+
+// T: edge of the Gram and square tiles; AM, AN: of the last product's
+template <int T, int AM, int AN, bool SPLIT, bool ONE>
+hipError_t run_products(const MuonPlan& p, const MuonArgs& a, _Float16* ws, float* diag, float* part, hipStream_t st) {
+    for (int i = 0; i < NS_STEPS; ++i) {
+        const int from = i & 1;
+        run_product<T, T, SPLIT, PH_GRAM, false>(p.grams, p, a, ws, diag, part, from, st);
+        if (p.sums) ns_gram_sum_kernel<T, SPLIT><<<p.sums, 256, 0, st>>>(p, ws, diag, part);
+        run_product<T, T, SPLIT, PH_SQUARE, false>(p.squares, p, a, ws, diag, part, from, st);
+        if (i + 1 < NS_STEPS) run_product<AM, AN, SPLIT, PH_APPLY, ONE>(p.applies, p, a, ws, diag, part, from, st);
+        else run_product<AM, AN, SPLIT, PH_LAST, ONE>(p.applies, p, a, ws, diag, part, from, st);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
+    MuonPlan p{};
+    p.n = n;
+    p.exact = exact;
+    const long long most = 0x7FFFFFFF;
+    auto up = [](long long v, long long m) { return (v + m - 1) / m * m; };
+    auto tiles = [&](int high, int wide) {              // of the last product
+        long long t = 0;
+        for (int i = 0; i < n; ++i) if (g[i].ortho) t += (long long)g[i].count * ((g[i].rows + high - 1) / high) * ((g[i].cols + wide - 1) / wide);
+        return t;
+    };
+    p.tile = !exact && tiles(256, 128) >= 480 ? 2 : tiles(128, 128) >= 256 ? 1 : 0;
+    const int edge = p.tile ? 128 : 64, high = p.tile == 2 ? 256 : edge;
+    long long halves = 0, floats = 0, diags = 0, chunks = 0, casts = 0, grams = 0, squares = 0, applies = 0, sums = 0, slabs = 0;
+    for (int i = 0; i < n; ++i) {
+        MuonGroup& q = p.g[i] = g[i];
+        q.tall = q.rows > q.cols;
+        q.rp = (int)up(q.rows, high); q.cp = (int)up(q.cols, edge);
+        q.mp = std::min(q.rp, q.cp);
+        const long long nt = q.mp / edge;
+        q.grams = (int)(nt * (nt + 1) / 2);
+        if (q.ortho) slabs += (long long)q.count * q.grams * (std::max(q.rp, q.cp) / 64);
+    }
+    // Gram tiles: as many parts along the contraction as make about two workgroups a CU of the launch, none shorter than eight slabs
+    const long long target = std::max<long long>(8, (slabs + 511) / 512);
+    for (int i = 0; i < n; ++i) {
+        MuonGroup& q = p.g[i];
+        const long long size = (long long)q.rows * q.cols;
+        q.chunk0 = (int)chunks; q.chunks = (int)((size + FLAT - 1) / FLAT);
+        chunks += (long long)q.count * q.chunks;
+        q.cast0 = (int)casts; q.gram0 = (int)grams; q.square0 = (int)squares; q.apply0 = (int)applies; q.sum0 = (int)sums;
+        if (chunks > most) return false;
+        if (!q.ortho) continue;
+        const long long nx = (long long)q.rp * q.cp, ns = (long long)q.mp * q.mp;
+        if ((long long)std::max(q.rp, q.cp) * 256 > most || nx / CAST * q.count > most) return false;
+        q.casts = (int)(nx / CAST);
+        casts += (long long)q.count * q.casts;
+        q.splits = (int)((std::max(q.rp, q.cp) / 64 + target - 1) / target);
+        grams += (long long)q.count * q.grams * q.splits;
+        squares += (long long)q.count * q.grams;
+        q.applies = (int)(nx / high / edge);
+        applies += (long long)q.count * q.applies;
+        q.xplane = nx * q.count; q.splane = ns * q.count;
+        for (int b = 0; b < 2; ++b) { q.x[b] = halves; halves += 2 * q.xplane; }
+        q.s = halves; halves += (exact ? 2 : 1) * q.splane;
+        q.b = halves; halves += (exact ? 2 : 1) * q.splane;
+        q.diag = diags; diags += 2LL * q.count * q.mp;
+        q.part = floats;
+        if (q.splits > 1) { floats += (long long)q.count * q.grams * q.splits * edge * edge; sums += (long long)q.count * q.grams * (p.tile ? 4 : 1); }
+        if (casts > most || grams > most || applies > most || sums > most) return false;
+    }
+    p.chunks = (int)chunks; p.casts = (int)casts; p.grams = (int)grams; p.squares = (int)squares; p.applies = (int)applies; p.sums = (int)sums;
+    auto to256 = [](size_t v) { return (v + 255) & ~size_t(255); };
+    p.sums_at = to256((size_t)halves * 2);
+    p.diag_at = p.sums_at + to256((size_t)chunks * 8);
+    p.part_at = p.diag_at + to256((size_t)diags * 4);
+    p.bytes = p.part_at + to256((size_t)floats * 4) + 256;
+    *out = p;
+    return true;
+}
+
+hipError_t launch_muon(const MuonPlan& p, const MuonArgs& a, void* scratch, hipStream_t st) {
+    _Float16* ws = static_cast<_Float16*>(scratch);
+    double* sums = reinterpret_cast<double*>(static_cast<char*>(scratch) + p.sums_at);
+    float* diag = reinterpret_cast<float*>(static_cast<char*>(scratch) + p.diag_at);
+    float* part = reinterpret_cast<float*>(static_cast<char*>(scratch) + p.part_at);
+    muon_momentum_kernel<<<p.chunks, 256, 0, st>>>(p, a, sums);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.casts == 0) return e;
+    muon_cast_kernel<<<p.casts, 256, 0, st>>>(p, a, sums, ws);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (p.tile == 2) return run_products<2, 4, 2, false, true>(p, a, ws, diag, part, st);
+    if (p.tile == 1) return p.exact ? run_products<2, 2, 2, true, false>(p, a, ws, diag, part, st) : run_products<2, 2, 2, false, false>(p, a, ws, diag, part, st);
+    return p.exact ? run_products<1, 1, 1, true, false>(p, a, ws, diag, part, st) : run_products<1, 1, 1, false, false>(p, a, ws, diag, part, st);
+}
+
+}  // namespace blstm

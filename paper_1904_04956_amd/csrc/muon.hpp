@@ -1,0 +1,45 @@
+// The orthogonalised update: plan and launcher (muon.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+
+namespace blstm {
+
+constexpr int MUON_MAX_GROUPS = 10;
+
+// `count` tensors of one shape in a flat vector: tensor k starts at element at + (k / inner_count) outer + (k % inner_count) inner.
+struct MuonGroup {
+    long long at, outer, inner;
+    int inner_count, count, rows, cols;
+    bool ortho;               // its update is orthogonalised; else the tensor takes the plain momentum update
+    // The rest is the plan's.  A matrix lies in scratch in halves, zero-padded to rp x cp; its Gram matrix has mp rows.  The second plane
+    // of each (what the first one's rounding left over) lies xplane or splane elements behind the first.
+    int rp, cp, mp, tall, splits;
+    long long x[2], s, b, xplane, splane;      // elements of 2 bytes from the scratch's start
+    long long diag;                            // of the diagonals of S, then of B: float elements from their start, count x mp each
+    long long part;                            // float elements from the partial sums' start
+    int chunk0, chunks;                        // the flat passes' units: the group's first one, how many a tensor has
+    int cast0, casts;
+    int gram0, grams;                          // product tiles of a matrix on and above the diagonal; gram0 counts every part
+    int square0, apply0, applies;
+    int sum0;
+};
+struct MuonPlan {
+    MuonGroup g[MUON_MAX_GROUPS];
+    int n;
+    int tile;                 // 0: 64 x 64 tiles, 1: 128 x 128, 2: 128 x 128 and, in the last product, 256 x 128
+    int exact;                // products of both planes (mode 0)
+    int chunks, casts, grams, squares, applies, sums;
+    size_t sums_at, diag_at, part_at, bytes;   // byte offsets in scratch: squares' sums (double), diagonals, partial Gram tiles (float)
+};
+struct MuonArgs {
+    float* theta; unsigned short* shadow;      // null: the update itself goes to out
+    const float* grad; float* velocity;        // velocity null: grad is what is orthogonalised
+    void* out; int out_bf16;
+    float lr, lr_rest, momentum, decay; int nesterov;
+};
+// False: sizes beyond what the kernels index.  g[].at .. ortho are given.
+bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out);
+hipError_t launch_muon(const MuonPlan& p, const MuonArgs& a, void* scratch, hipStream_t st);
+
+}  // namespace blstm
