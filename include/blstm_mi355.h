@@ -203,6 +203,33 @@ size_t muon_scratch_bytes(const blstm_ctx* ctx, int flags);                     
 int muon_step(const blstm_ctx* ctx, float* theta_master, void* theta_bf16_or_null, const float* grad, float* velocity_or_null, float lr, float lr_rest,
               float momentum, float weight_decay, int flags, void* scratch, size_t scratch_bytes, void* stream);
 
+/* ---- low-rank adapters of many sequences at once beside a projection that they share ------------------------------------
+   y = x W^T + b + scale * t B_a^T,  t = x A_a^T,  a = ids[sequence]: x [T][B][K], y [T][B][N], W [N][K], b [N], A [count][rank][K], Bm [count][N][rank]
+   in the mode's storage type; ids [B] int32 on the device; t [T][B][rank] float.  An id of BLSTM_NO_ADAPTER is a sequence without adapter (t is zero);
+   any other id outside [0, count) is never used as an index: that sequence's y, t and dx are NaN, and it adds nothing to dA and dB.  Any number of sequences may
+   share an adapter.  W and b may lie in a flat parameter vector: these tensors need no more alignment than their elements' (whole 16-byte words, width K
+   (backward: K and N) included, are the faster).  Nothing may overlap what is written.  Scratch as for the softmax calls: caller-owned, 16-byte aligned, holds
+   nothing between calls; calls that overlap need one each.  The same inputs give the same bits. */
+#define BLSTM_NO_ADAPTER (-1)
+#define BLSTM_MAX_ADAPTERS 4096
+#define BLSTM_MAX_ADAPTER_RANK 128
+#define ADAPTER_FORWARD  0
+#define ADAPTER_BACKWARD 1
+typedef struct {
+    int32_t T, B, K, N, rank, count;           /* frames, sequences, width of x and of y, rank and number of the adapters */
+    int32_t mode;                              /* as in blstm_config */
+    float   scale;
+} adapter_config;
+size_t adapter_scratch_bytes(const adapter_config* cfg, int call);                      /* 0 and an error text for sizes it does not take */
+/* y, and t where it is not NULL (adapter_backward reads it).  b NULL: no bias. */
+int adapter_forward(const adapter_config* cfg, const void* W, const void* b_or_null, const void* A, const void* Bm, const int32_t* ids, const void* x,
+                    void* y, float* t_or_null, void* scratch, size_t scratch_bytes, void* stream);
+/* With q = dy B_a:  dx = dy W + scale * q A_a;  dA_a = scale * sum q^T x,  dB_a = scale * sum dy^T t over the frames of a's sequences (float, overwritten;
+   zero for an adapter that no sequence has);  dW = sum dy^T x and db = sum dy over all frames (float).  t is what adapter_forward gave for the same x, A and ids.
+   dx NULL: not wanted; dW NULL (db NULL with it): the shared projection is not trained. */
+int adapter_backward(const adapter_config* cfg, const void* W, const void* A, const void* Bm, const int32_t* ids, const void* x, const float* t, const void* dy,
+                     void* dx_or_null, float* dA, float* dB, float* dW_or_null, float* db_or_null, void* scratch, size_t scratch_bytes, void* stream);
+
 /* Eq. 4, second line, for one matching of R replicas: for every pair {i, partner[i]} both members
    become (theta_i + theta_j)/2; partner[i] == i leaves replica i untouched.
    theta_master: HOST array of R device pointers (n floats each); theta_bf16_or_null: HOST array of R

@@ -21,12 +21,17 @@ BLSTM_MAX_TOP = 256
 BLSTM_MIN_TEMPERATURE = 1e-4
 SOFTMAX_LOGPROB, SOFTMAX_TOPK, SOFTMAX_DISTILL, SOFTMAX_POLICY = range(4)
 MUON_NESTEROV, MUON_GATES, MUON_SOFTMAX = 1, 2, 4
+BLSTM_NO_ADAPTER = -1
+BLSTM_MAX_ADAPTERS = 4096
+BLSTM_MAX_ADAPTER_RANK = 128
+ADAPTER_FORWARD, ADAPTER_BACKWARD = range(2)
 
 EXPORTS = [
     "blstm_create", "blstm_destroy", "blstm_param_count", "blstm_workspace_bytes", "blstm_param_offset",
     "blstm_bind", "blstm_forward", "softmax_xent_fwd_bwd", "softmax_xent_fwd_bwd_noalloc",
     "softmax_scratch_bytes", "softmax_logprob", "softmax_topk", "softmax_distill_fwd_bwd", "softmax_policy_fwd_bwd", "blstm_backward", "sgd_step", "adpsgd_mix",
     "muon_orthogonalize_scratch_bytes", "muon_orthogonalize", "muon_matrices_step", "muon_scratch_bytes", "muon_step",
+    "adapter_scratch_bytes", "adapter_forward", "adapter_backward",
     "sgd_mix_pair", "sync_average", "blstm_lr_schedule",
     "adpsgd_ring_partner", "blstm_shadow_refresh", "blstm_set_option", "blstm_weights_changed", "blstm_device_status", "blstm_profile_enable", "blstm_profile_read",
     "blstm_profile_classes", "blstm_profile_name", "blstm_last_error",
@@ -42,6 +47,10 @@ class BlstmError(RuntimeError):
 class blstm_config(ctypes.Structure):
     _fields_ = [("T", c_int32), ("B", c_int32), ("D", c_int32), ("H", c_int32), ("L", c_int32),
                 ("P", c_int32), ("V", c_int32), ("mode", c_int32), ("loss_scale", c_float)]
+
+
+class adapter_config(ctypes.Structure):
+    _fields_ = [("T", c_int32), ("B", c_int32), ("K", c_int32), ("N", c_int32), ("rank", c_int32), ("count", c_int32), ("mode", c_int32), ("scale", c_float)]
 
 
 _lib = None
@@ -97,6 +106,12 @@ def lib():
     L.muon_scratch_bytes.restype = c_size_t
     L.muon_step.argtypes = [c_void_p] * 5 + [c_float] * 4 + [c_int, c_void_p, c_size_t, c_void_p]
     L.muon_step.restype = c_int
+    L.adapter_scratch_bytes.argtypes = [POINTER(adapter_config), c_int]
+    L.adapter_scratch_bytes.restype = c_size_t
+    L.adapter_forward.argtypes = [POINTER(adapter_config)] + [c_void_p] * 9 + [c_size_t, c_void_p]
+    L.adapter_forward.restype = c_int
+    L.adapter_backward.argtypes = [POINTER(adapter_config)] + [c_void_p] * 13 + [c_size_t, c_void_p]
+    L.adapter_backward.restype = c_int
     L.adpsgd_mix.argtypes = [POINTER(c_void_p), POINTER(c_void_p), c_size_t, c_int, POINTER(c_int32), c_void_p]
     L.adpsgd_mix.restype = c_int
     L.sgd_mix_pair.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_float, c_float,
@@ -280,6 +295,22 @@ def muon_step(ctx, theta_master, theta_bf16_or_null, grad, velocity_or_null, lr,
               stream=None):
     return _check(lib().muon_step(ctx, _ptr(theta_master), _ptr(theta_bf16_or_null), _ptr(grad), _ptr(velocity_or_null), lr, lr_rest, momentum,
                                   weight_decay, flags, *_scratch(scratch, scratch_bytes), _stream(stream)))
+
+
+def adapter_scratch_bytes(cfg, call):
+    """Bytes of scratch that one of the two calls below needs (call: ADAPTER_FORWARD or ADAPTER_BACKWARD)."""
+    return _bytes(lib().adapter_scratch_bytes(None if cfg is None else byref(cfg), call))
+
+
+def adapter_forward(cfg, W, b_or_null, A, Bm, ids, x, y, t_or_null, scratch, scratch_bytes=None, stream=None):
+    return _check(lib().adapter_forward(None if cfg is None else byref(cfg), _ptr(W), _ptr(b_or_null), _ptr(A), _ptr(Bm), _ptr(ids), _ptr(x), _ptr(y),
+                                        _ptr(t_or_null), *_scratch(scratch, scratch_bytes), _stream(stream)))
+
+
+def adapter_backward(cfg, W, A, Bm, ids, x, t, dy, dx_or_null, dA, dB, dW_or_null, db_or_null, scratch, scratch_bytes=None, stream=None):
+    return _check(lib().adapter_backward(None if cfg is None else byref(cfg), _ptr(W), _ptr(A), _ptr(Bm), _ptr(ids), _ptr(x), _ptr(t), _ptr(dy),
+                                         _ptr(dx_or_null), _ptr(dA), _ptr(dB), _ptr(dW_or_null), _ptr(db_or_null), *_scratch(scratch, scratch_bytes),
+                                         _stream(stream)))
 
 
 def adpsgd_mix(theta_master, theta_bf16_or_null, n, R, partner, stream=None):

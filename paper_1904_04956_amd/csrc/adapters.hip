@@ -1,0 +1,510 @@
+// Low-rank adapters of many sequences at once beside the projection that they share:
+//   y = x W^T + b + s t B_a^T,  t = x A_a^T,   a = the adapter of the row's sequence          (W [N][K], A_a [r][K], B_a [N][r])
+//   dx = dy W + s q A_a,  q = dy B_a;   dA_a = s sum q^T x,   dB_a = s sum dy^T t             over the rows of a's sequences
+// The sequences are sorted by adapter on the device (adapt_plan_kernel), and no tile of rows holds two adapters' rows: A_a's rows ride along as
+// further rows of W in one pass over x, and s t B_a^T is one more product on the tile's accumulators before they leave.  dx is the same kernel on
+// dy with the transposed weights.  (W's gradient is an ordinary product: gemm.hip.)
+// Numbers: sums in float; t and q enter their products as two bf16 numbers (2^-17) for y and dx, which leave as bf16, and as three for
+// the gradients, which leave as float.
+#include "gemm_tile.hpp"
+#include "adapters.hpp"
+#include <algorithm>
+
+namespace blstm {
+namespace {
+
+// ---- which rows belong together ----------------------------------------------------------------------------------------
+// One workgroup: a stable counting sort of the sequences by key (the order within an adapter is the order of its sums), then the tables of tiles and
+// chunks.  64 sequences a wavefront at a time: a lane's rank among equal keys of its wavefront, and the wavefronts' counts in turn.
+constexpr int PLAN_THREADS = 1024;
+__global__ __launch_bounds__(PLAN_THREADS) void adapt_plan_kernel(AdaptShape s, AdaptPlan p, const int32_t* ids, char* plan) {
+    __shared__ int hist[ADAPT_MAX_COUNT + 2], first[ADAPT_MAX_COUNT + 3], tile0[ADAPT_MAX_COUNT + 3], chunk0[ADAPT_MAX_COUNT + 3], wave_sum[3][16];
+    int* counts = reinterpret_cast<int*>(plan + p.counts);
+    int* perm = reinterpret_cast<int*>(plan + p.perm);
+    const int keys = s.count + 2, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    for (int i = tid; i < keys; i += PLAN_THREADS) hist[i] = 0;
+    __syncthreads();
+    auto key_of = [&](int b) { const int id = ids[b]; return id >= 0 && id < s.count ? id : id == -1 ? s.count : s.count + 1; };
+    // a sequence's place among those of its key; kept in perm until the keys' places are known
+    for (int b0 = 0; b0 < s.B; b0 += PLAN_THREADS) {
+        const int b = b0 + tid;
+        const int key = b < s.B ? key_of(b) : -1;
+        int rank = 0, later = 0;
+        for (int j = 0; j < 64; ++j) {
+            const int k = __builtin_amdgcn_readlane(key, j);
+            if (k == key) { if (j < lane) ++rank; else if (j > lane) later = 1; }
+        }
+        for (int w = 0; w < PLAN_THREADS / 64 && b0 + 64 * w < s.B; ++w) {
+            if (w == wave && key >= 0) {
+                const int base = hist[key];
+                perm[b] = base + rank;
+                if (!later) hist[key] = base + rank + 1;       // (every lane of the wavefront has read before one writes: it runs in step)
+            }
+            __syncthreads();
+        }
+    }
+    // places, tiles and chunks in front of each key
+    const int per = (keys + PLAN_THREADS - 1) / PLAN_THREADS, k0 = min(keys, tid * per), k1 = min(keys, k0 + per);
+    int sum[3] = {0, 0, 0};
+    auto add = [&](int k) {
+        const long long rows = (long long)hist[k] * s.T;
+        sum[0] += hist[k];
+        sum[1] += (int)((rows + p.rows - 1) / p.rows);
+        if (p.chunk && k < s.count) sum[2] += (int)((rows + p.chunk - 1) / p.chunk);
+    };
+    for (int k = k0; k < k1; ++k) add(k);
+    int before[3];
+    for (int i = 0; i < 3; ++i) {
+        int v = sum[i];
+        for (int o = 1; o < 64; o <<= 1) { const int u = __shfl_up(v, o); if (lane >= o) v += u; }
+        if (lane == 63) wave_sum[i][wave] = v;
+        before[i] = v - sum[i];
+    }
+    __syncthreads();
+    for (int i = 0; i < 3; ++i) for (int w = 0; w < wave; ++w) before[i] += wave_sum[i][w];
+    for (int i = 0; i < 3; ++i) sum[i] = before[i];
+    for (int k = k0; k < k1; ++k) { first[k] = sum[0]; tile0[k] = sum[1]; chunk0[k] = sum[2]; add(k); }
+    if (k1 == keys && k0 < keys) { first[keys] = sum[0]; tile0[keys] = sum[1]; chunk0[keys] = sum[2]; }
+    __syncthreads();
+    const int tiles = tile0[keys], chunks = chunk0[keys];
+    if (tid == 0) { counts[0] = tiles; counts[1] = chunks; }
+    for (int k = tid; k <= keys; k += PLAN_THREADS) reinterpret_cast<int*>(plan + p.first)[k] = first[k];
+    if (p.chunk) for (int k = tid; k <= s.count; k += PLAN_THREADS) reinterpret_cast<int*>(plan + p.first_chunk)[k] = chunk0[k];
+    auto table = [&](const int* from, int n, int rows, int4* out) {
+        for (int i = tid; i < n; i += PLAN_THREADS) {
+            int lo = 0, hi = keys;                              // the key whose entries hold i: the last that starts at or before it
+            while (hi - lo > 1) { const int m = (lo + hi) >> 1; if (from[m] <= i) lo = m; else hi = m; }
+            const long long r0 = (long long)(i - from[lo]) * rows, all = (long long)hist[lo] * s.T;
+            out[i] = make_int4(lo, (int)r0, (int)min((long long)rows, all - r0), first[lo]);
+        }
+    };
+    table(tile0, tiles, p.rows, reinterpret_cast<int4*>(plan + p.tiles));
+    if (p.chunk) table(chunk0, chunks, p.chunk, reinterpret_cast<int4*>(plan + p.chunks));
+    // (a lane reads the place that it wrote itself, and the sorted list lies behind the places)
+    for (int b = tid; b < s.B; b += PLAN_THREADS) perm[s.B + first[key_of(b)] + perm[b]] = b;
+}
+
+// ---- products of 16-row tiles ------------------------------------------------------------------------------------------
+// A fragment is 16 bytes of a row: eight bf16 are a product's k of their lane group, four floats one k each of four products.
+template <typename T>
+__device__ __forceinline__ void mma16(f32x4_t& acc, const uint4& a, const uint4& b) {
+    if constexpr (sizeof(T) == 2) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
+    else {
+        const f32x4_t x = __builtin_bit_cast(f32x4_t, a), y = __builtin_bit_cast(f32x4_t, b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], acc, 0, 0, 0);
+    }
+}
+// elements [k, k + 16 bytes) of a row of n, zero beyond it
+template <typename T, bool VECTOR>
+__device__ __forceinline__ uint4 load_chunk(const T* row, int k, int n) {
+    constexpr int V = Vec<T>::N;
+    if constexpr (VECTOR) {
+        if (k < n) { const u32x4_t v = *reinterpret_cast<const u32x4_t*>(row + k); return make_uint4(v[0], v[1], v[2], v[3]); }
+        return make_uint4(0u, 0u, 0u, 0u);
+    } else {
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            if (k + e < n) {
+                if constexpr (sizeof(T) == 2) w[e >> 1] |= (uint32_t)row[k + e] << (16 * (e & 1));
+                else w[e] = __builtin_bit_cast(uint32_t, row[k + e]);
+            }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// One pass over a tile's rows: 16 MR rows x 128 columns of y and all 16 RB columns of t.  A slab is 128 bytes of every row (x, W, A_a), through registers
+// into swizzled LDS, double-buffered; wavefront w multiplies columns 32 w .. of y and rows 16 w .. of t (MR 4) or, with one row block, wavefront 0 t.
+constexpr int PN = 128;
+template <typename T, int MR, int RB, bool VECTOR>
+__global__ __launch_bounds__(256) void adapt_project_kernel(ProjectArgs a) {
+    constexpr int V = Vec<T>::N, SLAB = 8 * V, ROWS = 16 * MR, RP = 16 * RB;
+    constexpr int NX = ROWS * 8 / 256 > 0 ? ROWS * 8 / 256 : 1, NW = PN * 8 / 256, NA = (RP * 8 + 255) / 256;
+    constexpr int STAGE = (ROWS + PN + RP) * CHUNKS;
+    extern __shared__ uint4 smem[];
+    const AdaptShape& s = a.s;
+    const int ntn = a.y ? (s.N + PN - 1) / PN : 1, tile = blockIdx.x / ntn, col0 = blockIdx.x % ntn * PN;
+    if (tile >= reinterpret_cast<const int*>(a.plan + a.p.counts)[0]) return;
+    const int4 what = reinterpret_cast<const int4*>(a.plan + a.p.tiles)[tile];
+    const int key = what.x, nrows = what.z;
+    const int* order = reinterpret_cast<const int*>(a.plan + a.p.perm) + s.B + what.w;
+    const bool low = key < s.count;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    auto row_of = [&](int r) {                          // the row of x of the tile's row r
+        const int i = what.y + r, j = i / s.T;
+        return (long long)(i - j * s.T) * s.B + order[j];
+    };
+    const T* x = static_cast<const T*>(a.x);
+    const T* W = static_cast<const T*>(a.W);
+    const T* A = static_cast<const T*>(a.A) + (long long)(low ? key : 0) * s.rank * s.K;
+    const T* Bm = static_cast<const T*>(a.Bm) + (long long)(low ? key : 0) * s.rank * s.N;
+    const int ch = tid & 7;
+    const T* xr[NX];
+#pragma unroll
+    for (int i = 0; i < NX; ++i) { const int r = (tid >> 3) + 32 * i; xr[i] = r < nrows ? x + row_of(r) * s.K : nullptr; }
+    f32x4_t acc[MR][2], tac[RB];
+#pragma unroll
+    for (int i = 0; i < MR; ++i) { acc[i][0] = f32x4_t{}; acc[i][1] = f32x4_t{}; }
+#pragma unroll
+    for (int i = 0; i < RB; ++i) tac[i] = f32x4_t{};
+    uint4 rx[NX], rw[NW], ra[NA];
+    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+    auto load = [&](int k0) {
+        const int k = k0 + ch * V;
+#pragma unroll
+        for (int i = 0; i < NX; ++i) rx[i] = xr[i] ? load_chunk<T, VECTOR>(xr[i], k, s.K) : none;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) { const int n = col0 + (tid >> 3) + 32 * i; rw[i] = n < s.N ? load_chunk<T, VECTOR>(W + (long long)n * s.K, k, s.K) : none; }
+#pragma unroll
+        for (int i = 0; i < NA; ++i) { const int r = (tid >> 3) + 32 * i; ra[i] = low && r < s.rank ? load_chunk<T, VECTOR>(A + (long long)r * s.K, k, s.K) : none; }
+    };
+    auto store = [&](int buf) {
+        uint4* to = smem + buf * STAGE;
+        auto put = [&](int r, const uint4& v) { to[r * CHUNKS + (ch ^ swz(r))] = v; };
+#pragma unroll
+        for (int i = 0; i < NX; ++i) { const int r = (tid >> 3) + 32 * i; if (ROWS >= 32 || r < ROWS) put(r, rx[i]); }
+#pragma unroll
+        for (int i = 0; i < NW; ++i) put(ROWS + (tid >> 3) + 32 * i, rw[i]);
+#pragma unroll
+        for (int i = 0; i < NA; ++i) { const int r = (tid >> 3) + 32 * i; if (r < RP) put(ROWS + PN + r, ra[i]); }
+    };
+    const int fr = lane & 15, fg = lane >> 4;
+    const int slabs = (s.K + SLAB - 1) / SLAB;
+    const bool makes_t = MR == 4 || wave == 0;
+    const int trow = MR == 4 ? wave : 0;
+    load(0);
+    store(0);
+    __syncthreads();
+    for (int it = 0; it < slabs; ++it) {
+        const uint4* at = smem + (it & 1) * STAGE;
+        if (it + 1 < slabs) load((it + 1) * SLAB);
+        auto frag = [&](int r, int q) { return at[r * CHUNKS + ((4 * q + fg) ^ swz(r))]; };
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            uint4 fx[MR];
+#pragma unroll
+            for (int i = 0; i < MR; ++i) fx[i] = frag(16 * i + fr, q);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint4 fw = frag(ROWS + 32 * wave + 16 * j + fr, q);
+#pragma unroll
+                for (int i = 0; i < MR; ++i) mma16<T>(acc[i][j], fx[i], fw);
+            }
+            if (low && makes_t) {
+                const uint4 ft = MR == 4 ? frag(16 * trow + fr, q) : fx[0];
+#pragma unroll
+                for (int j = 0; j < RB; ++j) mma16<T>(tac[j], ft, frag(ROWS + PN + 16 * j + fr, q));
+            }
+        }
+        if (it + 1 < slabs) store((it + 1) & 1);
+        __syncthreads();
+    }
+    // t, for everybody: rows of RP floats
+    float* ts = reinterpret_cast<float*>(smem);
+    constexpr int TLD = RP + 4;
+    const float bad = key > s.count ? __builtin_nanf("") : 0.0f;
+    if (makes_t) {
+#pragma unroll
+        for (int j = 0; j < RB; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ts[(16 * trow + 4 * fg + e) * TLD + 16 * j + fr] = tac[j][e] + bad;
+    }
+    __syncthreads();
+    if (a.t && col0 == 0) {
+        for (int i = tid; i < nrows * s.rank; i += 256) { const int r = i / s.rank, c = i - r * s.rank; a.t[row_of(r) * s.rank + c] = ts[r * TLD + c]; }
+    }
+    if (!a.y) return;
+    if (low) {
+        // s t B_a^T: t in two bf16 parts, or as it is
+        constexpr int STEP = 4 * V;                     // columns of t a step
+#pragma unroll
+        for (int q = 0; q < (RP + STEP - 1) / STEP; ++q) {
+            const int c = q * STEP + fg * V;
+            uint4 fb[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int n = col0 + 32 * wave + 16 * j + fr;
+                fb[j] = n < s.N ? load_chunk<T, false>(Bm + (long long)n * s.rank, c, s.rank) : none;
+            }
+#pragma unroll
+            for (int i = 0; i < MR; ++i) {
+                float v[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = c < RP ? s.scale * ts[(16 * i + fr) * TLD + c + e] : 0.0f;
+                uint4 hi, lo;
+                if constexpr (sizeof(T) == 2) {
+                    uint32_t h[4], l[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        h[e] = pack_bf2(v[2 * e], v[2 * e + 1]);
+                        l[e] = pack_bf2(v[2 * e] - bf2f((bf16_t)h[e]), v[2 * e + 1] - bf2f((bf16_t)(h[e] >> 16)));
+                    }
+                    hi = make_uint4(h[0], h[1], h[2], h[3]); lo = make_uint4(l[0], l[1], l[2], l[3]);
+                } else hi = __builtin_bit_cast(uint4, f32x4_t{v[0], v[1], v[2], v[3]});
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if constexpr (sizeof(T) == 2) mma16<T>(acc[i][j], lo, fb[j]);
+                    mma16<T>(acc[i][j], hi, fb[j]);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    // out through LDS, whole 16-byte words of a row at a time
+    constexpr int OLD = PN + 4;
+    float* os = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int c = 32 * wave + 16 * j + fr, n = col0 + c;
+        float bias = bad;
+        if (a.b && n < s.N) bias += ld_f(static_cast<const T*>(a.b) + n);
+#pragma unroll
+        for (int i = 0; i < MR; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) os[(16 * i + 4 * fg + e) * OLD + c] = acc[i][j][e] + bias;
+    }
+    __syncthreads();
+    T* y = static_cast<T*>(a.y);
+    const bool words = s.N % V == 0 && (reinterpret_cast<uintptr_t>(y) & 15) == 0;
+    for (int i = tid; i < nrows * (PN / V); i += 256) {
+        const int r = i / (PN / V), c = i % (PN / V) * V, n = col0 + c;
+        if (n >= s.N) continue;
+        T* to = y + row_of(r) * s.N + n;
+        const float* v = os + r * OLD + c;
+        if (words) {
+            u32x4_t w;
+            if constexpr (sizeof(T) == 2) { w[0] = pack_bf2(v[0], v[1]); w[1] = pack_bf2(v[2], v[3]); w[2] = pack_bf2(v[4], v[5]); w[3] = pack_bf2(v[6], v[7]); }
+            else w = __builtin_bit_cast(u32x4_t, *reinterpret_cast<const f32x4_t*>(v));
+            *reinterpret_cast<u32x4_t*>(to) = w;
+        } else {
+            for (int e = 0; e < V && n + e < s.N; ++e) st_f(to + e, v[e]);
+        }
+    }
+}
+
+template <int MR, int RB, typename T>
+constexpr int project_lds() {
+    const int loop = 2 * (16 * MR + PN + 16 * RB) * 128, t = 16 * MR * (16 * RB + 4) * 4, out = 16 * MR * (PN + 4) * 4;
+    return std::max(loop, std::max(t, out));
+}
+template <typename T, int MR, int RB>
+void run_project(const ProjectArgs& a, bool vector, hipStream_t st) {
+    const int ntn = a.y ? (a.s.N + PN - 1) / PN : 1;
+    if (vector) adapt_project_kernel<T, MR, RB, true><<<a.p.max_tiles * ntn, 256, project_lds<MR, RB, T>(), st>>>(a);
+    else adapt_project_kernel<T, MR, RB, false><<<a.p.max_tiles * ntn, 256, project_lds<MR, RB, T>(), st>>>(a);
+}
+template <typename T>
+hipError_t project(const ProjectArgs& a, hipStream_t st) {
+    auto whole = [&](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
+    const bool vector = a.s.K % Vec<T>::N == 0 && whole(a.x) && whole(a.W) && whole(a.A);
+    const int rb = a.s.rank <= 16 ? 1 : a.s.rank <= 32 ? 2 : a.s.rank <= 64 ? 4 : 8;
+    if (a.p.rows == 16) {
+        if (rb == 1) run_project<T, 1, 1>(a, vector, st);
+        else if (rb == 2) run_project<T, 1, 2>(a, vector, st);
+        else if (rb == 4) run_project<T, 1, 4>(a, vector, st);
+        else run_project<T, 1, 8>(a, vector, st);
+    } else {
+        if (rb == 1) run_project<T, 4, 1>(a, vector, st);
+        else if (rb == 2) run_project<T, 4, 2>(a, vector, st);
+        else if (rb == 4) run_project<T, 4, 4>(a, vector, st);
+        else run_project<T, 4, 8>(a, vector, st);
+    }
+    return hipGetLastError();
+}
+
+// ---- transposed weights ----------------------------------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void adapt_transpose_kernel(TransposeArgs a) {
+    __shared__ T lds[32][33];
+    const AdaptShape& s = a.s;
+    auto tiles = [](int r, int c) { return ((r + 31) / 32) * ((c + 31) / 32); };
+    const int tw = tiles(s.N, s.K), ta = tiles(s.rank, s.K), tb = tiles(s.N, s.rank);
+    int id = blockIdx.x, R, C;
+    const T* from; T* to;
+    if (id < tw) { from = static_cast<const T*>(a.W); to = static_cast<T*>(a.Wt); R = s.N; C = s.K; }
+    else if ((id -= tw) < ta * s.count) { const long long k = id / ta; id %= ta; R = s.rank; C = s.K; from = static_cast<const T*>(a.A) + k * R * C; to = static_cast<T*>(a.At) + k * R * C; }
+    else { id -= ta * s.count; const long long k = id / tb; id %= tb; R = s.N; C = s.rank; from = static_cast<const T*>(a.Bm) + k * R * C; to = static_cast<T*>(a.Bt) + k * R * C; }
+    const int nc = (C + 31) / 32, r0 = id / nc * 32, c0 = id % nc * 32, i = threadIdx.x >> 5, j = threadIdx.x & 31;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) if (r0 + i + 8 * e < R && c0 + j < C) lds[i + 8 * e][j] = from[(long long)(r0 + i + 8 * e) * C + c0 + j];
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) if (c0 + i + 8 * e < C && r0 + j < R) to[(long long)(c0 + i + 8 * e) * R + r0 + j] = lds[j][i + 8 * e];
+}
+
+// ---- the adapters' gradients -------------------------------------------------------------------------------------------
+// sum over a chunk's rows of L[row][i] R[row][j]: L = q with R = x, L = t with R = dy.  A workgroup: a chunk and 128 columns of x or dy, 32 a
+// wavefront, 32 RB rows of the result.  64 rows at a time lie in LDS as they lie in memory; 16-bit ones are transposed by the LDS read.
+template <typename T, int RB, bool VECTOR>
+__global__ __launch_bounds__(256) void adapt_grad_kernel(AdaptGradArgs a) {
+    constexpr int V = Vec<T>::N, PARTS = sizeof(T) == 2 ? 3 : 1, RP = 32 * RB, ES = (int)sizeof(T);
+    constexpr int RLD = 128 * ES + 16, LLD = RP * ES + 16;                 // bytes of a row
+    constexpr int NR = 64 * 128 / V / 256;
+    extern __shared__ uint4 smem[];
+    char* rs = reinterpret_cast<char*>(smem);
+    char* ls = rs + 64 * RLD;
+    const AdaptShape& s = a.s;
+    const int nk = (s.K + 127) / 128, nn = (s.N + 127) / 128, chunk = blockIdx.x / (nk + nn), ct = blockIdx.x % (nk + nn);
+    if (chunk >= reinterpret_cast<const int*>(a.plan + a.p.counts)[1]) return;
+    const int4 what = reinterpret_cast<const int4*>(a.plan + a.p.chunks)[chunk];
+    const int* order = reinterpret_cast<const int*>(a.plan + a.p.perm) + s.B + what.w;
+    const bool second = ct >= nk;
+    const int width = second ? s.N : s.K, c0 = (second ? ct - nk : ct) * 128;
+    const T* R = static_cast<const T*>(second ? a.dy : a.x);
+    const float* L = second ? a.t : a.q;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    auto row_of = [&](int r) { const int i = what.y + r, j = i / s.T; return (long long)(i - j * s.T) * s.B + order[j]; };
+    f32x16_t acc[RB];
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
+    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+    for (int r0 = 0; r0 < what.z; r0 += 64) {
+        uint4 v[NR];
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int c = tid + 256 * i, r = c / (128 / V), k = c0 + c % (128 / V) * V;
+            v[i] = r0 + r < what.z ? load_chunk<T, VECTOR>(R + row_of(r0 + r) * width, k, width) : none;
+        }
+        float l[64 * RP / 256];
+#pragma unroll
+        for (int i = 0; i < 64 * RP / 256; ++i) {
+            const int c = tid + 256 * i, r = c / RP, k = c % RP;
+            l[i] = r0 + r < what.z && k < s.rank ? L[row_of(r0 + r) * s.rank + k] : 0.0f;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NR; ++i) { const int c = tid + 256 * i; *reinterpret_cast<uint4*>(rs + c / (128 / V) * RLD + c % (128 / V) * 16) = v[i]; }
+#pragma unroll
+        for (int i = 0; i < 64 * RP / 256; ++i) {
+            const int c = tid + 256 * i, r = c / RP, k = c % RP;
+            float left = l[i];
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) {
+                if constexpr (ES == 2) { const bf16_t h = f2bf(left); *reinterpret_cast<bf16_t*>(ls + (p * 64 + r) * LLD + 2 * k) = h; left -= bf2f(h); }
+                else *reinterpret_cast<float*>(ls + r * LLD + 4 * k) = left;
+            }
+        }
+        __syncthreads();
+        if constexpr (ES == 2) {
+            const int g = lane >> 4, li = lane & 15, at = (8 * (g >> 1) + (li >> 2)), off = 32 * (g & 1) + (li & 3) * 8;
+#pragma unroll
+            for (int k = 0; k < 64; k += 16) {
+                const uint4 fr = lfrag_tr<RLD>(rs + at * RLD + wave * 64 + off, k);
+#pragma unroll
+                for (int i = 0; i < RB; ++i)
+#pragma unroll
+                    for (int p = PARTS - 1; p >= 0; --p) {
+                        const uint4 fl = lfrag_tr<LLD>(ls + (p * 64 + at) * LLD + i * 64 + off, k);
+                        acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, fl), __builtin_bit_cast(bf16x8_t, fr), acc[i], 0, 0, 0);
+                    }
+            }
+        } else {
+#pragma unroll 8
+            for (int k = 0; k < 64; k += 2) {
+                const int r = k + (lane >> 5), c = lane & 31;
+                const float fr = *reinterpret_cast<const float*>(rs + r * RLD + (32 * wave + c) * 4);
+#pragma unroll
+                for (int i = 0; i < RB; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(ls + r * LLD + (32 * i + c) * 4), fr, acc[i], 0, 0, 0);
+            }
+        }
+    }
+    const int col = c0 + 32 * wave + (lane & 31);
+    if (col >= width) return;
+    float* out = a.part + (long long)chunk * s.rank * (s.K + s.N) + (second ? s.K : 0) + col;
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int r = 32 * i + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
+            if (r < s.rank) out[(long long)r * (s.K + s.N)] = acc[i][e];
+        }
+}
+
+// An adapter's chunks in order; dB leaves transposed (through LDS).
+__global__ __launch_bounds__(256) void adapt_grad_sum_kernel(AdaptGradArgs a) {
+    __shared__ float lds[32][33];
+    const AdaptShape& s = a.s;
+    const int wide = s.K + s.N, nr = (s.rank + 31) / 32, nc = (s.K + 31) / 32 + (s.N + 31) / 32;
+    const int key = blockIdx.x / (nr * nc), t = blockIdx.x % (nr * nc), r0 = t / nc * 32, ci = t % nc;
+    const bool second = ci >= (s.K + 31) / 32;
+    const int c0 = second ? (ci - (s.K + 31) / 32) * 32 : ci * 32, width = second ? s.N : s.K;
+    const int* first = reinterpret_cast<const int*>(a.plan + a.p.first_chunk);
+    const int from = first[key], to = first[key + 1], i = threadIdx.x >> 5, j = threadIdx.x & 31;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int r = r0 + i + 8 * e, c = c0 + j;
+        float v = 0.0f;
+        if (r < s.rank && c < width) for (int k = from; k < to; ++k) v += a.part[((long long)k * s.rank + r) * wide + (second ? s.K : 0) + c];
+        v *= s.scale;
+        if (!second) { if (r < s.rank && c < width) a.dA[((long long)key * s.rank + r) * s.K + c] = v; }
+        else lds[i + 8 * e][j] = v;
+    }
+    if (!second) return;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int c = c0 + i + 8 * e, r = r0 + j;
+        if (r < s.rank && c < s.N) a.dB[((long long)key * s.N + c) * s.rank + r] = lds[j][i + 8 * e];
+    }
+}
+
+template <typename T, int RB>
+void run_grad(const AdaptGradArgs& a, bool vector, hipStream_t st) {
+    constexpr int lds = 64 * (128 * (int)sizeof(T) + 16) + (sizeof(T) == 2 ? 3 : 1) * 64 * (32 * RB * (int)sizeof(T) + 16);
+    const int grid = a.p.max_chunks * ((a.s.K + 127) / 128 + (a.s.N + 127) / 128);
+    if (vector) adapt_grad_kernel<T, RB, true><<<grid, 256, lds, st>>>(a);
+    else adapt_grad_kernel<T, RB, false><<<grid, 256, lds, st>>>(a);
+}
+template <typename T>
+hipError_t grad(const AdaptGradArgs& a, hipStream_t st) {
+    auto whole = [&](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
+    const bool vector = a.s.K % Vec<T>::N == 0 && a.s.N % Vec<T>::N == 0 && whole(a.x) && whole(a.dy);
+    if (a.s.rank <= 32) run_grad<T, 1>(a, vector, st);
+    else if (a.s.rank <= 64) run_grad<T, 2>(a, vector, st);
+    else run_grad<T, 4>(a, vector, st);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int tiles = ((a.s.rank + 31) / 32) * ((a.s.K + 31) / 32 + (a.s.N + 31) / 32);
+    adapt_grad_sum_kernel<<<a.s.count * tiles, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+AdaptPlan adapt_plan(const AdaptShape& s, int rows, int chunk) {
+    AdaptPlan p{};
+    auto to256 = [](size_t v) { return (v + 255) & ~size_t(255); };
+    const long long M = (long long)s.T * s.B;
+    const int groups = std::min(s.B, s.count + 2);
+    p.rows = rows; p.chunk = chunk;
+    p.max_tiles = (int)(M / rows) + groups;
+    p.max_chunks = chunk ? (int)(M / chunk) + groups : 0;
+    p.counts = 0;
+    p.perm = 256;
+    p.first = p.perm + to256((size_t)s.B * 8);
+    p.first_chunk = p.first + to256(((size_t)s.count + 3) * 4);
+    p.tiles = p.first_chunk + to256(((size_t)s.count + 1) * 4);
+    p.chunks = p.tiles + to256((size_t)p.max_tiles * 16);
+    p.bytes = p.chunks + to256((size_t)p.max_chunks * 16);
+    return p;
+}
+
+hipError_t launch_adapt_plan(const AdaptShape& s, const AdaptPlan& p, const int32_t* ids, char* plan, hipStream_t st) {
+    adapt_plan_kernel<<<1, PLAN_THREADS, 0, st>>>(s, p, ids, plan);
+    return hipGetLastError();
+}
+hipError_t launch_adapt_project(const ProjectArgs& a, DType type, hipStream_t st) { return type == DT_BF16 ? project<bf16_t>(a, st) : project<float>(a, st); }
+hipError_t launch_adapt_transpose(const TransposeArgs& a, DType type, hipStream_t st) {
+    auto tiles = [](int r, int c) { return ((r + 31) / 32) * ((c + 31) / 32); };
+    const int n = tiles(a.s.N, a.s.K) + a.s.count * (tiles(a.s.rank, a.s.K) + tiles(a.s.N, a.s.rank));
+    if (type == DT_BF16) adapt_transpose_kernel<bf16_t><<<n, 256, 0, st>>>(a);
+    else adapt_transpose_kernel<float><<<n, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+hipError_t launch_adapt_grad(const AdaptGradArgs& a, DType type, hipStream_t st) { return type == DT_BF16 ? grad<bf16_t>(a, st) : grad<float>(a, st); }
+
+}  // namespace blstm

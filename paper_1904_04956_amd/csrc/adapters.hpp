@@ -1,0 +1,55 @@
+// Low-rank adapters of the sequences of a batch beside a projection that they share: launchers (adapters.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+#include "gemm.hpp"
+
+namespace blstm {
+
+constexpr int ADAPT_MAX_RANK = 128, ADAPT_MAX_COUNT = 4096;
+
+struct AdaptShape { int T, B, K, N, rank, count; float scale; };
+
+// Which sequences share an adapter, made on the device from ids: the sequences sorted by adapter, tiles of `rows` rows and, for the sums over rows,
+// chunks of `chunk` rows, none of them of two adapters.  The rows of an adapter: its sequences in order, each one's T frames.  Keys: the adapters, count
+// for sequences without one, count + 1 for ids out of range.
+struct AdaptPlan {
+    int rows, chunk;          // rows of a tile and of a chunk (0: no chunks)
+    int max_tiles, max_chunks;
+    size_t counts, perm, first, tiles, chunks, first_chunk, bytes;      // byte offsets from the plan's start
+};
+// counts: {tiles, chunks}; first [count + 3]: a key's first place in perm; first_chunk [count + 1]; tiles and chunks: {key, first row, its rows, first place in perm}
+AdaptPlan adapt_plan(const AdaptShape& s, int rows, int chunk);
+// Rows of a tile: 16 for a frame or few rows of an adapter, else 64.
+inline int adapter_tile_rows(const AdaptShape& s) { return s.T <= 16 && (long long)s.T * s.B <= 2048 ? 16 : 64; }
+hipError_t launch_adapt_plan(const AdaptShape& s, const AdaptPlan& p, const int32_t* ids, char* plan, hipStream_t st);
+
+// y [M][N] = x [M][K] W^T + b + scale t B_a^T, t [M][rank] = x A_a^T.  W [N][K], A [count][rank][K], Bm [count][N][rank].
+struct ProjectArgs {
+    AdaptShape s;
+    AdaptPlan p;
+    const char* plan;
+    const void *x, *W, *b, *A, *Bm;      // b null: none
+    void* y;                             // null: only t is wanted
+    float* t;                            // null: not wanted
+};
+hipError_t launch_adapt_project(const ProjectArgs& a, DType type, hipStream_t st);
+
+// W^T [K][N], A_a^T [K][rank], B_a^T [rank][N] of all adapters
+struct TransposeArgs { AdaptShape s; const void *W, *A, *Bm; void *Wt, *At, *Bt; };
+hipError_t launch_adapt_transpose(const TransposeArgs& a, DType type, hipStream_t st);
+
+// dA_a [rank][K] = scale sum q^T x, dB_a [N][rank] = scale sum dy^T t over an adapter's rows; zero for an adapter without any
+struct AdaptGradArgs {
+    AdaptShape s;
+    AdaptPlan p;
+    const char* plan;
+    const void *x, *dy;
+    const float *q, *t;                  // [M][rank]
+    float* part;                         // [chunks][rank][K + N]
+    float *dA, *dB;
+};
+hipError_t launch_adapt_grad(const AdaptGradArgs& a, DType type, hipStream_t st);
+
+}  // namespace blstm

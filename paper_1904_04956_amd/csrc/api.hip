@@ -3,17 +3,20 @@
 // kernels of gemm.hip, cell.hip, softmax.hip and update.hip.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <new>
 #include <string>
 #include <vector>
 
 #include "../../include/blstm_mi355.h"
+#include "adapters.hpp"
 #include "gemm.hpp"
 #include "kernels.hpp"
 #include "losses.hpp"
@@ -825,6 +828,54 @@ int muon_check(const char* name, const MuonArgs& a, int flags, int known, const 
     return BLSTM_OK;
 }
 
+// ---- low-rank adapters beside a projection ---------------------------------------------------------------------------
+// Where a call's scratch lies (byte offsets).
+struct AdapterScratch {
+    AdaptShape s;
+    DType type;
+    AdaptPlan plan;
+    size_t plan_at, q, part, wt, at, bt, gemm, gemm_bytes, bytes;
+};
+int adapter_sizes(const char* name, const adapter_config* c, int call, AdapterScratch* out) {
+    if (!c) return fail(BLSTM_ERR_NULL, "%s: null argument", name);
+    if (c->T < 1 || c->B < 1 || c->K < 1 || c->N < 1 || c->rank < 1 || c->rank > BLSTM_MAX_ADAPTER_RANK || c->count < 1 || c->count > BLSTM_MAX_ADAPTERS || (c->mode != 0 && c->mode != 1))
+        return fail(BLSTM_ERR_DIM, "%s: T, B, K and N must be positive, rank in 1..%d, count in 1..%d, mode 0 or 1", name, BLSTM_MAX_ADAPTER_RANK, BLSTM_MAX_ADAPTERS);
+    if (call != ADAPTER_FORWARD && call != ADAPTER_BACKWARD) return fail(BLSTM_ERR_DIM, "%s: no call %d", name, call);
+    const long long M = (long long)c->T * c->B, wide = (long long)c->K + c->N;
+    // (launches are sized in 32 bits: workgroups of tiles, and of 32 x 32 words of the adapters' transposes)
+    if (M > INT_MAX || (M / 16 + c->count + 2) * (wide / 128 + 2) > INT_MAX || (c->count * 4LL + c->N / 32 + 1) * (wide / 32 + 2) > INT_MAX)
+        return fail(BLSTM_ERR_DIM, "%s: T B below 2^31, T B (K + N) below 2^42 and count (K + N) below 2^33 are taken", name);
+    AdapterScratch& a = *out;
+    a = AdapterScratch{};
+    a.s = AdaptShape{c->T, c->B, c->K, c->N, c->rank, c->count, c->scale};
+    a.type = c->mode == 1 ? DT_BF16 : DT_F32;
+    const size_t e = c->mode == 1 ? 2 : 4;
+    // Rows of a chunk of the gradients' sums: about 64 chunks if one adapter has all rows
+    const int chunk = call == ADAPTER_FORWARD ? 0 : std::max(64, (int)((M + 4095) / 4096) * 64);
+    a.plan = adapt_plan(a.s, adapter_tile_rows(a.s), chunk);
+    size_t at = up256(a.plan.bytes);
+    auto take = [&](size_t n) { const size_t was = at; at += up256(n); return was; };
+    if (call == ADAPTER_BACKWARD) {
+        a.q = take((size_t)M * c->rank * 4);
+        a.part = take((size_t)a.plan.max_chunks * c->rank * wide * 4);
+        a.wt = take((size_t)c->K * c->N * e);
+        a.at = take((size_t)c->count * c->rank * c->K * e);
+        a.bt = take((size_t)c->count * c->rank * c->N * e);
+        a.gemm_bytes = gemm_partial_bytes(c->N, c->K, (int)M, 1, a.type);
+        a.gemm = take(a.gemm_bytes);
+    }
+    a.bytes = at;
+    return BLSTM_OK;
+}
+int adapter_check(const char* name, const AdapterScratch& l, const void* scratch, size_t scratch_bytes, std::initializer_list<const void*> stored, std::initializer_list<const void*> words) {
+    const uintptr_t e = l.type == DT_BF16 ? 1 : 3;
+    for (const void* p : stored) if (reinterpret_cast<uintptr_t>(p) & e) return fail(BLSTM_ERR_ALIGN, "%s: a tensor is not aligned to its elements", name);
+    for (const void* p : words) if (reinterpret_cast<uintptr_t>(p) & 3) return fail(BLSTM_ERR_ALIGN, "%s: a tensor is not aligned to its elements", name);
+    if (!aligned16(scratch)) return fail(BLSTM_ERR_ALIGN, "%s: scratch must be 16-byte aligned", name);
+    if (scratch_bytes < l.bytes) return fail(BLSTM_ERR_WORKSPACE, "%s: %zu bytes of scratch given, %zu needed", name, scratch_bytes, l.bytes);
+    return BLSTM_OK;
+}
+
 void drop_deferred(blstm_ctx* ctx) {
     if (ctx->pend_z) ctx->pend_z = nullptr;
     if (ctx->twin && ctx->twin->pend_z) ctx->twin->pend_z = nullptr;
@@ -1561,6 +1612,58 @@ int muon_matrices_step(float* theta, void* shadow, const float* grad, float* vel
     const MuonArgs a{theta, static_cast<unsigned short*>(shadow), grad, momentum != 0.0f ? velocity : nullptr, nullptr, 0, lr, 0.0f, momentum, weight_decay, (flags & MUON_NESTEROV) != 0};
     rc = muon_check("muon_matrices_step", a, flags, MUON_NESTEROV, p, scratch, scratch_bytes);
     return rc != BLSTM_OK ? rc : check_hip(launch_muon(p, a, scratch, static_cast<hipStream_t>(stream)), "muon_matrices_step");
+}
+
+size_t adapter_scratch_bytes(const adapter_config* cfg, int call) {
+    AdapterScratch l;
+    return adapter_sizes("adapter_scratch_bytes", cfg, call, &l) == BLSTM_OK ? l.bytes : 0;
+}
+
+int adapter_forward(const adapter_config* cfg, const void* W, const void* b, const void* A, const void* Bm, const int32_t* ids, const void* x, void* y, float* t,
+                    void* scratch, size_t scratch_bytes, void* stream) {
+    AdapterScratch l;
+    int rc = adapter_sizes("adapter_forward", cfg, ADAPTER_FORWARD, &l);
+    if (rc != BLSTM_OK) return rc;
+    if (!W || !A || !Bm || !ids || !x || !y || !scratch) return fail(BLSTM_ERR_NULL, "adapter_forward: null argument");
+    rc = adapter_check("adapter_forward", l, scratch, scratch_bytes, {W, b, A, Bm, x, y}, {ids, t});
+    if (rc != BLSTM_OK) return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    char* base = static_cast<char*>(scratch);
+    hipError_t e = launch_adapt_plan(l.s, l.plan, ids, base + l.plan_at, st);
+    if (e == hipSuccess) e = launch_adapt_project(ProjectArgs{l.s, l.plan, base + l.plan_at, x, W, b, A, Bm, y, t}, l.type, st);
+    return check_hip(e, "adapter_forward");
+}
+
+int adapter_backward(const adapter_config* cfg, const void* W, const void* A, const void* Bm, const int32_t* ids, const void* x, const float* t, const void* dy,
+                     void* dx, float* dA, float* dB, float* dW, float* db, void* scratch, size_t scratch_bytes, void* stream) {
+    AdapterScratch l;
+    int rc = adapter_sizes("adapter_backward", cfg, ADAPTER_BACKWARD, &l);
+    if (rc != BLSTM_OK) return rc;
+    if (!W || !A || !Bm || !ids || !x || !t || !dy || !dA || !dB || !scratch) return fail(BLSTM_ERR_NULL, "adapter_backward: null argument");
+    if (db && !dW) return fail(BLSTM_ERR_NULL, "adapter_backward: db needs dW");
+    rc = adapter_check("adapter_backward", l, scratch, scratch_bytes, {W, A, Bm, x, dy, dx}, {ids, t, dA, dB, dW, db});
+    if (rc != BLSTM_OK) return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    char* base = static_cast<char*>(scratch);
+    const char* plan = base + l.plan_at;
+    float* q = reinterpret_cast<float*>(base + l.q);
+    hipError_t e = launch_adapt_plan(l.s, l.plan, ids, base + l.plan_at, st);
+    if (e == hipSuccess) e = launch_adapt_transpose(TransposeArgs{l.s, W, A, Bm, base + l.wt, base + l.at, base + l.bt}, l.type, st);
+    // dx and q: the forward pass of dy with the transposed weights, x's part taken by dy and A's by B_a^T
+    AdaptShape turned = l.s;
+    turned.K = l.s.N; turned.N = l.s.K;
+    if (e == hipSuccess) e = launch_adapt_project(ProjectArgs{turned, l.plan, plan, dy, base + l.wt, nullptr, base + l.bt, base + l.at, dx, q}, l.type, st);
+    if (e == hipSuccess) e = launch_adapt_grad(AdaptGradArgs{l.s, l.plan, plan, x, dy, q, t, reinterpret_cast<float*>(base + l.part), dA, dB}, l.type, st);
+    if (e == hipSuccess && dW) {
+        GemmDesc d{};
+        d.nseg = 1; d.batch = 1; d.in_type = l.type; d.out_type = DT_F32;
+        d.partial = reinterpret_cast<float*>(base + l.gemm); d.partial_bytes = l.gemm_bytes;
+        d.M = l.s.N; d.N = l.s.K; d.atrans = true; d.btrans = true;
+        d.seg[0] = GemmSeg{dy, x, l.s.N, l.s.K, 0, 0, l.s.T * l.s.B};
+        d.C = dW; d.ldc = l.s.K; d.rowsum = db;
+        e = launch_gemm(d, st);
+    }
+    return check_hip(e, "adapter_backward");
 }
 
 int adpsgd_mix(float* const* theta, void* const* shadow, size_t n, int R, const int32_t* partner, void* stream) {
