@@ -512,6 +512,217 @@ __global__ __launch_bounds__(256) void ns_gram_sum_kernel(MuonPlan p, _Float16* 
     }
 }
 
+// ---- small matrices: all steps of a matrix in one workgroup -----------------------------------------------------------------
+// What the general path spends on them is twenty launches of a few microseconds.  A matrix whose short side is at most 64 and which fits LDS is read
+// once, taken through the five steps there and written once, by sixteen wavefronts; the tensors that are not orthogonalised are further workgroups of the same
+// launch.  [m][n] with m <= n in LDS as two planes of halves (rows of n + 8, so that sixteen rows' chunks spread over the banks); all products use both planes.
+constexpr int SMALL_THREADS = 1024, SMALL_SIDE = 64, SMALL_LDS = 160 * 1024 - 256;
+struct SmallLds { int ldn, lds, x, s, b, red, d, bytes; };      // row lengths in halves; byte offsets
+__host__ __device__ inline SmallLds small_lds(int m, int n, int mb) {
+    SmallLds l{};
+    const int mp = 16 * mb, kp = (mp + 31) / 32 * 32;
+    l.ldn = (n + 31) / 32 * 32 + 8;
+    l.lds = kp + 8;
+    l.x = 0;
+    l.s = l.x + 2 * mp * l.ldn * 2;
+    l.b = l.s + 2 * mp * l.lds * 2;
+    l.red = l.b + 2 * mp * l.lds * 2;
+    l.d = l.red + (16 / (mb * mb)) * mp * mp * 4;
+    l.bytes = l.d + 2 * mp * 4;
+    (void)m;
+    return l;
+}
+__device__ __forceinline__ void mma_halves(f32x4_t& acc, const uint4 (&a)[2], const uint4 (&b)[2]) {
+    auto one = [&](const uint4& x, const uint4& y) { acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, x), __builtin_bit_cast(f16x8_t, y), acc, 0, 0, 0); };
+    one(a[1], b[0]); one(a[0], b[1]); one(a[0], b[0]);
+}
+template <int MB>
+__global__ __launch_bounds__(SMALL_THREADS) void muon_small_kernel(MuonPlan p, MuonArgs a) {
+    extern __shared__ uint4 smem[];
+    __shared__ double lds_sum[16];
+    constexpr int MP = 16 * MB, TILES = MB * MB, PARTS = 16 / TILES, KS = (MP + 31) / 32;
+    const MuonGroup& g = p.g[group_of(p, blockIdx.x, [](const MuonGroup& x) { return x.apply0; })];
+    const int local = blockIdx.x - g.apply0, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    auto direction = [&](float gr, float v) { return !a.velocity ? gr : a.nesterov ? gr + a.momentum * v : v; };
+    if (!g.ortho) {
+        const int k = local / g.chunks;
+        const long long size = (long long)g.rows * g.cols, e0 = (long long)(local % g.chunks) * FLAT, at = tensor_at(g, k) + e0;
+        const int len = (int)min((long long)FLAT, size - e0);
+        for (int i = tid; i < len; i += SMALL_THREADS) {
+            const float gr = a.grad[at + i];
+            float v = 0.0f;
+            if (a.velocity) { v = a.momentum * a.velocity[at + i] + gr; a.velocity[at + i] = v; }
+            const float w = a.theta[at + i] - a.lr_rest * direction(gr, v);
+            a.theta[at + i] = w;
+            if (a.shadow) a.shadow[at + i] = f2bf(w);
+        }
+        return;
+    }
+    const long long at = tensor_at(g, local);
+    const int size = g.rows * g.cols, n = max(g.rows, g.cols);
+    const bool tall = g.tall != 0;
+    const SmallLds l = small_lds(min(g.rows, g.cols), n, MB);
+    char* base = reinterpret_cast<char*>(smem);
+    _Float16* X = reinterpret_cast<_Float16*>(base + l.x);
+    _Float16* S = reinterpret_cast<_Float16*>(base + l.s);
+    _Float16* Bq = reinterpret_cast<_Float16*>(base + l.b);
+    float* red = reinterpret_cast<float*>(base + l.red);
+    float* sd = reinterpret_cast<float*>(base + l.d);
+    float* bd = sd + MP;
+    const int xp = MP * l.ldn, sp = MP * l.lds;             // elements of a plane
+    for (int i = tid; i < (l.red - l.x) / 16; i += SMALL_THREADS) smem[i] = make_uint4(0u, 0u, 0u, 0u);
+    __syncthreads();
+    // Eight elements a thread on their way at a time.  d waits in LDS for its norm, its bits' upper half where the first half will be and the lower
+    // half where the second one will be; a thread comes back to its own elements.
+    auto place = [&](int i) { const int r = i / g.cols, c = i - r * g.cols; return tall ? c * l.ldn + r : r * l.ldn + c; };
+    auto eight = [&](auto&& f) {
+        for (int i0 = tid; i0 < size; i0 += 8 * SMALL_THREADS) f([&](int q) { return min(i0 + q * SMALL_THREADS, size - 1); }, [&](int q) { return i0 + q * SMALL_THREADS < size; });
+    };
+    unsigned short* bits = reinterpret_cast<unsigned short*>(X);
+    double sum = 0.0;
+    eight([&](auto at_q, auto in) {
+        float gr[8], v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) { gr[q] = a.grad[at + at_q(q)]; v[q] = a.velocity ? a.velocity[at + at_q(q)] : 0.0f; }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) if (in(q)) {
+            if (a.velocity) { v[q] = a.momentum * v[q] + gr[q]; a.velocity[at + at_q(q)] = v[q]; }
+            const float d = direction(gr[q], v[q]);
+            sum += (double)d * d;
+            const unsigned w = __builtin_bit_cast(unsigned, d);
+            const int o = place(at_q(q));
+            bits[o] = (unsigned short)(w >> 16);
+            bits[xp + o] = (unsigned short)w;
+        }
+    });
+    for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+    if (lane == 0) lds_sum[wave] = sum;
+    __syncthreads();
+    double norm2 = 0.0;
+    for (int i = 0; i < 16; ++i) norm2 += lds_sum[i];
+    const double scale = norm2 == 0.0 ? 0.0 : UP / sqrt(norm2);
+    const float whole = norm2 <= 1.7e308 ? 0.0f : __builtin_nanf("");
+#pragma unroll 4
+    for (int i = tid; i < size; i += SMALL_THREADS) {
+        const int o = place(i);
+        const float d = (float)(__builtin_bit_cast(float, (unsigned)bits[o] << 16 | bits[xp + o]) * scale) + whole;
+        const _Float16 h = (_Float16)d;
+        X[o] = h;
+        X[xp + o] = (_Float16)(d - (float)h);
+    }
+    __syncthreads();
+    const int fr = lane & 15, fg = lane >> 4, ksteps = (n + 31) / 32, cblocks = (n + 15) / 16;
+    const int tile = wave % TILES, part = wave / TILES, ti = tile / MB, tj = tile % MB;
+    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+    auto row_frag = [&](uint4 (&f)[2], const _Float16* m, int plane, int ld, int row, int k) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) f[q] = *reinterpret_cast<const uint4*>(m + q * plane + row * ld + k);
+    };
+    for (int step = 0; step < NS_STEPS; ++step) {
+        {   // S = X X^T: a wavefront one tile, every PARTS-th stretch of 32 columns
+            f32x4_t acc{};
+            for (int k = part; k < ksteps; k += PARTS) {
+                uint4 x[2], y[2];
+                row_frag(x, X, xp, l.ldn, 16 * ti + fr, 32 * k + 8 * fg);
+                row_frag(y, X, xp, l.ldn, 16 * tj + fr, 32 * k + 8 * fg);
+                mma_halves(acc, x, y);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) red[part * MP * MP + (16 * ti + 4 * fg + e) * MP + 16 * tj + fr] = acc[e];
+        }
+        __syncthreads();
+        for (int i = tid; i < MP * MP; i += SMALL_THREADS) {
+            float v = 0.0f;
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) v += red[q * MP * MP + i];
+            v *= DOWN;
+            const int r = i / MP, c = i % MP;
+            if (r == c) { sd[r] = DOWN * v; v = 0.0f; }
+            const _Float16 h = (_Float16)v;
+            S[r * l.lds + c] = h;
+            S[sp + r * l.lds + c] = (_Float16)(v - (float)h);
+        }
+        __syncthreads();
+        if (wave < TILES) {     // B = b S + c S^2
+            f32x4_t acc{};
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                uint4 x[2], y[2];
+                row_frag(x, S, sp, l.lds, 16 * ti + fr, 32 * k + 8 * fg);
+                row_frag(y, S, sp, l.lds, 16 * tj + fr, 32 * k + 8 * fg);
+                mma_halves(acc, x, y);
+            }
+            const int c = 16 * tj + fr;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = 16 * ti + 4 * fg + e, o = r * l.lds + c;
+                const float y = (float)S[o] + (float)S[sp + o], full = NS_C * DOWN * acc[e];
+                if (r == c) bd[r] = NS_B * sd[r] + NS_C * sd[r] * sd[r] + DOWN * full;
+                const float v = r == c ? 0.0f : NS_B * y + NS_C * (sd[r] + sd[c]) * y + full;
+                const _Float16 h = (_Float16)v;
+                Bq[o] = h;
+                Bq[sp + o] = (_Float16)(v - (float)h);
+            }
+        }
+        __syncthreads();
+        // X = a X + B X: a wavefront sixteen columns, which nobody else reads or writes
+        for (int cb = wave; cb < cblocks; cb += 16) {
+            f32x4_t acc[MB];
+#pragma unroll
+            for (int i = 0; i < MB; ++i) acc[i] = f32x4_t{};
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                uint4 y[2];
+                const int kr = 32 * k + 8 * fg;            // (rows beyond the matrix: zero, from a place that exists)
+                const bool in = kr < MP;
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const char* from = reinterpret_cast<const char*>(X + q * xp + ((in ? kr : 0) + (fr >> 2)) * l.ldn + 16 * cb + (fr & 3) * 4);
+                    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)from);
+                    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(from + 4 * l.ldn * 2));
+                    const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+                    y[q] = in ? make_uint4(l2.x, l2.y, h2.x, h2.y) : none;
+                }
+#pragma unroll
+                for (int i = 0; i < MB; ++i) {
+                    uint4 x[2];
+                    row_frag(x, Bq, sp, l.lds, 16 * i + fr, 32 * k + 8 * fg);
+                    mma_halves(acc[i], x, y);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = 16 * i + 4 * fg + e, o = r * l.ldn + 16 * cb + fr;
+                    const float v = (NS_A + bd[r]) * ((float)X[o] + (float)X[xp + o]) + DOWN * acc[i][e];
+                    const _Float16 h = (_Float16)v;
+                    X[o] = h;
+                    X[xp + o] = (_Float16)(v - (float)h);
+                }
+        }
+        __syncthreads();
+    }
+    const float shrink = 1.0f - a.lr * a.decay, step = a.lr * sqrtf(fmaxf(1.0f, (float)g.rows / (float)g.cols)) * DOWN;
+    eight([&](auto at_q, auto in) {
+        float w[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) w[q] = a.theta ? a.theta[at + at_q(q)] : 0.0f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) if (in(q)) {
+            const int o = place(at_q(q));
+            const long long to = at + at_q(q);
+            const float v = (float)X[o] + (float)X[xp + o];
+            if (a.theta) {
+                const float x = shrink * w[q] - step * v;
+                a.theta[to] = x;
+                if (a.shadow) a.shadow[to] = f2bf(x);
+            } else if (a.out_bf16) static_cast<unsigned short*>(a.out)[to] = f2bf(DOWN * v);
+            else static_cast<float*>(a.out)[to] = DOWN * v;
+        }
+    });
+}
+
 constexpr int lds_bytes(int TM, int TN, bool split, bool one) {
     const int loop = (one ? 1 : 2) * (split ? 2 : 1) * 64 * (TM + TN) * 128, values = 4 * 32 * (32 * TN + 4) * 4;
     return loop > values ? loop : values;
@@ -545,6 +756,34 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
     p.exact = exact;
     const long long most = 0x7FFFFFFF;
     auto up = [](long long v, long long m) { return (v + m - 1) / m * m; };
+    // small matrices only: a workgroup each
+    int side = 0;
+    for (int i = 0; i < n; ++i) if (g[i].ortho) side = std::max(side, std::min(g[i].rows, g[i].cols));
+    if (side >= 1 && side <= SMALL_SIDE) {
+        p.small = side <= 16 ? 1 : side <= 32 ? 2 : 4;
+        bool fits = true;
+        for (int i = 0; i < n; ++i) if (g[i].ortho) {
+            const int longer = std::max(g[i].rows, g[i].cols);
+            fits = fits && longer <= 4096;
+            if (fits) p.lds = std::max(p.lds, small_lds(std::min(g[i].rows, g[i].cols), longer, p.small).bytes);
+        }
+        if (fits && p.lds <= SMALL_LDS) {
+            long long groups = 0;
+            for (int i = 0; i < n; ++i) {
+                MuonGroup& q = p.g[i] = g[i];
+                q.tall = q.rows > q.cols;
+                q.chunks = (int)(((long long)q.rows * q.cols + FLAT - 1) / FLAT);
+                q.apply0 = (int)groups;
+                groups += (long long)q.count * (q.ortho ? 1 : q.chunks);
+                if (groups > most) return false;
+            }
+            p.tile = 3;
+            p.applies = (int)groups;
+            p.bytes = 256;
+            *out = p;
+            return true;
+        }
+    }
     auto tiles = [&](int high, int wide) {              // of the last product
         long long t = 0;
         for (int i = 0; i < n; ++i) if (g[i].ortho) t += (long long)g[i].count * ((g[i].rows + high - 1) / high) * ((g[i].cols + wide - 1) / wide);
@@ -601,6 +840,12 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
 }
 
 hipError_t launch_muon(const MuonPlan& p, const MuonArgs& a, void* scratch, hipStream_t st) {
+    if (p.tile == 3) {
+        if (p.small == 1) muon_small_kernel<1><<<p.applies, SMALL_THREADS, p.lds, st>>>(p, a);
+        else if (p.small == 2) muon_small_kernel<2><<<p.applies, SMALL_THREADS, p.lds, st>>>(p, a);
+        else muon_small_kernel<4><<<p.applies, SMALL_THREADS, p.lds, st>>>(p, a);
+        return hipGetLastError();
+    }
     _Float16* ws = static_cast<_Float16*>(scratch);
     double* sums = reinterpret_cast<double*>(static_cast<char*>(scratch) + p.sums_at);
     float* diag = reinterpret_cast<float*>(static_cast<char*>(scratch) + p.diag_at);
