@@ -517,6 +517,7 @@ __global__ __launch_bounds__(256) void ns_gram_sum_kernel(MuonPlan p, _Float16* 
 // once, taken through the five steps there and written once, by sixteen wavefronts; the tensors that are not orthogonalised are further workgroups of the same
 // launch.  [m][n] with m <= n in LDS as two planes of halves (rows of n + 8, so that sixteen rows' chunks spread over the banks); all products use both planes.
 constexpr int SMALL_THREADS = 1024, SMALL_SIDE = 64, SMALL_LDS = 160 * 1024 - 256;
+constexpr int small_parts(int mb) { return mb == 1 ? 16 : mb == 2 ? 4 : 1; }   // stretches of the columns that a tile of S is summed over
 struct SmallLds { int ldn, lds, x, s, b, red, d, bytes; };      // row lengths in halves; byte offsets
 __host__ __device__ inline SmallLds small_lds(int m, int n, int mb) {
     SmallLds l{};
@@ -527,20 +528,34 @@ __host__ __device__ inline SmallLds small_lds(int m, int n, int mb) {
     l.s = l.x + 2 * mp * l.ldn * 2;
     l.b = l.s + 2 * mp * l.lds * 2;
     l.red = l.b + 2 * mp * l.lds * 2;
-    l.d = l.red + (16 / (mb * mb)) * mp * mp * 4;
-    l.bytes = l.d + 2 * mp * 4;
+    l.d = l.red + (small_parts(mb) > 1 ? small_parts(mb) : 0) * mp * mp * 4;
+    l.bytes = l.d + mp * 4;
     (void)m;
     return l;
 }
-__device__ __forceinline__ void mma_halves(f32x4_t& acc, const uint4 (&a)[2], const uint4 (&b)[2]) {
-    auto one = [&](const uint4& x, const uint4& y) { acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, x), __builtin_bit_cast(f16x8_t, y), acc, 0, 0, 0); };
-    one(a[1], b[0]); one(a[0], b[1]); one(a[0], b[0]);
+// (three chains, so that none waits for another's end)
+__device__ __forceinline__ void mma_halves(f32x4_t (&acc)[3], const uint4 (&a)[2], const uint4 (&b)[2]) {
+    auto one = [&](f32x4_t& c, const uint4& x, const uint4& y) { c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, x), __builtin_bit_cast(f16x8_t, y), c, 0, 0, 0); };
+    one(acc[0], a[1], b[0]); one(acc[1], a[0], b[1]); one(acc[2], a[0], b[0]);
+}
+typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ f32x4_t four(const _Float16* at, int plane) {
+    const f16x4_t h = *reinterpret_cast<const f16x4_t*>(at), l = *reinterpret_cast<const f16x4_t*>(at + plane);
+    return f32x4_t{(float)h[0] + (float)l[0], (float)h[1] + (float)l[1], (float)h[2] + (float)l[2], (float)h[3] + (float)l[3]};
+}
+__device__ __forceinline__ void put_four(_Float16* at, int plane, const f32x4_t& v) {
+    f16x4_t h, l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { h[e] = (_Float16)v[e]; l[e] = (_Float16)(v[e] - (float)h[e]); }
+    *reinterpret_cast<f16x4_t*>(at) = h;
+    *reinterpret_cast<f16x4_t*>(at + plane) = l;
 }
 template <int MB>
 __global__ __launch_bounds__(SMALL_THREADS) void muon_small_kernel(MuonPlan p, MuonArgs a) {
     extern __shared__ uint4 smem[];
     __shared__ double lds_sum[16];
-    constexpr int MP = 16 * MB, TILES = MB * MB, PARTS = 16 / TILES, KS = (MP + 31) / 32;
+    constexpr int MP = 16 * MB, TILES = MB * MB, PARTS = small_parts(MB), KS = (MP + 31) / 32, PLACES = MB <= 2 ? 2 : 1;
+    constexpr bool KEEP = MB <= 2;          // B's fragments stay in registers
     const MuonGroup& g = p.g[group_of(p, blockIdx.x, [](const MuonGroup& x) { return x.apply0; })];
     const int local = blockIdx.x - g.apply0, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     auto direction = [&](float gr, float v) { return !a.velocity ? gr : a.nesterov ? gr + a.momentum * v : v; };
@@ -568,19 +583,29 @@ __global__ __launch_bounds__(SMALL_THREADS) void muon_small_kernel(MuonPlan p, M
     _Float16* Bq = reinterpret_cast<_Float16*>(base + l.b);
     float* red = reinterpret_cast<float*>(base + l.red);
     float* sd = reinterpret_cast<float*>(base + l.d);
-    float* bd = sd + MP;
     const int xp = MP * l.ldn, sp = MP * l.lds;             // elements of a plane
     for (int i = tid; i < (l.red - l.x) / 16; i += SMALL_THREADS) smem[i] = make_uint4(0u, 0u, 0u, 0u);
     __syncthreads();
     // Eight elements a thread on their way at a time.  d waits in LDS for its norm, its bits' upper half where the first half will be and the lower
     // half where the second one will be; a thread comes back to its own elements.
-    auto place = [&](int i) { const int r = i / g.cols, c = i - r * g.cols; return tall ? c * l.ldn + r : r * l.ldn + c; };
+    const int dr = SMALL_THREADS / g.cols, dc = SMALL_THREADS - dr * g.cols, r_first = tid / g.cols, c_first = tid - r_first * g.cols;
+    const int by_row = tall ? 1 : l.ldn, by_col = tall ? l.ldn : 1;
     auto eight = [&](auto&& f) {
-        for (int i0 = tid; i0 < size; i0 += 8 * SMALL_THREADS) f([&](int q) { return min(i0 + q * SMALL_THREADS, size - 1); }, [&](int q) { return i0 + q * SMALL_THREADS < size; });
+        int r = r_first, c = c_first;
+        for (int i0 = tid; i0 < size; i0 += 8 * SMALL_THREADS) {
+            int place[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                place[q] = r * by_row + c * by_col;
+                r += dr; c += dc;
+                if (c >= g.cols) { c -= g.cols; ++r; }
+            }
+            f([&](int q) { return min(i0 + q * SMALL_THREADS, size - 1); }, [&](int q) { return i0 + q * SMALL_THREADS < size; }, place);
+        }
     };
     unsigned short* bits = reinterpret_cast<unsigned short*>(X);
     double sum = 0.0;
-    eight([&](auto at_q, auto in) {
+    eight([&](auto at_q, auto in, const int (&place)[8]) {
         float gr[8], v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) { gr[q] = a.grad[at + at_q(q)]; v[q] = a.velocity ? a.velocity[at + at_q(q)] : 0.0f; }
@@ -590,7 +615,7 @@ __global__ __launch_bounds__(SMALL_THREADS) void muon_small_kernel(MuonPlan p, M
             const float d = direction(gr[q], v[q]);
             sum += (double)d * d;
             const unsigned w = __builtin_bit_cast(unsigned, d);
-            const int o = place(at_q(q));
+            const int o = place[q];
             bits[o] = (unsigned short)(w >> 16);
             bits[xp + o] = (unsigned short)w;
         }
@@ -602,14 +627,17 @@ __global__ __launch_bounds__(SMALL_THREADS) void muon_small_kernel(MuonPlan p, M
     for (int i = 0; i < 16; ++i) norm2 += lds_sum[i];
     const double scale = norm2 == 0.0 ? 0.0 : UP / sqrt(norm2);
     const float whole = norm2 <= 1.7e308 ? 0.0f : __builtin_nanf("");
-#pragma unroll 4
-    for (int i = tid; i < size; i += SMALL_THREADS) {
-        const int o = place(i);
-        const float d = (float)(__builtin_bit_cast(float, (unsigned)bits[o] << 16 | bits[xp + o]) * scale) + whole;
-        const _Float16 h = (_Float16)d;
-        X[o] = h;
-        X[xp + o] = (_Float16)(d - (float)h);
-    }
+    eight([&](auto, auto in, const int (&place)[8]) {
+        float d[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) if (in(q)) d[q] = (float)(__builtin_bit_cast(float, (unsigned)bits[place[q]] << 16 | bits[xp + place[q]]) * scale) + whole;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) if (in(q)) {
+            const _Float16 h = (_Float16)d[q];
+            X[place[q]] = h;
+            X[xp + place[q]] = (_Float16)(d[q] - (float)h);
+        }
+    });
     __syncthreads();
     const int fr = lane & 15, fg = lane >> 4, ksteps = (n + 31) / 32, cblocks = (n + 15) / 16;
     const int tile = wave % TILES, part = wave / TILES, ti = tile / MB, tj = tile % MB;
@@ -618,33 +646,44 @@ __global__ __launch_bounds__(SMALL_THREADS) void muon_small_kernel(MuonPlan p, M
 #pragma unroll
         for (int q = 0; q < 2; ++q) f[q] = *reinterpret_cast<const uint4*>(m + q * plane + row * ld + k);
     };
+#pragma unroll 1
     for (int step = 0; step < NS_STEPS; ++step) {
-        {   // S = X X^T: a wavefront one tile, every PARTS-th stretch of 32 columns
-            f32x4_t acc{};
+        // A lane's four results lie below one another in a column; S and B are symmetric, and X's tile is computed transposed: so they leave as four
+        // neighbours of a row.
+        // S = X X^T: a wavefront one tile, every PARTS-th stretch of 32 columns
+        auto put_s = [&](int r, int c, f32x4_t v) {         // columns c .. c + 3
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] *= DOWN;
+                if (r == c + e) { sd[r] = DOWN * v[e]; v[e] = 0.0f; }
+            }
+            put_four(S + r * l.lds + c, sp, v);
+        };
+        if (wave < TILES * PARTS) {
+            f32x4_t acc[3] = {};
+#pragma unroll 2
             for (int k = part; k < ksteps; k += PARTS) {
                 uint4 x[2], y[2];
                 row_frag(x, X, xp, l.ldn, 16 * ti + fr, 32 * k + 8 * fg);
-                row_frag(y, X, xp, l.ldn, 16 * tj + fr, 32 * k + 8 * fg);
+                if constexpr (MB > 1) row_frag(y, X, xp, l.ldn, 16 * tj + fr, 32 * k + 8 * fg); else { y[0] = x[0]; y[1] = x[1]; }
                 mma_halves(acc, x, y);
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) red[part * MP * MP + (16 * ti + 4 * fg + e) * MP + 16 * tj + fr] = acc[e];
+            const f32x4_t v = acc[2] + (acc[0] + acc[1]);
+            if constexpr (PARTS > 1) *reinterpret_cast<f32x4_t*>(red + part * MP * MP + (16 * tj + fr) * MP + 16 * ti + 4 * fg) = v;
+            else put_s(16 * tj + fr, 16 * ti + 4 * fg, v);
         }
         __syncthreads();
-        for (int i = tid; i < MP * MP; i += SMALL_THREADS) {
-            float v = 0.0f;
+        if constexpr (PARTS > 1) {
+            if (tid < MP * MP / 4) {
+                f32x4_t v{};
 #pragma unroll
-            for (int q = 0; q < PARTS; ++q) v += red[q * MP * MP + i];
-            v *= DOWN;
-            const int r = i / MP, c = i % MP;
-            if (r == c) { sd[r] = DOWN * v; v = 0.0f; }
-            const _Float16 h = (_Float16)v;
-            S[r * l.lds + c] = h;
-            S[sp + r * l.lds + c] = (_Float16)(v - (float)h);
+                for (int q = 0; q < PARTS; ++q) v += *reinterpret_cast<const f32x4_t*>(red + q * MP * MP + 4 * tid);
+                put_s(4 * tid / MP, 4 * tid % MP, v);
+            }
+            __syncthreads();
         }
-        __syncthreads();
-        if (wave < TILES) {     // B = b S + c S^2
-            f32x4_t acc{};
+        if (wave < TILES) {     // B = a + b S + c S^2: both planes are multiplied, so that its diagonal may lie in them
+            f32x4_t acc[3] = {};
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 uint4 x[2], y[2];
@@ -652,65 +691,69 @@ __global__ __launch_bounds__(SMALL_THREADS) void muon_small_kernel(MuonPlan p, M
                 row_frag(y, S, sp, l.lds, 16 * tj + fr, 32 * k + 8 * fg);
                 mma_halves(acc, x, y);
             }
-            const int c = 16 * tj + fr;
+            const int r = 16 * tj + fr, c = 16 * ti + 4 * fg;
+            const float dr_ = sd[r];
+            const f32x4_t old = four(S + r * l.lds + c, sp), dc_ = *reinterpret_cast<const f32x4_t*>(sd + c);
+            f32x4_t v;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int r = 16 * ti + 4 * fg + e, o = r * l.lds + c;
-                const float y = (float)S[o] + (float)S[sp + o], full = NS_C * DOWN * acc[e];
-                if (r == c) bd[r] = NS_B * sd[r] + NS_C * sd[r] * sd[r] + DOWN * full;
-                const float v = r == c ? 0.0f : NS_B * y + NS_C * (sd[r] + sd[c]) * y + full;
-                const _Float16 h = (_Float16)v;
-                Bq[o] = h;
-                Bq[sp + o] = (_Float16)(v - (float)h);
+                const float full = NS_C * DOWN * (acc[2][e] + (acc[0][e] + acc[1][e]));
+                v[e] = r == c + e ? UP * (NS_A + NS_B * dr_ + NS_C * dr_ * dr_) + full : NS_B * old[e] + NS_C * (dr_ + dc_[e]) * old[e] + full;
             }
+            put_four(Bq + r * l.lds + c, sp, v);
         }
         __syncthreads();
-        // X = a X + B X: a wavefront sixteen columns, which nobody else reads or writes
-        for (int cb = wave; cb < cblocks; cb += 16) {
-            f32x4_t acc[MB];
+        // X = B X: a wavefront whole columns, sixteen at a time (of low matrices in two places), which nobody else reads or writes; all
+        // that they need is read before the first is written
+        uint4 fb[KEEP ? MB : 1][KEEP ? KS : 1][2];
+        if constexpr (KEEP) {
 #pragma unroll
-            for (int i = 0; i < MB; ++i) acc[i] = f32x4_t{};
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int k = 0; k < KS; ++k) row_frag(fb[i][k], Bq, sp, l.lds, 16 * i + fr, 32 * k + 8 * fg);
+        }
+#pragma unroll 1
+        for (int cb = wave; cb < cblocks; cb += 16 * PLACES) {
+            const int at_col[2] = {16 * cb, 16 * (cb + 16 < cblocks ? cb + 16 : cb)};
+            f32x4_t acc[PLACES][MB][3] = {};
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                uint4 y[2];
+                uint4 y[PLACES][2];
                 const int kr = 32 * k + 8 * fg;            // (rows beyond the matrix: zero, from a place that exists)
                 const bool in = kr < MP;
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const char* from = reinterpret_cast<const char*>(X + q * xp + ((in ? kr : 0) + (fr >> 2)) * l.ldn + 16 * cb + (fr & 3) * 4);
-                    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)from);
-                    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(from + 4 * l.ldn * 2));
-                    const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
-                    y[q] = in ? make_uint4(l2.x, l2.y, h2.x, h2.y) : none;
-                }
+                for (int j = 0; j < PLACES; ++j)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const char* from = reinterpret_cast<const char*>(X + h * xp + ((in ? kr : 0) + (fr >> 2)) * l.ldn + at_col[j] + (fr & 3) * 4);
+                        const uint2 l2 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)from));
+                        const uint2 h2 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(from + 4 * l.ldn * 2)));
+                        y[j][h] = in ? make_uint4(l2.x, l2.y, h2.x, h2.y) : none;
+                    }
 #pragma unroll
                 for (int i = 0; i < MB; ++i) {
                     uint4 x[2];
-                    row_frag(x, Bq, sp, l.lds, 16 * i + fr, 32 * k + 8 * fg);
-                    mma_halves(acc[i], x, y);
+                    if constexpr (KEEP) { x[0] = fb[i][k][0]; x[1] = fb[i][k][1]; } else row_frag(x, Bq, sp, l.lds, 16 * i + fr, 32 * k + 8 * fg);
+#pragma unroll
+                    for (int j = 0; j < PLACES; ++j) mma_halves(acc[j][i], y[j], x);
                 }
             }
 #pragma unroll
             for (int i = 0; i < MB; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = 16 * i + 4 * fg + e, o = r * l.ldn + 16 * cb + fr;
-                    const float v = (NS_A + bd[r]) * ((float)X[o] + (float)X[xp + o]) + DOWN * acc[i][e];
-                    const _Float16 h = (_Float16)v;
-                    X[o] = h;
-                    X[xp + o] = (_Float16)(v - (float)h);
-                }
+                for (int j = 0; j < PLACES; ++j)            // (the same place twice where there is one block left)
+                    put_four(X + (16 * i + fr) * l.ldn + at_col[j] + 4 * fg, xp, DOWN * (acc[j][i][2] + (acc[j][i][0] + acc[j][i][1])));
         }
         __syncthreads();
     }
     const float shrink = 1.0f - a.lr * a.decay, step = a.lr * sqrtf(fmaxf(1.0f, (float)g.rows / (float)g.cols)) * DOWN;
-    eight([&](auto at_q, auto in) {
+    eight([&](auto at_q, auto in, const int (&place)[8]) {
         float w[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) w[q] = a.theta ? a.theta[at + at_q(q)] : 0.0f;
 #pragma unroll
         for (int q = 0; q < 8; ++q) if (in(q)) {
-            const int o = place(at_q(q));
+            const int o = place[q];
             const long long to = at + at_q(q);
             const float v = (float)X[o] + (float)X[xp + o];
             if (a.theta) {
@@ -760,7 +803,7 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
     int side = 0;
     for (int i = 0; i < n; ++i) if (g[i].ortho) side = std::max(side, std::min(g[i].rows, g[i].cols));
     if (side >= 1 && side <= SMALL_SIDE) {
-        p.small = side <= 16 ? 1 : side <= 32 ? 2 : 4;
+        p.small = (side + 15) / 16;
         bool fits = true;
         for (int i = 0; i < n; ++i) if (g[i].ortho) {
             const int longer = std::max(g[i].rows, g[i].cols);
@@ -843,6 +886,7 @@ hipError_t launch_muon(const MuonPlan& p, const MuonArgs& a, void* scratch, hipS
     if (p.tile == 3) {
         if (p.small == 1) muon_small_kernel<1><<<p.applies, SMALL_THREADS, p.lds, st>>>(p, a);
         else if (p.small == 2) muon_small_kernel<2><<<p.applies, SMALL_THREADS, p.lds, st>>>(p, a);
+        else if (p.small == 3) muon_small_kernel<3><<<p.applies, SMALL_THREADS, p.lds, st>>>(p, a);
         else muon_small_kernel<4><<<p.applies, SMALL_THREADS, p.lds, st>>>(p, a);
         return hipGetLastError();
     }
