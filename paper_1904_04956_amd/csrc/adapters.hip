@@ -16,19 +16,20 @@ namespace {
 // ---- which rows belong together ----------------------------------------------------------------------------------------
 // One workgroup: a stable counting sort of the sequences by key (the order within an adapter is the order of its sums), then the tables of tiles and
 // chunks.  64 sequences a wavefront at a time: a lane's rank among equal keys of its wavefront, and the wavefronts' counts in turn.
-constexpr int PLAN_THREADS = 1024;
-__global__ __launch_bounds__(PLAN_THREADS) void adapt_plan_kernel(AdaptShape s, AdaptPlan p, const int32_t* ids, char* plan) {
-    __shared__ int hist[ADAPT_MAX_COUNT + 2], first[ADAPT_MAX_COUNT + 3], tile0[ADAPT_MAX_COUNT + 3], chunk0[ADAPT_MAX_COUNT + 3], wave_sum[3][16];
+constexpr int PLAN_THREADS = 256;
+constexpr int plan_lds(int count) { return (4 * (count + 3) + 3 * (PLAN_THREADS / 64)) * 4; }
+__device__ __forceinline__ int key_of(int id, int count) { return id >= 0 && id < count ? id : id == -1 ? count : count + 1; }
+__device__ void make_plan(const AdaptShape& s, const AdaptPlan& p, const int32_t* ids, char* plan, int* lds) {
+    int *hist = lds, *first = hist + s.count + 3, *tile0 = first + s.count + 3, *chunk0 = tile0 + s.count + 3, *wave_sum = chunk0 + s.count + 3;
     int* counts = reinterpret_cast<int*>(plan + p.counts);
     int* perm = reinterpret_cast<int*>(plan + p.perm);
     const int keys = s.count + 2, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     for (int i = tid; i < keys; i += PLAN_THREADS) hist[i] = 0;
     __syncthreads();
-    auto key_of = [&](int b) { const int id = ids[b]; return id >= 0 && id < s.count ? id : id == -1 ? s.count : s.count + 1; };
     // a sequence's place among those of its key; kept in perm until the keys' places are known
     for (int b0 = 0; b0 < s.B; b0 += PLAN_THREADS) {
         const int b = b0 + tid;
-        const int key = b < s.B ? key_of(b) : -1;
+        const int key = b < s.B ? key_of(ids[b], s.count) : -1;
         int rank = 0, later = 0;
         for (int j = 0; j < 64; ++j) {
             const int k = __builtin_amdgcn_readlane(key, j);
@@ -57,11 +58,11 @@ __global__ __launch_bounds__(PLAN_THREADS) void adapt_plan_kernel(AdaptShape s, 
     for (int i = 0; i < 3; ++i) {
         int v = sum[i];
         for (int o = 1; o < 64; o <<= 1) { const int u = __shfl_up(v, o); if (lane >= o) v += u; }
-        if (lane == 63) wave_sum[i][wave] = v;
+        if (lane == 63) wave_sum[i * (PLAN_THREADS / 64) + wave] = v;
         before[i] = v - sum[i];
     }
     __syncthreads();
-    for (int i = 0; i < 3; ++i) for (int w = 0; w < wave; ++w) before[i] += wave_sum[i][w];
+    for (int i = 0; i < 3; ++i) for (int w = 0; w < wave; ++w) before[i] += wave_sum[i * (PLAN_THREADS / 64) + w];
     for (int i = 0; i < 3; ++i) sum[i] = before[i];
     for (int k = k0; k < k1; ++k) { first[k] = sum[0]; tile0[k] = sum[1]; chunk0[k] = sum[2]; add(k); }
     if (k1 == keys && k0 < keys) { first[keys] = sum[0]; tile0[keys] = sum[1]; chunk0[keys] = sum[2]; }
@@ -81,7 +82,11 @@ __global__ __launch_bounds__(PLAN_THREADS) void adapt_plan_kernel(AdaptShape s, 
     table(tile0, tiles, p.rows, reinterpret_cast<int4*>(plan + p.tiles));
     if (p.chunk) table(chunk0, chunks, p.chunk, reinterpret_cast<int4*>(plan + p.chunks));
     // (a lane reads the place that it wrote itself, and the sorted list lies behind the places)
-    for (int b = tid; b < s.B; b += PLAN_THREADS) perm[s.B + first[key_of(b)] + perm[b]] = b;
+    for (int b = tid; b < s.B; b += PLAN_THREADS) perm[s.B + first[key_of(ids[b], s.count)] + perm[b]] = b;
+}
+__global__ __launch_bounds__(PLAN_THREADS) void adapt_plan_kernel(AdaptShape s, AdaptPlan p, const int32_t* ids, char* plan) {
+    extern __shared__ int plan_words[];
+    make_plan(s, p, ids, plan, plan_words);
 }
 
 // ---- products of 16-row tiles ------------------------------------------------------------------------------------------
@@ -115,71 +120,186 @@ __device__ __forceinline__ uint4 load_chunk(const T* row, int k, int n) {
     }
 }
 
-// One pass over a tile's rows: 16 MR rows x 128 columns of y and all 16 RB columns of t.  A slab is 128 bytes of every row (x, W, A_a), through registers
-// into swizzled LDS, double-buffered; wavefront w multiplies columns 32 w .. of y and rows 16 w .. of t (MR 4) or, with one row block, wavefront 0 t.
+// A workgroup's tile: from the plan's table or, of up to FIND sequences, found in ids by every workgroup itself (a launch in front of this one costs ten
+// microseconds, looking for it one).  Adapters then come in the order of their first sequences.  False: there is no such tile.
+constexpr int FIND = 256, FIND_WORDS = 2 * FIND + 24;
+__device__ __forceinline__ bool find_tile(const ProjectArgs& a, int tile, int* lds, int4* what, const int** order) {
+    const AdaptShape& s = a.s;
+    if (a.plan) {
+        if (tile >= reinterpret_cast<const int*>(a.plan + a.p.counts)[0]) return false;
+        *what = reinterpret_cast<const int4*>(a.plan + a.p.tiles)[tile];
+        *order = reinterpret_cast<const int*>(a.plan + a.p.perm) + s.B + what->w;
+        return true;
+    }
+    int *keys = lds, *list = lds + FIND, *sums = list + FIND, *found = sums + 8;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
+    const int key = tid < s.B ? key_of(a.ids[tid], s.count) : -1;
+    if (tid < FIND) keys[tid] = key;
+    __syncthreads();
+    int rank = 0, size = 0;
+    for (int j = 0; j < s.B; j += 4) {
+        const int4 k = *reinterpret_cast<const int4*>(keys + j);
+        const int e0 = k.x == key, e1 = k.y == key, e2 = k.z == key, e3 = k.w == key;
+        size += e0 + e1 + e2 + e3;
+        rank += (e0 & (j < tid)) + (e1 & (j + 1 < tid)) + (e2 & (j + 2 < tid)) + (e3 & (j + 3 < tid));
+    }
+    const int rows = size * s.T, mine = tid < s.B && rank == 0 ? (rows + a.p.rows - 1) / a.p.rows : 0;
+    int upto = mine;
+    for (int o = 1; o < 64; o <<= 1) { const int u = __shfl_up(upto, o); if (lane >= o) upto += u; }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    int before = upto - mine, all = 0;
+    for (int w = 0; w < waves; ++w) { if (w < wave) before += sums[w]; all += sums[w]; }
+    if (tile >= all) return false;
+    if (tile >= before && tile < before + mine) {
+        const int r0 = (tile - before) * a.p.rows;
+        found[0] = key; found[1] = r0; found[2] = min(a.p.rows, rows - r0);
+    }
+    __syncthreads();
+    *what = make_int4(found[0], found[1], found[2], 0);
+    if (tid < s.B && key == what->x) list[rank] = tid;
+    __syncthreads();
+    *order = list;
+    return true;
+}
+__device__ __forceinline__ long long row_at(const AdaptShape& s, const int* order, int i) { const int j = i / s.T; return (long long)(i - j * s.T) * s.B + order[j]; }
+// the first V columns from c on of a row of B_a (zero beyond the rank)
+template <typename T>
+__device__ __forceinline__ uint4 low_chunk(const T* row, int c, int rank, bool vector) {
+    return vector ? load_chunk<T, true>(row, c, rank) : load_chunk<T, false>(row, c, rank);
+}
+
+// Few rows (a frame, a handful of rows an adapter): 16 rows x 32 columns.  What such a tile costs is the latency of its loads, so nothing is staged: eight wavefronts share the
+// contraction, each loads its fragments straight into registers, four steps at a time, and their sums meet in LDS.  s t B_a^T is then a dot product a
+// thread, in float.  One frame of one sequence (K 1024, N 256, rank 16): 16 us with the staged tile and its barriers, NOTE_ROWS here.
+constexpr int RN = 32, RWAVES = 8;
+template <typename T, int RB>
+__global__ __launch_bounds__(64 * RWAVES) void adapt_rows_kernel(ProjectArgs a, bool vector, bool low_vector) {
+    constexpr int V = Vec<T>::N, STEP = 4 * V, RP = 16 * RB, NB = RN / 16, DEEP = RB <= 2 ? 4 : RB == 4 ? 2 : 1;
+    extern __shared__ uint4 smem[];
+    __shared__ __align__(16) int words[FIND_WORDS];
+    const AdaptShape& s = a.s;
+    const int ntn = a.y ? (s.N + RN - 1) / RN : 1, col0 = blockIdx.x % ntn * RN;
+    int4 what;
+    const int* order;
+    if (!find_tile(a, blockIdx.x / ntn, words, &what, &order)) return;
+    const int key = what.x, nrows = what.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, fr = lane & 15, fg = lane >> 4;
+    const bool low = key < s.count;
+    const T* W = static_cast<const T*>(a.W);
+    const T* A = static_cast<const T*>(a.A) + (long long)(low ? key : 0) * s.rank * s.K;
+    const T* Bm = static_cast<const T*>(a.Bm) + (long long)(low ? key : 0) * s.rank * s.N;
+    // (rows of the last tile beyond the adapter's repeat the first: nothing of them leaves)
+    const T* xr = static_cast<const T*>(a.x) + row_at(s, order, what.y + (fr < nrows ? fr : 0)) * s.K;
+    // this thread's element of y, and the beginning of its row of B_a
+    const int orow = tid / RN, n = col0 + tid % RN;
+    uint4 fb[2] = {};
+    const T* br = Bm + (long long)min(n, s.N - 1) * s.rank;
+    if (low && a.y) { fb[0] = low_chunk<T>(br, 0, s.rank, low_vector); fb[1] = low_chunk<T>(br, V, s.rank, low_vector); }
+    f32x4_t acc[NB + RB];
+#pragma unroll
+    for (int i = 0; i < NB + RB; ++i) acc[i] = f32x4_t{};
+    const int steps = (s.K + STEP - 1) / STEP;
+    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+    auto run = [&](auto vec) {
+        constexpr bool VECTOR = decltype(vec)::value;
+        for (int s0 = wave; s0 < steps; s0 += RWAVES * DEEP) {
+            uint4 fx[DEEP], fw[DEEP][NB + RB];
+#pragma unroll
+            for (int d = 0; d < DEEP; ++d) {
+                const int k = (s0 + d * RWAVES) * STEP + fg * V;      // (beyond K: zeros)
+                fx[d] = load_chunk<T, VECTOR>(xr, k, s.K);
+#pragma unroll
+                for (int j = 0; j < NB; ++j) { const int c = col0 + 16 * j + fr; fw[d][j] = c < s.N ? load_chunk<T, VECTOR>(W + (long long)c * s.K, k, s.K) : none; }
+#pragma unroll
+                for (int j = 0; j < RB; ++j) { const int r = 16 * j + fr; fw[d][NB + j] = low && r < s.rank ? load_chunk<T, VECTOR>(A + (long long)r * s.K, k, s.K) : none; }
+            }
+#pragma unroll
+            for (int d = 0; d < DEEP; ++d)
+#pragma unroll
+                for (int j = 0; j < NB + RB; ++j) mma16<T>(acc[j], fx[d], fw[d][j]);
+        }
+    };
+    if (vector) run(std::true_type{}); else run(std::false_type{});
+    f32x4_t* part = reinterpret_cast<f32x4_t*>(smem);
+#pragma unroll
+    for (int j = 0; j < NB + RB; ++j) part[(wave * (NB + RB) + j) * 64 + lane] = acc[j];
+    float* ts = reinterpret_cast<float*>(part + RWAVES * (NB + RB) * 64);
+    constexpr int TLD = RP + 4;
+    float* os = ts + 16 * TLD;
+    const float bad = key > s.count ? __builtin_nanf("") : 0.0f;
+    __syncthreads();
+    for (int i = tid; i < (NB + RB) * 64; i += 64 * RWAVES) {
+        f32x4_t v = part[i];
+#pragma unroll
+        for (int w = 1; w < RWAVES; ++w) v += part[w * (NB + RB) * 64 + i];
+        const int j = i >> 6, l = i & 63, r = 4 * (l >> 4), c = l & 15;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { if (j < NB) os[(r + e) * (RN + 1) + 16 * j + c] = v[e] + bad; else ts[(r + e) * TLD + 16 * (j - NB) + c] = v[e] + bad; }
+    }
+    __syncthreads();
+    if (a.t && col0 == 0) {
+        for (int i = tid; i < nrows * s.rank; i += 64 * RWAVES) { const int r = i / s.rank, c = i - r * s.rank; a.t[row_at(s, order, what.y + r) * s.rank + c] = ts[r * TLD + c]; }
+    }
+    if (!a.y || orow >= nrows || n >= s.N) return;
+    float v = os[orow * (RN + 1) + tid % RN] + (a.b ? ld_f(static_cast<const T*>(a.b) + n) : 0.0f);
+    if (low) {
+        float sum = 0.0f;
+        auto dot = [&](const uint4& f, int c) {
+            float e[V];
+            if constexpr (sizeof(T) == 2) {
+                const uint32_t w[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) { e[2 * q] = bf2f((bf16_t)w[q]); e[2 * q + 1] = bf2f((bf16_t)(w[q] >> 16)); }
+            } else { const f32x4_t w = __builtin_bit_cast(f32x4_t, f); e[0] = w[0]; e[1] = w[1]; e[2] = w[2]; e[3] = w[3]; }
+#pragma unroll
+            for (int q = 0; q < V; ++q) sum += c + q < RP ? e[q] * ts[orow * TLD + c + q] : 0.0f;
+        };
+        dot(fb[0], 0);
+        dot(fb[1], V);
+        for (int c = 2 * V; c < s.rank; c += V) dot(low_chunk<T>(br, c, s.rank, low_vector), c);
+        v += s.scale * sum;
+    }
+    st_f(static_cast<T*>(a.y) + row_at(s, order, what.y + orow) * s.N + n, v);
+}
+
+// 64 rows x 128 columns of y and all 16 RB columns of t in one pass over x.  A slab is 128 bytes of every row (x, W, A_a) in swizzled LDS; wavefront w multiplies
+// columns 32 w .. of y and rows 16 w .. of t.  DIRECT (whole 16-byte words): slabs go from memory straight to LDS, NST - 1 ahead; else through registers, one ahead.
 constexpr int PN = 128;
-template <typename T, int MR, int RB, bool VECTOR>
-__global__ __launch_bounds__(256) void adapt_project_kernel(ProjectArgs a) {
-    constexpr int V = Vec<T>::N, SLAB = 8 * V, ROWS = 16 * MR, RP = 16 * RB;
-    constexpr int NX = ROWS * 8 / 256 > 0 ? ROWS * 8 / 256 : 1, NW = PN * 8 / 256, NA = (RP * 8 + 255) / 256;
+template <typename T, int RB, int NST, bool DIRECT>
+__global__ __launch_bounds__(256) void adapt_tile_kernel(ProjectArgs a, bool low_vector) {
+    constexpr int V = Vec<T>::N, SLAB = 8 * V, MR = 4, ROWS = 64, RP = 16 * RB, ES = (int)sizeof(T);
+    constexpr int NX = 2, NW = 4, NA = (RP * 8 + 255) / 256;
     constexpr int STAGE = (ROWS + PN + RP) * CHUNKS;
     extern __shared__ uint4 smem[];
+    __shared__ int rows[ROWS];
     const AdaptShape& s = a.s;
-    const int ntn = a.y ? (s.N + PN - 1) / PN : 1, tile = blockIdx.x / ntn, col0 = blockIdx.x % ntn * PN;
-    if (tile >= reinterpret_cast<const int*>(a.plan + a.p.counts)[0]) return;
-    const int4 what = reinterpret_cast<const int4*>(a.plan + a.p.tiles)[tile];
+    const int ntn = a.y ? (s.N + PN - 1) / PN : 1;
+    // ids go round-robin to the eight XCDs: a tile's column blocks stay on one, whose L2 then holds its rows of x
+    int lin = blockIdx.x;
+    const int n8 = gridDim.x & ~7;
+    if (lin < n8) lin = (lin & 7) * (n8 >> 3) + (lin >> 3);
+    const int col0 = lin % ntn * PN;
+    int4 what;
+    const int* order;
+    if (!find_tile(a, lin / ntn, reinterpret_cast<int*>(smem), &what, &order)) return;
     const int key = what.x, nrows = what.z;
-    const int* order = reinterpret_cast<const int*>(a.plan + a.p.perm) + s.B + what.w;
     const bool low = key < s.count;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    auto row_of = [&](int r) {                          // the row of x of the tile's row r
-        const int i = what.y + r, j = i / s.T;
-        return (long long)(i - j * s.T) * s.B + order[j];
-    };
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // (rows beyond the adapter's repeat its first: nothing of them leaves)
+    if (tid < ROWS) rows[tid] = (int)row_at(s, order, what.y + (tid < nrows ? tid : 0));
+    __syncthreads();
     const T* x = static_cast<const T*>(a.x);
     const T* W = static_cast<const T*>(a.W);
     const T* A = static_cast<const T*>(a.A) + (long long)(low ? key : 0) * s.rank * s.K;
     const T* Bm = static_cast<const T*>(a.Bm) + (long long)(low ? key : 0) * s.rank * s.N;
-    const int ch = tid & 7;
-    const T* xr[NX];
-#pragma unroll
-    for (int i = 0; i < NX; ++i) { const int r = (tid >> 3) + 32 * i; xr[i] = r < nrows ? x + row_of(r) * s.K : nullptr; }
     f32x4_t acc[MR][2], tac[RB];
 #pragma unroll
     for (int i = 0; i < MR; ++i) { acc[i][0] = f32x4_t{}; acc[i][1] = f32x4_t{}; }
 #pragma unroll
     for (int i = 0; i < RB; ++i) tac[i] = f32x4_t{};
-    uint4 rx[NX], rw[NW], ra[NA];
-    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-    auto load = [&](int k0) {
-        const int k = k0 + ch * V;
-#pragma unroll
-        for (int i = 0; i < NX; ++i) rx[i] = xr[i] ? load_chunk<T, VECTOR>(xr[i], k, s.K) : none;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) { const int n = col0 + (tid >> 3) + 32 * i; rw[i] = n < s.N ? load_chunk<T, VECTOR>(W + (long long)n * s.K, k, s.K) : none; }
-#pragma unroll
-        for (int i = 0; i < NA; ++i) { const int r = (tid >> 3) + 32 * i; ra[i] = low && r < s.rank ? load_chunk<T, VECTOR>(A + (long long)r * s.K, k, s.K) : none; }
-    };
-    auto store = [&](int buf) {
-        uint4* to = smem + buf * STAGE;
-        auto put = [&](int r, const uint4& v) { to[r * CHUNKS + (ch ^ swz(r))] = v; };
-#pragma unroll
-        for (int i = 0; i < NX; ++i) { const int r = (tid >> 3) + 32 * i; if (ROWS >= 32 || r < ROWS) put(r, rx[i]); }
-#pragma unroll
-        for (int i = 0; i < NW; ++i) put(ROWS + (tid >> 3) + 32 * i, rw[i]);
-#pragma unroll
-        for (int i = 0; i < NA; ++i) { const int r = (tid >> 3) + 32 * i; if (r < RP) put(ROWS + PN + r, ra[i]); }
-    };
     const int fr = lane & 15, fg = lane >> 4;
     const int slabs = (s.K + SLAB - 1) / SLAB;
-    const bool makes_t = MR == 4 || wave == 0;
-    const int trow = MR == 4 ? wave : 0;
-    load(0);
-    store(0);
-    __syncthreads();
-    for (int it = 0; it < slabs; ++it) {
-        const uint4* at = smem + (it & 1) * STAGE;
-        if (it + 1 < slabs) load((it + 1) * SLAB);
+    auto multiply = [&](const uint4* at) {
         auto frag = [&](int r, int q) { return at[r * CHUNKS + ((4 * q + fg) ^ swz(r))]; };
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
@@ -192,49 +312,132 @@ __global__ __launch_bounds__(256) void adapt_project_kernel(ProjectArgs a) {
 #pragma unroll
                 for (int i = 0; i < MR; ++i) mma16<T>(acc[i][j], fx[i], fw);
             }
-            if (low && makes_t) {
-                const uint4 ft = MR == 4 ? frag(16 * trow + fr, q) : fx[0];
+            if (low) {
+                const uint4 ft = frag(16 * wave + fr, q);
 #pragma unroll
                 for (int j = 0; j < RB; ++j) mma16<T>(tac[j], ft, frag(ROWS + PN + 16 * j + fr, q));
             }
         }
-        if (it + 1 < slabs) store((it + 1) & 1);
+    };
+    // B_a's part of the tile: asked for ahead of everything else
+    constexpr int BSTEP = 4 * V, BQ = (RP + BSTEP - 1) / BSTEP;      // columns of t a step
+    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+    uint4 fb[BQ][2];
+#pragma unroll
+    for (int q = 0; q < BQ; ++q)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int n = col0 + 32 * wave + 16 * j + fr;
+            fb[q][j] = low && a.y && n < s.N ? low_chunk<T>(Bm + (long long)n * s.rank, q * BSTEP + fg * V, s.rank, low_vector) : none;
+        }
+    if constexpr (DIRECT) {
+        // Instruction j of a wavefront fills eight rows: lane l fetches the chunk that belongs at slot l % 8 of row l / 8.  Rows beyond W's and A's repeat their last.
+        constexpr int NAI = RB >= 2 ? RB / 2 : 1;
+        const char* px[NX]; const char* pw[NW]; const char* pa[NAI];
+        const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
+        const int lr = lane >> 3;
+        auto chunk = [&](int r) { return ((lane & 7) ^ swz(r)) * 16; };
+#pragma unroll
+        for (int j = 0; j < NX; ++j) { const int r = 8 * (4 * j + wave) + lr; px[j] = reinterpret_cast<const char*>(x + (long long)rows[r] * s.K) + chunk(r); }
+#pragma unroll
+        for (int j = 0; j < NW; ++j) { const int r = 8 * (4 * j + wave) + lr; pw[j] = reinterpret_cast<const char*>(W + (long long)min(col0 + r, s.N - 1) * s.K) + chunk(ROWS + r); }
+        const bool has_a = RB >= 2 || wave < 2;              // (16 rows are two instructions)
+#pragma unroll
+        for (int j = 0; j < NAI; ++j) { const int r = 8 * (4 * j + wave) + lr; pa[j] = reinterpret_cast<const char*>(A + (long long)min(r, s.rank - 1) * s.K) + chunk(ROWS + PN + r); }
+        auto dma = [](unsigned lds_addr, const char* from) __attribute__((always_inline)) {
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(from) : "memory");
+        };
+        const int words = s.K / V;                           // 16-byte words of a row
+        auto issue = [&](int it) __attribute__((always_inline)) {
+            const unsigned sb = lds0 + (unsigned)(it % NST) * (STAGE * 16);
+            const long long off = (long long)it * 128;
+            const int left = words - it * 8;                 // (words beyond the row's end repeat its last, and are cleared below)
+            auto from = [&](const char* p, int r) { return p + off - (left < 8 ? max(((lane & 7) ^ swz(r)) - (left - 1), 0) * 16 : 0); };
+#pragma unroll
+            for (int j = 0; j < NX; ++j) dma(sb + (unsigned)(4 * j + wave) * 1024, from(px[j], 8 * (4 * j + wave) + lr));
+#pragma unroll
+            for (int j = 0; j < NW; ++j) dma(sb + ROWS * 128 + (unsigned)(4 * j + wave) * 1024, from(pw[j], ROWS + 8 * (4 * j + wave) + lr));
+            if (has_a) {
+#pragma unroll
+                for (int j = 0; j < NAI; ++j) dma(sb + (ROWS + PN) * 128 + (unsigned)(4 * j + wave) * 1024, from(pa[j], ROWS + PN + 8 * (4 * j + wave) + lr));
+            }
+        };
+        for (int i = 0; i < NST - 1; ++i) if (i < slabs) issue(i);
+        for (int it = 0; it < slabs; ++it) {
+            // this wavefront's loads of the slab have landed when at most the younger slab's are outstanding
+            if (NST == 2 || it + 1 >= slabs) asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+            else if (has_a) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(NX + NW + NAI) : "memory");
+            else asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(NX + NW) : "memory");
+            if (it + NST - 1 < slabs) issue(it + NST - 1);
+            uint4* at = smem + (it % NST) * STAGE;
+            if (words - it * 8 < 8) {
+                for (int i = tid; i < STAGE; i += 256) if (((i & 7) ^ swz(i >> 3)) >= words - it * 8) at[i] = none;
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            }
+            multiply(at);
+        }
         __syncthreads();
+    } else {
+        const int ch = tid & 7;
+        uint4 rx[NX], rw[NW], ra[NA];
+        auto load = [&](int k0) {
+            const int k = k0 + ch * V;
+#pragma unroll
+            for (int i = 0; i < NX; ++i) rx[i] = load_chunk<T, false>(x + (long long)rows[(tid >> 3) + 32 * i] * s.K, k, s.K);
+#pragma unroll
+            for (int i = 0; i < NW; ++i) { const int n = col0 + (tid >> 3) + 32 * i; rw[i] = n < s.N ? load_chunk<T, false>(W + (long long)n * s.K, k, s.K) : none; }
+#pragma unroll
+            for (int i = 0; i < NA; ++i) { const int r = (tid >> 3) + 32 * i; ra[i] = low && r < s.rank ? load_chunk<T, false>(A + (long long)r * s.K, k, s.K) : none; }
+        };
+        auto store = [&](int buf) {
+            uint4* to = smem + buf * STAGE;
+            auto put = [&](int r, const uint4& v) { to[r * CHUNKS + (ch ^ swz(r))] = v; };
+#pragma unroll
+            for (int i = 0; i < NX; ++i) put((tid >> 3) + 32 * i, rx[i]);
+#pragma unroll
+            for (int i = 0; i < NW; ++i) put(ROWS + (tid >> 3) + 32 * i, rw[i]);
+#pragma unroll
+            for (int i = 0; i < NA; ++i) { const int r = (tid >> 3) + 32 * i; if (r < RP) put(ROWS + PN + r, ra[i]); }
+        };
+        load(0);
+        store(0);
+        __syncthreads();
+        for (int it = 0; it < slabs; ++it) {
+            if (it + 1 < slabs) load((it + 1) * SLAB);
+            multiply(smem + (it & 1) * STAGE);
+            if (it + 1 < slabs) store((it + 1) & 1);
+            __syncthreads();
+        }
     }
-    // t, for everybody: rows of RP floats
+    // t, for everybody: rows of RP floats, zero beyond the rank
     float* ts = reinterpret_cast<float*>(smem);
     constexpr int TLD = RP + 4;
     const float bad = key > s.count ? __builtin_nanf("") : 0.0f;
-    if (makes_t) {
 #pragma unroll
-        for (int j = 0; j < RB; ++j)
+    for (int j = 0; j < RB; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) ts[(16 * trow + 4 * fg + e) * TLD + 16 * j + fr] = tac[j][e] + bad;
-    }
+        for (int e = 0; e < 4; ++e) ts[(16 * wave + 4 * fg + e) * TLD + 16 * j + fr] = 16 * j + fr < s.rank ? tac[j][e] + bad : 0.0f;
     __syncthreads();
     if (a.t && col0 == 0) {
-        for (int i = tid; i < nrows * s.rank; i += 256) { const int r = i / s.rank, c = i - r * s.rank; a.t[row_of(r) * s.rank + c] = ts[r * TLD + c]; }
+        for (int i = tid; i < nrows * s.rank; i += 256) { const int r = i / s.rank, c = i - r * s.rank; a.t[(long long)rows[r] * s.rank + c] = ts[r * TLD + c]; }
     }
     if (!a.y) return;
     if (low) {
         // s t B_a^T: t in two bf16 parts, or as it is
-        constexpr int STEP = 4 * V;                     // columns of t a step
 #pragma unroll
-        for (int q = 0; q < (RP + STEP - 1) / STEP; ++q) {
-            const int c = q * STEP + fg * V;
-            uint4 fb[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int n = col0 + 32 * wave + 16 * j + fr;
-                fb[j] = n < s.N ? load_chunk<T, false>(Bm + (long long)n * s.rank, c, s.rank) : none;
-            }
+        for (int q = 0; q < BQ; ++q) {
+            const int c = q * BSTEP + fg * V;
 #pragma unroll
             for (int i = 0; i < MR; ++i) {
                 float v[V];
 #pragma unroll
-                for (int e = 0; e < V; ++e) v[e] = c < RP ? s.scale * ts[(16 * i + fr) * TLD + c + e] : 0.0f;
+                for (int e = 0; e < V; e += 4) {
+                    const f32x4_t w = c < RP ? *reinterpret_cast<const f32x4_t*>(ts + (16 * i + fr) * TLD + c + e) : f32x4_t{};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[e + k] = s.scale * w[k];
+                }
                 uint4 hi, lo;
-                if constexpr (sizeof(T) == 2) {
+                if constexpr (ES == 2) {
                     uint32_t h[4], l[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -245,8 +448,8 @@ __global__ __launch_bounds__(256) void adapt_project_kernel(ProjectArgs a) {
                 } else hi = __builtin_bit_cast(uint4, f32x4_t{v[0], v[1], v[2], v[3]});
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    if constexpr (sizeof(T) == 2) mma16<T>(acc[i][j], lo, fb[j]);
-                    mma16<T>(acc[i][j], hi, fb[j]);
+                    if constexpr (ES == 2) mma16<T>(acc[i][j], lo, fb[q][j]);
+                    mma16<T>(acc[i][j], hi, fb[q][j]);
                 }
             }
         }
@@ -271,11 +474,11 @@ __global__ __launch_bounds__(256) void adapt_project_kernel(ProjectArgs a) {
     for (int i = tid; i < nrows * (PN / V); i += 256) {
         const int r = i / (PN / V), c = i % (PN / V) * V, n = col0 + c;
         if (n >= s.N) continue;
-        T* to = y + row_of(r) * s.N + n;
+        T* to = y + (long long)rows[r] * s.N + n;
         const float* v = os + r * OLD + c;
         if (words) {
             u32x4_t w;
-            if constexpr (sizeof(T) == 2) { w[0] = pack_bf2(v[0], v[1]); w[1] = pack_bf2(v[2], v[3]); w[2] = pack_bf2(v[4], v[5]); w[3] = pack_bf2(v[6], v[7]); }
+            if constexpr (ES == 2) { w[0] = pack_bf2(v[0], v[1]); w[1] = pack_bf2(v[2], v[3]); w[2] = pack_bf2(v[4], v[5]); w[3] = pack_bf2(v[6], v[7]); }
             else w = __builtin_bit_cast(u32x4_t, *reinterpret_cast<const f32x4_t*>(v));
             *reinterpret_cast<u32x4_t*>(to) = w;
         } else {
@@ -284,44 +487,49 @@ __global__ __launch_bounds__(256) void adapt_project_kernel(ProjectArgs a) {
     }
 }
 
-template <int MR, int RB, typename T>
-constexpr int project_lds() {
-    const int loop = 2 * (16 * MR + PN + 16 * RB) * 128, t = 16 * MR * (16 * RB + 4) * 4, out = 16 * MR * (PN + 4) * 4;
-    return std::max(loop, std::max(t, out));
+template <typename T, int RB>
+void run_rows(const ProjectArgs& a, bool vector, bool low_vector, hipStream_t st) {
+    constexpr int lds = RWAVES * (RN / 16 + RB) * 1024 + 16 * (16 * RB + 4) * 4 + 16 * (RN + 1) * 4;
+    const int ntn = a.y ? (a.s.N + RN - 1) / RN : 1;
+    adapt_rows_kernel<T, RB><<<a.p.max_tiles * ntn, 64 * RWAVES, lds, st>>>(a, vector, low_vector);
 }
-template <typename T, int MR, int RB>
-void run_project(const ProjectArgs& a, bool vector, hipStream_t st) {
+template <typename T, int RB, int NST, bool DIRECT>
+void run_tile(const ProjectArgs& a, bool low_vector, hipStream_t st) {
+    constexpr int loop = NST * (64 + PN + 16 * RB) * 128, t = 64 * (16 * RB + 4) * 4, out = 64 * (PN + 4) * 4;
+    constexpr int lds = loop > t ? loop > out ? loop : out : t > out ? t : out;
     const int ntn = a.y ? (a.s.N + PN - 1) / PN : 1;
-    if (vector) adapt_project_kernel<T, MR, RB, true><<<a.p.max_tiles * ntn, 256, project_lds<MR, RB, T>(), st>>>(a);
-    else adapt_project_kernel<T, MR, RB, false><<<a.p.max_tiles * ntn, 256, project_lds<MR, RB, T>(), st>>>(a);
+    adapt_tile_kernel<T, RB, NST, DIRECT><<<a.p.max_tiles * ntn, 256, lds, st>>>(a, low_vector);
+}
+template <typename T, int RB>
+void run_project(const ProjectArgs& a, bool vector, bool low_vector, hipStream_t st) {
+    // (three buffers where two workgroups a CU have room for them)
+    if (a.p.rows == 16) run_rows<T, RB>(a, vector, low_vector, st);
+    else if (vector) run_tile<T, RB, RB == 1 ? 3 : 2, true>(a, low_vector, st);
+    else run_tile<T, RB, 2, false>(a, low_vector, st);
 }
 template <typename T>
 hipError_t project(const ProjectArgs& a, hipStream_t st) {
     auto whole = [&](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
     const bool vector = a.s.K % Vec<T>::N == 0 && whole(a.x) && whole(a.W) && whole(a.A);
-    const int rb = a.s.rank <= 16 ? 1 : a.s.rank <= 32 ? 2 : a.s.rank <= 64 ? 4 : 8;
-    if (a.p.rows == 16) {
-        if (rb == 1) run_project<T, 1, 1>(a, vector, st);
-        else if (rb == 2) run_project<T, 1, 2>(a, vector, st);
-        else if (rb == 4) run_project<T, 1, 4>(a, vector, st);
-        else run_project<T, 1, 8>(a, vector, st);
-    } else {
-        if (rb == 1) run_project<T, 4, 1>(a, vector, st);
-        else if (rb == 2) run_project<T, 4, 2>(a, vector, st);
-        else if (rb == 4) run_project<T, 4, 4>(a, vector, st);
-        else run_project<T, 4, 8>(a, vector, st);
-    }
+    const bool low_vector = a.s.rank % Vec<T>::N == 0 && whole(a.Bm);
+    if (a.s.rank <= 16) run_project<T, 1>(a, vector, low_vector, st);
+    else if (a.s.rank <= 32) run_project<T, 2>(a, vector, low_vector, st);
+    else if (a.s.rank <= 64) run_project<T, 4>(a, vector, low_vector, st);
+    else run_project<T, 8>(a, vector, low_vector, st);
     return hipGetLastError();
 }
 
 // ---- transposed weights ----------------------------------------------------------------------------------------------
 template <typename T>
-__global__ __launch_bounds__(256) void adapt_transpose_kernel(TransposeArgs a) {
-    __shared__ T lds[32][33];
+__global__ __launch_bounds__(256) void adapt_transpose_kernel(TransposeArgs a, AdaptPlan p, const int32_t* ids, char* plan) {
+    extern __shared__ int words[];
+    T (*lds)[33] = reinterpret_cast<T (*)[33]>(words);
     const AdaptShape& s = a.s;
+    // (the plan is a chain of latencies: the first workgroup makes it while the others move)
+    if (blockIdx.x == 0) { make_plan(s, p, ids, plan, words); return; }
     auto tiles = [](int r, int c) { return ((r + 31) / 32) * ((c + 31) / 32); };
     const int tw = tiles(s.N, s.K), ta = tiles(s.rank, s.K), tb = tiles(s.N, s.rank);
-    int id = blockIdx.x, R, C;
+    int id = blockIdx.x - 1, R, C;
     const T* from; T* to;
     if (id < tw) { from = static_cast<const T*>(a.W); to = static_cast<T*>(a.Wt); R = s.N; C = s.K; }
     else if ((id -= tw) < ta * s.count) { const long long k = id / ta; id %= ta; R = s.rank; C = s.K; from = static_cast<const T*>(a.A) + k * R * C; to = static_cast<T*>(a.At) + k * R * C; }
@@ -494,15 +702,16 @@ AdaptPlan adapt_plan(const AdaptShape& s, int rows, int chunk) {
 }
 
 hipError_t launch_adapt_plan(const AdaptShape& s, const AdaptPlan& p, const int32_t* ids, char* plan, hipStream_t st) {
-    adapt_plan_kernel<<<1, PLAN_THREADS, 0, st>>>(s, p, ids, plan);
+    adapt_plan_kernel<<<1, PLAN_THREADS, plan_lds(s.count), st>>>(s, p, ids, plan);
     return hipGetLastError();
 }
 hipError_t launch_adapt_project(const ProjectArgs& a, DType type, hipStream_t st) { return type == DT_BF16 ? project<bf16_t>(a, st) : project<float>(a, st); }
-hipError_t launch_adapt_transpose(const TransposeArgs& a, DType type, hipStream_t st) {
+hipError_t launch_adapt_transpose(const TransposeArgs& a, const AdaptPlan& p, const int32_t* ids, char* plan, DType type, hipStream_t st) {
     auto tiles = [](int r, int c) { return ((r + 31) / 32) * ((c + 31) / 32); };
-    const int n = tiles(a.s.N, a.s.K) + a.s.count * (tiles(a.s.rank, a.s.K) + tiles(a.s.N, a.s.rank));
-    if (type == DT_BF16) adapt_transpose_kernel<bf16_t><<<n, 256, 0, st>>>(a);
-    else adapt_transpose_kernel<float><<<n, 256, 0, st>>>(a);
+    const int lds = std::max(plan_lds(a.s.count), 32 * 33 * 4);
+    const int n = 1 + tiles(a.s.N, a.s.K) + a.s.count * (tiles(a.s.rank, a.s.K) + tiles(a.s.N, a.s.rank));
+    if (type == DT_BF16) adapt_transpose_kernel<bf16_t><<<n, 256, lds, st>>>(a, p, ids, plan);
+    else adapt_transpose_kernel<float><<<n, 256, lds, st>>>(a, p, ids, plan);
     return hipGetLastError();
 }
 hipError_t launch_adapt_grad(const AdaptGradArgs& a, DType type, hipStream_t st) { return type == DT_BF16 ? grad<bf16_t>(a, st) : grad<float>(a, st); }

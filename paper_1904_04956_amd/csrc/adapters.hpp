@@ -19,6 +19,8 @@ struct AdaptPlan {
     int max_tiles, max_chunks;
     size_t counts, perm, first, tiles, chunks, first_chunk, bytes;      // byte offsets from the plan's start
 };
+// Batches of few sequences need no plan for adapt_project.
+inline bool adapt_finds(const AdaptShape& s) { return s.B <= 256; }
 // counts: {tiles, chunks}; first [count + 3]: a key's first place in perm; first_chunk [count + 1]; tiles and chunks: {key, first row, its rows, first place in perm}
 AdaptPlan adapt_plan(const AdaptShape& s, int rows, int chunk);
 // Rows of a tile: 16 for a frame or few rows of an adapter, else 64.
@@ -29,16 +31,17 @@ hipError_t launch_adapt_plan(const AdaptShape& s, const AdaptPlan& p, const int3
 struct ProjectArgs {
     AdaptShape s;
     AdaptPlan p;
-    const char* plan;
+    const char* plan;                    // null: every workgroup finds its tile in ids itself (adapt_finds)
+    const int32_t* ids;
     const void *x, *W, *b, *A, *Bm;      // b null: none
     void* y;                             // null: only t is wanted
     float* t;                            // null: not wanted
 };
 hipError_t launch_adapt_project(const ProjectArgs& a, DType type, hipStream_t st);
 
-// W^T [K][N], A_a^T [K][rank], B_a^T [rank][N] of all adapters
+// W^T [K][N], A_a^T [K][rank], B_a^T [rank][N] of all adapters, and the plan in the same launch
 struct TransposeArgs { AdaptShape s; const void *W, *A, *Bm; void *Wt, *At, *Bt; };
-hipError_t launch_adapt_transpose(const TransposeArgs& a, DType type, hipStream_t st);
+hipError_t launch_adapt_transpose(const TransposeArgs& a, const AdaptPlan& p, const int32_t* ids, char* plan, DType type, hipStream_t st);
 
 // dA_a [rank][K] = scale sum q^T x, dB_a [N][rank] = scale sum dy^T t over an adapter's rows; zero for an adapter without any
 struct AdaptGradArgs {

@@ -1629,8 +1629,9 @@ int adapter_forward(const adapter_config* cfg, const void* W, const void* b, con
     if (rc != BLSTM_OK) return rc;
     hipStream_t st = static_cast<hipStream_t>(stream);
     char* base = static_cast<char*>(scratch);
-    hipError_t e = launch_adapt_plan(l.s, l.plan, ids, base + l.plan_at, st);
-    if (e == hipSuccess) e = launch_adapt_project(ProjectArgs{l.s, l.plan, base + l.plan_at, x, W, b, A, Bm, y, t}, l.type, st);
+    const bool finds = adapt_finds(l.s);
+    hipError_t e = finds ? hipSuccess : launch_adapt_plan(l.s, l.plan, ids, base + l.plan_at, st);
+    if (e == hipSuccess) e = launch_adapt_project(ProjectArgs{l.s, l.plan, finds ? nullptr : base + l.plan_at, ids, x, W, b, A, Bm, y, t}, l.type, st);
     return check_hip(e, "adapter_forward");
 }
 
@@ -1647,12 +1648,11 @@ int adapter_backward(const adapter_config* cfg, const void* W, const void* A, co
     char* base = static_cast<char*>(scratch);
     const char* plan = base + l.plan_at;
     float* q = reinterpret_cast<float*>(base + l.q);
-    hipError_t e = launch_adapt_plan(l.s, l.plan, ids, base + l.plan_at, st);
-    if (e == hipSuccess) e = launch_adapt_transpose(TransposeArgs{l.s, W, A, Bm, base + l.wt, base + l.at, base + l.bt}, l.type, st);
+    hipError_t e = launch_adapt_transpose(TransposeArgs{l.s, W, A, Bm, base + l.wt, base + l.at, base + l.bt}, l.plan, ids, base + l.plan_at, l.type, st);
     // dx and q: the forward pass of dy with the transposed weights, x's part taken by dy and A's by B_a^T
     AdaptShape turned = l.s;
     turned.K = l.s.N; turned.N = l.s.K;
-    if (e == hipSuccess) e = launch_adapt_project(ProjectArgs{turned, l.plan, plan, dy, base + l.wt, nullptr, base + l.bt, base + l.at, dx, q}, l.type, st);
+    if (e == hipSuccess) e = launch_adapt_project(ProjectArgs{turned, l.plan, plan, ids, dy, base + l.wt, nullptr, base + l.bt, base + l.at, dx, q}, l.type, st);
     if (e == hipSuccess) e = launch_adapt_grad(AdaptGradArgs{l.s, l.plan, plan, x, dy, q, t, reinterpret_cast<float*>(base + l.part), dA, dB}, l.type, st);
     if (e == hipSuccess && dW) {
         GemmDesc d{};

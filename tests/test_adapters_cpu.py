@@ -104,7 +104,11 @@ def test_launches_and_failures(recorder):  # noqa: F811
         bwd = lambda dW: bl.adapter_backward(c, P, P, P, P, P, P, P, P, P, P, dW, dW, P, n[1], 0)
         for call in (fwd, lambda: bwd(P), lambda: bwd(None)):
             out.append([x for x in launches(call) if "adapt" not in x])
-        for part, call in ((b"adapt_plan", fwd), (b"adapt_project", fwd), (b"adapt_transpose", lambda: bwd(P)), (b"adapt_grad", lambda: bwd(P))):
+        # batches of few sequences find their tiles, others have a plan made first
+        many = bl.adapter_config(1, 300, 64, 24, 8, 5, 1, 1.0)
+        out.append([len(launches(fwd)), len(launches(lambda: bl.adapter_forward(many, P, P, P, P, P, P, P, P, P, 1 << 30, 0)))])
+        for part, call in ((b"adapt_plan", lambda: bl.adapter_forward(many, P, P, P, P, P, P, P, P, P, 1 << 30, 0)), (b"adapt_tile", fwd),
+                           (b"adapt_transpose", lambda: bwd(P)), (b"adapt_grad", lambda: bwd(P))):
             rec.recorder_fail(part)
             try:
                 call()
@@ -113,4 +117,5 @@ def test_launches_and_failures(recorder):  # noqa: F811
                 out.append(e.code)
     """)
     assert got[0] == [] and got[2] == [] and len(got[1]) >= 1            # the shared projection's gradient is an ordinary product
-    assert got[3:] == [-5, -5, -5, -5]
+    assert got[3] == [1, 2]
+    assert got[4:] == [-5, -5, -5, -5]
