@@ -23,8 +23,11 @@ struct AdaptPlan {
 inline bool adapt_finds(const AdaptShape& s) { return s.B <= 256; }
 // counts: {tiles, chunks}; first [count + 3]: a key's first place in perm; first_chunk [count + 1]; tiles and chunks: {key, first row, its rows, first place in perm}
 AdaptPlan adapt_plan(const AdaptShape& s, int rows, int chunk);
-// Rows of a tile: 16 for a frame or few rows of an adapter, else 64.
-inline int adapter_tile_rows(const AdaptShape& s) { return s.T <= 16 && (long long)s.T * s.B <= 2048 ? 16 : 64; }
+// Rows of a tile: 16 for a frame or few rows of an adapter, 128 where the adapters' rows fill several such tiles, else 64.
+inline int adapter_tile_rows(const AdaptShape& s) {
+    const long long M = (long long)s.T * s.B, groups = s.B < s.count + 1 ? s.B : s.count + 1;
+    return s.T <= 16 && M <= 2048 ? 16 : M >= 512 * groups && M >= 16384 ? 128 : 64;
+}
 hipError_t launch_adapt_plan(const AdaptShape& s, const AdaptPlan& p, const int32_t* ids, char* plan, hipStream_t st);
 
 // y [M][N] = x [M][K] W^T + b + scale t B_a^T, t [M][rank] = x A_a^T.  W [N][K], A [count][rank][K], Bm [count][N][rank].
