@@ -663,6 +663,102 @@ __global__ __launch_bounds__(256) void adapt_grad_kernel(AdaptGradArgs a) {
         }
 }
 
+// The same in bf16 where rows are whole 16-byte words: two slabs of 64 rows of x (or dy) and of q (or t) come straight to LDS in turn, one while the other is
+// multiplied; q's (t's) three bf16 parts are made of the slab that has landed.  256 sequences x 21 frames, K 1024, 100 adapters: 15 us through registers; 2048 sequences,
+// 24 adapters 70 us: NOTE_GRAD here.
+template <int RB>
+__global__ __launch_bounds__(256) void adapt_grad_direct_kernel(AdaptGradArgs a) {
+    constexpr int RP = 32 * RB, LLD = RP * 2 + 16, RS = 64 * 256, LS = 64 * RP * 4, STAGE = RS + LS, LCH = RP / 4;     // bytes; 16-byte words of a row of q
+    constexpr int NR = 4, NL = LS / 1024 / 4;                // load instructions of a wavefront and slab
+    extern __shared__ uint4 smem[];
+    __shared__ int rows[ADAPT_MAX_CHUNK];
+    char* base = reinterpret_cast<char*>(smem);
+    char* planes = base + 2 * STAGE;
+    const AdaptShape& s = a.s;
+    const int nk = (s.K + 127) / 128, nn = (s.N + 127) / 128, ncol = nk + nn;
+    // (a chunk's columns on one XCD: they share q)
+    const int slot = blockIdx.x >> 3, chunk = slot / ncol * 8 + (blockIdx.x & 7), ct = slot % ncol;
+    if (chunk >= reinterpret_cast<const int*>(a.plan + a.p.counts)[1]) return;
+    const int4 what = reinterpret_cast<const int4*>(a.plan + a.p.chunks)[chunk];
+    const int* order = reinterpret_cast<const int*>(a.plan + a.p.perm) + s.B + what.w;
+    const bool second = ct >= nk;
+    const int width = second ? s.N : s.K, c0 = (second ? ct - nk : ct) * 128, nrows = what.z, slabs = (nrows + 63) / 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    for (int r = tid; r < nrows; r += 256) rows[r] = (int)row_at(s, order, what.y + r);
+    __syncthreads();
+    const char* R = static_cast<const char*>(second ? a.dy : a.x) + c0 * 2;
+    const char* L = reinterpret_cast<const char*>(second ? a.t : a.q);
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
+    auto dma = [](unsigned lds_addr, const char* from) __attribute__((always_inline)) {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(from) : "memory");
+    };
+    const int last_word = (width - c0) / 8 - 1, last_low = s.rank / 4 - 1;
+    // (rows behind the chunk's last repeat it and are cleared; words beyond a row's end repeat its last: those columns go nowhere)
+    auto issue = [&](int it) __attribute__((always_inline)) {
+        const unsigned sb = lds0 + (unsigned)(it & 1) * STAGE;
+#pragma unroll
+        for (int j = 0; j < NR; ++j) {
+            const int jj = 4 * j + wave, kt = 4 * jj + (lane >> 4), pos = lane & 15, mc = (((pos >> 1) ^ tr_swz<16>(kt)) << 1) | (pos & 1);
+            dma(sb + jj * 1024, R + (long long)rows[min(64 * it + kt, nrows - 1)] * (2 * width) + min(mc, last_word) * 16);
+        }
+#pragma unroll
+        for (int j = 0; j < NL; ++j) {
+            const int w = (4 * j + wave) * 64 + lane, r = w / LCH, c = w % LCH;
+            dma(sb + RS + (4 * j + wave) * 1024, L + (long long)rows[min(64 * it + r, nrows - 1)] * (4 * s.rank) + min(c, last_low) * 16);
+        }
+    };
+    f32x16_t acc[RB];
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
+    issue(0);
+    const int g = lane >> 4, li = lane & 15, at = 8 * (g >> 1) + (li >> 2), off = 32 * (g & 1) + (li & 3) * 8;
+    const int tr = at * 256 + (((2 * wave + (g & 1)) ^ tr_swz<16>(li >> 2)) << 5) + (li & 3) * 8;
+    for (int it = 0; it < slabs; ++it) {
+        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        if (it + 1 < slabs) issue(it + 1);
+        char* rs = base + (it & 1) * STAGE;
+        const int left = nrows - 64 * it;
+        if (left < 64) for (int i = left * 16 + tid; i < 1024; i += 256) reinterpret_cast<uint4*>(rs)[i] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int j = 0; j < NL; ++j) {
+            const int w = tid + 256 * j, r = w / LCH, c = w % LCH * 4;
+            f32x4_t v = *reinterpret_cast<const f32x4_t*>(rs + RS + w * 16);
+            if (r >= left || c >= s.rank) v = f32x4_t{};
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                u32x2_t h;
+                h[0] = pack_bf2(v[0], v[1]); h[1] = pack_bf2(v[2], v[3]);
+                *reinterpret_cast<u32x2_t*>(planes + (p * 64 + r) * LLD + 2 * c) = h;
+                v[0] -= bf2f((bf16_t)h[0]); v[1] -= bf2f((bf16_t)(h[0] >> 16)); v[2] -= bf2f((bf16_t)h[1]); v[3] -= bf2f((bf16_t)(h[1] >> 16));
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+        for (int k = 0; k < 64; k += 16) {
+            const uint4 fr = lfrag_tr<256>(rs + tr, k);
+#pragma unroll
+            for (int i = 0; i < RB; ++i)
+#pragma unroll
+                for (int p = 2; p >= 0; --p) {
+                    const uint4 fl = lfrag_tr<LLD>(planes + (p * 64 + at) * LLD + i * 64 + off, k);
+                    acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, fl), __builtin_bit_cast(bf16x8_t, fr), acc[i], 0, 0, 0);
+                }
+        }
+    }
+    const int col = c0 + 32 * wave + (lane & 31);
+    if (col >= width) return;
+    float* out = a.part + (long long)chunk * s.rank * (s.K + s.N) + (second ? s.K : 0) + col;
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int r = 32 * i + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
+            if (r < s.rank) out[(long long)r * (s.K + s.N)] = acc[i][e];
+        }
+}
+
 // An adapter's chunks in order; dB leaves transposed (through LDS).
 __global__ __launch_bounds__(256) void adapt_grad_sum_kernel(AdaptGradArgs a) {
     __shared__ float lds[32][33];
@@ -693,6 +789,13 @@ __global__ __launch_bounds__(256) void adapt_grad_sum_kernel(AdaptGradArgs a) {
 
 template <typename T, int RB>
 void run_grad(const AdaptGradArgs& a, bool vector, hipStream_t st) {
+    if constexpr (sizeof(T) == 2) {
+        if (vector && a.s.rank % 4 == 0 && (reinterpret_cast<uintptr_t>(a.t) & 15) == 0) {
+            constexpr int lds = 2 * (64 * 256 + 64 * 32 * RB * 4) + 3 * 64 * (64 * RB + 16);
+            adapt_grad_direct_kernel<RB><<<(a.p.max_chunks + 7) / 8 * 8 * ((a.s.K + 127) / 128 + (a.s.N + 127) / 128), 256, lds, st>>>(a);
+            return;
+        }
+    }
     constexpr int lds = 64 * (128 * (int)sizeof(T) + 16) + (sizeof(T) == 2 ? 3 : 1) * 64 * (32 * RB * (int)sizeof(T) + 16);
     const int grid = a.p.max_chunks * ((a.s.K + 127) / 128 + (a.s.N + 127) / 128);
     if (vector) adapt_grad_kernel<T, RB, true><<<grid, 256, lds, st>>>(a);

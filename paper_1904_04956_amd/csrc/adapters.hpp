@@ -23,6 +23,9 @@ struct AdaptPlan {
 inline bool adapt_finds(const AdaptShape& s) { return s.B <= 256; }
 // counts: {tiles, chunks}; first [count + 3]: a key's first place in perm; first_chunk [count + 1]; tiles and chunks: {key, first row, its rows, first place in perm}
 AdaptPlan adapt_plan(const AdaptShape& s, int rows, int chunk);
+// Rows of a chunk of the gradients' sums: about 64 chunks if one adapter has all rows, at most ADAPT_MAX_CHUNK rows each.
+constexpr int ADAPT_MAX_CHUNK = 1024;
+inline int adapter_chunk_rows(const AdaptShape& s) { const long long M = (long long)s.T * s.B, r = (M + 4095) / 4096 * 64; return (int)(r < ADAPT_MAX_CHUNK ? r : ADAPT_MAX_CHUNK); }
 // Rows of a tile: 16 for a frame or few rows of an adapter, 128 where the adapters' rows fill several such tiles, else 64.
 inline int adapter_tile_rows(const AdaptShape& s) {
     const long long M = (long long)s.T * s.B, groups = s.B < s.count + 1 ? s.B : s.count + 1;

@@ -850,8 +850,7 @@ int adapter_sizes(const char* name, const adapter_config* c, int call, AdapterSc
     a.s = AdaptShape{c->T, c->B, c->K, c->N, c->rank, c->count, c->scale};
     a.type = c->mode == 1 ? DT_BF16 : DT_F32;
     const size_t e = c->mode == 1 ? 2 : 4;
-    // Rows of a chunk of the gradients' sums: about 64 chunks if one adapter has all rows
-    const int chunk = call == ADAPTER_FORWARD ? 0 : std::max(64, (int)((M + 4095) / 4096) * 64);
+    const int chunk = call == ADAPTER_FORWARD ? 0 : adapter_chunk_rows(a.s);
     a.plan = adapt_plan(a.s, adapter_tile_rows(a.s), chunk);
     size_t at = up256(a.plan.bytes);
     auto take = [&](size_t n) { const size_t was = at; at += up256(n); return was; };
