@@ -21,6 +21,9 @@ namespace blstm {
 namespace {
 
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+// (a tensor may start anywhere in the flat vector, and rows need not be whole words)
+typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned u32x2u_t __attribute__((ext_vector_type(2), aligned(2)));
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr int NS_STEPS = 5;
@@ -30,10 +33,11 @@ constexpr int CAST = 4096;
 
 enum { PH_GRAM = 0, PH_SQUARE = 1, PH_APPLY = 2, PH_LAST = 3 };
 
-template <typename F>
-__device__ __forceinline__ int group_of(const MuonPlan& p, int id, F&& first) {      // the last group that starts at or before id (empty ones share a start)
+// the last group that starts at or before id (empty ones share a start)
+__device__ __forceinline__ int group_of(const int (&first)[MUON_MAX_GROUPS], int id) {
     int k = 0;
-    for (int i = 1; i < p.n; ++i) if (id >= first(p.g[i])) k = i;
+#pragma unroll
+    for (int i = 1; i < MUON_MAX_GROUPS; ++i) k += id >= first[i] ? 1 : 0;
     return __builtin_amdgcn_readfirstlane(k);
 }
 // (the same in every lane: said for the scalar operand of a load)
@@ -53,8 +57,9 @@ __device__ __forceinline__ double block_sum(double v, double* lds) {
 }
 __global__ __launch_bounds__(256) void muon_momentum_kernel(MuonPlan p, MuonArgs a, double* sums) {
     __shared__ double lds[4];
-    const MuonGroup& g = p.g[group_of(p, blockIdx.x, [](const MuonGroup& x) { return x.chunk0; })];
-    const int local = blockIdx.x - g.chunk0, k = local / g.chunks, c = local % g.chunks;
+    const int group = group_of(p.at.chunk, blockIdx.x);
+    const MuonGroup& g = p.g[group];
+    const int local = blockIdx.x - p.at.chunk[group], k = local / g.chunks, c = local % g.chunks;
     const long long size = (long long)g.rows * g.cols, e0 = (long long)c * FLAT, at = tensor_at(g, k) + e0;
     const int len = (int)min((long long)FLAT, size - e0);
     const float* grad = a.grad + at;
@@ -116,17 +121,17 @@ __device__ __forceinline__ void put_halves(_Float16* hi, _Float16* lo, const flo
 }
 __global__ __launch_bounds__(256) void muon_cast_kernel(MuonPlan p, MuonArgs a, const double* sums, _Float16* ws) {
     __shared__ double lds[4];
-    const MuonGroup& g = p.g[group_of(p, blockIdx.x, [](const MuonGroup& x) { return x.cast0; })];
-    const int local = blockIdx.x - g.cast0, k = local / g.casts, c = local % g.casts;
+    const int group = group_of(p.at.cast, blockIdx.x);
+    const MuonGroup& g = p.g[group];
+    const int local = blockIdx.x - p.at.cast[group], k = local / g.casts, c = local % g.casts;
     double sum = 0.0;
-    for (int i = threadIdx.x; i < g.chunks; i += 256) sum += sums[g.chunk0 + k * g.chunks + i];
+    for (int i = threadIdx.x; i < g.chunks; i += 256) sum += sums[p.at.chunk[group] + k * g.chunks + i];
     const double norm2 = block_sum(sum, lds);
     // (a zero matrix stays one; an infinity or NaN anywhere makes all of it NaN)
     const double scale = norm2 == 0.0 ? 0.0 : UP / sqrt(norm2);
     const float whole = norm2 <= 1.7e308 ? 0.0f : __builtin_nanf("");
     const long long at = tensor_at(g, k);
     _Float16* x = ws + g.x[0] + (long long)k * g.rp * g.cp;
-    const bool vec = (at & 3) == 0 && (g.cols & 3) == 0;
 #pragma unroll
     for (int q = 0; q < CAST / 2048; ++q) {
         const long long e = (long long)c * CAST + q * 2048 + threadIdx.x * 8;
@@ -138,11 +143,11 @@ __global__ __launch_bounds__(256) void muon_cast_kernel(MuonPlan p, MuonArgs a, 
             const long long o = at + (long long)r * g.cols + c0;
             const int n = min(8, g.cols - c0);
             float gr[8], v[8];
-            if (vec) {
+            if (n == 8) {
 #pragma unroll
-                for (int w = 0; w < 2; ++w) if (4 * w < n) {
-                    const f32x4_t y = *reinterpret_cast<const f32x4_t*>(a.grad + o + 4 * w);
-                    const f32x4_t z = a.velocity ? *reinterpret_cast<const f32x4_t*>(a.velocity + o + 4 * w) : y;
+                for (int w = 0; w < 2; ++w) {
+                    const f32x4_t y = *reinterpret_cast<const f32x4u_t*>(a.grad + o + 4 * w);
+                    const f32x4_t z = a.velocity ? (f32x4_t)*reinterpret_cast<const f32x4u_t*>(a.velocity + o + 4 * w) : y;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) { gr[4 * w + j] = y[j]; v[4 * w + j] = z[j]; }
                 }
@@ -167,8 +172,9 @@ __global__ __launch_bounds__(256) void muon_cast_kernel(MuonPlan p, MuonArgs a, 
 // the next slab's loads go out behind a barrier and the products run from registers; two workgroups a CU take turns.
 struct NsOperand { const _Float16* p; long long ld, plane; };      // tile origin; elements to the second halves
 
-template <int TM, int TN, bool SPLIT, bool AS, bool BS, bool ONE>
+template <int TM, int TN, bool SPLIT, bool AS, bool BS, int NST>
 __device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand& A, const NsOperand& B, int slab0, int slab1, uint4* smem) {
+    constexpr bool ONE = NST == 1;
     static_assert(!ONE || !SPLIT, "the registers hold one plane's fragments");
     constexpr int BM = 64 * TM, BN = 64 * TN, PL = SPLIT ? 2 : 1, PA = BM * 8, PB = BN * 8, STAGE = PL * (PA + PB);   // (in 16-byte words)
     constexpr int NIA = 2 * TM, NIB = 2 * TN, CPA = BM / 8, CPB = BN / 8;
@@ -191,7 +197,7 @@ __device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand
     auto issue = [&](int it) __attribute__((always_inline)) {
         const char* pa = uniform(A.p + (AS ? (long long)it * 64 * A.ld : (long long)it * 64));
         const char* pb = uniform(B.p + (BS ? (long long)it * 64 * B.ld : (long long)it * 64));
-        const unsigned sb = lds0 + (ONE ? 0u : (unsigned)(((it - slab0) & 1) * STAGE * 16));
+        const unsigned sb = lds0 + (unsigned)(((it - slab0) % NST) * STAGE * 16);
 #pragma unroll
         for (int pl = 0; pl < PL; ++pl) {
 #pragma unroll
@@ -232,7 +238,8 @@ __device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand
             for (int j = 0; j < TN; ++j)
                 acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, x[i]), __builtin_bit_cast(f16x8_t, y[j]), acc[i][j], 0, 0, 0);
     };
-    if (slab0 < slab1) issue(slab0);
+#pragma unroll
+    for (int i = 0; i < (ONE ? 1 : NST - 1); ++i) if (slab0 + i < slab1) issue(slab0 + i);
     if constexpr (ONE) {
         uint4 fa[4][TM], fb[4][TN];
         for (int it = slab0; it < slab1; ++it) {
@@ -251,22 +258,34 @@ __device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand
         }
     } else {
         for (int it = slab0; it < slab1; ++it) {
-            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-            if (it + 1 < slab1) issue(it + 1);
-            const uint4* sa = smem + ((it - slab0) & 1) * STAGE;
+            // (this wavefront's loads of the slab have landed when at most the younger slabs' are outstanding)
+            constexpr int LOADS = PL * (NIA + NIB);
+            const int younger = min(NST - 2, slab1 - 1 - it);
+            if (NST >= 4 && younger == 2) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(2 * LOADS) : "memory");
+            else if (NST >= 3 && younger == 1) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(LOADS) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+            if (it + NST - 1 < slab1) issue(it + NST - 1);
+            const uint4* sa = smem + ((it - slab0) % NST) * STAGE;
             const uint4* sb = sa + PL * PA;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                uint4 af[PL][TM], bf[PL][TN];
+            // (the next fragments are on their way while these are multiplied)
+            constexpr int NF = SPLIT && TM == 2 ? 1 : 2;
+            uint4 af[NF][PL][TM], bf[NF][PL][TN];
+            auto read = [&](int q, uint4 (&x)[PL][TM], uint4 (&y)[PL][TN]) __attribute__((always_inline)) {
 #pragma unroll
                 for (int pl = 0; pl < PL; ++pl) {
 #pragma unroll
-                    for (int i = 0; i < TM; ++i) af[pl][i] = frag_a(sa + pl * PA, i, q);
+                    for (int i = 0; i < TM; ++i) x[pl][i] = frag_a(sa + pl * PA, i, q);
 #pragma unroll
-                    for (int i = 0; i < TN; ++i) bf[pl][i] = frag_b(sb + pl * PB, i, q);
+                    for (int i = 0; i < TN; ++i) y[pl][i] = frag_b(sb + pl * PB, i, q);
                 }
-                if constexpr (SPLIT) { mma(af[1], bf[0]); mma(af[0], bf[1]); }
-                mma(af[0], bf[0]);
+            };
+            if (NF == 2) read(0, af[0], bf[0]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (NF == 2) { if (q < 3) read(q + 1, af[(q + 1) % NF], bf[(q + 1) % NF]); }
+                else read(q, af[0], bf[0]);
+                if constexpr (SPLIT) { mma(af[q % NF][1], bf[q % NF][0]); mma(af[q % NF][0], bf[q % NF][1]); }
+                mma(af[q % NF][0], bf[q % NF][0]);
             }
         }
     }
@@ -327,15 +346,17 @@ __device__ __forceinline__ void upper(int t, int* row, int* col) {
     *row = t; *col = c;
 }
 
-template <int TM, int TN, bool SPLIT, int PH, bool ONE>
-__global__ __launch_bounds__(256, SPLIT && TM == 2 ? 1 : 2) void ns_product_kernel(MuonPlan p, MuonArgs a, _Float16* ws, float* diag, float* part, int from) {
+template <int TM, int TN, bool SPLIT, int PH, int NST>
+__global__ __launch_bounds__(256, SPLIT && TM == 2 || NST > 2 ? 1 : 2) void ns_product_kernel(MuonPlan p, MuonArgs a, _Float16* ws, float* diag, float* part, int from) {
     extern __shared__ uint4 smem[];
     constexpr int BM = 64 * TM, BN = 64 * TN;
     // ids go round-robin to the eight XCDs: each takes a contiguous range of tiles
     int lin = blockIdx.x;
     const int n8 = gridDim.x & ~7;
     if (lin < n8) lin = (lin & 7) * (n8 >> 3) + (lin >> 3);
-    const MuonGroup& g = p.g[group_of(p, lin, [](const MuonGroup& x) { return PH == PH_GRAM ? x.gram0 : PH == PH_SQUARE ? x.square0 : x.apply0; })];
+    const int (&starts)[MUON_MAX_GROUPS] = PH == PH_GRAM ? p.at.gram : PH == PH_SQUARE ? p.at.square : p.at.apply;
+    const int group = group_of(starts, lin);
+    const MuonGroup& g = p.g[group];
     f32x16_t acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
@@ -345,7 +366,7 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 ? 1 : 2) void ns_product_kern
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     if constexpr (PH == PH_GRAM || PH == PH_SQUARE) {
         static_assert(TM == TN, "tiles on the diagonal are squares");
-        int local = lin - (PH == PH_GRAM ? g.gram0 : g.square0), split = 0;
+        int local = lin - starts[group], split = 0;
         if (PH == PH_GRAM) { split = local % g.splits; local /= g.splits; }
         const int k = local / g.grams;
         int tr, tc;
@@ -362,8 +383,8 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 ? 1 : 2) void ns_product_kern
             const _Float16* x = ws + g.x[from] + (long long)k * g.rp * g.cp;
             const int slabs = (g.tall ? g.rp : g.cp) / 64, per = (slabs + g.splits - 1) / g.splits;
             const int s0 = min(slabs, split * per), s1 = min(slabs, s0 + per);
-            if (g.tall) ns_tile<TM, TN, SPLIT, true, true, ONE>(acc, {x + tr * BM, g.cp, g.xplane}, {x + tc * BM, g.cp, g.xplane}, s0, s1, smem);
-            else ns_tile<TM, TN, SPLIT, false, false, ONE>(acc, {x + (long long)tr * BM * g.cp, g.cp, g.xplane}, {x + (long long)tc * BM * g.cp, g.cp, g.xplane}, s0, s1, smem);
+            if (g.tall) ns_tile<TM, TN, SPLIT, true, true, NST>(acc, {x + tr * BM, g.cp, g.xplane}, {x + tc * BM, g.cp, g.xplane}, s0, s1, smem);
+            else ns_tile<TM, TN, SPLIT, false, false, NST>(acc, {x + (long long)tr * BM * g.cp, g.cp, g.xplane}, {x + (long long)tc * BM * g.cp, g.cp, g.xplane}, s0, s1, smem);
             const bool whole = g.splits == 1;
             float* sum = part + g.part + ((long long)local * g.splits + split) * BM * BM;
             ns_values(acc, smem, whole && tr != tc, [](int, int) { return 0; }, [&](int r, int c, float (&v)[8], int) {
@@ -383,7 +404,7 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 ? 1 : 2) void ns_product_kern
             }, mirror);
         } else {
             const NsOperand A{s + (long long)tr * BM * g.mp, g.mp, g.splane}, B{s + (long long)tc * BM * g.mp, g.mp, g.splane};
-            ns_tile<TM, TN, SPLIT, false, false, ONE>(acc, A, B, 0, g.mp / 64, smem);
+            ns_tile<TM, TN, SPLIT, false, false, NST>(acc, A, B, 0, g.mp / 64, smem);
             ns_values(acc, smem, tr != tc, [&](int r, int c) {
                 const int row = tr * BM + r, col = tc * BM + c;
                 const _Float16* at = s + (long long)row * g.mp + col;
@@ -407,12 +428,12 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 ? 1 : 2) void ns_product_kern
             }, mirror);
         }
     } else {
-        const int local = lin - g.apply0, k = local / g.applies, t = local % g.applies, nc = g.cp / BN;
+        const int local = lin - starts[group], k = local / g.applies, t = local % g.applies, nc = g.cp / BN;
         const int tr = t / nc, tc = t % nc;
         const _Float16* x = ws + g.x[from] + (long long)k * g.rp * g.cp;
         const _Float16* b = ws + g.b + (long long)k * g.mp * g.mp;
-        if (g.tall) ns_tile<TM, TN, SPLIT, false, false, ONE>(acc, {x + (long long)tr * BM * g.cp, g.cp, g.xplane}, {b + (long long)tc * BN * g.mp, g.mp, g.splane}, 0, g.mp / 64, smem);
-        else ns_tile<TM, TN, SPLIT, false, true, ONE>(acc, {b + (long long)tr * BM * g.mp, g.mp, g.splane}, {x + tc * BN, g.cp, g.xplane}, 0, g.mp / 64, smem);
+        if (g.tall) ns_tile<TM, TN, SPLIT, false, false, NST>(acc, {x + (long long)tr * BM * g.cp, g.cp, g.xplane}, {b + (long long)tc * BN * g.mp, g.mp, g.splane}, 0, g.mp / 64, smem);
+        else ns_tile<TM, TN, SPLIT, false, true, NST>(acc, {b + (long long)tr * BM * g.mp, g.mp, g.splane}, {x + tc * BN, g.cp, g.xplane}, 0, g.mp / 64, smem);
         _Float16* to = ws + g.x[from ^ 1] + (long long)k * g.rp * g.cp;
         const long long at = tensor_at(g, k);
         const float* bd = diag + g.diag + (long long)(g.count + k) * g.mp;
@@ -437,16 +458,16 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 ? 1 : 2) void ns_product_kern
                 const long long q = at + (long long)row * g.cols + col;
                 const int n = min(8, g.cols - col);
                 if (a.theta) {
-                    if (n == 8 && (q & 3) == 0) {
+                    if (n == 8) {
                         f32x4_t w[2];
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) w[i] = *reinterpret_cast<const f32x4_t*>(a.theta + q + 4 * i);
+                        for (int i = 0; i < 2; ++i) w[i] = *reinterpret_cast<const f32x4u_t*>(a.theta + q + 4 * i);
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
 #pragma unroll
                             for (int e = 0; e < 4; ++e) w[i][e] = shrink * w[i][e] - step * v[4 * i + e];
-                            *reinterpret_cast<f32x4_t*>(a.theta + q + 4 * i) = w[i];
-                            if (a.shadow) { u32x2_t z; z[0] = pack_bf2(w[i][0], w[i][1]); z[1] = pack_bf2(w[i][2], w[i][3]); *reinterpret_cast<u32x2_t*>(a.shadow + q + 4 * i) = z; }
+                            *reinterpret_cast<f32x4u_t*>(a.theta + q + 4 * i) = w[i];
+                            if (a.shadow) { u32x2_t z; z[0] = pack_bf2(w[i][0], w[i][1]); z[1] = pack_bf2(w[i][2], w[i][3]); *reinterpret_cast<u32x2u_t*>(a.shadow + q + 4 * i) = z; }
                         }
                     } else {
                         float w[8];
@@ -458,6 +479,13 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 ? 1 : 2) void ns_product_kern
                             a.theta[q + e] = w[e];
                             if (a.shadow) a.shadow[q + e] = f2bf(w[e]);
                         }
+                    }
+                } else if (n == 8) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const f32x4_t w{DOWN * v[4 * i], DOWN * v[4 * i + 1], DOWN * v[4 * i + 2], DOWN * v[4 * i + 3]};
+                        if (a.out_bf16) { u32x2_t z; z[0] = pack_bf2(w[0], w[1]); z[1] = pack_bf2(w[2], w[3]); *reinterpret_cast<u32x2u_t*>(static_cast<unsigned short*>(a.out) + q + 4 * i) = z; }
+                        else *reinterpret_cast<f32x4u_t*>(static_cast<float*>(a.out) + q + 4 * i) = w;
                     }
                 } else {
 #pragma unroll
@@ -476,14 +504,16 @@ template <int T, bool SPLIT>
 __global__ __launch_bounds__(256) void ns_gram_sum_kernel(MuonPlan p, _Float16* ws, float* diag, const float* part) {
     constexpr int BM = 64 * T, LD = 65;
     __shared__ float s[64 * LD];
-    const MuonGroup& g = p.g[group_of(p, blockIdx.x, [](const MuonGroup& x) { return x.sum0; })];
-    const int local = blockIdx.x - g.sum0, tile = local / (T * T), sub = local % (T * T), k = tile / g.grams;
+    const int group = group_of(p.at.sum, blockIdx.x);
+    const MuonGroup& g = p.g[group];
+    const int local = blockIdx.x - p.at.sum[group], tile = local / (T * T), sub = local % (T * T), k = tile / g.grams;
     int tr, tc;
     upper(tile % g.grams, &tr, &tc);
     const int sr = sub / T * 64, sc = sub % T * 64;
     const float* from = part + g.part + (long long)tile * g.splits * BM * BM;
     const int r = threadIdx.x >> 2, c0 = (threadIdx.x & 3) * 16;
     f32x4_t v[4] = {};
+#pragma unroll 4
     for (int i = 0; i < g.splits; ++i)
 #pragma unroll
         for (int w = 0; w < 4; ++w) v[w] += *reinterpret_cast<const f32x4_t*>(from + (long long)i * BM * BM + (sr + r) * BM + sc + c0 + 4 * w);
@@ -556,8 +586,9 @@ __global__ __launch_bounds__(SMALL_THREADS) void muon_small_kernel(MuonPlan p, M
     __shared__ double lds_sum[16];
     constexpr int MP = 16 * MB, TILES = MB * MB, PARTS = small_parts(MB), KS = (MP + 31) / 32, PLACES = MB <= 2 ? 2 : 1;
     constexpr bool KEEP = MB <= 2;          // B's fragments stay in registers
-    const MuonGroup& g = p.g[group_of(p, blockIdx.x, [](const MuonGroup& x) { return x.apply0; })];
-    const int local = blockIdx.x - g.apply0, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int group = group_of(p.at.apply, blockIdx.x);
+    const MuonGroup& g = p.g[group];
+    const int local = blockIdx.x - p.at.apply[group], tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     auto direction = [&](float gr, float v) { return !a.velocity ? gr : a.nesterov ? gr + a.momentum * v : v; };
     if (!g.ortho) {
         const int k = local / g.chunks;
@@ -766,25 +797,25 @@ __global__ __launch_bounds__(SMALL_THREADS) void muon_small_kernel(MuonPlan p, M
     });
 }
 
-constexpr int lds_bytes(int TM, int TN, bool split, bool one) {
-    const int loop = (one ? 1 : 2) * (split ? 2 : 1) * 64 * (TM + TN) * 128, values = 4 * 32 * (32 * TN + 4) * 4;
+constexpr int lds_bytes(int TM, int TN, bool split, int nst) {
+    const int loop = nst * (split ? 2 : 1) * 64 * (TM + TN) * 128, values = 4 * 32 * (32 * TN + 4) * 4;
     return loop > values ? loop : values;
 }
-template <int TM, int TN, bool SPLIT, int PH, bool ONE>
+template <int TM, int TN, bool SPLIT, int PH, int NST>
 void run_product(int n, const MuonPlan& p, const MuonArgs& a, _Float16* ws, float* diag, float* part, int from, hipStream_t st) {
-    ns_product_kernel<TM, TN, SPLIT, PH, ONE><<<n, 256, lds_bytes(TM, TN, SPLIT, ONE), st>>>(p, a, ws, diag, part, from);
+    ns_product_kernel<TM, TN, SPLIT, PH, NST><<<n, 256, lds_bytes(TM, TN, SPLIT, NST), st>>>(p, a, ws, diag, part, from);
 }
 
 // T: edge of the Gram and square tiles; AM, AN: of the last product's
-template <int T, int AM, int AN, bool SPLIT, bool ONE>
+template <int T, int AM, int AN, bool SPLIT, int SN, int AN_ST>
 hipError_t run_products(const MuonPlan& p, const MuonArgs& a, _Float16* ws, float* diag, float* part, hipStream_t st) {
     for (int i = 0; i < NS_STEPS; ++i) {
         const int from = i & 1;
-        run_product<T, T, SPLIT, PH_GRAM, false>(p.grams, p, a, ws, diag, part, from, st);
+        run_product<T, T, SPLIT, PH_GRAM, SN>(p.grams, p, a, ws, diag, part, from, st);
         if (p.sums) ns_gram_sum_kernel<T, SPLIT><<<p.sums, 256, 0, st>>>(p, ws, diag, part);
-        run_product<T, T, SPLIT, PH_SQUARE, false>(p.squares, p, a, ws, diag, part, from, st);
-        if (i + 1 < NS_STEPS) run_product<AM, AN, SPLIT, PH_APPLY, ONE>(p.applies, p, a, ws, diag, part, from, st);
-        else run_product<AM, AN, SPLIT, PH_LAST, ONE>(p.applies, p, a, ws, diag, part, from, st);
+        run_product<T, T, SPLIT, PH_SQUARE, SN>(p.squares, p, a, ws, diag, part, from, st);
+        if (i + 1 < NS_STEPS) run_product<AM, AN, SPLIT, PH_APPLY, AN_ST>(p.applies, p, a, ws, diag, part, from, st);
+        else run_product<AM, AN, SPLIT, PH_LAST, AN_ST>(p.applies, p, a, ws, diag, part, from, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -796,6 +827,7 @@ hipError_t run_products(const MuonPlan& p, const MuonArgs& a, _Float16* ws, floa
 bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
     MuonPlan p{};
     p.n = n;
+    for (int i = 0; i < MUON_MAX_GROUPS; ++i) p.at.chunk[i] = p.at.cast[i] = p.at.gram[i] = p.at.square[i] = p.at.apply[i] = p.at.sum[i] = 0x7FFFFFFF;
     p.exact = exact;
     const long long most = 0x7FFFFFFF;
     auto up = [](long long v, long long m) { return (v + m - 1) / m * m; };
@@ -816,7 +848,7 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
                 MuonGroup& q = p.g[i] = g[i];
                 q.tall = q.rows > q.cols;
                 q.chunks = (int)(((long long)q.rows * q.cols + FLAT - 1) / FLAT);
-                q.apply0 = (int)groups;
+                p.at.apply[i] = (int)groups;
                 groups += (long long)q.count * (q.ortho ? 1 : q.chunks);
                 if (groups > most) return false;
             }
@@ -832,7 +864,7 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
         for (int i = 0; i < n; ++i) if (g[i].ortho) t += (long long)g[i].count * ((g[i].rows + high - 1) / high) * ((g[i].cols + wide - 1) / wide);
         return t;
     };
-    p.tile = !exact && tiles(256, 128) >= 480 ? 2 : tiles(128, 128) >= 256 ? 1 : 0;
+    p.tile = !exact && tiles(256, 128) >= 480 ? 2 : tiles(128, 128) >= 700 ? 1 : 0;
     const int edge = p.tile ? 128 : 64, high = p.tile == 2 ? 256 : edge;
     long long halves = 0, floats = 0, diags = 0, chunks = 0, casts = 0, grams = 0, squares = 0, applies = 0, sums = 0, slabs = 0;
     for (int i = 0; i < n; ++i) {
@@ -845,20 +877,20 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
         if (q.ortho) slabs += (long long)q.count * q.grams * (std::max(q.rp, q.cp) / 64);
     }
     // Gram tiles: as many parts along the contraction as make about two workgroups a CU of the launch, none shorter than eight slabs
-    const long long target = std::max<long long>(8, (slabs + 511) / 512);
+    const long long target = std::max<long long>(8, slabs / 320);
     for (int i = 0; i < n; ++i) {
         MuonGroup& q = p.g[i];
         const long long size = (long long)q.rows * q.cols;
-        q.chunk0 = (int)chunks; q.chunks = (int)((size + FLAT - 1) / FLAT);
+        p.at.chunk[i] = (int)chunks; q.chunks = (int)((size + FLAT - 1) / FLAT);
         chunks += (long long)q.count * q.chunks;
-        q.cast0 = (int)casts; q.gram0 = (int)grams; q.square0 = (int)squares; q.apply0 = (int)applies; q.sum0 = (int)sums;
+        p.at.cast[i] = (int)casts; p.at.gram[i] = (int)grams; p.at.square[i] = (int)squares; p.at.apply[i] = (int)applies; p.at.sum[i] = (int)sums;
         if (chunks > most) return false;
         if (!q.ortho) continue;
         const long long nx = (long long)q.rp * q.cp, ns = (long long)q.mp * q.mp;
         if ((long long)std::max(q.rp, q.cp) * 256 > most || nx / CAST * q.count > most) return false;
         q.casts = (int)(nx / CAST);
         casts += (long long)q.count * q.casts;
-        q.splits = (int)((std::max(q.rp, q.cp) / 64 + target - 1) / target);
+        q.splits = std::max(1, (int)((std::max(q.rp, q.cp) / 64 + target / 2) / target));
         grams += (long long)q.count * q.grams * q.splits;
         squares += (long long)q.count * q.grams;
         q.applies = (int)(nx / high / edge);
@@ -900,9 +932,9 @@ hipError_t launch_muon(const MuonPlan& p, const MuonArgs& a, void* scratch, hipS
     muon_cast_kernel<<<p.casts, 256, 0, st>>>(p, a, sums, ws);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (p.tile == 2) return run_products<2, 4, 2, false, true>(p, a, ws, diag, part, st);
-    if (p.tile == 1) return p.exact ? run_products<2, 2, 2, true, false>(p, a, ws, diag, part, st) : run_products<2, 2, 2, false, false>(p, a, ws, diag, part, st);
-    return p.exact ? run_products<1, 1, 1, true, false>(p, a, ws, diag, part, st) : run_products<1, 1, 1, false, false>(p, a, ws, diag, part, st);
+    if (p.tile == 2) return run_products<2, 4, 2, false, 2, 1>(p, a, ws, diag, part, st);
+    if (p.tile == 1) return p.exact ? run_products<2, 2, 2, true, 2, 2>(p, a, ws, diag, part, st) : run_products<2, 2, 2, false, 2, 2>(p, a, ws, diag, part, st);
+    return p.exact ? run_products<1, 1, 1, true, 2, 2>(p, a, ws, diag, part, st) : run_products<1, 1, 1, false, 2, 2>(p, a, ws, diag, part, st);
 }
 
 }  // namespace blstm

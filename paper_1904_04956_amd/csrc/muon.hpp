@@ -18,14 +18,14 @@ struct MuonGroup {
     long long x[2], s, b, xplane, splane;      // elements of 2 bytes from the scratch's start
     long long diag;                            // of the diagonals of S, then of B: float elements from their start, count x mp each
     long long part;                            // float elements from the partial sums' start
-    int chunk0, chunks;                        // the flat passes' units: the group's first one, how many a tensor has
-    int cast0, casts;
-    int gram0, grams;                          // product tiles of a matrix on and above the diagonal; gram0 counts every part
-    int square0, apply0, applies;
-    int sum0;
+    int chunks, casts;                         // the flat passes' units of a tensor
+    int grams, applies;                        // product tiles of a matrix: on and above the diagonal, all
 };
+// Where each group's units begin in a launch (INT_MAX behind the last group): side by side, so that a workgroup finds its group with one wait.
+struct MuonStarts { int chunk[MUON_MAX_GROUPS], cast[MUON_MAX_GROUPS], gram[MUON_MAX_GROUPS], square[MUON_MAX_GROUPS], apply[MUON_MAX_GROUPS], sum[MUON_MAX_GROUPS]; };
 struct MuonPlan {
     MuonGroup g[MUON_MAX_GROUPS];
+    MuonStarts at;
     int n;
     int tile;                 // 0: 64 x 64 tiles, 1: 128 x 128, 2: 128 x 128 and, in the last product, 256 x 128;
                               // 3: a matrix a workgroup, all in LDS (small: blocks of 16 rows of the largest Gram matrix, lds: bytes)
