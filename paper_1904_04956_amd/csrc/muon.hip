@@ -6,8 +6,9 @@
 // entries of a normalised matrix, 1/sqrt(m n), and what their rounding leaves over away from the subnormals; none exceeds 2^8 for X and S and
 // about 2^12 for B.  Products accumulate in float.  X itself is kept as the sum of two halves (22 bits): a rounding of X adds noise in all
 // directions alike, and where a few directions hold most of |d| (gradients do) that noise is as large as the others; the step's other
-// roundings pass through B X, which is small where the singular value is.  So mode 1 multiplies by the first half only and adds a X from both: off by
-// about 3e-4 of X.  Mode 0 multiplies both halves (three products): off by about 1e-6.
+// roundings pass through B X, which is small where the singular value is.  So mode 1 multiplies the first halves only and adds a X from both: off by
+// about 4e-4 of X (of which X's rounding in S 3.3e-4, S's 1.7e-4, B's 1.6e-4, X's in B X 1.4e-4: 301 x 602; small launches, with time to spare, multiply both halves
+// for S: 2.8e-4).  Mode 0 multiplies both halves everywhere (three products): off by about 1e-6.
 // The diagonals of S and B, which near the end are most of them, stay out of the halves and the products, in float: with D the diagonal and R the rest,
 // S^2 = D^2 + D R + R D + R^2, and B X = D X + R X (rounded with the rest they alone put X off by 2e-3).
 // The Frobenius norm is summed in double (squares of floats leave float's range) in a fixed order.
@@ -346,7 +347,8 @@ __device__ __forceinline__ void upper(int t, int* row, int* col) {
     *row = t; *col = c;
 }
 
-template <int TM, int TN, bool SPLIT, int PH, int NST>
+// SPLIT: the operands' second halves are multiplied too; LO: S and B have second halves
+template <int TM, int TN, bool SPLIT, bool LO, int PH, int NST>
 __global__ __launch_bounds__(256, SPLIT && TM == 2 || NST > 2 ? 1 : 2) void ns_product_kernel(MuonPlan p, MuonArgs a, _Float16* ws, float* diag, float* part, int from) {
     extern __shared__ uint4 smem[];
     constexpr int BM = 64 * TM, BN = 64 * TN;
@@ -377,7 +379,7 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 || NST > 2 ? 1 : 2) void ns_p
         _Float16* out = PH == PH_GRAM ? s : ws + g.b + (long long)k * g.mp * g.mp;
         auto mirror = [&](int r, int c, const float (&v)[8]) {
             const long long o = (long long)(tc * BM + r) * g.mp + tr * BM + c;
-            put_halves(out + o, SPLIT ? out + g.splane + o : nullptr, v);
+            put_halves(out + o, LO ? out + g.splane + o : nullptr, v);
         };
         if constexpr (PH == PH_GRAM) {
             const _Float16* x = ws + g.x[from] + (long long)k * g.rp * g.cp;
@@ -400,7 +402,7 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 || NST > 2 ? 1 : 2) void ns_p
                     v[e] *= DOWN;
                     if (on == e) { sd[row] = DOWN * v[e]; v[e] = 0.0f; }
                 }
-                put_halves(out + o, SPLIT ? out + g.splane + o : nullptr, v);
+                put_halves(out + o, LO ? out + g.splane + o : nullptr, v);
             }, mirror);
         } else {
             const NsOperand A{s + (long long)tr * BM * g.mp, g.mp, g.splane}, B{s + (long long)tc * BM * g.mp, g.mp, g.splane};
@@ -410,7 +412,7 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 || NST > 2 ? 1 : 2) void ns_p
                 const _Float16* at = s + (long long)row * g.mp + col;
                 Halves x;
                 x.h = *reinterpret_cast<const f16x8_t*>(at);
-                if constexpr (SPLIT) x.l = *reinterpret_cast<const f16x8_t*>(at + g.splane); else x.l = f16x8_t{};
+                if constexpr (LO) x.l = *reinterpret_cast<const f16x8_t*>(at + g.splane); else x.l = f16x8_t{};
                 x.di = sd[row];
                 x.d0 = *reinterpret_cast<const f32x4_t*>(sd + col);
                 x.d1 = *reinterpret_cast<const f32x4_t*>(sd + col + 4);
@@ -424,7 +426,7 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 || NST > 2 ? 1 : 2) void ns_p
                     if (on == e) bd[row] = NS_B * x.di + NS_C * x.di * x.di + DOWN * full;
                     v[e] = on == e ? 0.0f : NS_B * y + NS_C * (x.di + (e < 4 ? x.d0[e & 3] : x.d1[e & 3])) * y + full;
                 }
-                put_halves(out + o, SPLIT ? out + g.splane + o : nullptr, v);
+                put_halves(out + o, LO ? out + g.splane + o : nullptr, v);
             }, mirror);
         }
     } else {
@@ -500,7 +502,7 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 || NST > 2 ? 1 : 2) void ns_p
 }
 
 // The parts of split Gram tiles, in order: 64 x 64 of a tile a workgroup.
-template <int T, bool SPLIT>
+template <int T, bool LO>
 __global__ __launch_bounds__(256) void ns_gram_sum_kernel(MuonPlan p, _Float16* ws, float* diag, const float* part) {
     constexpr int BM = 64 * T, LD = 65;
     __shared__ float s[64 * LD];
@@ -533,12 +535,12 @@ __global__ __launch_bounds__(256) void ns_gram_sum_kernel(MuonPlan p, _Float16* 
         const long long o = (long long)(tr * BM + sr + r) * g.mp + tc * BM + sc + c0 + 8 * w;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = s[r * LD + c0 + 8 * w + e];
-        put_halves(out + o, SPLIT ? out + g.splane + o : nullptr, x);
+        put_halves(out + o, LO ? out + g.splane + o : nullptr, x);
         if (tr == tc) continue;
         const long long m = (long long)(tc * BM + sc + r) * g.mp + tr * BM + sr + c0 + 8 * w;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = s[(c0 + 8 * w + e) * LD + r];
-        put_halves(out + m, SPLIT ? out + g.splane + m : nullptr, x);
+        put_halves(out + m, LO ? out + g.splane + m : nullptr, x);
     }
 }
 
@@ -801,21 +803,21 @@ constexpr int lds_bytes(int TM, int TN, bool split, int nst) {
     const int loop = nst * (split ? 2 : 1) * 64 * (TM + TN) * 128, values = 4 * 32 * (32 * TN + 4) * 4;
     return loop > values ? loop : values;
 }
-template <int TM, int TN, bool SPLIT, int PH, int NST>
+template <int TM, int TN, bool SPLIT, bool LO, int PH, int NST>
 void run_product(int n, const MuonPlan& p, const MuonArgs& a, _Float16* ws, float* diag, float* part, int from, hipStream_t st) {
-    ns_product_kernel<TM, TN, SPLIT, PH, NST><<<n, 256, lds_bytes(TM, TN, SPLIT, NST), st>>>(p, a, ws, diag, part, from);
+    ns_product_kernel<TM, TN, SPLIT, LO, PH, NST><<<n, 256, lds_bytes(TM, TN, SPLIT, NST), st>>>(p, a, ws, diag, part, from);
 }
 
 // T: edge of the Gram and square tiles; AM, AN: of the last product's
-template <int T, int AM, int AN, bool SPLIT, int SN, int AN_ST>
+template <int T, int AM, int AN, bool FINE, bool SPLIT, int SN, int AN_ST>
 hipError_t run_products(const MuonPlan& p, const MuonArgs& a, _Float16* ws, float* diag, float* part, hipStream_t st) {
     for (int i = 0; i < NS_STEPS; ++i) {
         const int from = i & 1;
-        run_product<T, T, SPLIT, PH_GRAM, SN>(p.grams, p, a, ws, diag, part, from, st);
+        run_product<T, T, FINE, SPLIT, PH_GRAM, SN>(p.grams, p, a, ws, diag, part, from, st);
         if (p.sums) ns_gram_sum_kernel<T, SPLIT><<<p.sums, 256, 0, st>>>(p, ws, diag, part);
-        run_product<T, T, SPLIT, PH_SQUARE, SN>(p.squares, p, a, ws, diag, part, from, st);
-        if (i + 1 < NS_STEPS) run_product<AM, AN, SPLIT, PH_APPLY, AN_ST>(p.applies, p, a, ws, diag, part, from, st);
-        else run_product<AM, AN, SPLIT, PH_LAST, AN_ST>(p.applies, p, a, ws, diag, part, from, st);
+        run_product<T, T, SPLIT, SPLIT, PH_SQUARE, SN>(p.squares, p, a, ws, diag, part, from, st);
+        if (i + 1 < NS_STEPS) run_product<AM, AN, SPLIT, SPLIT, PH_APPLY, AN_ST>(p.applies, p, a, ws, diag, part, from, st);
+        else run_product<AM, AN, SPLIT, SPLIT, PH_LAST, AN_ST>(p.applies, p, a, ws, diag, part, from, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -828,7 +830,6 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
     MuonPlan p{};
     p.n = n;
     for (int i = 0; i < MUON_MAX_GROUPS; ++i) p.at.chunk[i] = p.at.cast[i] = p.at.gram[i] = p.at.square[i] = p.at.apply[i] = p.at.sum[i] = 0x7FFFFFFF;
-    p.exact = exact;
     const long long most = 0x7FFFFFFF;
     auto up = [](long long v, long long m) { return (v + m - 1) / m * m; };
     // small matrices only: a workgroup each
@@ -859,6 +860,12 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
             return true;
         }
     }
+    // The entries of a step are lr / sqrt(cols) in size, so that O's error reaches the weights with 1 / sqrt(cols): matrices of few columns (512 a row over all of
+    // them) get products of both planes in mode 1 too.  Two layers of 301 cells, gates apart, all launches: 240 -> 295 us; it would be 911 -> 2100 for four of 512.
+    long long elements = 0, rows = 0;
+    for (int i = 0; i < n; ++i) if (g[i].ortho) { rows += (long long)g[i].count * g[i].rows; elements += (long long)g[i].count * g[i].rows * g[i].cols; }
+    exact = exact || elements < 512 * rows;
+    p.exact = exact;
     auto tiles = [&](int high, int wide) {              // of the last product
         long long t = 0;
         for (int i = 0; i < n; ++i) if (g[i].ortho) t += (long long)g[i].count * ((g[i].rows + high - 1) / high) * ((g[i].cols + wide - 1) / wide);
@@ -932,9 +939,9 @@ hipError_t launch_muon(const MuonPlan& p, const MuonArgs& a, void* scratch, hipS
     muon_cast_kernel<<<p.casts, 256, 0, st>>>(p, a, sums, ws);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (p.tile == 2) return run_products<2, 4, 2, false, 2, 1>(p, a, ws, diag, part, st);
-    if (p.tile == 1) return p.exact ? run_products<2, 2, 2, true, 2, 2>(p, a, ws, diag, part, st) : run_products<2, 2, 2, false, 2, 2>(p, a, ws, diag, part, st);
-    return p.exact ? run_products<1, 1, 1, true, 2, 2>(p, a, ws, diag, part, st) : run_products<1, 1, 1, false, 2, 2>(p, a, ws, diag, part, st);
+    if (p.tile == 2) return run_products<2, 4, 2, false, false, 2, 1>(p, a, ws, diag, part, st);
+    if (p.tile == 1) return p.exact ? run_products<2, 2, 2, true, true, 2, 2>(p, a, ws, diag, part, st) : run_products<2, 2, 2, false, false, 2, 2>(p, a, ws, diag, part, st);
+    return p.exact ? run_products<1, 1, 1, true, true, 2, 2>(p, a, ws, diag, part, st) : run_products<1, 1, 1, true, false, 2, 2>(p, a, ws, diag, part, st);
 }
 
 }  // namespace blstm
