@@ -64,13 +64,17 @@ class Learner:
         self.z = torch.zeros((T, B, self.zdim), dtype=self.act_dtype, device=dev)
         self.dz = torch.zeros((T, B, self.zdim), dtype=self.act_dtype, device=dev)
         self.loss = torch.zeros(1, dtype=torch.float32, device=dev)
-        self.scratch = {}         # of the softmax layer's calls beyond cross-entropy, each made when it is first used
+        self.scratch = {}         # of the calls that take scratch, each made when it is first used
+        self.adapters = None      # attach_adapters()
         self.held = None          # HYBRID only: the pulled weights the next gradient is taken on
 
     def close(self):
         if self.ctx is not None:
             bl.blstm_destroy(self.ctx)
             self.ctx = None
+        if getattr(self, "adapters", None) is not None:
+            self.adapters.close()
+            self.adapters = None
 
     def __del__(self):
         try:
@@ -89,6 +93,8 @@ class Learner:
     def weights_changed(self):
         """To be called after anything has written the weights (or the held copy) outside this class."""
         bl.blstm_weights_changed(self.ctx)
+        if self.adapters is not None:
+            bl.blstm_weights_changed(self.adapters.stack)
 
     def set_batch(self, x_f32: np.ndarray, labels_i32: np.ndarray):
         self.x.copy_(torch.from_numpy(x_f32).to(self.act_dtype))
@@ -186,6 +192,67 @@ class Learner:
         bl.sgd_step(self.theta, self.shadow, self.grad, self.n, lr, self.momentum, self.velocity, stream)
         self.weights_changed()
 
+    def apply_muon(self, lr, lr_rest, momentum=0.95, weight_decay=0.0, nesterov=True, gates=False, softmax=False, stream=None):
+        """W' = apply(W, g) with the matrices' updates orthogonalised (binding.muon_step): the LSTM's and the bottleneck's at lr, with `softmax` the softmax
+        layer's too; the rest at lr_rest.  `gates`: each gate's block is a matrix of its own.  The velocity is the learner's (made of zeros at first use)."""
+        if momentum != 0.0 and self.velocity is None:
+            self.velocity = self._zeros((self.n,), torch.float32, stream)
+        flags = (bl.MUON_NESTEROV if nesterov else 0) | (bl.MUON_GATES if gates else 0) | (bl.MUON_SOFTMAX if softmax else 0)
+        bl.muon_step(self.ctx, self.theta, self.shadow, self.grad, self.velocity, lr, lr_rest, momentum, weight_decay, flags,
+                     self._kept(("muon", flags), lambda: bl.muon_scratch_bytes(self.ctx, flags), stream), None, stream)
+        self.weights_changed()
+
+    def _kept(self, key, nbytes, stream):
+        """Scratch of a call, kept for the next time: a captured graph holds its address."""
+        if key not in self.scratch:
+            self.scratch[key] = self._empty((nbytes(),), torch.uint8, stream)
+        return self.scratch[key]
+
+    def _zeros(self, shape, dtype, stream):
+        if stream is not None and not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream), device=self.device)
+        with torch.cuda.stream(stream):
+            return torch.zeros(shape, dtype=dtype, device=self.device)
+
+    # ---- low-rank adapters beside the bottleneck's projection ------------------------------
+    def attach_adapters(self, count, rank, scale=1.0):
+        """`count` adapters of `rank` beside the bottleneck (binding.adapter_forward, W = W_p), each sequence's by adapters.ids [B] (BLSTM_NO_ADAPTER at first).
+        Their factors are adapters.A [count][rank][2H] and .Bm [count][P][rank], float, zero at first; after writing them call adapters.refresh()."""
+        if self.dims["P"] == 0:
+            raise ValueError("adapters stand beside the bottleneck's projection, and this model has none")
+        if self.adapters is not None:
+            self.adapters.close()
+        self.adapters = Adapters(self, count, rank, scale)
+        # the passes run on the stack's own context below, so nothing of the softmax layer's gradient may be left to this one's backward pass
+        bl.blstm_set_option(self.ctx, bl.BLSTM_OPT_DEFER_SOFTMAX_WGRAD, 0)
+        self.defer_softmax_wgrad = False
+        return self.adapters
+
+    def forward_adapted(self, stream=None):
+        """z of the batch with each sequence's adapter."""
+        a = self.adapters
+        bl.blstm_forward(a.stack, self.theta_fwd, self.x, a.h, stream)
+        bl.adapter_forward(a.cfg, a.W, a.b, a.A_fwd, a.Bm_fwd, a.ids, a.h, self.z, a.t, self._kept(("adapt", bl.ADAPTER_FORWARD), lambda: bl.adapter_scratch_bytes(a.cfg, bl.ADAPTER_FORWARD), stream),
+                           None, stream)
+
+    def calgrad_adapted(self, shared=True, stream=None):
+        """calgrad() with the adapters: their gradients in adapters.dA and .dB and, with `shared`, the model's in grad (without: the softmax layer's alone)."""
+        a = self.adapters
+        self.forward_adapted(stream)
+        bl.softmax_xent_fwd_bwd(self.ctx, self.theta_fwd, self.z, self.labels, self.loss, self.dz, self.grad, stream)
+        bl.adapter_backward(a.cfg, a.W, a.A_fwd, a.Bm_fwd, a.ids, a.h, a.t, self.dz, a.dh if shared else None, a.dA, a.dB, a.dW if shared else None,
+                            a.db if shared else None, self._kept(("adapt", bl.ADAPTER_BACKWARD), lambda: bl.adapter_scratch_bytes(a.cfg, bl.ADAPTER_BACKWARD), stream), None, stream)
+        if shared:
+            bl.blstm_backward(a.stack, self.theta_fwd, self.x, a.dh, self.grad, stream)
+
+    def apply_adapters(self, lr, momentum=0.95, weight_decay=0.0, nesterov=True, stream=None):
+        """The orthogonalised update of every adapter's two factors (binding.muon_matrices_step)."""
+        a = self.adapters
+        for name, theta, shadow, grad, velocity in (("A", a.A, a.A_bf16, a.dA, a.vA), ("B", a.Bm, a.Bm_bf16, a.dB, a.vB)):
+            sizes = (*theta.shape, self.mode)
+            bl.muon_matrices_step(theta, shadow, grad, velocity, *sizes, lr, momentum, weight_decay, bl.MUON_NESTEROV if nesterov else 0,
+                                  self._kept(("muon", name, sizes), lambda: bl.muon_orthogonalize_scratch_bytes(*sizes), stream), None, stream)
+
     def hold(self):
         """Keeps a copy of the weights as forward/backward read them now (a device-to-device copy on
         torch's current stream): what pull_weights() returned, for the next iteration's gradient."""
@@ -214,6 +281,49 @@ class Learner:
 
     def z_numpy(self) -> np.ndarray:
         return self.z.float().cpu().numpy()
+
+
+class Adapters:
+    """Buffers of a learner's adapters, and a context of the LSTM stack alone: its z is what the bottleneck's projection reads, and its parameters are the
+    beginning of the model's vector."""
+
+    def __init__(self, learner, count, rank, scale):
+        d, dev, kind = learner.dims, learner.device, learner.act_dtype
+        T, B, K, N = d["T"], d["B"], 2 * d["H"], d["P"]
+        self.cfg = bl.adapter_config(T, B, K, N, rank, count, learner.mode, scale)
+        bl.adapter_scratch_bytes(self.cfg, bl.ADAPTER_BACKWARD)          # refuses what the calls would
+        self.stack = bl.blstm_create(T, B, d["D"], d["H"], d["L"], 0, 1, learner.mode)
+        bl.blstm_set_option(self.stack, bl.BLSTM_OPT_KEEP_WEIGHT_COPIES, 1)
+        self.workspace = torch.empty(bl.blstm_workspace_bytes(self.stack), dtype=torch.uint8, device=dev)
+        bl.blstm_bind(self.stack, self.workspace)
+        real = lambda *shape: torch.zeros(shape, dtype=torch.float32, device=dev)  # noqa: E731
+        self.A, self.Bm, self.dA, self.dB, self.vA, self.vB = (real(count, *s) for s in 3 * ((rank, K), (N, rank)))
+        self.A_bf16, self.Bm_bf16 = (torch.zeros_like(t, dtype=torch.bfloat16) if learner.mode == 1 else None for t in (self.A, self.Bm))
+        self.ids = torch.full((B,), bl.BLSTM_NO_ADAPTER, dtype=torch.int32, device=dev)
+        self.h, self.dh = (torch.zeros((T, B, K), dtype=kind, device=dev) for _ in range(2))
+        self.t = real(T, B, rank)
+        part = lambda flat, which: flat[slice(*(lambda o, n: (o, o + n))(*bl.blstm_param_offset(learner.ctx, 0, 0, which)))]  # noqa: E731
+        self.W, self.b = part(learner.theta_fwd, bl.BLSTM_WP), part(learner.theta_fwd, bl.BLSTM_BP)
+        self.dW, self.db = part(learner.grad, bl.BLSTM_WP), part(learner.grad, bl.BLSTM_BP)
+
+    @property
+    def A_fwd(self):
+        return self.A if self.A_bf16 is None else self.A_bf16
+
+    @property
+    def Bm_fwd(self):
+        return self.Bm if self.Bm_bf16 is None else self.Bm_bf16
+
+    def refresh(self, stream=None):
+        """After writing A or Bm: their bf16 copies anew."""
+        for master, copy in ((self.A, self.A_bf16), (self.Bm, self.Bm_bf16)):
+            if copy is not None:
+                bl.blstm_shadow_refresh(master, copy, master.numel(), stream)
+
+    def close(self):
+        if self.stack is not None:
+            bl.blstm_destroy(self.stack)
+            self.stack = None
 
 
 def learner_for(workload: inputs.Workload, B=None, device="cuda:0", momentum=0.0) -> Learner:
