@@ -114,7 +114,8 @@ __device__ __forceinline__ void mma16(f32x4_t& acc, const uint4& a, const uint4&
         for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], acc, 0, 0, 0);
     }
 }
-// elements [k, k + 16 bytes) of a row of n, zero beyond it
+// elements [k, k + 16 bytes) of a row of n, zero beyond it.  VECTOR: rows are whole aligned 16-byte words; else words start anywhere and a row's last may be short.
+typedef uint32_t u32x4e_t __attribute__((ext_vector_type(4), aligned(2)));
 template <typename T, bool VECTOR>
 __device__ __forceinline__ uint4 load_chunk(const T* row, int k, int n) {
     constexpr int V = Vec<T>::N;
@@ -122,6 +123,7 @@ __device__ __forceinline__ uint4 load_chunk(const T* row, int k, int n) {
         if (k < n) { const u32x4_t v = *reinterpret_cast<const u32x4_t*>(row + k); return make_uint4(v[0], v[1], v[2], v[3]); }
         return make_uint4(0u, 0u, 0u, 0u);
     } else {
+        if (k + V <= n) { const u32x4_t v = *reinterpret_cast<const u32x4e_t*>(row + k); return make_uint4(v[0], v[1], v[2], v[3]); }
         uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
         for (int e = 0; e < V; ++e) {
@@ -488,7 +490,8 @@ __global__ __launch_bounds__(256) void adapt_tile_kernel(ProjectArgs a, bool low
     }
     // (the products are computed transposed: a lane holds four neighbouring columns of a row)
     T* y = static_cast<T*>(a.y);
-    const bool words = s.N % 4 == 0 && (reinterpret_cast<uintptr_t>(y) & (4 * ES - 1)) == 0;
+    typedef uint32_t u32x2e_t __attribute__((ext_vector_type(2), aligned(2)));
+    typedef float f32x4e_t __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int n = col0 + 32 * wave + 16 * j + 4 * fg;
@@ -503,9 +506,9 @@ __global__ __launch_bounds__(256) void adapt_tile_kernel(ProjectArgs a, bool low
             if (16 * i + fr >= nrows) continue;
             T* to = y + (long long)rows[16 * i + fr] * s.N + n;
             const f32x4_t v = acc[i][j] + bias;
-            if (words) {
-                if constexpr (ES == 2) { u32x2_t w; w[0] = pack_bf2(v[0], v[1]); w[1] = pack_bf2(v[2], v[3]); *reinterpret_cast<u32x2_t*>(to) = w; }
-                else *reinterpret_cast<f32x4_t*>(to) = v;
+            if (n + 4 <= s.N) {
+                if constexpr (ES == 2) { u32x2_t w; w[0] = pack_bf2(v[0], v[1]); w[1] = pack_bf2(v[2], v[3]); *reinterpret_cast<u32x2e_t*>(to) = w; }
+                else *reinterpret_cast<f32x4e_t*>(to) = v;
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) if (n + e < s.N) st_f(to + e, v[e]);
