@@ -352,13 +352,13 @@ template <int TM, int TN, bool SPLIT, bool LO, int PH, int NST>
 __global__ __launch_bounds__(256, SPLIT && TM == 2 || NST > 2 ? 1 : 2) void ns_product_kernel(MuonPlan p, MuonArgs a, _Float16* ws, float* diag, float* part, int from) {
     extern __shared__ uint4 smem[];
     constexpr int BM = 64 * TM, BN = 64 * TN;
-    // ids go round-robin to the eight XCDs: each takes a contiguous range of tiles
-    int lin = blockIdx.x;
-    const int n8 = gridDim.x & ~7;
-    if (lin < n8) lin = (lin & 7) * (n8 >> 3) + (lin >> 3);
+    // ids go round-robin to the eight XCDs: of each group (they differ in the length of their contractions) each XCD takes an eighth, neighbouring tiles
     const int (&starts)[MUON_MAX_GROUPS] = PH == PH_GRAM ? p.at.gram : PH == PH_SQUARE ? p.at.square : p.at.apply;
-    const int group = group_of(starts, lin);
+    const int group = group_of(starts, blockIdx.x);
     const MuonGroup& g = p.g[group];
+    const int units = g.count * (PH == PH_GRAM ? g.grams * g.splits : PH == PH_SQUARE ? g.grams : g.applies), own = blockIdx.x - starts[group];
+    const int lin = (own & 7) * ((units + 7) / 8) + (own >> 3);
+    if (lin >= units) return;
     f32x16_t acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
@@ -368,7 +368,7 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 || NST > 2 ? 1 : 2) void ns_p
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     if constexpr (PH == PH_GRAM || PH == PH_SQUARE) {
         static_assert(TM == TN, "tiles on the diagonal are squares");
-        int local = lin - starts[group], split = 0;
+        int local = lin, split = 0;
         if (PH == PH_GRAM) { split = local % g.splits; local /= g.splits; }
         const int k = local / g.grams;
         int tr, tc;
@@ -430,7 +430,7 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 || NST > 2 ? 1 : 2) void ns_p
             }, mirror);
         }
     } else {
-        const int local = lin - starts[group], k = local / g.applies, t = local % g.applies, nc = g.cp / BN;
+        const int local = lin, k = local / g.applies, t = local % g.applies, nc = g.cp / BN;
         const int tr = t / nc, tc = t % nc;
         const _Float16* x = ws + g.x[from] + (long long)k * g.rp * g.cp;
         const _Float16* b = ws + g.b + (long long)k * g.mp * g.mp;
@@ -829,6 +829,7 @@ hipError_t run_products(const MuonPlan& p, const MuonArgs& a, _Float16* ws, floa
 bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
     MuonPlan p{};
     p.n = n;
+    std::copy(g, g + n, p.g);
     for (int i = 0; i < MUON_MAX_GROUPS; ++i) p.at.chunk[i] = p.at.cast[i] = p.at.gram[i] = p.at.square[i] = p.at.apply[i] = p.at.sum[i] = 0x7FFFFFFF;
     const long long most = 0x7FFFFFFF;
     auto up = [](long long v, long long m) { return (v + m - 1) / m * m; };
@@ -846,7 +847,7 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
         if (fits && p.lds <= SMALL_LDS) {
             long long groups = 0;
             for (int i = 0; i < n; ++i) {
-                MuonGroup& q = p.g[i] = g[i];
+                MuonGroup& q = p.g[i];
                 q.tall = q.rows > q.cols;
                 q.chunks = (int)(((long long)q.rows * q.cols + FLAT - 1) / FLAT);
                 p.at.apply[i] = (int)groups;
@@ -874,8 +875,12 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
     p.tile = !exact && tiles(256, 128) >= 480 ? 2 : tiles(128, 128) >= 700 ? 1 : 0;
     const int edge = p.tile ? 128 : 64, high = p.tile == 2 ? 256 : edge;
     long long halves = 0, floats = 0, diags = 0, chunks = 0, casts = 0, grams = 0, squares = 0, applies = 0, sums = 0, slabs = 0;
+    // the longest contractions first: what is left at a launch's end is short
+    std::stable_sort(p.g, p.g + n, [](const MuonGroup& x, const MuonGroup& y) {
+        return (x.ortho ? std::min(x.rows, x.cols) : 0) > (y.ortho ? std::min(y.rows, y.cols) : 0);
+    });
     for (int i = 0; i < n; ++i) {
-        MuonGroup& q = p.g[i] = g[i];
+        MuonGroup& q = p.g[i];
         q.tall = q.rows > q.cols;
         q.rp = (int)up(q.rows, high); q.cp = (int)up(q.cols, edge);
         q.mp = std::min(q.rp, q.cp);
@@ -898,10 +903,11 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
         q.casts = (int)(nx / CAST);
         casts += (long long)q.count * q.casts;
         q.splits = std::max(1, (int)((std::max(q.rp, q.cp) / 64 + target / 2) / target));
-        grams += (long long)q.count * q.grams * q.splits;
-        squares += (long long)q.count * q.grams;
+        auto eighths = [](long long v) { return (v + 7) / 8 * 8; };
+        grams += eighths((long long)q.count * q.grams * q.splits);
+        squares += eighths((long long)q.count * q.grams);
         q.applies = (int)(nx / high / edge);
-        applies += (long long)q.count * q.applies;
+        applies += eighths((long long)q.count * q.applies);
         q.xplane = nx * q.count; q.splane = ns * q.count;
         for (int b = 0; b < 2; ++b) { q.x[b] = halves; halves += 2 * q.xplane; }
         q.s = halves; halves += (exact ? 2 : 1) * q.splane;
