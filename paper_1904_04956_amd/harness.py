@@ -232,8 +232,7 @@ class Learner:
         """z of the batch with each sequence's adapter."""
         a = self.adapters
         bl.blstm_forward(a.stack, self.theta_fwd, self.x, a.h, stream)
-        bl.adapter_forward(a.cfg, a.W, a.b, a.A_fwd, a.Bm_fwd, a.ids, a.h, self.z, a.t, self._kept(("adapt", bl.ADAPTER_FORWARD), lambda: bl.adapter_scratch_bytes(a.cfg, bl.ADAPTER_FORWARD), stream),
-                           None, stream)
+        bl.adapter_forward(a.cfg, a.W, a.b, a.A_fwd, a.Bm_fwd, a.ids, a.h, self.z, a.t, a.scratch(bl.ADAPTER_FORWARD, self, stream), None, stream)
 
     def calgrad_adapted(self, shared=True, stream=None):
         """calgrad() with the adapters: their gradients in adapters.dA and .dB and, with `shared`, the model's in grad (without: the softmax layer's alone)."""
@@ -241,7 +240,7 @@ class Learner:
         self.forward_adapted(stream)
         bl.softmax_xent_fwd_bwd(self.ctx, self.theta_fwd, self.z, self.labels, self.loss, self.dz, self.grad, stream)
         bl.adapter_backward(a.cfg, a.W, a.A_fwd, a.Bm_fwd, a.ids, a.h, a.t, self.dz, a.dh if shared else None, a.dA, a.dB, a.dW if shared else None,
-                            a.db if shared else None, self._kept(("adapt", bl.ADAPTER_BACKWARD), lambda: bl.adapter_scratch_bytes(a.cfg, bl.ADAPTER_BACKWARD), stream), None, stream)
+                            a.db if shared else None, a.scratch(bl.ADAPTER_BACKWARD, self, stream), None, stream)
         if shared:
             bl.blstm_backward(a.stack, self.theta_fwd, self.x, a.dh, self.grad, stream)
 
@@ -313,6 +312,9 @@ class Adapters:
     @property
     def Bm_fwd(self):
         return self.Bm if self.Bm_bf16 is None else self.Bm_bf16
+
+    def scratch(self, call, learner, stream):
+        return learner._kept(("adapt", call, self.cfg.rank, self.cfg.count), lambda: bl.adapter_scratch_bytes(self.cfg, call), stream)
 
     def refresh(self, stream=None):
         """After writing A or Bm: their bf16 copies anew."""

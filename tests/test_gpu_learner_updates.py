@@ -159,6 +159,26 @@ def test_a_captured_step_is_the_eager_one():
         two.close()
 
 
+def test_adapters_attached_anew():
+    # other sizes need other scratch
+    import torch
+    lrn, a, *_ = adapted(1, 86, count=2, rank=2, ids=[0, 1, -1, 1, 0, 1, 1, -1, 0])
+    try:
+        lrn.calgrad_adapted()
+        b = lrn.attach_adapters(300, 40)
+        b.A.normal_()
+        b.Bm.normal_()
+        b.refresh()
+        b.ids.copy_(torch.arange(9, dtype=torch.int32) * 30)
+        lrn.calgrad_adapted()
+        torch.cuda.synchronize()
+        used = torch.zeros(300, dtype=torch.bool, device="cuda:0")
+        used[b.ids.long()] = True
+        assert bool((b.dA[used].abs().amax((1, 2)) > 0).all()) and float(b.dA[~used].abs().max()) == 0.0 and bool(torch.isfinite(b.dB).all())
+    finally:
+        lrn.close()
+
+
 def test_a_model_without_bottleneck_has_no_place_for_adapters():
     lrn, *_ = learner(0, 85, P=0)
     try:

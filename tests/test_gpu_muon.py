@@ -59,21 +59,22 @@ def test_orthogonalize(mode, count, rows, cols):
 
 
 @pytest.mark.parametrize("mode", [0, 1])
-def test_gradients_of_any_size_zero_matrices_and_what_is_no_number(mode):
+@pytest.mark.parametrize("R,C", [(40, 70), (130, 200), (90, 700)], ids=["in one workgroup", "both halves", "long rows"])
+def test_gradients_of_any_size_zero_matrices_and_what_is_no_number(mode, R, C):
     import torch
     from paper_1904_04956_amd import binding as bl
     rng = np.random.default_rng(5)
-    G = gradient(rng, 8, 40, 70)
+    G = gradient(rng, 8, R, C)
     G[1] *= 1e-30                               # squares that float does not hold
     G[2] *= 1e30
     G[3] = 0
     G[4, 3, 5] = np.nan
-    G[5, 39, 69] = np.inf
+    G[5, R - 1, C - 1] = np.inf
     G[6, :, 3:] = 0                             # rank three
     G[7, 1:] = 0                                # one row
-    X = torch.empty((8, 40, 70), dtype=torch.bfloat16 if mode else torch.float32, device="cuda:0")
-    n = bl.muon_orthogonalize_scratch_bytes(8, 40, 70, mode)
-    bl.muon_orthogonalize(torch.from_numpy(G).to("cuda:0"), X, 8, 40, 70, mode, torch.empty(n, dtype=torch.uint8, device="cuda:0"))
+    X = torch.empty((8, R, C), dtype=torch.bfloat16 if mode else torch.float32, device="cuda:0")
+    n = bl.muon_orthogonalize_scratch_bytes(8, R, C, mode)
+    bl.muon_orthogonalize(torch.from_numpy(G).to("cuda:0"), X, 8, R, C, mode, torch.full((n,), 0x7F, dtype=torch.uint8, device="cuda:0"))
     got = X.float().cpu().numpy()
     assert np.all(got[3] == 0) and np.isnan(got[4]).all() and np.isnan(got[5]).all()
     for k in (0, 1, 2, 6, 7):
