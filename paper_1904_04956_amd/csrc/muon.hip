@@ -176,7 +176,6 @@ struct NsOperand { const _Float16* p; long long ld, plane; };      // tile origi
 template <int TM, int TN, bool SPLIT, bool AS, bool BS, int NST>
 __device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand& A, const NsOperand& B, int slab0, int slab1, uint4* smem) {
     constexpr bool ONE = NST == 1;
-    static_assert(!ONE || !SPLIT, "the registers hold one plane's fragments");
     constexpr int BM = 64 * TM, BN = 64 * TN, PL = SPLIT ? 2 : 1, PA = BM * 8, PB = BN * 8, STAGE = PL * (PA + PB);   // (in 16-byte words)
     constexpr int NIA = 2 * TM, NIB = 2 * TN, CPA = BM / 8, CPB = BN / 8;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv >> 1, wn = wv & 1;
@@ -242,20 +241,25 @@ __device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand
 #pragma unroll
     for (int i = 0; i < (ONE ? 1 : NST - 1); ++i) if (slab0 + i < slab1) issue(slab0 + i);
     if constexpr (ONE) {
-        uint4 fa[4][TM], fb[4][TN];
+        uint4 fa[4][PL][TM], fb[4][PL][TN];
         for (int it = slab0; it < slab1; ++it) {
             asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
+            for (int q = 0; q < 4; ++q)
 #pragma unroll
-                for (int i = 0; i < TM; ++i) fa[q][i] = frag_a(smem, i, q);
+                for (int pl = 0; pl < PL; ++pl) {
 #pragma unroll
-                for (int i = 0; i < TN; ++i) fb[q][i] = frag_b(smem + PA, i, q);
-            }
+                    for (int i = 0; i < TM; ++i) fa[q][pl][i] = frag_a(smem + pl * PA, i, q);
+#pragma unroll
+                    for (int i = 0; i < TN; ++i) fb[q][pl][i] = frag_b(smem + PL * PA + pl * PB, i, q);
+                }
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             if (it + 1 < slab1) issue(it + 1);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) mma(fa[q], fb[q]);
+            for (int q = 0; q < 4; ++q) {
+                if constexpr (SPLIT) { mma(fa[q][1], fb[q][0]); mma(fa[q][0], fb[q][1]); }
+                mma(fa[q][0], fb[q][0]);
+            }
         }
     } else {
         for (int it = slab0; it < slab1; ++it) {
@@ -349,7 +353,7 @@ __device__ __forceinline__ void upper(int t, int* row, int* col) {
 
 // SPLIT: the operands' second halves are multiplied too; LO: S and B have second halves
 template <int TM, int TN, bool SPLIT, bool LO, int PH, int NST>
-__global__ __launch_bounds__(256, SPLIT && TM == 2 || NST > 2 ? 1 : 2) void ns_product_kernel(MuonPlan p, MuonArgs a, _Float16* ws, float* diag, float* part, int from) {
+__global__ __launch_bounds__(256, SPLIT && TM == 2 && NST > 1 ? 1 : 2) void ns_product_kernel(MuonPlan p, MuonArgs a, _Float16* ws, float* diag, float* part, int from) {
     extern __shared__ uint4 smem[];
     constexpr int BM = 64 * TM, BN = 64 * TN;
     // ids go round-robin to the eight XCDs: of each group (they differ in the length of their contractions) each XCD takes an eighth, neighbouring tiles
@@ -946,7 +950,10 @@ hipError_t launch_muon(const MuonPlan& p, const MuonArgs& a, void* scratch, hipS
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (p.tile == 2) return run_products<2, 4, 2, false, false, 2, 1>(p, a, ws, diag, part, st);
-    if (p.tile == 1) return p.exact ? run_products<2, 2, 2, true, true, 2, 2>(p, a, ws, diag, part, st) : run_products<2, 2, 2, false, false, 2, 2>(p, a, ws, diag, part, st);
+    // (both planes' fragments of a slab fit the registers too: one buffer where workgroups share CUs, 865 -> 782 us a step of two layers of 512 cells in float, 289 -> 271 for two
+    // of 301 with gates apart; two buffers where they have a CU each, 210 us against 222 for two matrices of 1204 x 602)
+    if (p.tile == 0 && p.exact && p.applies >= 512) return run_products<1, 1, 1, true, true, 1, 1>(p, a, ws, diag, part, st);
+    if (p.tile == 1) return p.exact ? run_products<2, 2, 2, true, true, 1, 1>(p, a, ws, diag, part, st) : run_products<2, 2, 2, false, false, 2, 2>(p, a, ws, diag, part, st);
     return p.exact ? run_products<1, 1, 1, true, true, 2, 2>(p, a, ws, diag, part, st) : run_products<1, 1, 1, true, false, 2, 2>(p, a, ws, diag, part, st);
 }
 
