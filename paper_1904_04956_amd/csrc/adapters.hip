@@ -194,7 +194,8 @@ __device__ __forceinline__ uint4 low_chunk(const T* row, int c, int rank, bool v
 
 // Few rows (a frame, a handful of rows an adapter): 16 rows x 32 columns.  What such a tile costs is the latency of its loads, so nothing is staged: eight wavefronts share the
 // contraction, each loads its fragments straight into registers, four steps at a time, and their sums meet in LDS.  s t B_a^T is then a dot product a
-// thread, in float.  One frame of one sequence (K 1024, N 256, rank 16): 16 us with the staged tile and its barriers, NOTE_ROWS here.
+// thread, in float.  One frame of one sequence (K 1024, N 256, rank 16): 16 us with the staged tile and its barriers, 8 here, of which a launch that does nothing takes 3;
+// 64 sequences of as many adapters 12.
 constexpr int RN = 32, RWAVES = 8;
 template <typename T, int RB>
 __global__ __launch_bounds__(64 * RWAVES) void adapt_rows_kernel(ProjectArgs a, bool vector, bool low_vector) {
@@ -287,9 +288,13 @@ __global__ __launch_bounds__(64 * RWAVES) void adapt_rows_kernel(ProjectArgs a, 
 }
 
 // ROWS rows x 128 columns of y and all 16 RB columns of t in one pass over x.  A slab is 128 bytes of every row (x, W, A_a) in swizzled LDS; wavefront w multiplies
-// columns 32 w .. of y and rows 16 w .. (and 64 + 16 w ..) of t.  DIRECT (whole 16-byte words): slabs go from memory straight to LDS, NST - 1 ahead; else through registers, one ahead.
+// columns 32 w .. of y and rows 16 w .. (and 64 + 16 w ..) of t.  Two buffers; DIRECT (rows of whole 16-byte
+// words): slabs go from memory straight to LDS, else through registers.  What bounds it is a chain of latencies: of the 23 us of 256 sequences x 21 frames (K 1024, N 256,
+// rank 16: 93 tiles of 64 rows, two column blocks each) 12 are the launch, the search for the tile, t's way through LDS and the stores, 0.7 each of the sixteen slabs
+// (a third of it LDS reads).  Three and five buffers: 23.5 and 29.6 us (workgroups without a tile wait for a CU then).  128 rows where the adapters have them: dx of 2048
+// sequences 95 -> 83 us, of which stores 18, the low-rank part 14, slabs two to four 23.
 constexpr int PN = 128;
-template <typename T, int ROWS, int RB, int NST, bool DIRECT>
+template <typename T, int ROWS, int RB, bool DIRECT>
 __global__ __launch_bounds__(256) void adapt_tile_kernel(ProjectArgs a, bool low_vector) {
     constexpr int V = Vec<T>::N, SLAB = 8 * V, MR = ROWS / 16, TR = ROWS / 64, RP = 16 * RB, ES = (int)sizeof(T);
     constexpr int NX = ROWS / 32, NW = 4, NA = (RP * 8 + 255) / 256;
@@ -371,7 +376,7 @@ __global__ __launch_bounds__(256) void adapt_tile_kernel(ProjectArgs a, bool low
         };
         const int words = s.K / V;                           // 16-byte words of a row
         auto issue = [&](int it) __attribute__((always_inline)) {
-            const unsigned sb = lds0 + (unsigned)(it % NST) * (STAGE * 16);
+            const unsigned sb = lds0 + (unsigned)(it & 1) * (STAGE * 16);
             const long long off = (long long)it * 128;
             const int left = words - it * 8;                 // (words beyond the row's end repeat its last, and are cleared below)
             auto from = [&](const char* p, int r) { return p + off - (left < 8 ? max(((lane & 7) ^ swz(r)) - (left - 1), 0) * 16 : 0); };
@@ -384,20 +389,11 @@ __global__ __launch_bounds__(256) void adapt_tile_kernel(ProjectArgs a, bool low
                 for (int j = 0; j < NAI; ++j) dma(sb + (ROWS + PN) * 128 + (unsigned)(4 * j + wave) * 1024, from(pa[j], ROWS + PN + 8 * (4 * j + wave) + lr));
             }
         };
-        for (int i = 0; i < NST - 1; ++i) if (i < slabs) issue(i);
+        issue(0);
         for (int it = 0; it < slabs; ++it) {
-            // this wavefront's loads of the slab have landed when at most the younger slabs' are outstanding
-            const int younger = min(NST - 2, slabs - 1 - it);
-            auto wait = [&](auto n) __attribute__((always_inline)) {
-                constexpr int Y = decltype(n)::value;
-                if (has_a) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(Y * (NX + NW + NAI)) : "memory");
-                else asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(Y * (NX + NW)) : "memory");
-            };
-            static_assert(NST <= 3, "at most one younger slab");
-            if (younger == 1) wait(std::integral_constant<int, 1>{});
-            else wait(std::integral_constant<int, 0>{});
-            if (it + NST - 1 < slabs) issue(it + NST - 1);
-            uint4* at = smem + (it % NST) * STAGE;
+            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+            if (it + 1 < slabs) issue(it + 1);
+            uint4* at = smem + (it & 1) * STAGE;
             if (words - it * 8 < 8) {
                 for (int i = tid; i < STAGE; i += 256) if (((i & 7) ^ swz(i >> 3)) >= words - it * 8) at[i] = none;
                 asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -523,21 +519,19 @@ void run_rows(const ProjectArgs& a, bool vector, bool low_vector, hipStream_t st
     const int ntn = a.y ? (a.s.N + RN - 1) / RN : 1;
     adapt_rows_kernel<T, RB><<<(a.p.max_tiles + 7) / 8 * 8 * ntn, 64 * RWAVES, lds, st>>>(a, vector, low_vector);
 }
-template <typename T, int ROWS, int RB, int NST, bool DIRECT>
+template <typename T, int ROWS, int RB, bool DIRECT>
 void run_tile(const ProjectArgs& a, bool low_vector, hipStream_t st) {
-    constexpr int loop = NST * (ROWS + PN + 16 * RB) * 128, t = ROWS * (16 * RB + 4) * 4, lds = loop > t ? loop : t;
+    constexpr int loop = 2 * (ROWS + PN + 16 * RB) * 128, t = ROWS * (16 * RB + 4) * 4, lds = loop > t ? loop : t;
     static_assert(lds + 4 * ROWS <= 160 * 1024, "LDS of a CU");
     const int ntn = a.y ? (a.s.N + PN - 1) / PN : 1;
-    adapt_tile_kernel<T, ROWS, RB, NST, DIRECT><<<(a.p.max_tiles + 7) / 8 * 8 * ntn, 256, lds, st>>>(a, low_vector);
+    adapt_tile_kernel<T, ROWS, RB, DIRECT><<<(a.p.max_tiles + 7) / 8 * 8 * ntn, 256, lds, st>>>(a, low_vector);
 }
 template <typename T, int RB>
 void run_project(const ProjectArgs& a, bool vector, bool low_vector, hipStream_t st) {
-    // (three buffers where two workgroups a CU have room for them; five, one workgroup a CU: 256 sequences of 21 frames 29.6 us against 23.3, as the workgroups
-    // without a tile wait for a CU then)
     if (a.p.rows == 16) run_rows<T, RB>(a, vector, low_vector, st);
-    else if (a.p.rows == 128) { if (vector) run_tile<T, 128, RB, 2, true>(a, low_vector, st); else run_tile<T, 128, RB, 2, false>(a, low_vector, st); }
-    else if (!vector) run_tile<T, 64, RB, 2, false>(a, low_vector, st);
-    else run_tile<T, 64, RB, RB == 1 ? 3 : 2, true>(a, low_vector, st);
+    else if (a.p.rows == 128) { if (vector) run_tile<T, 128, RB, true>(a, low_vector, st); else run_tile<T, 128, RB, false>(a, low_vector, st); }
+    else if (vector) run_tile<T, 64, RB, true>(a, low_vector, st);
+    else run_tile<T, 64, RB, false>(a, low_vector, st);
 }
 template <typename T>
 hipError_t project(const ProjectArgs& a, hipStream_t st) {
@@ -668,7 +662,8 @@ __global__ __launch_bounds__(256) void adapt_grad_kernel(AdaptGradArgs a) {
 
 // The same in bf16 where rows are whole 16-byte words: two slabs of 64 rows of x (or dy) and of q (or t) come straight to LDS in turn, one while the other is
 // multiplied; q's (t's) three bf16 parts are made of the slab that has landed.  256 sequences x 21 frames, K 1024, 100 adapters: 15 us through registers; 2048 sequences,
-// 24 adapters 70 us: NOTE_GRAD here.
+// 24 adapters 70 us: 11 and 36 here, 3.1 TB/s
+// of x, dy and the parts of the sums.
 template <int RB>
 __global__ __launch_bounds__(256) void adapt_grad_direct_kernel(AdaptGradArgs a) {
     constexpr int RP = 32 * RB, LLD = RP * 2 + 16, RS = 64 * 256, LS = 64 * RP * 4, STAGE = RS + LS, LCH = RP / 4;     // bytes; 16-byte words of a row of q
