@@ -112,6 +112,36 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(MuonPlan p, MuonArgs
     }
 }
 
+// X where only its first halves are multiplied: the second part, times 2^10, in eight bits (e5m2, three significant bits: X to 2^-15), a quarter less to write and
+// read.  Four layers of 512 cells, all launches: NOTE_LO8.
+__device__ __forceinline__ void put_low(_Float16* hi, unsigned char* lo, const float (&v)[8]) {
+    f16x8_t h;
+    float r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { h[e] = (_Float16)v[e]; r[e] = 1024.0f * (v[e] - (float)h[e]); }
+    *reinterpret_cast<f16x8_t*>(hi) = h;
+    u32x2_t w;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        int x = __builtin_amdgcn_cvt_pk_bf8_f32(r[4 * i], r[4 * i + 1], 0, false);
+        w[i] = (unsigned)__builtin_amdgcn_cvt_pk_bf8_f32(r[4 * i + 2], r[4 * i + 3], x, true);
+    }
+    *reinterpret_cast<u32x2_t*>(lo) = w;
+}
+__device__ __forceinline__ f16x8_t low(u32x2_t w) {
+    f16x8_t l;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        l[4 * i] = (_Float16)(__builtin_amdgcn_cvt_f32_bf8((int)w[i], 0) * (1.0f / 1024.0f));
+        l[4 * i + 1] = (_Float16)(__builtin_amdgcn_cvt_f32_bf8((int)w[i], 1) * (1.0f / 1024.0f));
+        l[4 * i + 2] = (_Float16)(__builtin_amdgcn_cvt_f32_bf8((int)w[i], 2) * (1.0f / 1024.0f));
+        l[4 * i + 3] = (_Float16)(__builtin_amdgcn_cvt_f32_bf8((int)w[i], 3) * (1.0f / 1024.0f));
+    }
+    return l;
+}
+// the second part of matrix k of X in buffer b, in eight bits
+__device__ __forceinline__ unsigned char* low_of(const MuonGroup& g, _Float16* ws, int b, int k) { return reinterpret_cast<unsigned char*>(ws + g.x[b] + g.xplane) + (long long)k * g.rp * g.cp; }
+
 // ---- d / |d|_F as two halves, zero-padded ---------------------------------------------------------------------------
 __device__ __forceinline__ void put_halves(_Float16* hi, _Float16* lo, const float (&v)[8]) {
     f16x8_t h, l;
@@ -120,6 +150,7 @@ __device__ __forceinline__ void put_halves(_Float16* hi, _Float16* lo, const flo
     *reinterpret_cast<f16x8_t*>(hi) = h;
     if (lo) *reinterpret_cast<f16x8_t*>(lo) = l;
 }
+template <bool LOW>
 __global__ __launch_bounds__(256) void muon_cast_kernel(MuonPlan p, MuonArgs a, const double* sums, _Float16* ws) {
     __shared__ double lds[4];
     const int group = group_of(p.at.cast, blockIdx.x);
@@ -162,7 +193,8 @@ __global__ __launch_bounds__(256) void muon_cast_kernel(MuonPlan p, MuonArgs a, 
                 d[j] = (float)(f * scale) + whole;
             }
         }
-        put_halves(x + e, x + g.xplane + e, d);
+        if constexpr (LOW) put_low(x + e, low_of(g, ws, 0, k) + e, d);
+        else put_halves(x + e, x + g.xplane + e, d);
     }
 }
 
@@ -298,8 +330,8 @@ __device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand
 }
 
 // The tile's values, eight of a row at a time, each wavefront its own part through its own stretch of LDS, whose reads are conflict-free along
-// rows and columns.  What an element is combined with is loaded for a whole block of 32 rows before the first store (stores and loads in turn are a round trip
-// each): load(row, column) -> aux; f(row, column, values, aux) changes the values and stores them; mirror(row, column, values) gets the same
+// rows and columns.  What an element is combined with is asked for a block of 32 rows ahead, in front of the stores of the block before (a wavefront's memory answers come in
+// order, so that a load behind a store waits for it: NOTE_AHEAD): load(row, column) -> aux; f(row, column, values, aux) changes the values and stores them; mirror(row, column, values) gets the same
 // values of the transposed tile (`twice`).
 template <int TM, int TN, typename L, typename F, typename G>
 __device__ __forceinline__ void ns_values(const f32x16_t (&acc)[TM][TN], uint4* smem, bool twice, L&& load, F&& f, G&& mirror) {
@@ -307,12 +339,16 @@ __device__ __forceinline__ void ns_values(const f32x16_t (&acc)[TM][TN], uint4* 
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, wm = wv >> 1, wn = wv & 1;
     float* s = reinterpret_cast<float*>(smem) + wv * 32 * LD;
     const int col0 = wn * 32 * TN;
+    decltype(load(0, 0)) aux[2][NQ];
+    auto ask = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) { const int c = lane + 64 * q; aux[i & 1][q] = load(wm * 32 * TM + 32 * i + c / (4 * TN), col0 + c % (4 * TN) * 8); }
+    };
+    ask(0);
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int row0 = wm * 32 * TM + 32 * i;
-        decltype(load(0, 0)) aux[NQ];
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) { const int c = lane + 64 * q; aux[q] = load(row0 + c / (4 * TN), col0 + c % (4 * TN) * 8); }
+        if (i + 1 < TM) ask(i + 1);
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -324,7 +360,7 @@ __device__ __forceinline__ void ns_values(const f32x16_t (&acc)[TM][TN], uint4* 
             f32x4_t* at = reinterpret_cast<f32x4_t*>(s + r * LD + c0);
             const f32x4_t x = at[0], y = at[1];
             float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-            f(row0 + r, col0 + c0, v, aux[q]);
+            f(row0 + r, col0 + c0, v, aux[i & 1][q]);
             if (twice) { at[0] = f32x4_t{v[0], v[1], v[2], v[3]}; at[1] = f32x4_t{v[4], v[5], v[6], v[7]}; }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -343,6 +379,7 @@ __device__ __forceinline__ void ns_values(const f32x16_t (&acc)[TM][TN], uint4* 
     }
 }
 struct Halves { f16x8_t h, l; f32x4_t d0, d1; float di; };
+template <bool LOW, bool LAST> struct Applied { f16x8_t h; std::conditional_t<LOW, u32x2_t, f16x8_t> l; float di; f32x4_t w[LAST ? 2 : 1]; };
 
 // tile number t of those on and above the diagonal, column by column: row <= column
 __device__ __forceinline__ void upper(int t, int* row, int* col) {
@@ -351,8 +388,8 @@ __device__ __forceinline__ void upper(int t, int* row, int* col) {
     *row = t; *col = c;
 }
 
-// SPLIT: the operands' second halves are multiplied too; LO: S and B have second halves
-template <int TM, int TN, bool SPLIT, bool LO, int PH, int NST>
+// SPLIT: the operands' second halves are multiplied too; LO: S and B have second halves; LOW: X's second part is held in eight bits
+template <int TM, int TN, bool SPLIT, bool LO, bool LOW, int PH, int NST>
 __global__ __launch_bounds__(256, SPLIT && TM == 2 && NST > 1 ? 1 : 2) void ns_product_kernel(MuonPlan p, MuonArgs a, _Float16* ws, float* diag, float* part, int from) {
     extern __shared__ uint4 smem[];
     constexpr int BM = 64 * TM, BN = 64 * TN;
@@ -441,33 +478,48 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 && NST > 1 ? 1 : 2) void ns_p
         if (g.tall) ns_tile<TM, TN, SPLIT, false, false, NST>(acc, {x + (long long)tr * BM * g.cp, g.cp, g.xplane}, {b + (long long)tc * BN * g.mp, g.mp, g.splane}, 0, g.mp / 64, smem);
         else ns_tile<TM, TN, SPLIT, false, true, NST>(acc, {b + (long long)tr * BM * g.mp, g.mp, g.splane}, {x + tc * BN, g.cp, g.xplane}, 0, g.mp / 64, smem);
         _Float16* to = ws + g.x[from ^ 1] + (long long)k * g.rp * g.cp;
+        const unsigned char* xl = low_of(g, ws, from, k);
+        unsigned char* tl = low_of(g, ws, from ^ 1, k);
         const long long at = tensor_at(g, k);
         const float* bd = diag + g.diag + (long long)(g.count + k) * g.mp;
         const float shrink = 1.0f - a.lr * a.decay, step = a.lr * sqrtf(fmaxf(1.0f, (float)g.rows / (float)g.cols)) * DOWN;
+        // (a lane's columns are the same in all of its rows)
+        f32x4_t d0{}, d1{};
+        if (g.tall) {
+            const float* d = bd + tc * BN + (threadIdx.x >> 6 & 1) * 32 * TN + (threadIdx.x & 63) % (4 * TN) * 8;
+            d0 = *reinterpret_cast<const f32x4_t*>(d);
+            d1 = *reinterpret_cast<const f32x4_t*>(d + 4);
+        }
         ns_values(acc, smem, false, [&](int r, int c) {
             const int row = tr * BM + r, col = tc * BN + c;
-            const _Float16* y = x + (long long)row * g.cp + col;
-            Halves u;
-            u.h = *reinterpret_cast<const f16x8_t*>(y);
-            u.l = *reinterpret_cast<const f16x8_t*>(y + g.xplane);
-            if (g.tall) { u.d0 = *reinterpret_cast<const f32x4_t*>(bd + col); u.d1 = *reinterpret_cast<const f32x4_t*>(bd + col + 4); }
-            else { const float d = bd[row]; u.d0 = u.d1 = f32x4_t{d, d, d, d}; }
+            const long long o = (long long)row * g.cp + col;
+            Applied<LOW, PH == PH_LAST> u;
+            u.h = *reinterpret_cast<const f16x8_t*>(x + o);
+            if constexpr (LOW) u.l = *reinterpret_cast<const u32x2_t*>(xl + o); else u.l = *reinterpret_cast<const f16x8_t*>(x + g.xplane + o);
+            u.di = g.tall ? 0.0f : bd[row];
+            if constexpr (PH == PH_LAST) {
+                if (a.theta && row < g.rows && col + 8 <= g.cols) {
+                    const f32x4u_t* w = reinterpret_cast<const f32x4u_t*>(a.theta + at + (long long)row * g.cols + col);
+                    u.w[0] = w[0]; u.w[1] = w[1];
+                }
+            }
             return u;
-        }, [&](int r, int c, float (&v)[8], const Halves& u) {
+        }, [&](int r, int c, float (&v)[8], const Applied<LOW, PH == PH_LAST>& u) {
             const int row = tr * BM + r, col = tc * BN + c;
             const long long o = (long long)row * g.cp + col;
+            f16x8_t l;
+            if constexpr (LOW) l = low(u.l); else l = u.l;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = (NS_A + (e < 4 ? u.d0[e & 3] : u.d1[e & 3])) * ((float)u.h[e] + (float)u.l[e]) + DOWN * v[e];
-            if constexpr (PH == PH_APPLY) put_halves(to + o, to + g.xplane + o, v);
+            for (int e = 0; e < 8; ++e) v[e] = (NS_A + (g.tall ? (e < 4 ? d0[e & 3] : d1[e & 3]) : u.di)) * ((float)u.h[e] + (float)l[e]) + DOWN * v[e];
+            if constexpr (PH == PH_APPLY && LOW) put_low(to + o, tl + o, v);
+            else if constexpr (PH == PH_APPLY) put_halves(to + o, to + g.xplane + o, v);
             else {
                 if (row >= g.rows || col >= g.cols) return;
                 const long long q = at + (long long)row * g.cols + col;
                 const int n = min(8, g.cols - col);
                 if (a.theta) {
                     if (n == 8) {
-                        f32x4_t w[2];
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) w[i] = *reinterpret_cast<const f32x4u_t*>(a.theta + q + 4 * i);
+                        f32x4_t w[2] = {u.w[0], u.w[1]};
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
 #pragma unroll
@@ -807,9 +859,9 @@ constexpr int lds_bytes(int TM, int TN, bool split, int nst) {
     const int loop = nst * (split ? 2 : 1) * 64 * (TM + TN) * 128, values = 4 * 32 * (32 * TN + 4) * 4;
     return loop > values ? loop : values;
 }
-template <int TM, int TN, bool SPLIT, bool LO, int PH, int NST>
+template <int TM, int TN, bool SPLIT, bool LO, bool LOW, int PH, int NST>
 void run_product(int n, const MuonPlan& p, const MuonArgs& a, _Float16* ws, float* diag, float* part, int from, hipStream_t st) {
-    ns_product_kernel<TM, TN, SPLIT, LO, PH, NST><<<n, 256, lds_bytes(TM, TN, SPLIT, NST), st>>>(p, a, ws, diag, part, from);
+    ns_product_kernel<TM, TN, SPLIT, LO, LOW, PH, NST><<<n, 256, lds_bytes(TM, TN, SPLIT, NST), st>>>(p, a, ws, diag, part, from);
 }
 
 // T: edge of the Gram and square tiles; AM, AN: of the last product's
@@ -817,11 +869,11 @@ template <int T, int AM, int AN, bool FINE, bool SPLIT, int SN, int AN_ST>
 hipError_t run_products(const MuonPlan& p, const MuonArgs& a, _Float16* ws, float* diag, float* part, hipStream_t st) {
     for (int i = 0; i < NS_STEPS; ++i) {
         const int from = i & 1;
-        run_product<T, T, FINE, SPLIT, PH_GRAM, SN>(p.grams, p, a, ws, diag, part, from, st);
+        run_product<T, T, FINE, SPLIT, !FINE, PH_GRAM, SN>(p.grams, p, a, ws, diag, part, from, st);
         if (p.sums) ns_gram_sum_kernel<T, SPLIT><<<p.sums, 256, 0, st>>>(p, ws, diag, part);
-        run_product<T, T, SPLIT, SPLIT, PH_SQUARE, SN>(p.squares, p, a, ws, diag, part, from, st);
-        if (i + 1 < NS_STEPS) run_product<AM, AN, SPLIT, SPLIT, PH_APPLY, AN_ST>(p.applies, p, a, ws, diag, part, from, st);
-        else run_product<AM, AN, SPLIT, SPLIT, PH_LAST, AN_ST>(p.applies, p, a, ws, diag, part, from, st);
+        run_product<T, T, SPLIT, SPLIT, !FINE, PH_SQUARE, SN>(p.squares, p, a, ws, diag, part, from, st);
+        if (i + 1 < NS_STEPS) run_product<AM, AN, SPLIT, SPLIT, !FINE, PH_APPLY, AN_ST>(p.applies, p, a, ws, diag, part, from, st);
+        else run_product<AM, AN, SPLIT, SPLIT, !FINE, PH_LAST, AN_ST>(p.applies, p, a, ws, diag, part, from, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -946,7 +998,9 @@ hipError_t launch_muon(const MuonPlan& p, const MuonArgs& a, void* scratch, hipS
     muon_momentum_kernel<<<p.chunks, 256, 0, st>>>(p, a, sums);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.casts == 0) return e;
-    muon_cast_kernel<<<p.casts, 256, 0, st>>>(p, a, sums, ws);
+    // (second halves that are multiplied, in S at least, are halves)
+    if (p.tile == 0 || p.exact) muon_cast_kernel<false><<<p.casts, 256, 0, st>>>(p, a, sums, ws);
+    else muon_cast_kernel<true><<<p.casts, 256, 0, st>>>(p, a, sums, ws);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (p.tile == 2) return run_products<2, 4, 2, false, false, 2, 1>(p, a, ws, diag, part, st);
