@@ -14,6 +14,14 @@
 // The Frobenius norm is summed in double (squares of floats leave float's range) in a fixed order.
 //
 // S and B are symmetric: tiles on and above the diagonal are computed, and stored twice.
+//
+// All matrices of a call share each launch: the flat pass over v and g, the cast to halves, then S, B and the new X five times; the last X goes straight into
+// the weights.  What bounds them, four layers of 512 cells (43 M weights, 301 GFLOP), 776 us in all: the flat pass 82 us, 560 MB at 6.8 TB/s; the cast 54, 340 MB; S 39 each, 900 TFLOP/s
+// of what it would be without the symmetry; B 25, whose 311 tiles are 1.2 a CU; the new X 63, 35 GFLOP and 220 MB; the last 109, 465 MB.  Six of 1024: 353, 304, 301 (1460 TFLOP/s
+// likewise), 153, 518 (870 TFLOP/s, 1 GB), 724 (2 GB).
+// Built and dropped: three and four buffers of a slab where a CU has one workgroup (S 41 -> 56 us: what a lone workgroup waits for are its own LDS reads and products in turn,
+// 768 and 512 clocks a slab, not the loads); S in two, three or four parts of the contraction, summed by another launch (58, 66 and 77 us for 45); two steps'
+// B multiplied together, so that X is written three times instead of five (error 4e-4 -> 6e-4).
 #include "gemm_tile.hpp"
 #include "muon.hpp"
 #include <algorithm>
@@ -113,7 +121,7 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(MuonPlan p, MuonArgs
 }
 
 // X where only its first halves are multiplied: the second part, times 2^10, in eight bits (e5m2, three significant bits: X to 2^-15), a quarter less to write and
-// read.  Four layers of 512 cells, all launches: NOTE_LO8.
+// read (four layers of 512 cells 806 -> 796 us).
 __device__ __forceinline__ void put_low(_Float16* hi, unsigned char* lo, const float (&v)[8]) {
     f16x8_t h;
     float r[8];
@@ -331,7 +339,7 @@ __device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand
 
 // The tile's values, eight of a row at a time, each wavefront its own part through its own stretch of LDS, whose reads are conflict-free along
 // rows and columns.  What an element is combined with is asked for a block of 32 rows ahead, in front of the stores of the block before (a wavefront's memory answers come in
-// order, so that a load behind a store waits for it: NOTE_AHEAD): load(row, column) -> aux; f(row, column, values, aux) changes the values and stores them; mirror(row, column, values) gets the same
+// order, so that a load behind a store waits for it: 68 -> 63 us a product of four layers of 512 cells): load(row, column) -> aux; f(row, column, values, aux) changes the values and stores them; mirror(row, column, values) gets the same
 // values of the transposed tile (`twice`).
 template <int TM, int TN, typename L, typename F, typename G>
 __device__ __forceinline__ void ns_values(const f32x16_t (&acc)[TM][TN], uint4* smem, bool twice, L&& load, F&& f, G&& mirror) {
@@ -603,7 +611,8 @@ __global__ __launch_bounds__(256) void ns_gram_sum_kernel(MuonPlan p, _Float16* 
 // ---- small matrices: all steps of a matrix in one workgroup -----------------------------------------------------------------
 // What the general path spends on them is twenty launches of a few microseconds.  A matrix whose short side is at most 64 and which fits LDS is read
 // once, taken through the five steps there and written once, by sixteen wavefronts; the tensors that are not orthogonalised are further workgroups of the same
-// launch.  [m][n] with m <= n in LDS as two planes of halves (rows of n + 8, so that sixteen rows' chunks spread over the banks); all products use both planes.
+// launch.  48 factors of 16 x 1024 196 -> 28 us, a layer of 32 cells 94 -> 21: three to four microseconds are the launch, nine the way in and out, three a step (four barriers, and LDS, through
+// which all of X goes twice).  [m][n] with m <= n in LDS as two planes of halves (rows of n + 8, so that sixteen rows' chunks spread over the banks); all products use both planes.
 constexpr int SMALL_THREADS = 1024, SMALL_SIDE = 64, SMALL_LDS = 160 * 1024 - 256;
 constexpr int small_parts(int mb) { return mb == 1 ? 16 : mb == 2 ? 4 : 1; }   // stretches of the columns that a tile of S is summed over
 struct SmallLds { int ldn, lds, x, s, b, red, d, bytes; };      // row lengths in halves; byte offsets
