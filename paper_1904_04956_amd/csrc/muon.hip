@@ -214,11 +214,11 @@ __global__ __launch_bounds__(256) void muon_cast_kernel(MuonPlan p, MuonArgs a, 
 struct NsOperand { const _Float16* p; long long ld, plane; };      // tile origin; elements to the second halves
 
 template <int TM, int TN, bool SPLIT, bool AS, bool BS, int NST>
-__device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand& A, const NsOperand& B, int slab0, int slab1, uint4* smem) {
+__device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand& A, const NsOperand& B, int slab0, int slab1, int trips, uint4* smem) {
     constexpr bool ONE = NST == 1;
     constexpr int BM = 64 * TM, BN = 64 * TN, PL = SPLIT ? 2 : 1, PA = BM * 8, PB = BN * 8, STAGE = PL * (PA + PB);   // (in 16-byte words)
     constexpr int NIA = 2 * TM, NIB = 2 * TN, CPA = BM / 8, CPB = BN / 8;
-    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv >> 1, wn = wv & 1;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3), wm = wv >> 1, wn = wv & 1;
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
     unsigned voa[NIA], vob[NIB];
     auto place = [&](auto cpr, bool slow, int j, long long ld) {
@@ -302,7 +302,7 @@ __device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand
             }
         }
     } else {
-        for (int it = slab0; it < slab1; ++it) {
+        for (int it = slab0; it < slab0 + trips; ++it) {       // (every wavefront of the workgroup goes through as many barriers)
             // (this wavefront's loads of the slab have landed when at most the younger slabs' are outstanding)
             constexpr int LOADS = PL * (NIA + NIB);
             const int younger = min(NST - 2, slab1 - 1 - it);
@@ -312,6 +312,7 @@ __device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand
             if (it + NST - 1 < slab1) issue(it + NST - 1);
             const uint4* sa = smem + ((it - slab0) % NST) * STAGE;
             const uint4* sb = sa + PL * PA;
+            if (it >= slab1) continue;
             // (the next fragments are on their way while these are multiplied)
             constexpr int NF = SPLIT && TM == 2 ? 1 : 2;
             uint4 af[NF][PL][TM], bf[NF][PL][TN];
@@ -335,6 +336,38 @@ __device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand
         }
     }
     __syncthreads();                                        // the epilogue reuses the buffers
+}
+
+// The same by SETS sets of 2 x 2 wavefronts, each with buffers of its own and its part of the contraction; the first set is left with the sum.  For launches of
+// no more tiles than CUs: a workgroup alone on a CU waits for its LDS reads and its products in turn, two sets for one another's: a step of two matrices of
+// 1204 x 602 in float S 16 (in two parts and a sum) -> 13 us, B 13 -> 11; 1024 x 1024, five steps, 240 -> 217.
+template <int SETS, int TM, int TN, bool SPLIT, bool AS, bool BS, int NST>
+__device__ __forceinline__ void ns_tile_of_sets(f32x16_t (&acc)[TM][TN], const NsOperand& A, const NsOperand& B, int slab0, int slab1, uint4* smem) {
+    if constexpr (SETS == 1) ns_tile<TM, TN, SPLIT, AS, BS, NST>(acc, A, B, slab0, slab1, slab1 - slab0, smem);
+    else {
+        constexpr int WORDS = NST * (SPLIT ? 2 : 1) * 64 * (TM + TN) * 8;
+        const int set = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), part = (slab1 - slab0 + 1) / 2, t = threadIdx.x & 255;
+        ns_tile<TM, TN, SPLIT, AS, BS, NST>(acc, A, B, slab0 + set * part, set ? slab1 : slab0 + part, part, smem + set * WORDS);
+        f32x4_t* other = reinterpret_cast<f32x4_t*>(smem);
+        if (set) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) other[((i * TN + j) * 4 + e) * 256 + t] = f32x4_t{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+        }
+        __syncthreads();
+        if (!set) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[i][j][e] += other[((i * TN + j) * 4 + (e >> 2)) * 256 + t][e & 3];
+        }
+        __syncthreads();                                    // (the epilogue reuses the place)
+    }
 }
 
 // The tile's values, eight of a row at a time, each wavefront its own part through its own stretch of LDS, whose reads are conflict-free along
@@ -397,8 +430,8 @@ __device__ __forceinline__ void upper(int t, int* row, int* col) {
 }
 
 // SPLIT: the operands' second halves are multiplied too; LO: S and B have second halves; LOW: X's second part is held in eight bits
-template <int TM, int TN, bool SPLIT, bool LO, bool LOW, int PH, int NST>
-__global__ __launch_bounds__(256, SPLIT && TM == 2 && NST > 1 ? 1 : 2) void ns_product_kernel(MuonPlan p, MuonArgs a, _Float16* ws, float* diag, float* part, int from) {
+template <int TM, int TN, bool SPLIT, bool LO, bool LOW, int PH, int NST, int SETS>
+__global__ __launch_bounds__(256 * SETS, SPLIT && TM == 2 && NST > 1 ? 1 : 2) void ns_product_kernel(MuonPlan p, MuonArgs a, _Float16* ws, float* diag, float* part, int from) {
     extern __shared__ uint4 smem[];
     constexpr int BM = 64 * TM, BN = 64 * TN;
     // ids go round-robin to the eight XCDs: of each group (they differ in the length of their contractions) each XCD takes an eighth, neighbouring tiles
@@ -434,8 +467,9 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 && NST > 1 ? 1 : 2) void ns_p
             const _Float16* x = ws + g.x[from] + (long long)k * g.rp * g.cp;
             const int slabs = (g.tall ? g.rp : g.cp) / 64, per = (slabs + g.splits - 1) / g.splits;
             const int s0 = min(slabs, split * per), s1 = min(slabs, s0 + per);
-            if (g.tall) ns_tile<TM, TN, SPLIT, true, true, NST>(acc, {x + tr * BM, g.cp, g.xplane}, {x + tc * BM, g.cp, g.xplane}, s0, s1, smem);
-            else ns_tile<TM, TN, SPLIT, false, false, NST>(acc, {x + (long long)tr * BM * g.cp, g.cp, g.xplane}, {x + (long long)tc * BM * g.cp, g.cp, g.xplane}, s0, s1, smem);
+            if (g.tall) ns_tile_of_sets<SETS, TM, TN, SPLIT, true, true, NST>(acc, {x + tr * BM, g.cp, g.xplane}, {x + tc * BM, g.cp, g.xplane}, s0, s1, smem);
+            else ns_tile_of_sets<SETS, TM, TN, SPLIT, false, false, NST>(acc, {x + (long long)tr * BM * g.cp, g.cp, g.xplane}, {x + (long long)tc * BM * g.cp, g.cp, g.xplane}, s0, s1, smem);
+            if (SETS > 1 && threadIdx.x >= 256) return;
             const bool whole = g.splits == 1;
             float* sum = part + g.part + ((long long)local * g.splits + split) * BM * BM;
             ns_values(acc, smem, whole && tr != tc, [](int, int) { return 0; }, [&](int r, int c, float (&v)[8], int) {
@@ -455,7 +489,8 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 && NST > 1 ? 1 : 2) void ns_p
             }, mirror);
         } else {
             const NsOperand A{s + (long long)tr * BM * g.mp, g.mp, g.splane}, B{s + (long long)tc * BM * g.mp, g.mp, g.splane};
-            ns_tile<TM, TN, SPLIT, false, false, NST>(acc, A, B, 0, g.mp / 64, smem);
+            ns_tile_of_sets<SETS, TM, TN, SPLIT, false, false, NST>(acc, A, B, 0, g.mp / 64, smem);
+            if (SETS > 1 && threadIdx.x >= 256) return;
             ns_values(acc, smem, tr != tc, [&](int r, int c) {
                 const int row = tr * BM + r, col = tc * BM + c;
                 const _Float16* at = s + (long long)row * g.mp + col;
@@ -483,8 +518,9 @@ __global__ __launch_bounds__(256, SPLIT && TM == 2 && NST > 1 ? 1 : 2) void ns_p
         const int tr = t / nc, tc = t % nc;
         const _Float16* x = ws + g.x[from] + (long long)k * g.rp * g.cp;
         const _Float16* b = ws + g.b + (long long)k * g.mp * g.mp;
-        if (g.tall) ns_tile<TM, TN, SPLIT, false, false, NST>(acc, {x + (long long)tr * BM * g.cp, g.cp, g.xplane}, {b + (long long)tc * BN * g.mp, g.mp, g.splane}, 0, g.mp / 64, smem);
-        else ns_tile<TM, TN, SPLIT, false, true, NST>(acc, {b + (long long)tr * BM * g.mp, g.mp, g.splane}, {x + tc * BN, g.cp, g.xplane}, 0, g.mp / 64, smem);
+        if (g.tall) ns_tile_of_sets<SETS, TM, TN, SPLIT, false, false, NST>(acc, {x + (long long)tr * BM * g.cp, g.cp, g.xplane}, {b + (long long)tc * BN * g.mp, g.mp, g.splane}, 0, g.mp / 64, smem);
+        else ns_tile_of_sets<SETS, TM, TN, SPLIT, false, true, NST>(acc, {b + (long long)tr * BM * g.mp, g.mp, g.splane}, {x + tc * BN, g.cp, g.xplane}, 0, g.mp / 64, smem);
+        if (SETS > 1 && threadIdx.x >= 256) return;
         _Float16* to = ws + g.x[from ^ 1] + (long long)k * g.rp * g.cp;
         const unsigned char* xl = low_of(g, ws, from, k);
         unsigned char* tl = low_of(g, ws, from ^ 1, k);
@@ -864,25 +900,25 @@ __global__ __launch_bounds__(SMALL_THREADS) void muon_small_kernel(MuonPlan p, M
     });
 }
 
-constexpr int lds_bytes(int TM, int TN, bool split, int nst) {
-    const int loop = nst * (split ? 2 : 1) * 64 * (TM + TN) * 128, values = 4 * 32 * (32 * TN + 4) * 4;
+constexpr int lds_bytes(int TM, int TN, bool split, int nst, int sets) {
+    const int loop = sets * nst * (split ? 2 : 1) * 64 * (TM + TN) * 128, values = 4 * 32 * (32 * TN + 4) * 4;
     return loop > values ? loop : values;
 }
-template <int TM, int TN, bool SPLIT, bool LO, bool LOW, int PH, int NST>
+template <int TM, int TN, bool SPLIT, bool LO, bool LOW, int PH, int NST, int SETS>
 void run_product(int n, const MuonPlan& p, const MuonArgs& a, _Float16* ws, float* diag, float* part, int from, hipStream_t st) {
-    ns_product_kernel<TM, TN, SPLIT, LO, LOW, PH, NST><<<n, 256, lds_bytes(TM, TN, SPLIT, NST), st>>>(p, a, ws, diag, part, from);
+    ns_product_kernel<TM, TN, SPLIT, LO, LOW, PH, NST, SETS><<<n, 256 * SETS, lds_bytes(TM, TN, SPLIT, NST, SETS), st>>>(p, a, ws, diag, part, from);
 }
 
 // T: edge of the Gram and square tiles; AM, AN: of the last product's
-template <int T, int AM, int AN, bool FINE, bool SPLIT, int SN, int AN_ST>
+template <int T, int AM, int AN, bool FINE, bool SPLIT, int SN, int AN_ST, int SETS = 1>
 hipError_t run_products(const MuonPlan& p, const MuonArgs& a, _Float16* ws, float* diag, float* part, hipStream_t st) {
     for (int i = 0; i < NS_STEPS; ++i) {
         const int from = i & 1;
-        run_product<T, T, FINE, SPLIT, !FINE, PH_GRAM, SN>(p.grams, p, a, ws, diag, part, from, st);
+        run_product<T, T, FINE, SPLIT, !FINE, PH_GRAM, SN, SETS>(p.grams, p, a, ws, diag, part, from, st);
         if (p.sums) ns_gram_sum_kernel<T, SPLIT><<<p.sums, 256, 0, st>>>(p, ws, diag, part);
-        run_product<T, T, SPLIT, SPLIT, !FINE, PH_SQUARE, SN>(p.squares, p, a, ws, diag, part, from, st);
-        if (i + 1 < NS_STEPS) run_product<AM, AN, SPLIT, SPLIT, !FINE, PH_APPLY, AN_ST>(p.applies, p, a, ws, diag, part, from, st);
-        else run_product<AM, AN, SPLIT, SPLIT, !FINE, PH_LAST, AN_ST>(p.applies, p, a, ws, diag, part, from, st);
+        run_product<T, T, SPLIT, SPLIT, !FINE, PH_SQUARE, SN, SETS>(p.squares, p, a, ws, diag, part, from, st);
+        if (i + 1 < NS_STEPS) run_product<AM, AN, SPLIT, SPLIT, !FINE, PH_APPLY, AN_ST, 1>(p.applies, p, a, ws, diag, part, from, st);
+        else run_product<AM, AN, SPLIT, SPLIT, !FINE, PH_LAST, AN_ST, 1>(p.applies, p, a, ws, diag, part, from, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -939,7 +975,7 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
     };
     p.tile = !exact && tiles(256, 128) >= 480 ? 2 : tiles(128, 128) >= 700 ? 1 : 0;
     const int edge = p.tile ? 128 : 64, high = p.tile == 2 ? 256 : edge;
-    long long halves = 0, floats = 0, diags = 0, chunks = 0, casts = 0, grams = 0, squares = 0, applies = 0, sums = 0, slabs = 0;
+    long long halves = 0, floats = 0, diags = 0, chunks = 0, casts = 0, grams = 0, squares = 0, applies = 0, sums = 0, slabs = 0, tiles_s = 0;
     // the longest contractions first: what is left at a launch's end is short
     std::stable_sort(p.g, p.g + n, [](const MuonGroup& x, const MuonGroup& y) {
         return (x.ortho ? std::min(x.rows, x.cols) : 0) > (y.ortho ? std::min(y.rows, y.cols) : 0);
@@ -951,9 +987,10 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
         q.mp = std::min(q.rp, q.cp);
         const long long nt = q.mp / edge;
         q.grams = (int)(nt * (nt + 1) / 2);
-        if (q.ortho) slabs += (long long)q.count * q.grams * (std::max(q.rp, q.cp) / 64);
+        if (q.ortho) { tiles_s += (long long)q.count * q.grams; slabs += (long long)q.count * q.grams * (std::max(q.rp, q.cp) / 64); }
     }
-    // Gram tiles: as many parts along the contraction as make about two workgroups a CU of the launch, none shorter than eight slabs
+    // Gram tiles: parts along the contraction where it is long for their number, none shorter than eight slabs
+    p.lone = p.tile == 0 && tiles_s <= 256;
     const long long target = std::max<long long>(8, slabs / 320);
     for (int i = 0; i < n; ++i) {
         MuonGroup& q = p.g[i];
@@ -967,7 +1004,8 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
         if ((long long)std::max(q.rp, q.cp) * 256 > most || nx / CAST * q.count > most) return false;
         q.casts = (int)(nx / CAST);
         casts += (long long)q.count * q.casts;
-        q.splits = std::max(1, (int)((std::max(q.rp, q.cp) / 64 + target / 2) / target));
+        const int length = std::max(q.rp, q.cp) / 64;
+        q.splits = p.lone && length <= 24 ? 1 : std::clamp((int)((length + target / 2) / target), 1, 32);   // (the sum's launch is worth a dozen slabs, each part some more)
         auto eighths = [](long long v) { return (v + 7) / 8 * 8; };
         grams += eighths((long long)q.count * q.grams * q.splits);
         squares += eighths((long long)q.count * q.grams);
@@ -1015,8 +1053,9 @@ hipError_t launch_muon(const MuonPlan& p, const MuonArgs& a, void* scratch, hipS
     if (p.tile == 2) return run_products<2, 4, 2, false, false, 2, 1>(p, a, ws, diag, part, st);
     // (both planes' fragments of a slab fit the registers too: one buffer where workgroups share CUs, 865 -> 782 us a step of two layers of 512 cells in float, 289 -> 271 for two
     // of 301 with gates apart; two buffers where they have a CU each, 210 us against 222 for two matrices of 1204 x 602)
-    if (p.tile == 0 && p.exact && p.applies >= 512) return run_products<1, 1, 1, true, true, 1, 1>(p, a, ws, diag, part, st);
+    if (p.tile == 0 && p.exact && !p.lone && p.applies >= 512) return run_products<1, 1, 1, true, true, 1, 1>(p, a, ws, diag, part, st);
     if (p.tile == 1) return p.exact ? run_products<2, 2, 2, true, true, 1, 1>(p, a, ws, diag, part, st) : run_products<2, 2, 2, false, false, 2, 2>(p, a, ws, diag, part, st);
+    if (p.lone) return p.exact ? run_products<1, 1, 1, true, true, 2, 2, 2>(p, a, ws, diag, part, st) : run_products<1, 1, 1, true, false, 2, 2, 2>(p, a, ws, diag, part, st);
     return p.exact ? run_products<1, 1, 1, true, true, 2, 2>(p, a, ws, diag, part, st) : run_products<1, 1, 1, true, false, 2, 2>(p, a, ws, diag, part, st);
 }
 

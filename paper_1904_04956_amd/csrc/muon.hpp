@@ -30,6 +30,7 @@ struct MuonPlan {
     int tile;                 // 0: 64 x 64 tiles, 1: 128 x 128, 2: 128 x 128 and, in the last product, 256 x 128;
                               // 3: a matrix a workgroup, all in LDS (small: blocks of 16 rows of the largest Gram matrix, lds: bytes)
     int small, lds;
+    int lone;                 // no more tiles of S than CUs: two sets of wavefronts a tile
     int exact;                // products of both planes (mode 0)
     int chunks, casts, grams, squares, applies, sums;
     size_t sums_at, diag_at, part_at, bytes;   // byte offsets in scratch: squares' sums (double), diagonals, partial Gram tiles (float)
