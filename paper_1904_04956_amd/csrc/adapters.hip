@@ -73,7 +73,7 @@ __device__ void make_plan(const AdaptShape& s, const AdaptPlan& p, const int32_t
         before[i] = v - sum[i];
     }
     __syncthreads();
-    for (int i = 0; i < 3; ++i) for (int w = 0; w < wave; ++w) before[i] += wave_sum[i * (PLAN_THREADS / 64) + w];
+    if (k0 < keys) for (int w = 0; w < wave; ++w) for (int i = 0; i < 3; ++i) before[i] += wave_sum[i * (PLAN_THREADS / 64) + w];
     for (int i = 0; i < 3; ++i) sum[i] = before[i];
     for (int k = k0; k < k1; ++k) { first[k] = sum[0]; tile0[k] = sum[1]; chunk0[k] = sum[2]; add(k); }
     if (k1 == keys && k0 < keys) { first[keys] = sum[0]; tile0[keys] = sum[1]; chunk0[keys] = sum[2]; }
@@ -552,22 +552,35 @@ __global__ __launch_bounds__(PLAN_THREADS) void adapt_transpose_kernel(Transpose
     const AdaptShape& s = a.s;
     // (the plan is a chain of latencies: the first workgroup makes it while the others move)
     if (blockIdx.x == 0) { make_plan(s, p, ids, plan, words); return; }
-    // four tiles of 32 x 32 a workgroup, 256 threads each
+    // eight tiles of 32 x 32 a workgroup, 256 threads two of them (one: 13 us instead of 11 for 100 adapters of 16 x 1024 and 256 x 16)
     auto tiles = [](int r, int c) { return ((r + 31) / 32) * ((c + 31) / 32); };
-    const int tw = tiles(s.N, s.K), ta = tiles(s.rank, s.K), tb = tiles(s.N, s.rank), sub = threadIdx.x >> 8;
-    T (*lds)[33] = reinterpret_cast<T (*)[33]>(words) + 32 * sub;
-    int id = (blockIdx.x - 1) * 4 + sub, R = 0, C = 0;
-    const T* from = nullptr; T* to = nullptr;
-    if (id < tw) { from = static_cast<const T*>(a.W); to = static_cast<T*>(a.Wt); R = s.N; C = s.K; }
-    else if ((id -= tw) < ta * s.count) { const long long k = id / ta; id %= ta; R = s.rank; C = s.K; from = static_cast<const T*>(a.A) + k * R * C; to = static_cast<T*>(a.At) + k * R * C; }
-    else if ((id -= ta * s.count) < tb * s.count) { const long long k = id / tb; id %= tb; R = s.N; C = s.rank; from = static_cast<const T*>(a.Bm) + k * R * C; to = static_cast<T*>(a.Bt) + k * R * C; }
-    else id = 0;                                            // (the last workgroup's tiles beyond the last: empty)
-    const int nc = max(1, (C + 31) / 32), r0 = id / nc * 32, c0 = id % nc * 32, i = threadIdx.x >> 5 & 7, j = threadIdx.x & 31;
+    const int tw = tiles(s.N, s.K), ta = tiles(s.rank, s.K), tb = tiles(s.N, s.rank), sub = threadIdx.x >> 8, i = threadIdx.x >> 5 & 7, j = threadIdx.x & 31;
+    const T* from[2]; T* to[2];
+    int R[2], C[2], r0[2], c0[2];
+    T v[2][4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) if (r0 + i + 8 * e < R && c0 + j < C) lds[i + 8 * e][j] = from[(long long)(r0 + i + 8 * e) * C + c0 + j];
+    for (int q = 0; q < 2; ++q) {
+        int id = (blockIdx.x - 1) * 8 + sub * 2 + q;
+        from[q] = nullptr; to[q] = nullptr; R[q] = C[q] = 0;
+        if (id < tw) { from[q] = static_cast<const T*>(a.W); to[q] = static_cast<T*>(a.Wt); R[q] = s.N; C[q] = s.K; }
+        else if ((id -= tw) < ta * s.count) { const long long k = id / ta; id %= ta; R[q] = s.rank; C[q] = s.K; from[q] = static_cast<const T*>(a.A) + k * R[q] * C[q]; to[q] = static_cast<T*>(a.At) + k * R[q] * C[q]; }
+        else if ((id -= ta * s.count) < tb * s.count) { const long long k = id / tb; id %= tb; R[q] = s.N; C[q] = s.rank; from[q] = static_cast<const T*>(a.Bm) + k * R[q] * C[q]; to[q] = static_cast<T*>(a.Bt) + k * R[q] * C[q]; }
+        else id = 0;                                        // (the last workgroup's tiles beyond the last: empty)
+        const int nc = max(1, (C[q] + 31) / 32);
+        r0[q] = id / nc * 32; c0[q] = id % nc * 32;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (r0[q] + i + 8 * e < R[q] && c0[q] + j < C[q]) v[q][e] = from[q][(long long)(r0[q] + i + 8 * e) * C[q] + c0[q] + j];
+    }
+    T (*lds)[33] = reinterpret_cast<T (*)[33]>(words) + 64 * sub;
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (r0[q] + i + 8 * e < R[q] && c0[q] + j < C[q]) lds[32 * q + i + 8 * e][j] = v[q][e];
     __syncthreads();
 #pragma unroll
-    for (int e = 0; e < 4; ++e) if (c0 + i + 8 * e < C && r0 + j < R) to[(long long)(c0 + i + 8 * e) * R + r0 + j] = lds[j][i + 8 * e];
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (c0[q] + i + 8 * e < C[q] && r0[q] + j < R[q]) to[q][(long long)(c0[q] + i + 8 * e) * R[q] + r0[q] + j] = lds[32 * q + j][i + 8 * e];
 }
 
 // ---- the adapters' gradients -------------------------------------------------------------------------------------------
@@ -840,10 +853,10 @@ hipError_t launch_adapt_plan(const AdaptShape& s, const AdaptPlan& p, const int3
 hipError_t launch_adapt_project(const ProjectArgs& a, DType type, hipStream_t st) { return type == DT_BF16 ? project<bf16_t>(a, st) : project<float>(a, st); }
 hipError_t launch_adapt_transpose(const TransposeArgs& a, const AdaptPlan& p, const int32_t* ids, char* plan, DType type, hipStream_t st) {
     auto tiles = [](int r, int c) { return ((r + 31) / 32) * ((c + 31) / 32); };
-    const int lds = std::max(plan_lds(a.s.count), 4 * 32 * 33 * 4);
+    const int lds = std::max(plan_lds(a.s.count), 8 * 32 * 33 * 4);
     const int n = tiles(a.s.N, a.s.K) + a.s.count * (tiles(a.s.rank, a.s.K) + tiles(a.s.N, a.s.rank));
-    if (type == DT_BF16) adapt_transpose_kernel<bf16_t><<<1 + (n + 3) / 4, PLAN_THREADS, lds, st>>>(a, p, ids, plan);
-    else adapt_transpose_kernel<float><<<1 + (n + 3) / 4, PLAN_THREADS, lds, st>>>(a, p, ids, plan);
+    if (type == DT_BF16) adapt_transpose_kernel<bf16_t><<<1 + (n + 7) / 8, PLAN_THREADS, lds, st>>>(a, p, ids, plan);
+    else adapt_transpose_kernel<float><<<1 + (n + 7) / 8, PLAN_THREADS, lds, st>>>(a, p, ids, plan);
     return hipGetLastError();
 }
 hipError_t launch_adapt_grad(const AdaptGradArgs& a, DType type, hipStream_t st) { return type == DT_BF16 ? grad<bf16_t>(a, st) : grad<float>(a, st); }
