@@ -16,9 +16,9 @@
 // S and B are symmetric: tiles on and above the diagonal are computed, and stored twice.
 //
 // All matrices of a call share each launch: the flat pass over v and g, the cast to halves, then S, B and the new X five times; the last X goes straight into
-// the weights.  What bounds them, four layers of 512 cells (43 M weights, 301 GFLOP), 776 us in all: the flat pass 82 us, 560 MB at 6.8 TB/s; the cast 54, 340 MB; S 39 each, 900 TFLOP/s
-// of what it would be without the symmetry; B 25, whose 311 tiles are 1.2 a CU; the new X 63, 35 GFLOP and 220 MB; the last 109, 465 MB.  Six of 1024: 353, 304, 301 (1460 TFLOP/s
-// likewise), 153, 518 (870 TFLOP/s, 1 GB), 724 (2 GB).
+// the weights.  What bounds them, four layers of 512 cells (43 M weights, 301 GFLOP), 765 us in all: the flat pass 82 us, 560 MB at 6.8 TB/s; the cast 53, 340 MB; S 38 each, 900 TFLOP/s
+// of what it would be without the symmetry; B 24, whose 311 tiles are 1.2 a CU; the new X 62, 35 GFLOP and 220 MB; the last 108, 465 MB.  Six of 1024: 351, 301, 298 (1460 TFLOP/s
+// likewise), 151, 512 (870 TFLOP/s, 1 GB), 720 (2 GB).
 // Built and dropped: three and four buffers of a slab where a CU has one workgroup (S 41 -> 56 us: what a lone workgroup waits for are its own LDS reads and products in turn,
 // 768 and 512 clocks a slab, not the loads); S in two, three or four parts of the contraction, summed by another launch (58, 66 and 77 us for 45); two steps'
 // B multiplied together, so that X is written three times instead of five (error 4e-4 -> 6e-4).
@@ -1052,7 +1052,7 @@ hipError_t launch_muon(const MuonPlan& p, const MuonArgs& a, void* scratch, hipS
     if (e != hipSuccess) return e;
     if (p.tile == 2) return run_products<2, 4, 2, false, false, 2, 1>(p, a, ws, diag, part, st);
     // (both planes' fragments of a slab fit the registers too: one buffer where workgroups share CUs, 865 -> 782 us a step of two layers of 512 cells in float, 289 -> 271 for two
-    // of 301 with gates apart; two buffers where they have a CU each, 210 us against 222 for two matrices of 1204 x 602)
+    // of 301 with gates apart; two buffers where they have a CU each: with one set of wavefronts 210 us against 222 for two matrices of 1204 x 602)
     if (p.tile == 0 && p.exact && !p.lone && p.applies >= 512) return run_products<1, 1, 1, true, true, 1, 1>(p, a, ws, diag, part, st);
     if (p.tile == 1) return p.exact ? run_products<2, 2, 2, true, true, 1, 1>(p, a, ws, diag, part, st) : run_products<2, 2, 2, false, false, 2, 2>(p, a, ws, diag, part, st);
     if (p.lone) return p.exact ? run_products<1, 1, 1, true, true, 2, 2, 2>(p, a, ws, diag, part, st) : run_products<1, 1, 1, true, false, 2, 2, 2>(p, a, ws, diag, part, st);
