@@ -259,7 +259,7 @@ __global__ __launch_bounds__(64 * RWAVES) void adapt_rows_kernel(ProjectArgs a, 
         for (int w = 1; w < RWAVES; ++w) v += part[w * (NB + RB) * 64 + i];
         const int j = i >> 6, l = i & 63, r = 4 * (l >> 4), c = l & 15;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { if (j < NB) os[(r + e) * (RN + 1) + 16 * j + c] = v[e] + bad; else ts[(r + e) * TLD + 16 * (j - NB) + c] = v[e] + bad; }
+        for (int e = 0; e < 4; ++e) { if (j < NB) os[(r + e) * (RN + 1) + 16 * j + c] = v[e] + bad; else ts[(r + e) * TLD + 16 * (j - NB) + c] = (low && 16 * (j - NB) + c < s.rank ? v[e] : 0.0f) + bad; }
     }
     __syncthreads();
     if (a.t && col0 == 0) {

@@ -168,6 +168,19 @@ def test_what_one_sequence_or_adapter_holds_stays_with_it():
     assert torch.isnan(y2[:, 2].float()).any()
 
 
+@pytest.mark.parametrize("T", [1, 40])
+@pytest.mark.parametrize("mode", [0, 1])
+def test_an_infinite_input_without_adapter(T, mode):
+    # y is what the shared projection alone makes of it, t is zero
+    import torch
+    shape = (T, 4, 32, 16, 3, 2, mode)
+    s = tensors(10, *shape, ids=[0, -1, 1, -1])
+    s["x"][:, 1, 5] = float("inf")
+    y, t = run_forward(s, shape)
+    assert torch.equal(t[:, 1], torch.zeros_like(t[:, 1])) and torch.equal(t[:, 3], torch.zeros_like(t[:, 3]))
+    assert torch.equal(y[:, 1].float(), (s["W"][:, 5].float() * float("inf")).expand(T, 16))
+
+
 def test_replays_and_streams():
     import torch
     shape = (21, 40, 64, 48, 8, 6, 1)
