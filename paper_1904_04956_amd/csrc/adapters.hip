@@ -846,6 +846,17 @@ AdaptPlan adapt_plan(const AdaptShape& s, int rows, int chunk) {
     return p;
 }
 
+bool adapt_fits(const AdaptShape& s, const AdaptPlan& p, bool backward) {
+    auto up = [](long long v, long long m) { return (v + m - 1) / m; };
+    auto launch = [](long long groups, int threads) { return groups <= 0xFFFFFFFFLL / threads; };
+    auto project = [&](int n) { return p.rows == 16 ? launch(8 * up(p.max_tiles, 8) * up(n, RN), 64 * RWAVES) : launch(8 * up(p.max_tiles, 8) * up(n, PN), 256); };
+    if (!backward) return project(s.N);
+    auto tiles = [&](long long r, long long c) { return up(r, 32) * up(c, 32); };
+    return project(s.K) && launch(8 * up(p.max_chunks, 8) * (up(s.K, 128) + up(s.N, 128)), 256) &&
+           launch(s.count * up(s.rank, 32) * (up(s.K, 32) + up(s.N, 32)), 256) &&
+           launch(1 + up(tiles(s.N, s.K) + s.count * (tiles(s.rank, s.K) + tiles(s.N, s.rank)), 8), PLAN_THREADS);
+}
+
 hipError_t launch_adapt_plan(const AdaptShape& s, const AdaptPlan& p, const int32_t* ids, char* plan, hipStream_t st) {
     adapt_plan_kernel<<<1, PLAN_THREADS, plan_lds(s.count), st>>>(s, p, ids, plan);
     return hipGetLastError();

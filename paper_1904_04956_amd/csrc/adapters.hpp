@@ -23,6 +23,8 @@ struct AdaptPlan {
 inline bool adapt_finds(const AdaptShape& s) { return s.B <= 256; }
 // counts: {tiles, chunks}; first [count + 3]: a key's first place in perm; first_chunk [count + 1]; tiles and chunks: {key, first row, its rows, first place in perm}
 AdaptPlan adapt_plan(const AdaptShape& s, int rows, int chunk);
+// Whether each launch of a call has fewer than 2^32 threads, which is what a grid holds.
+bool adapt_fits(const AdaptShape& s, const AdaptPlan& p, bool backward);
 // Rows of a chunk of the gradients' sums: about 64 chunks if one adapter has all rows, at most ADAPT_MAX_CHUNK rows each.
 constexpr int ADAPT_MAX_CHUNK = 1024;
 inline int adapter_chunk_rows(const AdaptShape& s) { const long long M = (long long)s.T * s.B, r = (M + 4095) / 4096 * 64; return (int)(r < ADAPT_MAX_CHUNK ? r : ADAPT_MAX_CHUNK); }

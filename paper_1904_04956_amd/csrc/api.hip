@@ -777,8 +777,6 @@ int loss_run(blstm_ctx* ctx, const LossCall& given, const int32_t* labels, const
     return loss_products(ctx, c, teacher, dz, grad);
 }
 
-// What softmax_xent_fwd_bwd left to the next blstm_backward is written by the call itself.  (Calls of several threads share the context: where
-// nothing is pending, they only read it.)
 // ---- the orthogonalised update ---------------------------------------------------------------------------------------
 // The flat vector as groups of tensors of one shape at constant distances (layers beyond the first are alike).
 bool muon_model_plan(const blstm_ctx* c, int flags, MuonPlan* plan) {
@@ -842,9 +840,10 @@ int adapter_sizes(const char* name, const adapter_config* c, int call, AdapterSc
         return fail(BLSTM_ERR_DIM, "%s: T, B, K and N must be positive, rank in 1..%d, count in 1..%d, mode 0 or 1", name, BLSTM_MAX_ADAPTER_RANK, BLSTM_MAX_ADAPTERS);
     if (call != ADAPTER_FORWARD && call != ADAPTER_BACKWARD) return fail(BLSTM_ERR_DIM, "%s: no call %d", name, call);
     const long long M = (long long)c->T * c->B, wide = (long long)c->K + c->N;
-    // (launches are sized in 32 bits: workgroups of tiles, and of 32 x 32 words of the adapters' transposes)
-    if (M > INT_MAX || (M / 16 + c->count + 2) * (wide / 128 + 2) > INT_MAX || (c->count * 4LL + c->N / 32 + 1) * (wide / 32 + 2) > INT_MAX)
-        return fail(BLSTM_ERR_DIM, "%s: T B below 2^31, T B (K + N) below 2^42 and count (K + N) below 2^33 are taken", name);
+    // (rows and the workgroups of launches are counted in 32 bits, a launch's threads too)
+    static const char* const too_large = "%s: T B up to 2^30, T B (K + N) up to about 2^37 and count rank (K + N) up to about 2^34 are taken";
+    if (M > 1 << 30 || (M / 16 + c->count + 2) * (wide / 128 + 2) > INT_MAX || (c->count * 4LL + c->N / 32 + 1) * (wide / 32 + 2) > INT_MAX)
+        return fail(BLSTM_ERR_DIM, too_large, name);
     AdapterScratch& a = *out;
     a = AdapterScratch{};
     a.s = AdaptShape{c->T, c->B, c->K, c->N, c->rank, c->count, c->scale};
@@ -852,6 +851,7 @@ int adapter_sizes(const char* name, const adapter_config* c, int call, AdapterSc
     const size_t e = c->mode == 1 ? 2 : 4;
     const int chunk = call == ADAPTER_FORWARD ? 0 : adapter_chunk_rows(a.s);
     a.plan = adapt_plan(a.s, adapter_tile_rows(a.s), chunk);
+    if (!adapt_fits(a.s, a.plan, call == ADAPTER_BACKWARD)) return fail(BLSTM_ERR_DIM, too_large, name);
     size_t at = up256(a.plan.bytes);
     auto take = [&](size_t n) { const size_t was = at; at += up256(n); return was; };
     if (call == ADAPTER_BACKWARD) {
@@ -875,6 +875,8 @@ int adapter_check(const char* name, const AdapterScratch& l, const void* scratch
     return BLSTM_OK;
 }
 
+// What softmax_xent_fwd_bwd left to the next blstm_backward is written by the call itself.  (Calls of several threads share the context: where
+// nothing is pending, they only read it.)
 void drop_deferred(blstm_ctx* ctx) {
     if (ctx->pend_z) ctx->pend_z = nullptr;
     if (ctx->twin && ctx->twin->pend_z) ctx->twin->pend_z = nullptr;

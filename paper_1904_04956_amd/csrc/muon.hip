@@ -932,7 +932,7 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
     p.n = n;
     std::copy(g, g + n, p.g);
     for (int i = 0; i < MUON_MAX_GROUPS; ++i) p.at.chunk[i] = p.at.cast[i] = p.at.gram[i] = p.at.square[i] = p.at.apply[i] = p.at.sum[i] = 0x7FFFFFFF;
-    const long long most = 0x7FFFFFFF;
+    const long long index = 0x7FFFFFFF, most = 0xFFFFFFFF / 256;      // (a launch has fewer than 2^32 threads)
     auto up = [](long long v, long long m) { return (v + m - 1) / m * m; };
     // small matrices only: a workgroup each
     int side = 0;
@@ -953,7 +953,7 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
                 q.chunks = (int)(((long long)q.rows * q.cols + FLAT - 1) / FLAT);
                 p.at.apply[i] = (int)groups;
                 groups += (long long)q.count * (q.ortho ? 1 : q.chunks);
-                if (groups > most) return false;
+                if (groups > 0xFFFFFFFF / SMALL_THREADS) return false;
             }
             p.tile = 3;
             p.applies = (int)groups;
@@ -1001,7 +1001,7 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
         if (chunks > most) return false;
         if (!q.ortho) continue;
         const long long nx = (long long)q.rp * q.cp, ns = (long long)q.mp * q.mp;
-        if ((long long)std::max(q.rp, q.cp) * 256 > most || nx / CAST * q.count > most) return false;
+        if ((long long)std::max(q.rp, q.cp) * 256 > index || nx / CAST * q.count > most) return false;
         q.casts = (int)(nx / CAST);
         casts += (long long)q.count * q.casts;
         const int length = std::max(q.rp, q.cp) / 64;

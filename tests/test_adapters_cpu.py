@@ -87,6 +87,18 @@ def test_sizes_are_refused(change):
         assert e.value.code == -2
 
 
+@pytest.mark.parametrize("which,change", [(bl.ADAPTER_FORWARD, dict(T=(1 << 30) + 1, B=1, K=1, N=1)), (bl.ADAPTER_FORWARD, dict(T=1, B=2048, count=2048, N=200000)),
+                                          (bl.ADAPTER_FORWARD, dict(T=1 << 20, B=256, N=16384)), (bl.ADAPTER_BACKWARD, dict(T=1 << 20, B=256, K=16384)),
+                                          (bl.ADAPTER_BACKWARD, dict(count=4096, rank=128, N=32768)), (bl.ADAPTER_BACKWARD, dict(K=1 << 18, N=1 << 18))])
+def test_launches_beyond_a_grid_are_refused(which, change):
+    with pytest.raises(bl.BlstmError) as e:
+        bl.adapter_scratch_bytes(config(**change), which)
+    assert e.value.code == -2
+    with pytest.raises(bl.BlstmError) as e:
+        (forward if which == bl.ADAPTER_FORWARD else backward)(config(**change))
+    assert e.value.code == -2
+
+
 def test_no_config_and_no_such_call():
     for call in (lambda: bl.adapter_scratch_bytes(None, 0), lambda: bl.adapter_scratch_bytes(config(), 2), lambda: forward(None), lambda: backward(None)):
         with pytest.raises(bl.BlstmError):

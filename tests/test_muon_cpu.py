@@ -94,6 +94,10 @@ def test_models_and_matrices_are_refused(ctx):
     for sizes in ((0, 1, 1, 0), (1, 1, 0, 0), (1, 1, 1, 3), (1, 1 << 24, 1, 1), (1 << 30, 1 << 6, 1 << 6, 1)):
         with pytest.raises(bl.BlstmError):
             bl.muon_orthogonalize_scratch_bytes(*sizes)
+    # a workgroup of 1024 threads a matrix, and fewer than 2^32 threads a launch
+    assert bl.muon_orthogonalize_scratch_bytes((1 << 22) - 1, 1, 1, 1) > 0
+    with pytest.raises(bl.BlstmError):
+        bl.muon_orthogonalize_scratch_bytes(1 << 22, 1, 1, 1)
     with pytest.raises(bl.BlstmError):
         bl.muon_scratch_bytes(ctx, 8)
     ok = bl.muon_orthogonalize_scratch_bytes(1, 3, 4, 0)
