@@ -37,13 +37,15 @@ class Learner:
         self.mode = mode
         self.device = torch.device(device)
         self.ctx = bl.blstm_create(T, B, D, H, L, P, V, mode, loss_scale)
-        if recurrent_path:
-            bl.blstm_set_option(self.ctx, bl.BLSTM_OPT_RECURRENT_PATH, recurrent_path)
         # the copies the passes derive from the weights are kept across steps: every method below that changes the
         # weights reports it (weights_changed)
-        bl.blstm_set_option(self.ctx, bl.BLSTM_OPT_KEEP_WEIGHT_COPIES, int(bool(keep_weight_copies)))
+        self.options = {bl.BLSTM_OPT_KEEP_WEIGHT_COPIES: int(bool(keep_weight_copies))}
+        if recurrent_path:
+            self.options[bl.BLSTM_OPT_RECURRENT_PATH] = recurrent_path
         if recurrent_sync is not None:
-            bl.blstm_set_option(self.ctx, bl.BLSTM_OPT_RECURRENT_SYNC, recurrent_sync)
+            self.options[bl.BLSTM_OPT_RECURRENT_SYNC] = recurrent_sync
+        for option, value in self.options.items():
+            bl.blstm_set_option(self.ctx, option, value)
         # calgrad() always runs softmax_xent_fwd_bwd and blstm_backward back to back on the same gradient vector, so the
         # softmax layer's weight gradient may join the backward pass's grouped launch
         bl.blstm_set_option(self.ctx, bl.BLSTM_OPT_DEFER_SOFTMAX_WGRAD, int(bool(defer_softmax_wgrad)))
@@ -222,21 +224,27 @@ class Learner:
             raise ValueError("adapters stand beside the bottleneck's projection, and this model has none")
         if self.adapters is not None:
             self.adapters.close()
+            self.adapters = None
         self.adapters = Adapters(self, count, rank, scale)
         # the passes run on the stack's own context below, so nothing of the softmax layer's gradient may be left to this one's backward pass
         bl.blstm_set_option(self.ctx, bl.BLSTM_OPT_DEFER_SOFTMAX_WGRAD, 0)
         self.defer_softmax_wgrad = False
         return self.adapters
 
+    def _attached(self):
+        if self.adapters is None:
+            raise ValueError("no adapters are attached")
+        return self.adapters
+
     def forward_adapted(self, stream=None):
         """z of the batch with each sequence's adapter."""
-        a = self.adapters
+        a = self._attached()
         bl.blstm_forward(a.stack, self.theta_fwd, self.x, a.h, stream)
         bl.adapter_forward(a.cfg, a.W, a.b, a.A_fwd, a.Bm_fwd, a.ids, a.h, self.z, a.t, a.scratch(bl.ADAPTER_FORWARD, self, stream), None, stream)
 
     def calgrad_adapted(self, shared=True, stream=None):
         """calgrad() with the adapters: their gradients in adapters.dA and .dB and, with `shared`, the model's in grad (without: the softmax layer's alone)."""
-        a = self.adapters
+        a = self._attached()
         self.forward_adapted(stream)
         bl.softmax_xent_fwd_bwd(self.ctx, self.theta_fwd, self.z, self.labels, self.loss, self.dz, self.grad, stream)
         bl.adapter_backward(a.cfg, a.W, a.A_fwd, a.Bm_fwd, a.ids, a.h, a.t, self.dz, a.dh if shared else None, a.dA, a.dB, a.dW if shared else None,
@@ -246,7 +254,7 @@ class Learner:
 
     def apply_adapters(self, lr, momentum=0.95, weight_decay=0.0, nesterov=True, stream=None):
         """The orthogonalised update of every adapter's two factors (binding.muon_matrices_step)."""
-        a = self.adapters
+        a = self._attached()
         for name, theta, shadow, grad, velocity in (("A", a.A, a.A_bf16, a.dA, a.vA), ("B", a.Bm, a.Bm_bf16, a.dB, a.vB)):
             sizes = (*theta.shape, self.mode)
             bl.muon_matrices_step(theta, shadow, grad, velocity, *sizes, lr, momentum, weight_decay, bl.MUON_NESTEROV if nesterov else 0,
@@ -267,6 +275,8 @@ class Learner:
     def check_status(self, stream=None):
         """Synchronises and raises if a persistent kernel abandoned a wait."""
         bl.blstm_device_status(self.ctx, stream)
+        if self.adapters is not None:
+            bl.blstm_device_status(self.adapters.stack, stream)
 
     # ---- data out --------------------------------------------------------------------
     def loss_value(self) -> float:
@@ -292,7 +302,8 @@ class Adapters:
         self.cfg = bl.adapter_config(T, B, K, N, rank, count, learner.mode, scale)
         bl.adapter_scratch_bytes(self.cfg, bl.ADAPTER_BACKWARD)          # refuses what the calls would
         self.stack = bl.blstm_create(T, B, d["D"], d["H"], d["L"], 0, 1, learner.mode)
-        bl.blstm_set_option(self.stack, bl.BLSTM_OPT_KEEP_WEIGHT_COPIES, 1)
+        for option, value in learner.options.items():
+            bl.blstm_set_option(self.stack, option, value)
         self.workspace = torch.empty(bl.blstm_workspace_bytes(self.stack), dtype=torch.uint8, device=dev)
         bl.blstm_bind(self.stack, self.workspace)
         real = lambda *shape: torch.zeros(shape, dtype=torch.float32, device=dev)  # noqa: E731

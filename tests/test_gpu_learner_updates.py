@@ -12,11 +12,11 @@ DIMS = dict(T=5, B=9, D=12, H=16, L=2, P=24, V=50)
 IDS = [0, 1, -1, 2, 0, 1, 1, -1, 2]
 
 
-def learner(mode, seed, momentum=0.0, **dims):
+def learner(mode, seed, momentum=0.0, options={}, **dims):
     from paper_1904_04956_amd import inputs
     from paper_1904_04956_amd.harness import Learner
     d = dict(DIMS, **dims)
-    lrn = Learner(mode=mode, momentum=momentum, **d)
+    lrn = Learner(mode=mode, momentum=momentum, **d, **options)
     theta = inputs.make_theta(lrn.n, seed, bf16=mode == 1)
     x, labels = inputs.make_batch(d["T"], d["B"], d["D"], d["V"], seed, bf16=mode == 1)
     lrn.set_theta(theta)
@@ -175,6 +175,56 @@ def test_adapters_attached_anew():
         used = torch.zeros(300, dtype=torch.bool, device="cuda:0")
         used[b.ids.long()] = True
         assert bool((b.dA[used].abs().amax((1, 2)) > 0).all()) and float(b.dA[~used].abs().max()) == 0.0 and bool(torch.isfinite(b.dB).all())
+    finally:
+        lrn.close()
+
+
+def test_the_stack_has_the_learners_options():
+    # without kept copies, weights may be written without a word
+    import torch
+    one, a, *_ = adapted(1, 87, options=dict(keep_weight_copies=False), H=13, D=7)
+    two, b, *_ = adapted(1, 88, H=13, D=7)
+    try:
+        one.calgrad_adapted()
+        for to, of in ((one.theta, two.theta), (one.shadow, two.shadow), (one.x, two.x), (one.labels, two.labels), (a.A, b.A), (a.Bm, b.Bm), (a.A_bf16, b.A_bf16), (a.Bm_bf16, b.Bm_bf16)):
+            to.copy_(of)
+        one.calgrad_adapted()
+        two.calgrad_adapted()
+        torch.cuda.synchronize()
+        assert torch.equal(one.grad, two.grad) and torch.equal(a.dA, b.dA) and torch.equal(one.loss, two.loss)
+    finally:
+        one.close()
+        two.close()
+
+
+def test_the_stacks_status_is_the_learners(monkeypatch):
+    from paper_1904_04956_amd import binding as bl
+    lrn, a, *_ = adapted(1, 89)
+    try:
+        asked, real = [], bl.blstm_device_status
+        monkeypatch.setattr(bl, "blstm_device_status", lambda ctx, stream=None: (asked.append(ctx), real(ctx, stream)))
+        lrn.check_status()
+        assert asked == [lrn.ctx, a.stack]
+    finally:
+        lrn.close()
+
+
+def test_adapters_that_are_not_there():
+    from paper_1904_04956_amd import binding as bl
+    lrn, *_ = learner(1, 90)
+    try:
+        calls = (lrn.forward_adapted, lrn.calgrad_adapted, lambda: lrn.apply_adapters(0.1))
+        for attempt in range(2):
+            for call in calls:
+                with pytest.raises(ValueError):
+                    call()
+            if attempt == 0:                                            # refused adapters leave none, and a learner that works
+                lrn.attach_adapters(2, 4)
+                with pytest.raises(bl.BlstmError):
+                    lrn.attach_adapters(2, 129)
+        lrn.calgrad()
+        lrn.apply(0.1)
+        lrn.check_status()
     finally:
         lrn.close()
 
