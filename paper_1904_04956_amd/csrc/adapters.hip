@@ -391,7 +391,7 @@ __global__ __launch_bounds__(256) void adapt_tile_kernel(ProjectArgs a, bool low
         };
         issue(0);
         for (int it = 0; it < slabs; ++it) {
-            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // (the slab has landed, the reads of the other buffer have come)
             if (it + 1 < slabs) issue(it + 1);
             uint4* at = smem + (it & 1) * STAGE;
             if (words - it * 8 < 8) {
@@ -727,7 +727,7 @@ __global__ __launch_bounds__(256) void adapt_grad_direct_kernel(AdaptGradArgs a)
     const int g = lane >> 4, li = lane & 15, at = 8 * (g >> 1) + (li >> 2), off = 32 * (g & 1) + (li & 3) * 8;
     const int tr = at * 256 + (((2 * wave + (g & 1)) ^ tr_swz<16>(li >> 2)) << 5) + (li & 3) * 8;
     for (int it = 0; it < slabs; ++it) {
-        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // (the slab has landed, the reads of the other buffer have come)
         if (it + 1 < slabs) issue(it + 1);
         char* rs = base + (it & 1) * STAGE;
         const int left = nrows - 64 * it;

@@ -303,12 +303,12 @@ __device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand
         }
     } else {
         for (int it = slab0; it < slab0 + trips; ++it) {       // (every wavefront of the workgroup goes through as many barriers)
-            // (this wavefront's loads of the slab have landed when at most the younger slabs' are outstanding)
+            // (this wavefront's loads of the slab have landed when at most the younger slabs' are outstanding; its reads of the buffer that is filled next have come)
             constexpr int LOADS = PL * (NIA + NIB);
             const int younger = min(NST - 2, slab1 - 1 - it);
-            if (NST >= 4 && younger == 2) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(2 * LOADS) : "memory");
-            else if (NST >= 3 && younger == 1) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(LOADS) : "memory");
-            else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+            if (NST >= 4 && younger == 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(2 * LOADS) : "memory");
+            else if (NST >= 3 && younger == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LOADS) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
             if (it + NST - 1 < slab1) issue(it + NST - 1);
             const uint4* sa = smem + ((it - slab0) % NST) * STAGE;
             const uint4* sb = sa + PL * PA;
