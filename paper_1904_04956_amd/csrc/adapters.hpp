@@ -28,10 +28,12 @@ bool adapt_fits(const AdaptShape& s, const AdaptPlan& p, bool backward);
 // Rows of a chunk of the gradients' sums: about 64 chunks if one adapter has all rows, at most ADAPT_MAX_CHUNK rows each.
 constexpr int ADAPT_MAX_CHUNK = 1024;
 inline int adapter_chunk_rows(const AdaptShape& s) { const long long M = (long long)s.T * s.B, r = (M + 4095) / 4096 * 64; return (int)(r < ADAPT_MAX_CHUNK ? r : ADAPT_MAX_CHUNK); }
-// Rows of a tile: 16 for a frame or few rows of an adapter, 128 where the adapters' rows fill several such tiles, else 64.
-inline int adapter_tile_rows(const AdaptShape& s) {
+// Rows of a tile of y (backward: of dx): 16 where such tiles are few, 128 where the adapters' rows fill several such tiles, else 64.  16 against 64 rows, us, at W
+// workgroups of 16 rows x 32 columns (K 1024 or 640, N 256), bf16: W 104 10.5 and 14.3; 544 15.0 and 18.3; 896 26.3 and 19.4; 1040 41 and 20.5; float: 104 11 and 38; 544 22 and 57;
+// 1008 43 and 61; 1376 60 and 41.  The whole backward pass in float, whose contraction is short: 672 32 and 35, 840 34.7 and 33.7, 893 (of 67, no whole words) 39 and 29.
+inline int adapter_tile_rows(const AdaptShape& s, bool backward, DType type) {
     const long long M = (long long)s.T * s.B, groups = s.B < s.count + 1 ? s.B : s.count + 1;
-    return s.T <= 16 && M <= 2048 ? 16 : M >= 512 * groups && M >= 16384 ? 128 : 64;
+    return (M / 16 + groups) * (((backward ? s.K : s.N) + 31) / 32) <= (type == DT_BF16 || backward ? 640 : 1024) ? 16 : M >= 512 * groups && M >= 16384 ? 128 : 64;
 }
 hipError_t launch_adapt_plan(const AdaptShape& s, const AdaptPlan& p, const int32_t* ids, char* plan, hipStream_t st);
 

@@ -850,7 +850,7 @@ int adapter_sizes(const char* name, const adapter_config* c, int call, AdapterSc
     a.type = c->mode == 1 ? DT_BF16 : DT_F32;
     const size_t e = c->mode == 1 ? 2 : 4;
     const int chunk = call == ADAPTER_FORWARD ? 0 : adapter_chunk_rows(a.s);
-    a.plan = adapt_plan(a.s, adapter_tile_rows(a.s), chunk);
+    a.plan = adapt_plan(a.s, adapter_tile_rows(a.s, call == ADAPTER_BACKWARD, a.type), chunk);
     if (!adapt_fits(a.s, a.plan, call == ADAPTER_BACKWARD)) return fail(BLSTM_ERR_DIM, too_large, name);
     size_t at = up256(a.plan.bytes);
     auto take = [&](size_t n) { const size_t was = at; at += up256(n); return was; };

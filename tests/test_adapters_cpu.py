@@ -87,7 +87,7 @@ def test_sizes_are_refused(change):
         assert e.value.code == -2
 
 
-@pytest.mark.parametrize("which,change", [(bl.ADAPTER_FORWARD, dict(T=(1 << 30) + 1, B=1, K=1, N=1)), (bl.ADAPTER_FORWARD, dict(T=1, B=2048, count=2048, N=200000)),
+@pytest.mark.parametrize("which,change", [(bl.ADAPTER_FORWARD, dict(T=(1 << 30) + 1, B=1, K=1, N=1)), (bl.ADAPTER_FORWARD, dict(T=1, B=2048, count=2048, N=1 << 22)),
                                           (bl.ADAPTER_FORWARD, dict(T=1 << 20, B=256, N=16384)), (bl.ADAPTER_BACKWARD, dict(T=1 << 20, B=256, K=16384)),
                                           (bl.ADAPTER_BACKWARD, dict(count=4096, rank=128, N=32768)), (bl.ADAPTER_BACKWARD, dict(K=1 << 18, N=1 << 18))])
 def test_launches_beyond_a_grid_are_refused(which, change):
@@ -117,9 +117,10 @@ def test_launches_and_failures(recorder):  # noqa: F811
         for call in (fwd, lambda: bwd(P), lambda: bwd(None)):
             out.append([x for x in launches(call) if "adapt" not in x])
         # batches of few sequences find their tiles, others have a plan made first
-        many = bl.adapter_config(1, 300, 64, 24, 8, 5, 1, 1.0)
+        many, large = bl.adapter_config(1, 300, 64, 24, 8, 5, 1, 1.0), bl.adapter_config(100, 32, 64, 240, 8, 5, 1, 1.0)
         out.append([len(launches(fwd)), len(launches(lambda: bl.adapter_forward(many, P, P, P, P, P, P, P, P, P, 1 << 30, 0)))])
-        for part, call in ((b"adapt_plan", lambda: bl.adapter_forward(many, P, P, P, P, P, P, P, P, P, 1 << 30, 0)), (b"adapt_tile", fwd),
+        for part, call in ((b"adapt_plan", lambda: bl.adapter_forward(many, P, P, P, P, P, P, P, P, P, 1 << 30, 0)), (b"adapt_rows", fwd),
+                           (b"adapt_tile", lambda: bl.adapter_forward(large, P, P, P, P, P, P, P, P, P, 1 << 30, 0)),
                            (b"adapt_transpose", lambda: bwd(P)), (b"adapt_grad", lambda: bwd(P))):
             rec.recorder_fail(part)
             try:
@@ -130,4 +131,4 @@ def test_launches_and_failures(recorder):  # noqa: F811
     """)
     assert got[0] == [] and got[2] == [] and len(got[1]) >= 1            # the shared projection's gradient is an ordinary product
     assert got[3] == [1, 2]
-    assert got[4:] == [-5, -5, -5, -5]
+    assert got[4:] == [-5, -5, -5, -5, -5]

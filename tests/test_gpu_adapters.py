@@ -105,7 +105,10 @@ def check(seed, shape, scale=1.5, ids=None, bias=True, dx=True, shared=True):
 
 
 SHAPES = [(1, 1, 1, 1, 1, 1), (1, 1, 1024, 256, 16, 4), (1, 64, 1024, 256, 16, 64), (1, 3, 40, 130, 3, 2), (5, 1, 64, 64, 8, 1), (21, 30, 602, 67, 5, 7), (21, 40, 640, 128, 32, 3),
-          (4, 17, 72, 300, 33, 9), (2, 9, 129, 127, 128, 3), (70, 3, 96, 40, 64, 2), (300, 2, 50, 24, 17, 5), (1, 2500, 24, 16, 4, 2500), (3, 1100, 16, 8, 2, 700), (21, 256, 256, 128, 16, 100)]
+          (4, 17, 72, 300, 33, 9), (2, 9, 129, 127, 128, 3), (70, 3, 96, 40, 64, 2), (300, 2, 50, 24, 17, 5), (1, 2500, 24, 16, 4, 2500), (3, 1100, 16, 8, 2, 700), (21, 256, 256, 128, 16, 100),
+          # tiles of 64 rows, and of 128
+          (21, 60, 602, 467, 5, 7), (21, 80, 640, 328, 32, 3), (40, 40, 72, 500, 33, 9), (40, 40, 500, 72, 33, 9), (70, 30, 96, 300, 64, 2), (70, 30, 300, 96, 64, 2),
+          (20, 90, 129, 327, 128, 3), (20, 90, 327, 129, 128, 3), (300, 8, 50, 424, 17, 5), (130, 130, 40, 72, 20, 3), (130, 130, 37, 43, 5, 2)]
 
 
 @pytest.mark.parametrize("mode", [0, 1])
