@@ -984,7 +984,8 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
         MuonGroup& q = p.g[i];
         q.tall = q.rows > q.cols;
         q.rp = (int)up(q.rows, high); q.cp = (int)up(q.cols, edge);
-        q.mp = std::min(q.rp, q.cp);
+        // (the side that the last product's tiles walk along B: rows padded to 256 may be more than columns padded to 128 where rows <= columns)
+        q.mp = q.tall ? q.cp : q.rp;
         const long long nt = q.mp / edge;
         q.grams = (int)(nt * (nt + 1) / 2);
         if (q.ortho) { tiles_s += (long long)q.count * q.grams; slabs += (long long)q.count * q.grams * (std::max(q.rp, q.cp) / 64); }
