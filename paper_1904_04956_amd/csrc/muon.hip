@@ -934,6 +934,8 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
     for (int i = 0; i < MUON_MAX_GROUPS; ++i) p.at.chunk[i] = p.at.cast[i] = p.at.gram[i] = p.at.square[i] = p.at.apply[i] = p.at.sum[i] = 0x7FFFFFFF;
     const long long index = 0x7FFFFFFF, most = 0xFFFFFFFF / 256;      // (a launch has fewer than 2^32 threads)
     auto up = [](long long v, long long m) { return (v + m - 1) / m * m; };
+    // (what follows rounds sides up in 32 bits)
+    for (int i = 0; i < n; ++i) if (g[i].ortho && std::max(g[i].rows, g[i].cols) > 1 << 30) return false;
     // small matrices only: a workgroup each
     int side = 0;
     for (int i = 0; i < n; ++i) if (g[i].ortho) side = std::max(side, std::min(g[i].rows, g[i].cols));
@@ -983,12 +985,14 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
     for (int i = 0; i < n; ++i) {
         MuonGroup& q = p.g[i];
         q.tall = q.rows > q.cols;
+        if (!q.ortho) continue;
         q.rp = (int)up(q.rows, high); q.cp = (int)up(q.cols, edge);
         // (the side that the last product's tiles walk along B: rows padded to 256 may be more than columns padded to 128 where rows <= columns)
         q.mp = q.tall ? q.cp : q.rp;
         const long long nt = q.mp / edge;
         q.grams = (int)(nt * (nt + 1) / 2);
-        if (q.ortho) { tiles_s += (long long)q.count * q.grams; slabs += (long long)q.count * q.grams * (std::max(q.rp, q.cp) / 64); }
+        tiles_s += (long long)q.count * q.grams;
+        slabs += (long long)q.count * q.grams * (std::max(q.rp, q.cp) / 64);
     }
     // Gram tiles: parts along the contraction where it is long for their number, none shorter than eight slabs
     p.lone = p.tile == 0 && tiles_s <= 256;

@@ -157,3 +157,14 @@ def test_models_lie_inside(plans, flags):
                 if bad: out[str((dims, mode))] = bad[:2]
     """)
     assert got == {}
+
+
+@pytest.mark.parametrize("rows,cols", [(2 ** 31 - 1, 1), (1, 2 ** 31 - 1), (1, 2147483600), (2147483500, 1), (2 ** 30 + 1, 1), (1, 2 ** 30 + 1), (2 ** 31 - 1, 2 ** 8), (1, 2 ** 24)])
+@pytest.mark.parametrize("mode", [0, 1])
+def test_sides_that_no_padding_fits_are_refused(rows, cols, mode):
+    from paper_1904_04956_amd import binding as bl
+    for call in (lambda: bl.muon_orthogonalize_scratch_bytes(1, rows, cols, mode), lambda: bl.muon_orthogonalize(4096, 1 << 40, 1, rows, cols, mode, 4096, 1 << 62, 0),
+                 lambda: bl.muon_matrices_step(4096, None, 4096, None, 1, rows, cols, mode, 0.1, 0.0, 0.0, 0, 4096, 1 << 62, 0)):
+        with pytest.raises(bl.BlstmError) as e:
+            call()
+        assert e.value.code == -2
