@@ -209,7 +209,7 @@ int muon_step(const blstm_ctx* ctx, float* theta_master, void* theta_bf16_or_nul
    any other id outside [0, count) is never used as an index: that sequence's y, t and dx are NaN, and it adds nothing to dA and dB.  Any number of sequences may
    share an adapter.  W and b may lie in a flat parameter vector: these tensors need no more alignment than their elements' (whole 16-byte words, width K
    (backward: K and N) included, are the faster).  Nothing may overlap what is written.  Scratch as for the softmax calls: caller-owned, 16-byte aligned, holds
-   nothing between calls; calls that overlap need one each.  The same inputs give the same bits.  T B is at most 2^30. */
+   nothing between calls; calls that overlap need one each.  The same inputs give the same bits.  T B is at most 2^30, K and N are less. */
 #define BLSTM_NO_ADAPTER (-1)
 #define BLSTM_MAX_ADAPTERS 4096
 #define BLSTM_MAX_ADAPTER_RANK 128

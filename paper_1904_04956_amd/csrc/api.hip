@@ -840,9 +840,9 @@ int adapter_sizes(const char* name, const adapter_config* c, int call, AdapterSc
         return fail(BLSTM_ERR_DIM, "%s: T, B, K and N must be positive, rank in 1..%d, count in 1..%d, mode 0 or 1", name, BLSTM_MAX_ADAPTER_RANK, BLSTM_MAX_ADAPTERS);
     if (call != ADAPTER_FORWARD && call != ADAPTER_BACKWARD) return fail(BLSTM_ERR_DIM, "%s: no call %d", name, call);
     const long long M = (long long)c->T * c->B, wide = (long long)c->K + c->N;
-    // (rows and the workgroups of launches are counted in 32 bits, a launch's threads too)
-    static const char* const too_large = "%s: T B up to 2^30, T B (K + N) up to about 2^37 and count rank (K + N) up to about 2^34 are taken";
-    if (M > 1 << 30 || (M / 16 + c->count + 2) * (wide / 128 + 2) > INT_MAX || (c->count * 4LL + c->N / 32 + 1) * (wide / 32 + 2) > INT_MAX)
+    // (rows, the bytes of one and the workgroups of launches are counted in 32 bits, a launch's threads too)
+    static const char* const too_large = "%s: T B up to 2^30, K and N below 2^30, T B (K + N) up to about 2^37 and count rank (K + N) up to about 2^34 are taken";
+    if (M > 1 << 30 || c->K >= 1 << 30 || c->N >= 1 << 30 || (M / 16 + c->count + 2) * (wide / 128 + 2) > INT_MAX || (c->count * 4LL + c->N / 32 + 1) * (wide / 32 + 2) > INT_MAX)
         return fail(BLSTM_ERR_DIM, too_large, name);
     AdapterScratch& a = *out;
     a = AdapterScratch{};
