@@ -1,0 +1,139 @@
+"""The orthogonalised update's launches for many tiles in mode 1 (128 x 128, and 256 x 128 in the last product): tall, wide, ragged and near-square matrices, in float out of the
+weights themselves, and models of several groups.
+
+Bound (2-norm of the difference over 2-norm of the result, a matrix at a time).  A half's rounding has a root mean square of 2^-10 / sqrt(12) of a binade's beginning, whose values have
+one of sqrt(1.5 / ln 2): r = 2.0e-4 of what is rounded.  Where the singular values end up (0.7 to 1.2, the eigenvalues of S 0.5 to 1.4) d(bS + cS^2)/dS is between -2.7 and 1.1, -0.7 on
+average, so that in a step X's rounding in S arrives as 1.0 r, S's own off the diagonal (a fourth of it) as 0.2 r, B's off the diagonal and X's in the product with it as 0.3 r each:
+1.1 to 1.2 r, and the steps after hand an error of X on at about its relative size.  Five steps, independent: 2.7 r; a third more for how unevenly singular values lie: 3.5 r = 6.9e-4.
+(X without its second part, or with the diagonals rounded to halves, is off by 8.7e-4 to 1.3e-3: the same arithmetic in numpy.)"""
+import numpy as np
+import pytest
+
+from oracle import blstm_oracle as orc
+from oracle import muon
+from tests.test_muon_plans_cpu import plans  # noqa: F401
+
+R = 2.0 ** -10 / np.sqrt(12) / np.sqrt(1.5 / np.log(2))
+E1 = 3.5 * R
+
+# (count, rows, cols), and the tiles that they are to take (1: 128 x 128 everywhere, 2: 256 x 128 in the last product)
+SHAPES = [((40, 512, 520), 1), ((30, 520, 600), 1), ((30, 600, 514), 1), ((30, 514, 514), 1), ((36, 512, 1024), 2), ((40, 1300, 520), 2), ((44, 700, 1100), 2), ((300, 130, 515), 2), ((11, 1537, 1026), 2),
+          # 256 does not divide the padded columns: S and B have more rows than X has columns
+          ((24, 769, 769), 2), ((16, 1100, 1100), 2), ((8, 1300, 1400), 2), ((60, 600, 640), 2), ((2, 2600, 2600), 1), ((3, 2600, 2600), 2), ((1, 3900, 3900), 2)]
+MODELS = [(dict(D=260, H=512, L=4, P=256, V=300), 0), (dict(D=260, H=512, L=4, P=256, V=300), 3), (dict(D=300, H=500, L=4, P=201, V=300), 1), (dict(D=515, H=513, L=4, P=600, V=600), 5),
+          (dict(D=260, H=600, L=3, P=0, V=40), 2)]
+
+
+def test_the_cases_take_the_tiles_that_they_are_for(plans):  # noqa: F811
+    got = plans(f"""
+        out = [[plans(orthogonalize(*s, 1)[0])[0][3]["tile"] for s, _ in {SHAPES!r}]]
+        for dims, flags in {MODELS!r}:
+            p = plans(model(flags, dims["D"], dims["H"], dims["L"], dims["P"], dims["V"], 1)[0])[0][3]
+            out.append([p["tile"], p["exact"]])
+    """)
+    assert got[0] == [tile for _, tile in SHAPES] and got[1:] == [[2, 0]] * len(MODELS)
+
+
+def gradient(g, count, rows, cols):
+    """A few directions that are common, and noise; rows of unequal size."""
+    import torch
+    normal = lambda *shape: torch.randn(shape, device="cuda:0", generator=g)  # noqa: E731
+    return 1e-3 * torch.exp(0.5 * normal(count, rows, 1)) * (normal(count, rows, 4) @ normal(count, 4, cols) + normal(count, rows, cols))
+
+
+def orthogonalized(G):
+    """oracle.muon.orthogonalize in torch's doubles (the larger matrices take minutes in numpy)."""
+    X = G.double() / G.double().norm()
+    for _ in range(muon.STEPS):
+        if X.shape[0] <= X.shape[1]:
+            S = X @ X.t()
+            X = muon.A * X + (muon.B * S + muon.C * (S @ S)) @ X
+        else:
+            S = X.t() @ X
+            X = muon.A * X + X @ (muon.B * S + muon.C * (S @ S))
+    return X
+
+
+@pytest.mark.gpu
+def test_the_definition_in_doubles_is_the_oracles():
+    import torch
+    for shape in ((70, 90), (90, 70)):
+        G = gradient(torch.Generator(device="cuda:0").manual_seed(1), 1, *shape)[0]
+        assert np.abs(orthogonalized(G).cpu().numpy() - muon.orthogonalize(G.cpu().numpy())).max() < 1e-12
+
+
+def guarded(n):
+    import torch
+    t = torch.full((n + 4096,), 0x7F, dtype=torch.uint8, device="cuda:0")
+    return t, lambda: bool((t[n:] == 0x7F).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [s for s, _ in SHAPES], ids=str)
+def test_matrices(shape):
+    # from weights of zero at a rate of one the new weights are -sqrt(max(1, R / C)) O, in float
+    import torch
+    from paper_1904_04956_amd import binding as bl
+    G = gradient(torch.Generator(device="cuda:0").manual_seed(sum(shape)), *shape)
+    n = bl.muon_orthogonalize_scratch_bytes(*shape, 1)
+    scratch, kept = guarded(n)
+    theta, shadow = torch.zeros(shape, device="cuda:0"), torch.full(shape, 7.0, dtype=torch.bfloat16, device="cuda:0")
+    bl.muon_matrices_step(theta, shadow, G, None, *shape, 1, 1.0, 0.0, 0.0, 0, scratch, n)
+    assert kept() and torch.equal(shadow, theta.bfloat16())
+    for k in sorted({0, shape[0] // 2, shape[0] - 1}):
+        want = -np.sqrt(max(1.0, shape[1] / shape[2])) * orthogonalized(G[k])
+        off = float((theta[k].double() - want).norm() / want.norm())
+        assert off < E1, (k, off)
+    X = torch.empty(shape, dtype=torch.bfloat16, device="cuda:0")
+    bl.muon_orthogonalize(G, X, *shape, 1, scratch, n)
+    assert kept()
+    # (the same products in the same order: a rounding to bf16 away, and one to float where the factor is no power of two)
+    one = -theta / np.float32(np.sqrt(max(1.0, shape[1] / shape[2])))
+    assert float((X.float() - one).abs().max()) <= float(one.abs().max()) * (2.0 ** -8 + 2.0 ** -22)
+    again = torch.zeros_like(theta)
+    scratch.fill_(0x7F)
+    bl.muon_matrices_step(again, None, G, None, *shape, 1, 1.0, 0.0, 0.0, 0, scratch, n)
+    assert torch.equal(again, theta)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dims,flags", MODELS, ids=str)
+def test_models(dims, flags):
+    import torch
+    from paper_1904_04956_amd import binding as bl
+    dm = orc.Dims(T=1, B=1, **dims)
+    layout, n, g = orc.layout(dm), orc.param_count(dm), torch.Generator(device="cuda:0").manual_seed(dims["H"] + flags)
+    theta = torch.empty(n, device="cuda:0").uniform_(-0.1, 0.1, generator=g)
+    grad, velocity = torch.empty_like(theta), torch.empty_like(theta)
+    for _, at, shape in layout:
+        two = shape if len(shape) == 2 else (shape[0], 1)
+        for of, times in ((grad, 1.0), (velocity, 4.0)):
+            of[at:at + two[0] * two[1]] = times * gradient(g, 1, *two).reshape(-1)
+    lr, rest, mu, decay, nesterov = 0.02, 0.1, 0.9, 0.1, bool(flags & 1)
+    v = mu * velocity.double() + grad.double()
+    d = grad.double() + mu * v if nesterov else v
+    ctx = bl.blstm_create(1, 1, *(dims[k] for k in ("D", "H", "L", "P", "V")), 1)
+    try:
+        new, new_v, shadow = theta.clone(), velocity.clone(), torch.empty(n, dtype=torch.bfloat16, device="cuda:0")
+        nbytes = bl.muon_scratch_bytes(ctx, flags)
+        scratch, kept = guarded(nbytes)
+        bl.muon_step(ctx, new, shadow, grad, new_v, lr, rest, mu, decay, flags, scratch, nbytes)
+        assert kept() and torch.equal(shadow, new.bfloat16())
+        assert float((new_v.double() - v).abs().max()) <= 2.0 ** -23 * float(v.abs().max())
+        again, again_v = theta.clone(), velocity.clone()
+        scratch.fill_(0x7F)
+        bl.muon_step(ctx, again, None, grad, again_v, lr, rest, mu, decay, flags, scratch, nbytes)
+        assert torch.equal(again, new) and torch.equal(again_v, new_v)
+    finally:
+        bl.blstm_destroy(ctx)
+    left = torch.ones(n, dtype=torch.bool, device="cuda:0")
+    for at, rows, cols in muon.matrices(layout, bool(flags & 2), bool(flags & 4)):
+        part = slice(at, at + rows * cols)
+        left[part] = False
+        step = lr * np.sqrt(max(1.0, rows / cols)) * orthogonalized(d[part].view(rows, cols)).reshape(-1)
+        want = (1 - lr * decay) * theta[part].double() - step
+        # beside O's error three roundings in float of the weights
+        off = float((new[part].double() - want).norm())
+        assert off < E1 * float(step.norm()) + 3 * 2.0 ** -24 * float(want.norm()), (at, rows, cols)
+    want = theta.double() - rest * d
+    assert float((new.double() - want)[left].abs().max()) <= 2.0 ** -22 * float(want[left].abs().max())
