@@ -226,9 +226,6 @@ class Learner:
             self.adapters.close()
             self.adapters = None
         self.adapters = Adapters(self, count, rank, scale)
-        # the passes run on the stack's own context below, so nothing of the softmax layer's gradient may be left to this one's backward pass
-        bl.blstm_set_option(self.ctx, bl.BLSTM_OPT_DEFER_SOFTMAX_WGRAD, 0)
-        self.defer_softmax_wgrad = False
         return self.adapters
 
     def _attached(self):
@@ -246,7 +243,12 @@ class Learner:
         """calgrad() with the adapters: their gradients in adapters.dA and .dB and, with `shared`, the model's in grad (without: the softmax layer's alone)."""
         a = self._attached()
         self.forward_adapted(stream)
-        bl.softmax_xent_fwd_bwd(self.ctx, self.theta_fwd, self.z, self.labels, self.loss, self.dz, self.grad, stream)
+        # the backward pass runs on the stack's own context, so nothing of the softmax layer's gradient may be left to this one's
+        bl.blstm_set_option(self.ctx, bl.BLSTM_OPT_DEFER_SOFTMAX_WGRAD, 0)
+        try:
+            bl.softmax_xent_fwd_bwd(self.ctx, self.theta_fwd, self.z, self.labels, self.loss, self.dz, self.grad, stream)
+        finally:
+            bl.blstm_set_option(self.ctx, bl.BLSTM_OPT_DEFER_SOFTMAX_WGRAD, int(self.defer_softmax_wgrad))
         bl.adapter_backward(a.cfg, a.W, a.A_fwd, a.Bm_fwd, a.ids, a.h, a.t, self.dz, a.dh if shared else None, a.dA, a.dB, a.dW if shared else None,
                             a.db if shared else None, a.scratch(bl.ADAPTER_BACKWARD, self, stream), None, stream)
         if shared:
