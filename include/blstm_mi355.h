@@ -191,11 +191,17 @@ int sgd_step(float* theta_master, void* theta_bf16_or_null, const float* grad, s
 size_t muon_orthogonalize_scratch_bytes(int count, int rows, int cols, int mode);      /* 0 and an error text for sizes it does not take */
 int muon_orthogonalize(const float* G, void* X, int count, int rows, int cols, int mode, void* scratch, size_t scratch_bytes, void* stream);
 
-/* The update of `count` matrices [rows][cols] (a low-rank adapter's factors, say): v <- momentum * v + grad; d = v, or grad + momentum * v;
+/* The update of `count` matrices [rows][cols]: v <- momentum * v + grad; d = v, or grad + momentum * v;
    theta <- (1 - lr * weight_decay) * theta - lr * sqrt(max(1, rows / cols)) * O(d).  theta_bf16 and velocity as in sgd_step (momentum 0: velocity is not read
    or written and may be NULL).  0 <= momentum < 1, weight_decay >= 0, flags 0 or MUON_NESTEROV.  Scratch: muon_orthogonalize_scratch_bytes. */
 int muon_matrices_step(float* theta_master, void* theta_bf16_or_null, const float* grad, float* velocity_or_null, int count, int rows, int cols, int mode,
                        float lr, float momentum, float weight_decay, int flags, void* scratch, size_t scratch_bytes, void* stream);
+
+/* The same of the adapters that a batch has (grad: adapter_backward's dA or dB): matrix k takes its step where ids [n_ids] on the device, the adapter_config's, hold k.  The others, to
+   whom the batch says nothing, stay as they are, their velocities too: O(d) has no size, so that a velocity without new gradients would move them by whole steps, again and again.
+   count is at most BLSTM_MAX_ADAPTERS. */
+int muon_adapters_step(float* theta_master, void* theta_bf16_or_null, const float* grad, float* velocity_or_null, const int32_t* ids, int n_ids, int count, int rows, int cols,
+                       int mode, float lr, float momentum, float weight_decay, int flags, void* scratch, size_t scratch_bytes, void* stream);
 
 /* The update of a model's whole vector in ctx's layout and mode (no workspace needs to be bound): W_x, U_h and W_p, with MUON_SOFTMAX W_s, as in muon_matrices_step;
    the biases, else W_s too: theta <- theta - lr_rest * d. */

@@ -30,7 +30,7 @@ EXPORTS = [
     "blstm_create", "blstm_destroy", "blstm_param_count", "blstm_workspace_bytes", "blstm_param_offset",
     "blstm_bind", "blstm_forward", "softmax_xent_fwd_bwd", "softmax_xent_fwd_bwd_noalloc",
     "softmax_scratch_bytes", "softmax_logprob", "softmax_topk", "softmax_distill_fwd_bwd", "softmax_policy_fwd_bwd", "blstm_backward", "sgd_step", "adpsgd_mix",
-    "muon_orthogonalize_scratch_bytes", "muon_orthogonalize", "muon_matrices_step", "muon_scratch_bytes", "muon_step",
+    "muon_orthogonalize_scratch_bytes", "muon_orthogonalize", "muon_matrices_step", "muon_adapters_step", "muon_scratch_bytes", "muon_step",
     "adapter_scratch_bytes", "adapter_forward", "adapter_backward",
     "sgd_mix_pair", "sync_average", "blstm_lr_schedule",
     "adpsgd_ring_partner", "blstm_shadow_refresh", "blstm_set_option", "blstm_weights_changed", "blstm_device_status", "blstm_profile_enable", "blstm_profile_read",
@@ -102,6 +102,8 @@ def lib():
     L.muon_orthogonalize.restype = c_int
     L.muon_matrices_step.argtypes = [c_void_p] * 4 + [c_int] * 4 + [c_float] * 3 + [c_int, c_void_p, c_size_t, c_void_p]
     L.muon_matrices_step.restype = c_int
+    L.muon_adapters_step.argtypes = [c_void_p] * 5 + [c_int] * 5 + [c_float] * 3 + [c_int, c_void_p, c_size_t, c_void_p]
+    L.muon_adapters_step.restype = c_int
     L.muon_scratch_bytes.argtypes = [c_void_p, c_int]
     L.muon_scratch_bytes.restype = c_size_t
     L.muon_step.argtypes = [c_void_p] * 5 + [c_float] * 4 + [c_int, c_void_p, c_size_t, c_void_p]
@@ -284,6 +286,12 @@ def muon_orthogonalize(G, X, count, rows, cols, mode, scratch, scratch_bytes=Non
 def muon_matrices_step(theta_master, theta_bf16_or_null, grad, velocity_or_null, count, rows, cols, mode, lr, momentum, weight_decay, flags, scratch,
                        scratch_bytes=None, stream=None):
     return _check(lib().muon_matrices_step(_ptr(theta_master), _ptr(theta_bf16_or_null), _ptr(grad), _ptr(velocity_or_null), count, rows, cols, mode,
+                                           lr, momentum, weight_decay, flags, *_scratch(scratch, scratch_bytes), _stream(stream)))
+
+
+def muon_adapters_step(theta_master, theta_bf16_or_null, grad, velocity_or_null, ids, n_ids, count, rows, cols, mode, lr, momentum, weight_decay, flags, scratch,
+                       scratch_bytes=None, stream=None):
+    return _check(lib().muon_adapters_step(_ptr(theta_master), _ptr(theta_bf16_or_null), _ptr(grad), _ptr(velocity_or_null), _ptr(ids), n_ids, count, rows, cols, mode,
                                            lr, momentum, weight_decay, flags, *_scratch(scratch, scratch_bytes), _stream(stream)))
 
 

@@ -826,6 +826,16 @@ int muon_check(const char* name, const MuonArgs& a, int flags, int known, const 
     return BLSTM_OK;
 }
 
+int muon_matrices(const char* name, float* theta, void* shadow, const float* grad, float* velocity, const int32_t* ids, int n_ids, int count, int rows, int cols, int mode,
+                  float lr, float momentum, float weight_decay, int flags, void* scratch, size_t scratch_bytes, void* stream) {
+    MuonPlan p;
+    int rc = muon_matrices_plan(name, count, rows, cols, mode, &p);
+    if (rc != BLSTM_OK) return rc;
+    const MuonArgs a{theta, static_cast<unsigned short*>(shadow), grad, momentum != 0.0f ? velocity : nullptr, nullptr, 0, lr, 0.0f, momentum, weight_decay, (flags & MUON_NESTEROV) != 0};
+    rc = muon_check(name, a, flags, MUON_NESTEROV, p, scratch, scratch_bytes);
+    return rc != BLSTM_OK ? rc : check_hip(launch_muon(p, a, MuonIds{ids, n_ids}, scratch, static_cast<hipStream_t>(stream)), name);
+}
+
 // ---- low-rank adapters beside a projection ---------------------------------------------------------------------------
 // Where a call's scratch lies (byte offsets).
 struct AdapterScratch {
@@ -1585,7 +1595,7 @@ int muon_step(const blstm_ctx* ctx, float* theta, void* shadow, const float* gra
     if (!muon_model_plan(ctx, flags, &p)) return fail(BLSTM_ERR_DIM, "muon_step: too many elements");
     const MuonArgs a{theta, static_cast<unsigned short*>(shadow), grad, momentum != 0.0f ? velocity : nullptr, nullptr, 0, lr, lr_rest, momentum, weight_decay, (flags & MUON_NESTEROV) != 0};
     const int rc = muon_check("muon_step", a, flags, MUON_NESTEROV | MUON_GATES | MUON_SOFTMAX, p, scratch, scratch_bytes);
-    return rc != BLSTM_OK ? rc : check_hip(launch_muon(p, a, scratch, static_cast<hipStream_t>(stream)), "muon_step");
+    return rc != BLSTM_OK ? rc : check_hip(launch_muon(p, a, MuonIds{}, scratch, static_cast<hipStream_t>(stream)), "muon_step");
 }
 
 size_t muon_orthogonalize_scratch_bytes(int count, int rows, int cols, int mode) {
@@ -1602,17 +1612,20 @@ int muon_orthogonalize(const float* G, void* X, int count, int rows, int cols, i
     if (scratch_bytes < p.bytes) return fail(BLSTM_ERR_WORKSPACE, "muon_orthogonalize: %zu bytes of scratch given, %zu needed", scratch_bytes, p.bytes);
     MuonArgs a{};
     a.grad = G; a.out = X; a.out_bf16 = mode;
-    return check_hip(launch_muon(p, a, scratch, static_cast<hipStream_t>(stream)), "muon_orthogonalize");
+    return check_hip(launch_muon(p, a, MuonIds{}, scratch, static_cast<hipStream_t>(stream)), "muon_orthogonalize");
 }
 
 int muon_matrices_step(float* theta, void* shadow, const float* grad, float* velocity, int count, int rows, int cols, int mode, float lr, float momentum,
                        float weight_decay, int flags, void* scratch, size_t scratch_bytes, void* stream) {
-    MuonPlan p;
-    int rc = muon_matrices_plan("muon_matrices_step", count, rows, cols, mode, &p);
-    if (rc != BLSTM_OK) return rc;
-    const MuonArgs a{theta, static_cast<unsigned short*>(shadow), grad, momentum != 0.0f ? velocity : nullptr, nullptr, 0, lr, 0.0f, momentum, weight_decay, (flags & MUON_NESTEROV) != 0};
-    rc = muon_check("muon_matrices_step", a, flags, MUON_NESTEROV, p, scratch, scratch_bytes);
-    return rc != BLSTM_OK ? rc : check_hip(launch_muon(p, a, scratch, static_cast<hipStream_t>(stream)), "muon_matrices_step");
+    return muon_matrices("muon_matrices_step", theta, shadow, grad, velocity, nullptr, 0, count, rows, cols, mode, lr, momentum, weight_decay, flags, scratch, scratch_bytes, stream);
+}
+
+int muon_adapters_step(float* theta, void* shadow, const float* grad, float* velocity, const int32_t* ids, int n_ids, int count, int rows, int cols, int mode, float lr,
+                       float momentum, float weight_decay, int flags, void* scratch, size_t scratch_bytes, void* stream) {
+    if (n_ids < 1 || count > BLSTM_MAX_ADAPTERS) return fail(BLSTM_ERR_DIM, "muon_adapters_step: n_ids must be positive, count at most %d", BLSTM_MAX_ADAPTERS);
+    if (!ids) return fail(BLSTM_ERR_NULL, "muon_adapters_step: null argument");
+    if (reinterpret_cast<uintptr_t>(ids) & 3) return fail(BLSTM_ERR_ALIGN, "muon_adapters_step: ids are not aligned to their elements");
+    return muon_matrices("muon_adapters_step", theta, shadow, grad, velocity, ids, n_ids, count, rows, cols, mode, lr, momentum, weight_decay, flags, scratch, scratch_bytes, stream);
 }
 
 size_t adapter_scratch_bytes(const adapter_config* cfg, int call) {

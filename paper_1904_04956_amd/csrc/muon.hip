@@ -56,6 +56,13 @@ __device__ __forceinline__ const char* uniform(const void* p) {
 }
 __device__ __forceinline__ long long tensor_at(const MuonGroup& g, int k) { return g.at + (long long)(k / g.inner_count) * g.outer + (long long)(k % g.inner_count) * g.inner; }
 
+// Whether matrix k takes part.  (Ids are a batch's: some thousand at most.  The first launch looks through them and leaves the answer for the others.)
+__device__ __forceinline__ bool in_ids(const MuonIds& of, int k) {
+    int found = 0;
+    for (int i = threadIdx.x; i < of.n; i += blockDim.x) found |= of.ids[i] == k;
+    return __syncthreads_or(found) != 0;
+}
+
 // ---- v <- momentum v + g, the squares' sums, and the whole update of what is not orthogonalised ----------------------
 // 12 bytes an element of a matrix, 20 (22 with the bf16 copy) of the others.
 __device__ __forceinline__ double block_sum(double v, double* lds) {
@@ -64,11 +71,16 @@ __device__ __forceinline__ double block_sum(double v, double* lds) {
     __syncthreads();
     return lds[0] + lds[1] + lds[2] + lds[3];
 }
-__global__ __launch_bounds__(256) void muon_momentum_kernel(MuonPlan p, MuonArgs a, double* sums) {
+__global__ __launch_bounds__(256) void muon_momentum_kernel(MuonPlan p, MuonArgs a, double* sums, MuonIds of, int* here) {
     __shared__ double lds[4];
     const int group = group_of(p.at.chunk, blockIdx.x);
     const MuonGroup& g = p.g[group];
     const int local = blockIdx.x - p.at.chunk[group], k = local / g.chunks, c = local % g.chunks;
+    if (of.ids) {
+        const bool in = in_ids(of, k);
+        if (c == 0 && threadIdx.x == 0) here[k] = in;
+        if (!in) return;
+    }
     const long long size = (long long)g.rows * g.cols, e0 = (long long)c * FLAT, at = tensor_at(g, k) + e0;
     const int len = (int)min((long long)FLAT, size - e0);
     const float* grad = a.grad + at;
@@ -431,7 +443,7 @@ __device__ __forceinline__ void upper(int t, int* row, int* col) {
 
 // SPLIT: the operands' second halves are multiplied too; LO: S and B have second halves; LOW: X's second part is held in eight bits
 template <int TM, int TN, bool SPLIT, bool LO, bool LOW, int PH, int NST, int SETS>
-__global__ __launch_bounds__(256 * SETS, SPLIT && TM == 2 && NST > 1 ? 1 : 2) void ns_product_kernel(MuonPlan p, MuonArgs a, _Float16* ws, float* diag, float* part, int from) {
+__global__ __launch_bounds__(256 * SETS, SPLIT && TM == 2 && NST > 1 ? 1 : 2) void ns_product_kernel(MuonPlan p, MuonArgs a, _Float16* ws, float* diag, float* part, int from, const int* here) {
     extern __shared__ uint4 smem[];
     constexpr int BM = 64 * TM, BN = 64 * TN;
     // ids go round-robin to the eight XCDs: of each group (they differ in the length of their contractions) each XCD takes an eighth, neighbouring tiles
@@ -441,6 +453,8 @@ __global__ __launch_bounds__(256 * SETS, SPLIT && TM == 2 && NST > 1 ? 1 : 2) vo
     const int units = g.count * (PH == PH_GRAM ? g.grams * g.splits : PH == PH_SQUARE ? g.grams : g.applies), own = blockIdx.x - starts[group];
     const int lin = (own & 7) * ((units + 7) / 8) + (own >> 3);
     if (lin >= units) return;
+    // (matrices that take no part are multiplied all the same: asked in every launch, the question costs the calls without ids 1 %)
+    if (PH == PH_LAST && here && !here[lin / g.applies]) return;
     f32x16_t acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
@@ -684,7 +698,7 @@ __device__ __forceinline__ void put_four(_Float16* at, int plane, const f32x4_t&
     *reinterpret_cast<f16x4_t*>(at + plane) = l;
 }
 template <int MB>
-__global__ __launch_bounds__(SMALL_THREADS) void muon_small_kernel(MuonPlan p, MuonArgs a) {
+__global__ __launch_bounds__(SMALL_THREADS) void muon_small_kernel(MuonPlan p, MuonArgs a, MuonIds of) {
     extern __shared__ uint4 smem[];
     __shared__ double lds_sum[16];
     constexpr int MP = 16 * MB, TILES = MB * MB, PARTS = small_parts(MB), KS = (MP + 31) / 32, PLACES = MB <= 2 ? 2 : 1;
@@ -707,6 +721,7 @@ __global__ __launch_bounds__(SMALL_THREADS) void muon_small_kernel(MuonPlan p, M
         }
         return;
     }
+    if (of.ids && !in_ids(of, local)) return;
     const long long at = tensor_at(g, local);
     const int size = g.rows * g.cols, n = max(g.rows, g.cols);
     const bool tall = g.tall != 0;
@@ -905,20 +920,20 @@ constexpr int lds_bytes(int TM, int TN, bool split, int nst, int sets) {
     return loop > values ? loop : values;
 }
 template <int TM, int TN, bool SPLIT, bool LO, bool LOW, int PH, int NST, int SETS>
-void run_product(int n, const MuonPlan& p, const MuonArgs& a, _Float16* ws, float* diag, float* part, int from, hipStream_t st) {
-    ns_product_kernel<TM, TN, SPLIT, LO, LOW, PH, NST, SETS><<<n, 256 * SETS, lds_bytes(TM, TN, SPLIT, NST, SETS), st>>>(p, a, ws, diag, part, from);
+void run_product(int n, const MuonPlan& p, const MuonArgs& a, _Float16* ws, float* diag, float* part, const int* here, int from, hipStream_t st) {
+    ns_product_kernel<TM, TN, SPLIT, LO, LOW, PH, NST, SETS><<<n, 256 * SETS, lds_bytes(TM, TN, SPLIT, NST, SETS), st>>>(p, a, ws, diag, part, from, here);
 }
 
 // T: edge of the Gram and square tiles; AM, AN: of the last product's
 template <int T, int AM, int AN, bool FINE, bool SPLIT, int SN, int AN_ST, int SETS = 1>
-hipError_t run_products(const MuonPlan& p, const MuonArgs& a, _Float16* ws, float* diag, float* part, hipStream_t st) {
+hipError_t run_products(const MuonPlan& p, const MuonArgs& a, _Float16* ws, float* diag, float* part, const int* here, hipStream_t st) {
     for (int i = 0; i < NS_STEPS; ++i) {
         const int from = i & 1;
-        run_product<T, T, FINE, SPLIT, !FINE, PH_GRAM, SN, SETS>(p.grams, p, a, ws, diag, part, from, st);
+        run_product<T, T, FINE, SPLIT, !FINE, PH_GRAM, SN, SETS>(p.grams, p, a, ws, diag, part, here, from, st);
         if (p.sums) ns_gram_sum_kernel<T, SPLIT><<<p.sums, 256, 0, st>>>(p, ws, diag, part);
-        run_product<T, T, SPLIT, SPLIT, !FINE, PH_SQUARE, SN, SETS>(p.squares, p, a, ws, diag, part, from, st);
-        if (i + 1 < NS_STEPS) run_product<AM, AN, SPLIT, SPLIT, !FINE, PH_APPLY, AN_ST, 1>(p.applies, p, a, ws, diag, part, from, st);
-        else run_product<AM, AN, SPLIT, SPLIT, !FINE, PH_LAST, AN_ST, 1>(p.applies, p, a, ws, diag, part, from, st);
+        run_product<T, T, SPLIT, SPLIT, !FINE, PH_SQUARE, SN, SETS>(p.squares, p, a, ws, diag, part, here, from, st);
+        if (i + 1 < NS_STEPS) run_product<AM, AN, SPLIT, SPLIT, !FINE, PH_APPLY, AN_ST, 1>(p.applies, p, a, ws, diag, part, here, from, st);
+        else run_product<AM, AN, SPLIT, SPLIT, !FINE, PH_LAST, AN_ST, 1>(p.applies, p, a, ws, diag, part, here, from, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -1030,24 +1045,26 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
     p.sums_at = to256((size_t)halves * 2);
     p.diag_at = p.sums_at + to256((size_t)chunks * 8);
     p.part_at = p.diag_at + to256((size_t)diags * 4);
-    p.bytes = p.part_at + to256((size_t)floats * 4) + 256;
+    p.here_at = p.part_at + to256((size_t)floats * 4);
+    p.bytes = p.here_at + to256(n == 1 ? (size_t)p.g[0].count * 4 : 0) + 256;
     *out = p;
     return true;
 }
 
-hipError_t launch_muon(const MuonPlan& p, const MuonArgs& a, void* scratch, hipStream_t st) {
+hipError_t launch_muon(const MuonPlan& p, const MuonArgs& a, const MuonIds& ids, void* scratch, hipStream_t st) {
     if (p.tile == 3) {
-        if (p.small == 1) muon_small_kernel<1><<<p.applies, SMALL_THREADS, p.lds, st>>>(p, a);
-        else if (p.small == 2) muon_small_kernel<2><<<p.applies, SMALL_THREADS, p.lds, st>>>(p, a);
-        else if (p.small == 3) muon_small_kernel<3><<<p.applies, SMALL_THREADS, p.lds, st>>>(p, a);
-        else muon_small_kernel<4><<<p.applies, SMALL_THREADS, p.lds, st>>>(p, a);
+        if (p.small == 1) muon_small_kernel<1><<<p.applies, SMALL_THREADS, p.lds, st>>>(p, a, ids);
+        else if (p.small == 2) muon_small_kernel<2><<<p.applies, SMALL_THREADS, p.lds, st>>>(p, a, ids);
+        else if (p.small == 3) muon_small_kernel<3><<<p.applies, SMALL_THREADS, p.lds, st>>>(p, a, ids);
+        else muon_small_kernel<4><<<p.applies, SMALL_THREADS, p.lds, st>>>(p, a, ids);
         return hipGetLastError();
     }
     _Float16* ws = static_cast<_Float16*>(scratch);
     double* sums = reinterpret_cast<double*>(static_cast<char*>(scratch) + p.sums_at);
     float* diag = reinterpret_cast<float*>(static_cast<char*>(scratch) + p.diag_at);
     float* part = reinterpret_cast<float*>(static_cast<char*>(scratch) + p.part_at);
-    muon_momentum_kernel<<<p.chunks, 256, 0, st>>>(p, a, sums);
+    int* here = ids.ids ? reinterpret_cast<int*>(static_cast<char*>(scratch) + p.here_at) : nullptr;
+    muon_momentum_kernel<<<p.chunks, 256, 0, st>>>(p, a, sums, ids, here);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.casts == 0) return e;
     // (second halves that are multiplied, in S at least, are halves)
@@ -1055,13 +1072,13 @@ hipError_t launch_muon(const MuonPlan& p, const MuonArgs& a, void* scratch, hipS
     else muon_cast_kernel<true><<<p.casts, 256, 0, st>>>(p, a, sums, ws);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (p.tile == 2) return run_products<2, 4, 2, false, false, 2, 1>(p, a, ws, diag, part, st);
+    if (p.tile == 2) return run_products<2, 4, 2, false, false, 2, 1>(p, a, ws, diag, part, here, st);
     // (both planes' fragments of a slab fit the registers too: one buffer where workgroups share CUs, 865 -> 782 us a step of two layers of 512 cells in float, 289 -> 271 for two
     // of 301 with gates apart; two buffers where they have a CU each: with one set of wavefronts 210 us against 222 for two matrices of 1204 x 602)
-    if (p.tile == 0 && p.exact && !p.lone && p.applies >= 512) return run_products<1, 1, 1, true, true, 1, 1>(p, a, ws, diag, part, st);
-    if (p.tile == 1) return p.exact ? run_products<2, 2, 2, true, true, 1, 1>(p, a, ws, diag, part, st) : run_products<2, 2, 2, false, false, 2, 2>(p, a, ws, diag, part, st);
-    if (p.lone) return p.exact ? run_products<1, 1, 1, true, true, 2, 2, 2>(p, a, ws, diag, part, st) : run_products<1, 1, 1, true, false, 2, 2, 2>(p, a, ws, diag, part, st);
-    return p.exact ? run_products<1, 1, 1, true, true, 2, 2>(p, a, ws, diag, part, st) : run_products<1, 1, 1, true, false, 2, 2>(p, a, ws, diag, part, st);
+    if (p.tile == 0 && p.exact && !p.lone && p.applies >= 512) return run_products<1, 1, 1, true, true, 1, 1>(p, a, ws, diag, part, here, st);
+    if (p.tile == 1) return p.exact ? run_products<2, 2, 2, true, true, 1, 1>(p, a, ws, diag, part, here, st) : run_products<2, 2, 2, false, false, 2, 2>(p, a, ws, diag, part, here, st);
+    if (p.lone) return p.exact ? run_products<1, 1, 1, true, true, 2, 2, 2>(p, a, ws, diag, part, here, st) : run_products<1, 1, 1, true, false, 2, 2, 2>(p, a, ws, diag, part, here, st);
+    return p.exact ? run_products<1, 1, 1, true, true, 2, 2>(p, a, ws, diag, part, here, st) : run_products<1, 1, 1, true, false, 2, 2>(p, a, ws, diag, part, here, st);
 }
 
 }  // namespace blstm

@@ -31,9 +31,9 @@ struct MuonPlan {
                               // 3: a matrix a workgroup, all in LDS (small: blocks of 16 rows of the largest Gram matrix, lds: bytes)
     int small, lds;
     int lone;                 // no more tiles of S than CUs: two sets of wavefronts a tile
-    int exact;                // products of both planes (mode 0)
+    int exact;                // products of both planes
     int chunks, casts, grams, squares, applies, sums;
-    size_t sums_at, diag_at, part_at, bytes;   // byte offsets in scratch: squares' sums (double), diagonals, partial Gram tiles (float)
+    size_t sums_at, diag_at, part_at, here_at, bytes;   // byte offsets in scratch: squares' sums (double), diagonals, partial Gram tiles (float), whether a matrix is in ids (int)
 };
 struct MuonArgs {
     float* theta; unsigned short* shadow;      // null: the update itself goes to out
@@ -41,8 +41,9 @@ struct MuonArgs {
     void* out; int out_bf16;
     float lr, lr_rest, momentum, decay; int nesterov;
 };
+struct MuonIds { const int* ids; int n; };     // ids not null: of the call's only group, the matrices that ids holds; the others stay as they are
 // False: sizes beyond what the kernels index.  g[].at .. ortho are given.
 bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out);
-hipError_t launch_muon(const MuonPlan& p, const MuonArgs& a, void* scratch, hipStream_t st);
+hipError_t launch_muon(const MuonPlan& p, const MuonArgs& a, const MuonIds& ids, void* scratch, hipStream_t st);
 
 }  // namespace blstm

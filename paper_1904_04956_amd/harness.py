@@ -242,6 +242,7 @@ class Learner:
     def calgrad_adapted(self, shared=True, stream=None):
         """calgrad() with the adapters: their gradients in adapters.dA and .dB and, with `shared`, the model's in grad (without: the softmax layer's alone)."""
         a = self._attached()
+        a.take_ids(stream)
         self.forward_adapted(stream)
         # the backward pass runs on the stack's own context, so nothing of the softmax layer's gradient may be left to this one's
         bl.blstm_set_option(self.ctx, bl.BLSTM_OPT_DEFER_SOFTMAX_WGRAD, 0)
@@ -255,11 +256,11 @@ class Learner:
             bl.blstm_backward(a.stack, self.theta_fwd, self.x, a.dh, self.grad, stream)
 
     def apply_adapters(self, lr, momentum=0.95, weight_decay=0.0, nesterov=True, stream=None):
-        """The orthogonalised update of every adapter's two factors (binding.muon_matrices_step)."""
+        """The orthogonalised update of both factors of the adapters that the batch of the last calgrad_adapted had (binding.muon_adapters_step)."""
         a = self._attached()
         for name, theta, shadow, grad, velocity in (("A", a.A, a.A_bf16, a.dA, a.vA), ("B", a.Bm, a.Bm_bf16, a.dB, a.vB)):
             sizes = (*theta.shape, self.mode)
-            bl.muon_matrices_step(theta, shadow, grad, velocity, *sizes, lr, momentum, weight_decay, bl.MUON_NESTEROV if nesterov else 0,
+            bl.muon_adapters_step(theta, shadow, grad, velocity, a.ids_taken, a.ids_taken.numel(), *sizes, lr, momentum, weight_decay, bl.MUON_NESTEROV if nesterov else 0,
                                   self._kept(("muon", name, sizes), lambda: bl.muon_orthogonalize_scratch_bytes(*sizes), stream), None, stream)
 
     def hold(self):
@@ -311,7 +312,7 @@ class Adapters:
         real = lambda *shape: torch.zeros(shape, dtype=torch.float32, device=dev)  # noqa: E731
         self.A, self.Bm, self.dA, self.dB, self.vA, self.vB = (real(count, *s) for s in 3 * ((rank, K), (N, rank)))
         self.A_bf16, self.Bm_bf16 = (torch.zeros_like(t, dtype=torch.bfloat16) if learner.mode == 1 else None for t in (self.A, self.Bm))
-        self.ids = torch.full((B,), bl.BLSTM_NO_ADAPTER, dtype=torch.int32, device=dev)
+        self.ids, self.ids_taken = (torch.full((B,), bl.BLSTM_NO_ADAPTER, dtype=torch.int32, device=dev) for _ in range(2))
         self.h, self.dh = (torch.zeros((T, B, K), dtype=kind, device=dev) for _ in range(2))
         self.t = real(T, B, rank)
         part = lambda flat, which: flat[slice(*(lambda o, n: (o, o + n))(*bl.blstm_param_offset(learner.ctx, 0, 0, which)))]  # noqa: E731
@@ -328,6 +329,13 @@ class Adapters:
 
     def scratch(self, call, learner, stream):
         return learner._kept(("adapt", call, self.cfg.rank, self.cfg.count), lambda: bl.adapter_scratch_bytes(self.cfg, call), stream)
+
+    def take_ids(self, stream=None):
+        """Keeps whose gradients dA and dB are: ids may be the next batch's when the update comes."""
+        if stream is not None and not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream), device=self.ids.device)
+        with torch.cuda.stream(stream):
+            torch.add(self.ids, 0, out=self.ids_taken)               # (a kernel: a captured copy would be a node of another kind)
 
     def refresh(self, stream=None):
         """After writing A or Bm: their bf16 copies anew."""

@@ -35,3 +35,37 @@ def test_plain_calls_leave_the_softmax_layers_gradient_to_the_backward_pass_as_b
     finally:
         plain.close()
         other.close()
+
+
+@pytest.mark.parametrize("mode", [0, 1])
+def test_speakers_who_were_not_in_the_batch_stay_as_they_are(mode):
+    import torch
+    from oracle import muon
+    lrn, a, *_ = adapted(mode, 92, count=5, ids=[0, 1, -1, 2, 0, 1, 4, 4, 2])
+    wide = lambda t: t.double().cpu().numpy()  # noqa: E731
+    try:
+        E = 16 * 2.0 ** -22
+        vA, vB = wide(a.vA), wide(a.vB)
+        for k, ids in enumerate(([0, 1, -1, 2, 0, 1, 4, 4, 2], [4, 4, -1, -1, 0, 0, 0, 7, -5], [-1] * 9, [3] * 9)):
+            a.ids.copy_(torch.tensor(ids, dtype=torch.int32))
+            lrn.calgrad_adapted()
+            a.ids.fill_(1)                                               # (the next batch's may be there already)
+            before = [t.clone() for t in (a.A, a.Bm, a.vA, a.vB)] + [t.clone() for t in (a.A_bf16, a.Bm_bf16) if t is not None]
+            A, Bm, dA, dB = (wide(t) for t in (a.A, a.Bm, a.dA, a.dB))
+            lrn.apply_adapters(0.02, momentum=0.9, weight_decay=0.1)
+            after = [a.A, a.Bm, a.vA, a.vB] + [t for t in (a.A_bf16, a.Bm_bf16) if t is not None]
+            there = sorted({i for i in ids if 0 <= i < 5})
+            absent = [i for i in range(5) if i not in there]
+            for p, q in zip(before, after):
+                assert torch.equal(p[absent], q[absent]), k
+            if there and k != 1:                                         # (an invalid id makes the loss and everything after it NaN)
+                for got, theta, g, v in ((a.A, A, dA, vA), (a.Bm, Bm, dB, vB)):
+                    want, _ = muon.matrices_step(theta[there], g[there], v[there], 0.02, 0.9, 0.1, True)
+                    assert np.linalg.norm(wide(got)[there] - want) <= 1.2 * 0.02 * E * np.sqrt(want.size) * max(1, np.sqrt(max(want.shape[1:]) / min(want.shape[1:]))) + 4 * 2.0 ** -24 * np.linalg.norm(want)
+            if k == 1:
+                for t in (a.A, a.Bm, a.vA, a.vB):
+                    t[there] = 0.01 * torch.randn_like(t[there])
+                a.refresh()
+            vA, vB = wide(a.vA), wide(a.vB)
+    finally:
+        lrn.close()
