@@ -186,6 +186,7 @@ int sgd_step(float* theta_master, void* theta_bf16_or_null, const float* grad, s
 #define MUON_NESTEROV 1                        /* the update's direction is grad + momentum * velocity, else the velocity */
 #define MUON_GATES    2                        /* muon_step: each gate's block [H][..] of W_x and U_h is a matrix of its own, else the four together are one */
 #define MUON_SOFTMAX  4                        /* muon_step: W_s is orthogonalised as well */
+#define MUON_FULL     16                       /* muon_step in mode 1: as exact as mode 0, at about twice the time (muon_matrices_step: mode 0, which takes a bf16 copy too) */
 
 /* X <- O(G) of `count` matrices [rows][cols], one behind the other.  G float; X bfloat16 in mode 1, float in mode 0; they may not overlap. */
 size_t muon_orthogonalize_scratch_bytes(int count, int rows, int cols, int mode);      /* 0 and an error text for sizes it does not take */

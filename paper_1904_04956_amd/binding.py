@@ -20,7 +20,7 @@ BLSTM_NO_LABEL = -1
 BLSTM_MAX_TOP = 256
 BLSTM_MIN_TEMPERATURE = 1e-4
 SOFTMAX_LOGPROB, SOFTMAX_TOPK, SOFTMAX_DISTILL, SOFTMAX_POLICY = range(4)
-MUON_NESTEROV, MUON_GATES, MUON_SOFTMAX = 1, 2, 4
+MUON_NESTEROV, MUON_GATES, MUON_SOFTMAX, MUON_FULL = 1, 2, 4, 16
 BLSTM_NO_ADAPTER = -1
 BLSTM_MAX_ADAPTERS = 4096
 BLSTM_MAX_ADAPTER_RANK = 128

@@ -778,6 +778,7 @@ int loss_run(blstm_ctx* ctx, const LossCall& given, const int32_t* labels, const
 }
 
 // ---- the orthogonalised update ---------------------------------------------------------------------------------------
+constexpr int MUON_STEP_FLAGS = MUON_NESTEROV | MUON_GATES | MUON_SOFTMAX | MUON_FULL;
 // The flat vector as groups of tensors of one shape at constant distances (layers beyond the first are alike).
 bool muon_model_plan(const blstm_ctx* c, int flags, MuonPlan* plan) {
     MuonGroup g[MUON_MAX_GROUPS];
@@ -803,7 +804,7 @@ bool muon_model_plan(const blstm_ctx* c, int flags, MuonPlan* plan) {
     }
     add(c->off_ws, 0, 1, 1, c->V, c->zdim, (flags & MUON_SOFTMAX) != 0);
     add(c->off_bs, 0, 1, 1, c->V, 1, false);
-    return muon_plan(g, n, c->st == DT_F32, plan);
+    return muon_plan(g, n, c->st == DT_F32 || (flags & MUON_FULL), plan);
 }
 
 int muon_matrices_plan(const char* name, int count, int rows, int cols, int mode, MuonPlan* plan) {
@@ -1583,7 +1584,7 @@ int sgd_step(float* theta, void* shadow, const float* grad, size_t n, float lr, 
 size_t muon_scratch_bytes(const blstm_ctx* ctx, int flags) {
     MuonPlan p;
     if (!ctx) { fail(BLSTM_ERR_NULL, "muon_scratch_bytes: null argument"); return 0; }
-    if (flags & ~(MUON_NESTEROV | MUON_GATES | MUON_SOFTMAX)) { fail(BLSTM_ERR_DIM, "muon_scratch_bytes: unknown flags"); return 0; }
+    if (flags & ~MUON_STEP_FLAGS) { fail(BLSTM_ERR_DIM, "muon_scratch_bytes: unknown flags"); return 0; }
     if (!muon_model_plan(ctx, flags, &p)) { fail(BLSTM_ERR_DIM, "muon_scratch_bytes: too many elements"); return 0; }
     return p.bytes;
 }
@@ -1594,7 +1595,7 @@ int muon_step(const blstm_ctx* ctx, float* theta, void* shadow, const float* gra
     MuonPlan p;
     if (!muon_model_plan(ctx, flags, &p)) return fail(BLSTM_ERR_DIM, "muon_step: too many elements");
     const MuonArgs a{theta, static_cast<unsigned short*>(shadow), grad, momentum != 0.0f ? velocity : nullptr, nullptr, 0, lr, lr_rest, momentum, weight_decay, (flags & MUON_NESTEROV) != 0};
-    const int rc = muon_check("muon_step", a, flags, MUON_NESTEROV | MUON_GATES | MUON_SOFTMAX, p, scratch, scratch_bytes);
+    const int rc = muon_check("muon_step", a, flags, MUON_STEP_FLAGS, p, scratch, scratch_bytes);
     return rc != BLSTM_OK ? rc : check_hip(launch_muon(p, a, MuonIds{}, scratch, static_cast<hipStream_t>(stream)), "muon_step");
 }
 

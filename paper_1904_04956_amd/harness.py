@@ -194,12 +194,12 @@ class Learner:
         bl.sgd_step(self.theta, self.shadow, self.grad, self.n, lr, self.momentum, self.velocity, stream)
         self.weights_changed()
 
-    def apply_muon(self, lr, lr_rest, momentum=0.95, weight_decay=0.0, nesterov=True, gates=False, softmax=False, stream=None):
+    def apply_muon(self, lr, lr_rest, momentum=0.95, weight_decay=0.0, nesterov=True, gates=False, softmax=False, full=False, stream=None):
         """W' = apply(W, g) with the matrices' updates orthogonalised (binding.muon_step): the LSTM's and the bottleneck's at lr, with `softmax` the softmax
-        layer's too; the rest at lr_rest.  `gates`: each gate's block is a matrix of its own.  The velocity is the learner's (made of zeros at first use)."""
+        layer's too; the rest at lr_rest.  `gates`: each gate's block is a matrix of its own.  `full`: mode 1 is as exact as mode 0.  The velocity is the learner's (made of zeros at first use)."""
         if momentum != 0.0 and self.velocity is None:
             self.velocity = self._zeros((self.n,), torch.float32, stream)
-        flags = (bl.MUON_NESTEROV if nesterov else 0) | (bl.MUON_GATES if gates else 0) | (bl.MUON_SOFTMAX if softmax else 0)
+        flags = (bl.MUON_NESTEROV if nesterov else 0) | (bl.MUON_GATES if gates else 0) | (bl.MUON_SOFTMAX if softmax else 0) | (bl.MUON_FULL if full else 0)
         bl.muon_step(self.ctx, self.theta, self.shadow, self.grad, self.velocity, lr, lr_rest, momentum, weight_decay, flags,
                      self._kept(("muon", flags), lambda: bl.muon_scratch_bytes(self.ctx, flags), stream), None, stream)
         self.weights_changed()
