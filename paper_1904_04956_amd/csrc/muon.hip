@@ -227,6 +227,7 @@ struct NsOperand { const _Float16* p; long long ld, plane; };      // tile origi
 
 template <int TM, int TN, bool SPLIT, bool AS, bool BS, int NST>
 __device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand& A, const NsOperand& B, int slab0, int slab1, int trips, uint4* smem) {
+    static_assert(NST == 1 || (NST == 2 && !(SPLIT && TM == 2)), "one buffer, or two");
     constexpr bool ONE = NST == 1;
     constexpr int BM = 64 * TM, BN = 64 * TN, PL = SPLIT ? 2 : 1, PA = BM * 8, PB = BN * 8, STAGE = PL * (PA + PB);   // (in 16-byte words)
     constexpr int NIA = 2 * TM, NIB = 2 * TN, CPA = BM / 8, CPB = BN / 8;
@@ -290,8 +291,7 @@ __device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand
             for (int j = 0; j < TN; ++j)
                 acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, x[i]), __builtin_bit_cast(f16x8_t, y[j]), acc[i][j], 0, 0, 0);
     };
-#pragma unroll
-    for (int i = 0; i < (ONE ? 1 : NST - 1); ++i) if (slab0 + i < slab1) issue(slab0 + i);
+    if (slab0 < slab1) issue(slab0);
     if constexpr (ONE) {
         uint4 fa[4][PL][TM], fb[4][PL][TN];
         for (int it = slab0; it < slab1; ++it) {
@@ -315,19 +315,14 @@ __device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand
         }
     } else {
         for (int it = slab0; it < slab0 + trips; ++it) {       // (every wavefront of the workgroup goes through as many barriers)
-            // (this wavefront's loads of the slab have landed when at most the younger slabs' are outstanding; its reads of the buffer that is filled next have come)
-            constexpr int LOADS = PL * (NIA + NIB);
-            const int younger = min(NST - 2, slab1 - 1 - it);
-            if (NST >= 4 && younger == 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(2 * LOADS) : "memory");
-            else if (NST >= 3 && younger == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LOADS) : "memory");
-            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            if (it + NST - 1 < slab1) issue(it + NST - 1);
+            // (the slab has landed, this wavefront's reads of the buffer that is filled next have come)
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if (it + 1 < slab1) issue(it + 1);
             const uint4* sa = smem + ((it - slab0) % NST) * STAGE;
             const uint4* sb = sa + PL * PA;
             if (it >= slab1) continue;
             // (the next fragments are on their way while these are multiplied)
-            constexpr int NF = SPLIT && TM == 2 ? 1 : 2;
-            uint4 af[NF][PL][TM], bf[NF][PL][TN];
+            uint4 af[2][PL][TM], bf[2][PL][TN];
             auto read = [&](int q, uint4 (&x)[PL][TM], uint4 (&y)[PL][TN]) __attribute__((always_inline)) {
 #pragma unroll
                 for (int pl = 0; pl < PL; ++pl) {
@@ -337,13 +332,12 @@ __device__ __forceinline__ void ns_tile(f32x16_t (&acc)[TM][TN], const NsOperand
                     for (int i = 0; i < TN; ++i) y[pl][i] = frag_b(sb + pl * PB, i, q);
                 }
             };
-            if (NF == 2) read(0, af[0], bf[0]);
+            read(0, af[0], bf[0]);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                if (NF == 2) { if (q < 3) read(q + 1, af[(q + 1) % NF], bf[(q + 1) % NF]); }
-                else read(q, af[0], bf[0]);
-                if constexpr (SPLIT) { mma(af[q % NF][1], bf[q % NF][0]); mma(af[q % NF][0], bf[q % NF][1]); }
-                mma(af[q % NF][0], bf[q % NF][0]);
+                if (q < 3) read(q + 1, af[(q + 1) & 1], bf[(q + 1) & 1]);
+                if constexpr (SPLIT) { mma(af[q & 1][1], bf[q & 1][0]); mma(af[q & 1][0], bf[q & 1][1]); }
+                mma(af[q & 1][0], bf[q & 1][0]);
             }
         }
     }
@@ -443,7 +437,7 @@ __device__ __forceinline__ void upper(int t, int* row, int* col) {
 
 // SPLIT: the operands' second halves are multiplied too; LO: S and B have second halves; LOW: X's second part is held in eight bits
 template <int TM, int TN, bool SPLIT, bool LO, bool LOW, int PH, int NST, int SETS>
-__global__ __launch_bounds__(256 * SETS, SPLIT && TM == 2 && NST > 1 ? 1 : 2) void ns_product_kernel(MuonPlan p, MuonArgs a, _Float16* ws, float* diag, float* part, int from, const int* here) {
+__global__ __launch_bounds__(256 * SETS, 2) void ns_product_kernel(MuonPlan p, MuonArgs a, _Float16* ws, float* diag, float* part, int from, const int* here) {
     extern __shared__ uint4 smem[];
     constexpr int BM = 64 * TM, BN = 64 * TN;
     // ids go round-robin to the eight XCDs: of each group (they differ in the length of their contractions) each XCD takes an eighth, neighbouring tiles
@@ -666,7 +660,7 @@ __global__ __launch_bounds__(256) void ns_gram_sum_kernel(MuonPlan p, _Float16* 
 constexpr int SMALL_THREADS = 1024, SMALL_SIDE = 64, SMALL_LDS = 160 * 1024 - 256;
 constexpr int small_parts(int mb) { return mb == 1 ? 16 : mb == 2 ? 4 : 1; }   // stretches of the columns that a tile of S is summed over
 struct SmallLds { int ldn, lds, x, s, b, red, d, bytes; };      // row lengths in halves; byte offsets
-__host__ __device__ inline SmallLds small_lds(int m, int n, int mb) {
+__host__ __device__ inline SmallLds small_lds(int n, int mb) {
     SmallLds l{};
     const int mp = 16 * mb, kp = (mp + 31) / 32 * 32;
     l.ldn = (n + 31) / 32 * 32 + 8;
@@ -677,7 +671,6 @@ __host__ __device__ inline SmallLds small_lds(int m, int n, int mb) {
     l.red = l.b + 2 * mp * l.lds * 2;
     l.d = l.red + (small_parts(mb) > 1 ? small_parts(mb) : 0) * mp * mp * 4;
     l.bytes = l.d + mp * 4;
-    (void)m;
     return l;
 }
 // (three chains, so that none waits for another's end)
@@ -725,7 +718,7 @@ __global__ __launch_bounds__(SMALL_THREADS) void muon_small_kernel(MuonPlan p, M
     const long long at = tensor_at(g, local);
     const int size = g.rows * g.cols, n = max(g.rows, g.cols);
     const bool tall = g.tall != 0;
-    const SmallLds l = small_lds(min(g.rows, g.cols), n, MB);
+    const SmallLds l = small_lds(n, MB);
     char* base = reinterpret_cast<char*>(smem);
     _Float16* X = reinterpret_cast<_Float16*>(base + l.x);
     _Float16* S = reinterpret_cast<_Float16*>(base + l.s);
@@ -960,7 +953,7 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
         for (int i = 0; i < n; ++i) if (g[i].ortho) {
             const int longer = std::max(g[i].rows, g[i].cols);
             fits = fits && longer <= 4096;
-            if (fits) p.lds = std::max(p.lds, small_lds(std::min(g[i].rows, g[i].cols), longer, p.small).bytes);
+            if (fits) p.lds = std::max(p.lds, small_lds(longer, p.small).bytes);
         }
         if (fits && p.lds <= SMALL_LDS) {
             long long groups = 0;
