@@ -196,7 +196,8 @@ class Learner:
 
     def apply_muon(self, lr, lr_rest, momentum=0.95, weight_decay=0.0, nesterov=True, gates=False, softmax=False, full=False, stream=None):
         """W' = apply(W, g) with the matrices' updates orthogonalised (binding.muon_step): the LSTM's and the bottleneck's at lr, with `softmax` the softmax
-        layer's too; the rest at lr_rest.  `gates`: each gate's block is a matrix of its own.  `full`: mode 1 is as exact as mode 0.  The velocity is the learner's (made of zeros at first use)."""
+        layer's too; the rest at lr_rest.  `gates`: each gate's block is a matrix of its own.  `full`: mode 1 is as exact as mode 0.  The velocity is the learner's (made of zeros at first
+        use, which a graph cannot hold)."""
         if momentum != 0.0 and self.velocity is None:
             self.velocity = self._zeros((self.n,), torch.float32, stream)
         flags = (bl.MUON_NESTEROV if nesterov else 0) | (bl.MUON_GATES if gates else 0) | (bl.MUON_SOFTMAX if softmax else 0) | (bl.MUON_FULL if full else 0)
@@ -214,6 +215,8 @@ class Learner:
         if stream is not None and not isinstance(stream, torch.cuda.Stream):
             stream = torch.cuda.ExternalStream(int(stream), device=self.device)
         with torch.cuda.stream(stream):
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("zeros made while a graph is captured would be made again by every replay: call once before")
             return torch.zeros(shape, dtype=dtype, device=self.device)
 
     # ---- low-rank adapters beside the bottleneck's projection ------------------------------
