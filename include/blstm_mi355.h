@@ -181,7 +181,7 @@ int sgd_step(float* theta_master, void* theta_bf16_or_null, const float* grad, s
      X <- a X + b S X + c S^2 X,  S = X X^T (R <= C; else X <- a X + b X S + c X S^2,  S = X^T X),  (a, b, c) = (3.4445, -4.7750, 2.0315)
    G's singular vectors with singular values of 0.7 to 1.2, the smallest ones less (they grow 485-fold at most).  O of a zero matrix is zero; an infinity or a NaN anywhere
    in G makes all of O(G) NaN.  Mode 1 multiplies in halves (11 bits, of values scaled for them; sums in float): O(G) is off by about 4e-4 of its norm.
-   Mode 0, and mode 1 where the call's matrices have less than 512 elements a row, multiplies pairs of halves: about 1e-6.  The same inputs give the same bits.
+   Mode 0, mode 1 where the call's matrices together have less than 512 elements a row, and mode 1 with MUON_FULL multiply pairs of halves: about 1e-6.  The same inputs give the same bits.
    `scratch` as for the softmax calls: caller-owned, 16-byte aligned, holds nothing between calls; calls that overlap need one each. */
 #define MUON_NESTEROV 1                        /* the update's direction is grad + momentum * velocity, else the velocity */
 #define MUON_GATES    2                        /* muon_step: each gate's block [H][..] of W_x and U_h is a matrix of its own, else the four together are one */

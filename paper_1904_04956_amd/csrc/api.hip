@@ -781,6 +781,7 @@ int loss_run(blstm_ctx* ctx, const LossCall& given, const int32_t* labels, const
 constexpr int MUON_STEP_FLAGS = MUON_NESTEROV | MUON_GATES | MUON_SOFTMAX | MUON_FULL;
 // The flat vector as groups of tensors of one shape at constant distances (layers beyond the first are alike).
 bool muon_model_plan(const blstm_ctx* c, int flags, MuonPlan* plan) {
+    static_assert(MUON_MAX_GROUPS >= 3 + 3 + 2 + 2, "two kinds of layers, the bottleneck, the softmax layer");
     MuonGroup g[MUON_MAX_GROUPS];
     int n = 0;
     auto add = [&](size_t at, long long outer, int parts, int count, int rows, int cols, bool ortho) {

@@ -3,12 +3,12 @@
 // which keeps the singular vectors and takes every singular value s to a s + b s^3 + c s^5: in five steps what is not tiny lands in 0.7 .. 1.2.
 //
 // Numbers.  Everything that a product reads is a half (the matrix cores' rate is that of bf16, with three more bits) times 2^8, which keeps the
-// entries of a normalised matrix, 1/sqrt(m n), and what their rounding leaves over away from the subnormals; none exceeds 2^8 for X and S and
-// about 2^12 for B.  Products accumulate in float.  X itself is kept as the sum of two halves (22 bits): a rounding of X adds noise in all
+// entries of a normalised matrix, 1/sqrt(m n), and what their rounding leaves over away from the subnormals; with singular values below 1.21 none
+// exceeds 1.21 * 2^8 for X, 1.47 * 2^8 for S and 3.45 * 2^8 for B.  Products accumulate in float.  X itself is kept as the sum of two halves (22 bits): a rounding of X adds noise in all
 // directions alike, and where a few directions hold most of |d| (gradients do) that noise is as large as the others; the step's other
 // roundings pass through B X, which is small where the singular value is.  So mode 1 multiplies the first halves only and adds a X from both: off by
 // about 4e-4 of X (of which X's rounding in S 3.3e-4, S's 1.7e-4, B's 1.6e-4, X's in B X 1.4e-4: 301 x 602; small launches, with time to spare, multiply both halves
-// for S: 2.8e-4).  Mode 0 multiplies both halves everywhere (three products): off by about 1e-6.
+// for S: 2.8e-4).  Mode 0, mode 1 where matrices have few columns (muon_plan) and where the caller asks for it multiply both halves everywhere (three products): off by about 1e-6.
 // The diagonals of S and B, which near the end are most of them, stay out of the halves and the products, in float: with D the diagonal and R the rest,
 // S^2 = D^2 + D R + R D + R^2, and B X = D X + R X (rounded with the rest they alone put X off by 2e-3).
 // The Frobenius norm is summed in double (squares of floats leave float's range) in a fixed order.
@@ -16,9 +16,9 @@
 // S and B are symmetric: tiles on and above the diagonal are computed, and stored twice.
 //
 // All matrices of a call share each launch: the flat pass over v and g, the cast to halves, then S, B and the new X five times; the last X goes straight into
-// the weights.  What bounds them, four layers of 512 cells (43 M weights, 301 GFLOP), 765 us in all: the flat pass 82 us, 560 MB at 6.8 TB/s; the cast 53, 340 MB; S 38 each, 900 TFLOP/s
-// of what it would be without the symmetry; B 24, whose 311 tiles are 1.2 a CU; the new X 62, 35 GFLOP and 220 MB; the last 108, 465 MB.  Six of 1024: 351, 301, 298 (1460 TFLOP/s
-// likewise), 151, 512 (870 TFLOP/s, 1 GB), 720 (2 GB).
+// the weights.  What bounds them, four layers of 512 cells (22.3 M weights in matrices and 8.2 M others, 301 GFLOP), 740 to 790 us in all, bytes as counted behind the L2: the flat pass 82 us, 449 MB
+// at 5.5 TB/s; the cast 53, 255 MB; S 38 each, 35 GFLOP without the symmetry at 920 TFLOP/s, 101 MB; B 24, whose 311 tiles are 1.2 a CU, 49 MB; the new X 62, 35 GFLOP and 209 MB; the
+// last 107, 407 MB.  Six of 1024: 351 (1.83 GB), 301 (1.52), 298 (448 GFLOP likewise at 1500 TFLOP/s, 0.82 GB), 151 (0.4), 512 (870 TFLOP/s, 1.75 GB), 720 (2.98 GB).
 // Built and dropped: three and four buffers of a slab where a CU has one workgroup (S 41 -> 56 us: what a lone workgroup waits for are its own LDS reads and products in turn,
 // 768 and 512 clocks a slab, not the loads); S in two, three or four parts of the contraction, summed by another launch (58, 66 and 77 us for 45); two steps'
 // B multiplied together, so that X is written three times instead of five (error 4e-4 -> 6e-4).
@@ -973,7 +973,7 @@ bool muon_plan(const MuonGroup* g, int n, bool exact, MuonPlan* out) {
         }
     }
     // The entries of a step are lr / sqrt(cols) in size, so that O's error reaches the weights with 1 / sqrt(cols): matrices of few columns (512 a row over all of
-    // them) get products of both planes in mode 1 too.  Two layers of 301 cells, gates apart, all launches: 240 -> 295 us; it would be 911 -> 2100 for four of 512.
+    // them) get products of both planes in mode 1 too.  Two layers of 301 cells, gates apart, all launches: 240 -> 295 us; four of 512 would go from 790 to 1380.
     long long elements = 0, rows = 0;
     for (int i = 0; i < n; ++i) if (g[i].ortho) { rows += (long long)g[i].count * g[i].rows; elements += (long long)g[i].count * g[i].rows * g[i].cols; }
     exact = exact || elements < 512 * rows;

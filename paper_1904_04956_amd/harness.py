@@ -153,7 +153,7 @@ class Learner:
         return weights
 
     def log_probs(self, labels=None, weights=None, stream=None):
-        """log p[label] [T][B] of the batch (of `labels` if given, else its own): a forward pass, then the softmax layer."""
+        """log p[label] [T][B] of the batch (of `labels` if given, else its own): a forward pass (without adapters), then the softmax layer."""
         labels = self.labels if labels is None else self._frames("labels", labels, torch.int32)
         th = self._forward_on(weights, stream)
         out = self._empty(self.labels.shape, torch.float32, stream)
@@ -161,7 +161,7 @@ class Learner:
         return out
 
     def top_logits(self, K, weights=None, stream=None):
-        """Values and classes [T][B][K] of the batch's K largest logits: what a student's calgrad_distill takes."""
+        """Values and classes [T][B][K] of the batch's K largest logits (without adapters): what a student's calgrad_distill takes."""
         th = self._forward_on(weights, stream)
         shape = (*self.labels.shape, K)
         values, classes = self._empty(shape, torch.float32, stream), self._empty(shape, torch.int32, stream)
@@ -222,7 +222,8 @@ class Learner:
     # ---- low-rank adapters beside the bottleneck's projection ------------------------------
     def attach_adapters(self, count, rank, scale=1.0):
         """`count` adapters of `rank` beside the bottleneck (binding.adapter_forward, W = W_p), each sequence's by adapters.ids [B] (BLSTM_NO_ADAPTER at first).
-        Their factors are adapters.A [count][rank][2H] and .Bm [count][P][rank], float, zero at first; after writing them call adapters.refresh()."""
+        Their factors are adapters.A [count][rank][2H] and .Bm [count][P][rank], float, zero at first (write one of the two: both gradients are zero where both factors are); after writing
+        them call adapters.refresh().  They take part in forward_adapted and calgrad_adapted; all other passes of the learner are the model's without them."""
         if self.dims["P"] == 0:
             raise ValueError("adapters stand beside the bottleneck's projection, and this model has none")
         if self.adapters is not None:
@@ -243,7 +244,8 @@ class Learner:
         bl.adapter_forward(a.cfg, a.W, a.b, a.A_fwd, a.Bm_fwd, a.ids, a.h, self.z, a.t, a.scratch(bl.ADAPTER_FORWARD, self, stream), None, stream)
 
     def calgrad_adapted(self, shared=True, stream=None):
-        """calgrad() with the adapters: their gradients in adapters.dA and .dB and, with `shared`, the model's in grad (without: the softmax layer's alone)."""
+        """calgrad() with the adapters: their gradients in adapters.dA and .dB and, with `shared`, the model's in grad (without: the softmax layer's alone; elsewhere grad is
+        what it was, and not for an apply())."""
         a = self._attached()
         a.take_ids(stream)
         self.forward_adapted(stream)
