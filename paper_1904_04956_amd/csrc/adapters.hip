@@ -294,7 +294,7 @@ __global__ __launch_bounds__(64 * RWAVES) void adapt_rows_kernel(ProjectArgs a, 
 // rank 16: 93 tiles of 64 rows, two column blocks each) 12 are the launch, the search for the tile, t's way through LDS and the stores, 0.7 each of the sixteen slabs
 // (a third of it LDS reads).  Three and five buffers: 23.5 and 29.6 us (workgroups without a tile wait for a CU then).  128 rows where the adapters have them: dx of 2048
 // sequences 95 -> 83 us, of which stores 18, the low-rank part 14, slabs two to four 23.  Two workgroups a CU are asked for where they fit: the accumulators then
-// share the ordinary registers (256 sequences 23.8 -> 23.2 us).
+// share the ordinary registers (256 sequences 23.8 -> 23.2 us, dx of 2048 83 -> 79).
 constexpr int PN = 128;
 template <typename T, int ROWS, int RB, bool DIRECT>
 __global__ __launch_bounds__(256, DIRECT && RB <= 2 ? 2 : 1) void adapt_tile_kernel(ProjectArgs a, bool low_vector) {
