@@ -5,7 +5,8 @@
 // further rows of W in one pass over x, and s t B_a^T is one more product on the tile's accumulators before they leave.  dx is the same kernel on
 // dy with the transposed weights.  (W's gradient is an ordinary product: gemm.hip.)
 // Numbers: sums in float; t and q enter their products as two bf16 numbers (2^-17) for y and dx, which leave as bf16, and as three for
-// the gradients, which leave as float.  Parts are no parts where something is infinite (inf - inf, 0 inf): there the sums are made element by element in float.
+// the gradients, which leave as float.  Parts are no parts where something is infinite (inf - inf, 0 inf): what they make of it is always NaN,
+// and an element that is NaN is made once more from its definition in float.
 #include "gemm_tile.hpp"
 #include "adapters.hpp"
 #include <algorithm>
@@ -116,7 +117,6 @@ __device__ __forceinline__ void mma16(f32x4_t& acc, const uint4& a, const uint4&
 }
 // elements [k, k + 16 bytes) of a row of n, zero beyond it.  VECTOR: rows are whole aligned 16-byte words; else words start anywhere and a row's last may be short.
 typedef uint32_t u32x4e_t __attribute__((ext_vector_type(4), aligned(2)));
-typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
 template <typename T, bool VECTOR>
 __device__ __forceinline__ uint4 load_chunk(const T* row, int k, int n) {
     constexpr int V = Vec<T>::N;
@@ -191,6 +191,25 @@ __device__ __forceinline__ long long row_at(const AdaptShape& s, const int* orde
 template <typename T>
 __device__ __forceinline__ uint4 low_chunk(const T* row, int c, int rank, bool vector) {
     return vector ? load_chunk<T, true>(row, c, rank) : load_chunk<T, false>(row, c, rank);
+}
+
+// The NaNs among a lane's V x E values, as bits (none, hardly ever: asked in pairs first).
+template <int V, int E, typename F>
+__device__ __forceinline__ unsigned long long nans(F&& value) {
+    static_assert(V * E <= 64 && E % 2 == 0, "bits");
+    bool any = false;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int e = 0; e < E; e += 2) any |= __builtin_isunordered(value(v, e), value(v, e + 1));
+    unsigned long long found = 0;
+    if (__any(any)) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int e = 0; e < E; ++e) found |= (unsigned long long)(value(v, e) != value(v, e)) << (E * v + e);
+    }
+    return found;
 }
 
 // Few rows (a frame, a handful of rows an adapter): 16 rows x 32 columns.  What such a tile costs is the latency of its loads, so nothing is staged: eight wavefronts share the
@@ -294,7 +313,7 @@ __global__ __launch_bounds__(64 * RWAVES) void adapt_rows_kernel(ProjectArgs a, 
 // rank 16: 93 tiles of 64 rows, two column blocks each) 12 are the launch, the search for the tile, t's way through LDS and the stores, 0.7 each of the sixteen slabs
 // (a third of it LDS reads).  Three and five buffers: 23.5 and 29.6 us (workgroups without a tile wait for a CU then).  128 rows where the adapters have them: dx of 2048
 // sequences 95 -> 83 us, of which stores 18, the low-rank part 14, slabs two to four 23.  Two workgroups a CU are asked for where they fit: the accumulators then
-// share the ordinary registers (256 sequences 23.8 -> 23.2 us, dx of 2048 83 -> 79).
+// share the ordinary registers (256 sequences 23.8 -> 22.2 us, dx of 2048 83 -> 79).
 constexpr int PN = 128;
 template <typename T, int ROWS, int RB, bool DIRECT>
 __global__ __launch_bounds__(256, DIRECT && RB <= 2 ? 2 : 1) void adapt_tile_kernel(ProjectArgs a, bool low_vector) {
@@ -302,13 +321,12 @@ __global__ __launch_bounds__(256, DIRECT && RB <= 2 ? 2 : 1) void adapt_tile_ker
     constexpr int NX = ROWS / 32, NW = 4, NA = (RP * 8 + 255) / 256;
     constexpr int STAGE = (ROWS + PN + RP) * CHUNKS;
     extern __shared__ uint4 smem[];
-    __shared__ int rows[ROWS], any_odd;
+    __shared__ int rows[ROWS];
     const AdaptShape& s = a.s;
     int4 what;
     const int* order;
     int col0;
     if (!find_tile(a, a.y ? (s.N + PN - 1) / PN : 1, reinterpret_cast<int*>(smem), &what, &order, &col0)) return;
-    if (threadIdx.x == 0) any_odd = 0;
     col0 *= PN;
     const int key = what.x, nrows = what.z;
     const bool low = key < s.count;
@@ -440,20 +458,6 @@ __global__ __launch_bounds__(256, DIRECT && RB <= 2 ? 2 : 1) void adapt_tile_ker
     float* ts = reinterpret_cast<float*>(smem);
     constexpr int TLD = RP + 4;
     const float bad = key > s.count ? __builtin_nanf("") : 0.0f;
-    constexpr float END = 3.38e38f;                          // (below what rounds to an infinity in bf16)
-    bool odd = false;                                        // (ES 2: something infinite, in t or B_a)
-    if constexpr (ES == 2) {
-        u16x2_t most = 0;
-#pragma unroll
-        for (int q = 0; q < BQ; ++q)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const uint32_t w[4] = {fb[q][j].x, fb[q][j].y, fb[q][j].z, fb[q][j].w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2_t, w[e] & 0x7FFF7FFFu));
-            }
-        odd = most[0] >= 0x7F80 || most[1] >= 0x7F80;
-    }
 #pragma unroll
     for (int i = 0; i < TR; ++i)
 #pragma unroll
@@ -461,10 +465,9 @@ __global__ __launch_bounds__(256, DIRECT && RB <= 2 ? 2 : 1) void adapt_tile_ker
         {
             f32x4_t v;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { v[e] = 16 * j + 4 * fg + e < s.rank ? tac[i][j][e] + bad : 0.0f; odd |= fabsf(s.scale * v[e]) >= END; }
+            for (int e = 0; e < 4; ++e) v[e] = 16 * j + 4 * fg + e < s.rank ? tac[i][j][e] + bad : 0.0f;
             *reinterpret_cast<f32x4_t*>(ts + (64 * i + 16 * wave + fr) * TLD + 16 * j + 4 * fg) = v;
         }
-    if (ES == 2 && __any(odd)) any_odd = 1;
     __syncthreads();
     if (a.t && col0 == 0) {
         for (int i = tid; i < nrows * s.rank; i += 256) { const int r = i / s.rank, c = i - r * s.rank; a.t[(long long)rows[r] * s.rank + c] = ts[r * TLD + c]; }
@@ -472,25 +475,6 @@ __global__ __launch_bounds__(256, DIRECT && RB <= 2 ? 2 : 1) void adapt_tile_ker
     if (!a.y) return;
     T* y = static_cast<T*>(a.y);
     if (low) {
-        if constexpr (ES == 2) {
-            if (__builtin_expect(any_odd != 0, 0)) {
-                // (column n of row r of this lane: acc as below)
-#pragma unroll
-                for (int i = 0; i < MR; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int r = 16 * i + fr, n = col0 + 32 * wave + 16 * j + 4 * fg + e;
-                            if (r >= nrows || n >= s.N) continue;
-                            float sum = 0.0f;
-#pragma unroll 1
-                            for (int c = 0; c < s.rank; ++c) sum += ts[r * TLD + c] * ld_f(Bm + (long long)n * s.rank + c);
-                            st_f(y + (long long)rows[r] * s.N + n, acc[i][j][e] + (a.b ? ld_f(static_cast<const T*>(a.b) + n) : 0.0f) + s.scale * sum);
-                        }
-                return;
-            }
-        }
         // s t B_a^T: t in two bf16 parts, or as it is
 #pragma unroll
         for (int q = 0; q < BQ; ++q) {
@@ -546,6 +530,21 @@ __global__ __launch_bounds__(256, DIRECT && RB <= 2 ? 2 : 1) void adapt_tile_ker
 #pragma unroll
                 for (int e = 0; e < 4; ++e) if (n + e < s.N) st_f(to + e, v[e]);
             }
+        }
+    }
+    if (ES == 2 && low) {
+        unsigned long long odd = nans<2 * MR, 4>([&](int v, int e) { return acc[v >> 1][v & 1][e]; });
+#pragma unroll 1
+        for (; odd; odd &= odd - 1) {
+            const int b = __ffsll(odd) - 1, r = 16 * (b >> 3) + fr, n = col0 + 32 * wave + 16 * (b >> 2 & 1) + 4 * fg + (b & 3);
+            if (r >= nrows || n >= s.N) continue;
+            float part = 0.0f, sum = a.b ? ld_f(static_cast<const T*>(a.b) + n) : 0.0f;
+#pragma unroll 1
+            for (int c = 0; c < s.rank; ++c) part += ts[r * TLD + c] * ld_f(Bm + (long long)n * s.rank + c);
+            if (part != part) continue;
+#pragma unroll 4
+            for (int k = 0; k < s.K; ++k) sum += ld_f(x + (long long)rows[r] * s.K + k) * ld_f(W + (long long)n * s.K + k);
+            st_f(y + (long long)rows[r] * s.N + n, sum + s.scale * part);
         }
     }
 }
@@ -650,28 +649,20 @@ __device__ __forceinline__ void grad_out(const AdaptGradArgs& a, int chunk, int 
     }
 }
 
-// Whether a sum of the workgroup's is NaN, and if so the chunk's 128 columns once more, element by element in float.  What the second and third bf16 parts of q (or t) make of
-// infinities is always NaN, which the definition seldom has.  (The parts cleared in every product where they meet infinities: 196 us for 2048 sequences became 206; asked afterwards: 196.  A batch all of NaN: 2 ms.)
-template <int RB>
-__device__ __forceinline__ bool any_nan(const f32x16_t (&acc)[RB], int* flag) {
-    bool odd = false;
-#pragma unroll
-    for (int i = 0; i < RB; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) odd |= __builtin_isunordered(acc[i][e], acc[i][e + 1]);
-    if (__any(odd)) *flag = 1;
-    __syncthreads();
-    return *flag != 0;
-}
-template <typename T, typename F>
-__device__ __forceinline__ void grad_plain(const AdaptGradArgs& a, int chunk, int key, bool only, bool second, int c0, int nrows, F&& row_of) {
+// The sums of a lane that are NaN, once more in float.  (The parts cleared in every product where they meet infinities: 196 us for 2048 sequences became 206; looked for afterwards: 196.
+// A batch all of NaN: 2 ms.)
+template <typename T, int RB, typename F>
+__device__ __forceinline__ void grad_again(const AdaptGradArgs& a, int chunk, int key, bool only, bool second, int col, const f32x16_t (&acc)[RB], int nrows, F&& row_of) {
+    unsigned long long odd = nans<RB, 16>([&](int v, int e) { return acc[v][e]; });
     const AdaptShape& s = a.s;
-    const int width = second ? s.N : s.K, cols = min(128, width - c0);
+    const int width = second ? s.N : s.K;
+    if (col >= width) return;
     const T* R = static_cast<const T*>(second ? a.dy : a.x);
     const float* L = second ? a.t : a.q;
 #pragma unroll 1
-    for (int i = threadIdx.x; i < s.rank * cols; i += 256) {
-        const int r = i / cols, col = c0 + i % cols;
+    for (; odd; odd &= odd - 1) {
+        const int b = __ffsll(odd) - 1, r = 8 * (b >> 2) + 4 * ((threadIdx.x & 63) >> 5) + (b & 3);
+        if (r >= s.rank) continue;
         float sum = 0.0f;
 #pragma unroll 4
         for (int k = 0; k < nrows; ++k) { const long long row = row_of(k); sum += L[row * s.rank + r] * ld_f(R + row * width + col); }
@@ -689,7 +680,6 @@ __global__ __launch_bounds__(256) void adapt_grad_kernel(AdaptGradArgs a) {
     constexpr int RLD = 128 * ES + 16, LLD = RP * ES + 16;                 // bytes of a row
     constexpr int NR = 64 * 128 / V / 256;
     extern __shared__ uint4 smem[];
-    __shared__ int odd;
     char* rs = reinterpret_cast<char*>(smem);
     char* ls = rs + 64 * RLD;
     const AdaptShape& s = a.s;
@@ -704,7 +694,6 @@ __global__ __launch_bounds__(256) void adapt_grad_kernel(AdaptGradArgs a) {
     const T* R = static_cast<const T*>(second ? a.dy : a.x);
     const float* L = second ? a.t : a.q;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    if (tid == 0) odd = 0;
     auto row_of = [&](int r) { const int i = what.y + r, j = i / s.T; return (long long)(i - j * s.T) * s.B + order[j]; };
     f32x16_t acc[RB];
 #pragma unroll
@@ -763,8 +752,9 @@ __global__ __launch_bounds__(256) void adapt_grad_kernel(AdaptGradArgs a) {
         }
     }
     const bool only = chunks_of[1] - chunks_of[0] == 1;
-    if (ES == 2 && any_nan(acc, &odd)) grad_plain<T>(a, chunk, what.x, only, second, c0, what.z, row_of);
-    else grad_out<RB>(a, chunk, what.x, only, second, c0 + 32 * wave + (lane & 31), acc);
+    const int col = c0 + 32 * wave + (lane & 31);
+    grad_out<RB>(a, chunk, what.x, only, second, col, acc);
+    if constexpr (ES == 2) grad_again<T, RB>(a, chunk, what.x, only, second, col, acc, what.z, row_of);
 }
 
 // The same in bf16 where rows are whole 16-byte words: two slabs of 64 rows of x (or dy) and of q (or t) come straight to LDS in turn, one while the other is
@@ -776,7 +766,7 @@ __global__ __launch_bounds__(256) void adapt_grad_direct_kernel(AdaptGradArgs a)
     constexpr int RP = 32 * RB, LLD = RP * 2 + 16, RS = 64 * 256, LS = 64 * RP * 4, STAGE = RS + LS, LCH = RP / 4;     // bytes; 16-byte words of a row of q
     constexpr int NR = 4, NL = LS / 1024 / 4;                // load instructions of a wavefront and slab
     extern __shared__ uint4 smem[];
-    __shared__ int rows[ADAPT_MAX_CHUNK], odd;
+    __shared__ int rows[ADAPT_MAX_CHUNK];
     char* base = reinterpret_cast<char*>(smem);
     char* planes = base + 2 * STAGE;
     const AdaptShape& s = a.s;
@@ -792,7 +782,6 @@ __global__ __launch_bounds__(256) void adapt_grad_direct_kernel(AdaptGradArgs a)
     const int width = second ? s.N : s.K, c0 = (second ? ct - nk : ct) * 128, nrows = what.z, slabs = (nrows + 63) / 64;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     for (int r = tid; r < nrows; r += 256) rows[r] = (int)row_at(s, order, what.y + r);
-    if (tid == 0) odd = 0;
     __syncthreads();
     const char* R = static_cast<const char*>(second ? a.dy : a.x) + c0 * 2;
     const char* L = reinterpret_cast<const char*>(second ? a.t : a.q);
@@ -856,8 +845,9 @@ __global__ __launch_bounds__(256) void adapt_grad_direct_kernel(AdaptGradArgs a)
         }
     }
     const bool only = chunks_of[1] - chunks_of[0] == 1;
-    if (any_nan(acc, &odd)) grad_plain<bf16_t>(a, chunk, what.x, only, second, c0, nrows, [&](int k) { return (long long)rows[k]; });
-    else grad_out<RB>(a, chunk, what.x, only, second, c0 + 32 * wave + (lane & 31), acc);
+    const int col = c0 + 32 * wave + (lane & 31);
+    grad_out<RB>(a, chunk, what.x, only, second, col, acc);
+    grad_again<bf16_t, RB>(a, chunk, what.x, only, second, col, acc, nrows, [&](int k) { return (long long)rows[k]; });
 }
 
 // An adapter's chunks in order, where it has none or several; dB leaves transposed (through LDS).  `groups` workgroups an adapter.

@@ -68,3 +68,31 @@ def test_infinities_in_the_gradients(where, shape, mode):
     assert all(np.isinf(want[k]).any() == (k in touched) and not np.isnan(want[k]).any() for k in want)
     for k in want:
         same_kind(got[k], want[k], k)
+
+
+@pytest.mark.parametrize("mode", [0, 1])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_neighbours_of_an_infinity_keep_their_bits(shape, mode):
+    # sequences of the same adapter, in the same tiles, and the same adapter's other columns
+    T, B, K, N, rank, count = shape
+    s = tensors(13, *shape, mode, np.zeros(B))
+    y, t = run_forward(s, (*shape, mode))
+    clean = run_backward(s, (*shape, mode), t, 1.5)
+    others = [b for b in range(B) if b != 1]
+    before = {k: s[k].clone() for k in ("x", "dy")}
+    s["x"][T // 2, 1, K // 2] = float("inf")
+    y2, t2 = run_forward(s, (*shape, mode))
+    assert torch.equal(y[:, others], y2[:, others]) and torch.equal(t[:, others], t2[:, others]) and not torch.isfinite(y2[T // 2, 1]).any()
+    frames = [i for i in range(T) if i != T // 2]
+    assert torch.equal(y[frames, 1], y2[frames, 1])
+    got = run_backward(s, (*shape, mode), t, 1.5)                # x's infinity is in one column of dA and of dW
+    columns = [k for k in range(K) if k != K // 2]
+    assert torch.equal(got["dx"], clean["dx"]) and torch.equal(got["dB"], clean["dB"])
+    assert torch.equal(got["dA"][0][:, columns], clean["dA"][0][:, columns]) and not torch.isfinite(got["dA"][0][:, K // 2]).any()
+    s["x"].copy_(before["x"])
+    infinite = t.clone()
+    infinite[T // 2, 1, rank - 1] = float("inf")                 # t's in one column of dB
+    got = run_backward(s, (*shape, mode), infinite, 1.5)
+    columns = list(range(rank - 1))
+    assert torch.equal(got["dA"], clean["dA"]) and torch.equal(got["dx"], clean["dx"])
+    assert torch.equal(got["dB"][0][:, columns], clean["dB"][0][:, columns]) and not torch.isfinite(got["dB"][0][:, rank - 1]).any()
