@@ -180,7 +180,7 @@ int sgd_step(float* theta_master, void* theta_bf16_or_null, const float* grad, s
    Another apply(W, g).  Of a matrix G [R][C], |G| its Frobenius norm, O(G) is what five Newton-Schulz steps make of X = G / |G|:
      X <- a X + b S X + c S^2 X,  S = X X^T (R <= C; else X <- a X + b X S + c X S^2,  S = X^T X),  (a, b, c) = (3.4445, -4.7750, 2.0315)
    G's singular vectors with singular values of 0.7 to 1.2, the smallest ones less (they grow 485-fold at most).  O of a zero matrix is zero; an infinity or a NaN anywhere
-   in G makes all of O(G) NaN.  Mode 1 multiplies in halves (11 bits, of values scaled for them; sums in float): O(G) is off by about 4e-4 of its norm.
+   in G makes all of O(G) NaN.  Mode 1 multiplies in halves (11 bits, of values scaled for them; sums in float): O(G) is off by 3e-4 to 6e-4 of its norm.
    Mode 0, mode 1 where the call's matrices together have less than 512 elements a row, and mode 1 with MUON_FULL multiply pairs of halves: about 1e-6.  The same inputs give the same bits.
    `scratch` as for the softmax calls: caller-owned, 16-byte aligned, holds nothing between calls; calls that overlap need one each. */
 #define MUON_NESTEROV 1                        /* the update's direction is grad + momentum * velocity, else the velocity */

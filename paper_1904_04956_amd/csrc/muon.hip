@@ -7,7 +7,7 @@
 // exceeds 1.21 * 2^8 for X, 1.47 * 2^8 for S and 3.45 * 2^8 for B.  Products accumulate in float.  X itself is kept as the sum of two halves (22 bits): a rounding of X adds noise in all
 // directions alike, and where a few directions hold most of |d| (gradients do) that noise is as large as the others; the step's other
 // roundings pass through B X, which is small where the singular value is.  So mode 1 multiplies the first halves only and adds a X from both: off by
-// about 4e-4 of X (of which X's rounding in S 3.3e-4, S's 1.7e-4, B's 1.6e-4, X's in B X 1.4e-4: 301 x 602; small launches, with time to spare, multiply both halves
+// 3e-4 to 5.4e-4 of X (4e-4, of which X's rounding in S 3.3e-4, S's 1.7e-4, B's 1.6e-4, X's in B X 1.4e-4: 301 x 602; small launches, with time to spare, multiply both halves
 // for S: 2.8e-4).  Mode 0, mode 1 where matrices have few columns (muon_plan) and where the caller asks for it multiply both halves everywhere (three products): off by about 1e-6.
 // The diagonals of S and B, which near the end are most of them, stay out of the halves and the products, in float: with D the diagonal and R the rest,
 // S^2 = D^2 + D R + R D + R^2, and B X = D X + R X (rounded with the rest they alone put X off by 2e-3).

@@ -2,9 +2,9 @@
 weights themselves, and models of several groups.
 
 Bound (2-norm of the difference over 2-norm of the result, a matrix at a time).  A half's rounding has a root mean square of 2^-10 / sqrt(12) of a binade's beginning, whose values have
-one of sqrt(1.5 / ln 2): r = 2.0e-4 of what is rounded.  Where the singular values end up (0.7 to 1.2, the eigenvalues of S 0.5 to 1.4) d(bS + cS^2)/dS is between -2.7 and 1.1, -0.7 on
+one of sqrt(1.5 / ln 2): r = 1.9e-4 of what is rounded.  Where the singular values end up (0.7 to 1.2, the eigenvalues of S 0.5 to 1.4) d(bS + cS^2)/dS is between -2.7 and 1.1, -0.7 on
 average, so that in a step X's rounding in S arrives as 1.0 r, S's own off the diagonal (a fourth of it) as 0.2 r, B's off the diagonal and X's in the product with it as 0.3 r each:
-1.1 to 1.2 r, and the steps after hand an error of X on at about its relative size.  Five steps, independent: 2.7 r; a third more for how unevenly singular values lie: 3.5 r = 6.9e-4.
+1.1 to 1.2 r, and the steps after hand an error of X on at about its relative size.  Five steps, independent: 2.7 r; a third more for how unevenly singular values lie: 3.5 r = 6.7e-4.
 (X without its second part, or with the diagonals rounded to halves, is off by 8.7e-4 to 1.3e-3: the same arithmetic in numpy.)"""
 import numpy as np
 import pytest
